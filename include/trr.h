@@ -71,6 +71,11 @@
  *   Everything else (b = 2 and 4, scales, positions, masks) is stored as above.
  *   Page allocation: entries are taken in array order; an entry of class c whose
  *   (layer, seq) has ntok % P == 0 opens page next_page[c]++ .
+ *   Shared pages: after trr_fork several sequences of a layer may name the same full page;
+ *   a partly filled page always belongs to one sequence.  After trr_evict a sequence's
+ *   ntok counts the tokens still stored.  Entries of page_table, page_first and page_last
+ *   past a class's ceil(ntok / P) are -1 in the rows that trr_fork, trr_evict and
+ *   trr_free_seqs write.
  *   Per-head modes (head_modes = 1): the last 16 bytes of KV head h's slice hold a
  *   little-endian uint64 (then 8 zero bytes): bit `slot` set <=> the token in that slot
  *   stores KV head h.  A page starts with every bit clear when its slot 0 is written.
@@ -305,6 +310,83 @@ TRR_API trr_status trr_decode_attn_routed(trr_cache* cache, int32_t layer, int32
                                           const void* q_bf16, const float* mode_logits,
                                           const int32_t* windows, int32_t window_scalar,
                                           float softmax_scale, void* out_bf16, void* stream);
+
+/* ---------------------------------------------------------------- shared prompts --
+ *
+ * Sequences that share a past (samples of one prompt, beams), sequences that stream past
+ * their window, and the pages behind them.  The paper stores every token once per
+ * sequence (Sec. 3.8); these calls keep its cache and its modes, and let sequences name
+ * the same pages.
+ *
+ * Calls that take a workspace use `workspace_bytes` bytes of device memory at `workspace`
+ * (256-byte aligned), at least trr_workspace_bytes(cache), only while they run: one
+ * workspace serves every call on the cache, and caches whose calls do not overlap may use
+ * one between them.  A smaller or misaligned one returns TRR_ERR_OUT_OF_MEMORY and
+ * enqueues nothing. */
+TRR_API trr_status trr_workspace_bytes(const trr_cache* cache, uint64_t* bytes);
+
+/* Fork: for each entry i and every layer, sequence dst_seqs[i] becomes a copy of sequence
+ * src_seqs[i] as it was after its position lengths[i] - 1: the same stored tokens, the
+ * same last position (or lengths[i] - 1 where that is less).  What dst_seqs[i] held is
+ * forgotten.  Pages whose P slots are all below lengths[i] are shared; the one page per
+ * layer and class that is not is copied to a page of its own, so that either sequence
+ * can be appended to.  dst_seqs[i] == src_seqs[i] cuts the sequence back to lengths[i]
+ * positions.  Page ids of the copies: next_page upwards, in order of (layer, entry).
+ *   src_seqs, dst_seqs, lengths: int32, device; 0 <= n <= min(max_seqs, 4096).
+ *   Device-detected errors: a sequence id out of range, a negative length, a dst_seqs
+ *   value that appears twice or is another entry's source (INVALID_ARG), a pool running
+ *   out (OUT_OF_PAGES).  Any of these makes the whole call a no-op. */
+TRR_API trr_status trr_fork(trr_cache* cache, int32_t n, const int32_t* src_seqs, const int32_t* dst_seqs,
+                            const int32_t* lengths, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Evict: for each entry i and every layer, forget the full pages of sequence seq_ids[i]
+ * whose tokens all lie in [sinks, keep_from[i]): what attention with `sinks` first tokens
+ * and a window that starts at keep_from[i] does not read.  Their tokens count as not
+ * stored from then on, in every mode; pages that hold a token to keep stay whole.
+ *   seq_ids, keep_from: int32, device; 0 <= n <= min(max_seqs, 4096); sinks >= 0.
+ *   Device-detected errors: a sequence id out of range or named before in the call
+ *   (INVALID_ARG); that entry does nothing, the others take effect. */
+TRR_API trr_status trr_evict(trr_cache* cache, int32_t n, const int32_t* seq_ids, const int32_t* keep_from,
+                             int32_t sinks, void* stream);
+
+/* Free: forget sequences seq_ids[0..n) in every layer (as new, any position may come
+ * next).  Pages go back to the pools with the next trr_compact.
+ *   seq_ids: int32, device; 0 <= n <= min(max_seqs, 4096).  An id out of range records
+ *   INVALID_ARG; the others take effect. */
+TRR_API trr_status trr_free_seqs(trr_cache* cache, int32_t n, const int32_t* seq_ids, void* stream);
+
+/* Compact: give the pages that no sequence names back to the pools.  In each class, with
+ * m pages in use, the pages with ids m and above move, in ascending order, to the unused
+ * ids below m in ascending order; page tables follow, and next_page becomes m.  Stored
+ * tokens, and so every attention result, stay as they were. */
+TRR_API trr_status trr_compact(trr_cache* cache, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Decode attention with sinks: trr_decode_attn, but a local query also sees the first
+ * `sinks` positions: local: the stored tokens j <= t with j >= t-w+1 or j < sinks.
+ *   sinks >= 0 (0: trr_decode_attn's results).  seq_ids, q_positions, modes, windows:
+ *   device, read after the previous kernel of the stream has finished; q, out 16-byte
+ *   aligned.  Otherwise the arguments, results and error contract of trr_decode_attn; a
+ *   cache with head_modes returns TRR_ERR_UNSUPPORTED. */
+TRR_API trr_status trr_decode_attn_sinks(trr_cache* cache, int32_t layer, int32_t n, const int32_t* seq_ids,
+                                         const int32_t* q_positions, const void* q_bf16, const uint8_t* modes,
+                                         const int32_t* windows, int32_t window_scalar, int32_t sinks,
+                                         float softmax_scale, void* out_bf16, void* workspace,
+                                         uint64_t workspace_bytes, void* stream);
+
+/* Decode attention of queries whose sequences share pages: trr_decode_attn_sinks with the
+ * queries given in groups, queries group_offsets[i] .. group_offsets[i+1]-1 forming group
+ * i (queries outside every group stand alone).  The results do not depend on the groups.
+ * In each class, the leading pages that all full queries of a group name and see whole
+ * are read once for the group; so put sequences forked from one prompt in one group, and
+ * a sequence that shares nothing in none.
+ *   group_offsets: int32[num_groups + 1], device, ascending from >= 0 to <= n;
+ *   0 <= num_groups <= n.  Offsets that are not make every row zero and record
+ *   INVALID_ARG.  Otherwise as trr_decode_attn_sinks. */
+TRR_API trr_status trr_decode_attn_shared(trr_cache* cache, int32_t layer, int32_t n, const int32_t* seq_ids,
+                                          const int32_t* q_positions, const void* q_bf16, const uint8_t* modes,
+                                          const int32_t* windows, int32_t window_scalar, int32_t sinks,
+                                          int32_t num_groups, const int32_t* group_offsets, float softmax_scale,
+                                          void* out_bf16, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Free library-owned memory (waits for the device first).  A caller pool is not
  * freed.  NULL is accepted. */

@@ -310,4 +310,5 @@ void cache_note_call(trr_cache* c, int layer) {
   c->recent[1] = c->recent[0];
   c->recent[0] = layer;
 }
+void cache_note_every_layer(trr_cache* c) { cache_note_call(c, -2); }
 }  // namespace trr

@@ -20,6 +20,9 @@ enum Ctrl : int {
   kNextPage = 4,      // [4] pages handed out per class
   kAppendOk = 10,     // append: 1 when the plan kernel committed the call
   kAppendDone = 11,   // one-kernel append: CTAs finished (the last one commits)
+  kForkDone = 12,     // fork: CTAs of the plan finished (the last one hands out pages)
+  kForkError = 13,    // fork: an entry is invalid
+  kForkOk = 14,       // fork: 1 when the plan may be carried out
   kCtrlInts = 64
 };
 
@@ -168,7 +171,19 @@ void cache_set_launches(trr_cache* c, int n);
 // kernel before that one has finished).  cache_note_call records a call.
 bool cache_layer_settled(const trr_cache* c, int layer);
 void cache_note_call(trr_cache* c, int layer);
+void cache_note_every_layer(trr_cache* c);  // a call that changes the state of every layer
 uint64_t cache_wait_ns(const trr_cache* c);
+
+// Workspace that callers bring (trr_workspace_bytes): the most that any call needs.
+int64_t pages_workspace_bytes(const Layout& l);  // defined in trr_pages.cu
+int64_t group_workspace_bytes(const Layout& l);  // defined in trr_group.cu
+inline trr_status check_workspace(const trr_cache* c, const void* workspace, uint64_t bytes) {
+  uint64_t need = 0;
+  const trr_status st = trr_workspace_bytes(c, &need);
+  if (st != TRR_OK) return st;
+  if (!workspace || bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255)) return TRR_ERR_OUT_OF_MEMORY;
+  return TRR_OK;
+}
 
 // One-time kernel attribute setup (defined in trr_attn.cu).
 cudaError_t attn_configure();

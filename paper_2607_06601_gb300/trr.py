@@ -42,7 +42,8 @@ class trr_cache_config(ctypes.Structure):
 EXPORTS = ("trr_cache_required_bytes", "trr_create_cache", "trr_kv_append", "trr_decode_attn",
            "trr_decode_step", "trr_decode_attn_static", "trr_route_decisions", "trr_kv_append_routed",
            "trr_decode_attn_routed", "trr_destroy", "trr_get_status", "trr_set_wait_limit", "trr_reset",
-           "trr_get_region",
+           "trr_get_region", "trr_workspace_bytes", "trr_fork", "trr_evict", "trr_free_seqs", "trr_compact",
+           "trr_decode_attn_sinks", "trr_decode_attn_shared",
            "trr_last_launch_count")
 
 _lib = None
@@ -79,6 +80,13 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     L.trr_reset.argtypes = [P, P]
     L.trr_get_region.argtypes = [P, I32, ctypes.POINTER(P), ctypes.POINTER(U64)]
     L.trr_last_launch_count.argtypes = [P]
+    L.trr_workspace_bytes.argtypes = [P, ctypes.POINTER(U64)]
+    L.trr_fork.argtypes = [P, I32, P, P, P, P, U64, P]
+    L.trr_evict.argtypes = [P, I32, P, P, I32, P]
+    L.trr_free_seqs.argtypes = [P, I32, P, P]
+    L.trr_compact.argtypes = [P, P, U64, P]
+    L.trr_decode_attn_sinks.argtypes = [P, I32, I32, P, P, P, P, P, I32, I32, ctypes.c_float, P, P, U64, P]
+    L.trr_decode_attn_shared.argtypes = [P, I32, I32, P, P, P, P, P, I32, I32, I32, P, ctypes.c_float, P, P, U64, P]
     for name in EXPORTS:
         getattr(L, name).restype = I32
     _lib = L
@@ -229,6 +237,79 @@ def trr_decode_attn_routed(cache, layer, seq_ids, q_positions, q, mode_logits, w
         _dev(out, torch.bfloat16, "out"), _stream(stream)))
 
 
+def trr_workspace_bytes(cache) -> int:
+    out = ctypes.c_uint64()
+    _check("trr_workspace_bytes", load().trr_workspace_bytes(cache, ctypes.byref(out)))
+    return int(out.value)
+
+
+def _same_length(n, **tensors):
+    for name, t in tensors.items():
+        if t.numel() != n:
+            raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+
+
+def trr_fork(cache, src_seqs, dst_seqs, lengths, workspace, stream=None):
+    """dst_seqs[i] becomes src_seqs[i] up to position lengths[i] - 1, sharing its full pages."""
+    n = src_seqs.numel()
+    _same_length(n, dst_seqs=dst_seqs, lengths=lengths)
+    _check("trr_fork", load().trr_fork(
+        cache, n, _dev(src_seqs, torch.int32, "src_seqs"), _dev(dst_seqs, torch.int32, "dst_seqs"),
+        _dev(lengths, torch.int32, "lengths"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _stream(stream)))
+
+
+def trr_evict(cache, seq_ids, keep_from, sinks, stream=None):
+    """Forget the full pages of each sequence that lie in [sinks, keep_from[i])."""
+    n = seq_ids.numel()
+    _same_length(n, keep_from=keep_from)
+    _check("trr_evict", load().trr_evict(cache, n, _dev(seq_ids, torch.int32, "seq_ids"),
+                                         _dev(keep_from, torch.int32, "keep_from"), int(sinks), _stream(stream)))
+
+
+def trr_free_seqs(cache, seq_ids, stream=None):
+    _check("trr_free_seqs", load().trr_free_seqs(cache, seq_ids.numel(), _dev(seq_ids, torch.int32, "seq_ids"),
+                                                 _stream(stream)))
+
+
+def trr_compact(cache, workspace, stream=None):
+    _check("trr_compact", load().trr_compact(cache, _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                             _stream(stream)))
+
+
+def _check_queries(n, q_positions, modes, windows):
+    _same_length(n, q_positions=q_positions, modes=modes)
+    if windows is not None:
+        _same_length(n, windows=windows)
+
+
+def trr_decode_attn_sinks(cache, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
+                          softmax_scale, out, workspace, stream=None):
+    """trr_decode_attn whose local queries also see the first `sinks` positions."""
+    n = seq_ids.numel()
+    _check_queries(n, q_positions, modes, windows)
+    _check("trr_decode_attn_sinks", load().trr_decode_attn_sinks(
+        cache, layer, n, _dev(seq_ids, torch.int32, "seq_ids"), _dev(q_positions, torch.int32, "q_positions"),
+        _dev(q, torch.bfloat16, "q"), _dev(modes, torch.uint8, "modes"), _opt(windows, torch.int32, "windows"),
+        int(window_scalar), int(sinks), float(softmax_scale), _dev(out, torch.bfloat16, "out"),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+
+
+def trr_decode_attn_shared(cache, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
+                           group_offsets, softmax_scale, out, workspace, stream=None):
+    """trr_decode_attn_sinks with the pages that a group's full queries share read once."""
+    n = seq_ids.numel()
+    _check_queries(n, q_positions, modes, windows)
+    if group_offsets.numel() < 1:
+        raise ValueError("group_offsets must have an element more than there are groups")
+    _check("trr_decode_attn_shared", load().trr_decode_attn_shared(
+        cache, layer, n, _dev(seq_ids, torch.int32, "seq_ids"), _dev(q_positions, torch.int32, "q_positions"),
+        _dev(q, torch.bfloat16, "q"), _dev(modes, torch.uint8, "modes"), _opt(windows, torch.int32, "windows"),
+        int(window_scalar), int(sinks), group_offsets.numel() - 1,
+        _dev(group_offsets, torch.int32, "group_offsets"), float(softmax_scale), _dev(out, torch.bfloat16, "out"),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+
+
 def trr_destroy(cache):
     _check("trr_destroy", load().trr_destroy(cache))
 
@@ -268,6 +349,7 @@ class Cache:
         self.handle = trr_create_cache(self.cfg, self.pool)
         self.L, self.S, self.Hq, self.Hkv = num_layers, max_seqs, num_q_heads, num_kv_heads
         self.d, self.G, self.P, self.max_context = head_dim, group_size, page_size, max_context
+        self._workspace = None
 
     def _check_modes(self, modes, n):
         want = n * (self.Hq if self.head_modes else 1)
@@ -306,6 +388,55 @@ class Cache:
             out = torch.empty((seq_ids.numel(), self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
         trr_decode_attn_routed(self.handle, layer, seq_ids, q_positions, q, mode_logits, windows,
                                window_scalar, softmax_scale, out, stream)
+        return out
+
+    def workspace(self) -> torch.Tensor:
+        """Device memory of the calls below, allocated once for the cache: call it before capturing
+        them in a CUDA graph."""
+        if self._workspace is None:
+            self._workspace = torch.empty(trr_workspace_bytes(self.handle), dtype=torch.uint8, device=self.pool.device)
+        return self._workspace
+
+    def fork(self, src_seqs, dst_seqs, lengths, stream=None):
+        """Sequence dst_seqs[i] becomes a copy of src_seqs[i] up to position lengths[i] - 1, in every
+        layer, sharing its full pages."""
+        trr_fork(self.handle, src_seqs, dst_seqs, lengths, self.workspace(), stream)
+
+    def evict(self, seq_ids, keep_from, sinks=0, stream=None):
+        """Forget the full pages of each sequence that lie in [sinks, keep_from[i]), in every layer."""
+        trr_evict(self.handle, seq_ids, keep_from, sinks, stream)
+
+    def free(self, seq_ids, stream=None):
+        """Forget the sequences, in every layer; compact() gives their pages back."""
+        trr_free_seqs(self.handle, seq_ids, stream)
+
+    def compact(self, stream=None):
+        """Give the pages that no sequence names back to the pools."""
+        trr_compact(self.handle, self.workspace(), stream)
+
+    def _rows(self, seq_ids, q, out):
+        """The output of an attention call: q and out are [n][Hq][d]."""
+        n = seq_ids.numel() * self.Hq * self.d
+        if q.numel() != n or (out is not None and out.numel() != n):
+            raise ValueError(f"q and out must have {n} elements ([n][Hq][d])")
+        return out if out is not None else torch.empty((seq_ids.numel(), self.Hq, self.d), dtype=torch.bfloat16,
+                                                       device=q.device)
+
+    def decode_attn_sinks(self, layer, seq_ids, q_positions, q, modes, sinks, windows=None, window_scalar=0,
+                          softmax_scale=0.0, out=None, stream=None):
+        """decode_attn whose local queries also see the first `sinks` positions."""
+        out = self._rows(seq_ids, q, out)
+        trr_decode_attn_sinks(self.handle, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
+                              softmax_scale, out, self.workspace(), stream)
+        return out
+
+    def decode_attn_shared(self, layer, seq_ids, q_positions, q, modes, group_offsets, windows=None, window_scalar=0,
+                           sinks=0, softmax_scale=0.0, out=None, stream=None):
+        """decode_attn_sinks of queries in groups (group_offsets, int32, one more than there are groups):
+        the pages that a group's full queries share are read once for the group."""
+        out = self._rows(seq_ids, q, out)
+        trr_decode_attn_shared(self.handle, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
+                               group_offsets, softmax_scale, out, self.workspace(), stream)
         return out
 
     def status(self, stream=None) -> int:

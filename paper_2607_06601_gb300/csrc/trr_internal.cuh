@@ -23,6 +23,7 @@ enum Ctrl : int {
   kForkDone = 12,     // fork: CTAs of the plan finished (the last one hands out pages)
   kForkError = 13,    // fork: an entry is invalid
   kForkOk = 14,       // fork: 1 when the plan may be carried out
+  kGroupDone = 15,    // attention over groups: CTAs of the plan finished (the last one makes the jobs)
   kCtrlInts = 64
 };
 
@@ -176,7 +177,7 @@ uint64_t cache_wait_ns(const trr_cache* c);
 
 // Workspace that callers bring (trr_workspace_bytes): the most that any call needs.
 int64_t pages_workspace_bytes(const Layout& l);  // defined in trr_pages.cu
-int64_t group_workspace_bytes(const Layout& l);  // defined in trr_group.cu
+int64_t group_workspace_bytes(const Layout& l, int ctas);  // defined in trr_group.cu
 inline trr_status check_workspace(const trr_cache* c, const void* workspace, uint64_t bytes) {
   uint64_t need = 0;
   const trr_status st = trr_workspace_bytes(c, &need);
@@ -187,6 +188,7 @@ inline trr_status check_workspace(const trr_cache* c, const void* workspace, uin
 
 // One-time kernel attribute setup (defined in trr_attn.cu).
 cudaError_t attn_configure();
+cudaError_t configure_group();  // defined in trr_group.cu
 
 // ------------------------------------------------------------------ PTX helpers --
 

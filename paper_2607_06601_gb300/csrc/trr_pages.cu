@@ -477,7 +477,7 @@ using namespace trr;
 extern "C" trr_status trr_workspace_bytes(const trr_cache* cache, uint64_t* bytes) {
   if (!cache || !bytes) return TRR_ERR_INVALID_ARG;
   const Layout& l = cache_layout(cache);
-  *bytes = static_cast<uint64_t>(std::max(pages_workspace_bytes(l), group_workspace_bytes(l)));
+  *bytes = static_cast<uint64_t>(std::max(pages_workspace_bytes(l), group_workspace_bytes(l, cache_num_sms(cache))));
   return TRR_OK;
 }
 

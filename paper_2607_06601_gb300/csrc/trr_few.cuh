@@ -1,0 +1,631 @@
+// trr_few.cuh - attention of a segment with few rows (the query heads of one KV head for one
+// query): warps that work alone, on codes as they are stored.
+//
+// Every warp takes one equal run of blocks (up to 32 tokens of a page, for one KV head) of the
+// call's private segments, laid end to end.  It brings the blocks into its own ring of shared
+// memory with bulk copies issued several blocks ahead, and multiplies with warp-wide products
+// of 16 x 8 x 16 (binary32 sums):
+//   scores   S^T = K Q^T: 16 tokens x 8 columns.  A column is a (query head, group) pair: the
+//            query row restricted to one quantiser group, so that sum_g s_g (q c)_g + z_g sum(q)_g
+//            needs only the codes.  Rows are 16 tokens; a quad of lanes holds a token's row, a
+//            lane a quarter of it in a run, so codes come in whole words.
+//   output   O^T += V^T W: 16 dimensions x 8 columns, W = p s.  A lane holds an eighth of the
+//            dimensions of two pairs of tokens; byte permutes pair the tokens' codes.
+// A code is used as the binary16 number `offset + code` made by setting its bits under an
+// exponent (16 + c, 4 + c, 1024 + c for 4, 2, 8 bits: no conversion, no subtraction); the
+// offset's part of every sum is taken off at the end in binary32.
+//
+// The softmax reference m follows the largest score plus log2 of the token's V scale, so that
+// W = p s stays below 2^9 in binary16 whatever the size of the values; 16-bit pages keep p as a
+// sum of two bf16 numbers.
+//
+// What bounds it: instructions, about 0.13 per byte for each warp; bytes are read once.
+#pragma once
+
+#include "trr_group.cuh"
+
+namespace trr {
+
+constexpr int kFewWarps = 8;      // warps of a CTA
+constexpr int kFewCtas = 2;       // CTAs of an SM
+constexpr int kFewStages = 6;     // blocks in a warp's ring
+constexpr int kFewRows = 8;       // most rows of a segment
+
+// A block in the ring.
+struct FewBlock {
+  int cls, keys, off, pos;      // pos < 0: all its tokens are in sight
+  int valid, lo, t, sinks;
+  int query, kvh, dest, state;  // state: 1 first block of a segment's piece, 2 last one
+};
+
+template <int D>
+struct FewSmem {
+  static constexpr int kQ = kFewRows * D * 2;
+  static constexpr int kBlocks = kQ + 64;                              // after Q: a factor for each row
+  static constexpr int kBars = kBlocks + kFewStages * static_cast<int>(sizeof(FewBlock));
+  static constexpr int kRing = (kBars + 8 * kFewStages + 127) / 128 * 128;
+  static constexpr int kWarp = 112 * 1024 / kFewWarps / 128 * 128;     // a warp's share
+  static constexpr int kRingBytes = kWarp - kRing;
+  static constexpr int kTotal = kWarp * kFewWarps;
+};
+static_assert(FewSmem<128>::kRingBytes >= 32 * 288 + 128, "the widest block");
+
+template <int B>
+struct Codes;
+template <>
+struct Codes<2> { static constexpr float kOffset = 4.f; };
+template <>
+struct Codes<4> { static constexpr float kOffset = 16.f; };
+template <>
+struct Codes<8> { static constexpr float kOffset = 1024.f; };
+template <>
+struct Codes<16> { static constexpr float kOffset = 0.f; };
+
+// Codes i of both 16-bit halves of x as binary16 numbers offset + code.
+__device__ __forceinline__ uint32_t codes4(uint32_t x, int i) {
+  const uint32_t y = i == 0 ? x << 6 : i == 1 ? x << 2 : i == 2 ? x >> 2 : x >> 6;
+  return (y & 0x03C003C0u) | 0x4C004C00u;
+}
+__device__ __forceinline__ uint32_t codes2(uint32_t x, int i) {
+  const uint32_t y = i < 4 ? x << (8 - 2 * i) : x >> (2 * i - 8);
+  return (y & 0x03000300u) | 0x44004400u;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// One warp's running state of a segment.
+template <int D, int NG>
+struct FewState {
+  static constexpr int kSteps = D / 16;          // products over the dimensions
+  static constexpr int kHeads = NG == 1 ? 2 : 1; // query heads of the lane's two columns
+  float acc[kSteps][4];                          // O^T: dimensions 2 i, 2 i + 1 of the lane's run x its two columns
+  float m[kHeads], l[kHeads], f[kHeads];         // reference, sum, factor from products to base-2 exponents
+  float corr[2];                                 // sum p z - offset W of the lane's columns
+  float qsum[2];
+  uint32_t q[kSteps][2];                         // the columns' query rows, in the order of q_class's codes
+  int q_class;
+};
+
+// The query rows as the second operand, in the order in which class B's codes come out of their words.
+template <int D, int NG, int B>
+__device__ __forceinline__ void few_load_q(FewState<D, NG>& s, const uint8_t* smem, int heads, int lane) {
+  constexpr int kRun = D / 4;  // a lane's dimensions
+  const int n = lane >> 2, part = lane & 3, head = n / NG;
+  const bool live = head < heads && part * NG / 4 == n % NG;  // the lane's dimensions lie in the column's group
+  const float down = live ? reinterpret_cast<const float*>(smem + FewSmem<D>::kQ)[head + 8] : 0.f;
+  const uint16_t* row = reinterpret_cast<const uint16_t*>(smem) + (live ? head : 0) * D + part * kRun;
+  auto value = [&](int e) { return live ? __uint_as_float(static_cast<uint32_t>(row[e]) << 16) * down : 0.f; };
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) {
+    int e0, e1, e2, e3;
+    if (B == 2) {
+      e0 = t / 4 * 16 + 2 * (t % 4); e1 = e0 + 8; e2 = e0 + 1; e3 = e0 + 9;
+    } else if (B == 4) {
+      e0 = t / 2 * 8 + 2 * (t % 2); e1 = e0 + 4; e2 = e0 + 1; e3 = e0 + 5;
+    } else {
+      e0 = 4 * t; e1 = e0 + 1; e2 = e0 + 2; e3 = e0 + 3;
+    }
+    if (B == 16) {
+      const __nv_bfloat162 x = __floats2bfloat162_rn(value(e0), value(e1)), y = __floats2bfloat162_rn(value(e2), value(e3));
+      s.q[t][0] = *reinterpret_cast<const uint32_t*>(&x);
+      s.q[t][1] = *reinterpret_cast<const uint32_t*>(&y);
+    } else {
+      const __half2 x = __floats2half2_rn(value(e0), value(e1)), y = __floats2half2_rn(value(e2), value(e3));
+      s.q[t][0] = as_u32(x);
+      s.q[t][1] = as_u32(y);
+      sum += __low2float(x) + __high2float(x) + __low2float(y) + __high2float(y);
+    }
+  }
+  if (B != 16) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    s.qsum[0] = __shfl_sync(0xffffffffu, sum, 8 * part);
+    s.qsum[1] = __shfl_sync(0xffffffffu, sum, 8 * part + 4);
+  }
+  s.q_class = B;
+}
+
+// One block of 16 NB tokens: K codes, V codes, K scales, V scales side by side at blk; bit k of
+// mask: token k is in sight.
+template <int D, int NG, int B, int NB>
+__device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk, uint32_t mask, bool swz, int lane) {
+  using S = FewState<D, NG>;
+  constexpr int kRow = D * B / 8, kKeys = 16 * NB;
+  constexpr float kOff = Codes<B>::kOffset;
+  const int quad = lane >> 2, part = lane & 3;
+  const bool sw = swz && B >= 8;
+  auto at = [&](int o) { return blk + (sw ? static_cast<int>(swz_off(o)) : o); };
+  const uint32_t* ksz = reinterpret_cast<const uint32_t*>(blk + 2 * kKeys * kRow);
+  const uint32_t* vsz = ksz + kKeys * NG;
+  const int g0 = NG == 1 ? 0 : (2 * part) % NG, g1 = NG == 1 ? 0 : g0 + 1;  // the groups of the lane's two columns
+
+  float x[NB][2][S::kHeads];      // scores in base-2 exponents
+  uint32_t vs[NB][2][2];          // V's (scale, zero) of the lane's tokens and columns
+  float top[S::kHeads];
+#pragma unroll
+  for (int h = 0; h < S::kHeads; ++h) top[h] = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    float c[4] = {0.f, 0.f, 0.f, 0.f};
+    const int k0 = (16 * b + quad) * kRow + part * (kRow / 4), k1 = k0 + 8 * kRow;
+    if (B == 2) {
+#pragma unroll
+      for (int w = 0; w < D / 64; ++w) {
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(blk + k0 + 4 * w), v = *reinterpret_cast<const uint32_t*>(blk + k1 + 4 * w);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          mma16816<false>(c, codes2(u, 2 * t), codes2(v, 2 * t), codes2(u, 2 * t + 1), codes2(v, 2 * t + 1), s.q[4 * w + t][0], s.q[4 * w + t][1]);
+      }
+    } else if (B == 4) {
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) {
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(blk + k0 + 4 * w), v = *reinterpret_cast<const uint32_t*>(blk + k1 + 4 * w);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          mma16816<false>(c, codes4(u, 2 * t), codes4(v, 2 * t), codes4(u, 2 * t + 1), codes4(v, 2 * t + 1), s.q[2 * w + t][0], s.q[2 * w + t][1]);
+      }
+    } else if (B == 8) {
+#pragma unroll
+      for (int w = 0; w < D / 64; ++w) {
+        const uint4 u4 = *reinterpret_cast<const uint4*>(at(k0 + 16 * w)), v4 = *reinterpret_cast<const uint4*>(at(k1 + 16 * w));
+        const uint32_t u[4] = {u4.x, u4.y, u4.z, u4.w}, v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          mma16816<false>(c, __byte_perm(u[t], 0x64646464u, 0x4140), __byte_perm(v[t], 0x64646464u, 0x4140), __byte_perm(u[t], 0x64646464u, 0x4342),
+                          __byte_perm(v[t], 0x64646464u, 0x4342), s.q[4 * w + t][0], s.q[4 * w + t][1]);
+      }
+    } else {
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) {
+        const uint4 u = *reinterpret_cast<const uint4*>(at(k0 + 16 * w)), v = *reinterpret_cast<const uint4*>(at(k1 + 16 * w));
+        mma16816<true>(c, u.x, v.x, u.y, v.y, s.q[2 * w][0], s.q[2 * w][1]);
+        mma16816<true>(c, u.z, v.z, u.w, v.w, s.q[2 * w + 1][0], s.q[2 * w + 1][1]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {  // tokens 16 b + quad and + 8
+      const int key = 16 * b + 8 * r + quad;
+      const bool seen = mask >> key & 1;
+      float y[S::kHeads], grow = 0.f;
+      if (B == 16) {
+        if (NG == 1) { y[0] = c[2 * r]; y[S::kHeads - 1] = c[2 * r + 1]; }
+        else y[0] = c[2 * r] + c[2 * r + 1];
+      } else {
+        const __half2 k0s = as_half2(ksz[key * NG + g0]), k1s = as_half2(ksz[key * NG + g1]);
+        const float y0 = __low2float(k0s) * (c[2 * r] - kOff * s.qsum[0]) + __high2float(k0s) * s.qsum[0];
+        const float y1 = __low2float(k1s) * (c[2 * r + 1] - kOff * s.qsum[1]) + __high2float(k1s) * s.qsum[1];
+        if (NG == 1) { y[0] = y0; y[S::kHeads - 1] = y1; }
+        else y[0] = y0 + y1;
+        vs[b][r][0] = vsz[key * NG + g0];
+        vs[b][r][1] = vsz[key * NG + g1];
+        uint32_t e = max(vs[b][r][0] & 0x7C00u, vs[b][r][1] & 0x7C00u);  // the larger scale's exponent
+        if (NG == 4) e = max(e, __shfl_xor_sync(0xffffffffu, e, 1));
+        grow = static_cast<float>(static_cast<int>(e >> 10) - 15);
+      }
+      if (NG == 4) y[0] += __shfl_xor_sync(0xffffffffu, y[0], 1);
+#pragma unroll
+      for (int h = 0; h < S::kHeads; ++h) {
+        x[b][r][h] = seen ? y[h] * s.f[h] : -INFINITY;
+        if (seen) top[h] = fmaxf(top[h], x[b][r][h] + grow);
+      }
+    }
+  }
+  bool far = top[0] > s.m[0] + 8.f;
+  if (S::kHeads == 2) far |= top[S::kHeads - 1] > s.m[S::kHeads - 1] + 8.f;
+  if (__any_sync(0xffffffffu, far)) {  // a new reference, the same for all lanes of a column
+#pragma unroll
+    for (int h = 0; h < S::kHeads; ++h) {
+      float t = top[h];
+      for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+      const float next = fmaxf(s.m[h], t), by = s.m[h] == -INFINITY ? 0.f : exp2_approx(s.m[h] - next);
+      s.m[h] = next;
+      s.l[h] *= by;
+#pragma unroll
+      for (int col = 0; col < 2; ++col)
+        if (S::kHeads == 1 || col == h) {
+          s.corr[col] *= by;
+#pragma unroll
+          for (int i = 0; i < S::kSteps; ++i) s.acc[i][col] *= by, s.acc[i][2 + col] *= by;
+        }
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    uint32_t w[2][2];  // weights of token rows quad, quad + 8: binary16, or bf16 high and low parts
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const bool seen = mask >> (16 * b + 8 * r + quad) & 1;
+      float p[S::kHeads];
+#pragma unroll
+      for (int h = 0; h < S::kHeads; ++h) {
+        p[h] = seen ? exp2_approx(x[b][r][h] - s.m[h]) : 0.f;
+        s.l[h] += p[h];
+      }
+      const float p0 = p[0], p1 = p[S::kHeads - 1];
+      if (B == 16) {
+        const __nv_bfloat162 hi = __floats2bfloat162_rn(p0, p1);
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(p0 - __low2float(hi), p1 - __high2float(hi));
+        w[r][0] = *reinterpret_cast<const uint32_t*>(&hi);
+        w[r][1] = *reinterpret_cast<const uint32_t*>(&lo);
+      } else {
+        const __half2 v0 = as_half2(vs[b][r][0]), v1 = as_half2(vs[b][r][1]);
+        __half2 wv = __floats2half2_rn(p0 * __low2float(v0), p1 * __low2float(v1));
+        if (!seen) wv = as_half2(0u);  // the scale of a slot that holds nothing may be anything
+        w[r][0] = as_u32(wv);
+        if (seen) {
+          s.corr[0] += p0 * __high2float(v0) - kOff * __low2float(wv);
+          s.corr[1] += p1 * __high2float(v1) - kOff * __high2float(wv);
+        }
+      }
+    }
+    const uint32_t b0 = transpose8(w[0][0]), b1 = transpose8(w[1][0]);
+    uint32_t l0 = 0, l1 = 0;
+    if (B == 16) l0 = transpose8(w[0][1]), l1 = transpose8(w[1][1]);
+    // tokens 2 part, 2 part + 1 (and 8 further on): an eighth of the dimensions, from quad * D / 8
+    const int kp = 16 * b + 2 * part;
+    const int v0 = kKeys * kRow + kp * kRow + quad * (kRow / 8);
+    if (B == 2) {
+      uint32_t lo, hi;  // pairs of tokens: 8 codes of each of two
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint8_t* p = blk + v0 + 2 * i;
+        lo = *reinterpret_cast<const uint16_t*>(p) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p + kRow)) << 16;
+        hi = *reinterpret_cast<const uint16_t*>(p + 8 * kRow) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p + 9 * kRow)) << 16;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          mma16816<false>(s.acc[4 * i + t], codes2(lo, 2 * t), codes2(lo, 2 * t + 1), codes2(hi, 2 * t), codes2(hi, 2 * t + 1), b0, b1);
+      }
+    } else if (B == 4) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint8_t* p = blk + v0 + 4 * i;
+        const uint32_t w0 = *reinterpret_cast<const uint32_t*>(p), w1 = *reinterpret_cast<const uint32_t*>(p + kRow);
+        const uint32_t w8 = *reinterpret_cast<const uint32_t*>(p + 8 * kRow), w9 = *reinterpret_cast<const uint32_t*>(p + 9 * kRow);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t lo = __byte_perm(w0, w1, u ? 0x7632 : 0x5410), hi = __byte_perm(w8, w9, u ? 0x7632 : 0x5410);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            mma16816<false>(s.acc[4 * i + 2 * u + t], codes4(lo, 2 * t), codes4(lo, 2 * t + 1), codes4(hi, 2 * t), codes4(hi, 2 * t + 1), b0, b1);
+        }
+      }
+    } else if (B == 8) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint2 w0 = *reinterpret_cast<const uint2*>(at(v0 + 8 * i)), w1 = *reinterpret_cast<const uint2*>(at(v0 + kRow + 8 * i));
+        const uint2 w8 = *reinterpret_cast<const uint2*>(at(v0 + 8 * kRow + 8 * i)), w9 = *reinterpret_cast<const uint2*>(at(v0 + 9 * kRow + 8 * i));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {  // dimensions 2 u, 2 u + 1
+          const uint32_t sel = u & 1 ? 0x7362 : 0x5140;
+          const uint32_t lo = __byte_perm(u < 2 ? w0.x : w0.y, u < 2 ? w1.x : w1.y, sel), hi = __byte_perm(u < 2 ? w8.x : w8.y, u < 2 ? w9.x : w9.y, sel);
+          mma16816<false>(s.acc[4 * i + u], __byte_perm(lo, 0x64646464u, 0x4140), __byte_perm(lo, 0x64646464u, 0x4342),
+                          __byte_perm(hi, 0x64646464u, 0x4140), __byte_perm(hi, 0x64646464u, 0x4342), b0, b1);
+        }
+      }
+    } else {
+      // rows out of sight become zero: their weight of 0 times infinity would not be
+      const uint32_t ma = (mask >> kp & 1 ? 0x0000FFFFu : 0u) | (mask >> (kp + 1) & 1 ? 0xFFFF0000u : 0u);
+      const uint32_t mb = (mask >> (kp + 8) & 1 ? 0x0000FFFFu : 0u) | (mask >> (kp + 9) & 1 ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint4 q0 = *reinterpret_cast<const uint4*>(at(v0 + 16 * i)), q1 = *reinterpret_cast<const uint4*>(at(v0 + kRow + 16 * i));
+        const uint4 q8 = *reinterpret_cast<const uint4*>(at(v0 + 8 * kRow + 16 * i)), q9 = *reinterpret_cast<const uint4*>(at(v0 + 9 * kRow + 16 * i));
+        const uint32_t a0[4] = {q0.x, q0.y, q0.z, q0.w}, a1[4] = {q1.x, q1.y, q1.z, q1.w}, a8[4] = {q8.x, q8.y, q8.z, q8.w},
+                       a9[4] = {q9.x, q9.y, q9.z, q9.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t e0 = __byte_perm(a0[u], a1[u], 0x5410) & ma, e1 = __byte_perm(a0[u], a1[u], 0x7632) & ma;
+          const uint32_t e2 = __byte_perm(a8[u], a9[u], 0x5410) & mb, e3 = __byte_perm(a8[u], a9[u], 0x7632) & mb;
+          mma16816<true>(s.acc[4 * i + u], e0, e1, e2, e3, b0, b1);
+          mma16816<true>(s.acc[4 * i + u], e0, e1, e2, e3, l0, l1);
+        }
+      }
+    }
+  }
+}
+
+template <int D, int NG, int B>
+__device__ __forceinline__ void few_class(FewState<D, NG>& s, const uint8_t* smem, const uint8_t* blk, int keys, uint32_t mask, bool swz,
+                                          int heads, int lane) {
+  if (s.q_class != B) few_load_q<D, NG, B>(s, smem, heads, lane);
+  if (B == 16 || keys == 16) few_block<D, NG, B, 1>(s, blk, mask, swz, lane);
+  else few_block<D, NG, B, B == 16 ? 1 : 2>(s, blk, mask, swz, lane);
+}
+
+// A segment's piece begins: its query rows, each with the power of two that brings its largest
+// element to [1, 2), and an empty state.
+template <int D, int NG>
+__device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g, uint8_t* smem, const FewBlock& b, int heads, int lane) {
+  const uint4* src = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(b.query) * g.a.Hq + b.kvh * heads) * D);
+  float* factor = reinterpret_cast<float*>(smem + FewSmem<D>::kQ);
+  __syncwarp();
+  constexpr int kLanes = D / 8;  // lanes of a row
+  for (int i = lane; i < (heads * kLanes + 31) / 32 * 32; i += 32) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (i < heads * kLanes) u = src[i];
+    uint32_t top = 0;
+    for (const uint32_t w : {u.x, u.y, u.z, u.w}) top = max(top, max(w & 0x7FFFu, (w >> 16) & 0x7FFFu));
+    for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
+    e = max(-100, min(120, e));
+    if (i < heads * kLanes) {
+      reinterpret_cast<uint4*>(smem)[i] = u;
+      if (i % kLanes == 0) {
+        factor[i / kLanes] = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
+        factor[i / kLanes + 8] = __int_as_float((127 - e) << 23);
+      }
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s.acc[i][k] = 0.f;
+#pragma unroll
+  for (int h = 0; h < FewState<D, NG>::kHeads; ++h) {
+    const int head = NG == 1 ? 2 * (lane & 3) + h : 2 * (lane & 3) / NG;
+    s.m[h] = -INFINITY;
+    s.l[h] = 0.f;
+    s.f[h] = head < heads ? factor[head] : 1.f;
+  }
+  s.corr[0] = s.corr[1] = 0.f;
+  s.q_class = 0;
+}
+
+// It ends: the row, or its part.
+template <int D, int NG>
+__device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, const FewBlock& b, int heads, int lane) {
+  using S = FewState<D, NG>;
+  constexpr int kRun = D / 8;
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) {
+#pragma unroll
+    for (int h = 0; h < S::kHeads; ++h) s.l[h] += __shfl_xor_sync(0xffffffffu, s.l[h], o);
+    s.corr[0] += __shfl_xor_sync(0xffffffffu, s.corr[0], o);
+    s.corr[1] += __shfl_xor_sync(0xffffffffu, s.corr[1], o);
+  }
+  const int quad = lane >> 2, part = lane & 3, group = quad * NG / 8;  // the group of the lane's dimensions
+#pragma unroll
+  for (int col = 0; col < 2; ++col) {
+    const int n = 2 * part + col, head = n / NG, h = NG == 1 ? col : 0;
+    if (head >= heads || n % NG != group) continue;
+    const int hq = b.kvh * heads + head;
+    const int64_t home = (static_cast<int64_t>(g.n) + b.query) * g.a.Hq + hq;
+    float v[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = s.acc[i / 2][i % 2 * 2 + col] + s.corr[col];
+    if (b.dest == -2) {
+      const float inv = s.l[h] != 0.f ? 1.f / s.l[h] : 0.f;
+      uint16_t* out = g.out + (static_cast<int64_t>(b.query) * g.a.Hq + hq) * D + quad * kRun;
+#pragma unroll
+      for (int i = 0; i < kRun; i += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const __nv_bfloat162 x = __floats2bfloat162_rn(v[i + 2 * k] * inv, v[i + 2 * k + 1] * inv);
+          w[k] = *reinterpret_cast<const uint32_t*>(&x);
+        }
+        *reinterpret_cast<uint4*>(out + i) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    } else {
+      const int64_t row = static_cast<int64_t>(b.dest) * kFewRows + head;
+      float* to = (b.dest >= 0 ? g.few_o + row * D : g.home_o + home * D) + quad * kRun;
+      if (quad == 0) (b.dest >= 0 ? g.few_ml[row] : g.home_ml[home]) = make_float2(s.m[h], s.l[h]);
+#pragma unroll
+      for (int i = 0; i < kRun; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+  }
+}
+
+template <int D, int NG>
+__global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(const __grid_constant__ GroupArgs g) {
+  extern __shared__ __align__(128) uint8_t dyn[];
+  using L = FewSmem<D>;
+  const LayerArgs& a = g.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* smem = dyn + warp * L::kWarp;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  FewBlock* blocks = reinterpret_cast<FewBlock*>(smem + L::kBlocks);
+  if (lane == 0) {
+    for (int i = 0; i < kFewStages; ++i) mbar_init(bars + i, 1);
+    fence_barrier_init();
+  }
+  __syncwarp();
+  pdl_wait();
+  pdl_trigger();
+  const int64_t per = g.head->few_per, work = g.head->few_work;
+  const int64_t me = static_cast<int64_t>(blockIdx.x) * kFewWarps + warp;
+  const int64_t b0 = min(work, me * per), b1 = min(work, b0 + per);
+  if (b0 >= b1) return;
+  const int P = a.P, heads = a.Hq / a.Hkv, jobs = g.n;
+  const Job* all = g.jobs + g.groups;
+  const int sub_q = P > 32 ? P / 32 : 1, sub_w = P / 16;  // blocks of a page
+
+  // ---- the copies' cursor: job, segment, block
+  int j;
+  {
+    int lo = 0, hi = jobs;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && g.few_base[i] <= b0));
+      const int last = lo + (k - 1) * step;
+      hi = min(hi, last + step);
+      lo = last;
+      if (step == 1) break;
+    }
+    j = lo;
+  }
+  int word = 0, nt = 0, tiles = 0;           // the job's words, one per lane; its sequence's token counts; its blocks
+  int64_t jbase = 0;
+  int seg = 0, tile = 0, tile0 = 0, tile1 = 0, batch = -1;
+  int head[kClasses], first[kClasses], upto[kClasses + 1];
+  int page = 0, cls = 0, valid = 0;          // the lane's page of a batch of 32
+  bool whole = true, more = true;
+  auto field = [&](int i) { return __shfl_sync(0xffffffffu, word, i); };
+  auto open_segment = [&]() -> bool {        // the first segment from `seg` on with blocks for this warp
+    for (; seg < a.Hkv; ++seg) {
+      const int64_t S = jbase + seg * few_cost(tiles);
+      if (S >= b1) return false;
+      tile0 = few_before(b0 - S, tiles);
+      tile1 = few_before(b1 - S, tiles);
+      if (tile0 < tile1) {
+        tile = tile0;
+        return true;
+      }
+    }
+    return false;
+  };
+  auto open_job = [&]() -> bool {            // the first job from `j` on with blocks for this warp
+    for (; j < jobs; ++j) {
+      jbase = g.few_base[j];
+      if (jbase >= b1) return false;
+      word = reinterpret_cast<const int*>(all + j)[lane];
+      tiles = field(19);
+      if (tiles == 0) continue;
+      upto[0] = 0;
+#pragma unroll
+      for (int c = 0; c < kClasses; ++c) {
+        head[c] = field(4 + c);
+        first[c] = field(8 + c);
+        upto[c + 1] = upto[c] + head[c] + field(12 + c);
+      }
+      const int seq = field(0);
+      nt = lane < kClasses ? a.ntok[static_cast<int64_t>(seq) * kClasses + lane] : 0;
+      batch = -1;
+      seg = static_cast<int>(max(static_cast<int64_t>(0), (b0 - jbase) / few_cost(tiles)));
+      if (open_segment()) return true;
+    }
+    return false;
+  };
+  more = open_job();
+
+  int issued = 0, taken = 0;                 // blocks brought, blocks used
+  int ring_head = 0, my_start = 0;           // lane s: where slot s's block starts
+  auto room = [&](int need) -> int {         // where `need` bytes fit in the ring, -1 if they do not
+    if (issued - taken >= kFewStages) return -1;
+    if (issued == taken) return need <= L::kRingBytes ? 0 : -1;
+    const int tail = __shfl_sync(0xffffffffu, my_start, taken % kFewStages);
+    if (ring_head > tail) return ring_head + need <= L::kRingBytes ? ring_head : need < tail ? 0 : -1;
+    return ring_head + need < tail ? ring_head : -1;
+  };
+  auto bring = [&]() -> bool {               // the next block's copies; false when the ring is full
+    const bool wide = tile >= sub_q * upto[3];
+    const int sub = wide ? (tile - sub_q * upto[3]) % sub_w : tile % sub_q;
+    const int i0 = wide ? upto[3] + (tile - sub_q * upto[3]) / sub_w : tile / sub_q;
+    if (i0 / 32 != batch) {
+      batch = i0 / 32;
+      const int i = batch * 32 + lane;
+      cls = i >= upto[3] ? 3 : i >= upto[2] ? 2 : i >= upto[1] ? 1 : 0;
+      const int seq = field(0), jlo = field(1), jt = field(2), sinks = field(3);
+      int h = head[0], f = first[0], n = __shfl_sync(0xffffffffu, nt, 0), u = 0;
+#pragma unroll
+      for (int c = 1; c < kClasses; ++c) {
+        const int m = __shfl_sync(0xffffffffu, nt, c);
+        if (cls == c) h = head[c], f = first[c], n = m, u = upto[c];
+      }
+      if (i < upto[4]) {
+        const int in = i - u, k = in < h ? in : f + in - h;
+        const int64_t at = (static_cast<int64_t>(seq) * kClasses + cls) * a.MP + k;
+        page = a.pt[at];
+        const int pf = a.pfirst[at], pl = a.plast[at];
+        valid = min(P, n - k * P);
+        whole = valid == P && pl <= jt && (pf >= jlo || pl < sinks);
+      }
+    }
+    const int from = i0 % 32;
+    const int c = __shfl_sync(0xffffffffu, cls, from), pg = __shfl_sync(0xffffffffu, page, from);
+    const bool all_in = __shfl_sync(0xffffffffu, static_cast<int>(whole), from);
+    const int keys = min(P, c == 3 ? 16 : 32), fill = min(keys, max(0, __shfl_sync(0xffffffffu, valid, from) - sub * keys));
+    const int row = D * bits_of_class(c) / 8, szb = c < 3 ? NG * 4 : 0;
+    const int bytes = keys * 2 * (row + szb), need = (bytes + 127) / 128 * 128 + (all_in ? 0 : 128);
+    const int off = room(need);
+    if (off < 0) return false;
+    ring_head = off + need;
+    const int slot = issued % kFewStages;
+    if (lane == slot) my_start = off;
+    const int state = (tile == tile0 ? 1 : 0) | (tile == tile1 - 1 ? 2 : 0);
+    const int joined = field(22);
+    const int dest = tile1 - tile0 < tiles ? static_cast<int>(2 * me + (tile0 > 0 ? 0 : 1)) : joined ? -1 : -2;
+    const int lo = field(1), t = field(2), sinks = field(3), query = field(21);
+    if (lane == 0) {
+      FewBlock& r = blocks[slot];
+      r.cls = c; r.keys = keys; r.off = off; r.pos = all_in ? -1 : off + (bytes + 127) / 128 * 128;
+      r.valid = fill; r.lo = lo; r.t = t; r.sinks = sinks;
+      r.query = query; r.kvh = seg; r.dest = dest; r.state = state;
+      mbar_arrive_expect_tx(bars + slot, bytes + (all_in ? 0 : 4 * keys));
+    }
+    __syncwarp();
+    const uint8_t* pool = c == 0 ? a.pool[0] : c == 1 ? a.pool[1] : c == 2 ? a.pool[2] : a.pool[3];
+    const int64_t pb = c == 0 ? a.page_bytes[0] : c == 1 ? a.page_bytes[1] : c == 2 ? a.page_bytes[2] : a.page_bytes[3];
+    const int slice = c == 0 ? a.slice[0] : c == 1 ? a.slice[1] : c == 2 ? a.slice[2] : a.slice[3];
+    const uint8_t* src = pool + pg * pb;
+    const uint8_t* sl = src + a.hdr + static_cast<int64_t>(seg) * slice;
+    uint8_t* to = smem + L::kRing + off;
+    if (keys == P) {  // the block is the whole slice
+      if (lane == 0) bulk_g2s(to, sl, bytes, bars + slot);
+    } else if (lane < (c < 3 ? 4 : 2)) {  // K codes, V codes, K scales, V scales
+      const int each = lane < 2 ? row : szb, past = lane < 2 ? 0 : 2 * row;
+      bulk_g2s(to + keys * (past + (lane & 1) * each), sl + P * (past + (lane & 1) * each) + sub * keys * each, keys * each, bars + slot);
+    }
+    if (!all_in && lane == 4) bulk_g2s(to + (bytes + 127) / 128 * 128, src + 4 * sub * keys, 4 * keys, bars + slot);
+    ++issued;
+    if (++tile == tile1) {  // on to the next segment, or job
+      ++seg;
+      if (!open_segment()) {
+        ++j;
+        more = open_job();
+      }
+    }
+    return true;
+  };
+
+  FewState<D, NG> s;
+  bool late = false;
+  while (more || taken < issued) {
+    while (more && bring()) {
+    }
+    const int slot = taken % kFewStages;
+    late = !__all_sync(0xffffffffu, mbar_wait(bars + slot, (taken / kFewStages) & 1, a.wait_ns));
+    if (late) break;
+    const FewBlock b = blocks[slot];
+    const uint8_t* ring = smem + L::kRing;
+    if (b.state & 1) few_begin<D, NG>(s, g, smem, b, heads, lane);
+    bool seen = lane < b.keys;
+    if (b.pos >= 0 && seen) {
+      const int pos = reinterpret_cast<const int32_t*>(ring + b.pos)[lane];
+      seen = lane < b.valid && pos <= b.t && (pos >= b.lo || pos < b.sinks);
+    }
+    const uint32_t mask = __ballot_sync(0xffffffffu, seen);
+    if (mask) {
+      if (b.cls == 0) few_class<D, NG, 2>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
+      else if (b.cls == 1) few_class<D, NG, 4>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
+      else if (b.cls == 2) few_class<D, NG, 8>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
+      else few_class<D, NG, 16>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
+    }
+    if (b.state & 2) few_end<D, NG>(s, g, b, heads, lane);
+    __syncwarp();
+    ++taken;
+  }
+  if (late) {  // the warp stays until its copies have landed
+    for (int k = taken; k < issued; ++k) mbar_wait(bars + k % kFewStages, (k / kFewStages) & 1);
+    if (lane == 0) set_status(a.ctrl, TRR_ERR_TIMEOUT);
+  }
+}
+
+}  // namespace trr

@@ -27,75 +27,9 @@
 #include <algorithm>
 #include <climits>
 
-#include "trr_tc.cuh"
+#include "trr_few.cuh"
 
 namespace trr {
-
-constexpr int kRows = 128;       // rows of a segment: lanes of TMEM
-constexpr int kTileKeys = 128;   // most tokens of a tile (64 of 16-bit pages: half the ring per copy)
-constexpr int kRawSlots = 8;     // tiles in the ring of raw pages
-constexpr int kSegSlots = 4;     // segments announced ahead
-constexpr int kSoftmaxWarps = 4, kExpandWarps = 8;
-constexpr int kGroupThreads = 32 * (kSoftmaxWarps + kExpandWarps + 2);
-constexpr int kPlanThreads = 128;
-
-// One job, 32 words.
-struct Job {
-  int seq, lo, t, sinks;                  // tokens in sight: pos <= t and (pos >= lo or pos < sinks)
-  int head[kClasses];                     // pages [0, head) hold the sinks
-  int first[kClasses], count[kClasses];   // pages [first, first + count)
-  int rows, row_blocks, tiles_q, tiles;   // rows = queries x heads of a KV head; tiles of 2-, 4-, 8-bit pages, of all
-  int kind;                               // 0: shared, 1: private
-  int qbase;                              // shared: its queries in the list; private: the query
-  int joined;                             // private: the query has a shared job as well
-  int pad[9];
-};
-static_assert(sizeof(Job) == 128, "a warp loads a job one word per lane");
-
-// One query, as the plan sees it.
-struct QueryPlan {
-  int err, mode, group, member;           // member: a full query in a group
-  int seq, t, lo, rank;
-  int common[kClasses];                   // leading pages that it shares with its group's first full query and sees whole
-  int head[kClasses], first[kClasses], end[kClasses];
-  int shared, pad[7];                     // shared: its row is in its group's shared job
-};
-static_assert(sizeof(QueryPlan) == 128, "");
-
-struct GroupHeader {
-  int64_t work, per;  // all segments' cost, a CTA's share
-  int jobs;
-};
-
-struct GroupArgs {
-  LayerArgs a;
-  int n, window_scalar, sinks, groups, ctas;
-  float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
-  const int32_t *seq_ids, *positions, *windows, *offsets;
-  const uint8_t* modes;
-  const uint16_t* q;
-  uint16_t* out;
-  // workspace
-  GroupHeader* head;
-  QueryPlan* plan;
-  int32_t* list;      // [n] a group's rows: its full queries in order, from the group's offset on
-  Job* jobs;          // [groups] shared, then [n] private
-  int64_t* base;      // [jobs + 1] cost before each job
-  float2* home_ml;    // [2][n][Hq] (m, l) of a row of a whole segment, by kind of job
-  float* home_o;      // [2][n][Hq][D]
-  float2* part_ml;    // [2 * ctas][128] of a piece of a segment: a CTA's first one, or its last
-  float* part_o;
-};
-
-// The cost of a segment: tiles, and a fixed part for its start and end.
-constexpr int kTileCost = 2, kSegmentCost = 2;
-__device__ __forceinline__ int64_t segment_cost(int tiles) { return kSegmentCost + static_cast<int64_t>(kTileCost) * tiles; }
-// Tiles of a segment that lie before cost x (counted from the segment's start).
-__device__ __forceinline__ int tiles_before(int64_t x, int tiles) {
-  if (x <= kSegmentCost) return 0;
-  const int64_t t = (x - kSegmentCost + kTileCost - 1) / kTileCost;
-  return t < tiles ? static_cast<int>(t) : tiles;
-}
 
 // ------------------------------------------------------------------------------ plan --
 
@@ -260,38 +194,45 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
     job->rows = heads;
     job->row_blocks = (heads + kRows - 1) / kRows;
     job->tiles_q = (nq + ppt - 1) / ppt;
-    job->tiles = job->tiles_q + (n16 + ppt16 - 1) / ppt16;
+    job->tiles = g.few ? nq * (a.P > 32 ? a.P / 32 : 1) + n16 * (a.P / 16) : job->tiles_q + (n16 + ppt16 - 1) / ppt16;
     job->kind = 1; job->qbase = j; job->joined = __ldcg(&q.shared);
   }
   __syncthreads();
   // cost before each job
-  const int jobs = g.groups + g.n;
-  int64_t before = 0;
-  for (int j0 = 0; j0 < jobs; j0 += kPlanThreads) {
-    const int j = j0 + threadIdx.x;
-    int64_t x = 0;
-    if (j < jobs && g.jobs[j].tiles > 0)
-      x = segment_cost(g.jobs[j].tiles) * a.Hkv * g.jobs[j].row_blocks;
-    int64_t y = x;
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t z = __shfl_up_sync(0xffffffffu, y, o);
-      if (lane >= o) y += z;
+  auto prefix = [&](const Job* list, int jobs, bool few, int64_t* base) -> int64_t {
+    int64_t before = 0;
+    for (int j0 = 0; j0 < jobs; j0 += kPlanThreads) {
+      const int j = j0 + threadIdx.x;
+      int64_t x = 0;
+      if (j < jobs && list[j].tiles > 0)
+        x = few ? few_cost(list[j].tiles) * a.Hkv : segment_cost(list[j].tiles) * a.Hkv * list[j].row_blocks;
+      int64_t y = x;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t z = __shfl_up_sync(0xffffffffu, y, o);
+        if (lane >= o) y += z;
+      }
+      if (lane == 31) s_sum[c] = y;
+      __syncthreads();
+      int64_t all = 0;
+      for (int k = 0; k < kPlanThreads / 32; ++k) {
+        if (k < c) y += s_sum[k];
+        all += s_sum[k];
+      }
+      if (j < jobs) base[j] = before + y - x;
+      before += all;
+      __syncthreads();
     }
-    if (lane == 31) s_sum[c] = y;
-    __syncthreads();
-    int64_t all = 0;
-    for (int k = 0; k < kPlanThreads / 32; ++k) {
-      if (k < c) y += s_sum[k];
-      all += s_sum[k];
-    }
-    if (j < jobs) g.base[j] = before + y - x;
-    before += all;
-    __syncthreads();
-  }
+    if (threadIdx.x == 0) base[jobs] = before;
+    return before;
+  };
+  const int jobs = g.few ? g.groups : g.groups + g.n;
+  const int64_t work = prefix(g.jobs, jobs, false, g.base);
+  const int64_t few_work = g.few ? prefix(g.jobs + g.groups, g.n, true, g.few_base) : 0;
   if (threadIdx.x == 0) {
-    g.base[jobs] = before;
-    g.head->work = before;
-    g.head->per = (before + g.ctas - 1) / g.ctas;
+    g.head->work = work;
+    g.head->per = (work + g.ctas - 1) / g.ctas;
+    g.head->few_work = few_work;
+    g.head->few_per = (few_work + g.few_warps - 1) / g.few_warps;
     g.head->jobs = jobs;
     if (s_first_err != INT_MAX) set_status(a.ctrl, s_first_err % 16);
   }
@@ -543,9 +484,6 @@ __device__ void group_produce(const GroupArgs& g, const Ctx<D>& x, int lane) {
   for (int k = max(0, it - kRawSlots); k < it; ++k) mbar_wait(x.raw_full(k % kRawSlots), (k / kRawSlots) & 1);
 }
 
-__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<__half2*>(&w); }
-__device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
-
 // z + c s of eight codes, given as four words of two binary16 values 1024 + c, rounded once.
 template <bool CLAMP>
 __device__ __forceinline__ uint4 expand8(uint32_t p0, uint32_t p1, uint32_t p2, uint32_t p3, __half2 s, __half2 z) {
@@ -753,12 +691,6 @@ __device__ void group_mma(const Ctx<D>& x) {
   }
   tc_commit(x.drained());  // nothing is in flight when the CTA ends
   mbar_wait(x.drained(), 0);
-}
-
-__device__ __forceinline__ float exp2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 
 template <int D>
@@ -1047,7 +979,6 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
   const int query = static_cast<int>(at / g.a.Hq), head = static_cast<int>(at % g.a.Hq), kvh = head / heads;
   const QueryPlan& p = g.plan[query];
   const bool reads = !p.err && p.mode != TRR_MODE_SKIP;
-  const int64_t per = g.head->per;
   constexpr int E = D / 32;
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
@@ -1066,14 +997,20 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
     const int tiles = g.jobs[j].tiles, blocks = g.jobs[j].row_blocks;
     if (tiles == 0) continue;
     const int rr = (kind == 0 ? p.rank * heads : 0) + head % heads;
-    const int64_t cost = segment_cost(tiles), S = g.base[j] + (static_cast<int64_t>(kvh) * blocks + rr / kRows) * cost;
-    for (int64_t c = S / per; c * per < S + cost; ++c) {
-      const int t0 = tiles_before(c * per - S, tiles), t1 = tiles_before((c + 1) * per - S, tiles);
+    const int64_t home = (static_cast<int64_t>(kind) * g.n + query) * g.a.Hq + head;
+    const bool few = kind == 1 && g.few;
+    const int64_t cost = few ? few_cost(tiles) : segment_cost(tiles), share = few ? g.head->few_per : g.head->per;
+    const int64_t S = few ? g.few_base[query] + kvh * cost : g.base[j] + (static_cast<int64_t>(kvh) * blocks + rr / kRows) * cost;
+    for (int64_t c = S / share; c * share < S + cost; ++c) {
+      const int t0 = few ? few_before(c * share - S, tiles) : tiles_before(c * share - S, tiles);
+      const int t1 = few ? few_before((c + 1) * share - S, tiles) : tiles_before((c + 1) * share - S, tiles);
       if (t0 >= t1) continue;
       if (t1 - t0 == tiles) {
         if (!g.jobs[j].joined) return;  // the row is in place
-        const int64_t home = (static_cast<int64_t>(kind) * g.n + query) * g.a.Hq + head;
         join(g.home_ml[home], g.home_o + home * D);
+      } else if (few) {
+        const int64_t slot = (2 * c + (t0 > 0 ? 0 : 1)) * kFewRows + rr;
+        join(g.few_ml[slot], g.few_o + slot * D);
       } else {
         const int64_t slot = (2 * c + (t0 > 0 ? 0 : 1)) * kRows + rr % kRows;
         join(g.part_ml[slot], g.part_o + slot * D);
@@ -1094,7 +1031,7 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
 // ----------------------------------------------------------------------------- calls --
 
 // Lays the workspace out for n queries (b == nullptr: counts its bytes).
-static int64_t lay_workspace(GroupArgs* g, uint8_t* b, const Layout& l, int n, int ctas) {
+static int64_t lay_workspace(GroupArgs* g, uint8_t* b, const Layout& l, int n, int ctas, int few_warps) {
   int64_t off = 0;
   auto take = [&](int64_t bytes) {
     uint8_t* p = b + off;
@@ -1111,28 +1048,60 @@ static int64_t lay_workspace(GroupArgs* g, uint8_t* b, const Layout& l, int n, i
   g->home_o = reinterpret_cast<float*>(take(4 * 2 * rows * l.d));
   g->part_ml = reinterpret_cast<float2*>(take(8 * parts));
   g->part_o = reinterpret_cast<float*>(take(4 * parts * l.d));
+  g->few_base = reinterpret_cast<int64_t*>(take(8ll * (n + 1)));
+  g->few_ml = reinterpret_cast<float2*>(take(8ll * 2 * few_warps * kFewRows));
+  g->few_o = reinterpret_cast<float*>(take(4ll * 2 * few_warps * kFewRows * l.d));
   return off;
 }
 
 int64_t group_workspace_bytes(const Layout& l, int ctas) {
   GroupArgs g;
-  return lay_workspace(&g, nullptr, l, l.max_queries, ctas);
+  return lay_workspace(&g, nullptr, l, l.max_queries, ctas, ctas * kFewCtas * kFewWarps);
+}
+
+// The kernel for few rows of a layout, nullptr where its columns (query heads of a KV head x
+// groups) are more than a product's eight.
+static void (*few_kernel(const Layout& l))(GroupArgs) {
+  const int ng = l.d / l.G;
+  if (l.Hq / l.Hkv * ng > 8) return nullptr;
+  if (l.d == 64) return ng == 1 ? group_few_kernel<64, 1> : group_few_kernel<64, 2>;
+  return ng == 1 ? group_few_kernel<128, 1> : ng == 2 ? group_few_kernel<128, 2> : group_few_kernel<128, 4>;
 }
 
 cudaError_t configure_group() {
+  for (auto k : {group_few_kernel<64, 1>, group_few_kernel<64, 2>}) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, FewSmem<64>::kTotal);
+    if (e != cudaSuccess) return e;
+  }
+  for (auto k : {group_few_kernel<128, 1>, group_few_kernel<128, 2>, group_few_kernel<128, 4>}) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, FewSmem<128>::kTotal);
+    if (e != cudaSuccess) return e;
+  }
   cudaError_t e = cudaFuncSetAttribute(group_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, GroupSmem<64>::kTotal + 1024);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(group_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, GroupSmem<128>::kTotal + 1024);
 }
 
 template <int D>
-static cudaError_t launch_kernels(const GroupArgs& g, cudaStream_t s) {
+static cudaError_t launch_kernels(const GroupArgs& g, void (*few)(GroupArgs), cudaStream_t s, int* launches) {
+  *launches = 0;
   cudaError_t e = launch_pdl(group_plan_kernel, dim3(g.n), dim3(kPlanThreads), 0, s, g);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(group_attn_kernel<D>, dim3(g.ctas), dim3(kGroupThreads), GroupSmem<D>::kTotal + 1024, s, g);
-  if (e != cudaSuccess) return e;
+  ++*launches;
+  if (few) {
+    e = launch_pdl(few, dim3(g.few_warps / kFewWarps), dim3(32 * kFewWarps), FewSmem<D>::kTotal, s, g);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  if (!few || g.groups > 0) {
+    e = launch_pdl(group_attn_kernel<D>, dim3(g.ctas), dim3(kGroupThreads), GroupSmem<D>::kTotal + 1024, s, g);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
   const int64_t rows = static_cast<int64_t>(g.n) * g.a.Hq;
-  return launch_pdl(group_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, s, g);
+  e = launch_pdl(group_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, s, g);
+  if (e == cudaSuccess) ++*launches;
+  return e;
 }
 
 static trr_status launch_group(trr_cache* cache, int layer, int n, const int32_t* seq_ids, const int32_t* positions,
@@ -1158,12 +1127,16 @@ static trr_status launch_group(trr_cache* cache, int layer, int n, const int32_t
   g.out = static_cast<uint16_t*>(out);
   g.a.wait_ns = cache_wait_ns(cache);
   g.ctas = cache_num_sms(cache);
-  lay_workspace(&g, static_cast<uint8_t*>(workspace), l, n, g.ctas);
+  const auto few = few_kernel(l);
+  g.few = few != nullptr;
+  g.few_warps = g.ctas * kFewCtas * kFewWarps;
+  lay_workspace(&g, static_cast<uint8_t*>(workspace), l, n, g.ctas, g.few_warps);
   cache_note_call(cache, layer);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((l.d == 64 ? launch_kernels<64>(g, s) : launch_kernels<128>(g, s)) != cudaSuccess) return TRR_ERR_CUDA;
-  cache_set_launches(cache, 3);
-  return TRR_OK;
+  int launches = 0;
+  const cudaError_t e = l.d == 64 ? launch_kernels<64>(g, few, s, &launches) : launch_kernels<128>(g, few, s, &launches);
+  cache_set_launches(cache, launches);
+  return e == cudaSuccess ? TRR_OK : TRR_ERR_CUDA;
 }
 
 }  // namespace trr

@@ -1,0 +1,97 @@
+// trr_group.cuh - what the kernels of attention over groups and sinks share: jobs, the call's
+// arguments and workspace, and how work is cut into equal runs.
+#pragma once
+
+#include "trr_tc.cuh"
+
+namespace trr {
+
+constexpr int kRows = 128;       // rows of a segment: lanes of TMEM
+constexpr int kTileKeys = 128;   // most tokens of a tile (64 of 16-bit pages: half the ring per copy)
+constexpr int kRawSlots = 8;     // tiles in the ring of raw pages
+constexpr int kSegSlots = 4;     // segments announced ahead
+constexpr int kSoftmaxWarps = 4, kExpandWarps = 8;
+constexpr int kGroupThreads = 32 * (kSoftmaxWarps + kExpandWarps + 2);
+constexpr int kPlanThreads = 128;
+
+// One job, 32 words.
+struct Job {
+  int seq, lo, t, sinks;                  // tokens in sight: pos <= t and (pos >= lo or pos < sinks)
+  int head[kClasses];                     // pages [0, head) hold the sinks
+  int first[kClasses], count[kClasses];   // pages [first, first + count)
+  int rows, row_blocks, tiles_q, tiles;   // rows = queries x heads of a KV head; tiles of 2-, 4-, 8-bit pages, of all
+                                          // (few rows: tiles is the number of blocks)
+  int kind;                               // 0: shared, 1: private
+  int qbase;                              // shared: its queries in the list; private: the query
+  int joined;                             // private: the query has a shared job as well
+  int pad[9];
+};
+static_assert(sizeof(Job) == 128, "a warp loads a job one word per lane");
+
+// One query, as the plan sees it.
+struct QueryPlan {
+  int err, mode, group, member;           // member: a full query in a group
+  int seq, t, lo, rank;
+  int common[kClasses];                   // leading pages that it shares with its group's first full query and sees whole
+  int head[kClasses], first[kClasses], end[kClasses];
+  int shared, pad[7];                     // shared: its row is in its group's shared job
+};
+static_assert(sizeof(QueryPlan) == 128, "");
+
+struct GroupHeader {
+  int64_t work, per;          // cost of the tensor kernel's segments, a CTA's share
+  int64_t few_work, few_per;  // cost of the private segments of few rows, a warp's share
+  int jobs;                   // of the tensor kernel
+};
+
+struct GroupArgs {
+  LayerArgs a;
+  int n, window_scalar, sinks, groups, ctas;
+  int few, few_warps;         // private segments go to the kernel for few rows, with that many warps
+  float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
+  const int32_t *seq_ids, *positions, *windows, *offsets;
+  const uint8_t* modes;
+  const uint16_t* q;
+  uint16_t* out;
+  // workspace
+  GroupHeader* head;
+  QueryPlan* plan;
+  int32_t* list;      // [n] a group's rows: its full queries in order, from the group's offset on
+  Job* jobs;          // [groups] shared, then [n] private
+  int64_t* base;      // [jobs + 1] cost before each job
+  float2* home_ml;    // [2][n][Hq] (m, l) of a row of a whole segment, by kind of job
+  float* home_o;      // [2][n][Hq][D]
+  float2* part_ml;    // [2 * ctas][128] of a piece of a segment: a CTA's first one, or its last
+  float* part_o;
+  int64_t* few_base;  // [n + 1] cost before each private job, of the kernel for few rows
+  float2* few_ml;     // [2 * few_warps][8] of a warp's first piece, or its last
+  float* few_o;
+};
+
+// The cost of a segment: tiles, and a fixed part for its start and end.
+constexpr int kTileCost = 2, kSegmentCost = 2;
+__device__ __forceinline__ int64_t segment_cost(int tiles) { return kSegmentCost + static_cast<int64_t>(kTileCost) * tiles; }
+// Tiles of a segment that lie before cost x (counted from the segment's start).
+__device__ __forceinline__ int tiles_before(int64_t x, int tiles) {
+  if (x <= kSegmentCost) return 0;
+  const int64_t t = (x - kSegmentCost + kTileCost - 1) / kTileCost;
+  return t < tiles ? static_cast<int>(t) : tiles;
+}
+
+// The same for the kernel for few rows, in blocks.
+constexpr int kFewSegmentCost = 1;
+__device__ __forceinline__ int64_t few_cost(int blocks) { return kFewSegmentCost + blocks; }
+__device__ __forceinline__ int few_before(int64_t x, int blocks) {
+  return x <= kFewSegmentCost ? 0 : x - kFewSegmentCost < blocks ? static_cast<int>(x - kFewSegmentCost) : blocks;
+}
+
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<__half2*>(&w); }
+__device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+}  // namespace trr

@@ -30,6 +30,7 @@ constexpr int kFewWarps = 8;      // warps of a CTA
 constexpr int kFewCtas = 2;       // CTAs of an SM
 constexpr int kFewStages = 6;     // blocks in a warp's ring
 constexpr int kFewRows = 8;       // most rows of a segment
+constexpr int kFewSmem = 112 * 1024;  // of a CTA
 
 // A block in the ring.
 struct FewBlock {
@@ -38,17 +39,18 @@ struct FewBlock {
   int query, kvh, dest, state;  // state: 1 first block of a segment's piece, 2 last one
 };
 
-template <int D>
+template <int D, int NG>
 struct FewSmem {
-  static constexpr int kQ = kFewRows * D * 2;
-  static constexpr int kBlocks = kQ + 64;                              // after Q: a factor for each row
-  static constexpr int kBars = kBlocks + kFewStages * static_cast<int>(sizeof(FewBlock));
+  static constexpr int kQ = kFewRows / NG * D * 2;                          // query rows in binary16, then in bf16, scaled
+  static constexpr int kFactor = 2 * kQ;                               // a factor for each row, sums of its groups
+  static constexpr int kBlocks = kFactor + 4 * kFewRows + 4 * kFewRows * 4;
+  static constexpr int kJob = kBlocks + kFewStages * static_cast<int>(sizeof(FewBlock));  // the cursor's job, then its token counts
+  static constexpr int kBars = kJob + static_cast<int>(sizeof(Job)) + 16;
   static constexpr int kRing = (kBars + 8 * kFewStages + 127) / 128 * 128;
-  static constexpr int kWarp = 112 * 1024 / kFewWarps / 128 * 128;     // a warp's share
+  static constexpr int kWarp = kFewSmem / kFewWarps;                   // a warp's share
   static constexpr int kRingBytes = kWarp - kRing;
-  static constexpr int kTotal = kWarp * kFewWarps;
 };
-static_assert(FewSmem<128>::kRingBytes >= 32 * 288 + 128, "the widest block");
+static_assert(FewSmem<128, 1>::kRingBytes >= 32 * 264 + 128 && FewSmem<128, 4>::kRingBytes >= 32 * 288 + 128, "the widest blocks");
 
 template <int B>
 struct Codes;
@@ -101,69 +103,67 @@ struct FewState {
   int q_class;
 };
 
-// The query rows as the second operand, in the order in which class B's codes come out of their words.
+// The query rows as the second operand, in the order in which class B's codes come out of their
+// words (4 bits: elements i and i + 4 together, 2 bits: i and i + 8).
 template <int D, int NG, int B>
 __device__ __forceinline__ void few_load_q(FewState<D, NG>& s, const uint8_t* smem, int heads, int lane) {
-  constexpr int kRun = D / 4;  // a lane's dimensions
   const int n = lane >> 2, part = lane & 3, head = n / NG;
   const bool live = head < heads && part * NG / 4 == n % NG;  // the lane's dimensions lie in the column's group
-  const float down = live ? reinterpret_cast<const float*>(smem + FewSmem<D>::kQ)[head + 8] : 0.f;
-  const uint16_t* row = reinterpret_cast<const uint16_t*>(smem) + (live ? head : 0) * D + part * kRun;
-  auto value = [&](int e) { return live ? __uint_as_float(static_cast<uint32_t>(row[e]) << 16) * down : 0.f; };
-  float sum = 0.f;
+  const uint4* row = reinterpret_cast<const uint4*>(smem + (B == 16 ? FewSmem<D, NG>::kQ : 0) + ((live ? head : 0) * D + part * (D / 4)) * 2);
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) {
-    int e0, e1, e2, e3;
-    if (B == 2) {
-      e0 = t / 4 * 16 + 2 * (t % 4); e1 = e0 + 8; e2 = e0 + 1; e3 = e0 + 9;
-    } else if (B == 4) {
-      e0 = t / 2 * 8 + 2 * (t % 2); e1 = e0 + 4; e2 = e0 + 1; e3 = e0 + 5;
-    } else {
-      e0 = 4 * t; e1 = e0 + 1; e2 = e0 + 2; e3 = e0 + 3;
+  for (int i = 0; i < D / 64; ++i) {  // 16 elements
+    uint4 u = row[2 * i], v = row[2 * i + 1];
+    if (!live) u = v = make_uint4(0, 0, 0, 0);
+    const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (B == 2) {
+        s.q[4 * i + t][0] = __byte_perm(w[t], w[t + 4], 0x5410);
+        s.q[4 * i + t][1] = __byte_perm(w[t], w[t + 4], 0x7632);
+      } else if (B == 4) {
+        const int k = t / 2 * 4 + t % 2;
+        s.q[4 * i + t][0] = __byte_perm(w[k], w[k + 2], 0x5410);
+        s.q[4 * i + t][1] = __byte_perm(w[k], w[k + 2], 0x7632);
+      } else {
+        s.q[4 * i + t][0] = w[2 * t];
+        s.q[4 * i + t][1] = w[2 * t + 1];
+      }
     }
-    if (B == 16) {
-      const __nv_bfloat162 x = __floats2bfloat162_rn(value(e0), value(e1)), y = __floats2bfloat162_rn(value(e2), value(e3));
-      s.q[t][0] = *reinterpret_cast<const uint32_t*>(&x);
-      s.q[t][1] = *reinterpret_cast<const uint32_t*>(&y);
-    } else {
-      const __half2 x = __floats2half2_rn(value(e0), value(e1)), y = __floats2half2_rn(value(e2), value(e3));
-      s.q[t][0] = as_u32(x);
-      s.q[t][1] = as_u32(y);
-      sum += __low2float(x) + __high2float(x) + __low2float(y) + __high2float(y);
-    }
-  }
-  if (B != 16) {
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    s.qsum[0] = __shfl_sync(0xffffffffu, sum, 8 * part);
-    s.qsum[1] = __shfl_sync(0xffffffffu, sum, 8 * part + 4);
   }
   s.q_class = B;
 }
 
-// One block of 16 NB tokens: K codes, V codes, K scales, V scales side by side at blk; bit k of
-// mask: token k is in sight.
-template <int D, int NG, int B, int NB>
-__device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk, uint32_t mask, bool swz, int lane) {
+// 16 tokens of a block of `keys`, from token b on: K codes, V codes, K scales, V scales side by
+// side at blk; bit k of mask: token b + k is in sight.
+template <int D, int NG, int B>
+__device__ __forceinline__ void few_tokens(FewState<D, NG>& s, const uint8_t* blk, int keys, int b, uint32_t mask, bool swz, int lane) {
   using S = FewState<D, NG>;
-  constexpr int kRow = D * B / 8, kKeys = 16 * NB;
+  constexpr int kRow = D * B / 8;
   constexpr float kOff = Codes<B>::kOffset;
   const int quad = lane >> 2, part = lane & 3;
   const bool sw = swz && B >= 8;
   auto at = [&](int o) { return blk + (sw ? static_cast<int>(swz_off(o)) : o); };
-  const uint32_t* ksz = reinterpret_cast<const uint32_t*>(blk + 2 * kKeys * kRow);
-  const uint32_t* vsz = ksz + kKeys * NG;
-  const int g0 = NG == 1 ? 0 : (2 * part) % NG, g1 = NG == 1 ? 0 : g0 + 1;  // the groups of the lane's two columns
+  const uint32_t* ksz = reinterpret_cast<const uint32_t*>(blk + 2 * keys * kRow);
+  const uint32_t* vsz = ksz + keys * NG;
+  const int g0 = NG == 1 ? 0 : (2 * part) % NG;  // the group of the lane's first column; the second's is the next
+  auto scales = [&](const uint32_t* sz, int key, uint32_t (&to)[2]) {
+    if (NG == 1) {
+      to[0] = to[1] = sz[key];
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(sz + key * NG + g0);
+      to[0] = u.x;
+      to[1] = u.y;
+    }
+  };
 
-  float x[NB][2][S::kHeads];      // scores in base-2 exponents
-  uint32_t vs[NB][2][2];          // V's (scale, zero) of the lane's tokens and columns
+  float x[2][S::kHeads];      // scores in base-2 exponents of tokens b + quad and + 8
+  uint32_t vs[2][2];          // V's (scale, zero) of the lane's tokens and columns
   float top[S::kHeads];
 #pragma unroll
   for (int h = 0; h < S::kHeads; ++h) top[h] = -INFINITY;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
+  {
     float c[4] = {0.f, 0.f, 0.f, 0.f};
-    const int k0 = (16 * b + quad) * kRow + part * (kRow / 4), k1 = k0 + 8 * kRow;
+    const int k0 = (b + quad) * kRow + part * (kRow / 4), k1 = k0 + 8 * kRow;
     if (B == 2) {
 #pragma unroll
       for (int w = 0; w < D / 64; ++w) {
@@ -199,30 +199,31 @@ __device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk
       }
     }
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {  // tokens 16 b + quad and + 8
-      const int key = 16 * b + 8 * r + quad;
-      const bool seen = mask >> key & 1;
+    for (int r = 0; r < 2; ++r) {
+      const int key = b + 8 * r + quad;
+      const bool seen = mask >> (8 * r + quad) & 1;
       float y[S::kHeads], grow = 0.f;
       if (B == 16) {
         if (NG == 1) { y[0] = c[2 * r]; y[S::kHeads - 1] = c[2 * r + 1]; }
         else y[0] = c[2 * r] + c[2 * r + 1];
       } else {
-        const __half2 k0s = as_half2(ksz[key * NG + g0]), k1s = as_half2(ksz[key * NG + g1]);
+        uint32_t ks[2];
+        scales(ksz, key, ks);
+        scales(vsz, key, vs[r]);
+        const __half2 k0s = as_half2(ks[0]), k1s = as_half2(ks[1]);
         const float y0 = __low2float(k0s) * (c[2 * r] - kOff * s.qsum[0]) + __high2float(k0s) * s.qsum[0];
         const float y1 = __low2float(k1s) * (c[2 * r + 1] - kOff * s.qsum[1]) + __high2float(k1s) * s.qsum[1];
         if (NG == 1) { y[0] = y0; y[S::kHeads - 1] = y1; }
         else y[0] = y0 + y1;
-        vs[b][r][0] = vsz[key * NG + g0];
-        vs[b][r][1] = vsz[key * NG + g1];
-        uint32_t e = max(vs[b][r][0] & 0x7C00u, vs[b][r][1] & 0x7C00u);  // the larger scale's exponent
+        uint32_t e = max(vs[r][0] & 0x7C00u, vs[r][1] & 0x7C00u);  // the larger scale's exponent
         if (NG == 4) e = max(e, __shfl_xor_sync(0xffffffffu, e, 1));
         grow = static_cast<float>(static_cast<int>(e >> 10) - 15);
       }
       if (NG == 4) y[0] += __shfl_xor_sync(0xffffffffu, y[0], 1);
 #pragma unroll
       for (int h = 0; h < S::kHeads; ++h) {
-        x[b][r][h] = seen ? y[h] * s.f[h] : -INFINITY;
-        if (seen) top[h] = fmaxf(top[h], x[b][r][h] + grow);
+        x[r][h] = seen ? y[h] * s.f[h] : -INFINITY;
+        if (seen) top[h] = fmaxf(top[h], x[r][h] + grow);
       }
     }
   }
@@ -245,16 +246,15 @@ __device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk
         }
     }
   }
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
+  {
     uint32_t w[2][2];  // weights of token rows quad, quad + 8: binary16, or bf16 high and low parts
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const bool seen = mask >> (16 * b + 8 * r + quad) & 1;
+      const bool seen = mask >> (8 * r + quad) & 1;
       float p[S::kHeads];
 #pragma unroll
       for (int h = 0; h < S::kHeads; ++h) {
-        p[h] = seen ? exp2_approx(x[b][r][h] - s.m[h]) : 0.f;
+        p[h] = seen ? exp2_approx(x[r][h] - s.m[h]) : 0.f;
         s.l[h] += p[h];
       }
       const float p0 = p[0], p1 = p[S::kHeads - 1];
@@ -264,7 +264,7 @@ __device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk
         w[r][0] = *reinterpret_cast<const uint32_t*>(&hi);
         w[r][1] = *reinterpret_cast<const uint32_t*>(&lo);
       } else {
-        const __half2 v0 = as_half2(vs[b][r][0]), v1 = as_half2(vs[b][r][1]);
+        const __half2 v0 = as_half2(vs[r][0]), v1 = as_half2(vs[r][1]);
         __half2 wv = __floats2half2_rn(p0 * __low2float(v0), p1 * __low2float(v1));
         if (!seen) wv = as_half2(0u);  // the scale of a slot that holds nothing may be anything
         w[r][0] = as_u32(wv);
@@ -278,8 +278,8 @@ __device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk
     uint32_t l0 = 0, l1 = 0;
     if (B == 16) l0 = transpose8(w[0][1]), l1 = transpose8(w[1][1]);
     // tokens 2 part, 2 part + 1 (and 8 further on): an eighth of the dimensions, from quad * D / 8
-    const int kp = 16 * b + 2 * part;
-    const int v0 = kKeys * kRow + kp * kRow + quad * (kRow / 8);
+    const int kp = b + 2 * part;
+    const int v0 = (keys + kp) * kRow + quad * (kRow / 8);
     if (B == 2) {
       uint32_t lo, hi;  // pairs of tokens: 8 codes of each of two
 #pragma unroll
@@ -320,8 +320,9 @@ __device__ __forceinline__ void few_block(FewState<D, NG>& s, const uint8_t* blk
       }
     } else {
       // rows out of sight become zero: their weight of 0 times infinity would not be
-      const uint32_t ma = (mask >> kp & 1 ? 0x0000FFFFu : 0u) | (mask >> (kp + 1) & 1 ? 0xFFFF0000u : 0u);
-      const uint32_t mb = (mask >> (kp + 8) & 1 ? 0x0000FFFFu : 0u) | (mask >> (kp + 9) & 1 ? 0xFFFF0000u : 0u);
+      const uint32_t seen = mask >> (2 * part);
+      const uint32_t ma = (seen & 1 ? 0x0000FFFFu : 0u) | (seen & 2 ? 0xFFFF0000u : 0u);
+      const uint32_t mb = (seen & 0x100 ? 0x0000FFFFu : 0u) | (seen & 0x200 ? 0xFFFF0000u : 0u);
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
         const uint4 q0 = *reinterpret_cast<const uint4*>(at(v0 + 16 * i)), q1 = *reinterpret_cast<const uint4*>(at(v0 + kRow + 16 * i));
@@ -344,8 +345,10 @@ template <int D, int NG, int B>
 __device__ __forceinline__ void few_class(FewState<D, NG>& s, const uint8_t* smem, const uint8_t* blk, int keys, uint32_t mask, bool swz,
                                           int heads, int lane) {
   if (s.q_class != B) few_load_q<D, NG, B>(s, smem, heads, lane);
-  if (B == 16 || keys == 16) few_block<D, NG, B, 1>(s, blk, mask, swz, lane);
-  else few_block<D, NG, B, B == 16 ? 1 : 2>(s, blk, mask, swz, lane);
+  // one copy of the code for both halves of a block: the warps' instructions have to fit the cache together
+#pragma unroll 1
+  for (int b = 0; b < keys; b += 16)
+    if (mask >> b & 0xFFFFu) few_tokens<D, NG, B>(s, blk, keys, b, mask >> b & 0xFFFFu, swz, lane);
 }
 
 // A segment's piece begins: its query rows, each with the power of two that brings its largest
@@ -353,26 +356,47 @@ __device__ __forceinline__ void few_class(FewState<D, NG>& s, const uint8_t* sme
 template <int D, int NG>
 __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g, uint8_t* smem, const FewBlock& b, int heads, int lane) {
   const uint4* src = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(b.query) * g.a.Hq + b.kvh * heads) * D);
-  float* factor = reinterpret_cast<float*>(smem + FewSmem<D>::kQ);
+  float* factor = reinterpret_cast<float*>(smem + FewSmem<D, NG>::kFactor);
+  float* sums = factor + kFewRows;  // [row][group] of the binary16 elements
   __syncwarp();
-  constexpr int kLanes = D / 8;  // lanes of a row
+  constexpr int kLanes = D / 8, kGroupLanes = kLanes / NG;  // lanes of a row, of a group
   for (int i = lane; i < (heads * kLanes + 31) / 32 * 32; i += 32) {
+    const bool live = i < heads * kLanes;
     uint4 u = make_uint4(0, 0, 0, 0);
-    if (i < heads * kLanes) u = src[i];
+    if (live) u = src[i];
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     uint32_t top = 0;
-    for (const uint32_t w : {u.x, u.y, u.z, u.w}) top = max(top, max(w & 0x7FFFu, (w >> 16) & 0x7FFFu));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
     for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
     e = max(-100, min(120, e));
-    if (i < heads * kLanes) {
-      reinterpret_cast<uint4*>(smem)[i] = u;
-      if (i % kLanes == 0) {
-        factor[i / kLanes] = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
-        factor[i / kLanes + 8] = __int_as_float((127 - e) << 23);
-      }
+    const float down = __int_as_float((127 - e) << 23);
+    uint32_t h[4], b16[4];
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float lo = bf16lo(w[k]) * down, hi = bf16hi(w[k]) * down;
+      const __half2 x = __floats2half2_rn(lo, hi);
+      const __nv_bfloat162 y = __floats2bfloat162_rn(lo, hi);
+      h[k] = as_u32(x);
+      b16[k] = *reinterpret_cast<const uint32_t*>(&y);
+      sum += __low2float(x) + __high2float(x);
+    }
+    for (int o = 1; o < kGroupLanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (live) {
+      reinterpret_cast<uint4*>(smem)[i] = make_uint4(h[0], h[1], h[2], h[3]);
+      reinterpret_cast<uint4*>(smem + FewSmem<D, NG>::kQ)[i] = make_uint4(b16[0], b16[1], b16[2], b16[3]);
+      if (i % kLanes == 0) factor[i / kLanes] = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
+      if (i % kGroupLanes == 0) sums[i / kGroupLanes] = sum;
     }
   }
   __syncwarp();
+#pragma unroll
+  for (int col = 0; col < 2; ++col) {
+    const int n = 2 * (lane & 3) + col;
+    s.qsum[col] = n / NG < heads ? sums[n] : 0.f;
+  }
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -436,7 +460,7 @@ __device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, 
 template <int D, int NG>
 __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(const __grid_constant__ GroupArgs g) {
   extern __shared__ __align__(128) uint8_t dyn[];
-  using L = FewSmem<D>;
+  using L = FewSmem<D, NG>;
   const LayerArgs& a = g.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* smem = dyn + warp * L::kWarp;
@@ -471,13 +495,13 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     }
     j = lo;
   }
-  int word = 0, nt = 0, tiles = 0;           // the job's words, one per lane; its sequence's token counts; its blocks
+  Job& job = *reinterpret_cast<Job*>(smem + L::kJob);
+  int32_t* counts = reinterpret_cast<int32_t*>(smem + L::kJob + sizeof(Job));
+  int tiles = 0, pages_q = 0, pages = 0;     // the job's blocks, its pages of 2, 4 and 8 bits, all of them
   int64_t jbase = 0;
   int seg = 0, tile = 0, tile0 = 0, tile1 = 0, batch = -1;
-  int head[kClasses], first[kClasses], upto[kClasses + 1];
-  int page = 0, cls = 0, valid = 0;          // the lane's page of a batch of 32
-  bool whole = true, more = true;
-  auto field = [&](int i) { return __shfl_sync(0xffffffffu, word, i); };
+  int page = 0, info = 0;                    // the lane's page of a batch of 32: id; class | tokens << 2 | all in sight << 16
+  bool more = true;
   auto open_segment = [&]() -> bool {        // the first segment from `seg` on with blocks for this warp
     for (; seg < a.Hkv; ++seg) {
       const int64_t S = jbase + seg * few_cost(tiles);
@@ -495,18 +519,18 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     for (; j < jobs; ++j) {
       jbase = g.few_base[j];
       if (jbase >= b1) return false;
-      word = reinterpret_cast<const int*>(all + j)[lane];
-      tiles = field(19);
+      const int word = reinterpret_cast<const int*>(all + j)[lane];
+      __syncwarp();
+      reinterpret_cast<int*>(&job)[lane] = word;
+      __syncwarp();
+      tiles = job.tiles;
       if (tiles == 0) continue;
-      upto[0] = 0;
+      if (lane < kClasses) counts[lane] = a.ntok[static_cast<int64_t>(job.seq) * kClasses + lane];
+      pages_q = 0;
 #pragma unroll
-      for (int c = 0; c < kClasses; ++c) {
-        head[c] = field(4 + c);
-        first[c] = field(8 + c);
-        upto[c + 1] = upto[c] + head[c] + field(12 + c);
-      }
-      const int seq = field(0);
-      nt = lane < kClasses ? a.ntok[static_cast<int64_t>(seq) * kClasses + lane] : 0;
+      for (int c = 0; c < 3; ++c) pages_q += job.head[c] + job.count[c];
+      pages = pages_q + job.head[3] + job.count[3];
+      __syncwarp();
       batch = -1;
       seg = static_cast<int>(max(static_cast<int64_t>(0), (b0 - jbase) / few_cost(tiles)));
       if (open_segment()) return true;
@@ -524,66 +548,72 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     if (ring_head > tail) return ring_head + need <= L::kRingBytes ? ring_head : need < tail ? 0 : -1;
     return ring_head + need < tail ? ring_head : -1;
   };
-  auto bring = [&]() -> bool {               // the next block's copies; false when the ring is full
-    const bool wide = tile >= sub_q * upto[3];
-    const int sub = wide ? (tile - sub_q * upto[3]) % sub_w : tile % sub_q;
-    const int i0 = wide ? upto[3] + (tile - sub_q * upto[3]) / sub_w : tile / sub_q;
+  // the block that comes next: class, page, whether all of it is in sight, tokens, bytes
+  int nc = 0, npage = 0, nkeys = 0, nfill = 0, nsub = 0, nbytes = 0;
+  bool nall = true;
+  auto prepare = [&]() {
+    const int nq = sub_q * pages_q;
+    const bool wide = tile >= nq;
+    nsub = wide ? (tile - nq) & (sub_w - 1) : tile & (sub_q - 1);
+    const int i0 = wide ? pages_q + (tile - nq) / sub_w : tile / sub_q;
     if (i0 / 32 != batch) {
       batch = i0 / 32;
-      const int i = batch * 32 + lane;
-      cls = i >= upto[3] ? 3 : i >= upto[2] ? 2 : i >= upto[1] ? 1 : 0;
-      const int seq = field(0), jlo = field(1), jt = field(2), sinks = field(3);
-      int h = head[0], f = first[0], n = __shfl_sync(0xffffffffu, nt, 0), u = 0;
-#pragma unroll
-      for (int c = 1; c < kClasses; ++c) {
-        const int m = __shfl_sync(0xffffffffu, nt, c);
-        if (cls == c) h = head[c], f = first[c], n = m, u = upto[c];
-      }
-      if (i < upto[4]) {
-        const int in = i - u, k = in < h ? in : f + in - h;
-        const int64_t at = (static_cast<int64_t>(seq) * kClasses + cls) * a.MP + k;
+      int in = batch * 32 + lane, c = 0;
+      if (in < pages) {
+#pragma unroll 1
+        for (; c < 3; ++c) {
+          const int m = job.head[c] + job.count[c];
+          if (in < m) break;
+          in -= m;
+        }
+        const int h = job.head[c], k = in < h ? in : job.first[c] + in - h;
+        const int64_t at = (static_cast<int64_t>(job.seq) * kClasses + c) * a.MP + k;
         page = a.pt[at];
-        const int pf = a.pfirst[at], pl = a.plast[at];
-        valid = min(P, n - k * P);
-        whole = valid == P && pl <= jt && (pf >= jlo || pl < sinks);
+        const int pf = a.pfirst[at], pl = a.plast[at], valid = min(P, counts[c] - k * P);
+        const bool whole = valid == P && pl <= job.t && (pf >= job.lo || pl < job.sinks);
+        info = c | valid << 2 | (whole ? 1 << 16 : 0);
       }
+      __syncwarp();
     }
-    const int from = i0 % 32;
-    const int c = __shfl_sync(0xffffffffu, cls, from), pg = __shfl_sync(0xffffffffu, page, from);
-    const bool all_in = __shfl_sync(0xffffffffu, static_cast<int>(whole), from);
-    const int keys = min(P, c == 3 ? 16 : 32), fill = min(keys, max(0, __shfl_sync(0xffffffffu, valid, from) - sub * keys));
-    const int row = D * bits_of_class(c) / 8, szb = c < 3 ? NG * 4 : 0;
-    const int bytes = keys * 2 * (row + szb), need = (bytes + 127) / 128 * 128 + (all_in ? 0 : 128);
+    const int got = __shfl_sync(0xffffffffu, info, i0 & 31);
+    npage = __shfl_sync(0xffffffffu, page, i0 & 31);
+    nc = got & 3;
+    nall = got >> 16;
+    nkeys = min(P, nc == 3 ? 16 : 32);
+    nfill = min(nkeys, max(0, ((got >> 2) & 0x3FF) - nsub * nkeys));
+    nbytes = nkeys * ((D / 4) << (nc + 1)) + (nc < 3 ? nkeys * NG * 8 : 0);  // two rows of D (2 << nc) / 8 bytes, scales
+  };
+  if (more) prepare();
+  auto bring = [&]() -> bool {               // its copies; false when the ring is full
+    const int need = (nbytes + 127) / 128 * 128 + (nall ? 0 : 128);
     const int off = room(need);
     if (off < 0) return false;
     ring_head = off + need;
     const int slot = issued % kFewStages;
     if (lane == slot) my_start = off;
     const int state = (tile == tile0 ? 1 : 0) | (tile == tile1 - 1 ? 2 : 0);
-    const int joined = field(22);
-    const int dest = tile1 - tile0 < tiles ? static_cast<int>(2 * me + (tile0 > 0 ? 0 : 1)) : joined ? -1 : -2;
-    const int lo = field(1), t = field(2), sinks = field(3), query = field(21);
     if (lane == 0) {
       FewBlock& r = blocks[slot];
-      r.cls = c; r.keys = keys; r.off = off; r.pos = all_in ? -1 : off + (bytes + 127) / 128 * 128;
-      r.valid = fill; r.lo = lo; r.t = t; r.sinks = sinks;
-      r.query = query; r.kvh = seg; r.dest = dest; r.state = state;
-      mbar_arrive_expect_tx(bars + slot, bytes + (all_in ? 0 : 4 * keys));
+      r.cls = nc; r.keys = nkeys; r.off = off; r.pos = nall ? -1 : off + need - 128;
+      r.valid = nfill; r.lo = job.lo; r.t = job.t; r.sinks = job.sinks;
+      r.query = job.qbase; r.kvh = seg; r.state = state;
+      r.dest = tile1 - tile0 < tiles ? static_cast<int>(2 * me + (tile0 > 0 ? 0 : 1)) : job.joined ? -1 : -2;
+      mbar_arrive_expect_tx(bars + slot, nbytes + (nall ? 0 : 4 * nkeys));
     }
     __syncwarp();
-    const uint8_t* pool = c == 0 ? a.pool[0] : c == 1 ? a.pool[1] : c == 2 ? a.pool[2] : a.pool[3];
-    const int64_t pb = c == 0 ? a.page_bytes[0] : c == 1 ? a.page_bytes[1] : c == 2 ? a.page_bytes[2] : a.page_bytes[3];
-    const int slice = c == 0 ? a.slice[0] : c == 1 ? a.slice[1] : c == 2 ? a.slice[2] : a.slice[3];
-    const uint8_t* src = pool + pg * pb;
+    const uint8_t* pool = nc == 0 ? a.pool[0] : nc == 1 ? a.pool[1] : nc == 2 ? a.pool[2] : a.pool[3];
+    const int64_t pb = nc == 0 ? a.page_bytes[0] : nc == 1 ? a.page_bytes[1] : nc == 2 ? a.page_bytes[2] : a.page_bytes[3];
+    const int slice = nc == 0 ? a.slice[0] : nc == 1 ? a.slice[1] : nc == 2 ? a.slice[2] : a.slice[3];
+    const uint8_t* src = pool + npage * pb;
     const uint8_t* sl = src + a.hdr + static_cast<int64_t>(seg) * slice;
     uint8_t* to = smem + L::kRing + off;
-    if (keys == P) {  // the block is the whole slice
-      if (lane == 0) bulk_g2s(to, sl, bytes, bars + slot);
-    } else if (lane < (c < 3 ? 4 : 2)) {  // K codes, V codes, K scales, V scales
-      const int each = lane < 2 ? row : szb, past = lane < 2 ? 0 : 2 * row;
-      bulk_g2s(to + keys * (past + (lane & 1) * each), sl + P * (past + (lane & 1) * each) + sub * keys * each, keys * each, bars + slot);
+    if (nkeys == P) {  // the block is the whole slice
+      if (lane == 0) bulk_g2s(to, sl, nbytes, bars + slot);
+    } else if (lane < (nc < 3 ? 4 : 2)) {  // K codes, V codes, K scales, V scales
+      const int row = (D / 8) << (nc + 1), each = lane < 2 ? row : NG * 4, past = lane < 2 ? 0 : 2 * row;
+      bulk_g2s(to + nkeys * (past + (lane & 1) * each), sl + P * (past + (lane & 1) * each) + nsub * nkeys * each, nkeys * each, bars + slot);
     }
-    if (!all_in && lane == 4) bulk_g2s(to + (bytes + 127) / 128 * 128, src + 4 * sub * keys, 4 * keys, bars + slot);
+    if (!nall && lane == 4) bulk_g2s(to + need - 128, src + 4 * nsub * nkeys, 4 * nkeys, bars + slot);
     ++issued;
     if (++tile == tile1) {  // on to the next segment, or job
       ++seg;
@@ -592,6 +622,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
         more = open_job();
       }
     }
+    if (more) prepare();
     return true;
   };
 

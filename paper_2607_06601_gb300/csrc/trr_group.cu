@@ -1070,11 +1070,11 @@ static void (*few_kernel(const Layout& l))(GroupArgs) {
 
 cudaError_t configure_group() {
   for (auto k : {group_few_kernel<64, 1>, group_few_kernel<64, 2>}) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, FewSmem<64>::kTotal);
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
   }
   for (auto k : {group_few_kernel<128, 1>, group_few_kernel<128, 2>, group_few_kernel<128, 4>}) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, FewSmem<128>::kTotal);
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
   }
   cudaError_t e = cudaFuncSetAttribute(group_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, GroupSmem<64>::kTotal + 1024);
@@ -1089,7 +1089,7 @@ static cudaError_t launch_kernels(const GroupArgs& g, void (*few)(GroupArgs), cu
   if (e != cudaSuccess) return e;
   ++*launches;
   if (few) {
-    e = launch_pdl(few, dim3(g.few_warps / kFewWarps), dim3(32 * kFewWarps), FewSmem<D>::kTotal, s, g);
+    e = launch_pdl(few, dim3(g.few_warps / kFewWarps), dim3(32 * kFewWarps), kFewSmem, s, g);
     if (e != cudaSuccess) return e;
     ++*launches;
   }

@@ -27,10 +27,19 @@
 namespace trr {
 
 constexpr int kFewWarps = 8;      // warps of a CTA
-constexpr int kFewCtas = 2;       // CTAs of an SM
-constexpr int kFewStages = 6;     // blocks in a warp's ring
+constexpr int kFewCtas = 2;       // CTAs of an SM (three of 80 registers a thread are slower: 56 against 44 us on 64 sequences of
+                                  // 32 heads with windows of 511)
+constexpr int kFewStages = 8;     // blocks in a warp's ring
 constexpr int kFewRows = 8;       // most rows of a segment
 constexpr int kFewSmem = 112 * 1024;  // of a CTA
+
+// Where a warp's copies stand; in shared memory, since few instructions of a block need it.
+struct FewCursor {
+  int64_t b0, b1, base;         // the warp's run of cost, the job's start
+  int j, seg, tile0, pad0;      // job, segment, its first block for this warp
+  int tiles, pages_q, pad;      // the job's blocks, its pages of 2, 4 and 8 bits
+  int counts[kClasses];         // tokens of its sequence
+};
 
 // A block in the ring.
 struct FewBlock {
@@ -44,13 +53,16 @@ struct FewSmem {
   static constexpr int kQ = kFewRows / NG * D * 2;                          // query rows in binary16, then in bf16, scaled
   static constexpr int kFactor = 2 * kQ;                               // a factor for each row, sums of its groups
   static constexpr int kBlocks = kFactor + 4 * kFewRows + 4 * kFewRows * 4;
-  static constexpr int kJob = kBlocks + kFewStages * static_cast<int>(sizeof(FewBlock));  // the cursor's job, then its token counts
-  static constexpr int kBars = kJob + static_cast<int>(sizeof(Job)) + 16;
+  static constexpr int kJob = kBlocks + kFewStages * static_cast<int>(sizeof(FewBlock));  // the cursor's job
+  static constexpr int kCursor = kJob + static_cast<int>(sizeof(Job));
+  static constexpr int kBars = kCursor + static_cast<int>(sizeof(FewCursor));
   static constexpr int kRing = (kBars + 8 * kFewStages + 127) / 128 * 128;
-  static constexpr int kWarp = kFewSmem / kFewWarps;                   // a warp's share
+  static constexpr int kWarp = kFewSmem / kFewWarps / 128 * 128;  // a warp's share
   static constexpr int kRingBytes = kWarp - kRing;
 };
-static_assert(FewSmem<128, 1>::kRingBytes >= 32 * 264 + 128 && FewSmem<128, 4>::kRingBytes >= 32 * 288 + 128, "the widest blocks");
+static_assert(FewSmem<64, 1>::kRingBytes >= 32 * 136 + 128 && FewSmem<64, 2>::kRingBytes >= 32 * 144 + 128 &&
+                  FewSmem<128, 1>::kRingBytes >= 32 * 264 + 128 && FewSmem<128, 4>::kRingBytes >= 32 * 288 + 128,
+              "the widest blocks");
 
 template <int B>
 struct Codes;
@@ -141,8 +153,8 @@ __device__ __forceinline__ void few_tokens(FewState<D, NG>& s, const uint8_t* bl
   constexpr int kRow = D * B / 8;
   constexpr float kOff = Codes<B>::kOffset;
   const int quad = lane >> 2, part = lane & 3;
-  const bool sw = swz && B >= 8;
-  auto at = [&](int o) { return blk + (sw ? static_cast<int>(swz_off(o)) : o); };
+  const int flip = swz ? 0x70 : 0;  // permuted rows: chunk ^ line % 8 (swz_off)
+  auto at = [&](int o) { return blk + (B >= 8 ? o ^ ((o >> 3) & flip) : o); };
   const uint32_t* ksz = reinterpret_cast<const uint32_t*>(blk + 2 * keys * kRow);
   const uint32_t* vsz = ksz + keys * NG;
   const int g0 = NG == 1 ? 0 : (2 * part) % NG;  // the group of the lane's first column; the second's is the next
@@ -174,11 +186,14 @@ __device__ __forceinline__ void few_tokens(FewState<D, NG>& s, const uint8_t* bl
       }
     } else if (B == 4) {
 #pragma unroll
-      for (int w = 0; w < D / 32; ++w) {
-        const uint32_t u = *reinterpret_cast<const uint32_t*>(blk + k0 + 4 * w), v = *reinterpret_cast<const uint32_t*>(blk + k1 + 4 * w);
+      for (int w = 0; w < D / 64; ++w) {
+        const uint2 u2 = *reinterpret_cast<const uint2*>(blk + k0 + 8 * w), v2 = *reinterpret_cast<const uint2*>(blk + k1 + 8 * w);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          mma16816<false>(c, codes4(u, 2 * t), codes4(v, 2 * t), codes4(u, 2 * t + 1), codes4(v, 2 * t + 1), s.q[2 * w + t][0], s.q[2 * w + t][1]);
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t u = t < 2 ? u2.x : u2.y, v = t < 2 ? v2.x : v2.y;
+          mma16816<false>(c, codes4(u, 2 * (t & 1)), codes4(v, 2 * (t & 1)), codes4(u, 2 * (t & 1) + 1), codes4(v, 2 * (t & 1) + 1), s.q[4 * w + t][0],
+                          s.q[4 * w + t][1]);
+        }
       }
     } else if (B == 8) {
 #pragma unroll
@@ -473,18 +488,19 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
   __syncwarp();
   pdl_wait();
   pdl_trigger();
-  const int64_t per = g.head->few_per, work = g.head->few_work;
-  const int64_t me = static_cast<int64_t>(blockIdx.x) * kFewWarps + warp;
-  const int64_t b0 = min(work, me * per), b1 = min(work, b0 + per);
-  if (b0 >= b1) return;
-  const int P = a.P, heads = a.Hq / a.Hkv, jobs = g.n;
-  const Job* all = g.jobs + g.groups;
-  const int sub_q = P > 32 ? P / 32 : 1, sub_w = P / 16;  // blocks of a page
-
-  // ---- the copies' cursor: job, segment, block
-  int j;
+  FewCursor& cur = *reinterpret_cast<FewCursor*>(smem + L::kCursor);
+  Job& job = *reinterpret_cast<Job*>(smem + L::kJob);
+  const int me = blockIdx.x * kFewWarps + warp, P = a.P, heads = a.Hq / a.Hkv;
+  const int lg_p = __ffs(P) - 1, lg_q = max(0, lg_p - 5), lg_w = lg_p - 4;  // log2 of the blocks of a page: 32 tokens, 16 of 16 bits
+  int tile = 0, tile1 = 0, batch = -1;       // the segment's next block, its end for this warp; batch of 32 blocks that the lanes hold
+  // the lane's block of the batch: its K codes in KV head 0, and class | all in sight << 2 |
+  // tokens << 3 | 16 slots instead of 32 << 9 | bytes / 16 << 10
+  const uint8_t* mine = nullptr;
+  uint32_t info = 0;
   {
-    int lo = 0, hi = jobs;
+    const int64_t per = g.head->few_per, work = g.head->few_work, b0 = min(work, me * per), b1 = min(work, b0 + per);
+    if (b0 >= b1) return;
+    int lo = 0, hi = g.n;  // the job that holds cost b0: the last one that starts at or before it
     while (hi - lo > 1) {
       const int step = (hi - lo + 31) / 32, i = lo + lane * step;
       const int k = __popc(__ballot_sync(0xffffffffu, i < hi && g.few_base[i] <= b0));
@@ -493,144 +509,158 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
       lo = last;
       if (step == 1) break;
     }
-    j = lo;
+    if (lane == 0) cur.b0 = b0, cur.b1 = b1, cur.j = lo;
+    __syncwarp();
   }
-  Job& job = *reinterpret_cast<Job*>(smem + L::kJob);
-  int32_t* counts = reinterpret_cast<int32_t*>(smem + L::kJob + sizeof(Job));
-  int tiles = 0, pages_q = 0, pages = 0;     // the job's blocks, its pages of 2, 4 and 8 bits, all of them
-  int64_t jbase = 0;
-  int seg = 0, tile = 0, tile0 = 0, tile1 = 0, batch = -1;
-  int page = 0, info = 0;                    // the lane's page of a batch of 32: id; class | tokens << 2 | all in sight << 16
-  bool more = true;
-  auto open_segment = [&]() -> bool {        // the first segment from `seg` on with blocks for this warp
+
+  // The copies' cursor.  Every lane reads and works out the same; lane 0 writes.
+  auto open_segment = [&](int seg) -> bool {  // the job's first segment from `seg` on with blocks for this warp
+    const int64_t b0 = cur.b0, b1 = cur.b1, base = cur.base;
+    const int tiles = cur.tiles;
     for (; seg < a.Hkv; ++seg) {
-      const int64_t S = jbase + seg * few_cost(tiles);
+      const int64_t S = base + seg * few_cost(tiles);
       if (S >= b1) return false;
-      tile0 = few_before(b0 - S, tiles);
-      tile1 = few_before(b1 - S, tiles);
-      if (tile0 < tile1) {
-        tile = tile0;
+      const int t0 = few_before(b0 - S, tiles), t1 = few_before(b1 - S, tiles);
+      if (t0 < t1) {
+        tile = t0;
+        tile1 = t1;
+        __syncwarp();
+        if (lane == 0) cur.seg = seg, cur.tile0 = t0;
+        __syncwarp();
         return true;
       }
     }
     return false;
   };
-  auto open_job = [&]() -> bool {            // the first job from `j` on with blocks for this warp
-    for (; j < jobs; ++j) {
-      jbase = g.few_base[j];
-      if (jbase >= b1) return false;
+  auto open_job = [&](int j) -> bool {        // the first job from `j` on with blocks for this warp
+    const Job* all = g.jobs + g.groups;
+    for (; j < g.n; ++j) {
+      const int64_t base = g.few_base[j];
+      if (base >= cur.b1) return false;
       const int word = reinterpret_cast<const int*>(all + j)[lane];
       __syncwarp();
       reinterpret_cast<int*>(&job)[lane] = word;
       __syncwarp();
-      tiles = job.tiles;
+      const int tiles = job.tiles;
       if (tiles == 0) continue;
-      if (lane < kClasses) counts[lane] = a.ntok[static_cast<int64_t>(job.seq) * kClasses + lane];
-      pages_q = 0;
-#pragma unroll
-      for (int c = 0; c < 3; ++c) pages_q += job.head[c] + job.count[c];
-      pages = pages_q + job.head[3] + job.count[3];
+      if (lane < kClasses) cur.counts[lane] = a.ntok[static_cast<int64_t>(job.seq) * kClasses + lane];
+      if (lane == 0) {
+        int q = 0;
+        for (int c = 0; c < 3; ++c) q += job.head[c] + job.count[c];
+        cur.pages_q = q;
+        cur.tiles = tiles;
+        cur.base = base;
+        cur.j = j;
+      }
       __syncwarp();
       batch = -1;
-      seg = static_cast<int>(max(static_cast<int64_t>(0), (b0 - jbase) / few_cost(tiles)));
-      if (open_segment()) return true;
+      if (open_segment(static_cast<int>(max(static_cast<int64_t>(0), (cur.b0 - base) / few_cost(tiles))))) return true;
     }
     return false;
   };
-  more = open_job();
+  bool more = open_job(cur.j);
 
-  int issued = 0, taken = 0;                 // blocks brought, blocks used
-  int ring_head = 0, my_start = 0;           // lane s: where slot s's block starts
-  auto room = [&](int need) -> int {         // where `need` bytes fit in the ring, -1 if they do not
-    if (issued - taken >= kFewStages) return -1;
-    if (issued == taken) return need <= L::kRingBytes ? 0 : -1;
-    const int tail = __shfl_sync(0xffffffffu, my_start, taken % kFewStages);
-    if (ring_head > tail) return ring_head + need <= L::kRingBytes ? ring_head : need < tail ? 0 : -1;
-    return ring_head + need < tail ? ring_head : -1;
-  };
-  // the block that comes next: class, page, whether all of it is in sight, tokens, bytes
-  int nc = 0, npage = 0, nkeys = 0, nfill = 0, nsub = 0, nbytes = 0;
-  bool nall = true;
-  auto prepare = [&]() {
-    const int nq = sub_q * pages_q;
-    const bool wide = tile >= nq;
-    nsub = wide ? (tile - nq) & (sub_w - 1) : tile & (sub_q - 1);
-    const int i0 = wide ? pages_q + (tile - nq) / sub_w : tile / sub_q;
-    if (i0 / 32 != batch) {
-      batch = i0 / 32;
-      int in = batch * 32 + lane, c = 0;
-      if (in < pages) {
+  auto load_batch = [&]() {
+    batch = tile >> 5;
+    const int i = (batch << 5) + lane;
+    if (i < cur.tiles) {
+      const int nq = cur.pages_q << lg_q;
+      const bool wide = i >= nq;
+      const int lg = wide ? lg_w : lg_q, n = wide ? i - nq : i, sub = n & ((1 << lg) - 1);
+      int in = n >> lg, c = wide ? 3 : 0;
+      if (!wide) {
 #pragma unroll 1
-        for (; c < 3; ++c) {
+        for (; c < 2; ++c) {
           const int m = job.head[c] + job.count[c];
           if (in < m) break;
           in -= m;
         }
-        const int h = job.head[c], k = in < h ? in : job.first[c] + in - h;
-        const int64_t at = (static_cast<int64_t>(job.seq) * kClasses + c) * a.MP + k;
-        page = a.pt[at];
-        const int pf = a.pfirst[at], pl = a.plast[at], valid = min(P, counts[c] - k * P);
-        const bool whole = valid == P && pl <= job.t && (pf >= job.lo || pl < job.sinks);
-        info = c | valid << 2 | (whole ? 1 << 16 : 0);
       }
-      __syncwarp();
-    }
-    const int got = __shfl_sync(0xffffffffu, info, i0 & 31);
-    npage = __shfl_sync(0xffffffffu, page, i0 & 31);
-    nc = got & 3;
-    nall = got >> 16;
-    nkeys = min(P, nc == 3 ? 16 : 32);
-    nfill = min(nkeys, max(0, ((got >> 2) & 0x3FF) - nsub * nkeys));
-    nbytes = nkeys * ((D / 4) << (nc + 1)) + (nc < 3 ? nkeys * NG * 8 : 0);  // two rows of D (2 << nc) / 8 bytes, scales
-  };
-  if (more) prepare();
-  auto bring = [&]() -> bool {               // its copies; false when the ring is full
-    const int need = (nbytes + 127) / 128 * 128 + (nall ? 0 : 128);
-    const int off = room(need);
-    if (off < 0) return false;
-    ring_head = off + need;
-    const int slot = issued % kFewStages;
-    if (lane == slot) my_start = off;
-    const int state = (tile == tile0 ? 1 : 0) | (tile == tile1 - 1 ? 2 : 0);
-    if (lane == 0) {
-      FewBlock& r = blocks[slot];
-      r.cls = nc; r.keys = nkeys; r.off = off; r.pos = nall ? -1 : off + need - 128;
-      r.valid = nfill; r.lo = job.lo; r.t = job.t; r.sinks = job.sinks;
-      r.query = job.qbase; r.kvh = seg; r.state = state;
-      r.dest = tile1 - tile0 < tiles ? static_cast<int>(2 * me + (tile0 > 0 ? 0 : 1)) : job.joined ? -1 : -2;
-      mbar_arrive_expect_tx(bars + slot, nbytes + (nall ? 0 : 4 * nkeys));
+      const int h = job.head[c], k = in < h ? in : job.first[c] + in - h;
+      const int64_t at = (static_cast<int64_t>(job.seq) * kClasses + c) * a.MP + k;
+      const int page = a.pt[at], pf = a.pfirst[at], pl = a.plast[at], valid = min(P, cur.counts[c] - k * P);
+      const bool whole = valid == P && pl <= job.t && (pf >= job.lo || pl < job.sinks);
+      // no more slots than hold a token, or, of a page that ends before the window, than can be sinks
+      // (slot x of page k holds position k P + x or a later one)
+      const int slot0 = sub << (wide ? 4 : 5), fill = max(0, valid - slot0);
+      const int most = pl < job.lo ? min(fill, max(1, job.sinks - k * P - slot0)) : fill;
+      const int keys = min(P, wide || most <= 16 ? 16 : 32), row = (D / 8) << (c + 1), block = min(P, wide ? 16 : 32);
+      const int bytes = 2 * keys * (row + (wide ? 0 : NG * 4));
+      mine = a.pool[c] + page * a.page_bytes[c] + a.hdr + sub * block * row;
+      info = c | (whole ? 4 : 0) | min(keys, fill) << 3 | (keys == 16 ? 1 << 9 : 0) | bytes / 16 << 10;
     }
     __syncwarp();
-    const uint8_t* pool = nc == 0 ? a.pool[0] : nc == 1 ? a.pool[1] : nc == 2 ? a.pool[2] : a.pool[3];
-    const int64_t pb = nc == 0 ? a.page_bytes[0] : nc == 1 ? a.page_bytes[1] : nc == 2 ? a.page_bytes[2] : a.page_bytes[3];
-    const int slice = nc == 0 ? a.slice[0] : nc == 1 ? a.slice[1] : nc == 2 ? a.slice[2] : a.slice[3];
-    const uint8_t* src = pool + npage * pb;
-    const uint8_t* sl = src + a.hdr + static_cast<int64_t>(seg) * slice;
-    uint8_t* to = smem + L::kRing + off;
-    if (nkeys == P) {  // the block is the whole slice
-      if (lane == 0) bulk_g2s(to, sl, nbytes, bars + slot);
-    } else if (lane < (nc < 3 ? 4 : 2)) {  // K codes, V codes, K scales, V scales
-      const int row = (D / 8) << (nc + 1), each = lane < 2 ? row : NG * 4, past = lane < 2 ? 0 : 2 * row;
-      bulk_g2s(to + nkeys * (past + (lane & 1) * each), sl + P * (past + (lane & 1) * each) + nsub * nkeys * each, nkeys * each, bars + slot);
+  };
+
+  int issued = 0, taken = 0;                 // blocks brought, blocks used
+  int ring_head = 0, low = 0;                // where the next one goes; the ring is filled up when no more than `low` are left
+  // Brings as many of the segment's next blocks as the batch holds and the ring has room for, one per lane.
+  auto bring = [&]() {
+    if (tile >> 5 != batch) load_batch();
+    const int l0 = tile & 31, want = min(min(32 - l0, tile1 - tile), kFewStages - (issued - taken));
+    const int r = lane - l0;
+    const bool cand = r >= 0 && r < want;
+    const bool all_in = info & 4;
+    const int bytes = (info >> 10) * 16, body = (bytes + 127) & ~127, need = cand ? body + (all_in ? 0 : 128) : 0;
+    int upto = need;
+#pragma unroll
+    for (int o = 1; o < kFewStages; o <<= 1) {  // lanes outside the candidates add nothing
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
     }
-    if (!nall && lane == 4) bulk_g2s(to + need - 128, src + 4 * nsub * nkeys, 4 * nkeys, bars + slot);
-    ++issued;
-    if (++tile == tile1) {  // on to the next segment, or job
-      ++seg;
-      if (!open_segment()) {
-        ++j;
-        more = open_job();
+    int start = ring_head, space = L::kRingBytes;
+    if (issued == taken) {
+      start = 0;
+    } else {
+      const int tail = blocks[taken % kFewStages].off;
+      if (ring_head <= tail) {
+        space = tail - ring_head - 1;
+      } else {
+        space = L::kRingBytes - ring_head;
+        if (__shfl_sync(0xffffffffu, need, l0) > space) start = 0, space = tail - 1;
       }
     }
-    if (more) prepare();
-    return true;
+    const int k = __popc(__ballot_sync(0xffffffffu, cand && upto <= space));
+    if (k == 0) return;
+    const int seg = cur.seg, tile0 = cur.tile0, tiles = cur.tiles;
+    if (cand && r < k) {
+      const int slot = (issued + r) % kFewStages, c = info & 3, keys = info & 512 ? 16 : 32, off = start + upto - need;
+      FewBlock& b = blocks[slot];
+      b.cls = c; b.keys = keys; b.off = off; b.pos = all_in ? -1 : off + body;
+      b.valid = info >> 3 & 63; b.lo = job.lo; b.t = job.t; b.sinks = job.sinks;
+      b.query = job.qbase; b.kvh = seg; b.state = (tile + r == tile0 ? 1 : 0) | (tile + r == tile1 - 1 ? 2 : 0);
+      b.dest = tile1 - tile0 < tiles ? 2 * me + (tile0 > 0 ? 0 : 1) : job.joined ? -1 : -2;
+      mbar_arrive_expect_tx(bars + slot, bytes + (all_in ? 0 : 4 * keys));
+      const uint8_t* src = mine + static_cast<int64_t>(seg) * a.slice[c];
+      uint8_t* to = smem + L::kRing + off;
+      const int row = (D / 8) << (c + 1);  // `sub`: the block's first slot in its page
+      const int sub = ((tile + r - (c == 3 ? cur.pages_q << lg_q : 0)) & ((1 << (c == 3 ? lg_w : lg_q)) - 1)) * min(P, c == 3 ? 16 : 32);
+      if (keys == P) {  // the block is the whole slice
+        bulk_g2s(to, src, bytes, bars + slot);
+      } else {          // K codes, V codes, K scales, V scales
+        const uint8_t* sz = src - sub * row + 2 * P * row + sub * NG * 4;
+        bulk_g2s(to, src, keys * row, bars + slot);
+        bulk_g2s(to + keys * row, src + P * row, keys * row, bars + slot);
+        if (c < 3) {
+          bulk_g2s(to + 2 * keys * row, sz, keys * NG * 4, bars + slot);
+          bulk_g2s(to + keys * (2 * row + NG * 4), sz + P * NG * 4, keys * NG * 4, bars + slot);
+        }
+      }
+      if (!all_in) bulk_g2s(to + body, mine - sub * row - a.hdr + 4 * sub, 4 * keys, bars + slot);
+    }
+    __syncwarp();
+    ring_head = start + __shfl_sync(0xffffffffu, upto, l0 + k - 1);
+    issued += k;
+    tile += k;
+    low = (issued - taken) / 2;
+    if (tile == tile1 && !open_segment(seg + 1)) more = open_job(cur.j + 1);  // on to the next segment, or job
   };
 
   FewState<D, NG> s;
   bool late = false;
   while (more || taken < issued) {
-    while (more && bring()) {
-    }
+    if (more && issued - taken <= low) bring();
+    if (issued == taken) continue;  // the segment's end left the ring empty
     const int slot = taken % kFewStages;
     late = !__all_sync(0xffffffffu, mbar_wait(bars + slot, (taken / kFewStages) & 1, a.wait_ns));
     if (late) break;

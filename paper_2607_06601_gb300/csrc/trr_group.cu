@@ -55,24 +55,36 @@ __device__ __forceinline__ int count_below(const int32_t* x, int n, int v, int l
   return lo;
 }
 
-// CTA i plans query i, warp c its class c; the CTA that finishes last makes the jobs.
-__global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
-  __shared__ int s_bad, s_group, s_leader, s_last, s_first_err;
+// Tiles (or blocks) of a job of nq pages of 2, 4 and 8 bits and n16 of 16.
+__device__ __forceinline__ int job_tiles(const GroupArgs& g, bool few, int nq, int n16, int* tiles_q) {
+  const int P = g.a.P, ppt = kTileKeys / P, ppt16 = kTileKeys / 2 / P;
+  *tiles_q = (nq + ppt - 1) / ppt;
+  return few ? nq * (P > 32 ? P / 32 : 1) + n16 * (P / 16) : *tiles_q + (n16 + ppt16 - 1) / ppt16;
+}
+
+// CTA i plans query i, warp c its class c; the CTA that finishes last plans the groups and lays
+// the jobs end to end.  All of it is chains of dependent loads, so what a query's CTA can settle
+// alone (its private job unless it is a full query of a group, the zero rows of a query that reads
+// nothing) does not wait for the last one.
+__global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_constant__ GroupArgs g) {
+  __shared__ int s_bad, s_group, s_leader, s_last, s_first_err, s_there;
   __shared__ int64_t s_sum[kPlanThreads / 32];
+  __shared__ Job s_job;
   const LayerArgs& a = g.a;
+  const int lane = threadIdx.x & 31, c = threadIdx.x >> 5, i = blockIdx.x, heads = a.Hq / a.Hkv;
+  if (threadIdx.x == 0) s_bad = 0, s_group = -1, s_leader = INT_MAX, s_first_err = INT_MAX;
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31, c = threadIdx.x >> 5, i = blockIdx.x;
-  if (threadIdx.x == 0) s_bad = 0, s_group = -1, s_leader = INT_MAX, s_first_err = INT_MAX;
   __syncthreads();
   for (int x = threadIdx.x; x <= g.groups && g.groups > 0; x += kPlanThreads) {
     const int o = g.offsets[x], next = x < g.groups ? g.offsets[x + 1] : o;
     if (o < 0 || o > g.n || next < o) s_bad = 1;
     if (o <= i && i < next) s_group = x;
   }
-  __syncthreads();
-  const int err = s_bad ? TRR_ERR_INVALID_ARG : query_error(g, i);
+  int err = query_error(g, i);
   const int mode = g.modes[i], t = g.positions[i], seq = g.seq_ids[i];
+  __syncthreads();
+  if (s_bad) err = TRR_ERR_INVALID_ARG;
   const bool reads = !err && mode != TRR_MODE_SKIP;
   const bool member = reads && mode == TRR_MODE_FULL && s_group >= 0;
   if (member) {  // the group's first full query, whose pages the others' are compared with
@@ -81,9 +93,8 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
         atomicMin(&s_leader, j);
         break;
       }
+    __syncthreads();
   }
-  __syncthreads();
-  QueryPlan& p = g.plan[i];
   const int lo = mode == TRR_MODE_LOCAL ? t - (g.windows ? g.windows[i] : g.window_scalar) + 1 : INT_MIN;
   int head = 0, first = 0, end = 0, common = 0;
   if (reads) {
@@ -123,10 +134,32 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
       }
     }
   }
-  if (lane == 0) p.common[c] = common, p.head[c] = head, p.first[c] = first, p.end[c] = end;
+  QueryPlan& p = g.plan[i];
+  if (lane == 0) {
+    p.common[c] = common;
+    s_job.head[c] = head;
+    s_job.first[c] = first;
+    s_job.count[c] = max(0, end - first);
+  }
+  __syncthreads();
   if (threadIdx.x == 0) {
-    p.err = err; p.mode = mode; p.group = s_group; p.member = member;
-    p.seq = seq; p.t = t; p.lo = lo; p.rank = 0; p.shared = 0;
+    int nq = 0;
+    for (int k = 0; k < 3; ++k) nq += s_job.head[k] + s_job.count[k];
+    s_job.seq = seq; s_job.lo = lo; s_job.t = t; s_job.sinks = mode == TRR_MODE_LOCAL ? g.sinks : 0;
+    s_job.rows = heads;
+    s_job.row_blocks = (heads + kRows - 1) / kRows;
+    s_job.tiles = job_tiles(g, g.few, nq, s_job.head[3] + s_job.count[3], &s_job.tiles_q);
+    s_job.kind = 1; s_job.qbase = i; s_job.joined = 0;
+    const int there = reads && (member || s_job.tiles > 0);
+    p.reads = there; p.group = member ? s_group : -1; p.rank = 0; p.shared = 0;
+    g.tiles[g.groups + i] = err ? -err : there ? s_job.tiles : 0;
+    s_there = there;
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) reinterpret_cast<int*>(g.jobs + g.groups + i)[threadIdx.x] = reinterpret_cast<const int*>(&s_job)[threadIdx.x];
+  if (!s_there) {  // nothing in sight
+    uint4* out = reinterpret_cast<uint4*>(g.out + static_cast<int64_t>(i) * a.Hq * a.d);
+    for (int x = threadIdx.x; x < a.Hq * a.d / 8; x += kPlanThreads) out[x] = make_uint4(0, 0, 0, 0);
   }
   __syncthreads();
   if (threadIdx.x == 0) s_last = atom_add_acq_rel(a.ctrl + kGroupDone, 1) == static_cast<int>(gridDim.x) - 1;
@@ -134,22 +167,23 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
   if (!s_last) return;
   if (threadIdx.x == 0) a.ctrl[kGroupDone] = 0;
 
-  // groups: a warp each
-  const int ppt = kTileKeys / a.P, ppt16 = kTileKeys / 2 / a.P, heads = a.Hq / a.Hkv;
-  const bool grouped = !s_bad;
-  for (int x = c; x < g.groups; x += kPlanThreads / 32) {
+  for (int x = c; x < g.groups; x += kPlanThreads / 32) {  // groups: a warp each
     Job* job = g.jobs + x;
     int members = 0, least[kClasses] = {INT_MAX, INT_MAX, INT_MAX, INT_MAX};
-    const int q0 = grouped ? g.offsets[x] : 0, q1 = grouped ? g.offsets[x + 1] : 0;
+    const int q0 = s_bad ? 0 : g.offsets[x], q1 = s_bad ? 0 : g.offsets[x + 1];
     for (int j0 = q0; j0 < q1; j0 += 32) {
       const int j = j0 + lane;
-      const bool in = j < q1 && __ldcg(&g.plan[j].member);
+      const bool in = j < q1 && __ldcg(&g.plan[j].group) >= 0;
       const unsigned m = __ballot_sync(0xffffffffu, in);
       if (in) {
         const int rank = members + __popc(m & ((1u << lane) - 1));
+        const int4 common = __ldcg(reinterpret_cast<const int4*>(g.plan[j].common));
         g.list[q0 + rank] = j;
         g.plan[j].rank = rank;
-        for (int k = 0; k < kClasses; ++k) least[k] = min(least[k], __ldcg(&g.plan[j].common[k]));
+        least[0] = min(least[0], common.x);
+        least[1] = min(least[1], common.y);
+        least[2] = min(least[2], common.z);
+        least[3] = min(least[3], common.w);
       }
       members += __popc(m);
     }
@@ -159,53 +193,51 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
       if (members < 2) least[k] = 0;  // nobody to share with
       pages += least[k];
     }
-    for (int j = q0 + lane; j < q1; j += 32)
-      if (__ldcg(&g.plan[j].member)) {
-        g.plan[j].shared = pages > 0;
-        for (int k = 0; k < kClasses; ++k) g.plan[j].first[k] = least[k];
-      }
+    __syncwarp();
+    if (pages > 0)  // the members' private jobs start behind the shared pages
+      for (int j = q0 + lane; j < q1; j += 32)
+        if (__ldcg(&g.plan[j].group) >= 0) {
+          Job* own = g.jobs + g.groups + j;
+          int nq = 0, n16 = 0, tiles_q;
+          for (int k = 0; k < kClasses; ++k) {
+            const int left = max(0, __ldcg(&own->count[k]) - least[k]);
+            own->first[k] = least[k];
+            own->count[k] = left;
+            (k < 3 ? nq : n16) += left;
+          }
+          const int tiles = job_tiles(g, g.few, nq, n16, &tiles_q);
+          own->tiles_q = tiles_q;
+          own->tiles = tiles;
+          own->joined = 1;
+          g.tiles[g.groups + j] = tiles;
+          g.plan[j].shared = 1;
+        }
     if (lane == 0) {
-      const int nq = least[0] + least[1] + least[2];
-      const bool any = members > 1;
-      job->seq = any ? __ldcg(&g.plan[g.list[q0]].seq) : 0;
+      job->seq = pages > 0 ? __ldcg(&g.jobs[g.groups + g.list[q0]].seq) : 0;
       job->lo = INT_MIN; job->t = INT_MAX; job->sinks = 0;
-      for (int k = 0; k < kClasses; ++k) job->head[k] = 0, job->first[k] = 0, job->count[k] = any ? least[k] : 0;
+      for (int k = 0; k < kClasses; ++k) job->head[k] = 0, job->first[k] = 0, job->count[k] = least[k];
       job->rows = members * heads;
       job->row_blocks = (job->rows + kRows - 1) / kRows;
-      job->tiles_q = any ? (nq + ppt - 1) / ppt : 0;
-      job->tiles = job->tiles_q + (any ? (least[3] + ppt16 - 1) / ppt16 : 0);
+      int tiles_q = 0;
+      const int tiles = pages > 0 ? job_tiles(g, false, least[0] + least[1] + least[2], least[3], &tiles_q) : 0;
+      job->tiles_q = tiles_q;
+      job->tiles = tiles;
       job->kind = 0; job->qbase = q0; job->joined = 1;
+      g.tiles[x] = tiles;
     }
-  }
-  __syncthreads();
-  // private jobs, and the errors
-  for (int j = threadIdx.x; j < g.n; j += kPlanThreads) {
-    const QueryPlan& q = g.plan[j];
-    Job* job = g.jobs + g.groups + j;
-    const int e = __ldcg(&q.err), md = __ldcg(&q.mode);
-    if (e) atomicMin(&s_first_err, j * 16 + e);
-    int nq = 0, n16 = 0;
-    job->seq = __ldcg(&q.seq); job->lo = __ldcg(&q.lo); job->t = __ldcg(&q.t); job->sinks = md == TRR_MODE_LOCAL ? g.sinks : 0;
-    for (int k = 0; k < kClasses; ++k) {
-      const int hd = __ldcg(&q.head[k]), f = __ldcg(&q.first[k]), m = max(0, __ldcg(&q.end[k]) - f);
-      job->head[k] = hd; job->first[k] = f; job->count[k] = m;
-      (k < 3 ? nq : n16) += hd + m;
-    }
-    job->rows = heads;
-    job->row_blocks = (heads + kRows - 1) / kRows;
-    job->tiles_q = (nq + ppt - 1) / ppt;
-    job->tiles = g.few ? nq * (a.P > 32 ? a.P / 32 : 1) + n16 * (a.P / 16) : job->tiles_q + (n16 + ppt16 - 1) / ppt16;
-    job->kind = 1; job->qbase = j; job->joined = __ldcg(&q.shared);
   }
   __syncthreads();
   // cost before each job
-  auto prefix = [&](const Job* list, int jobs, bool few, int64_t* base) -> int64_t {
+  const int private_blocks = (heads + kRows - 1) / kRows;
+  auto prefix = [&](int from, int jobs, bool few, int64_t* base) -> int64_t {
     int64_t before = 0;
     for (int j0 = 0; j0 < jobs; j0 += kPlanThreads) {
-      const int j = j0 + threadIdx.x;
+      const int j = j0 + threadIdx.x, at = from + j, tiles = j < jobs ? __ldcg(g.tiles + at) : 0;
       int64_t x = 0;
-      if (j < jobs && list[j].tiles > 0)
-        x = few ? few_cost(list[j].tiles) * a.Hkv : segment_cost(list[j].tiles) * a.Hkv * list[j].row_blocks;
+      if (tiles > 0)
+        x = few ? few_cost(tiles) * a.Hkv
+                : segment_cost(tiles) * a.Hkv * (at < g.groups ? __ldcg(&g.jobs[at].row_blocks) : private_blocks);
+      if (tiles < 0) atomicMin(&s_first_err, (at - g.groups) * 16 - tiles);
       int64_t y = x;
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t z = __shfl_up_sync(0xffffffffu, y, o);
@@ -226,8 +258,8 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(GroupArgs g) {
     return before;
   };
   const int jobs = g.few ? g.groups : g.groups + g.n;
-  const int64_t work = prefix(g.jobs, jobs, false, g.base);
-  const int64_t few_work = g.few ? prefix(g.jobs + g.groups, g.n, true, g.few_base) : 0;
+  const int64_t work = prefix(0, jobs, false, g.base);
+  const int64_t few_work = g.few ? prefix(g.groups, g.n, true, g.few_base) : 0;
   if (threadIdx.x == 0) {
     g.head->work = work;
     g.head->per = (work + g.ctas - 1) / g.ctas;
@@ -968,52 +1000,78 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __gr
 // ----------------------------------------------------------------------------- join --
 
 // One warp per (query, head): the parts of its row, at most one shared and one private
-// segment, each whole or in one piece per CTA.  Rows that read nothing become zero.
+// segment, each whole or in one piece per CTA (or warp).  A lane looks up one part; the parts'
+// rows are then read four at a time.
 template <int D>
 __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constant__ GroupArgs g) {
-  pdl_wait();
-  pdl_trigger();
+  constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, heads = g.a.Hq / g.a.Hkv;
   const int64_t at = blockIdx.x * 4ll + (threadIdx.x >> 5);
   if (at >= static_cast<int64_t>(g.n) * g.a.Hq) return;
   const int query = static_cast<int>(at / g.a.Hq), head = static_cast<int>(at % g.a.Hq), kvh = head / heads;
-  const QueryPlan& p = g.plan[query];
-  const bool reads = !p.err && p.mode != TRR_MODE_SKIP;
-  constexpr int E = D / 32;
+  pdl_wait();
+  pdl_trigger();
+  const int4 p = *reinterpret_cast<const int4*>(g.plan + query);  // reads, group, rank, shared
+  if (!p.x) return;
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  auto join = [&](float2 v, const float* row) {
-    if (v.x == -INFINITY) return;
-    const float next = fmaxf(m, v.x), f0 = m == -INFINITY ? 0.f : exp2_approx(m - next), f1 = exp2_approx(v.x - next);
-    l = l * f0 + v.y * f1;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f0 + row[lane * E + e] * f1;
-    m = next;
-  };
-  for (int kind = 0; kind < 2 && reads; ++kind) {
-    if (kind == 0 && !p.shared) continue;
-    const int j = kind == 0 ? p.group : g.groups + query;
-    const int tiles = g.jobs[j].tiles, blocks = g.jobs[j].row_blocks;
-    if (tiles == 0) continue;
-    const int rr = (kind == 0 ? p.rank * heads : 0) + head % heads;
-    const int64_t home = (static_cast<int64_t>(kind) * g.n + query) * g.a.Hq + head;
+#pragma unroll 1
+  for (int kind = p.w ? 0 : 1; kind < 2; ++kind) {
+    const int j = kind == 0 ? p.y : g.groups + query, tiles = g.tiles[j];
+    if (tiles <= 0) continue;
     const bool few = kind == 1 && g.few;
+    const int rr = (kind == 0 ? p.z * heads : 0) + head % heads;
     const int64_t cost = few ? few_cost(tiles) : segment_cost(tiles), share = few ? g.head->few_per : g.head->per;
-    const int64_t S = few ? g.few_base[query] + kvh * cost : g.base[j] + (static_cast<int64_t>(kvh) * blocks + rr / kRows) * cost;
-    for (int64_t c = S / share; c * share < S + cost; ++c) {
-      const int t0 = few ? few_before(c * share - S, tiles) : tiles_before(c * share - S, tiles);
-      const int t1 = few ? few_before((c + 1) * share - S, tiles) : tiles_before((c + 1) * share - S, tiles);
-      if (t0 >= t1) continue;
-      if (t1 - t0 == tiles) {
-        if (!g.jobs[j].joined) return;  // the row is in place
-        join(g.home_ml[home], g.home_o + home * D);
-      } else if (few) {
-        const int64_t slot = (2 * c + (t0 > 0 ? 0 : 1)) * kFewRows + rr;
-        join(g.few_ml[slot], g.few_o + slot * D);
-      } else {
-        const int64_t slot = (2 * c + (t0 > 0 ? 0 : 1)) * kRows + rr % kRows;
-        join(g.part_ml[slot], g.part_o + slot * D);
+    const int64_t S = few ? g.few_base[query] + kvh * cost
+                          : g.base[j] + (static_cast<int64_t>(kvh) * (kind == 0 ? g.jobs[j].row_blocks : (heads + kRows - 1) / kRows) + rr / kRows) * cost;
+    const int64_t last = S + cost - 1;
+    int64_t c0, c1;
+    if (last < 0x7fffffff) c0 = static_cast<uint32_t>(S) / static_cast<uint32_t>(share), c1 = static_cast<uint32_t>(last) / static_cast<uint32_t>(share);
+    else c0 = S / share, c1 = last / share;
+    const float2* mls = few ? g.few_ml : g.part_ml;
+    const float* rows = few ? g.few_o : g.part_o;
+    const int pitch = few ? kFewRows : kRows, sub = few ? rr : rr % kRows;
+    for (int64_t b = c0; b <= c1; b += 32) {
+      const int64_t x0 = (b + lane) * share - S, x1 = x0 + share;
+      const int t0 = few ? few_before(x0, tiles) : tiles_before(x0, tiles), t1 = few ? few_before(x1, tiles) : tiles_before(x1, tiles);
+      const bool there = b + lane <= c1 && t0 < t1;
+      int64_t slot = (2 * (b + lane) + (t0 > 0 ? 0 : 1)) * pitch + sub;
+      if (__any_sync(0xffffffffu, there && t1 - t0 == tiles)) {  // all of it in one part
+        if (!p.w) return;                                        // which is the row, in place
+        slot = (static_cast<int64_t>(kind) * g.n + query) * g.a.Hq + head;
+        mls = g.home_ml;
+        rows = g.home_o;
+      }
+      const float2 v = there ? mls[slot] : make_float2(-INFINITY, 0.f);
+      float top = v.x;
+      for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+      const float next = fmaxf(m, top);
+      if (next == -INFINITY) continue;
+      const float w = v.x == -INFINITY ? 0.f : exp2_approx(v.x - next), by = m == -INFINITY ? 0.f : exp2_approx(m - next);
+      float sum = v.x == -INFINITY ? 0.f : v.y * w;
+      for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+      l = l * by + sum;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= by;
+      m = next;
+      unsigned parts = __ballot_sync(0xffffffffu, v.x != -INFINITY);
+      while (parts) {
+        float row[4][E], f[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int from = parts ? __ffs(parts) - 1 : 0;
+          const int64_t s = __shfl_sync(0xffffffffu, slot, from);
+          f[u] = __shfl_sync(0xffffffffu, w, from);
+          if (!parts) f[u] = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) row[u][e] = parts ? rows[s * D + lane * E + e] : 0.f;
+          parts &= parts - 1;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] += row[u][e] * f[u];
       }
     }
   }
@@ -1043,6 +1101,7 @@ static int64_t lay_workspace(GroupArgs* g, uint8_t* b, const Layout& l, int n, i
   g->plan = reinterpret_cast<QueryPlan*>(take(static_cast<int64_t>(sizeof(QueryPlan)) * n));
   g->list = reinterpret_cast<int32_t*>(take(4ll * n));
   g->jobs = reinterpret_cast<Job*>(take(static_cast<int64_t>(sizeof(Job)) * 2 * n));
+  g->tiles = reinterpret_cast<int32_t*>(take(4ll * 2 * n));
   g->base = reinterpret_cast<int64_t*>(take(8ll * (2 * n + 1)));
   g->home_ml = reinterpret_cast<float2*>(take(8 * 2 * rows));
   g->home_o = reinterpret_cast<float*>(take(4 * 2 * rows * l.d));

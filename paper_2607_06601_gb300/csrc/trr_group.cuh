@@ -28,15 +28,13 @@ struct Job {
 };
 static_assert(sizeof(Job) == 128, "a warp loads a job one word per lane");
 
-// One query, as the plan sees it.
+// One query, as the join needs it.
 struct QueryPlan {
-  int err, mode, group, member;           // member: a full query in a group
-  int seq, t, lo, rank;
+  int reads;                              // 0: its rows are in place
+  int group, rank, shared;                // its group's shared job, its place among that job's queries, whether it is one of them
   int common[kClasses];                   // leading pages that it shares with its group's first full query and sees whole
-  int head[kClasses], first[kClasses], end[kClasses];
-  int shared, pad[7];                     // shared: its row is in its group's shared job
 };
-static_assert(sizeof(QueryPlan) == 128, "");
+static_assert(sizeof(QueryPlan) == 32, "two 16-byte loads");
 
 struct GroupHeader {
   int64_t work, per;          // cost of the tensor kernel's segments, a CTA's share
@@ -58,6 +56,7 @@ struct GroupArgs {
   QueryPlan* plan;
   int32_t* list;      // [n] a group's rows: its full queries in order, from the group's offset on
   Job* jobs;          // [groups] shared, then [n] private
+  int32_t* tiles;     // [jobs] tiles (or blocks) of each job; minus the error of a query in error
   int64_t* base;      // [jobs + 1] cost before each job
   float2* home_ml;    // [2][n][Hq] (m, l) of a row of a whole segment, by kind of job
   float* home_o;      // [2][n][Hq][D]

@@ -16,18 +16,11 @@
 //                         is spread over many CTAs and a CTA takes many short ones.
 //   group_combine_kernel  joins the parts of every row.
 //
-// In the attention kernel a producer warp brings each tile's page slices into a ring of shared
-// memory with bulk copies; eight warps expand them to 16-bit rows in the tensor core's layout;
-// one thread issues the products S = Q K^T and O += P V (tcgen05, sums in TMEM); four warps do
-// the softmax, one row of TMEM per thread.  Pages of 2, 4 and 8 bits become binary16 (z + c s
-// rounded once, 11 bits), pages of 16 bits stay bf16; p is rounded to the same type, sums and
-// statistics are binary32.  A segment of 64 or 32 rows or fewer fills the 128 lanes with two or
-// four copies of its rows, each of which takes its own part of a tile's tokens, so that all
-// four warps share the exponentials.
 #include <algorithm>
 #include <climits>
 
 #include "trr_few.cuh"
+#include "trr_group_tc.cuh"
 
 namespace trr {
 
@@ -268,733 +261,6 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     g.head->jobs = jobs;
     if (s_first_err != INT_MAX) set_status(a.ctrl, s_first_err % 16);
   }
-}
-
-// ------------------------------------------------------------------------- attention --
-
-// A segment, or a CTA's piece of one, as the softmax warps need it.
-struct Segment {
-  int tiles;          // 0: no more
-  int row0, rows;     // its rows in the job, at most 128
-  int kind, qbase, kvh;
-  int dest;           // -2: the output row, -1: the home row, else the piece's slot
-  int pad;
-};
-
-struct RawPage {
-  int off, pos;       // slice and slot positions in the ring; pos < 0: every token in sight
-  int valid, cls;     // slots that hold a token
-};
-struct RawTile {
-  int pages, bf16, first, end;
-  int lo, t, sinks, pad;
-  RawPage page[kTileKeys / 16];
-};
-struct TileMeta {
-  int keys, bf16, first, end;
-  uint32_t mask[4];   // tokens in sight
-};
-
-template <int D>
-struct GroupSmem {
-  static constexpr int kStages = D == 64 ? 3 : 2;      // expanded tiles
-  static constexpr int kTile = kTileKeys * D * 2;      // bytes of K or V of one
-  static constexpr int kScratch = kStages * 2 * kTile; // merge of row copies: [128][33] floats, then (m, l)
-  static constexpr int kMl = kScratch + kRows * 33 * 4;
-  static constexpr int kRaw = kMl + kRows * 8;
-  static constexpr int kSeg = kRaw + kRawSlots * static_cast<int>(sizeof(RawTile));
-  static constexpr int kMeta = kSeg + kSegSlots * static_cast<int>(sizeof(Segment));
-  static constexpr int kBars = kMeta + kStages * static_cast<int>(sizeof(TileMeta));
-  static constexpr int kNumBars = 2 * kRawSlots + 2 * kSegSlots + 2 * kStages + 2 + 2 + 5;
-  static constexpr int kRing = (kBars + kNumBars * 8 + 16 + 127) / 128 * 128;
-  static constexpr int kTotal = 225 * 1024;  // of the 227 KB a CTA may have; 1 KB aligns the base
-  static constexpr int kRingBytes = (kTotal - kRing) / 128 * 128;
-};
-
-template <int D>
-struct Ctx {
-  using L = GroupSmem<D>;
-  uint8_t* base;  // 1024-byte aligned
-  uint32_t tmem;
-  uint64_t wait_ns;
-  volatile int* abort_flag;
-  __device__ uint64_t* bar(int i) const { return reinterpret_cast<uint64_t*>(base + L::kBars) + i; }
-  __device__ uint64_t* raw_full(int i) const { return bar(i); }
-  __device__ uint64_t* raw_empty(int i) const { return bar(kRawSlots + i); }
-  __device__ uint64_t* seg_full(int i) const { return bar(2 * kRawSlots + i); }
-  __device__ uint64_t* seg_empty(int i) const { return bar(2 * kRawSlots + kSegSlots + i); }
-  __device__ uint64_t* kv_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + i); }
-  __device__ uint64_t* kv_empty(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + L::kStages + i); }
-  __device__ uint64_t* s_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + 2 * L::kStages + i); }
-  __device__ uint64_t* p_full(int i) const { return s_full(2 + i); }
-  __device__ uint64_t* o_done(int i) const { return s_full(4 + i); }
-  __device__ uint64_t* q_full() const { return s_full(6); }
-  __device__ uint64_t* drained() const { return s_full(7); }
-  __device__ uint64_t* merged() const { return s_full(8); }
-  __device__ RawTile& raw(int i) const { return reinterpret_cast<RawTile*>(base + L::kRaw)[i]; }
-  __device__ Segment& seg(int i) const { return reinterpret_cast<Segment*>(base + L::kSeg)[i]; }
-  __device__ TileMeta& meta(int i) const { return reinterpret_cast<TileMeta*>(base + L::kMeta)[i]; }
-  __device__ uint32_t tile(int stage, int which) const { return smem_u32(base) + (2 * stage + which) * L::kTile; }
-  // A bounded wait; once one has given up, none waits any more.
-  __device__ bool wait(uint64_t* b, uint32_t parity) const {
-    if (mbar_poll(smem_u32(b), parity, wait_ns)) return true;
-    const uint64_t t0 = global_ns();
-    while (!mbar_poll(smem_u32(b), parity, wait_ns)) {
-      if (*abort_flag || global_ns() - t0 >= wait_ns) {
-        *abort_flag = 1;
-        return false;
-      }
-    }
-    return true;
-  }
-  // The same by a whole warp: all of its lanes get the same answer.
-  __device__ bool wait_warp(uint64_t* b, uint32_t parity) const { return __all_sync(0xffffffffu, wait(b, parity)); }
-};
-
-constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // TMEM columns: O, two S (P over S), Q in binary16 and bf16
-
-// The producer warp: segments and tiles of this CTA's run, and the copies of their pages.
-template <int D>
-__device__ void group_produce(const GroupArgs& g, const Ctx<D>& x, int lane) {
-  using L = GroupSmem<D>;
-  const LayerArgs& a = g.a;
-  const int64_t per = g.head->per, work = g.head->work;
-  const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
-  const int jobs = g.head->jobs, P = a.P;
-  int it = 0, freed = 0;           // tiles pushed, tiles whose ring bytes are known to be free
-  int ring_head = 0, my_start = 0; // lane s: where slot s's tile starts
-  int segs = 0;
-  bool ok = true;
-
-  // room for `need` bytes and a record; the offset in the ring
-  auto book = [&](int need) -> int {
-    for (;;) {
-      if (it - freed < kRawSlots) {
-        if (it == freed) { ring_head = need; return 0; }
-        const int tail = __shfl_sync(0xffffffffu, my_start, freed % kRawSlots);
-        if (ring_head > tail) {
-          if (ring_head + need <= L::kRingBytes) { ring_head += need; return ring_head - need; }
-          if (need < tail) { ring_head = need; return 0; }
-        } else if (ring_head + need < tail) {
-          ring_head += need;
-          return ring_head - need;
-        }
-      }
-      if (!x.wait_warp(x.raw_empty(freed % kRawSlots), (freed / kRawSlots) & 1)) return -1;
-      ++freed;
-    }
-  };
-
-  if (b0 < b1) {
-    // the job that holds cost b0: the last one that starts at or before it
-    int lo = 0, hi = jobs;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && g.base[i] <= b0));
-      const int last = lo + (k - 1) * step;
-      hi = min(hi, last + step);
-      lo = last;
-      if (step == 1) break;
-    }
-    for (int j = lo; j < jobs && ok; ++j) {
-      const int64_t jbase = g.base[j];
-      if (jbase >= b1) break;
-      const int w = reinterpret_cast<const int*>(g.jobs + j)[lane];
-      auto field = [&](int i) { return __shfl_sync(0xffffffffu, w, i); };
-      const int tiles = field(19);
-      if (tiles == 0) continue;
-      const int seq = field(0), jlo = field(1), jt = field(2), sinks = field(3);
-      int head[kClasses], first[kClasses], upto[kClasses + 1];
-      upto[0] = 0;
-      for (int c = 0; c < kClasses; ++c) {
-        head[c] = field(4 + c);
-        first[c] = field(8 + c);
-        upto[c + 1] = upto[c] + head[c] + field(12 + c);
-      }
-      const int rows = field(16), row_blocks = field(17), tiles_q = field(18), kind = field(20), qbase = field(21), joined = field(22);
-      const int nt = lane < kClasses ? a.ntok[static_cast<int64_t>(seq) * kClasses + lane] : 0;
-      const int64_t cost = segment_cost(tiles);
-      const int nsegs = a.Hkv * row_blocks;
-      for (int s = static_cast<int>(max(static_cast<int64_t>(0), (b0 - jbase) / cost)); s < nsegs && ok; ++s) {
-        const int64_t S = jbase + s * cost;
-        if (S >= b1) break;
-        const int t0 = tiles_before(b0 - S, tiles), t1 = tiles_before(b1 - S, tiles);
-        if (t0 >= t1) continue;
-        const int kvh = s / row_blocks, rb = s % row_blocks;
-        ok = x.wait_warp(x.seg_empty(segs % kSegSlots), ((segs / kSegSlots) & 1) ^ 1);
-        if (!ok) break;
-        if (lane == 0) {
-          Segment& sg = x.seg(segs % kSegSlots);
-          sg.tiles = t1 - t0;
-          sg.row0 = rb * kRows;
-          sg.rows = min(kRows, rows - rb * kRows);
-          sg.kind = kind; sg.qbase = qbase; sg.kvh = kvh;
-          sg.dest = t1 - t0 == tiles ? (joined ? -1 : -2) : 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
-          mbar_arrive(x.seg_full(segs % kSegSlots));
-        }
-        ++segs;
-        // batches of 32 pages, one per lane, of the 2-, 4- and 8-bit pages, then of the others
-        int batch = -1, page = 0, cls = 0, valid = 0;
-        bool whole = true;
-        for (int tile = t0; tile < t1 && ok; ++tile) {
-          const bool wide = tile >= tiles_q;
-          const int ppt = (wide ? kTileKeys / 2 : kTileKeys) / P;
-          const int i0 = (wide ? tile - tiles_q : tile) * ppt, end = wide ? upto[4] - upto[3] : upto[3];
-          const int b = (wide ? 1 << 28 : 0) + i0 / 32;
-          if (b != batch) {
-            batch = b;
-            const int i = i0 / 32 * 32 + lane;
-            cls = wide ? 3 : i >= upto[2] ? 2 : i >= upto[1] ? 1 : 0;
-            const int in = wide ? i : i - upto[cls];
-            int h = head[0], f = first[0], n = __shfl_sync(0xffffffffu, nt, 0);
-#pragma unroll
-            for (int c = 1; c < kClasses; ++c) {
-              const int m = __shfl_sync(0xffffffffu, nt, c);
-              if (cls == c) h = head[c], f = first[c], n = m;
-            }
-            if (i < end) {
-              const int k = in < h ? in : f + in - h;
-              const int64_t at = (static_cast<int64_t>(seq) * kClasses + cls) * a.MP + k;
-              page = a.pt[at];
-              const int pf = a.pfirst[at], pl = a.plast[at];
-              valid = min(P, n - k * P);
-              whole = valid == P && pl <= jt && (pf >= jlo || pl < sinks);
-            }
-          }
-          const int pages = min(ppt, end - i0), l0 = i0 % 32;
-          const bool mine = lane >= l0 && lane < l0 + pages;
-          const int slice = cls == 0 ? a.slice[0] : cls == 1 ? a.slice[1] : cls == 2 ? a.slice[2] : a.slice[3];
-          const int room = mine ? (slice + 127) / 128 * 128 + (whole ? 0 : (4 * P + 127) / 128 * 128) : 0;
-          int off = room;
-          for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, off, o);
-            if (lane >= o) off += y;
-          }
-          const int need = __shfl_sync(0xffffffffu, off, 31);
-          const int bytes = __reduce_add_sync(0xffffffffu, mine ? slice + (whole ? 0 : 4 * P) : 0);
-          const int at = book(need);
-          if (at < 0) { ok = false; break; }
-          const int slot = it % kRawSlots;
-          if (lane == slot) my_start = at;
-          off += at - room;
-          RawTile& r = x.raw(slot);
-          if (mine) r.page[lane - l0] = RawPage{off, whole ? -1 : off + (slice + 127) / 128 * 128, valid, cls};
-          if (lane == 0) {
-            r.pages = pages; r.bf16 = wide; r.first = tile == t0; r.end = 0;
-            r.lo = jlo; r.t = jt; r.sinks = sinks;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive_expect_tx(x.raw_full(slot), bytes);
-          __syncwarp();
-          if (mine) {
-            const uint8_t* pool = cls == 0 ? a.pool[0] : cls == 1 ? a.pool[1] : cls == 2 ? a.pool[2] : a.pool[3];
-            const int64_t pb = cls == 0 ? a.page_bytes[0] : cls == 1 ? a.page_bytes[1] : cls == 2 ? a.page_bytes[2] : a.page_bytes[3];
-            const uint8_t* src = pool + page * pb;
-            bulk_g2s(x.base + L::kRing + off, src + a.hdr + static_cast<int64_t>(kvh) * slice, slice, x.raw_full(slot));
-            if (!whole) bulk_g2s(x.base + L::kRing + off + (slice + 127) / 128 * 128, src, 4 * P, x.raw_full(slot));
-          }
-          ++it;
-        }
-      }
-    }
-  }
-  if (ok) {  // no more tiles, no more segments
-    ok = x.wait_warp(x.seg_empty(segs % kSegSlots), ((segs / kSegSlots) & 1) ^ 1);
-    if (ok && lane == 0) {
-      x.seg(segs % kSegSlots).tiles = 0;
-      mbar_arrive(x.seg_full(segs % kSegSlots));
-    }
-    if (ok && book(0) >= 0) {
-      if (lane == 0) {
-        x.raw(it % kRawSlots).end = 1;
-        mbar_arrive(x.raw_full(it % kRawSlots));
-      }
-      ++it;
-    }
-  }
-  // the CTA stays until its copies have landed
-  for (int k = max(0, it - kRawSlots); k < it; ++k) mbar_wait(x.raw_full(k % kRawSlots), (k / kRawSlots) & 1);
-}
-
-// z + c s of eight codes, given as four words of two binary16 values 1024 + c, rounded once.
-template <bool CLAMP>
-__device__ __forceinline__ uint4 expand8(uint32_t p0, uint32_t p1, uint32_t p2, uint32_t p3, __half2 s, __half2 z) {
-  const __half2 k = as_half2(0x64006400u);  // 1024: the difference is exact
-  __half2 v[4] = {__hfma2(__hsub2(as_half2(p0), k), s, z), __hfma2(__hsub2(as_half2(p1), k), s, z),
-                  __hfma2(__hsub2(as_half2(p2), k), s, z), __hfma2(__hsub2(as_half2(p3), k), s, z)};
-  if (CLAMP) {  // a value that rounds past 65504 stays finite
-    const __half2 top = as_half2(0x7BFF7BFFu), low = as_half2(0xFBFFFBFFu);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __hmax2(__hmin2(v[i], top), low);
-  }
-  return make_uint4(as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3]));
-}
-
-// Chunk e (8 elements) of row `key` of an expanded tile.
-template <int D>
-__device__ __forceinline__ uint8_t* tile_chunk(uint8_t* tile, int key, int e) {
-  return tile + (e >> 3) * (kTileKeys * 128) + key * 128 + (((e ^ key) & 7) << 4);
-}
-
-// Expands one row of a 2-, 4- or 8-bit page: K or V (which) of slot `slot` of the slice at sl.
-template <int D, int B, bool CLAMP>
-__device__ __forceinline__ void expand_row(const uint8_t* sl, int which, int slot, int P, int lg_group, bool swz, int lane,
-                                           uint8_t* tile, int key) {
-  constexpr int kRow = D * B / 8, kN = kRow / 16;  // bytes and 16-byte chunks of a row
-  constexpr int kPer = 128 / B;                    // elements of a chunk
-  const int ng = D >> lg_group;
-  const uint32_t* sz = reinterpret_cast<const uint32_t*>(sl + 2 * P * kRow) + (which * P + slot) * ng;
-  const int row = (which * P + slot) * kRow;
-#pragma unroll
-  for (int i = 0; i < kN; ++i) {
-    // rows of 128 bytes in a plain order: each lane starts at its own chunk, so that eight lanes read eight banks
-    const int j = kN == 8 && !swz ? (i + lane) & 7 : i;
-    const int o = row + 16 * j;
-    const uint4 raw = *reinterpret_cast<const uint4*>(sl + (B == 8 && swz ? static_cast<int>(swz_off(o)) : o));
-    const uint32_t word[4] = {raw.x, raw.y, raw.z, raw.w};
-    uint32_t szw = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int el = j * kPer + q * (kPer / 4);  // the word's first element
-      if (q == 0 || (kPer == 64 && q == 2)) szw = sz[el >> lg_group];  // a group holds 32 elements or more
-      const __half2 s = as_half2(__byte_perm(szw, 0, 0x1010)), z = as_half2(__byte_perm(szw, 0, 0x3232));
-      const uint32_t w = word[q];
-      if (B == 8) {
-        if (q & 1) continue;
-        const uint32_t w2 = word[q | 1];
-        *reinterpret_cast<uint4*>(tile_chunk<D>(tile, key, el >> 3)) =
-            expand8<CLAMP>(__byte_perm(w, 0x64646464u, 0x4140), __byte_perm(w, 0x64646464u, 0x4342),
-                           __byte_perm(w2, 0x64646464u, 0x4140), __byte_perm(w2, 0x64646464u, 0x4342), s, z);
-      } else if (B == 4) {
-        uint32_t t[4];  // elements k and k + 4
-#pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = ((w >> (4 * k)) & 0x000F000Fu) | 0x64006400u;
-        *reinterpret_cast<uint4*>(tile_chunk<D>(tile, key, el >> 3)) =
-            expand8<CLAMP>(__byte_perm(t[0], t[1], 0x5410), __byte_perm(t[2], t[3], 0x5410), __byte_perm(t[0], t[1], 0x7632),
-                           __byte_perm(t[2], t[3], 0x7632), s, z);
-      } else {
-        uint32_t t[8];  // elements k and k + 8
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = ((w >> (2 * k)) & 0x00030003u) | 0x64006400u;
-        *reinterpret_cast<uint4*>(tile_chunk<D>(tile, key, el >> 3)) =
-            expand8<CLAMP>(__byte_perm(t[0], t[1], 0x5410), __byte_perm(t[2], t[3], 0x5410), __byte_perm(t[4], t[5], 0x5410),
-                           __byte_perm(t[6], t[7], 0x5410), s, z);
-        *reinterpret_cast<uint4*>(tile_chunk<D>(tile, key, (el >> 3) + 1)) =
-            expand8<CLAMP>(__byte_perm(t[0], t[1], 0x7632), __byte_perm(t[2], t[3], 0x7632), __byte_perm(t[4], t[5], 0x7632),
-                           __byte_perm(t[6], t[7], 0x7632), s, z);
-      }
-    }
-  }
-}
-
-// Whether a group's largest level rounds past binary16's largest value.
-template <int D, int B>
-__device__ __forceinline__ bool level_overflows(const uint8_t* sl, int which, int slot, int P, int lg_group) {
-  const int ng = D >> lg_group;
-  const uint32_t* sz = reinterpret_cast<const uint32_t*>(sl + 2 * P * (D * B / 8)) + (which * P + slot) * ng;
-  bool over = false;
-  for (int i = 0; i < ng; ++i) {
-    const __half2 h = as_half2(sz[i]);
-    const float top = static_cast<float>((1 << B) - 1) * __low2float(h) + __high2float(h);
-    over |= !(fabsf(top) < 65504.f);
-  }
-  return over;
-}
-
-template <int D, int B>
-__device__ __forceinline__ void expand(const uint8_t* sl, int which, int slot, int P, int lg_group, bool swz, int lane, uint8_t* tile,
-                                       int key) {
-  if (level_overflows<D, B>(sl, which, slot, P, lg_group)) expand_row<D, B, true>(sl, which, slot, P, lg_group, swz, lane, tile, key);
-  else expand_row<D, B, false>(sl, which, slot, P, lg_group, swz, lane, tile, key);
-}
-
-// The expanding warps: warps 0-3 write K, 4-7 V; a thread has one token of the tile.
-template <int D>
-__device__ void group_expand(const GroupArgs& g, const Ctx<D>& x, int warp, int lane) {
-  using L = GroupSmem<D>;
-  const LayerArgs& a = g.a;
-  const int which = warp >> 2, key = (warp & 3) * 32 + lane, P = a.P, lg_p = __ffs(P) - 1, lg_group = __ffs(a.G) - 1;
-  const bool swz = a.swz;
-  for (int it = 0;; ++it) {
-    const int slot = it % kRawSlots, stage = it % L::kStages;
-    if (!x.wait_warp(x.raw_full(slot), (it / kRawSlots) & 1)) return;
-    if (!x.wait_warp(x.kv_empty(stage), ((it / L::kStages) & 1) ^ 1)) return;
-    const RawTile& r = x.raw(slot);
-    TileMeta& m = x.meta(stage);
-    const bool end = r.end;
-    if (!end) {
-      const int keys = r.pages << lg_p;
-      const bool in = key < keys;
-      const RawPage pg = r.page[in ? key >> lg_p : 0];
-      const int at = key & (P - 1);
-      const uint8_t* ring = x.base + L::kRing;
-      bool seen = in;
-      if (in && pg.pos >= 0) {
-        const int pos = reinterpret_cast<const int32_t*>(ring + pg.pos)[at];
-        seen = at < pg.valid && pos <= r.t && (pos >= r.lo || pos < r.sinks);
-      }
-      const unsigned mask = __ballot_sync(0xffffffffu, seen);
-      if (which == 0 && lane == 0) m.mask[warp & 3] = mask;
-      if (warp == 0 && lane == 0) m.keys = keys, m.bf16 = r.bf16, m.first = r.first, m.end = 0;
-      uint8_t* tile = x.base + (2 * stage + which) * L::kTile;
-      if (r.bf16) {  // rows copied 16 bytes at a time, consecutive lanes along a row
-        constexpr int kN = D / 8;
-#pragma unroll 4
-        for (int i = 0; i < kN; ++i) {
-          const int row = (i * 32 + lane) / kN, e = (i * 32 + lane) % kN, k = (warp & 3) * 32 + row;
-          if (k < keys) {
-            uint4 v = make_uint4(0, 0, 0, 0);  // a V row out of sight is zero: its weight of 0 times infinity would not be
-            if (which == 0 || (mask >> row & 1)) {
-              const int o = (which * P + (k & (P - 1))) * D * 2 + 16 * e;
-              v = *reinterpret_cast<const uint4*>(ring + r.page[k >> lg_p].off + (swz ? static_cast<int>(swz_off(o)) : o));
-            }
-            *reinterpret_cast<uint4*>(tile_chunk<D>(tile, k, e)) = v;
-          }
-        }
-      } else if (in) {
-        if (which == 1 && !seen) {
-          for (int e = 0; e < D / 8; ++e) *reinterpret_cast<uint4*>(tile_chunk<D>(tile, key, e)) = make_uint4(0, 0, 0, 0);
-        } else {
-          const uint8_t* sl = ring + pg.off;
-          if (pg.cls == 0) expand<D, 2>(sl, which, at, P, lg_group, swz, lane, tile, key);
-          else if (pg.cls == 1) expand<D, 4>(sl, which, at, P, lg_group, swz, lane, tile, key);
-          else expand<D, 8>(sl, which, at, P, lg_group, swz, lane, tile, key);
-        }
-      }
-      fence_proxy_async_smem();
-    } else if (warp == 0 && lane == 0) {
-      m.end = 1;
-    }
-    __syncwarp();
-    if (lane == 0) {
-      mbar_arrive(x.raw_empty(slot));
-      mbar_arrive(x.kv_full(stage));
-    }
-    if (end) return;
-  }
-}
-
-// The thread that issues the products.  Tile it's scores are issued before tile it-1's P V, so
-// that the tensor core works while the softmax does.
-template <int D>
-__device__ void group_mma(const Ctx<D>& x) {
-  using L = GroupSmem<D>;
-  int segs = 0, keys_before = 0;
-  bool bf16_before = false, first_before = false, pending = false;
-  auto pv = [&](int it) -> bool {  // O += P V of tile it
-    if (!x.wait(x.p_full(it & 1), (it >> 1) & 1)) return false;
-    tc_fence_after();
-    const uint32_t id = tc_idesc(bf16_before, D, true);
-    const uint64_t d = tc_desc(x.tile(it % L::kStages, 1), kTileKeys * 128);
-    for (int k = 0; k < keys_before / 16; ++k)
-      tc_mma(x.tmem + kColO, x.tmem + kColS + 128 * (it & 1) + 8 * k, d + k * (2048 >> 4), id, !(first_before && k == 0));
-    tc_commit(x.kv_empty(it % L::kStages));
-    tc_commit(x.o_done(it & 1));
-    pending = false;
-    return true;
-  };
-  for (int it = 0;; ++it) {
-    const int stage = it % L::kStages;
-    if (!x.wait(x.kv_full(stage), (it / L::kStages) & 1)) break;
-    const TileMeta& m = x.meta(stage);
-    if (m.end) {
-      if (pending) pv(it - 1);
-      break;
-    }
-    const int keys = m.keys;
-    const bool bf16 = m.bf16, first = m.first;
-    if (it >= 2 && !x.wait(x.o_done(it & 1), ((it - 2) >> 1) & 1)) break;  // tile it-2's weights, under the new scores, have been used
-    if (first) {
-      if (pending && !pv(it - 1)) break;
-      if (!x.wait(x.q_full(), segs & 1)) break;
-      ++segs;
-    }
-    tc_fence_after();
-    const uint32_t id = tc_idesc(bf16, keys, false);
-    const uint32_t qcol = x.tmem + kColQ + (bf16 ? 64 : 0);
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k)
-      tc_mma(x.tmem + kColS + 128 * (it & 1), qcol + 8 * k,
-             tc_desc(x.tile(stage, 0) + (k >> 2) * (kTileKeys * 128) + (k & 3) * 32, 16), id, k > 0);
-    tc_commit(x.s_full(it & 1));
-    if (pending && !pv(it - 1)) break;
-    pending = true;
-    keys_before = keys; bf16_before = bf16; first_before = first;
-  }
-  tc_commit(x.drained());  // nothing is in flight when the CTA ends
-  mbar_wait(x.drained(), 0);
-}
-
-template <int D>
-__device__ void group_softmax(const GroupArgs& g, const Ctx<D>& x, int warp, int lane) {
-  using L = GroupSmem<D>;
-  const int tid = warp * 32 + lane, heads = g.a.Hq / g.a.Hkv;
-  const uint32_t lanes = x.tmem + (static_cast<uint32_t>(warp) << 21);  // this warp's 32 lanes
-  float* scratch = reinterpret_cast<float*>(x.base + L::kScratch);
-  float2* ml = reinterpret_cast<float2*>(x.base + L::kMl);
-  uint32_t meets = 0;
-  auto meet = [&]() -> bool {  // the softmax warps wait for one another (bounded, unlike a CTA barrier)
-    mbar_arrive(x.merged());
-    return x.wait_warp(x.merged(), meets++ & 1);
-  };
-
-  // (query, head) of row r of a segment
-  auto row_of = [&](const Segment& sg, int r, int* query, int* head) {
-    const int rr = sg.row0 + r;
-    *query = sg.kind == 0 ? g.list[sg.qbase + rr / heads] : sg.qbase;
-    *head = sg.kvh * heads + rr % heads;
-  };
-  // Q of a segment into TMEM; the row's factor from products to base-2 exponents.  Each row is
-  // scaled by a power of two that brings its largest element to [1, 2): binary16 then holds
-  // what it needs of it.
-  float factor = 0.f;
-  auto load_q = [&](const Segment& sg, int copies) {
-    const int r = tid & (kRows / copies - 1);
-    uint32_t w[D / 2];
-    uint32_t top = 0;
-    if (r < sg.rows) {
-      int query, head;
-      row_of(sg, r, &query, &head);
-      const uint4* src = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(query) * g.a.Hq + head) * D);
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        const uint4 u = src[i];
-        w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
-      }
-#pragma unroll
-      for (int i = 0; i < D / 2; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
-    } else {
-#pragma unroll
-      for (int i = 0; i < D / 2; ++i) w[i] = 0;
-    }
-    int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
-    e = max(-100, min(120, e));
-    const float down = __int_as_float((127 - e) << 23);
-    factor = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
-#pragma unroll
-    for (int half = 0; half < D / 64; ++half) {
-      uint32_t o[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        o[i] = as_u32(__floats2half2_rn(bf16lo(w[32 * half + i]) * down, bf16hi(w[32 * half + i]) * down));
-      tmem_st32(lanes + kColQ + 32 * half, o);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(bf16lo(w[32 * half + i]) * down, bf16hi(w[32 * half + i]) * down);
-        o[i] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-      tmem_st32(lanes + kColQ + 64 + 32 * half, o);
-    }
-    tmem_wait_st();
-    tc_fence_before();
-    mbar_arrive(x.q_full());
-  };
-  auto copies_of = [](int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; };
-
-  int it = 0, segs = 0;
-  if (!x.wait_warp(x.seg_full(0), 0)) return;
-  Segment sg = x.seg(0);
-  int copies = copies_of(sg.rows);
-  if (sg.tiles > 0) load_q(sg, copies);
-  while (sg.tiles > 0) {
-    const int chunks = 4 / copies, chunk0 = copies == 1 ? 0 : copies == 2 ? (warp >> 1) * 2 : warp;  // this warp's 32-token chunks
-    const float f = factor;
-    float m = -INFINITY, l = 0.f;
-    for (int tile = 0; tile < sg.tiles; ++tile, ++it) {
-      const int stage = it % L::kStages;
-      if (!x.wait_warp(x.kv_full(stage), (it / L::kStages) & 1)) return;
-      const TileMeta& meta = x.meta(stage);
-      const int keys = meta.keys;
-      const bool bf16 = meta.bf16;
-      if (!x.wait_warp(x.s_full(it & 1), (it >> 1) & 1)) return;
-      tc_fence_after();
-      const uint32_t scol = lanes + kColS + 128 * (it & 1);
-      float top = -INFINITY;
-      for (int c = chunk0; c < chunk0 + chunks; ++c) {
-        const uint32_t mask = 32 * c < keys ? meta.mask[c] : 0;
-        if (mask == 0) continue;
-        uint32_t s[32];
-        tmem_ld32(s, scol + 32 * c);
-        if (mask == 0xffffffffu) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (mask >> i & 1) top = fmaxf(top, __uint_as_float(s[i]));
-        }
-      }
-      top *= f;
-      // m follows the maximum only when that has grown by more than 2^8: p stays within binary16, and O is rarely rescaled
-      if (__any_sync(0xffffffffu, top > m + 8.f)) {
-        const float next = fmaxf(m, top), by = m == -INFINITY ? 0.f : exp2_approx(m - next);
-        l *= by;
-        m = next;
-        if (tile > 0) {
-          if (!x.wait_warp(x.o_done((it - 1) & 1), ((it - 1) >> 1) & 1)) return;
-          tc_fence_after();
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(o, lanes + kColO + 32 * c);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
-            tmem_st32(lanes + kColO + 32 * c, o);
-          }
-        }
-      }
-      const float shift = m == -INFINITY ? 0.f : -m;
-      for (int c = 0; c < 4 && 32 * c < keys; ++c) {
-        uint32_t p[16];
-        const uint32_t mask = c >= chunk0 && c < chunk0 + chunks ? meta.mask[c] : 0;
-        if (mask == 0) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) p[i] = 0;
-        } else {
-          uint32_t s[32];
-          tmem_ld32(s, scol + 32 * c);
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            float p0 = exp2_approx(fmaf(__uint_as_float(s[i]), f, shift)), p1 = exp2_approx(fmaf(__uint_as_float(s[i + 1]), f, shift));
-            if (mask != 0xffffffffu) {
-              if (!(mask >> i & 1)) p0 = 0.f;
-              if (!(mask >> (i + 1) & 1)) p1 = 0.f;
-            }
-            l += p0 + p1;
-            if (bf16) {
-              const __nv_bfloat162 b = __floats2bfloat162_rn(p0, p1);
-              p[i / 2] = *reinterpret_cast<const uint32_t*>(&b);
-            } else {
-              p[i / 2] = as_u32(__floats2half2_rn(p0, p1));
-            }
-          }
-        }
-        tmem_st16(scol + 16 * c, p);  // over scores that have been read
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(x.p_full(it & 1));
-    }
-    // the next segment's rows go in while this one's last product runs
-    const Segment done = sg;
-    const int done_copies = copies;
-    ++segs;
-    if (!x.wait_warp(x.seg_full(segs % kSegSlots), (segs / kSegSlots) & 1)) return;
-    sg = x.seg(segs % kSegSlots);
-    copies = copies_of(sg.rows);
-    if (sg.tiles > 0) load_q(sg, copies);
-    if (!x.wait_warp(x.o_done((it - 1) & 1), ((it - 1) >> 1) & 1)) return;
-    tc_fence_after();
-
-    // rows out: the output itself, or (m, l, o) for the join
-    const int width = kRows / done_copies;
-    float weight = 1.f, sum = l, high = m;
-    if (done_copies > 1) {
-      ml[tid] = make_float2(m, l);
-      if (!meet()) return;
-      high = -INFINITY;
-      for (int k = 0; k < done_copies; ++k) high = fmaxf(high, ml[(tid & (width - 1)) + k * width].x);
-      sum = 0.f;
-      for (int k = 0; k < done_copies; ++k) {
-        const float2 v = ml[(tid & (width - 1)) + k * width];
-        if (v.x != -INFINITY) sum += v.y * exp2_approx(v.x - high);
-      }
-      weight = m == -INFINITY ? 0.f : exp2_approx(m - high);
-      if (!meet()) return;
-      if (tid < width) ml[tid] = make_float2(high, sum);
-      if (!meet()) return;
-    }
-    // thread -> row and columns of each 32 that it writes
-    const int r = tid / done_copies, cols = 32 / done_copies, c0 = (tid % done_copies) * cols;
-    int query = 0, head = 0;
-    float2 mine = make_float2(high, sum);
-    if (done_copies > 1) mine = ml[r];
-    const bool live = r < done.rows;
-    if (live) row_of(done, r, &query, &head);
-    const int64_t home = (static_cast<int64_t>(done.kind) * g.n + query) * g.a.Hq + head;
-    float* to = done.dest >= 0 ? g.part_o + (static_cast<int64_t>(done.dest) * kRows + r) * D : g.home_o + home * D;
-    uint16_t* out = g.out + (static_cast<int64_t>(query) * g.a.Hq + head) * D;
-    const float inv = mine.y != 0.f ? 1.f / mine.y : 0.f;
-    if (live && c0 == 0 && done.dest > -2)
-      (done.dest >= 0 ? g.part_ml[static_cast<int64_t>(done.dest) * kRows + r] : g.home_ml[home]) = mine;
-    auto put = [&](int col, const float4 v) {
-      if (done.dest == -2) {
-        const __nv_bfloat162 b0 = __floats2bfloat162_rn(v.x * inv, v.y * inv), b1 = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-        *reinterpret_cast<uint2*>(out + col) = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
-      } else {
-        *reinterpret_cast<float4*>(to + col) = v;
-      }
-    };
-#pragma unroll 1
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t o[32];
-      tmem_ld32(o, lanes + kColO + 32 * c);
-      if (done_copies == 1) {
-        if (live)
-#pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            put(32 * c + i, make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3])));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) scratch[tid * 33 + i] = m == -INFINITY ? 0.f : __uint_as_float(o[i]) * weight;
-        if (!meet()) return;
-        if (live)
-          for (int i = 0; i < cols; i += 4) {
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int k = 0; k < done_copies; ++k)
-#pragma unroll
-              for (int u = 0; u < 4; ++u) v[u] += scratch[(r + k * width) * 33 + c0 + i + u];
-            put(32 * c + c0 + i, make_float4(v[0], v[1], v[2], v[3]));
-          }
-        if (!meet()) return;
-      }
-    }
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(x.seg_empty((segs - 1) % kSegSlots));
-  }
-}
-
-template <int D>
-__global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __grid_constant__ GroupArgs g) {
-  extern __shared__ uint8_t dyn[];
-  using L = GroupSmem<D>;
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
-  Ctx<D> x;
-  x.base = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);
-  x.wait_ns = g.a.wait_ns;
-  x.abort_flag = &s_abort;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kMmaWarp = kSoftmaxWarps + kExpandWarps, kProducer = kMmaWarp + 1;
-  if (threadIdx.x == 0) {
-    s_abort = 0;
-    for (int i = 0; i < kRawSlots; ++i) mbar_init(x.raw_full(i), 1), mbar_init(x.raw_empty(i), kExpandWarps);
-    for (int i = 0; i < kSegSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kSoftmaxWarps);
-    for (int i = 0; i < L::kStages; ++i) mbar_init(x.kv_full(i), kExpandWarps), mbar_init(x.kv_empty(i), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(x.s_full(i), 1), mbar_init(x.p_full(i), 32 * kSoftmaxWarps), mbar_init(x.o_done(i), 1);
-    mbar_init(x.q_full(), 32 * kSoftmaxWarps);
-    mbar_init(x.drained(), 1);
-    mbar_init(x.merged(), 32 * kSoftmaxWarps);
-    fence_barrier_init();
-  }
-  if (warp == kMmaWarp) tmem_alloc(&s_tmem);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  x.tmem = s_tmem;
-  pdl_wait();
-  pdl_trigger();
-  if (warp < kSoftmaxWarps) group_softmax<D>(g, x, warp, lane);
-  else if (warp < kMmaWarp) group_expand<D>(g, x, warp - kSoftmaxWarps, lane);
-  else if (warp == kProducer) group_produce<D>(g, x, lane);
-  else if (lane == 0) group_mma<D>(x);
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (warp == kMmaWarp) tmem_free(s_tmem);
-  if (threadIdx.x == 0 && s_abort) set_status(g.a.ctrl, TRR_ERR_TIMEOUT);
 }
 
 // ----------------------------------------------------------------------------- join --

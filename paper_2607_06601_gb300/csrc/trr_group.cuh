@@ -8,10 +8,6 @@ namespace trr {
 
 constexpr int kRows = 128;       // rows of a segment: lanes of TMEM
 constexpr int kTileKeys = 128;   // most tokens of a tile (64 of 16-bit pages: half the ring per copy)
-constexpr int kRawSlots = 8;     // tiles in the ring of raw pages
-constexpr int kSegSlots = 4;     // segments announced ahead
-constexpr int kSoftmaxWarps = 4, kExpandWarps = 8;
-constexpr int kGroupThreads = 32 * (kSoftmaxWarps + kExpandWarps + 2);
 constexpr int kPlanThreads = 128;
 
 // One job, 32 words.

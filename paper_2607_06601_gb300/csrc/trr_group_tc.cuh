@@ -1,0 +1,821 @@
+// trr_group_tc.cuh - attention of segments with many rows on the tensor cores (tcgen05).
+//
+// One CTA per SM.  A producer warp brings each tile's page slices into a ring of shared memory
+// with bulk copies; sixteen warps expand them to 16-bit rows in the tensor core's layout; one
+// thread issues the products S = Q K^T and O += P V (sums in TMEM); eight warps do the softmax,
+// two threads for each row of TMEM.  Pages of 2, 4 and 8 bits become binary16 (z + c s rounded
+// once, 11 bits), pages of 16 bits stay bf16; p is rounded to the same type, sums and
+// statistics are binary32.  A segment of 64 or 32 rows or fewer fills the 128 lanes with two or
+// four copies of its rows, each of which takes its own part of a tile's tokens, so that all
+// warps share the exponentials.
+//
+// What bounds it, for a tile of 128 tokens at d 128: the products take about 1024 cycles, the
+// exponentials 1024 (16 a cycle), the expansion's integer instructions about as long.
+#pragma once
+
+#include "trr_group.cuh"
+
+namespace trr {
+
+constexpr int kRawSlots = 8;     // tiles in the ring of raw pages
+constexpr int kSegSlots = 4;     // segments announced ahead
+constexpr int kSoftmaxWarps = 8, kExpandWarps = 16;
+constexpr int kMmaWarp = kSoftmaxWarps + kExpandWarps, kProducer = kMmaWarp + 1;
+constexpr int kGroupThreads = 32 * (kProducer + 1);
+
+// A segment, or a CTA's piece of one, as the softmax warps need it.
+struct Segment {
+  int tiles;          // 0: no more
+  int row0, rows;     // its rows in the job, at most 128
+  int kind, qbase, kvh;
+  int dest;           // -2: the output row, -1: the home row, else the piece's slot
+  int pad;
+};
+
+struct RawPage {
+  int off, pos;       // slice and slot positions in the ring; pos < 0: every token in sight
+  int valid, cls;     // slots that hold a token
+};
+struct RawTile {
+  int pages, bf16, first, end;
+  int lo, t, sinks, pad;
+  RawPage page[kTileKeys / 16];
+};
+struct TileMeta {
+  int keys, bf16, first, end;
+  uint16_t mask[kTileKeys / 16];  // tokens in sight
+};
+
+template <int D>
+struct GroupSmem {
+  static constexpr int kStages = D == 64 ? 3 : 2;       // expanded tiles
+  static constexpr int kTile = kTileKeys * D * 2;       // bytes of K or V of one
+  static constexpr int kScratch = kStages * 2 * kTile;  // merge of row copies: [2 halves][128][17] floats
+  static constexpr int kMl = kScratch + 2 * kRows * 17 * 4;  // [2][128] (m, l)
+  static constexpr int kTops = kMl + 2 * kRows * 8;          // [2 tiles][2][128] maxima
+  static constexpr int kRaw = kTops + 4 * kRows * 4;
+  static constexpr int kSeg = kRaw + kRawSlots * static_cast<int>(sizeof(RawTile));
+  static constexpr int kMeta = kSeg + kSegSlots * static_cast<int>(sizeof(Segment));
+  static constexpr int kBars = kMeta + kStages * static_cast<int>(sizeof(TileMeta));
+  static constexpr int kNumBars = 2 * kRawSlots + 2 * kSegSlots + 2 * kStages + 13;
+  static constexpr int kRing = (kBars + kNumBars * 8 + 127) / 128 * 128;
+  static constexpr int kTotal = 225 * 1024;  // of the 227 KB a CTA may have; 1 KB aligns the base
+  static constexpr int kRingBytes = (kTotal - kRing) / 128 * 128;
+  // the widest tile: 8-bit pages with four groups (d 128), or 64 tokens of 16 bits; slot positions of each page
+  static_assert(kRingBytes >= kTileKeys * (2 * D + 8 * (D / 32)) + 8 * 256, "a tile must fit the ring");
+};
+
+template <int D>
+struct Ctx {
+  using L = GroupSmem<D>;
+  uint8_t* base;  // 1024-byte aligned
+  uint32_t tmem;
+  uint64_t wait_ns;
+  volatile int* abort_flag;
+  __device__ uint64_t* bar(int i) const { return reinterpret_cast<uint64_t*>(base + L::kBars) + i; }
+  __device__ uint64_t* raw_full(int i) const { return bar(i); }
+  __device__ uint64_t* raw_empty(int i) const { return bar(kRawSlots + i); }
+  __device__ uint64_t* seg_full(int i) const { return bar(2 * kRawSlots + i); }
+  __device__ uint64_t* seg_empty(int i) const { return bar(2 * kRawSlots + kSegSlots + i); }
+  __device__ uint64_t* kv_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + i); }
+  __device__ uint64_t* kv_empty(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + L::kStages + i); }
+  __device__ uint64_t* s_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + 2 * L::kStages + i); }
+  __device__ uint64_t* p_full(int i) const { return s_full(2 + i); }
+  __device__ uint64_t* o_done(int i) const { return s_full(4 + i); }
+  __device__ uint64_t* q_full() const { return s_full(6); }
+  __device__ uint64_t* drained() const { return s_full(7); }
+  __device__ uint64_t* merged() const { return s_full(8); }
+  __device__ uint64_t* pair(int i) const { return s_full(9 + i); }
+  __device__ RawTile& raw(int i) const { return reinterpret_cast<RawTile*>(base + L::kRaw)[i]; }
+  __device__ Segment& seg(int i) const { return reinterpret_cast<Segment*>(base + L::kSeg)[i]; }
+  __device__ TileMeta& meta(int i) const { return reinterpret_cast<TileMeta*>(base + L::kMeta)[i]; }
+  __device__ uint32_t tile(int stage, int which) const { return smem_u32(base) + (2 * stage + which) * L::kTile; }
+  // A bounded wait; once one has given up, none waits any more.
+  __device__ bool wait(uint64_t* b, uint32_t parity) const {
+    if (mbar_poll(smem_u32(b), parity, wait_ns)) return true;
+    const uint64_t t0 = global_ns();
+    while (!mbar_poll(smem_u32(b), parity, wait_ns)) {
+      if (*abort_flag || global_ns() - t0 >= wait_ns) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+    return true;
+  }
+  // The same by a whole warp: all of its lanes get the same answer.
+  __device__ bool wait_warp(uint64_t* b, uint32_t parity) const { return __all_sync(0xffffffffu, wait(b, parity)); }
+};
+
+constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // TMEM columns: O, two S (P over S), Q in binary16 and bf16
+
+// The producer warp: segments and tiles of this CTA's run, and the copies of their pages.
+template <int D>
+__device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& x, int lane) {
+  using L = GroupSmem<D>;
+  const LayerArgs& a = g.a;
+  const int64_t per = g.head->per, work = g.head->work;
+  const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
+  const int jobs = g.head->jobs, P = a.P, lg_p = __ffs(P) - 1;
+  int it = 0, freed = 0;  // tiles pushed, tiles whose ring bytes are known to be free
+  int ring_head = 0, segs = 0;
+  bool ok = true;
+
+  // room for `need` bytes and a record; the offset in the ring
+  auto book = [&](int need) -> int {
+    for (;;) {
+      if (it - freed < kRawSlots) {
+        if (it == freed) { ring_head = need; return 0; }
+        const int tail = x.raw(freed % kRawSlots).page[0].off;
+        if (ring_head > tail) {
+          if (ring_head + need <= L::kRingBytes) { ring_head += need; return ring_head - need; }
+          if (need < tail) { ring_head = need; return 0; }
+        } else if (ring_head + need < tail) {
+          ring_head += need;
+          return ring_head - need;
+        }
+      }
+      if (!x.wait_warp(x.raw_empty(freed % kRawSlots), (freed / kRawSlots) & 1)) return -1;
+      ++freed;
+    }
+  };
+
+  if (b0 < b1) {
+    // the job that holds cost b0: the last one that starts at or before it
+    int lo = 0, hi = jobs;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && g.base[i] <= b0));
+      const int last = lo + (k - 1) * step;
+      hi = min(hi, last + step);
+      lo = last;
+      if (step == 1) break;
+    }
+    for (int j = lo; j < jobs && ok; ++j) {
+      const int64_t jbase = g.base[j];
+      if (jbase >= b1) break;
+      const int w = reinterpret_cast<const int*>(g.jobs + j)[lane];
+      auto field = [&](int i) { return __shfl_sync(0xffffffffu, w, i); };
+      const int tiles = g.tiles[j];
+      if (tiles <= 0) continue;
+      const int seq = field(0), jlo = field(1), jt = field(2), sinks = field(3);
+      int head[kClasses], first[kClasses], upto[kClasses + 1];
+      upto[0] = 0;
+      for (int c = 0; c < kClasses; ++c) {
+        head[c] = field(4 + c);
+        first[c] = field(8 + c);
+        upto[c + 1] = upto[c] + head[c] + field(12 + c);
+      }
+      const int rows = field(16), row_blocks = field(17), tiles_q = field(18), kind = field(20), qbase = field(21), joined = field(22);
+      const int nt = lane < kClasses ? a.ntok[static_cast<int64_t>(seq) * kClasses + lane] : 0;
+      const int64_t cost = segment_cost(tiles);
+      const int nsegs = a.Hkv * row_blocks;
+      // a batch of 32 pages, one per lane, of the 2-, 4- and 8-bit pages or of the others
+      int batch = -1, slice = 0, room = 0, bytes = 0, valid = 0, cls = 0;
+      bool whole = true;
+      const uint8_t* src = nullptr;  // the page
+      for (int s = static_cast<int>(max(static_cast<int64_t>(0), (b0 - jbase) / cost)); s < nsegs && ok; ++s) {
+        const int64_t S = jbase + s * cost;
+        if (S >= b1) break;
+        const int t0 = tiles_before(b0 - S, tiles), t1 = tiles_before(b1 - S, tiles);
+        if (t0 >= t1) continue;
+        const int kvh = s / row_blocks, rb = s % row_blocks;
+        ok = x.wait_warp(x.seg_empty(segs % kSegSlots), ((segs / kSegSlots) & 1) ^ 1);
+        if (!ok) break;
+        if (lane == 0) {
+          Segment& sg = x.seg(segs % kSegSlots);
+          sg.tiles = t1 - t0;
+          sg.row0 = rb * kRows;
+          sg.rows = min(kRows, rows - rb * kRows);
+          sg.kind = kind; sg.qbase = qbase; sg.kvh = kvh;
+          sg.dest = t1 - t0 == tiles ? (joined ? -1 : -2) : 2 * blockIdx.x + (t0 > 0 ? 0 : 1);
+          mbar_arrive(x.seg_full(segs % kSegSlots));
+        }
+        ++segs;
+        for (int tile = t0; tile < t1; ++tile) {
+          const bool wide = tile >= tiles_q;
+          const int lg = wide ? 6 - lg_p : 7 - lg_p;  // log2 of a tile's pages
+          const int i0 = (wide ? tile - tiles_q : tile) << lg, end = wide ? upto[4] - upto[3] : upto[3];
+          const int b = (i0 >> 5) + (wide ? 1 << 28 : 0);
+          if (b != batch) {
+            batch = b;
+            const int i = (i0 & ~31) + lane;
+            cls = wide ? 3 : i >= upto[2] ? 2 : i >= upto[1] ? 1 : 0;
+            const int in = wide ? i : i - (cls == 2 ? upto[2] : cls == 1 ? upto[1] : 0);
+            int h = head[0], f = first[0], n = __shfl_sync(0xffffffffu, nt, 0);
+#pragma unroll
+            for (int c = 1; c < kClasses; ++c) {
+              const int m = __shfl_sync(0xffffffffu, nt, c);
+              if (cls == c) h = head[c], f = first[c], n = m;
+            }
+            if (i < end) {
+              const int k = in < h ? in : f + in - h;
+              const int64_t at = (static_cast<int64_t>(seq) * kClasses + cls) * a.MP + k;
+              const int page = a.pt[at], pf = a.pfirst[at], pl = a.plast[at];
+              valid = min(P, n - k * P);
+              whole = valid == P && pl <= jt && (pf >= jlo || pl < sinks);
+              slice = a.slice[cls];
+              src = a.pool[cls] + page * a.page_bytes[cls];
+              room = (slice + 127) / 128 * 128 + (whole ? 0 : (4 * P + 127) / 128 * 128);
+              bytes = slice + (whole ? 0 : 4 * P);
+            }
+            __syncwarp();
+          }
+          const int pages = min(1 << lg, end - i0), l0 = i0 & 31, r = lane - l0;
+          const bool mine = r >= 0 && r < pages;
+          int off = mine ? room : 0;
+#pragma unroll
+          for (int o = 1; o < kTileKeys / 16; o <<= 1) {  // at most eight pages
+            const int y = __shfl_up_sync(0xffffffffu, off, o);
+            if (lane >= o) off += y;
+          }
+          const int need = __shfl_sync(0xffffffffu, off, l0 + pages - 1);
+          const int total = __reduce_add_sync(0xffffffffu, mine ? bytes : 0);
+          const int at = book(need);
+          if (at < 0) { ok = false; break; }
+          const int slot = it % kRawSlots;
+          RawTile& rec = x.raw(slot);
+          if (mine) {
+            off += at - room;
+            rec.page[r] = RawPage{off, whole ? -1 : off + (slice + 127) / 128 * 128, valid, cls};
+          }
+          if (lane == 0) {
+            rec.pages = pages; rec.bf16 = wide; rec.first = tile == t0; rec.end = 0;
+            rec.lo = jlo; rec.t = jt; rec.sinks = sinks;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive_expect_tx(x.raw_full(slot), total);
+          __syncwarp();
+          if (mine) {
+            uint8_t* to = x.base + L::kRing + off;
+            bulk_g2s(to, src + a.hdr + static_cast<int64_t>(kvh) * slice, slice, x.raw_full(slot));
+            if (!whole) bulk_g2s(to + (slice + 127) / 128 * 128, src, 4 * P, x.raw_full(slot));
+          }
+          ++it;
+        }
+      }
+    }
+  }
+  if (ok) {  // no more tiles, no more segments
+    ok = x.wait_warp(x.seg_empty(segs % kSegSlots), ((segs / kSegSlots) & 1) ^ 1);
+    if (ok && lane == 0) {
+      x.seg(segs % kSegSlots).tiles = 0;
+      mbar_arrive(x.seg_full(segs % kSegSlots));
+    }
+    if (ok && book(0) >= 0) {
+      if (lane == 0) {
+        x.raw(it % kRawSlots).end = 1;
+        mbar_arrive(x.raw_full(it % kRawSlots));
+      }
+      ++it;
+    }
+  }
+  // the CTA stays until its copies have landed
+  for (int k = max(0, it - kRawSlots); k < it; ++k) mbar_wait(x.raw_full(k % kRawSlots), (k / kRawSlots) & 1);
+}
+
+// Chunk e (8 elements) of row `key` of an expanded tile.
+__device__ __forceinline__ uint8_t* tile_chunk(uint8_t* tile, int key, int e) {
+  return tile + (e >> 3) * (kTileKeys * 128) + key * 128 + (((e ^ key) & 7) << 4);
+}
+
+// z + c s of eight codes, given as four words of two binary16 values 1024 + c, rounded once.
+__device__ __forceinline__ uint4 expand8(uint32_t p0, uint32_t p1, uint32_t p2, uint32_t p3, __half2 s, __half2 z) {
+  const __half2 k = as_half2(0x64006400u);  // 1024: the difference is exact
+  return make_uint4(as_u32(__hfma2(__hsub2(as_half2(p0), k), s, z)), as_u32(__hfma2(__hsub2(as_half2(p1), k), s, z)),
+                    as_u32(__hfma2(__hsub2(as_half2(p2), k), s, z)), as_u32(__hfma2(__hsub2(as_half2(p3), k), s, z)));
+}
+
+__device__ __forceinline__ void store16(uint32_t smem, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(smem), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// 32 elements of one group into the four chunks at `to`, which differ in the two lowest bits of
+// their place in a line only.  codes: chunk i of an 8-bit row lies at 16 i ^ flip.
+template <int B>
+__device__ __forceinline__ void expand32(const uint8_t* codes, int flip, __half2 s, __half2 z, uint32_t to) {
+  if (B == 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 raw = *reinterpret_cast<const uint4*>(codes + (16 * i ^ flip));
+      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        store16(to ^ (32 * i + 16 * q),
+                expand8(__byte_perm(w[2 * q], 0x64646464u, 0x4140), __byte_perm(w[2 * q], 0x64646464u, 0x4342),
+                        __byte_perm(w[2 * q + 1], 0x64646464u, 0x4140), __byte_perm(w[2 * q + 1], 0x64646464u, 0x4342), s, z));
+    }
+  } else if (B == 4) {
+    const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t t[4];  // elements k and k + 4
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[k] = ((w[q] >> (4 * k)) & 0x000F000Fu) | 0x64006400u;
+      store16(to ^ 16 * q, expand8(__byte_perm(t[0], t[1], 0x5410), __byte_perm(t[2], t[3], 0x5410), __byte_perm(t[0], t[1], 0x7632),
+                                   __byte_perm(t[2], t[3], 0x7632), s, z));
+    }
+  } else {
+    const uint2 raw = *reinterpret_cast<const uint2*>(codes);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const uint32_t w = q ? raw.y : raw.x;
+      uint32_t t[8];  // elements k and k + 8
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = ((w >> (2 * k)) & 0x00030003u) | 0x64006400u;
+      store16(to ^ 32 * q, expand8(__byte_perm(t[0], t[1], 0x5410), __byte_perm(t[2], t[3], 0x5410), __byte_perm(t[4], t[5], 0x5410),
+                                   __byte_perm(t[6], t[7], 0x5410), s, z));
+      store16(to ^ (32 * q + 16), expand8(__byte_perm(t[0], t[1], 0x7632), __byte_perm(t[2], t[3], 0x7632), __byte_perm(t[4], t[5], 0x7632),
+                                          __byte_perm(t[6], t[7], 0x7632), s, z));
+    }
+  }
+}
+
+// The same one element at a time, for a group whose largest level rounds past binary16's
+// largest value: such a value stays at it.
+__device__ __noinline__ void expand32_capped(const uint8_t* codes, int flip, int b, uint32_t sz, uint32_t to) {
+  const float s = __low2float(as_half2(sz)), z = __high2float(as_half2(sz));
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    const int bit = i * b, at = bit >> 3;
+    const int code = (codes[b == 8 ? at ^ flip : at] >> (bit & 7)) & ((1 << b) - 1);
+    const float v = fminf(fmaxf(z + code * s, -65504.f), 65504.f);
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"((to ^ (i >> 3) * 16) + 2 * (i & 7)), "h"(__half_as_ushort(__float2half_rn(v))) : "memory");
+  }
+}
+
+// A lane's units of a token's row: every other 32 of its dimensions.
+template <int D, int B>
+__device__ __forceinline__ void expand_row(const uint8_t* sl, const uint32_t* sz, int o, bool swz, int lg_units, bool zero, int odd, uint32_t to) {
+#pragma unroll 1
+  for (int i = 0; i < D / 64; ++i, to += kTileKeys * 128) {
+    const int u = 2 * i + odd, ou = o + u * 4 * B;
+    if (zero) {
+      for (int q = 0; q < 4; ++q) store16(to ^ 16 * q, make_uint4(0, 0, 0, 0));
+      continue;
+    }
+    const uint32_t w = sz[u >> lg_units];
+    // permuted rows of 8 bits: the bits that the chunks' order in their line of 128 bytes flips
+    const int flip = B == 8 && swz ? (ou >> 3) & 0x70 : 0;
+    const uint8_t* codes = sl + (ou ^ (flip & 0x60));
+    const __half2 s = as_half2(__byte_perm(w, 0, 0x1010)), z = as_half2(__byte_perm(w, 0, 0x3232));
+    const __half2 top = __hfma2(__float2half2_rn(static_cast<float>((1 << B) - 1)), s, z);
+    if ((as_u32(top) & 0x7C00u) == 0x7C00u) expand32_capped(codes, flip & 0x10, B, w, to);
+    else expand32<B>(codes, flip & 0x10, s, z, to);
+  }
+}
+
+// The expanding warps: warps 0-7 write K, 8-15 V, each of 16 tokens.  Two lanes share a token
+// and 64 dimensions of its row, so that eight lanes' chunks of a store lie in eight banks.
+template <int D>
+__device__ __forceinline__ void group_expand(const GroupArgs& g, const Ctx<D>& x, int warp, int lane) {
+  using L = GroupSmem<D>;
+  const LayerArgs& a = g.a;
+  const int which = warp >> 3, key0 = (warp & 7) * 16, key = key0 + (lane >> 1), P = a.P, lg_p = __ffs(P) - 1, ng = D / a.G;
+  const int lg_units = __ffs(a.G) - 6;  // log2 of a group's units of 32 dimensions
+  const uint8_t* ring = x.base + L::kRing;
+  for (int it = 0;; ++it) {
+    const int slot = it % kRawSlots, stage = it % L::kStages;
+    if (!x.wait_warp(x.raw_full(slot), (it / kRawSlots) & 1)) return;
+    if (!x.wait_warp(x.kv_empty(stage), ((it / L::kStages) & 1) ^ 1)) return;
+    const RawTile& r = x.raw(slot);
+    TileMeta& m = x.meta(stage);
+    const bool end = r.end;
+    if (!end) {
+      const int keys = r.pages << lg_p;
+      if (warp == 0 && lane == 0) m.keys = keys, m.bf16 = r.bf16, m.first = r.first, m.end = 0;
+      if (key0 < keys) {  // a page holds 16 tokens or more: all 16 of the warp are in one
+        const RawPage pg = r.page[key0 >> lg_p];
+        bool seen = true;
+        if (pg.pos >= 0) {
+          const int at = (key0 & (P - 1)) + (lane & 15), pos = reinterpret_cast<const int32_t*>(ring + pg.pos)[at];
+          seen = at < pg.valid && pos <= r.t && (pos >= r.lo || pos < r.sinks);
+        }
+        const uint32_t mask = __ballot_sync(0xffffffffu, seen) & 0xFFFFu;
+        if (which == 0 && lane == 0) m.mask[warp] = static_cast<uint16_t>(mask);
+        uint8_t* tile = x.base + (2 * stage + which) * L::kTile;
+        const uint8_t* sl = ring + pg.off;
+        if (r.bf16) {  // rows copied 16 bytes at a time, consecutive lanes along a row
+          const int flip = a.swz ? 0x70 : 0;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            constexpr int kN = D / 8;
+            const int row = (i * 32 + lane) / kN, e = (i * 32 + lane) % kN, k = key0 + row;
+            uint4 v = make_uint4(0, 0, 0, 0);  // a V row out of sight is zero: its weight of 0 times infinity would not be
+            if (which == 0 || (mask >> row & 1)) {
+              const int o = (which * P + (k & (P - 1))) * D * 2 + 16 * e;
+              v = *reinterpret_cast<const uint4*>(sl + (o ^ ((o >> 3) & flip)));
+            }
+            *reinterpret_cast<uint4*>(tile_chunk(tile, k, e)) = v;
+          }
+        } else {
+          const int row = (D / 8) << (pg.cls + 1), at = which * P + (key & (P - 1)), odd = lane & 1;
+          const uint32_t* sz = reinterpret_cast<const uint32_t*>(sl + 2 * P * row) + at * ng;
+          const bool zero = which == 1 && !(mask >> (lane >> 1) & 1);
+          const uint32_t to = x.tile(stage, which) + key * 128 + (((4 * odd ^ key) & 7) << 4);
+          if (pg.cls == 0) expand_row<D, 2>(sl, sz, at * row, false, lg_units, zero, odd, to);
+          else if (pg.cls == 1) expand_row<D, 4>(sl, sz, at * row, false, lg_units, zero, odd, to);
+          else expand_row<D, 8>(sl, sz, at * row, a.swz, lg_units, zero, odd, to);
+        }
+      } else if (which == 0 && lane == 0) {
+        m.mask[warp] = 0;
+      }
+      fence_proxy_async_smem();
+    } else if (warp == 0 && lane == 0) {
+      m.end = 1;
+    }
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(x.raw_empty(slot));
+      mbar_arrive(x.kv_full(stage));
+    }
+    if (end) return;
+  }
+}
+
+// The thread that issues the products.  Tile it's scores are issued before tile it-1's P V, so
+// that the tensor core works while the softmax does.
+template <int D>
+__device__ __forceinline__ void group_mma(const Ctx<D>& x) {
+  using L = GroupSmem<D>;
+  int segs = 0, keys_before = 0;
+  bool bf16_before = false, first_before = false, pending = false;
+  auto pv = [&](int it) -> bool {  // O += P V of tile it
+    if (!x.wait(x.p_full(it & 1), (it >> 1) & 1)) return false;
+    tc_fence_after();
+    const uint32_t id = tc_idesc(bf16_before, D, true);
+    const uint64_t d = tc_desc(x.tile(it % L::kStages, 1), kTileKeys * 128);
+    const uint32_t p = x.tmem + kColS + 128 * (it & 1);  // 16 weights in the first 8 of their scores' 16 columns
+    for (int k = 0; k < keys_before / 16; ++k) tc_mma(x.tmem + kColO, p + 16 * k, d + k * (2048 >> 4), id, !(first_before && k == 0));
+    tc_commit(x.kv_empty(it % L::kStages));
+    tc_commit(x.o_done(it & 1));
+    pending = false;
+    return true;
+  };
+  for (int it = 0;; ++it) {
+    const int stage = it % L::kStages;
+    if (!x.wait(x.kv_full(stage), (it / L::kStages) & 1)) break;
+    const TileMeta& m = x.meta(stage);
+    if (m.end) {
+      if (pending) pv(it - 1);
+      break;
+    }
+    const int keys = m.keys;
+    const bool bf16 = m.bf16, first = m.first;
+    if (it >= 2 && !x.wait(x.o_done(it & 1), ((it - 2) >> 1) & 1)) break;  // tile it-2's weights, under the new scores, have been used
+    if (first) {
+      if (pending && !pv(it - 1)) break;
+      if (!x.wait(x.q_full(), segs & 1)) break;
+      ++segs;
+    }
+    tc_fence_after();
+    const uint32_t id = tc_idesc(bf16, keys, false);
+    const uint32_t qcol = x.tmem + kColQ + (bf16 ? 64 : 0);
+    const uint64_t d = tc_desc(x.tile(stage, 0), 16);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+      tc_mma(x.tmem + kColS + 128 * (it & 1), qcol + 8 * k, d + (((k >> 2) * (kTileKeys * 128) + (k & 3) * 32) >> 4), id, k > 0);
+    tc_commit(x.s_full(it & 1));
+    if (pending && !pv(it - 1)) break;
+    pending = true;
+    keys_before = keys; bf16_before = bf16; first_before = first;
+  }
+  tc_commit(x.drained());  // nothing is in flight when the CTA ends
+  mbar_wait(x.drained(), 0);
+}
+
+__device__ __forceinline__ uint32_t pack16(bool bf16, float a, float b) {
+  if (bf16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  return as_u32(__floats2half2_rn(a, b));
+}
+
+// Maximum of t and 16 scores, of those that mask has.
+template <bool ALL>
+__device__ __forceinline__ float highest16(float t, const uint32_t (&s)[16], uint32_t mask) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    if (ALL) {
+      asm("max.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(__uint_as_float(s[i])), "f"(__uint_as_float(s[i + 1])));
+    } else {
+      if (mask >> i & 1) t = fmaxf(t, __uint_as_float(s[i]));
+      if (mask >> (i + 1) & 1) t = fmaxf(t, __uint_as_float(s[i + 1]));
+    }
+  }
+  return t;
+}
+
+// Their weights 2^(s f + shift), packed, and their sum added to l.
+template <bool ALL, bool BF16>
+__device__ __forceinline__ void weigh16(const uint32_t (&s)[16], uint32_t (&p)[8], float f, float shift, uint32_t mask, float* l) {
+  uint64_t sum = 0, ff, hh;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(ff) : "f"(f));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(hh) : "f"(shift));
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    uint64_t x;
+    float x0, x1;
+    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %4;\n}" : "=l"(x) : "r"(s[i]), "r"(s[i + 1]), "l"(ff), "l"(hh));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x));
+    float p0 = exp2_approx(x0), p1 = exp2_approx(x1);
+    if (!ALL) {
+      if (!(mask >> i & 1)) p0 = 0.f;
+      if (!(mask >> (i + 1) & 1)) p1 = 0.f;
+    }
+    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum) : "f"(p0), "f"(p1));
+    p[i / 2] = pack16(BF16, p0, p1);
+  }
+  float s0, s1;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum));
+  *l += s0 + s1;
+}
+
+// The softmax warps.  Warps w and w + 4 share 32 rows (lanes of TMEM); of a tile's eight runs of
+// 16 tokens the first takes the even ones, the second the odd ones.
+template <int D>
+__device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& x, int warp, int lane) {
+  using L = GroupSmem<D>;
+  const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, heads = g.a.Hq / g.a.Hkv;
+  const uint32_t lanes = x.tmem + (static_cast<uint32_t>(quad) << 21);  // the warp's 32 lanes
+  float* scratch = reinterpret_cast<float*>(x.base + L::kScratch) + half * kRows * 17;
+  float2* ml = reinterpret_cast<float2*>(x.base + L::kMl);
+  float* tops = reinterpret_cast<float*>(x.base + L::kTops);
+  uint32_t meets = 0;
+  auto meet = [&]() -> bool {  // the softmax warps wait for one another (bounded, unlike a CTA barrier)
+    mbar_arrive(x.merged());
+    return x.wait_warp(x.merged(), meets++ & 1);
+  };
+
+  // (query, head) of row r of a segment
+  auto row_of = [&](const Segment& sg, int r, int* query, int* head) {
+    const int rr = sg.row0 + r;
+    *query = sg.kind == 0 ? g.list[sg.qbase + rr / heads] : sg.qbase;
+    *head = sg.kvh * heads + rr % heads;
+  };
+  // Half of the row's dimensions of Q into TMEM; the row's factor from products to base-2
+  // exponents.  Each row is scaled by a power of two that brings its largest element to [1, 2):
+  // binary16 then holds what it needs of it.
+  float factor = 0.f;
+  auto load_q = [&](const Segment& sg, int copies) {
+    const int r = row & (kRows / copies - 1);
+    uint32_t w[D / 4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < D / 4; ++i) w[i] = 0;
+    if (r < sg.rows) {
+      int query, head;
+      row_of(sg, r, &query, &head);
+      const uint4* src = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(query) * g.a.Hq + head) * D);
+      uint4 other[D / 16];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) other[i] = src[(half ^ 1) * (D / 16) + i];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const uint4 u = src[half * (D / 16) + i];
+        w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const uint32_t v[4] = {other[i].x, other[i].y, other[i].z, other[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          top = max(top, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
+          top = max(top, max(w[4 * i + k] & 0x7FFFu, (w[4 * i + k] >> 16) & 0x7FFFu));
+        }
+      }
+    }
+    int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
+    e = max(-100, min(120, e));
+    const float down = __int_as_float((127 - e) << 23);
+    factor = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      uint32_t o[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) o[k] = pack16(false, bf16lo(w[16 * i + k]) * down, bf16hi(w[16 * i + k]) * down);
+      tmem_st16(lanes + kColQ + half * (D / 4) + 16 * i, o);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) o[k] = pack16(true, bf16lo(w[16 * i + k]) * down, bf16hi(w[16 * i + k]) * down);
+      tmem_st16(lanes + kColQ + 64 + half * (D / 4) + 16 * i, o);
+    }
+    tmem_wait_st();
+    tc_fence_before();
+    mbar_arrive(x.q_full());
+  };
+  auto copies_of = [](int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; };
+
+  int it = 0, segs = 0;
+  if (!x.wait_warp(x.seg_full(0), 0)) return;
+  Segment sg = x.seg(0);
+  int copies = copies_of(sg.rows);
+  if (sg.tiles > 0) load_q(sg, copies);
+  while (sg.tiles > 0) {
+    // this copy's runs: 8 / copies from run0 on, every other one this warp's
+    const int runs = 8 / copies, run0 = quad * copies / 4 * runs;
+    const float f = factor;
+    float m = -INFINITY, l = 0.f;
+    for (int tile = 0; tile < sg.tiles; ++tile, ++it) {
+      const int stage = it % L::kStages;
+      if (!x.wait_warp(x.kv_full(stage), (it / L::kStages) & 1)) return;
+      const TileMeta& meta = x.meta(stage);
+      const int keys = meta.keys;
+      const bool bf16 = meta.bf16;
+      if (!x.wait_warp(x.s_full(it & 1), (it >> 1) & 1)) return;
+      tc_fence_after();
+      const uint32_t scol = lanes + kColS + 128 * (it & 1);
+      uint32_t s[2][16];  // a pair of runs
+      float top = -INFINITY;
+      auto load_pair = [&](int u) {  // runs u and u + 2
+        tmem_ld16x2(s[0], scol + 16 * u, s[1], scol + 16 * (u + 2 < 8 ? u + 2 : u));
+      };
+      auto mask_of = [&](int u) -> uint32_t { return u < run0 + runs && 16 * u < keys ? meta.mask[u] : 0; };
+      auto highest = [&](int u) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t mask = mask_of(u + 2 * k);
+          if (mask == 0xFFFFu) top = highest16<true>(top, s[k], mask);
+          else if (mask) top = highest16<false>(top, s[k], mask);
+        }
+      };
+      const int u0 = run0 + half;
+      load_pair(u0);
+      highest(u0);
+      const bool more = runs == 8 && 16 * (u0 + 4) < keys;  // runs u0 + 4 and u0 + 6
+      if (more) {
+        load_pair(u0 + 4);
+        highest(u0 + 4);
+      }
+      // the row's maximum over both warps
+      float* xch = tops + (it & 1) * 2 * kRows;
+      xch[half * kRows + row] = top;
+      mbar_arrive(x.pair(quad));
+      if (!x.wait_warp(x.pair(quad), it & 1)) return;
+      top = fmaxf(top, xch[(half ^ 1) * kRows + row]) * f;
+      // m follows the maximum only when that has grown by more than 2^8: p stays within binary16, and O is rarely rescaled
+      if (__any_sync(0xffffffffu, top > m + 8.f)) {
+        const float next = fmaxf(m, top), by = m == -INFINITY ? 0.f : exp2_approx(m - next);
+        l *= by;
+        m = next;
+        if (tile > 0) {  // half of O's columns each
+          if (!x.wait_warp(x.o_done((it - 1) & 1), ((it - 1) >> 1) & 1)) return;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[16];
+            const uint32_t at = lanes + kColO + half * (D / 2) + 16 * c;
+            tmem_ld16(o, at);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
+            tmem_st16(at, o);
+          }
+        }
+      }
+      const float shift = m == -INFINITY ? 0.f : -m;
+      auto weigh = [&](int u) {  // the loaded pair becomes weights, in place
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t mask = mask_of(u + 2 * k);
+          uint32_t p[8];
+          if (mask == 0xFFFFu) {
+            if (bf16) weigh16<true, true>(s[k], p, f, shift, mask, &l);
+            else weigh16<true, false>(s[k], p, f, shift, mask, &l);
+          } else if (mask) {
+            if (bf16) weigh16<false, true>(s[k], p, f, shift, mask, &l);
+            else weigh16<false, false>(s[k], p, f, shift, mask, &l);
+          } else {
+            continue;
+          }
+          tmem_st8(scol + 16 * (u + 2 * k), p);
+        }
+      };
+      if (more) {
+        weigh(u0 + 4);
+        load_pair(u0);
+      }
+      weigh(u0);
+      // weights of the other copies' tokens, and of runs with no token in sight
+      for (int u = half; 16 * u < keys; u += 2)
+        if (u < run0 || mask_of(u) == 0) {
+          const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          tmem_st8(scol + 16 * u, none);
+        }
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(x.p_full(it & 1));
+    }
+    // the next segment's rows go in while this one's last product runs
+    const Segment done = sg;
+    const int done_copies = copies;
+    ++segs;
+    if (!x.wait_warp(x.seg_full(segs % kSegSlots), (segs / kSegSlots) & 1)) return;
+    sg = x.seg(segs % kSegSlots);
+    copies = copies_of(sg.rows);
+    if (sg.tiles > 0) load_q(sg, copies);
+    if (!x.wait_warp(x.o_done((it - 1) & 1), ((it - 1) >> 1) & 1)) return;
+    tc_fence_after();
+
+    // rows out: the output itself, or (m, l, o) for the join.  Both warps of a row have its m and
+    // half of its l; copies have their own of both.
+    const int width = kRows / done_copies;
+    ml[half * kRows + row] = make_float2(m, l);
+    if (!meet()) return;
+    const int r = row / done_copies, cols = 16 / done_copies, c0 = (row % done_copies) * cols;  // what this thread writes of 16 columns
+    float high = -INFINITY, sum = 0.f;
+    for (int k = 0; k < done_copies; ++k) high = fmaxf(high, ml[r + k * width].x);
+    for (int k = 0; k < done_copies; ++k) {
+      const float2 v = ml[r + k * width];
+      if (v.x != -INFINITY) sum += (v.y + ml[kRows + r + k * width].y) * exp2_approx(v.x - high);
+    }
+    float own_high = -INFINITY;  // of the row whose columns of O this thread reads
+    for (int k = 0; k < done_copies; ++k) own_high = fmaxf(own_high, ml[(row & (width - 1)) + k * width].x);
+    const float weight = m == -INFINITY ? 0.f : exp2_approx(m - own_high);
+    int query = 0, head = 0;
+    const bool live = r < done.rows;
+    if (live) row_of(done, r, &query, &head);
+    const int64_t home = (static_cast<int64_t>(done.kind) * g.n + query) * g.a.Hq + head;
+    float* to = done.dest >= 0 ? g.part_o + (static_cast<int64_t>(done.dest) * kRows + r) * D : g.home_o + home * D;
+    uint16_t* out = g.out + (static_cast<int64_t>(query) * g.a.Hq + head) * D;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    if (live && c0 == 0 && half == 0 && done.dest > -2)
+      (done.dest >= 0 ? g.part_ml[static_cast<int64_t>(done.dest) * kRows + r] : g.home_ml[home]) = make_float2(high, sum);
+    auto put = [&](int col, const float4 v) {
+      if (done.dest == -2) *reinterpret_cast<uint2*>(out + col) = make_uint2(pack16(true, v.x * inv, v.y * inv), pack16(true, v.z * inv, v.w * inv));
+      else *reinterpret_cast<float4*>(to + col) = v;
+    };
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[16];
+      const int col = half * (D / 2) + 16 * c;
+      tmem_ld16(o, lanes + kColO + col);
+      if (done_copies == 1) {
+        if (live) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            put(col + i, make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3])));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) scratch[row * 17 + i] = m == -INFINITY ? 0.f : __uint_as_float(o[i]) * weight;
+        if (!meet()) return;
+        if (live)
+          for (int i = 0; i < cols; i += 4) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < done_copies; ++k)
+#pragma unroll
+              for (int u = 0; u < 4; ++u) v[u] += scratch[(r + k * width) * 17 + c0 + i + u];
+            put(col + c0 + i, make_float4(v[0], v[1], v[2], v[3]));
+          }
+        if (!meet()) return;
+      }
+    }
+    if (!meet()) return;  // (m, l) and O have been read
+    tc_fence_before();
+    if (lane == 0) mbar_arrive(x.seg_empty((segs - 1) % kSegSlots));
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __grid_constant__ GroupArgs g) {
+  extern __shared__ uint8_t dyn[];
+  using L = GroupSmem<D>;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  Ctx<D> x;
+  x.base = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);
+  x.wait_ns = g.a.wait_ns;
+  x.abort_flag = &s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int i = 0; i < kRawSlots; ++i) mbar_init(x.raw_full(i), 1), mbar_init(x.raw_empty(i), kExpandWarps);
+    for (int i = 0; i < kSegSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kSoftmaxWarps);
+    for (int i = 0; i < L::kStages; ++i) mbar_init(x.kv_full(i), kExpandWarps), mbar_init(x.kv_empty(i), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(x.s_full(i), 1), mbar_init(x.p_full(i), 32 * kSoftmaxWarps), mbar_init(x.o_done(i), 1);
+    mbar_init(x.q_full(), 32 * kSoftmaxWarps);
+    mbar_init(x.drained(), 1);
+    mbar_init(x.merged(), 32 * kSoftmaxWarps);
+    for (int i = 0; i < 4; ++i) mbar_init(x.pair(i), 64);
+    fence_barrier_init();
+  }
+  if (warp == kMmaWarp) tmem_alloc(&s_tmem);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  x.tmem = s_tmem;
+  pdl_wait();
+  pdl_trigger();
+  if (warp < kSoftmaxWarps) group_softmax<D>(g, x, warp, lane);
+  else if (warp < kMmaWarp) group_expand<D>(g, x, warp - kSoftmaxWarps, lane);
+  else if (warp == kProducer) group_produce<D>(g, x, lane);
+  else if (lane == 0) group_mma<D>(x);
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_free(s_tmem);
+  if (threadIdx.x == 0 && s_abort) set_status(g.a.ctrl, TRR_ERR_TIMEOUT);
+}
+
+}  // namespace trr

@@ -19,6 +19,7 @@ namespace trr {
 
 constexpr int kRawSlots = 8;     // tiles in the ring of raw pages
 constexpr int kSegSlots = 4;     // segments announced ahead
+constexpr int kMetaSlots = 8;    // tiles whose record the softmax may still need: at least kStages + 2
 constexpr int kSoftmaxWarps = 8, kExpandWarps = 16;
 constexpr int kMmaWarp = kSoftmaxWarps + kExpandWarps, kProducer = kMmaWarp + 1;
 constexpr int kGroupThreads = 32 * (kProducer + 1);
@@ -56,8 +57,8 @@ struct GroupSmem {
   static constexpr int kRaw = kTops + 4 * kRows * 4;
   static constexpr int kSeg = kRaw + kRawSlots * static_cast<int>(sizeof(RawTile));
   static constexpr int kMeta = kSeg + kSegSlots * static_cast<int>(sizeof(Segment));
-  static constexpr int kBars = kMeta + kStages * static_cast<int>(sizeof(TileMeta));
-  static constexpr int kNumBars = 2 * kRawSlots + 2 * kSegSlots + 2 * kStages + 13;
+  static constexpr int kBars = kMeta + kMetaSlots * static_cast<int>(sizeof(TileMeta));
+  static constexpr int kNumBars = 2 * kRawSlots + 2 * kSegSlots + 4 * kStages + 13;
   static constexpr int kRing = (kBars + kNumBars * 8 + 127) / 128 * 128;
   static constexpr int kTotal = 225 * 1024;  // of the 227 KB a CTA may have; 1 KB aligns the base
   static constexpr int kRingBytes = (kTotal - kRing) / 128 * 128;
@@ -77,9 +78,10 @@ struct Ctx {
   __device__ uint64_t* raw_empty(int i) const { return bar(kRawSlots + i); }
   __device__ uint64_t* seg_full(int i) const { return bar(2 * kRawSlots + i); }
   __device__ uint64_t* seg_empty(int i) const { return bar(2 * kRawSlots + kSegSlots + i); }
-  __device__ uint64_t* kv_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + i); }
-  __device__ uint64_t* kv_empty(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + L::kStages + i); }
-  __device__ uint64_t* s_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + 2 * L::kStages + i); }
+  // which: 0 K, 1 V
+  __device__ uint64_t* kv_full(int which, int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + which * L::kStages + i); }
+  __device__ uint64_t* kv_empty(int which, int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + (2 + which) * L::kStages + i); }
+  __device__ uint64_t* s_full(int i) const { return bar(2 * kRawSlots + 2 * kSegSlots + 4 * L::kStages + i); }
   __device__ uint64_t* p_full(int i) const { return s_full(2 + i); }
   __device__ uint64_t* o_done(int i) const { return s_full(4 + i); }
   __device__ uint64_t* q_full() const { return s_full(6); }
@@ -377,9 +379,9 @@ __device__ __forceinline__ void group_expand(const GroupArgs& g, const Ctx<D>& x
   for (int it = 0;; ++it) {
     const int slot = it % kRawSlots, stage = it % L::kStages;
     if (!x.wait_warp(x.raw_full(slot), (it / kRawSlots) & 1)) return;
-    if (!x.wait_warp(x.kv_empty(stage), ((it / L::kStages) & 1) ^ 1)) return;
+    if (!x.wait_warp(x.kv_empty(which, stage), ((it / L::kStages) & 1) ^ 1)) return;
     const RawTile& r = x.raw(slot);
-    TileMeta& m = x.meta(stage);
+    TileMeta& m = x.meta(it % kMetaSlots);
     const bool end = r.end;
     if (!end) {
       const int keys = r.pages << lg_p;
@@ -427,35 +429,38 @@ __device__ __forceinline__ void group_expand(const GroupArgs& g, const Ctx<D>& x
     __syncwarp();
     if (lane == 0) {
       mbar_arrive(x.raw_empty(slot));
-      mbar_arrive(x.kv_full(stage));
+      mbar_arrive(x.kv_full(which, stage));
     }
     if (end) return;
   }
 }
 
 // The thread that issues the products.  Tile it's scores are issued before tile it-1's P V, so
-// that the tensor core works while the softmax does.
+// that the tensor core works while the softmax does; K's place is free again once its scores
+// are, V's once its product is.
 template <int D>
 __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
   using L = GroupSmem<D>;
   int segs = 0, keys_before = 0;
   bool bf16_before = false, first_before = false, pending = false;
   auto pv = [&](int it) -> bool {  // O += P V of tile it
-    if (!x.wait(x.p_full(it & 1), (it >> 1) & 1)) return false;
+    const int stage = it % L::kStages;
+    if (!x.wait(x.kv_full(1, stage), (it / L::kStages) & 1) || !x.wait(x.p_full(it & 1), (it >> 1) & 1)) return false;
     tc_fence_after();
     const uint32_t id = tc_idesc(bf16_before, D, true);
-    const uint64_t d = tc_desc(x.tile(it % L::kStages, 1), kTileKeys * 128);
+    const uint64_t d = tc_desc(x.tile(stage, 1), kTileKeys * 128);
     const uint32_t p = x.tmem + kColS + 128 * (it & 1);  // 16 weights in the first 8 of their scores' 16 columns
+#pragma unroll 1
     for (int k = 0; k < keys_before / 16; ++k) tc_mma(x.tmem + kColO, p + 16 * k, d + k * (2048 >> 4), id, !(first_before && k == 0));
-    tc_commit(x.kv_empty(it % L::kStages));
+    tc_commit(x.kv_empty(1, stage));
     tc_commit(x.o_done(it & 1));
     pending = false;
     return true;
   };
   for (int it = 0;; ++it) {
     const int stage = it % L::kStages;
-    if (!x.wait(x.kv_full(stage), (it / L::kStages) & 1)) break;
-    const TileMeta& m = x.meta(stage);
+    if (!x.wait(x.kv_full(0, stage), (it / L::kStages) & 1)) break;
+    const TileMeta& m = x.meta(it % kMetaSlots);
     if (m.end) {
       if (pending) pv(it - 1);
       break;
@@ -472,10 +477,11 @@ __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
     const uint32_t id = tc_idesc(bf16, keys, false);
     const uint32_t qcol = x.tmem + kColQ + (bf16 ? 64 : 0);
     const uint64_t d = tc_desc(x.tile(stage, 0), 16);
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < D / 16; ++k)
       tc_mma(x.tmem + kColS + 128 * (it & 1), qcol + 8 * k, d + (((k >> 2) * (kTileKeys * 128) + (k & 3) * 32) >> 4), id, k > 0);
     tc_commit(x.s_full(it & 1));
+    tc_commit(x.kv_empty(0, stage));
     if (pending && !pv(it - 1)) break;
     pending = true;
     keys_before = keys; bf16_before = bf16; first_before = first;
@@ -492,24 +498,23 @@ __device__ __forceinline__ uint32_t pack16(bool bf16, float a, float b) {
   return as_u32(__floats2half2_rn(a, b));
 }
 
-// Maximum of t and 16 scores, of those that mask has.
-template <bool ALL>
-__device__ __forceinline__ float highest16(float t, const uint32_t (&s)[16], uint32_t mask) {
+// Scores out of sight become -infinity: their weight is 0 and they are no maximum.
+__device__ __forceinline__ void mask16(uint32_t (&s)[16], uint32_t mask) {
+  if (mask != 0xFFFFu) {
 #pragma unroll
-  for (int i = 0; i < 16; i += 2) {
-    if (ALL) {
-      asm("max.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(__uint_as_float(s[i])), "f"(__uint_as_float(s[i + 1])));
-    } else {
-      if (mask >> i & 1) t = fmaxf(t, __uint_as_float(s[i]));
-      if (mask >> (i + 1) & 1) t = fmaxf(t, __uint_as_float(s[i + 1]));
-    }
+    for (int i = 0; i < 16; ++i)
+      if (!(mask >> i & 1)) s[i] = 0xFF800000u;
   }
+}
+
+__device__ __forceinline__ float highest16(float t, const uint32_t (&s)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(__uint_as_float(s[i])), "f"(__uint_as_float(s[i + 1])));
   return t;
 }
 
-// Their weights 2^(s f + shift), packed, and their sum added to l.
-template <bool ALL, bool BF16>
-__device__ __forceinline__ void weigh16(const uint32_t (&s)[16], uint32_t (&p)[8], float f, float shift, uint32_t mask, float* l) {
+// Weights 2^(s f + shift) of 16 scores, packed; their sum is added to l.
+__device__ __forceinline__ void weigh16(uint32_t (&s)[16], uint32_t (&p)[8], bool bf16, float f, float shift, float* l) {
   uint64_t sum = 0, ff, hh;
   asm("mov.b64 %0, {%1, %1};" : "=l"(ff) : "f"(f));
   asm("mov.b64 %0, {%1, %1};" : "=l"(hh) : "f"(shift));
@@ -519,13 +524,18 @@ __device__ __forceinline__ void weigh16(const uint32_t (&s)[16], uint32_t (&p)[8
     float x0, x1;
     asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %4;\n}" : "=l"(x) : "r"(s[i]), "r"(s[i + 1]), "l"(ff), "l"(hh));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x));
-    float p0 = exp2_approx(x0), p1 = exp2_approx(x1);
-    if (!ALL) {
-      if (!(mask >> i & 1)) p0 = 0.f;
-      if (!(mask >> (i + 1) & 1)) p1 = 0.f;
-    }
-    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum) : "f"(p0), "f"(p1));
-    p[i / 2] = pack16(BF16, p0, p1);
+    x0 = exp2_approx(x0);
+    x1 = exp2_approx(x1);
+    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum) : "f"(x0), "f"(x1));
+    s[i] = __float_as_uint(x0);
+    s[i + 1] = __float_as_uint(x1);
+  }
+  if (bf16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = pack16(true, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = pack16(false, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
   }
   float s0, s1;
   asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum));
@@ -617,35 +627,26 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
     const float f = factor;
     float m = -INFINITY, l = 0.f;
     for (int tile = 0; tile < sg.tiles; ++tile, ++it) {
-      const int stage = it % L::kStages;
-      if (!x.wait_warp(x.kv_full(stage), (it / L::kStages) & 1)) return;
-      const TileMeta& meta = x.meta(stage);
-      const int keys = meta.keys;
-      const bool bf16 = meta.bf16;
       if (!x.wait_warp(x.s_full(it & 1), (it >> 1) & 1)) return;
       tc_fence_after();
+      const TileMeta& meta = x.meta(it % kMetaSlots);
+      const int keys = meta.keys;
+      const bool bf16 = meta.bf16;
       const uint32_t scol = lanes + kColS + 128 * (it & 1);
-      uint32_t s[2][16];  // a pair of runs
+      // this warp's runs: u0, u0 + 2 and, with all eight its copy's own, u0 + 4, u0 + 6
+      const int u0 = run0 + half, last = runs == 8 && 16 * (u0 + 4) < keys ? 4 : 0;
+      uint32_t s[2][16];  // a pair of them
       float top = -INFINITY;
-      auto load_pair = [&](int u) {  // runs u and u + 2
+      auto load_pair = [&](int u) {
         tmem_ld16x2(s[0], scol + 16 * u, s[1], scol + 16 * (u + 2 < 8 ? u + 2 : u));
+        mask16(s[0], 16 * u < keys ? meta.mask[u] : 0);
+        mask16(s[1], u + 2 < run0 + runs && 16 * (u + 2) < keys ? meta.mask[u + 2] : 0);
       };
-      auto mask_of = [&](int u) -> uint32_t { return u < run0 + runs && 16 * u < keys ? meta.mask[u] : 0; };
-      auto highest = [&](int u) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t mask = mask_of(u + 2 * k);
-          if (mask == 0xFFFFu) top = highest16<true>(top, s[k], mask);
-          else if (mask) top = highest16<false>(top, s[k], mask);
-        }
-      };
-      const int u0 = run0 + half;
-      load_pair(u0);
-      highest(u0);
-      const bool more = runs == 8 && 16 * (u0 + 4) < keys;  // runs u0 + 4 and u0 + 6
-      if (more) {
-        load_pair(u0 + 4);
-        highest(u0 + 4);
+      // one copy of the code for both pairs: the warps' instructions have to fit the cache together
+#pragma unroll 1
+      for (int v = 0; v <= last; v += 4) {
+        load_pair(u0 + v);
+        top = highest16(highest16(top, s[0]), s[1]);
       }
       // the row's maximum over both warps
       float* xch = tops + (it & 1) * 2 * kRows;
@@ -673,34 +674,23 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
         }
       }
       const float shift = m == -INFINITY ? 0.f : -m;
-      auto weigh = [&](int u) {  // the loaded pair becomes weights, in place
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t mask = mask_of(u + 2 * k);
-          uint32_t p[8];
-          if (mask == 0xFFFFu) {
-            if (bf16) weigh16<true, true>(s[k], p, f, shift, mask, &l);
-            else weigh16<true, false>(s[k], p, f, shift, mask, &l);
-          } else if (mask) {
-            if (bf16) weigh16<false, true>(s[k], p, f, shift, mask, &l);
-            else weigh16<false, false>(s[k], p, f, shift, mask, &l);
-          } else {
-            continue;
-          }
-          tmem_st8(scol + 16 * (u + 2 * k), p);
+#pragma unroll 1
+      for (int v = last; v >= 0; v -= 4) {  // weights, in the scores' place; the last pair is still here
+        const int u = u0 + v;
+        if (v != last) load_pair(u);
+        uint32_t p[8];
+        weigh16(s[0], p, bf16, f, shift, &l);
+        if (16 * u < keys) tmem_st8(scol + 16 * u, p);
+        if (runs > 2) {
+          weigh16(s[1], p, bf16, f, shift, &l);
+          if (16 * (u + 2) < keys) tmem_st8(scol + 16 * (u + 2), p);
         }
-      };
-      if (more) {
-        weigh(u0 + 4);
-        load_pair(u0);
       }
-      weigh(u0);
-      // weights of the other copies' tokens, and of runs with no token in sight
-      for (int u = half; 16 * u < keys; u += 2)
-        if (u < run0 || mask_of(u) == 0) {
-          const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-          tmem_st8(scol + 16 * u, none);
-        }
+      if (runs < 8) {  // no weight on the other copies' tokens
+        const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int u = half; 16 * u < keys; u += 2)
+          if (u < run0 || u >= run0 + runs) tmem_st8(scol + 16 * u, none);
+      }
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(x.p_full(it & 1));
@@ -791,7 +781,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __gr
     s_abort = 0;
     for (int i = 0; i < kRawSlots; ++i) mbar_init(x.raw_full(i), 1), mbar_init(x.raw_empty(i), kExpandWarps);
     for (int i = 0; i < kSegSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kSoftmaxWarps);
-    for (int i = 0; i < L::kStages; ++i) mbar_init(x.kv_full(i), kExpandWarps), mbar_init(x.kv_empty(i), 1);
+    for (int i = 0; i < 2 * L::kStages; ++i) mbar_init(x.kv_full(0, i), kExpandWarps / 2), mbar_init(x.kv_empty(0, i), 1);  // K, V
     for (int i = 0; i < 2; ++i) mbar_init(x.s_full(i), 1), mbar_init(x.p_full(i), 32 * kSoftmaxWarps), mbar_init(x.o_done(i), 1);
     mbar_init(x.q_full(), 32 * kSoftmaxWarps);
     mbar_init(x.drained(), 1);

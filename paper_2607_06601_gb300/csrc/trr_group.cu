@@ -402,9 +402,17 @@ cudaError_t configure_group() {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
   }
-  cudaError_t e = cudaFuncSetAttribute(group_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, GroupSmem<64>::kTotal + 1024);
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(group_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, GroupSmem<128>::kTotal + 1024);
+  auto tensor_kernel = [](void (*k)(GroupArgs), int bytes) {
+    // its warpgroups share out the registers of the launch: no fewer than they were counted on
+    cudaFuncAttributes at;
+    cudaError_t e = cudaFuncGetAttributes(&at, k);
+    if (e != cudaSuccess) return e;
+    if (at.numRegs * kGroupThreads < 32 * kSoftmaxWarps * kSoftmaxRegisters + (kGroupThreads - 32 * kSoftmaxWarps) * kOtherRegisters)
+      return cudaErrorInvalidConfiguration;
+    return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  const cudaError_t e = tensor_kernel(group_attn_kernel<64>, GroupSmem<64>::kTotal + 1024);
+  return e != cudaSuccess ? e : tensor_kernel(group_attn_kernel<128>, GroupSmem<128>::kTotal + 1024);
 }
 
 template <int D>

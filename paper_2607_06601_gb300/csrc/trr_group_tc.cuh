@@ -22,7 +22,11 @@ constexpr int kSegSlots = 4;     // segments announced ahead
 constexpr int kMetaSlots = 8;    // tiles whose record the softmax may still need: at least kStages + 2
 constexpr int kSoftmaxWarps = 8, kExpandWarps = 16;
 constexpr int kMmaWarp = kSoftmaxWarps + kExpandWarps, kProducer = kMmaWarp + 1;
-constexpr int kGroupThreads = 32 * (kProducer + 1);
+constexpr int kGroupThreads = 32 * (kProducer + 3);  // whole warpgroups: two warps more that do nothing
+// Registers a thread: 72 at launch; two softmax warpgroups take what the other five give up
+// (256 x 112 + 640 x 56 = 896 x 72).
+constexpr int kSoftmaxRegisters = 112, kOtherRegisters = 56;
+static_assert(32 * kSoftmaxWarps * kSoftmaxRegisters + (kGroupThreads - 32 * kSoftmaxWarps) * kOtherRegisters <= kGroupThreads * 72, "");
 
 // A segment, or a CTA's piece of one, as the softmax warps need it.
 struct Segment {
@@ -39,12 +43,13 @@ struct RawPage {
 };
 struct RawTile {
   int pages, bf16, first, end;
-  int lo, t, sinks, pad;
+  int lo, t, sinks, all;
   RawPage page[kTileKeys / 16];
 };
 struct TileMeta {
-  int keys, bf16, first, end;
-  uint16_t mask[kTileKeys / 16];  // tokens in sight
+  int keys, bf16, first, end, all;  // all: 128 tokens, every one in sight
+  uint16_t mask[kTileKeys / 16];    // tokens in sight
+  int pad[3];
 };
 
 template <int D>
@@ -231,6 +236,7 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
             if (lane >= o) off += y;
           }
           const int need = __shfl_sync(0xffffffffu, off, l0 + pages - 1);
+          const bool all_in = __all_sync(0xffffffffu, !mine || whole);
           const int total = __reduce_add_sync(0xffffffffu, mine ? bytes : 0);
           const int at = book(need);
           if (at < 0) { ok = false; break; }
@@ -242,7 +248,7 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
           }
           if (lane == 0) {
             rec.pages = pages; rec.bf16 = wide; rec.first = tile == t0; rec.end = 0;
-            rec.lo = jlo; rec.t = jt; rec.sinks = sinks;
+            rec.lo = jlo; rec.t = jt; rec.sinks = sinks; rec.all = all_in && pages << lg_p == kTileKeys;
           }
           __syncwarp();
           if (lane == 0) mbar_arrive_expect_tx(x.raw_full(slot), total);
@@ -385,7 +391,7 @@ __device__ __forceinline__ void group_expand(const GroupArgs& g, const Ctx<D>& x
     const bool end = r.end;
     if (!end) {
       const int keys = r.pages << lg_p;
-      if (warp == 0 && lane == 0) m.keys = keys, m.bf16 = r.bf16, m.first = r.first, m.end = 0;
+      if (warp == 0 && lane == 0) m.keys = keys, m.bf16 = r.bf16, m.first = r.first, m.end = 0, m.all = r.all;
       if (key0 < keys) {  // a page holds 16 tokens or more: all 16 of the warp are in one
         const RawPage pg = r.page[key0 >> lg_p];
         bool seen = true;
@@ -435,9 +441,10 @@ __device__ __forceinline__ void group_expand(const GroupArgs& g, const Ctx<D>& x
   }
 }
 
-// The thread that issues the products.  Tile it's scores are issued before tile it-1's P V, so
-// that the tensor core works while the softmax does; K's place is free again once its scores
-// are, V's once its product is.
+// The warp that issues the products (one elected lane does; the whole warp goes along, so that
+// addresses and descriptors stay in uniform registers).  Tile it's scores are issued before tile
+// it-1's P V, so that the tensor core works while the softmax does; K's place is free again once
+// its scores are, V's once its product is.
 template <int D>
 __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
   using L = GroupSmem<D>;
@@ -445,48 +452,56 @@ __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
   bool bf16_before = false, first_before = false, pending = false;
   auto pv = [&](int it) -> bool {  // O += P V of tile it
     const int stage = it % L::kStages;
-    if (!x.wait(x.kv_full(1, stage), (it / L::kStages) & 1) || !x.wait(x.p_full(it & 1), (it >> 1) & 1)) return false;
+    if (!x.wait_warp(x.kv_full(1, stage), (it / L::kStages) & 1) || !x.wait_warp(x.p_full(it & 1), (it >> 1) & 1)) return false;
     tc_fence_after();
     const uint32_t id = tc_idesc(bf16_before, D, true);
     const uint64_t d = tc_desc(x.tile(stage, 1), kTileKeys * 128);
     const uint32_t p = x.tmem + kColS + 128 * (it & 1);  // 16 weights in the first 8 of their scores' 16 columns
-#pragma unroll 1
-    for (int k = 0; k < keys_before / 16; ++k) tc_mma(x.tmem + kColO, p + 16 * k, d + k * (2048 >> 4), id, !(first_before && k == 0));
-    tc_commit(x.kv_empty(1, stage));
-    tc_commit(x.o_done(it & 1));
+    if (elected()) {
+#pragma unroll
+      for (int k = 0; k < kTileKeys / 16; ++k)
+        if (16 * k < keys_before) tc_mma(x.tmem + kColO, p + 16 * k, d + k * (2048 >> 4), id, k > 0 || !first_before);
+      tc_commit(x.kv_empty(1, stage));
+      tc_commit(x.o_done(it & 1));
+    }
+    __syncwarp();
     pending = false;
     return true;
   };
   for (int it = 0;; ++it) {
     const int stage = it % L::kStages;
-    if (!x.wait(x.kv_full(0, stage), (it / L::kStages) & 1)) break;
+    if (!x.wait_warp(x.kv_full(0, stage), (it / L::kStages) & 1)) break;
     const TileMeta& m = x.meta(it % kMetaSlots);
-    if (m.end) {
+    if (__shfl_sync(0xffffffffu, m.end, 0)) {
       if (pending) pv(it - 1);
       break;
     }
-    const int keys = m.keys;
-    const bool bf16 = m.bf16, first = m.first;
-    if (it >= 2 && !x.wait(x.o_done(it & 1), ((it - 2) >> 1) & 1)) break;  // tile it-2's weights, under the new scores, have been used
+    const int keys = __shfl_sync(0xffffffffu, m.keys, 0);
+    const bool bf16 = __shfl_sync(0xffffffffu, m.bf16, 0), first = __shfl_sync(0xffffffffu, m.first, 0);
+    if (it >= 2 && !x.wait_warp(x.o_done(it & 1), ((it - 2) >> 1) & 1)) break;  // tile it-2's weights, under the new scores, have been used
     if (first) {
       if (pending && !pv(it - 1)) break;
-      if (!x.wait(x.q_full(), segs & 1)) break;
+      if (!x.wait_warp(x.q_full(), segs & 1)) break;
       ++segs;
     }
     tc_fence_after();
     const uint32_t id = tc_idesc(bf16, keys, false);
     const uint32_t qcol = x.tmem + kColQ + (bf16 ? 64 : 0);
     const uint64_t d = tc_desc(x.tile(stage, 0), 16);
-#pragma unroll 1
-    for (int k = 0; k < D / 16; ++k)
-      tc_mma(x.tmem + kColS + 128 * (it & 1), qcol + 8 * k, d + (((k >> 2) * (kTileKeys * 128) + (k & 3) * 32) >> 4), id, k > 0);
-    tc_commit(x.s_full(it & 1));
-    tc_commit(x.kv_empty(0, stage));
+    if (elected()) {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        tc_mma(x.tmem + kColS + 128 * (it & 1), qcol + 8 * k, d + (((k >> 2) * (kTileKeys * 128) + (k & 3) * 32) >> 4), id, k > 0);
+      tc_commit(x.s_full(it & 1));
+      tc_commit(x.kv_empty(0, stage));
+    }
+    __syncwarp();
     if (pending && !pv(it - 1)) break;
     pending = true;
     keys_before = keys; bf16_before = bf16; first_before = first;
   }
-  tc_commit(x.drained());  // nothing is in flight when the CTA ends
+  if (elected()) tc_commit(x.drained());  // nothing is in flight when the CTA ends
+  __syncwarp();
   mbar_wait(x.drained(), 0);
 }
 
@@ -513,8 +528,8 @@ __device__ __forceinline__ float highest16(float t, const uint32_t (&s)[16]) {
   return t;
 }
 
-// Weights 2^(s f + shift) of 16 scores, packed; their sum is added to l.
-__device__ __forceinline__ void weigh16(uint32_t (&s)[16], uint32_t (&p)[8], bool bf16, float f, float shift, float* l) {
+// 16 scores become their weights 2^(s f + shift); returns the weights' sum.
+__device__ __forceinline__ float weigh16(uint32_t (&s)[16], float f, float shift) {
   uint64_t sum = 0, ff, hh;
   asm("mov.b64 %0, {%1, %1};" : "=l"(ff) : "f"(f));
   asm("mov.b64 %0, {%1, %1};" : "=l"(hh) : "f"(shift));
@@ -530,6 +545,11 @@ __device__ __forceinline__ void weigh16(uint32_t (&s)[16], uint32_t (&p)[8], boo
     s[i] = __float_as_uint(x0);
     s[i + 1] = __float_as_uint(x1);
   }
+  float s0, s1;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum));
+  return s0 + s1;
+}
+__device__ __forceinline__ void pack_weights(const uint32_t (&s)[16], uint32_t (&p)[8], bool bf16) {
   if (bf16) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = pack16(true, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
@@ -537,9 +557,6 @@ __device__ __forceinline__ void weigh16(uint32_t (&s)[16], uint32_t (&p)[8], boo
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[i] = pack16(false, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
   }
-  float s0, s1;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum));
-  *l += s0 + s1;
 }
 
 // The softmax warps.  Warps w and w + 4 share 32 rows (lanes of TMEM); of a tile's eight runs of
@@ -554,7 +571,8 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
   float* tops = reinterpret_cast<float*>(x.base + L::kTops);
   uint32_t meets = 0;
   auto meet = [&]() -> bool {  // the softmax warps wait for one another (bounded, unlike a CTA barrier)
-    mbar_arrive(x.merged());
+    __syncwarp();
+    if (lane == 0) mbar_arrive(x.merged());
     return x.wait_warp(x.merged(), meets++ & 1);
   };
 
@@ -612,7 +630,8 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
     }
     tmem_wait_st();
     tc_fence_before();
-    mbar_arrive(x.q_full());
+    __syncwarp();
+    if (lane == 0) mbar_arrive(x.q_full());
   };
   auto copies_of = [](int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; };
 
@@ -633,25 +652,35 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
       const int keys = meta.keys;
       const bool bf16 = meta.bf16;
       const uint32_t scol = lanes + kColS + 128 * (it & 1);
-      // this warp's runs: u0, u0 + 2 and, with all eight its copy's own, u0 + 4, u0 + 6
-      const int u0 = run0 + half, last = runs == 8 && 16 * (u0 + 4) < keys ? 4 : 0;
-      uint32_t s[2][16];  // a pair of them
+      const int u0 = run0 + half;  // this warp's runs: u0 and every other one from there
+      uint32_t s[4][16];
       float top = -INFINITY;
-      auto load_pair = [&](int u) {
-        tmem_ld16x2(s[0], scol + 16 * u, s[1], scol + 16 * (u + 2 < 8 ? u + 2 : u));
-        mask16(s[0], 16 * u < keys ? meta.mask[u] : 0);
-        mask16(s[1], u + 2 < run0 + runs && 16 * (u + 2) < keys ? meta.mask[u + 2] : 0);
-      };
-      // one copy of the code for both pairs: the warps' instructions have to fit the cache together
-#pragma unroll 1
-      for (int v = 0; v <= last; v += 4) {
-        load_pair(u0 + v);
-        top = highest16(highest16(top, s[0]), s[1]);
+      if (runs == 8) {
+        tmem_ld16x4(s[0], scol + 16 * u0, s[1], scol + 16 * u0 + 32, s[2], scol + 16 * u0 + 64, s[3], scol + 16 * u0 + 96);
+      } else {
+        tmem_ld16x2(s[0], scol + 16 * u0, s[1], scol + 16 * (runs == 4 ? u0 + 2 : u0));
+      }
+      // a full tile with one copy of the rows is the common case of many rows: no branch parts its four runs
+      const bool full = runs == 8 && meta.all;
+      auto mine = [&](int k) { return 2 * k < runs && 16 * (u0 + 2 * k) < keys; };
+      if (full) {
+        float t[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = highest16(-INFINITY, s[k]);
+        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (mine(k)) {
+            mask16(s[k], meta.mask[u0 + 2 * k]);
+            top = highest16(top, s[k]);
+          }
       }
       // the row's maximum over both warps
       float* xch = tops + (it & 1) * 2 * kRows;
       xch[half * kRows + row] = top;
-      mbar_arrive(x.pair(quad));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(x.pair(quad));
       if (!x.wait_warp(x.pair(quad), it & 1)) return;
       top = fmaxf(top, xch[(half ^ 1) * kRows + row]) * f;
       // m follows the maximum only when that has grown by more than 2^8: p stays within binary16, and O is rarely rescaled
@@ -674,17 +703,27 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
         }
       }
       const float shift = m == -INFINITY ? 0.f : -m;
-#pragma unroll 1
-      for (int v = last; v >= 0; v -= 4) {  // weights, in the scores' place; the last pair is still here
-        const int u = u0 + v;
-        if (v != last) load_pair(u);
-        uint32_t p[8];
-        weigh16(s[0], p, bf16, f, shift, &l);
-        if (16 * u < keys) tmem_st8(scol + 16 * u, p);
-        if (runs > 2) {
-          weigh16(s[1], p, bf16, f, shift, &l);
-          if (16 * (u + 2) < keys) tmem_st8(scol + 16 * (u + 2), p);
+      // weights, in the scores' place
+      if (full) {
+        float sums[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sums[k] = weigh16(s[k], f, shift);
+        l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t p[8];
+          pack_weights(s[k], p, bf16);
+          tmem_st8(scol + 16 * (u0 + 2 * k), p);
         }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (mine(k)) {
+            uint32_t p[8];
+            l += weigh16(s[k], f, shift);
+            pack_weights(s[k], p, bf16);
+            tmem_st8(scol + 16 * (u0 + 2 * k), p);
+          }
       }
       if (runs < 8) {  // no weight on the other copies' tokens
         const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -693,7 +732,8 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
       }
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive(x.p_full(it & 1));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(x.p_full(it & 1));
     }
     // the next segment's rows go in while this one's last product runs
     const Segment done = sg;
@@ -782,11 +822,11 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __gr
     for (int i = 0; i < kRawSlots; ++i) mbar_init(x.raw_full(i), 1), mbar_init(x.raw_empty(i), kExpandWarps);
     for (int i = 0; i < kSegSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kSoftmaxWarps);
     for (int i = 0; i < 2 * L::kStages; ++i) mbar_init(x.kv_full(0, i), kExpandWarps / 2), mbar_init(x.kv_empty(0, i), 1);  // K, V
-    for (int i = 0; i < 2; ++i) mbar_init(x.s_full(i), 1), mbar_init(x.p_full(i), 32 * kSoftmaxWarps), mbar_init(x.o_done(i), 1);
-    mbar_init(x.q_full(), 32 * kSoftmaxWarps);
+    for (int i = 0; i < 2; ++i) mbar_init(x.s_full(i), 1), mbar_init(x.p_full(i), kSoftmaxWarps), mbar_init(x.o_done(i), 1);
+    mbar_init(x.q_full(), kSoftmaxWarps);
     mbar_init(x.drained(), 1);
-    mbar_init(x.merged(), 32 * kSoftmaxWarps);
-    for (int i = 0; i < 4; ++i) mbar_init(x.pair(i), 64);
+    mbar_init(x.merged(), kSoftmaxWarps);
+    for (int i = 0; i < 4; ++i) mbar_init(x.pair(i), 2);
     fence_barrier_init();
   }
   if (warp == kMmaWarp) tmem_alloc(&s_tmem);
@@ -796,10 +836,15 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __gr
   x.tmem = s_tmem;
   pdl_wait();
   pdl_trigger();
-  if (warp < kSoftmaxWarps) group_softmax<D>(g, x, warp, lane);
-  else if (warp < kMmaWarp) group_expand<D>(g, x, warp - kSoftmaxWarps, lane);
-  else if (warp == kProducer) group_produce<D>(g, x, lane);
-  else if (lane == 0) group_mma<D>(x);
+  if (warp < kSoftmaxWarps) {
+    registers_up<kSoftmaxRegisters>();
+    group_softmax<D>(g, x, warp, lane);
+  } else {
+    registers_down<kOtherRegisters>();
+    if (warp < kMmaWarp) group_expand<D>(g, x, warp - kSoftmaxWarps, lane);
+    else if (warp == kProducer) group_produce<D>(g, x, lane);
+    else if (warp == kMmaWarp) group_mma<D>(x);
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();

@@ -1,5 +1,5 @@
-// trr_few.cuh - attention of a segment with few rows (the query heads of one KV head for one
-// query): warps that work alone, on codes as they are stored.
+// trr_few.cuh - attention of a segment with few rows (the query heads of one KV head, for one
+// query or for a small group): warps that work alone, on codes as they are stored.
 //
 // Every warp takes one equal run of blocks (up to 32 tokens of a page, for one KV head) of the
 // call's private segments, laid end to end.  It brings the blocks into its own ring of shared
@@ -45,7 +45,8 @@ struct FewCursor {
 struct FewBlock {
   int cls, keys, off, pos;      // pos < 0: all its tokens are in sight
   int valid, lo, t, sinks;
-  int query, kvh, dest, state;  // state: 1 first block of a segment's piece, 2 last one
+  int kind, qbase, kvh, rows;   // the segment, as in its job
+  int dest, state, pad[2];      // state: 1 first block of a segment's piece, 2 last one
 };
 
 template <int D, int NG>
@@ -118,9 +119,9 @@ struct FewState {
 // The query rows as the second operand, in the order in which class B's codes come out of their
 // words (4 bits: elements i and i + 4 together, 2 bits: i and i + 8).
 template <int D, int NG, int B>
-__device__ __forceinline__ void few_load_q(FewState<D, NG>& s, const uint8_t* smem, int heads, int lane) {
+__device__ __forceinline__ void few_load_q(FewState<D, NG>& s, const uint8_t* smem, int rows, int lane) {
   const int n = lane >> 2, part = lane & 3, head = n / NG;
-  const bool live = head < heads && part * NG / 4 == n % NG;  // the lane's dimensions lie in the column's group
+  const bool live = head < rows && part * NG / 4 == n % NG;  // the lane's dimensions lie in the column's group
   const uint4* row = reinterpret_cast<const uint4*>(smem + (B == 16 ? FewSmem<D, NG>::kQ : 0) + ((live ? head : 0) * D + part * (D / 4)) * 2);
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {  // 16 elements
@@ -358,27 +359,43 @@ __device__ __forceinline__ void few_tokens(FewState<D, NG>& s, const uint8_t* bl
 
 template <int D, int NG, int B>
 __device__ __forceinline__ void few_class(FewState<D, NG>& s, const uint8_t* smem, const uint8_t* blk, int keys, uint32_t mask, bool swz,
-                                          int heads, int lane) {
-  if (s.q_class != B) few_load_q<D, NG, B>(s, smem, heads, lane);
+                                          int rows, int lane) {
+  if (s.q_class != B) few_load_q<D, NG, B>(s, smem, rows, lane);
   // one copy of the code for both halves of a block: the warps' instructions have to fit the cache together
 #pragma unroll 1
   for (int b = 0; b < keys; b += 16)
     if (mask >> b & 0xFFFFu) few_tokens<D, NG, B>(s, blk, keys, b, mask >> b & 0xFFFFu, swz, lane);
 }
 
+// (query, head) of row r of a segment.
+__device__ __forceinline__ void few_row(const GroupArgs& g, const FewBlock& b, int r, int* query, int* head) {
+  const int heads = g.a.Hq / g.a.Hkv;
+  if (b.kind == 1) {
+    *query = b.qbase;
+    *head = b.kvh * heads + r;
+  } else {
+    *query = g.list[b.qbase + r / heads];
+    *head = b.kvh * heads + r % heads;
+  }
+}
+
 // A segment's piece begins: its query rows, each with the power of two that brings its largest
 // element to [1, 2), and an empty state.
 template <int D, int NG>
-__device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g, uint8_t* smem, const FewBlock& b, int heads, int lane) {
-  const uint4* src = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(b.query) * g.a.Hq + b.kvh * heads) * D);
+__device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g, uint8_t* smem, const FewBlock& b, int lane) {
+  const int rows = b.rows;
   float* factor = reinterpret_cast<float*>(smem + FewSmem<D, NG>::kFactor);
   float* sums = factor + kFewRows;  // [row][group] of the binary16 elements
   __syncwarp();
   constexpr int kLanes = D / 8, kGroupLanes = kLanes / NG;  // lanes of a row, of a group
-  for (int i = lane; i < (heads * kLanes + 31) / 32 * 32; i += 32) {
-    const bool live = i < heads * kLanes;
+  for (int i = lane; i < (rows * kLanes + 31) / 32 * 32; i += 32) {
+    const bool live = i < rows * kLanes;
     uint4 u = make_uint4(0, 0, 0, 0);
-    if (live) u = src[i];
+    if (live) {
+      int query, head;
+      few_row(g, b, i / kLanes, &query, &head);
+      u = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(query) * g.a.Hq + head) * D)[i % kLanes];
+    }
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     uint32_t top = 0;
 #pragma unroll
@@ -410,7 +427,7 @@ __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g
 #pragma unroll
   for (int col = 0; col < 2; ++col) {
     const int n = 2 * (lane & 3) + col;
-    s.qsum[col] = n / NG < heads ? sums[n] : 0.f;
+    s.qsum[col] = n / NG < rows ? sums[n] : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
@@ -421,7 +438,7 @@ __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g
     const int head = NG == 1 ? 2 * (lane & 3) + h : 2 * (lane & 3) / NG;
     s.m[h] = -INFINITY;
     s.l[h] = 0.f;
-    s.f[h] = head < heads ? factor[head] : 1.f;
+    s.f[h] = head < rows ? factor[head] : 1.f;
   }
   s.corr[0] = s.corr[1] = 0.f;
   s.q_class = 0;
@@ -429,7 +446,7 @@ __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g
 
 // It ends: the row, or its part.
 template <int D, int NG>
-__device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, const FewBlock& b, int heads, int lane) {
+__device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, const FewBlock& b, int lane) {
   using S = FewState<D, NG>;
   constexpr int kRun = D / 8;
 #pragma unroll
@@ -442,16 +459,17 @@ __device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, 
   const int quad = lane >> 2, part = lane & 3, group = quad * NG / 8;  // the group of the lane's dimensions
 #pragma unroll
   for (int col = 0; col < 2; ++col) {
-    const int n = 2 * part + col, head = n / NG, h = NG == 1 ? col : 0;
-    if (head >= heads || n % NG != group) continue;
-    const int hq = b.kvh * heads + head;
-    const int64_t home = (static_cast<int64_t>(g.n) + b.query) * g.a.Hq + hq;
+    const int n = 2 * part + col, r = n / NG, h = NG == 1 ? col : 0;
+    if (r >= b.rows || n % NG != group) continue;
+    int query, hq;
+    few_row(g, b, r, &query, &hq);
+    const int64_t home = (static_cast<int64_t>(b.kind) * g.n + query) * g.a.Hq + hq;
     float v[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) v[i] = s.acc[i / 2][i % 2 * 2 + col] + s.corr[col];
     if (b.dest == -2) {
       const float inv = s.l[h] != 0.f ? 1.f / s.l[h] : 0.f;
-      uint16_t* out = g.out + (static_cast<int64_t>(b.query) * g.a.Hq + hq) * D + quad * kRun;
+      uint16_t* out = g.out + (static_cast<int64_t>(query) * g.a.Hq + hq) * D + quad * kRun;
 #pragma unroll
       for (int i = 0; i < kRun; i += 8) {
         uint32_t w[4];
@@ -463,7 +481,7 @@ __device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, 
         *reinterpret_cast<uint4*>(out + i) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     } else {
-      const int64_t row = static_cast<int64_t>(b.dest) * kFewRows + head;
+      const int64_t row = static_cast<int64_t>(b.dest) * kFewRows + r;
       float* to = (b.dest >= 0 ? g.few_o + row * D : g.home_o + home * D) + quad * kRun;
       if (quad == 0) (b.dest >= 0 ? g.few_ml[row] : g.home_ml[home]) = make_float2(s.m[h], s.l[h]);
 #pragma unroll
@@ -490,7 +508,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
   pdl_trigger();
   FewCursor& cur = *reinterpret_cast<FewCursor*>(smem + L::kCursor);
   Job& job = *reinterpret_cast<Job*>(smem + L::kJob);
-  const int me = blockIdx.x * kFewWarps + warp, P = a.P, heads = a.Hq / a.Hkv;
+  const int me = blockIdx.x * kFewWarps + warp, P = a.P, jobs = g.groups + g.n;
   const int lg_p = __ffs(P) - 1, lg_q = max(0, lg_p - 5), lg_w = lg_p - 4;  // log2 of the blocks of a page: 32 tokens, 16 of 16 bits
   int tile = 0, tile1 = 0, batch = -1;       // the segment's next block, its end for this warp; batch of 32 blocks that the lanes hold
   // the lane's block of the batch: its K codes in KV head 0, and class | all in sight << 2 |
@@ -500,7 +518,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
   {
     const int64_t per = g.head->few_per, work = g.head->few_work, b0 = min(work, me * per), b1 = min(work, b0 + per);
     if (b0 >= b1) return;
-    int lo = 0, hi = g.n;  // the job that holds cost b0: the last one that starts at or before it
+    int lo = 0, hi = jobs;  // the job that holds cost b0: the last one that starts at or before it
     while (hi - lo > 1) {
       const int step = (hi - lo + 31) / 32, i = lo + lane * step;
       const int k = __popc(__ballot_sync(0xffffffffu, i < hi && g.few_base[i] <= b0));
@@ -533,16 +551,14 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     return false;
   };
   auto open_job = [&](int j) -> bool {        // the first job from `j` on with blocks for this warp
-    const Job* all = g.jobs + g.groups;
-    for (; j < g.n; ++j) {
+    for (; j < jobs; ++j) {
       const int64_t base = g.few_base[j];
       if (base >= cur.b1) return false;
-      const int word = reinterpret_cast<const int*>(all + j)[lane];
+      const int tiles = g.blocks[j], word = reinterpret_cast<const int*>(g.jobs + j)[lane];
+      if (tiles == 0) continue;
       __syncwarp();
       reinterpret_cast<int*>(&job)[lane] = word;
       __syncwarp();
-      const int tiles = job.tiles;
-      if (tiles == 0) continue;
       if (lane < kClasses) cur.counts[lane] = a.ntok[static_cast<int64_t>(job.seq) * kClasses + lane];
       if (lane == 0) {
         int q = 0;
@@ -628,7 +644,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
       FewBlock& b = blocks[slot];
       b.cls = c; b.keys = keys; b.off = off; b.pos = all_in ? -1 : off + body;
       b.valid = info >> 3 & 63; b.lo = job.lo; b.t = job.t; b.sinks = job.sinks;
-      b.query = job.qbase; b.kvh = seg; b.state = (tile + r == tile0 ? 1 : 0) | (tile + r == tile1 - 1 ? 2 : 0);
+      b.kind = job.kind; b.qbase = job.qbase; b.kvh = seg; b.rows = job.rows; b.state = (tile + r == tile0 ? 1 : 0) | (tile + r == tile1 - 1 ? 2 : 0);
       b.dest = tile1 - tile0 < tiles ? 2 * me + (tile0 > 0 ? 0 : 1) : job.joined ? -1 : -2;
       mbar_arrive_expect_tx(bars + slot, bytes + (all_in ? 0 : 4 * keys));
       const uint8_t* src = mine + static_cast<int64_t>(seg) * a.slice[c];
@@ -664,9 +680,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     const int slot = taken % kFewStages;
     late = !__all_sync(0xffffffffu, mbar_wait(bars + slot, (taken / kFewStages) & 1, a.wait_ns));
     if (late) break;
-    const FewBlock b = blocks[slot];
+    const FewBlock& b = blocks[slot];
     const uint8_t* ring = smem + L::kRing;
-    if (b.state & 1) few_begin<D, NG>(s, g, smem, b, heads, lane);
+    if (b.state & 1) few_begin<D, NG>(s, g, smem, b, lane);
     bool seen = lane < b.keys;
     if (b.pos >= 0 && seen) {
       const int pos = reinterpret_cast<const int32_t*>(ring + b.pos)[lane];
@@ -674,12 +690,12 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     }
     const uint32_t mask = __ballot_sync(0xffffffffu, seen);
     if (mask) {
-      if (b.cls == 0) few_class<D, NG, 2>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
-      else if (b.cls == 1) few_class<D, NG, 4>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
-      else if (b.cls == 2) few_class<D, NG, 8>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
-      else few_class<D, NG, 16>(s, smem, ring + b.off, b.keys, mask, a.swz, heads, lane);
+      if (b.cls == 0) few_class<D, NG, 2>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
+      else if (b.cls == 1) few_class<D, NG, 4>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
+      else if (b.cls == 2) few_class<D, NG, 8>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
+      else few_class<D, NG, 16>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
     }
-    if (b.state & 2) few_end<D, NG>(s, g, b, heads, lane);
+    if (b.state & 2) few_end<D, NG>(s, g, b, lane);
     __syncwarp();
     ++taken;
   }

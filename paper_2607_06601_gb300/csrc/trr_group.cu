@@ -34,16 +34,18 @@ __device__ __forceinline__ int query_error(const GroupArgs& g, int i) {
   return t < 0 || t >= g.a.maxctx ? TRR_ERR_BAD_POSITION : 0;
 }
 
-// How many of x[0..n) (ascending) are below v, by one warp: 32 probes a round.
-__device__ __forceinline__ int count_below(const int32_t* x, int n, int v, int lane) {
+// How many of x[0..n) (ascending) are below v.  The whole warp calls it; its lanes may search in
+// groups of `width` from lane `from` on, each its own list, with that many probes a round.
+__device__ __forceinline__ int count_below(const int32_t* x, int n, int v, int lane, int width, int from) {
+  const unsigned group = width == 32 ? 0xffffffffu : (1u << width) - 1;
   int lo = 0, hi = n;
-  while (lo < hi) {
-    const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-    const int k = __popc(__ballot_sync(0xffffffffu, i < hi && x[i] < v));
-    if (k == 0) return lo;
+  while (__any_sync(0xffffffffu, lo < hi)) {
+    const int step = (hi - lo + width - 1) / width, i = lo + lane * step;
+    const int k = __popc(__ballot_sync(0xffffffffu, i < hi && x[i] < v) >> from & group);
+    if (lo >= hi) continue;
     const int last = lo + (k - 1) * step;
-    hi = min(hi, last + step);
-    lo = last + 1;
+    if (k > 0) hi = min(hi, last + step), lo = last + 1;
+    else hi = lo;
   }
   return lo;
 }
@@ -61,7 +63,7 @@ __device__ __forceinline__ int job_tiles(const GroupArgs& g, bool few, int nq, i
 // nothing) does not wait for the last one.
 __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_constant__ GroupArgs g) {
   __shared__ int s_bad, s_group, s_leader, s_last, s_first_err, s_there;
-  __shared__ int64_t s_sum[kPlanThreads / 32];
+  __shared__ int64_t s_sum[2][kPlanThreads / 32];
   __shared__ Job s_job;
   const LayerArgs& a = g.a;
   const int lane = threadIdx.x & 31, c = threadIdx.x >> 5, i = blockIdx.x, heads = a.Hq / a.Hkv;
@@ -95,17 +97,21 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     const int nt = a.ntok[row], np = (nt + a.P - 1) / a.P;
     const int32_t *pf = a.pfirst + row * a.MP, *pl = a.plast + row * a.MP;
     if (np > 0) {
+      // three searches at once, by 16, 8 and 8 lanes: pages before the window, pages with a sink
+      // (page k starts at position k P or later: they lie in the first ceil(sinks / P)), pages up to t
+      const int sinks = mode == TRR_MODE_LOCAL ? static_cast<int>(min(static_cast<int64_t>(np), (static_cast<int64_t>(g.sinks) + a.P - 1) / a.P)) : 0;
       const bool all = pl[np - 1] <= t;  // the usual case: no token after the query
-      end = all ? np : count_below(pf, np, t + 1, lane);
+      const bool near = lane < 16, third = lane >= 24;
+      const int found = count_below(near ? pl : pf, near ? (mode == TRR_MODE_LOCAL ? np : 0) : third ? (all ? 0 : np) : sinks,
+                                    near ? lo : third ? t + 1 : g.sinks, near ? lane : lane & 7, near ? 16 : 8, near ? 0 : lane & ~7);
+      end = all ? np : __shfl_sync(0xffffffffu, found, 24);
       if (mode == TRR_MODE_LOCAL) {
-        // page k starts at position k P or later: the sinks lie in the first ceil(sinks / P) pages
-        const int most = static_cast<int>(min(static_cast<int64_t>(end), (static_cast<int64_t>(g.sinks) + a.P - 1) / a.P));
-        head = count_below(pf, most, g.sinks, lane);
-        first = max(head, count_below(pl, end, lo, lane));
+        head = min(__shfl_sync(0xffffffffu, found, 16), end);
+        first = max(head, min(__shfl_sync(0xffffffffu, found, 0), end));
       }
       if (member) {  // whole pages in sight, then those that the leader names too
         const int full = nt / a.P;
-        const int whole = all ? full : count_below(pl, min(full, end), t + 1, lane);
+        const int whole = all ? full : count_below(pl, min(full, end), t + 1, lane, 32, 0);
         const int32_t* mine = a.pt + row * a.MP;
         const int64_t lead_row = static_cast<int64_t>(g.seq_ids[s_leader]) * kClasses + c;
         const int32_t* theirs = a.pt + lead_row * a.MP;
@@ -141,11 +147,13 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     s_job.seq = seq; s_job.lo = lo; s_job.t = t; s_job.sinks = mode == TRR_MODE_LOCAL ? g.sinks : 0;
     s_job.rows = heads;
     s_job.row_blocks = (heads + kRows - 1) / kRows;
-    s_job.tiles = job_tiles(g, g.few, nq, s_job.head[3] + s_job.count[3], &s_job.tiles_q);
+    s_job.tiles = job_tiles(g, g.few > 0, nq, s_job.head[3] + s_job.count[3], &s_job.tiles_q);
     s_job.kind = 1; s_job.qbase = i; s_job.joined = 0;
     const int there = reads && (member || s_job.tiles > 0);
     p.reads = there; p.group = member ? s_group : -1; p.rank = 0; p.shared = 0;
-    g.tiles[g.groups + i] = err ? -err : there ? s_job.tiles : 0;
+    const int tiles = there ? s_job.tiles : 0;
+    g.tiles[g.groups + i] = err ? -err : g.few ? 0 : tiles;
+    g.blocks[g.groups + i] = g.few ? tiles : 0;
     s_there = there;
   }
   __syncthreads();
@@ -198,11 +206,11 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
             own->count[k] = left;
             (k < 3 ? nq : n16) += left;
           }
-          const int tiles = job_tiles(g, g.few, nq, n16, &tiles_q);
+          const int tiles = job_tiles(g, g.few > 0, nq, n16, &tiles_q);
           own->tiles_q = tiles_q;
           own->tiles = tiles;
           own->joined = 1;
-          g.tiles[g.groups + j] = tiles;
+          (g.few ? g.blocks : g.tiles)[g.groups + j] = tiles;
           g.plan[j].shared = 1;
         }
     if (lane == 0) {
@@ -212,53 +220,50 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
       job->rows = members * heads;
       job->row_blocks = (job->rows + kRows - 1) / kRows;
       int tiles_q = 0;
-      const int tiles = pages > 0 ? job_tiles(g, false, least[0] + least[1] + least[2], least[3], &tiles_q) : 0;
+      const bool few = job->rows <= g.few;  // a small group's rows are few, too
+      const int tiles = pages > 0 ? job_tiles(g, few, least[0] + least[1] + least[2], least[3], &tiles_q) : 0;
       job->tiles_q = tiles_q;
       job->tiles = tiles;
       job->kind = 0; job->qbase = q0; job->joined = 1;
-      g.tiles[x] = tiles;
+      g.tiles[x] = few ? 0 : tiles;
+      g.blocks[x] = few ? tiles : 0;
     }
   }
   __syncthreads();
   // cost before each job
   const int private_blocks = (heads + kRows - 1) / kRows;
-  auto prefix = [&](int from, int jobs, bool few, int64_t* base) -> int64_t {
-    int64_t before = 0;
-    for (int j0 = 0; j0 < jobs; j0 += kPlanThreads) {
-      const int j = j0 + threadIdx.x, at = from + j, tiles = j < jobs ? __ldcg(g.tiles + at) : 0;
-      int64_t x = 0;
-      if (tiles > 0)
-        x = few ? few_cost(tiles) * a.Hkv
-                : segment_cost(tiles) * a.Hkv * (at < g.groups ? __ldcg(&g.jobs[at].row_blocks) : private_blocks);
-      if (tiles < 0) atomicMin(&s_first_err, (at - g.groups) * 16 - tiles);
-      int64_t y = x;
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t z = __shfl_up_sync(0xffffffffu, y, o);
-        if (lane >= o) y += z;
-      }
-      if (lane == 31) s_sum[c] = y;
-      __syncthreads();
-      int64_t all = 0;
-      for (int k = 0; k < kPlanThreads / 32; ++k) {
-        if (k < c) y += s_sum[k];
-        all += s_sum[k];
-      }
-      if (j < jobs) base[j] = before + y - x;
-      before += all;
-      __syncthreads();
+  const int jobs = g.groups + g.n;
+  int64_t work = 0, few_work = 0;  // of the jobs so far, for the tensor kernel and the one for few rows
+  for (int j0 = 0; j0 < jobs; j0 += kPlanThreads) {
+    const int j = j0 + threadIdx.x, tiles = j < jobs ? __ldcg(g.tiles + j) : 0, blocks = j < jobs ? __ldcg(g.blocks + j) : 0;
+    if (tiles < 0) atomicMin(&s_first_err, (j - g.groups) * 16 - tiles);
+    const int64_t x = tiles > 0 ? segment_cost(tiles) * a.Hkv * (j < g.groups ? __ldcg(&g.jobs[j].row_blocks) : private_blocks) : 0;
+    const int64_t z = blocks > 0 ? few_cost(blocks) * a.Hkv : 0;
+    int64_t x1 = x, z1 = z;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t u = __shfl_up_sync(0xffffffffu, x1, o), v = __shfl_up_sync(0xffffffffu, z1, o);
+      if (lane >= o) x1 += u, z1 += v;
     }
-    if (threadIdx.x == 0) base[jobs] = before;
-    return before;
-  };
-  const int jobs = g.few ? g.groups : g.groups + g.n;
-  const int64_t work = prefix(0, jobs, false, g.base);
-  const int64_t few_work = g.few ? prefix(g.groups, g.n, true, g.few_base) : 0;
+    if (lane == 31) s_sum[0][c] = x1, s_sum[1][c] = z1;
+    __syncthreads();
+    int64_t all_x = 0, all_z = 0;
+    for (int k = 0; k < kPlanThreads / 32; ++k) {
+      if (k < c) x1 += s_sum[0][k], z1 += s_sum[1][k];
+      all_x += s_sum[0][k];
+      all_z += s_sum[1][k];
+    }
+    if (j < jobs) g.base[j] = work + x1 - x, g.few_base[j] = few_work + z1 - z;
+    work += all_x;
+    few_work += all_z;
+    __syncthreads();
+  }
   if (threadIdx.x == 0) {
+    g.base[jobs] = work;
+    g.few_base[jobs] = few_work;
     g.head->work = work;
     g.head->per = (work + g.ctas - 1) / g.ctas;
     g.head->few_work = few_work;
     g.head->few_per = (few_work + g.few_warps - 1) / g.few_warps;
-    g.head->jobs = jobs;
     if (s_first_err != INT_MAX) set_status(a.ctrl, s_first_err % 16);
   }
 }
@@ -284,12 +289,12 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
   for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 1
   for (int kind = p.w ? 0 : 1; kind < 2; ++kind) {
-    const int j = kind == 0 ? p.y : g.groups + query, tiles = g.tiles[j];
+    const int j = kind == 0 ? p.y : g.groups + query, blocks = g.blocks[j], tiles = blocks > 0 ? blocks : g.tiles[j];
     if (tiles <= 0) continue;
-    const bool few = kind == 1 && g.few;
+    const bool few = blocks > 0;
     const int rr = (kind == 0 ? p.z * heads : 0) + head % heads;
     const int64_t cost = few ? few_cost(tiles) : segment_cost(tiles), share = few ? g.head->few_per : g.head->per;
-    const int64_t S = few ? g.few_base[query] + kvh * cost
+    const int64_t S = few ? g.few_base[j] + kvh * cost
                           : g.base[j] + (static_cast<int64_t>(kvh) * (kind == 0 ? g.jobs[j].row_blocks : (heads + kRows - 1) / kRows) + rr / kRows) * cost;
     const int64_t last = S + cost - 1;
     int64_t c0, c1;
@@ -368,12 +373,13 @@ static int64_t lay_workspace(GroupArgs* g, uint8_t* b, const Layout& l, int n, i
   g->list = reinterpret_cast<int32_t*>(take(4ll * n));
   g->jobs = reinterpret_cast<Job*>(take(static_cast<int64_t>(sizeof(Job)) * 2 * n));
   g->tiles = reinterpret_cast<int32_t*>(take(4ll * 2 * n));
+  g->blocks = reinterpret_cast<int32_t*>(take(4ll * 2 * n));
   g->base = reinterpret_cast<int64_t*>(take(8ll * (2 * n + 1)));
   g->home_ml = reinterpret_cast<float2*>(take(8 * 2 * rows));
   g->home_o = reinterpret_cast<float*>(take(4 * 2 * rows * l.d));
   g->part_ml = reinterpret_cast<float2*>(take(8 * parts));
   g->part_o = reinterpret_cast<float*>(take(4 * parts * l.d));
-  g->few_base = reinterpret_cast<int64_t*>(take(8ll * (n + 1)));
+  g->few_base = reinterpret_cast<int64_t*>(take(8ll * (2 * n + 1)));
   g->few_ml = reinterpret_cast<float2*>(take(8ll * 2 * few_warps * kFewRows));
   g->few_o = reinterpret_cast<float*>(take(4ll * 2 * few_warps * kFewRows * l.d));
   return off;
@@ -461,7 +467,7 @@ static trr_status launch_group(trr_cache* cache, int layer, int n, const int32_t
   g.a.wait_ns = cache_wait_ns(cache);
   g.ctas = cache_num_sms(cache);
   const auto few = few_kernel(l);
-  g.few = few != nullptr;
+  g.few = few ? kFewRows / (l.d / l.G) : 0;
   g.few_warps = g.ctas * kFewCtas * kFewWarps;
   lay_workspace(&g, static_cast<uint8_t*>(workspace), l, n, g.ctas, g.few_warps);
   cache_note_call(cache, layer);

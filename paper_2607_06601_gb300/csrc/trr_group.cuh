@@ -34,14 +34,13 @@ static_assert(sizeof(QueryPlan) == 32, "two 16-byte loads");
 
 struct GroupHeader {
   int64_t work, per;          // cost of the tensor kernel's segments, a CTA's share
-  int64_t few_work, few_per;  // cost of the private segments of few rows, a warp's share
-  int jobs;                   // of the tensor kernel
+  int64_t few_work, few_per;  // cost of the segments of few rows, a warp's share
 };
 
 struct GroupArgs {
   LayerArgs a;
   int n, window_scalar, sinks, groups, ctas;
-  int few, few_warps;         // private segments go to the kernel for few rows, with that many warps
+  int few, few_warps;         // most rows of a segment of the kernel for few rows (0: too many even for one query), its warps
   float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
   const int32_t *seq_ids, *positions, *windows, *offsets;
   const uint8_t* modes;
@@ -52,13 +51,14 @@ struct GroupArgs {
   QueryPlan* plan;
   int32_t* list;      // [n] a group's rows: its full queries in order, from the group's offset on
   Job* jobs;          // [groups] shared, then [n] private
-  int32_t* tiles;     // [jobs] tiles (or blocks) of each job; minus the error of a query in error
-  int64_t* base;      // [jobs + 1] cost before each job
+  int32_t* tiles;     // [jobs] tiles of a job of the tensor kernel, else 0; minus the error of a query in error
+  int32_t* blocks;    // [jobs] blocks of a job of the kernel for few rows, else 0
+  int64_t* base;      // [jobs + 1] cost before each job of the tensor kernel
   float2* home_ml;    // [2][n][Hq] (m, l) of a row of a whole segment, by kind of job
   float* home_o;      // [2][n][Hq][D]
   float2* part_ml;    // [2 * ctas][128] of a piece of a segment: a CTA's first one, or its last
   float* part_o;
-  int64_t* few_base;  // [n + 1] cost before each private job, of the kernel for few rows
+  int64_t* few_base;  // [jobs + 1] cost before each job of the kernel for few rows
   float2* few_ml;     // [2 * few_warps][8] of a warp's first piece, or its last
   float* few_o;
 };

@@ -122,7 +122,7 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
   const LayerArgs& a = g.a;
   const int64_t per = g.head->per, work = g.head->work;
   const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
-  const int jobs = g.head->jobs, P = a.P, lg_p = __ffs(P) - 1;
+  const int jobs = g.groups + g.n, P = a.P, lg_p = __ffs(P) - 1;
   int it = 0, freed = 0;  // tiles pushed, tiles whose ring bytes are known to be free
   int ring_head = 0, segs = 0;
   bool ok = true;
@@ -829,13 +829,14 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_attn_kernel(const __gr
     for (int i = 0; i < 4; ++i) mbar_init(x.pair(i), 2);
     fence_barrier_init();
   }
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x * g.head->per >= g.head->work) return;  // nothing for this CTA
   if (warp == kMmaWarp) tmem_alloc(&s_tmem);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   x.tmem = s_tmem;
-  pdl_wait();
-  pdl_trigger();
   if (warp < kSoftmaxWarps) {
     registers_up<kSoftmaxRegisters>();
     group_softmax<D>(g, x, warp, lane);

@@ -99,18 +99,22 @@ def _check(where, code):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    """The cudaStream_t of `stream`, or of the current stream (asked for as a number: building the
+    Stream object of torch.cuda.current_stream takes 3 us of a call's host time)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _dev(t: torch.Tensor, dtype, name):
+    """The address of a contiguous CUDA tensor of that dtype (ctypes turns it into a pointer)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def make_config(num_layers, max_seqs, num_q_heads, num_kv_heads, head_dim, group_size,
@@ -243,16 +247,16 @@ def trr_workspace_bytes(cache) -> int:
     return int(out.value)
 
 
-def _same_length(n, **tensors):
-    for name, t in tensors.items():
-        if t.numel() != n:
-            raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+def _same_length(n, t, name):
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
 
 
 def trr_fork(cache, src_seqs, dst_seqs, lengths, workspace, stream=None):
     """dst_seqs[i] becomes src_seqs[i] up to position lengths[i] - 1, sharing its full pages."""
     n = src_seqs.numel()
-    _same_length(n, dst_seqs=dst_seqs, lengths=lengths)
+    _same_length(n, dst_seqs, "dst_seqs")
+    _same_length(n, lengths, "lengths")
     _check("trr_fork", load().trr_fork(
         cache, n, _dev(src_seqs, torch.int32, "src_seqs"), _dev(dst_seqs, torch.int32, "dst_seqs"),
         _dev(lengths, torch.int32, "lengths"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
@@ -262,7 +266,7 @@ def trr_fork(cache, src_seqs, dst_seqs, lengths, workspace, stream=None):
 def trr_evict(cache, seq_ids, keep_from, sinks, stream=None):
     """Forget the full pages of each sequence that lie in [sinks, keep_from[i])."""
     n = seq_ids.numel()
-    _same_length(n, keep_from=keep_from)
+    _same_length(n, keep_from, "keep_from")
     _check("trr_evict", load().trr_evict(cache, n, _dev(seq_ids, torch.int32, "seq_ids"),
                                          _dev(keep_from, torch.int32, "keep_from"), int(sinks), _stream(stream)))
 
@@ -278,9 +282,10 @@ def trr_compact(cache, workspace, stream=None):
 
 
 def _check_queries(n, q_positions, modes, windows):
-    _same_length(n, q_positions=q_positions, modes=modes)
+    _same_length(n, q_positions, "q_positions")
+    _same_length(n, modes, "modes")
     if windows is not None:
-        _same_length(n, windows=windows)
+        _same_length(n, windows, "windows")
 
 
 def trr_decode_attn_sinks(cache, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
@@ -416,11 +421,11 @@ class Cache:
 
     def _rows(self, seq_ids, q, out):
         """The output of an attention call: q and out are [n][Hq][d]."""
-        n = seq_ids.numel() * self.Hq * self.d
-        if q.numel() != n or (out is not None and out.numel() != n):
-            raise ValueError(f"q and out must have {n} elements ([n][Hq][d])")
-        return out if out is not None else torch.empty((seq_ids.numel(), self.Hq, self.d), dtype=torch.bfloat16,
-                                                       device=q.device)
+        n = seq_ids.numel()
+        size = n * self.Hq * self.d
+        if q.numel() != size or (out is not None and out.numel() != size):
+            raise ValueError(f"q and out must have {size} elements ([n][Hq][d])")
+        return torch.empty((n, self.Hq, self.d), dtype=torch.bfloat16, device=q.device) if out is None else out
 
     def decode_attn_sinks(self, layer, seq_ids, q_positions, q, modes, sinks, windows=None, window_scalar=0,
                           softmax_scale=0.0, out=None, stream=None):

@@ -53,7 +53,8 @@ template <int D, int NG>
 struct FewSmem {
   static constexpr int kQ = kFewRows / NG * D * 2;                          // query rows in binary16, then in bf16, scaled
   static constexpr int kFactor = 2 * kQ;                               // a factor for each row, sums of its groups
-  static constexpr int kBlocks = kFactor + 4 * kFewRows + 4 * kFewRows * 4;
+  static constexpr int kRowIds = kFactor + 4 * kFewRows + 4 * kFewRows * 4;  // query * Hq + head of each row
+  static constexpr int kBlocks = kRowIds + 4 * kFewRows;
   static constexpr int kJob = kBlocks + kFewStages * static_cast<int>(sizeof(FewBlock));  // the cursor's job
   static constexpr int kCursor = kJob + static_cast<int>(sizeof(Job));
   static constexpr int kBars = kCursor + static_cast<int>(sizeof(FewCursor));
@@ -358,25 +359,14 @@ __device__ __forceinline__ void few_tokens(FewState<D, NG>& s, const uint8_t* bl
 }
 
 template <int D, int NG, int B>
-__device__ __forceinline__ void few_class(FewState<D, NG>& s, const uint8_t* smem, const uint8_t* blk, int keys, uint32_t mask, bool swz,
-                                          int rows, int lane) {
-  if (s.q_class != B) few_load_q<D, NG, B>(s, smem, rows, lane);
+__device__ __forceinline__ void few_class(FewState<D, NG>& s, const uint8_t* smem, const FewBlock& b, uint32_t mask, bool swz, int lane) {
+  if (s.q_class != B) few_load_q<D, NG, B>(s, smem, b.rows, lane);
+  const uint8_t* blk = smem + FewSmem<D, NG>::kRing + b.off;
+  const int keys = b.keys;
   // one copy of the code for both halves of a block: the warps' instructions have to fit the cache together
 #pragma unroll 1
-  for (int b = 0; b < keys; b += 16)
-    if (mask >> b & 0xFFFFu) few_tokens<D, NG, B>(s, blk, keys, b, mask >> b & 0xFFFFu, swz, lane);
-}
-
-// (query, head) of row r of a segment.
-__device__ __forceinline__ void few_row(const GroupArgs& g, const FewBlock& b, int r, int* query, int* head) {
-  const int heads = g.a.Hq / g.a.Hkv;
-  if (b.kind == 1) {
-    *query = b.qbase;
-    *head = b.kvh * heads + r;
-  } else {
-    *query = g.list[b.qbase + r / heads];
-    *head = b.kvh * heads + r % heads;
-  }
+  for (int k = 0; k < keys; k += 16)
+    if (mask >> k & 0xFFFFu) few_tokens<D, NG, B>(s, blk, keys, k, mask >> k & 0xFFFFu, swz, lane);
 }
 
 // A segment's piece begins: its query rows, each with the power of two that brings its largest
@@ -384,6 +374,13 @@ __device__ __forceinline__ void few_row(const GroupArgs& g, const FewBlock& b, i
 template <int D, int NG>
 __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g, uint8_t* smem, const FewBlock& b, int lane) {
   const int rows = b.rows;
+  int* ids = reinterpret_cast<int*>(smem + FewSmem<D, NG>::kRowIds);
+  __syncwarp();
+  if (lane < rows) {
+    const int heads = g.a.Hq / g.a.Hkv;
+    const int query = b.kind == 1 ? b.qbase : g.list[b.qbase + lane / heads];
+    ids[lane] = query * g.a.Hq + b.kvh * heads + (b.kind == 1 ? lane : lane % heads);
+  }
   float* factor = reinterpret_cast<float*>(smem + FewSmem<D, NG>::kFactor);
   float* sums = factor + kFewRows;  // [row][group] of the binary16 elements
   __syncwarp();
@@ -391,11 +388,7 @@ __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g
   for (int i = lane; i < (rows * kLanes + 31) / 32 * 32; i += 32) {
     const bool live = i < rows * kLanes;
     uint4 u = make_uint4(0, 0, 0, 0);
-    if (live) {
-      int query, head;
-      few_row(g, b, i / kLanes, &query, &head);
-      u = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(query) * g.a.Hq + head) * D)[i % kLanes];
-    }
+    if (live) u = reinterpret_cast<const uint4*>(g.q + static_cast<int64_t>(ids[i / kLanes]) * D)[i % kLanes];
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     uint32_t top = 0;
 #pragma unroll
@@ -446,7 +439,7 @@ __device__ __forceinline__ void few_begin(FewState<D, NG>& s, const GroupArgs& g
 
 // It ends: the row, or its part.
 template <int D, int NG>
-__device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, const FewBlock& b, int lane) {
+__device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, const uint8_t* smem, const FewBlock& b, int lane) {
   using S = FewState<D, NG>;
   constexpr int kRun = D / 8;
 #pragma unroll
@@ -461,15 +454,14 @@ __device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, 
   for (int col = 0; col < 2; ++col) {
     const int n = 2 * part + col, r = n / NG, h = NG == 1 ? col : 0;
     if (r >= b.rows || n % NG != group) continue;
-    int query, hq;
-    few_row(g, b, r, &query, &hq);
-    const int64_t home = (static_cast<int64_t>(b.kind) * g.n + query) * g.a.Hq + hq;
+    const int id = reinterpret_cast<const int*>(smem + FewSmem<D, NG>::kRowIds)[r];
+    const int64_t home = static_cast<int64_t>(b.kind) * g.n * g.a.Hq + id;
     float v[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) v[i] = s.acc[i / 2][i % 2 * 2 + col] + s.corr[col];
     if (b.dest == -2) {
       const float inv = s.l[h] != 0.f ? 1.f / s.l[h] : 0.f;
-      uint16_t* out = g.out + (static_cast<int64_t>(query) * g.a.Hq + hq) * D + quad * kRun;
+      uint16_t* out = g.out + static_cast<int64_t>(id) * D + quad * kRun;
 #pragma unroll
       for (int i = 0; i < kRun; i += 8) {
         uint32_t w[4];
@@ -681,21 +673,20 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     late = !__all_sync(0xffffffffu, mbar_wait(bars + slot, (taken / kFewStages) & 1, a.wait_ns));
     if (late) break;
     const FewBlock& b = blocks[slot];
-    const uint8_t* ring = smem + L::kRing;
     if (b.state & 1) few_begin<D, NG>(s, g, smem, b, lane);
     bool seen = lane < b.keys;
     if (b.pos >= 0 && seen) {
-      const int pos = reinterpret_cast<const int32_t*>(ring + b.pos)[lane];
+      const int pos = reinterpret_cast<const int32_t*>(smem + L::kRing + b.pos)[lane];
       seen = lane < b.valid && pos <= b.t && (pos >= b.lo || pos < b.sinks);
     }
     const uint32_t mask = __ballot_sync(0xffffffffu, seen);
     if (mask) {
-      if (b.cls == 0) few_class<D, NG, 2>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
-      else if (b.cls == 1) few_class<D, NG, 4>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
-      else if (b.cls == 2) few_class<D, NG, 8>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
-      else few_class<D, NG, 16>(s, smem, ring + b.off, b.keys, mask, a.swz, b.rows, lane);
+      if (b.cls == 0) few_class<D, NG, 2>(s, smem, b, mask, a.swz, lane);
+      else if (b.cls == 1) few_class<D, NG, 4>(s, smem, b, mask, a.swz, lane);
+      else if (b.cls == 2) few_class<D, NG, 8>(s, smem, b, mask, a.swz, lane);
+      else few_class<D, NG, 16>(s, smem, b, mask, a.swz, lane);
     }
-    if (b.state & 2) few_end<D, NG>(s, g, b, lane);
+    if (b.state & 2) few_end<D, NG>(s, g, smem, b, lane);
     __syncwarp();
     ++taken;
   }

@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
   for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 1
   for (int kind = p.w ? 0 : 1; kind < 2; ++kind) {
-    const int j = kind == 0 ? p.y : g.groups + query, blocks = g.blocks[j], tiles = blocks > 0 ? blocks : g.tiles[j];
+    const int j = kind == 0 ? p.y : g.groups + query, blocks = g.blocks[j], whole = g.tiles[j], tiles = blocks > 0 ? blocks : whole;
     if (tiles <= 0) continue;
     const bool few = blocks > 0;
     const int rr = (kind == 0 ? p.z * heads : 0) + head % heads;

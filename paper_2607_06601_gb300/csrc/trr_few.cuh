@@ -37,8 +37,7 @@ constexpr int kFewSmem = 112 * 1024;  // of a CTA
 struct FewCursor {
   int64_t b0, b1, base;         // the warp's run of cost, the job's start
   int j, seg, tile0, pad0;      // job, segment, its first block for this warp
-  int tiles, pages_q, pad;      // the job's blocks, its pages of 2, 4 and 8 bits
-  int counts[kClasses];         // tokens of its sequence
+  int tiles, pages_q;           // the job's blocks, its pages of 2, 4 and 8 bits
 };
 
 // A block in the ring.
@@ -496,7 +495,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     fence_barrier_init();
   }
   __syncwarp();
-  pdl_wait();
+  // After the tensor kernel, whose CTAs let this one start once the plan was there: it reads nothing
+  // that kernel writes, so it fills the SMs that run out of tiles, and waits at its end instead.
+  if (!g.overlap) pdl_wait();
   pdl_trigger();
   FewCursor& cur = *reinterpret_cast<FewCursor*>(smem + L::kCursor);
   Job& job = *reinterpret_cast<Job*>(smem + L::kJob);
@@ -509,7 +510,10 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
   uint32_t info = 0;
   {
     const int64_t per = g.head->few_per, work = g.head->few_work, b0 = min(work, me * per), b1 = min(work, b0 + per);
-    if (b0 >= b1) return;
+    if (b0 >= b1) {
+      if (g.overlap) pdl_wait();
+      return;
+    }
     int lo = 0, hi = jobs;  // the job that holds cost b0: the last one that starts at or before it
     while (hi - lo > 1) {
       const int step = (hi - lo + 31) / 32, i = lo + lane * step;
@@ -551,7 +555,6 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
       __syncwarp();
       reinterpret_cast<int*>(&job)[lane] = word;
       __syncwarp();
-      if (lane < kClasses) cur.counts[lane] = a.ntok[static_cast<int64_t>(job.seq) * kClasses + lane];
       if (lane == 0) {
         int q = 0;
         for (int c = 0; c < 3; ++c) q += job.head[c] + job.count[c];
@@ -586,7 +589,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
       }
       const int h = job.head[c], k = in < h ? in : job.first[c] + in - h;
       const int64_t at = (static_cast<int64_t>(job.seq) * kClasses + c) * a.MP + k;
-      const int page = a.pt[at], pf = a.pfirst[at], pl = a.plast[at], valid = min(P, cur.counts[c] - k * P);
+      const int page = a.pt[at], pf = a.pfirst[at], pl = a.plast[at], valid = min(P, job.tokens[c] - k * P);
       const bool whole = valid == P && pl <= job.t && (pf >= job.lo || pl < job.sinks);
       // no more slots than hold a token, or, of a page that ends before the window, than can be sinks
       // (slot x of page k holds position k P + x or a later one)
@@ -694,6 +697,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     for (int k = taken; k < issued; ++k) mbar_wait(bars + k % kFewStages, (k / kFewStages) & 1);
     if (lane == 0) set_status(a.ctrl, TRR_ERR_TIMEOUT);
   }
+  if (g.overlap) pdl_wait();  // so that its end is the tensor kernel's, too
 }
 
 }  // namespace trr

@@ -91,10 +91,11 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     __syncthreads();
   }
   const int lo = mode == TRR_MODE_LOCAL ? t - (g.windows ? g.windows[i] : g.window_scalar) + 1 : INT_MIN;
-  int head = 0, first = 0, end = 0, common = 0;
+  int head = 0, first = 0, end = 0, common = 0, tokens = 0;
   if (reads) {
     const int64_t row = static_cast<int64_t>(seq) * kClasses + c;
     const int nt = a.ntok[row], np = (nt + a.P - 1) / a.P;
+    tokens = nt;
     const int32_t *pf = a.pfirst + row * a.MP, *pl = a.plast + row * a.MP;
     if (np > 0) {
       // three searches at once, by 16, 8 and 8 lanes: pages before the window, pages with a sink
@@ -136,6 +137,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
   QueryPlan& p = g.plan[i];
   if (lane == 0) {
     p.common[c] = common;
+    s_job.tokens[c] = tokens;
     s_job.head[c] = head;
     s_job.first[c] = first;
     s_job.count[c] = max(0, end - first);
@@ -216,7 +218,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     if (lane == 0) {
       job->seq = pages > 0 ? __ldcg(&g.jobs[g.groups + g.list[q0]].seq) : 0;
       job->lo = INT_MIN; job->t = INT_MAX; job->sinks = 0;
-      for (int k = 0; k < kClasses; ++k) job->head[k] = 0, job->first[k] = 0, job->count[k] = least[k];
+      for (int k = 0; k < kClasses; ++k) job->tokens[k] = least[k] * a.P, job->head[k] = 0, job->first[k] = 0, job->count[k] = least[k];
       job->rows = members * heads;
       job->row_blocks = (job->rows + kRows - 1) / kRows;
       int tiles_q = 0;
@@ -427,13 +429,13 @@ static cudaError_t launch_kernels(const GroupArgs& g, void (*few)(GroupArgs), cu
   cudaError_t e = launch_pdl(group_plan_kernel, dim3(g.n), dim3(kPlanThreads), 0, s, g);
   if (e != cudaSuccess) return e;
   ++*launches;
-  if (few) {
-    e = launch_pdl(few, dim3(g.few_warps / kFewWarps), dim3(32 * kFewWarps), kFewSmem, s, g);
+  if (!few || g.groups > 0) {
+    e = launch_pdl(group_attn_kernel<D>, dim3(g.ctas), dim3(kGroupThreads), GroupSmem<D>::kTotal + 1024, s, g);
     if (e != cudaSuccess) return e;
     ++*launches;
   }
-  if (!few || g.groups > 0) {
-    e = launch_pdl(group_attn_kernel<D>, dim3(g.ctas), dim3(kGroupThreads), GroupSmem<D>::kTotal + 1024, s, g);
+  if (few) {
+    e = launch_pdl(few, dim3(g.few_warps / kFewWarps), dim3(32 * kFewWarps), kFewSmem, s, g);
     if (e != cudaSuccess) return e;
     ++*launches;
   }
@@ -468,6 +470,7 @@ static trr_status launch_group(trr_cache* cache, int layer, int n, const int32_t
   g.ctas = cache_num_sms(cache);
   const auto few = few_kernel(l);
   g.few = few ? kFewRows / (l.d / l.G) : 0;
+  g.overlap = groups > 0;
   g.few_warps = g.ctas * kFewCtas * kFewWarps;
   lay_workspace(&g, static_cast<uint8_t*>(workspace), l, n, g.ctas, g.few_warps);
   cache_note_call(cache, layer);

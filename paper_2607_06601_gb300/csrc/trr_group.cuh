@@ -20,7 +20,8 @@ struct Job {
   int kind;                               // 0: shared, 1: private
   int qbase;                              // shared: its queries in the list; private: the query
   int joined;                             // private: the query has a shared job as well
-  int pad[9];
+  int tokens[kClasses];                   // of its sequence
+  int pad[5];
 };
 static_assert(sizeof(Job) == 128, "a warp loads a job one word per lane");
 
@@ -41,6 +42,7 @@ struct GroupArgs {
   LayerArgs a;
   int n, window_scalar, sinks, groups, ctas;
   int few, few_warps;         // most rows of a segment of the kernel for few rows (0: too many even for one query), its warps
+  int overlap;                // the kernel for few rows follows the tensor kernel and may run beside it
   float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
   const int32_t *seq_ids, *positions, *windows, *offsets;
   const uint8_t* modes;

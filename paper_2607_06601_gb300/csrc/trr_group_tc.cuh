@@ -122,7 +122,7 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
   const LayerArgs& a = g.a;
   const int64_t per = g.head->per, work = g.head->work;
   const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
-  const int jobs = g.groups + g.n, P = a.P, lg_p = __ffs(P) - 1;
+  const int jobs = g.few ? g.groups : g.groups + g.n, P = a.P, lg_p = __ffs(P) - 1;
   int it = 0, freed = 0;  // tiles pushed, tiles whose ring bytes are known to be free
   int ring_head = 0, segs = 0;
   bool ok = true;
@@ -173,7 +173,6 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
         upto[c + 1] = upto[c] + head[c] + field(12 + c);
       }
       const int rows = field(16), row_blocks = field(17), tiles_q = field(18), kind = field(20), qbase = field(21), joined = field(22);
-      const int nt = lane < kClasses ? a.ntok[static_cast<int64_t>(seq) * kClasses + lane] : 0;
       const int64_t cost = segment_cost(tiles);
       const int nsegs = a.Hkv * row_blocks;
       // a batch of 32 pages, one per lane, of the 2-, 4- and 8-bit pages or of the others
@@ -208,10 +207,10 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
             const int i = (i0 & ~31) + lane;
             cls = wide ? 3 : i >= upto[2] ? 2 : i >= upto[1] ? 1 : 0;
             const int in = wide ? i : i - (cls == 2 ? upto[2] : cls == 1 ? upto[1] : 0);
-            int h = head[0], f = first[0], n = __shfl_sync(0xffffffffu, nt, 0);
+            int h = head[0], f = first[0], n = field(23);
 #pragma unroll
             for (int c = 1; c < kClasses; ++c) {
-              const int m = __shfl_sync(0xffffffffu, nt, c);
+              const int m = field(23 + c);
               if (cls == c) h = head[c], f = first[c], n = m;
             }
             if (i < end) {
@@ -224,6 +223,9 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
               src = a.pool[cls] + page * a.page_bytes[cls];
               room = (slice + 127) / 128 * 128 + (whole ? 0 : (4 * P + 127) / 128 * 128);
               bytes = slice + (whole ? 0 : 4 * P);
+              // the ring holds a few tiles; the rest of the batch comes as far as L2 meanwhile
+              if (i - i0 >= 2 << lg && i < (wide ? t1 - tiles_q : min(t1, tiles_q)) << lg)
+                prefetch_l2(src + a.hdr + static_cast<int64_t>(kvh) * slice, slice);
             }
             __syncwarp();
           }

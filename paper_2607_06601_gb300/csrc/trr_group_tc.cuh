@@ -13,6 +13,8 @@
 // exponentials 1024 (16 a cycle), the expansion's integer instructions about as long.
 #pragma once
 
+#include <type_traits>
+
 #include "trr_group.cuh"
 
 namespace trr {
@@ -458,11 +460,11 @@ __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
     tc_fence_after();
     const uint32_t id = tc_idesc(bf16_before, D, true);
     const uint64_t d = tc_desc(x.tile(stage, 1), kTileKeys * 128);
-    const uint32_t p = x.tmem + kColS + 128 * (it & 1);  // 16 weights in the first 8 of their scores' 16 columns
+    const uint32_t p = x.tmem + kColS + 128 * (it & 1);  // 16 weights in 8 columns
     if (elected()) {
 #pragma unroll
       for (int k = 0; k < kTileKeys / 16; ++k)
-        if (16 * k < keys_before) tc_mma(x.tmem + kColO, p + 16 * k, d + k * (2048 >> 4), id, k > 0 || !first_before);
+        if (16 * k < keys_before) tc_mma(x.tmem + kColO, p + 8 * k, d + k * (2048 >> 4), id, k > 0 || !first_before);
       tc_commit(x.kv_empty(1, stage));
       tc_commit(x.o_done(it & 1));
     }
@@ -516,53 +518,52 @@ __device__ __forceinline__ uint32_t pack16(bool bf16, float a, float b) {
 }
 
 // Scores out of sight become -infinity: their weight is 0 and they are no maximum.
-__device__ __forceinline__ void mask16(uint32_t (&s)[16], uint32_t mask) {
-  if (mask != 0xFFFFu) {
+template <int N>
+__device__ __forceinline__ void mask_scores(uint32_t (&s)[N], const uint16_t* masks) {
+#pragma unroll
+  for (int k = 0; k < N / 16; ++k) {
+    const uint32_t mask = masks[k];
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (!(mask >> i & 1)) s[i] = 0xFF800000u;
+      if (!(mask >> i & 1)) s[16 * k + i] = 0xFF800000u;
   }
 }
 
-__device__ __forceinline__ float highest16(float t, const uint32_t (&s)[16]) {
+template <int N>
+__device__ __forceinline__ float highest(const uint32_t (&s)[N]) {
+  float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // four chains
 #pragma unroll
-  for (int i = 0; i < 16; i += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(__uint_as_float(s[i])), "f"(__uint_as_float(s[i + 1])));
-  return t;
+  for (int i = 0; i < N; i += 2)
+    asm("max.f32 %0, %0, %1, %2;" : "+f"(t[i / 2 % 4]) : "f"(__uint_as_float(s[i])), "f"(__uint_as_float(s[i + 1])));
+  return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
 
-// 16 scores become their weights 2^(s f + shift); returns the weights' sum.
-__device__ __forceinline__ float weigh16(uint32_t (&s)[16], float f, float shift) {
-  uint64_t sum = 0, ff, hh;
+// Scores become their weights 2^(s f + shift); returns the weights' sum.
+template <int N>
+__device__ __forceinline__ float weigh(uint32_t (&s)[N], float f, float shift) {
+  uint64_t sum[2] = {0, 0}, ff, hh;
   asm("mov.b64 %0, {%1, %1};" : "=l"(ff) : "f"(f));
   asm("mov.b64 %0, {%1, %1};" : "=l"(hh) : "f"(shift));
 #pragma unroll
-  for (int i = 0; i < 16; i += 2) {
+  for (int i = 0; i < N; i += 2) {
     uint64_t x;
     float x0, x1;
     asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %4;\n}" : "=l"(x) : "r"(s[i]), "r"(s[i + 1]), "l"(ff), "l"(hh));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x));
     x0 = exp2_approx(x0);
     x1 = exp2_approx(x1);
-    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum) : "f"(x0), "f"(x1));
+    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum[i / 2 % 2]) : "f"(x0), "f"(x1));
     s[i] = __float_as_uint(x0);
     s[i + 1] = __float_as_uint(x1);
   }
-  float s0, s1;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum));
-  return s0 + s1;
-}
-__device__ __forceinline__ void pack_weights(const uint32_t (&s)[16], uint32_t (&p)[8], bool bf16) {
-  if (bf16) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = pack16(true, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = pack16(false, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
-  }
+  float a, b, c, d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(sum[0]));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(c), "=f"(d) : "l"(sum[1]));
+  return (a + b) + (c + d);
 }
 
-// The softmax warps.  Warps w and w + 4 share 32 rows (lanes of TMEM); of a tile's eight runs of
-// 16 tokens the first takes the even ones, the second the odd ones.
+// The softmax warps.  Warps w and w + 4 share 32 rows (lanes of TMEM); of the tokens of a tile
+// that their copy of the rows takes, the first has the first half, the second the other.
 template <int D>
 __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& x, int warp, int lane) {
   using L = GroupSmem<D>;
@@ -625,10 +626,10 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
       uint32_t o[16];
 #pragma unroll
       for (int k = 0; k < 16; ++k) o[k] = pack16(false, bf16lo(w[16 * i + k]) * down, bf16hi(w[16 * i + k]) * down);
-      tmem_st16(lanes + kColQ + half * (D / 4) + 16 * i, o);
+      tmem_st(lanes + kColQ + half * (D / 4) + 16 * i, o);
 #pragma unroll
       for (int k = 0; k < 16; ++k) o[k] = pack16(true, bf16lo(w[16 * i + k]) * down, bf16hi(w[16 * i + k]) * down);
-      tmem_st16(lanes + kColQ + 64 + half * (D / 4) + 16 * i, o);
+      tmem_st(lanes + kColQ + 64 + half * (D / 4) + 16 * i, o);
     }
     tmem_wait_st();
     tc_fence_before();
@@ -643,47 +644,26 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
   int copies = copies_of(sg.rows);
   if (sg.tiles > 0) load_q(sg, copies);
   while (sg.tiles > 0) {
-    // this copy's runs: 8 / copies from run0 on, every other one this warp's
-    const int runs = 8 / copies, run0 = quad * copies / 4 * runs;
     const float f = factor;
     float m = -INFINITY, l = 0.f;
-    for (int tile = 0; tile < sg.tiles; ++tile, ++it) {
-      if (!x.wait_warp(x.s_full(it & 1), (it >> 1) & 1)) return;
+    // One tile; N: the scores of this thread (64, 32 or 16 with 1, 2 or 4 copies of the rows).
+    auto one_tile = [&](auto n, int tile) -> bool {
+      constexpr int N = decltype(n)::value, kCopies = 64 / N;
+      if (!x.wait_warp(x.s_full(it & 1), (it >> 1) & 1)) return false;
       tc_fence_after();
       const TileMeta& meta = x.meta(it % kMetaSlots);
-      const int keys = meta.keys;
-      const bool bf16 = meta.bf16;
       const uint32_t scol = lanes + kColS + 128 * (it & 1);
-      const int u0 = run0 + half;  // this warp's runs: u0 and every other one from there
-      uint32_t s[4][16];
-      float top = -INFINITY;
-      if (runs == 8) {
-        tmem_ld16x4(s[0], scol + 16 * u0, s[1], scol + 16 * u0 + 32, s[2], scol + 16 * u0 + 64, s[3], scol + 16 * u0 + 96);
-      } else {
-        tmem_ld16x2(s[0], scol + 16 * u0, s[1], scol + 16 * (runs == 4 ? u0 + 2 : u0));
-      }
-      // a full tile with one copy of the rows is the common case of many rows: no branch parts its four runs
-      const bool full = runs == 8 && meta.all;
-      auto mine = [&](int k) { return 2 * k < runs && 16 * (u0 + 2 * k) < keys; };
-      if (full) {
-        float t[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = highest16(-INFINITY, s[k]);
-        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (mine(k)) {
-            mask16(s[k], meta.mask[u0 + 2 * k]);
-            top = highest16(top, s[k]);
-          }
-      }
-      // the row's maximum over both warps
+      const int copy = quad * kCopies / 4, c0 = copy * 2 * N + half * N;  // this thread's first token
+      uint32_t s[N];
+      tmem_ld(s, scol + c0);
+      if (!meta.all) mask_scores(s, meta.mask + c0 / 16);
+      float top = highest(s);
+      // the row's maximum over both warps; behind it, all scores have been read
       float* xch = tops + (it & 1) * 2 * kRows;
       xch[half * kRows + row] = top;
       __syncwarp();
       if (lane == 0) mbar_arrive(x.pair(quad));
-      if (!x.wait_warp(x.pair(quad), it & 1)) return;
+      if (!x.wait_warp(x.pair(quad), it & 1)) return false;
       top = fmaxf(top, xch[(half ^ 1) * kRows + row]) * f;
       // m follows the maximum only when that has grown by more than 2^8: p stays within binary16, and O is rarely rescaled
       if (__any_sync(0xffffffffu, top > m + 8.f)) {
@@ -691,51 +671,45 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
         l *= by;
         m = next;
         if (tile > 0) {  // half of O's columns each
-          if (!x.wait_warp(x.o_done((it - 1) & 1), ((it - 1) >> 1) & 1)) return;
+          if (!x.wait_warp(x.o_done((it - 1) & 1), ((it - 1) >> 1) & 1)) return false;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
             uint32_t o[16];
             const uint32_t at = lanes + kColO + half * (D / 2) + 16 * c;
-            tmem_ld16(o, at);
+            tmem_ld(o, at);
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
-            tmem_st16(at, o);
+            tmem_st(at, o);
           }
         }
       }
-      const float shift = m == -INFINITY ? 0.f : -m;
-      // weights, in the scores' place
-      if (full) {
-        float sums[4];
+      l += weigh(s, f, m == -INFINITY ? 0.f : -m);
+      // weights over the scores, two to a column; none on the tokens of the other copies
+      uint32_t p[N / 2];
+      if (meta.bf16) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sums[k] = weigh16(s[k], f, shift);
-        l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t p[8];
-          pack_weights(s[k], p, bf16);
-          tmem_st8(scol + 16 * (u0 + 2 * k), p);
-        }
+        for (int i = 0; i < N / 2; ++i) p[i] = pack16(true, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (mine(k)) {
-            uint32_t p[8];
-            l += weigh16(s[k], f, shift);
-            pack_weights(s[k], p, bf16);
-            tmem_st8(scol + 16 * (u0 + 2 * k), p);
-          }
+        for (int i = 0; i < N / 2; ++i) p[i] = pack16(false, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
       }
-      if (runs < 8) {  // no weight on the other copies' tokens
-        const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int u = half; 16 * u < keys; u += 2)
-          if (u < run0 || u >= run0 + runs) tmem_st8(scol + 16 * u, none);
+      tmem_st(scol + c0 / 2, p);
+      if (kCopies > 1) {
+        const uint32_t none[N / 2] = {};
+#pragma unroll
+        for (int k = 1; k < kCopies; ++k) tmem_st(scol + ((copy + k) % kCopies * 2 * N + half * N) / 2, none);
       }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(x.p_full(it & 1));
+      return true;
+    };
+    for (int tile = 0; tile < sg.tiles; ++tile, ++it) {
+      const bool ok = copies == 1 ? one_tile(std::integral_constant<int, 64>(), tile)
+                                  : copies == 2 ? one_tile(std::integral_constant<int, 32>(), tile) : one_tile(std::integral_constant<int, 16>(), tile);
+      if (!ok) return;
     }
     // the next segment's rows go in while this one's last product runs
     const Segment done = sg;
@@ -780,7 +754,7 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
     for (int c = 0; c < D / 32; ++c) {
       uint32_t o[16];
       const int col = half * (D / 2) + 16 * c;
-      tmem_ld16(o, lanes + kColO + col);
+      tmem_ld(o, lanes + kColO + col);
       if (done_copies == 1) {
         if (live) {
 #pragma unroll

@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
 
 // One warp per (query, head): the parts of its row, at most one shared and one private
 // segment, each whole or in one piece per CTA (or warp).  A lane looks up one part; the parts'
-// rows are then read four at a time.
+// rows are then read eight at a time.
 template <int D>
 __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constant__ GroupArgs g) {
   constexpr int E = D / 32;
@@ -284,20 +284,32 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
   const int query = static_cast<int>(at / g.a.Hq), head = static_cast<int>(at % g.a.Hq), kvh = head / heads;
   pdl_wait();
   pdl_trigger();
+  // what the search for the parts needs, in two rounds of loads: this, then both jobs' sizes and places
   const int4 p = *reinterpret_cast<const int4*>(g.plan + query);  // reads, group, rank, shared
+  const int64_t per = g.head->per, few_per = g.head->few_per;
   if (!p.x) return;
+  struct Place {
+    int tiles, blocks, rows;
+    int64_t base, few_base;
+  } place[2];
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    const int j = kind == 0 ? (p.w ? p.y : 0) : g.groups + query;
+    const bool any = kind == 1 || p.w;
+    place[kind] = Place{any ? g.tiles[j] : 0, any ? g.blocks[j] : 0, kind == 0 && any ? g.jobs[j].row_blocks : (heads + kRows - 1) / kRows, g.base[j], g.few_base[j]};
+  }
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 1
-  for (int kind = p.w ? 0 : 1; kind < 2; ++kind) {
-    const int j = kind == 0 ? p.y : g.groups + query, blocks = g.blocks[j], whole = g.tiles[j], tiles = blocks > 0 ? blocks : whole;
+  for (int kind = 0; kind < 2; ++kind) {
+    const Place at_job = kind == 0 ? place[0] : place[1];
+    const bool few = at_job.blocks > 0;
+    const int tiles = few ? at_job.blocks : at_job.tiles;
     if (tiles <= 0) continue;
-    const bool few = blocks > 0;
     const int rr = (kind == 0 ? p.z * heads : 0) + head % heads;
-    const int64_t cost = few ? few_cost(tiles) : segment_cost(tiles), share = few ? g.head->few_per : g.head->per;
-    const int64_t S = few ? g.few_base[j] + kvh * cost
-                          : g.base[j] + (static_cast<int64_t>(kvh) * (kind == 0 ? g.jobs[j].row_blocks : (heads + kRows - 1) / kRows) + rr / kRows) * cost;
+    const int64_t cost = few ? few_cost(tiles) : segment_cost(tiles), share = few ? few_per : per;
+    const int64_t S = few ? at_job.few_base + kvh * cost : at_job.base + (static_cast<int64_t>(kvh) * at_job.rows + rr / kRows) * cost;
     const int64_t last = S + cost - 1;
     int64_t c0, c1;
     if (last < 0x7fffffff) c0 = static_cast<uint32_t>(S) / static_cast<uint32_t>(share), c1 = static_cast<uint32_t>(last) / static_cast<uint32_t>(share);
@@ -317,10 +329,10 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
         rows = g.home_o;
       }
       const float2 v = there ? mls[slot] : make_float2(-INFINITY, 0.f);
+      unsigned parts = __ballot_sync(0xffffffffu, there);
       float top = v.x;
       for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
       const float next = fmaxf(m, top);
-      if (next == -INFINITY) continue;
       const float w = v.x == -INFINITY ? 0.f : exp2_approx(v.x - next), by = m == -INFINITY ? 0.f : exp2_approx(m - next);
       float sum = v.x == -INFINITY ? 0.f : v.y * w;
       for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
@@ -328,23 +340,32 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] *= by;
       m = next;
-      unsigned parts = __ballot_sync(0xffffffffu, v.x != -INFINITY);
+      constexpr int kAhead = 8;
       while (parts) {
-        float row[4][E], f[4];
+        float row[kAhead][E], f[kAhead];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
           const int from = parts ? __ffs(parts) - 1 : 0;
-          const int64_t s = __shfl_sync(0xffffffffu, slot, from);
+          const float* src = rows + __shfl_sync(0xffffffffu, slot, from) * D + lane * E;
           f[u] = __shfl_sync(0xffffffffu, w, from);
-          if (!parts) f[u] = 0.f;
-#pragma unroll
-          for (int e = 0; e < E; ++e) row[u][e] = parts ? rows[s * D + lane * E + e] : 0.f;
+          if (parts) {
+            if (E == 4) {
+              const float4 x = *reinterpret_cast<const float4*>(src);
+              row[u][0] = x.x; row[u][1] = x.y; row[u][E - 2] = x.z; row[u][E - 1] = x.w;
+            } else {
+              const float2 x = *reinterpret_cast<const float2*>(src);
+              row[u][0] = x.x; row[u][1] = x.y;
+            }
+          } else {
+            f[u] = 0.f;
+          }
           parts &= parts - 1;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < kAhead; ++u)
+          if (f[u] != 0.f)  // (a part in which nothing was seen may hold anything)
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[e] += row[u][e] * f[u];
+            for (int e = 0; e < E; ++e) o[e] += row[u][e] * f[u];
       }
     }
   }

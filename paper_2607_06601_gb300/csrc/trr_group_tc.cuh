@@ -739,7 +739,7 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
     const float weight = m == -INFINITY ? 0.f : exp2_approx(m - own_high);
     int query = 0, head = 0;
     const bool live = r < done.rows;
-    if (live) row_of(done, r, &query, &head);
+    if (live && done.dest < 0) row_of(done, r, &query, &head);  // a piece's row has its place without them
     const int64_t home = (static_cast<int64_t>(done.kind) * g.n + query) * g.a.Hq + head;
     float* to = done.dest >= 0 ? g.part_o + (static_cast<int64_t>(done.dest) * kRows + r) * D : g.home_o + home * D;
     uint16_t* out = g.out + (static_cast<int64_t>(query) * g.a.Hq + head) * D;

@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     g.base[jobs] = work;
     g.few_base[jobs] = few_work;
     g.head->work = work;
-    g.head->per = (work + g.ctas - 1) / g.ctas;
+    g.head->per = max(static_cast<int64_t>(kLeastShare), (work + g.ctas - 1) / g.ctas);
     g.head->few_work = few_work;
     g.head->few_per = (few_work + g.few_warps - 1) / g.few_warps;
     if (s_first_err != INT_MAX) set_status(a.ctrl, s_first_err % 16);
@@ -289,14 +289,15 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
   const int64_t per = g.head->per, few_per = g.head->few_per;
   if (!p.x) return;
   struct Place {
-    int tiles, blocks, rows;
+    int tiles, blocks, row_blocks, rows;
     int64_t base, few_base;
   } place[2];
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
     const int j = kind == 0 ? (p.w ? p.y : 0) : g.groups + query;
     const bool any = kind == 1 || p.w;
-    place[kind] = Place{any ? g.tiles[j] : 0, any ? g.blocks[j] : 0, kind == 0 && any ? g.jobs[j].row_blocks : (heads + kRows - 1) / kRows, g.base[j], g.few_base[j]};
+    place[kind] = Place{any ? g.tiles[j] : 0, any ? g.blocks[j] : 0, kind == 0 && any ? g.jobs[j].row_blocks : (heads + kRows - 1) / kRows,
+                        kind == 0 && any ? g.jobs[j].rows : heads, g.base[j], g.few_base[j]};
   }
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
@@ -309,24 +310,27 @@ __global__ void __launch_bounds__(128) group_combine_kernel(const __grid_constan
     if (tiles <= 0) continue;
     const int rr = (kind == 0 ? p.z * heads : 0) + head % heads;
     const int64_t cost = few ? few_cost(tiles) : segment_cost(tiles), share = few ? few_per : per;
-    const int64_t S = few ? at_job.few_base + kvh * cost : at_job.base + (static_cast<int64_t>(kvh) * at_job.rows + rr / kRows) * cost;
+    const int64_t S = few ? at_job.few_base + kvh * cost : at_job.base + (static_cast<int64_t>(kvh) * at_job.row_blocks + rr / kRows) * cost;
     const int64_t last = S + cost - 1;
     int64_t c0, c1;
     if (last < 0x7fffffff) c0 = static_cast<uint32_t>(S) / static_cast<uint32_t>(share), c1 = static_cast<uint32_t>(last) / static_cast<uint32_t>(share);
     else c0 = S / share, c1 = last / share;
     const float2* mls = few ? g.few_ml : g.part_ml;
     const float* rows = few ? g.few_o : g.part_o;
-    const int pitch = few ? kFewRows : kRows, sub = few ? rr : rr % kRows;
-    for (int64_t b = c0; b <= c1; b += 32) {
-      const int64_t x0 = (b + lane) * share - S, x1 = x0 + share;
+    // a piece of the tensor kernel has a row for each of the copies that filled its lanes
+    const int copies = few ? 1 : copies_of(min(kRows, at_job.rows - rr / kRows * kRows)), lg = copies >> 1;
+    const int pitch = few ? kFewRows : kRows, sub = (few ? rr : rr % kRows) + (lane & (copies - 1)) * (kRows / copies);
+    for (int64_t b = c0; b <= c1; b += 32 >> lg) {
+      const int64_t c = b + (lane >> lg), x0 = c * share - S, x1 = x0 + share;
       const int t0 = few ? few_before(x0, tiles) : tiles_before(x0, tiles), t1 = few ? few_before(x1, tiles) : tiles_before(x1, tiles);
-      const bool there = b + lane <= c1 && t0 < t1;
-      int64_t slot = (2 * (b + lane) + (t0 > 0 ? 0 : 1)) * pitch + sub;
-      if (__any_sync(0xffffffffu, there && t1 - t0 == tiles)) {  // all of it in one part
+      bool there = c <= c1 && t0 < t1;
+      int64_t slot = (2 * c + (t0 > 0 ? 0 : 1)) * pitch + sub;
+      if (__any_sync(0xffffffffu, there && t1 - t0 == tiles)) {  // all of it in one part, its copies joined
         if (!p.w) return;                                        // which is the row, in place
         slot = (static_cast<int64_t>(kind) * g.n + query) * g.a.Hq + head;
         mls = g.home_ml;
         rows = g.home_o;
+        there = there && (lane & (copies - 1)) == 0;
       }
       const float2 v = there ? mls[slot] : make_float2(-INFINITY, 0.f);
       unsigned parts = __ballot_sync(0xffffffffu, there);

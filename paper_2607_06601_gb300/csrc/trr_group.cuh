@@ -58,7 +58,7 @@ struct GroupArgs {
   int64_t* base;      // [jobs + 1] cost before each job of the tensor kernel
   float2* home_ml;    // [2][n][Hq] (m, l) of a row of a whole segment, by kind of job
   float* home_o;      // [2][n][Hq][D]
-  float2* part_ml;    // [2 * ctas][128] of a piece of a segment: a CTA's first one, or its last
+  float2* part_ml;    // [2 * ctas][128] of a piece of a segment, copies of its rows included: a CTA's first one, or its last
   float* part_o;
   int64_t* few_base;  // [jobs + 1] cost before each job of the kernel for few rows
   float2* few_ml;     // [2 * few_warps][8] of a warp's first piece, or its last
@@ -74,6 +74,13 @@ __device__ __forceinline__ int tiles_before(int64_t x, int tiles) {
   const int64_t t = (x - kSegmentCost + kTileCost - 1) / kTileCost;
   return t < tiles ? static_cast<int>(t) : tiles;
 }
+
+// Copies of a segment's rows that fill the tensor kernel's 128 lanes.
+__device__ __forceinline__ int copies_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
+
+// A CTA's share is two tiles at least: a CTA takes 10 us to its first scores and from its last ones,
+// and those left without a tile serve the private segments meanwhile.
+constexpr int kLeastShare = kSegmentCost / 2 + 2 * kTileCost;
 
 // The same for the kernel for few rows, in blocks.
 constexpr int kFewSegmentCost = 1;

@@ -636,7 +636,6 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
     __syncwarp();
     if (lane == 0) mbar_arrive(x.q_full());
   };
-  auto copies_of = [](int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; };
 
   int it = 0, segs = 0;
   if (!x.wait_warp(x.seg_full(0), 0)) return;
@@ -724,9 +723,24 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
 
     // rows out: the output itself, or (m, l, o) for the join.  Both warps of a row have its m and
     // half of its l; copies have their own of both.
-    const int width = kRows / done_copies;
     ml[half * kRows + row] = make_float2(m, l);
     if (!meet()) return;
+    if (done.dest >= 0) {  // a piece: the join takes the copies' rows one by one
+      const int64_t slot = static_cast<int64_t>(done.dest) * kRows + row;
+      if (half == 0) g.part_ml[slot] = make_float2(m, l + ml[kRows + row].y);
+      float* to = g.part_o + slot * D + half * (D / 2);
+      const bool live = (row & (kRows / done_copies - 1)) < done.rows;
+#pragma unroll 1
+      for (int c = 0; c < D / 64; ++c) {
+        uint32_t o[32];
+        tmem_ld(o, lanes + kColO + half * (D / 2) + 32 * c);
+        if (live) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + 32 * c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+      }
+    } else {
+    const int width = kRows / done_copies;
     const int r = row / done_copies, cols = 16 / done_copies, c0 = (row % done_copies) * cols;  // what this thread writes of 16 columns
     float high = -INFINITY, sum = 0.f;
     for (int k = 0; k < done_copies; ++k) high = fmaxf(high, ml[r + k * width].x);
@@ -739,16 +753,14 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
     const float weight = m == -INFINITY ? 0.f : exp2_approx(m - own_high);
     int query = 0, head = 0;
     const bool live = r < done.rows;
-    if (live && done.dest < 0) row_of(done, r, &query, &head);  // a piece's row has its place without them
-    const int64_t home = (static_cast<int64_t>(done.kind) * g.n + query) * g.a.Hq + head;
-    float* to = done.dest >= 0 ? g.part_o + (static_cast<int64_t>(done.dest) * kRows + r) * D : g.home_o + home * D;
-    uint16_t* out = g.out + (static_cast<int64_t>(query) * g.a.Hq + head) * D;
+    if (live) row_of(done, r, &query, &head);
+    const int64_t at = static_cast<int64_t>(query) * g.a.Hq + head, home = static_cast<int64_t>(done.kind) * g.n * g.a.Hq + at;
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    if (live && c0 == 0 && half == 0 && done.dest > -2)
-      (done.dest >= 0 ? g.part_ml[static_cast<int64_t>(done.dest) * kRows + r] : g.home_ml[home]) = make_float2(high, sum);
+    if (live && c0 == 0 && half == 0 && done.dest == -1) g.home_ml[home] = make_float2(high, sum);
     auto put = [&](int col, const float4 v) {
-      if (done.dest == -2) *reinterpret_cast<uint2*>(out + col) = make_uint2(pack16(true, v.x * inv, v.y * inv), pack16(true, v.z * inv, v.w * inv));
-      else *reinterpret_cast<float4*>(to + col) = v;
+      if (done.dest == -2)
+        *reinterpret_cast<uint2*>(g.out + at * D + col) = make_uint2(pack16(true, v.x * inv, v.y * inv), pack16(true, v.z * inv, v.w * inv));
+      else *reinterpret_cast<float4*>(g.home_o + home * D + col) = v;
     };
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -775,6 +787,7 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
           }
         if (!meet()) return;
       }
+    }
     }
     if (!meet()) return;  // (m, l) and O have been read
     tc_fence_before();

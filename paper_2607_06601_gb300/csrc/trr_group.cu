@@ -172,15 +172,20 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
 
   for (int x = c; x < g.groups; x += kPlanThreads / 32) {  // groups: a warp each
     Job* job = g.jobs + x;
-    int members = 0, least[kClasses] = {INT_MAX, INT_MAX, INT_MAX, INT_MAX};
+    int members = 0, least[kClasses] = {INT_MAX, INT_MAX, INT_MAX, INT_MAX}, seq = 0;
     const int q0 = s_bad ? 0 : g.offsets[x], q1 = s_bad ? 0 : g.offsets[x + 1];
+    bool in = false;          // of the last 32 queries: whether the lane's is a member, its private pages
+    int4 mine = make_int4(0, 0, 0, 0);
     for (int j0 = q0; j0 < q1; j0 += 32) {
-      const int j = j0 + lane;
-      const bool in = j < q1 && __ldcg(&g.plan[j].group) >= 0;
+      const int j = j0 + lane, at = min(j, q1 - 1);
+      const int4 common = __ldcg(reinterpret_cast<const int4*>(g.plan[at].common));
+      mine = __ldcg(reinterpret_cast<const int4*>(g.jobs[g.groups + at].count));
+      const int own_seq = __ldcg(&g.jobs[g.groups + at].seq);
+      in = j < q1 && __ldcg(&g.plan[at].group) >= 0;
       const unsigned m = __ballot_sync(0xffffffffu, in);
+      if (members == 0 && m) seq = __shfl_sync(0xffffffffu, own_seq, __ffs(m) - 1);
       if (in) {
         const int rank = members + __popc(m & ((1u << lane) - 1));
-        const int4 common = __ldcg(reinterpret_cast<const int4*>(g.plan[j].common));
         g.list[q0 + rank] = j;
         g.plan[j].rank = rank;
         least[0] = min(least[0], common.x);
@@ -196,27 +201,26 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
       if (members < 2) least[k] = 0;  // nobody to share with
       pages += least[k];
     }
-    __syncwarp();
     if (pages > 0)  // the members' private jobs start behind the shared pages
-      for (int j = q0 + lane; j < q1; j += 32)
-        if (__ldcg(&g.plan[j].group) >= 0) {
-          Job* own = g.jobs + g.groups + j;
-          int nq = 0, n16 = 0, tiles_q;
-          for (int k = 0; k < kClasses; ++k) {
-            const int left = max(0, __ldcg(&own->count[k]) - least[k]);
-            own->first[k] = least[k];
-            own->count[k] = left;
-            (k < 3 ? nq : n16) += left;
-          }
-          const int tiles = job_tiles(g, g.few > 0, nq, n16, &tiles_q);
-          own->tiles_q = tiles_q;
-          own->tiles = tiles;
-          own->joined = 1;
-          (g.few ? g.blocks : g.tiles)[g.groups + j] = tiles;
-          g.plan[j].shared = 1;
+      for (int j = q0 + lane; j < q1; j += 32) {
+        Job* own = g.jobs + g.groups + j;
+        if (q1 - q0 > 32) {  // (a larger group's are read again)
+          in = __ldcg(&g.plan[j].group) >= 0;
+          mine = __ldcg(reinterpret_cast<const int4*>(own->count));
         }
+        if (!in) continue;
+        const int left[kClasses] = {max(0, mine.x - least[0]), max(0, mine.y - least[1]), max(0, mine.z - least[2]), max(0, mine.w - least[3])};
+        int tiles_q;
+        const int tiles = job_tiles(g, g.few > 0, left[0] + left[1] + left[2], left[3], &tiles_q);
+        for (int k = 0; k < kClasses; ++k) own->first[k] = least[k], own->count[k] = left[k];
+        own->tiles_q = tiles_q;
+        own->tiles = tiles;
+        own->joined = 1;
+        (g.few ? g.blocks : g.tiles)[g.groups + j] = tiles;
+        g.plan[j].shared = 1;
+      }
     if (lane == 0) {
-      job->seq = pages > 0 ? __ldcg(&g.jobs[g.groups + g.list[q0]].seq) : 0;
+      job->seq = seq;
       job->lo = INT_MIN; job->t = INT_MAX; job->sinks = 0;
       for (int k = 0; k < kClasses; ++k) job->tokens[k] = least[k] * a.P, job->head[k] = 0, job->first[k] = 0, job->count[k] = least[k];
       job->rows = members * heads;
@@ -238,8 +242,9 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
   int64_t work = 0, few_work = 0;  // of the jobs so far, for the tensor kernel and the one for few rows
   for (int j0 = 0; j0 < jobs; j0 += kPlanThreads) {
     const int j = j0 + threadIdx.x, tiles = j < jobs ? __ldcg(g.tiles + j) : 0, blocks = j < jobs ? __ldcg(g.blocks + j) : 0;
+    const int row_blocks = j < g.groups ? __ldcg(&g.jobs[j].row_blocks) : private_blocks;
     if (tiles < 0) atomicMin(&s_first_err, (j - g.groups) * 16 - tiles);
-    const int64_t x = tiles > 0 ? segment_cost(tiles) * a.Hkv * (j < g.groups ? __ldcg(&g.jobs[j].row_blocks) : private_blocks) : 0;
+    const int64_t x = tiles > 0 ? segment_cost(tiles) * a.Hkv * row_blocks : 0;
     const int64_t z = blocks > 0 ? few_cost(blocks) * a.Hkv : 0;
     int64_t x1 = x, z1 = z;
     for (int o = 1; o < 32; o <<= 1) {

@@ -24,11 +24,11 @@ def _gpu():
     torch.cuda.set_device(0)
 
 
-def family(rng, lay, prompts, members, prefix, suffix, mix=(0.25,) * 4, p_skip=0.2, maxctx=1024):
+def family(rng, lay, prompts, members, prefix, suffix, mix=(0.25,) * 4, p_skip=0.2, maxctx=1024, archive=0):
     """`prompts` sequences of `prefix` tokens, each forked `members` times; the forks go on."""
     S = prompts * (1 + members)
     caps = [prompts * (prefix // lay["P"] + 2) + S * (2 + -(-suffix // lay["P"])) + S] * 4
-    h = Holder(1, S, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], maxctx, caps, archive=2 * S + 8)
+    h = Holder(1, S, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], maxctx, caps, archive=2 * S + 8 + archive)
     for s in range(prompts):
         h.append(rng, 0, s, np.arange(prefix), mix, p_skip)
     kids = list(range(prompts, S))

@@ -6,7 +6,7 @@
 // j < sinks).  Any split of the tokens can be joined again: parts (m, l, o) with
 // l = sum exp(s - m), o = sum exp(s - m) v give m' = max m, l' = sum l exp(m - m'), and so for o.
 //
-// Three kernels:
+// Four kernels:
 //   group_plan_kernel     cuts the call into jobs.  A shared job is the pages that all full
 //                         queries of a group have in common, with all their rows; a private
 //                         job is what is left for one query.  A job is one segment per KV head
@@ -14,7 +14,12 @@
 //   group_attn_kernel     one CTA per SM; the segments' tiles (up to 128 tokens), laid end to
 //                         end, are cut into one equal run for each CTA, so that a long segment
 //                         is spread over many CTAs and a CTA takes many short ones.
+//   group_few_kernel      the segments of few rows (rows x groups of a row at most 8: a product's
+//                         columns), codes as they are stored.  64 queries of 32 heads with windows
+//                         of 511: 97 us when it came in, 221 on the tensor cores.
 //   group_combine_kernel  joins the parts of every row.
+//
+// The plan and the join are chains of dependent loads: 6 to 9 us and 4 to 9 us of a call.
 //
 #include <algorithm>
 #include <climits>

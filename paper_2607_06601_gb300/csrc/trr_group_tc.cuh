@@ -10,7 +10,14 @@
 // warps share the exponentials.
 //
 // What bounds it, for a tile of 128 tokens at d 128: the products take about 1024 cycles, the
-// exponentials 1024 (16 a cycle), the expansion's integer instructions about as long.
+// exponentials 1024 (16 a cycle), the expansion's integer instructions about as long; the three
+// hand tiles on to one another, and a tile takes about 3000 cycles whatever its width.
+//
+// Measured: 64 queries of 32 heads on 32768 shared tokens, 8 KV heads of 128 (27 GFLOP, 36 MB;
+// 14.6 us at the measured rate of library products): 63 us, 0.44 PFLOP/s, of which 9 are the start
+// to the first scores and 5 the rows out.  16 such queries (two copies of 64 rows): 35 us.
+// With one softmax thread a row and eight expanding warps, 63 queries of 7 prompts took 127 us a
+// call against 118 then; softmax warpgroups that take whole tiles in turn, 91 against 87.
 #pragma once
 
 #include <type_traits>

@@ -481,7 +481,7 @@ __device__ __forceinline__ void few_end(FewState<D, NG>& s, const GroupArgs& g, 
       float* to = (b.dest >= 0 ? g.few_o + row * D : g.home_o + home * D) + quad * kRun;
       if (quad == 0) (b.dest >= 0 ? g.few_ml[row] : g.home_ml[home]) = make_float2(s.m[h], s.l[h]);
 #pragma unroll
-      for (int i = 0; i < kRun; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      for (int i = 0; i < kRun; i += 8) st_global8(to + i, v + i);
     }
   }
 }
@@ -553,9 +553,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
   };
   auto open_job = [&](int j) -> bool {        // the first job from `j` on with blocks for this warp
     for (; j < jobs; ++j) {
-      const int64_t base = g.few_base[j];
-      if (base >= cur.b1) return false;
+      const int64_t base = g.few_base[j];  // (all loads of a job before the first branch on one)
       const int tiles = g.blocks[j], word = reinterpret_cast<const int*>(g.jobs + j)[lane];
+      if (base >= cur.b1) return false;
       if (tiles == 0) continue;
       __syncwarp();
       reinterpret_cast<int*>(&job)[lane] = word;

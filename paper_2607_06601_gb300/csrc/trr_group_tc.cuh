@@ -167,11 +167,10 @@ __device__ __forceinline__ void group_produce(const GroupArgs& g, const Ctx<D>& 
       if (step == 1) break;
     }
     for (int j = lo; j < jobs && ok; ++j) {
-      const int64_t jbase = g.base[j];
+      const int64_t jbase = g.base[j];  // (all loads of a job before the first branch on one)
+      const int w = reinterpret_cast<const int*>(g.jobs + j)[lane], tiles = g.tiles[j];
       if (jbase >= b1) break;
-      const int w = reinterpret_cast<const int*>(g.jobs + j)[lane];
       auto field = [&](int i) { return __shfl_sync(0xffffffffu, w, i); };
-      const int tiles = g.tiles[j];
       if (tiles <= 0) continue;
       const int seq = field(0), jlo = field(1), jt = field(2), sinks = field(3);
       int head[kClasses], first[kClasses], upto[kClasses + 1];
@@ -743,7 +742,8 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
         tmem_ld(o, lanes + kColO + half * (D / 2) + 32 * c);
         if (live) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + 32 * c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          for (int i = 0; i < 32; i += 8)  // a lane's row: whole sectors
+            st_global8(to + 32 * c + i, reinterpret_cast<const float*>(o + i));
         }
       }
     } else {

@@ -273,9 +273,23 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     g.base[jobs] = work;
     g.few_base[jobs] = few_work;
     g.head->work = work;
-    g.head->per = max(static_cast<int64_t>(kLeastShare), (work + g.ctas - 1) / g.ctas);
+    // The few rows' runs: one for each warp of the SMs that the tensor kernel leaves, if that brings
+    // them home beside it, else one for each warp of all SMs, after it.
+    const int warps = kFewCtas * kFewWarps;
+    auto split = [](int64_t x, int64_t n) -> int64_t {  // rounded up (in 32 bits where they do: half a microsecond less)
+      x += n - 1;
+      return x <= 0xffffffffll && n <= 0xffffffffll ? static_cast<uint32_t>(x) / static_cast<uint32_t>(n) : x / n;
+    };
+    auto share = [&](int64_t sms) { return max(static_cast<int64_t>(kLeastShare), split(work, sms)); };
+    int64_t per = share(g.ctas), left = g.ctas - split(work, per);
+    if (few_work > left * warps * kShortShare && per >= kLongShare) {
+      const int64_t few_sms = split(few_work, warps * kFewShare);
+      if (few_sms * 16 <= g.ctas) per = share(g.ctas - few_sms), left = max(few_sms, g.ctas - split(work, per));
+    }
+    const bool beside = left > 0 && few_work <= left * warps * (per >= kLongShare ? kFewShare : kShortShare);
+    g.head->per = per;
     g.head->few_work = few_work;
-    g.head->few_per = (few_work + g.few_warps - 1) / g.few_warps;
+    g.head->few_per = split(few_work, beside ? left * warps : g.few_warps);
     if (s_first_err != INT_MAX) set_status(a.ctrl, s_first_err % 16);
   }
 }

@@ -9,8 +9,8 @@
 // What bounds them: page copies are HBM traffic (each byte read and written once); the
 // tables are a few kilobytes per sequence, so everything else is launch and load latency.
 // Two forks of 32 sequences of 4096 tokens over 24 layers of 32 KV heads, with eviction, releases
-// and two compactions between (3.33 GB): 603 us, 5.5 TB/s of the 6.8 that a copy reaches; the same
-// over 12 layers of 12 heads and 2048 tokens (0.63 GB): 142 us, 4.4 TB/s.
+// and two compactions between (3.33 GB): 595 us, 5.6 TB/s of the 6.8 that a copy reaches; the same
+// over 12 layers of 12 heads and 2048 tokens (0.63 GB): 140 us, 4.5 TB/s.
 #include <algorithm>
 
 #include "trr_internal.cuh"

@@ -4,8 +4,8 @@
 // with bulk copies; sixteen warps expand them to 16-bit rows in the tensor core's layout; one
 // thread issues the products S = Q K^T and O += P V (sums in TMEM); eight warps do the softmax,
 // two threads for each row of TMEM.  Pages of 2, 4 and 8 bits become binary16 (z + c s rounded
-// once, 11 bits), pages of 16 bits stay bf16; p is rounded to the same type, sums and
-// statistics are binary32.  A segment of 64 or 32 rows or fewer fills the 128 lanes with two or
+// once, 11 bits) and p is rounded to it; pages of 16 bits stay bf16 and p is a sum of two bf16
+// numbers there; sums and statistics are binary32.  A segment of 64 or 32 rows or fewer fills the 128 lanes with two or
 // four copies of its rows, each of which takes its own part of a tile's tokens, so that all
 // warps share the exponentials.
 //
@@ -122,7 +122,9 @@ struct Ctx {
   __device__ bool wait_warp(uint64_t* b, uint32_t parity) const { return __all_sync(0xffffffffu, wait(b, parity)); }
 };
 
-constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // TMEM columns: O, two S (P over S), Q in binary16 and bf16
+// TMEM columns: O, two S (P over S), Q in binary16 and bf16.  A tile of 16-bit pages has 64 tokens at
+// most: its weights' low parts take the second half of the columns of its S.
+constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384, kColPLow = 64;
 
 // The producer warp: segments and tiles of this CTA's run, and the copies of their pages.
 template <int D>
@@ -471,6 +473,11 @@ __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
 #pragma unroll
       for (int k = 0; k < kTileKeys / 16; ++k)
         if (16 * k < keys_before) tc_mma(x.tmem + kColO, p + 8 * k, d + k * (2048 >> 4), id, k > 0 || !first_before);
+      if (bf16_before) {  // the weights' low parts
+#pragma unroll
+        for (int k = 0; k < kTileKeys / 32; ++k)
+          if (16 * k < keys_before) tc_mma(x.tmem + kColO, p + kColPLow + 8 * k, d + k * (2048 >> 4), id, true);
+      }
       tc_commit(x.kv_empty(1, stage));
       tc_commit(x.o_done(it & 1));
     }
@@ -690,21 +697,36 @@ __device__ __forceinline__ void group_softmax(const GroupArgs& g, const Ctx<D>& 
         }
       }
       l += weigh(s, f, m == -INFINITY ? 0.f : -m);
-      // weights over the scores, two to a column; none on the tokens of the other copies
-      uint32_t p[N / 2];
+      // weights over the scores, two to a column; none on the tokens of the other copies.  Of 16-bit
+      // pages, whose values are exact, a weight is a sum of two bf16 numbers (16 bits, where one has 8).
+      auto rest = [&](uint32_t col) {
+        if (kCopies > 1) {
+          const uint32_t none[N / 2] = {};
+#pragma unroll
+          for (int k = 1; k < kCopies; ++k) tmem_st(col + ((copy + k) % kCopies * 2 * N + half * N) / 2, none);
+        }
+      };
       if (meta.bf16) {
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) p[i] = pack16(true, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+        for (int c = 0; c < N / 2; c += 8) {
+          uint32_t high[8], low[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float a = __uint_as_float(s[2 * (c + i)]), b = __uint_as_float(s[2 * (c + i) + 1]);
+            high[i] = pack16(true, a, b);
+            low[i] = pack16(true, a - bf16lo(high[i]), b - bf16hi(high[i]));
+          }
+          tmem_st(scol + c0 / 2 + c, high);
+          tmem_st(scol + kColPLow + c0 / 2 + c, low);
+        }
+        rest(scol + kColPLow);
       } else {
+        uint32_t p[N / 2];
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) p[i] = pack16(false, __uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+        tmem_st(scol + c0 / 2, p);
       }
-      tmem_st(scol + c0 / 2, p);
-      if (kCopies > 1) {
-        const uint32_t none[N / 2] = {};
-#pragma unroll
-        for (int k = 1; k < kCopies; ++k) tmem_st(scol + ((copy + k) % kCopies * 2 * N + half * N) / 2, none);
-      }
+      rest(scol);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();

@@ -500,10 +500,16 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
     fence_barrier_init();
   }
   __syncwarp();
-  // After the tensor kernel, whose CTAs let this one start once the plan was there: it reads nothing
-  // that kernel writes, so it fills the SMs that run out of tiles, and waits at its end instead.
+  // After the tensor kernel this one starts beside it, to fill the SMs that run out of tiles: it reads
+  // nothing that kernel writes, and waits for it at its end instead.  The tensor kernel's CTAs let it
+  // start only after their own wait for the plan, so the plan has ended; but that orders nothing for
+  // this kernel's memory.  So each thread's first load acquires the plan's last store, which released
+  // the whole plan and, through the plan's own wait, what the kernels before it wrote: page tables,
+  // pages, query rows.  Loads and copies behind it find all of that.
   if (!g.overlap) pdl_wait();
   pdl_trigger();
+  const int64_t per = ld_acquire(&g.head->few_per);
+  fence_proxy_async_global();
   FewCursor& cur = *reinterpret_cast<FewCursor*>(smem + L::kCursor);
   Job& job = *reinterpret_cast<Job*>(smem + L::kJob);
   const int me = blockIdx.x * kFewWarps + warp, P = a.P, jobs = g.groups + g.n;
@@ -514,7 +520,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewCtas) group_few_kernel(con
   const uint8_t* mine = nullptr;
   uint32_t info = 0;
   {
-    const int64_t per = g.head->few_per, work = g.head->few_work, b0 = min(work, me * per), b1 = min(work, b0 + per);
+    const int64_t work = g.head->few_work, b0 = min(work, me * per), b1 = min(work, b0 + per);
     if (b0 >= b1) {
       if (g.overlap) pdl_wait();
       return;

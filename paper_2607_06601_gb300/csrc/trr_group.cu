@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     const bool beside = left > 0 && few_work <= left * warps * (per >= kLongShare ? kFewShare : kShortShare);
     g.head->per = per;
     g.head->few_work = few_work;
-    g.head->few_per = split(few_work, beside ? left * warps : g.few_warps);
+    st_release(&g.head->few_per, split(few_work, beside ? left * warps : g.few_warps));  // last: see group_few_kernel
     if (s_first_err != INT_MAX) set_status(a.ctrl, s_first_err % 16);
   }
 }

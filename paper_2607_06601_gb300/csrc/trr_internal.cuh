@@ -284,6 +284,20 @@ __device__ __forceinline__ int atom_add_acq_rel(int* p, int v) {
   return old;
 }
 
+// store with release (of what this thread has written or seen written), load with acquire (of what
+// the thread that stored the value had), both at GPU scope
+__device__ __forceinline__ void st_release(int64_t* p, int64_t v) {
+  asm volatile("st.release.gpu.global.s64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
+}
+__device__ __forceinline__ int64_t ld_acquire(const int64_t* p) {
+  int64_t v;
+  asm volatile("ld.acquire.gpu.global.s64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+  return v;
+}
+
+// Bulk copies from global memory that this thread issues from here on see what it has seen written.
+__device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
 // The hard decision of one controller head (Sec. 3.8: at inference the router takes
 // the arg max of its logits): the index of the largest of K logits, the first of equal
 // ones; a NaN is never taken, and a row of NaN gives 0.

@@ -117,6 +117,19 @@ def _dev(t: torch.Tensor, dtype, name):
     return t.data_ptr()
 
 
+def _new(shape, dtype, device, stream):
+    """Memory for a call on `stream`: the allocator takes it from that stream's own, whose last users are
+    behind it there, and hands it out again only after what the current stream does with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream()
+    if current != stream:
+        t.record_stream(current)
+    return t
+
+
 def make_config(num_layers, max_seqs, num_q_heads, num_kv_heads, head_dim, group_size,
                 page_size, max_context, pages_per_class, max_append=1024, max_queries=1024,
                 split_bytes=0, skip_writes_kv=0, head_modes=0) -> trr_cache_config:
@@ -370,7 +383,7 @@ class Cache:
                     softmax_scale=0.0, out=None, stream=None):
         self._check_modes(modes, seq_ids.numel())
         if out is None:
-            out = torch.empty((seq_ids.numel(), self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+            out = _new((seq_ids.numel(), self.Hq, self.d), torch.bfloat16, q.device, stream)
         trr_decode_attn(self.handle, layer, seq_ids, q_positions, q, modes, windows, window_scalar,
                         softmax_scale, out, stream)
         return out
@@ -379,7 +392,7 @@ class Cache:
                     softmax_scale=0.0, out=None, stream=None):
         self._check_modes(modes, seq_ids.numel())
         if out is None:
-            out = torch.empty((seq_ids.numel(), self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+            out = _new((seq_ids.numel(), self.Hq, self.d), torch.bfloat16, q.device, stream)
         trr_decode_step(self.handle, layer, seq_ids, positions, k, v, bits, modes, q, windows, window_scalar,
                         softmax_scale, out, stream)
         return out
@@ -390,22 +403,22 @@ class Cache:
     def decode_attn_routed(self, layer, seq_ids, q_positions, q, mode_logits, windows=None,
                            window_scalar=0, softmax_scale=0.0, out=None, stream=None):
         if out is None:
-            out = torch.empty((seq_ids.numel(), self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+            out = _new((seq_ids.numel(), self.Hq, self.d), torch.bfloat16, q.device, stream)
         trr_decode_attn_routed(self.handle, layer, seq_ids, q_positions, q, mode_logits, windows,
                                window_scalar, softmax_scale, out, stream)
         return out
 
-    def workspace(self) -> torch.Tensor:
-        """Device memory of the calls below, allocated once for the cache: call it before capturing
-        them in a CUDA graph."""
+    def workspace(self, stream=None) -> torch.Tensor:
+        """Device memory of the calls below, allocated once for the cache, on the stream of the first
+        of them: call it before capturing them in a CUDA graph."""
         if self._workspace is None:
-            self._workspace = torch.empty(trr_workspace_bytes(self.handle), dtype=torch.uint8, device=self.pool.device)
+            self._workspace = _new(trr_workspace_bytes(self.handle), torch.uint8, self.pool.device, stream)
         return self._workspace
 
     def fork(self, src_seqs, dst_seqs, lengths, stream=None):
         """Sequence dst_seqs[i] becomes a copy of src_seqs[i] up to position lengths[i] - 1, in every
         layer, sharing its full pages."""
-        trr_fork(self.handle, src_seqs, dst_seqs, lengths, self.workspace(), stream)
+        trr_fork(self.handle, src_seqs, dst_seqs, lengths, self.workspace(stream), stream)
 
     def evict(self, seq_ids, keep_from, sinks=0, stream=None):
         """Forget the full pages of each sequence that lie in [sinks, keep_from[i]), in every layer."""
@@ -417,31 +430,31 @@ class Cache:
 
     def compact(self, stream=None):
         """Give the pages that no sequence names back to the pools."""
-        trr_compact(self.handle, self.workspace(), stream)
+        trr_compact(self.handle, self.workspace(stream), stream)
 
-    def _rows(self, seq_ids, q, out):
+    def _rows(self, seq_ids, q, out, stream):
         """The output of an attention call: q and out are [n][Hq][d]."""
         n = seq_ids.numel()
         size = n * self.Hq * self.d
         if q.numel() != size or (out is not None and out.numel() != size):
             raise ValueError(f"q and out must have {size} elements ([n][Hq][d])")
-        return torch.empty((n, self.Hq, self.d), dtype=torch.bfloat16, device=q.device) if out is None else out
+        return _new((n, self.Hq, self.d), torch.bfloat16, q.device, stream) if out is None else out
 
     def decode_attn_sinks(self, layer, seq_ids, q_positions, q, modes, sinks, windows=None, window_scalar=0,
                           softmax_scale=0.0, out=None, stream=None):
         """decode_attn whose local queries also see the first `sinks` positions."""
-        out = self._rows(seq_ids, q, out)
+        out = self._rows(seq_ids, q, out, stream)
         trr_decode_attn_sinks(self.handle, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
-                              softmax_scale, out, self.workspace(), stream)
+                              softmax_scale, out, self.workspace(stream), stream)
         return out
 
     def decode_attn_shared(self, layer, seq_ids, q_positions, q, modes, group_offsets, windows=None, window_scalar=0,
                            sinks=0, softmax_scale=0.0, out=None, stream=None):
         """decode_attn_sinks of queries in groups (group_offsets, int32, one more than there are groups):
         the pages that a group's full queries share are read once for the group."""
-        out = self._rows(seq_ids, q, out)
+        out = self._rows(seq_ids, q, out, stream)
         trr_decode_attn_shared(self.handle, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
-                               group_offsets, softmax_scale, out, self.workspace(), stream)
+                               group_offsets, softmax_scale, out, self.workspace(stream), stream)
         return out
 
     def status(self, stream=None) -> int:

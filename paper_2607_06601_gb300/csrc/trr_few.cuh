@@ -12,8 +12,10 @@
 //   output   O^T += V^T W: 16 dimensions x 8 columns, W = p s.  A lane holds an eighth of the
 //            dimensions of two pairs of tokens; byte permutes pair the tokens' codes.
 // A code is used as the binary16 number `offset + code` made by setting its bits under an
-// exponent (16 + c, 4 + c, 1024 + c for 4, 2, 8 bits: no conversion, no subtraction); the
-// offset's part of every sum is taken off at the end in binary32.
+// exponent (16 + c, 4 + c, 1024 + c for 4, 2, 8 bits: no conversion, no subtraction).  The offset's
+// part of a score is taken off in binary32; that of the output, and half the codes' range with it,
+// by a product of the same weights with a constant, block by block, so that the running sums hold
+// centred values: z + s (middle of the range), the rest of a value, is added up apart.
 //
 // The softmax reference m follows the largest score plus log2 of the token's V scale, so that
 // W = p s stays below 2^9 in binary16 whatever the size of the values; 16-bit pages keep p as a
@@ -70,16 +72,18 @@ static_assert(FewSmem<64, 1>::kRingBytes >= 32 * 136 + 128 && FewSmem<64, 2>::kR
                   FewSmem<128, 1>::kRingBytes >= 32 * 264 + 128 && FewSmem<128, 4>::kRingBytes >= 32 * 288 + 128,
               "the widest blocks");
 
+// A code as a binary16 number has kOffset added to it; kMiddle lies halfway between a class's least
+// and largest code, and kMinus is -(kOffset + kMiddle) twice.
 template <int B>
 struct Codes;
 template <>
-struct Codes<2> { static constexpr float kOffset = 4.f; };
+struct Codes<2> { static constexpr float kOffset = 4.f, kMiddle = 1.5f; static constexpr uint32_t kMinus = 0xC580C580u; };
 template <>
-struct Codes<4> { static constexpr float kOffset = 16.f; };
+struct Codes<4> { static constexpr float kOffset = 16.f, kMiddle = 7.5f; static constexpr uint32_t kMinus = 0xCDE0CDE0u; };
 template <>
-struct Codes<8> { static constexpr float kOffset = 1024.f; };
+struct Codes<8> { static constexpr float kOffset = 1024.f, kMiddle = 128.f; static constexpr uint32_t kMinus = 0xE480E480u; };
 template <>
-struct Codes<16> { static constexpr float kOffset = 0.f; };
+struct Codes<16> { static constexpr float kOffset = 0.f, kMiddle = 0.f; static constexpr uint32_t kMinus = 0; };
 
 // Codes i of both 16-bit halves of x as binary16 numbers offset + code.
 __device__ __forceinline__ uint32_t codes4(uint32_t x, int i) {
@@ -115,7 +119,7 @@ struct FewState {
   static constexpr int kHeads = NG == 1 ? 2 : 1; // query heads of the lane's two columns
   float acc[kSteps][4];                          // O^T: dimensions 2 i, 2 i + 1 of the lane's run x its two columns
   float m[kHeads], l[kHeads], f[kHeads];         // reference, sum, factor from products to base-2 exponents
-  float corr[2];                                 // sum p z - offset W of the lane's columns
+  float corr[2];                                 // sum p (z + s kMiddle) of the lane's columns
   float qsum[2];
   uint32_t q[kSteps][2];                         // the columns' query rows, in the order of q_class's codes
   int q_class;
@@ -290,14 +294,21 @@ __device__ __forceinline__ void few_tokens(FewState<D, NG>& s, const uint8_t* bl
         if (!seen) wv = as_half2(0u);  // the scale of a slot that holds nothing may be anything
         w[r][0] = as_u32(wv);
         if (seen) {
-          s.corr[0] += p0 * __high2float(v0) - kOff * __low2float(wv);
-          s.corr[1] += p1 * __high2float(v1) - kOff * __high2float(wv);
+          s.corr[0] += p0 * fmaf(Codes<B>::kMiddle, __low2float(v0), __high2float(v0));
+          s.corr[1] += p1 * fmaf(Codes<B>::kMiddle, __low2float(v1), __high2float(v1));
         }
       }
     }
     const uint32_t b0 = transpose8(w[0][0]), b1 = transpose8(w[1][0]);
     uint32_t l0 = 0, l1 = 0;
     if (B == 16) l0 = transpose8(w[0][1]), l1 = transpose8(w[1][1]);
+    // The sums run over all of a warp's tokens of a segment: they take in V's distance from the middle
+    // of its range alone.  The offset, ten times and more the size of a value, would cost them their
+    // last bits with every product (rows over 30,000 tokens of 8 bits came out 9 % off).
+    if (B != 16) {
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) mma16816<false>(s.acc[i], Codes<B>::kMinus, Codes<B>::kMinus, Codes<B>::kMinus, Codes<B>::kMinus, b0, b1);
+    }
     // tokens 2 part, 2 part + 1 (and 8 further on): an eighth of the dimensions, from quad * D / 8
     const int kp = b + 2 * part;
     const int v0 = (keys + kp) * kRow + quad * (kRow / 8);

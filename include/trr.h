@@ -363,9 +363,10 @@ TRR_API trr_status trr_compact(trr_cache* cache, void* workspace, uint64_t works
 
 /* Decode attention with sinks: trr_decode_attn, but a local query also sees the first
  * `sinks` positions: local: the stored tokens j <= t with j >= t-w+1 or j < sinks.
- *   sinks >= 0 (0: trr_decode_attn's results).  seq_ids, q_positions, modes, windows:
- *   device, read after the previous kernel of the stream has finished; q, out 16-byte
- *   aligned.  Otherwise the arguments, results and error contract of trr_decode_attn; a
+ *   sinks >= 0 (0: trr_decode_attn's results, but for rounding; that call is one launch and
+ *   the faster one where no sinks are kept: see trr_decode_attn_shared).  seq_ids,
+ *   q_positions, modes, windows: device, read after the previous kernel of the stream has
+ *   finished; q, out 16-byte aligned.  Otherwise the arguments, results and error contract of trr_decode_attn; a
  *   cache with head_modes returns TRR_ERR_UNSUPPORTED. */
 TRR_API trr_status trr_decode_attn_sinks(trr_cache* cache, int32_t layer, int32_t n, const int32_t* seq_ids,
                                          const int32_t* q_positions, const void* q_bf16, const uint8_t* modes,
@@ -375,10 +376,19 @@ TRR_API trr_status trr_decode_attn_sinks(trr_cache* cache, int32_t layer, int32_
 
 /* Decode attention of queries whose sequences share pages: trr_decode_attn_sinks with the
  * queries given in groups, queries group_offsets[i] .. group_offsets[i+1]-1 forming group
- * i (queries outside every group stand alone).  The results do not depend on the groups.
+ * i (queries outside every group stand alone).  Groups change no result but for rounding.
  * In each class, the leading pages that all full queries of a group name and see whole
  * are read once for the group; so put sequences forked from one prompt in one group, and
  * a sequence that shares nothing in none.
+ *   Which call: this one pays where many rows share a long past.  GPU time of a call, this
+ *   one against trr_decode_attn, no sinks: 64 queries of 32 heads on 32,768 shared tokens
+ *   of 8 KV heads of 128, 93 and 526 us; 16 of them, 60 and 165; 8 of one sequence (a
+ *   chunk), 62 and 139, on 8,192 tokens 44 and 48.  A KV head for each query head: 32
+ *   queries of 12 heads on 2,048 tokens, 32 and 30; 63 routed queries on 7 prompts of
+ *   4,099, 71 and 63.  Short prompts of a few samples each are better left to
+ *   trr_decode_attn (4 queries of 12 heads on each of 128 prompts of 512: 123 and 73), and
+ *   so are windows without sinks (64 queries of 32 heads, window 511: 47 and 29; 128
+ *   queries on 8 KV heads of 128, window 1024: 59 and 57).
  *   group_offsets: int32[num_groups + 1], device, ascending from >= 0 to <= n;
  *   0 <= num_groups <= n.  Offsets that are not make every row zero and record
  *   INVALID_ARG.  Otherwise as trr_decode_attn_sinks. */

@@ -19,15 +19,17 @@
 //
 // The softmax reference m follows the largest score plus log2 of the token's V scale, so that
 // W = p s stays below 2^9 in binary16 whatever the size of the values; 16-bit pages keep p as a
-// sum of two bf16 numbers.
+// sum of two bf16 numbers.  Groups of a row share the reference: one whose scale is a thousand times
+// below the other's keeps fewer bits of its own dimensions (an error 11 times the output's rounding
+// there, and none that the row's largest values would show).
 //
 // What bounds it: instructions and their latency (four warps a scheduler keep it half busy): about
 // 230 for 16 tokens of a KV head and as many for each block, whatever the width.  The partial
 // pages at a window's edge and the sinks' add half as many bytes again.
 //
-// Measured on 64 queries of 32 heads of 64 with windows of 511 and 16 sinks (67.5 MB, 10 us at the
-// copy rate): 36 us beside the plan's 6 and the join's 4, 1.9 TB/s; 128 queries on 8 KV heads of 128
-// with windows of 1024 (95.4 MB): 49 us, 1.9 TB/s.
+// Measured by itself, caches cold, on 64 queries of 32 heads of 64 with windows of 511 and 16 sinks
+// (67.5 MB, 10 us at the copy rate): 41 us, 1.6 TB/s; 128 queries on 8 KV heads of 128 with windows
+// of 1024 (95.4 MB): 53 us, 1.8 TB/s.  The product that centres the codes costs 0 to 2 % of that.
 #pragma once
 
 #include "trr_group.cuh"

@@ -83,10 +83,11 @@ __device__ __forceinline__ int copies_of(int rows) { return rows <= 32 ? 4 : row
 constexpr int kLeastShare = kSegmentCost / 2 + 2 * kTileCost;
 
 // Blocks of a warp's run of few rows that are done beside the tensor kernel's shortest share, and beside
-// one of kLongShare.  Measured on the SMs that the tensor kernel leaves against all of them after it: 32
-// queries on 2048 + 64 tokens of 12 KV heads of 64, 27 us against 33; 16 queries on 65536 + 256 tokens of
-// 8 KV heads of 128, 67.7 against 73.0 (eight SMs left to them), on 32768 + 256, 51.9 against 53.2.  64
-// such queries would need 32 SMs, and the tensor kernel would lose more than they gain.
+// one of kLongShare.  Measured, when the rule came in, on the SMs that the tensor kernel leaves against all
+// of them after it: 32 queries on 2048 + 64 tokens of 12 KV heads of 64, 27 us against 33; 16 queries on
+// 65536 + 256 tokens of 8 KV heads of 128, 67.7 against 73.0 (eight SMs left to them), on 32768 + 256, 51.9
+// against 53.2.  64 such queries would need 32 SMs, and the tensor kernel would lose more than they gain.
+// A block is taken for as long as another whatever its width and d, which is rough.
 constexpr int kShortShare = 6, kFewShare = 12, kLongShare = 20;
 
 // The same for the kernel for few rows, in blocks.

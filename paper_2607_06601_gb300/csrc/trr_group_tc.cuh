@@ -9,13 +9,22 @@
 // four copies of its rows, each of which takes its own part of a tile's tokens, so that all
 // warps share the exponentials.
 //
+// Binary16 keys are the coarsest step: a twelfth bit of a value against the 8 of its code, so at most
+// a sixteenth of an 8-bit group's step, unless all of the group's values lie far from zero together.
+// Rows of random data come out 1.02 times the output's rounding off (root mean square), with scores
+// of standard deviation 16 or single channels 30 times the others 1.2 times, with 50 added to every
+// element of K 3.3 to 5.5 times.
+//
 // What bounds it, for a tile of 128 tokens at d 128: the products take about 1024 cycles, the
 // exponentials 1024 (16 a cycle), the expansion's integer instructions about as long; the three
-// hand tiles on to one another, and a tile takes about 3000 cycles whatever its width.
+// hand tiles on to one another.  A tile more for every CTA takes 3600 cycles with 2 or 4 bits, 6000
+// with 8 (the ring then holds two tiles instead of four and more; whether that is why was not
+// tried), and 4800 for the 64 tokens of a tile of 16 bits.
 //
 // Measured: 64 queries of 32 heads on 32768 shared tokens, 8 KV heads of 128 (27 GFLOP, 36 MB;
-// 14.6 us at the measured rate of library products): 63 us, 0.44 PFLOP/s, of which 9 are the start
-// to the first scores and 5 the rows out.  16 such queries (two copies of 64 rows): 35 us.
+// 14.6 us at the measured rate of library products): 65 us, 0.42 PFLOP/s, of which 9 are the start
+// to the first scores and 5 the rows out.  16 such queries (two copies of 64 rows): 41 us (both by
+// themselves, caches cold).
 // With one softmax thread a row and eight expanding warps, 63 queries of 7 prompts took 127 us a
 // call against 118 then; softmax warpgroups that take whole tiles in turn, 91 against 87.
 #pragma once

@@ -108,6 +108,8 @@ typedef enum {
   TRR_ERR_TIMEOUT = 8        /* a bounded wait inside a kernel gave up */
 } trr_status;
 
+enum { TRR_F32 = 0, TRR_BF16 = 1 }; /* types of trr_kv_read's outputs */
+
 enum { TRR_MODE_SKIP = 0, TRR_MODE_LOCAL = 1, TRR_MODE_FULL = 2 }; /* a_t, Eq. 2 */
 
 typedef struct trr_cache_config {
@@ -397,6 +399,69 @@ TRR_API trr_status trr_decode_attn_shared(trr_cache* cache, int32_t layer, int32
                                           const int32_t* windows, int32_t window_scalar, int32_t sinks,
                                           int32_t num_groups, const int32_t* group_offsets, float softmax_scale,
                                           void* out_bf16, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------- prompts by chunks --
+ *
+ * Calls on stretches of consecutive positions: stretch i is positions starts[i],
+ * starts[i] + 1, ... of sequence seq_ids[i], and its rows in the call's other arrays are
+ * offsets[i] .. offsets[i+1]-1.  seq_ids[n], starts[n], offsets[n + 1]: int32, device, read
+ * after the previous kernel of the stream has finished (so they may be its outputs);
+ * 0 <= n <= 4096.  A stretch may be empty (its sequence and start are then not looked at),
+ * a sequence may be named more than once.  Rows in no stretch are left as they are.
+ * Device-detected errors: offsets that do not ascend from >= 0 to <= the call's rows make
+ * every row zero and record INVALID_ARG; a sequence id out of range (INVALID_ARG) or a
+ * stretch that leaves [0, max_context) (BAD_POSITION) makes the stretch's rows zero; the
+ * error of the lowest failing row is recorded. */
+
+/* Bytes of workspace for trr_chunk_attn of num_chunks chunks with num_tokens queries whose
+ * positions, and all before them, number at most max_keys: the sum of starts[i] + length
+ * of chunk i (counting what is stored is enough, and chunks of local queries count their
+ * windows and sinks only). */
+TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num_chunks, int32_t num_tokens,
+                                             int64_t max_keys, uint64_t* bytes);
+
+/* Attention of chunks of new tokens: the queries of a prompt's chunk, or of a few drafted
+ * tokens, over everything that their sequences have stored up to them.  Append the
+ * chunk's tokens first (trr_kv_append): a query sees its own token and the chunk's earlier
+ * ones as they are stored.
+ *   Chunks are stretches (above) of num_tokens rows: query r of chunk i stands at
+ *   t = starts[i] + r - offsets[i], has rows q[r][Hq][d] (bf16) and mode modes[r]:
+ *     skip : out row = 0
+ *     local: softmax attention over the stored tokens j <= t with j >= t-w+1 or
+ *            j < sinks, w = windows[r] (or window_scalar when windows == NULL), w >= 1
+ *     full : softmax attention over the stored tokens j <= t,
+ *   as trr_decode_attn_sinks computes it for the same queries: out[r][Hq][d] (bf16), a zero
+ *   row where nothing is in sight.  lse (may be NULL): lse[r][Hq] float32, the natural
+ *   logarithm of the sum of exp(softmax_scale * q.k) over the tokens in sight, -infinity
+ *   for a zero row; with it, rows over parts of a past can be joined.
+ *   seq_ids, starts, offsets, q, modes, windows, out, lse: device; q and out 16-byte
+ *   aligned; 0 <= num_tokens <= 2^20; sinks >= 0.
+ *   workspace: device memory, 256-byte aligned, trr_chunk_workspace_bytes of it, used only
+ *   while the call runs.  One that is smaller than that of max_keys 0 or misaligned returns
+ *   TRR_ERR_OUT_OF_MEMORY and enqueues nothing; one that turns out too small for what is
+ *   stored makes every row zero and records OUT_OF_MEMORY.
+ *   Device-detected errors: those of stretches; a mode not allowed or a local query with a
+ *   window below 1 (INVALID_ARG) makes that query's rows zero.  A cache with head_modes
+ *   returns TRR_ERR_UNSUPPORTED. */
+TRR_API trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t num_chunks, const int32_t* seq_ids,
+                                  const int32_t* starts, const int32_t* offsets, int32_t num_tokens, const void* q_bf16,
+                                  const uint8_t* modes, const int32_t* windows, int32_t window_scalar, int32_t sinks,
+                                  float softmax_scale, void* out_bf16, float* lse, void* workspace,
+                                  uint64_t workspace_bytes, void* stream);
+
+/* Read back: K and V of stretches (above), dequantised, one row a position.
+ *   Row r: k_out[r * k_stride + h*d + j] = z + c*s (rounded once to binary32) or the stored
+ *   bf16 value of the token at the row's position, for KV head h < Hkv; so for v_out; zeros
+ *   where the sequence stores no token (or, with head_modes, the token not that head).
+ *   type: TRR_F32, or TRR_BF16 (that value rounded to bf16).  Strides in elements, at least
+ *   Hkv * d, rows and both arrays 16-byte aligned.  bits_out (may be NULL): [num_rows][Hkv]
+ *   uint8, the width (2, 4, 8 or 16) that the row's token is stored at, 0 for zeros.
+ *   Appending the rows again at their widths stores values as near to these as Eq. 4
+ *   comes; it does not always give the same codes (scale and zero are taken anew).
+ *   0 <= num_rows <= 2^30.  Device-detected errors: those of stretches. */
+TRR_API trr_status trr_kv_read(trr_cache* cache, int32_t layer, int32_t n, const int32_t* seq_ids, const int32_t* starts,
+                               const int32_t* offsets, int32_t num_rows, int32_t type, void* k_out, int64_t k_stride,
+                               void* v_out, int64_t v_stride, uint8_t* bits_out, void* stream);
 
 /* Free library-owned memory (waits for the device first).  A caller pool is not
  * freed.  NULL is accepted. */

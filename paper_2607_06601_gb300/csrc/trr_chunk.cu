@@ -1,0 +1,589 @@
+// trr_chunk.cu - trr_chunk_attn: attention of chunks of new tokens over the paged cache.
+//
+//   o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - m_i) / sum_j exp(s_ij - m_i),  s_ij = scale q_i k_j
+// over the stored tokens j that query i sees: j <= t_i and (full, or j >= t_i-w_i+1, or j < sinks).
+//
+// A chunk's many queries read the same tokens, so those are brought back from their codes once, not
+// once for each block of rows:
+//   chunk_plan_kernel    a CTA per chunk: its queries sorted by mode (a block of rows then has one mode
+//                        and reads no more than that mode sees), the positions that any of them sees,
+//                        how many tokens are stored there; the CTA that ends last lays chunks end to end.
+//   chunk_stage_kernel   the stored tokens in sight, in order of position, as tiles of 128 tokens in the
+//                        layout that the tensor core reads: binary16 for 2, 4 and 8 bits (z + c s rounded
+//                        once, 11 bits against the 8 of the output), bf16 for 16 bits, in lists of their
+//                        own, since a product's operands have one type.  And each block's tiles.
+//   chunk_rows_kernel    the rows.
+#include <algorithm>
+#include <climits>
+
+#include "trr_chunk.cuh"
+
+namespace trr {
+
+// ------------------------------------------------------------------------------ plan --
+
+// Error of chunk i, 0 when it is valid (the offsets are).
+__device__ __forceinline__ int chunk_error(const ChunkArgs& g, int i) {
+  const int seq = g.seq_ids[i], start = g.starts[i], len = g.offsets[i + 1] - g.offsets[i];
+  if (seq < 0 || seq >= g.a.S) return TRR_ERR_INVALID_ARG;
+  return start < 0 || start > g.a.maxctx - len ? TRR_ERR_BAD_POSITION : 0;
+}
+
+// Errors of a call: the lowest failing query's, kept as INT_MAX - (16 query + error) so that 0 means none.
+__device__ __forceinline__ void chunk_fail(const ChunkArgs& g, int query, int err) {
+  atomicMax(g.a.ctrl + kChunkBad, INT_MAX - (16 * query + err));
+}
+
+// Sum over the CTA's threads before this one (and over all, in *total).  Every thread calls it.
+__device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* warp_sums, int64_t* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
+  int64_t s = x;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = s;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+  for (int w = 0; w < warps; ++w) {
+    if (w < warp) before += warp_sums[w];
+    all += warp_sums[w];
+  }
+  *total = all;
+  return before + s - x;
+}
+
+__global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __grid_constant__ ChunkArgs g) {
+  __shared__ int s_bad, s_lo, s_count[2], s_warp[2][kPlanChunkThreads / 32], s_before[3][kClasses], s_last;
+  __shared__ int64_t s_sums[kPlanChunkThreads / 32];
+  const LayerArgs& a = g.a;
+  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) s_bad = 0, s_lo = INT_MAX, s_count[0] = s_count[1] = 0;
+  pdl_wait();
+  pdl_trigger();
+  __syncthreads();
+  for (int x = tid; x <= g.n; x += kPlanChunkThreads) {
+    const int o = g.offsets[x], next = x < g.n ? g.offsets[x + 1] : o;
+    if (o < 0 || o > g.num_tokens || next < o) s_bad = 1;
+  }
+  for (int h = tid; h < a.Hkv; h += kPlanChunkThreads) g.flag[static_cast<int64_t>(i) * a.Hkv + h] = 0;
+  __syncthreads();
+  const bool bad = s_bad;
+  const int row0 = bad ? 0 : g.offsets[i], len = bad ? 0 : g.offsets[i + 1] - row0;
+  const int seq = g.seq_ids[i], start = g.starts[i], err = bad ? TRR_ERR_INVALID_ARG : chunk_error(g, i);
+  if (tid == 0 && err && (bad || len > 0)) chunk_fail(g, row0, err);
+  // a query's place: 0 full, 1 local, 2 a zero row
+  auto kind_of = [&](int k, int* window) -> int {
+    const int q = row0 + k, mode = g.modes[q];
+    if (err) return 2;
+    if (mode > TRR_MODE_FULL) {
+      chunk_fail(g, q, TRR_ERR_INVALID_ARG);
+      return 2;
+    }
+    if (mode == TRR_MODE_SKIP) return 2;
+    if (mode == TRR_MODE_FULL) return 0;
+    *window = g.windows ? g.windows[q] : g.window_scalar;
+    if (*window >= 1) return 1;
+    chunk_fail(g, q, TRR_ERR_INVALID_ARG);
+    return 2;
+  };
+  int full = 0, local = 0, lo = INT_MAX;
+  for (int k = tid; k < len; k += kPlanChunkThreads) {
+    int w = 0;
+    const int kind = kind_of(k, &w);
+    full += kind == 0;
+    local += kind == 1;
+    if (kind == 1) lo = min(lo, max(0, start + k - w + 1));
+  }
+  full = __reduce_add_sync(0xffffffffu, full);
+  local = __reduce_add_sync(0xffffffffu, local);
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  if (lane == 0) {
+    atomicAdd(&s_count[0], full);
+    atomicAdd(&s_count[1], local);
+    atomicMin(&s_lo, lo);
+  }
+  __syncthreads();
+  full = s_count[0];
+  local = s_count[1];
+  // queries of one kind behind another, each kind in order
+  int done[3] = {0, full, full + local};
+  for (int k0 = 0; k0 < len; k0 += kPlanChunkThreads) {
+    const int k = k0 + tid;
+    int w = 0;
+    const int kind = k < len ? kind_of(k, &w) : 3;
+    const uint32_t below = (1u << lane) - 1;
+    const uint32_t b0 = __ballot_sync(0xffffffffu, kind == 0), b1 = __ballot_sync(0xffffffffu, kind == 1), b2 = __ballot_sync(0xffffffffu, kind == 2);
+    if (lane == 0) s_warp[0][warp] = __popc(b0) | __popc(b1) << 16, s_warp[1][warp] = __popc(b2);
+    __syncthreads();
+    int at[3] = {done[0], done[1], done[2]};
+    for (int v = 0; v < kPlanChunkThreads / 32; ++v) {
+      const int x = s_warp[0][v], y = s_warp[1][v];
+      if (v < warp) at[0] += x & 0xFFFF, at[1] += x >> 16, at[2] += y;
+      done[0] += x & 0xFFFF, done[1] += x >> 16, done[2] += y;
+    }
+    if (kind < 3) g.list[row0 + (kind == 0 ? at[0] + __popc(b0 & below) : kind == 1 ? at[1] + __popc(b1 & below) : at[2] + __popc(b2 & below))] = row0 + k;
+    __syncthreads();
+  }
+  // the positions in sight of any query, and the tokens stored there
+  const bool reads = full + local > 0;
+  lo = full > 0 ? 0 : s_lo;
+  const int end = start + len, sinks = reads ? min(g.sinks, lo) : 0;
+  if (tid < 3 * kClasses && reads) s_before[tid / kClasses][tid % kClasses] = place_of(a, seq, tid % kClasses, tid < 4 ? sinks : tid < 8 ? lo : end).before;
+  __syncthreads();
+  const int heads = a.Hq / a.Hkv;
+  if (tid == 0) {
+    ChunkPlan c = {};
+    c.seq = seq; c.start = start; c.len = len; c.row0 = row0;
+    c.full = full; c.local = local;
+    if (reads) {
+      c.sinks = sinks; c.lo = lo; c.end = end; c.span = sinks + end - lo;
+      for (int k = 0; k < kClasses; ++k) {
+        c.dropped[k == 3] += s_before[1][k] - s_before[0][k];
+        c.tokens[k == 3] += s_before[2][k] - s_before[1][k] + s_before[0][k];
+      }
+      for (int k = 0; k < 2; ++k) c.tiles[k] = (c.tokens[k] + kChunkTile - 1) / kChunkTile;
+      c.units = (c.span + kSpan - 1) / kSpan;
+      c.blocks = (full * heads + kBlockRows - 1) / kBlockRows + (local * heads + kBlockRows - 1) / kBlockRows;
+    }
+    g.chunk[i] = c;
+    s_last = atom_add_acq_rel(a.ctrl + kChunkDone, 1) == g.n - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  // the last CTA: chunks end to end
+  int64_t tiles = 0, units = 0, blocks = 0;
+  for (int x0 = 0; x0 < g.n; x0 += kPlanChunkThreads) {
+    const int x = x0 + tid;
+    int t = 0, u = 0, b = 0;
+    if (x < g.n) {
+      const volatile ChunkPlan* c = g.chunk + x;
+      t = c->tiles[0] + c->tiles[1]; u = c->units; b = c->blocks;
+    }
+    int64_t all;
+    const int64_t t0 = tiles + scan_before(t, s_sums, &all);
+    tiles += all;
+    const int64_t u0 = units + scan_before(u, s_sums, &all);
+    units += all;
+    const int64_t b0 = blocks + scan_before(b, s_sums, &all);
+    blocks += all;
+    if (x < g.n) {
+      ChunkPlan* c = g.chunk + x;
+      c->tile0 = static_cast<int>(min(t0, static_cast<int64_t>(INT_MAX)));
+      c->unit0 = static_cast<int>(min(u0, static_cast<int64_t>(INT_MAX)));
+      c->block0 = static_cast<int>(b0);
+    }
+  }
+  if (tid == 0) {
+    int whole = bad ? TRR_ERR_INVALID_ARG : 0;
+    if (!whole && tiles > g.most_tiles) {  // the workspace is too small for what is stored
+      whole = TRR_ERR_OUT_OF_MEMORY;
+      chunk_fail(g, 0, whole);
+    }
+    ChunkHeader h = {};
+    h.bad = whole;
+    if (!whole) {
+      h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units); h.tiles = static_cast<int>(tiles);
+      // a small call's heads are shared out among CTAs, so that staging fills the GPU
+      const int64_t most = (2 * a.Hkv + kSpanThreads / 32 - 1) / (kSpanThreads / 32);
+      h.splits = static_cast<int>(units > 0 ? max(static_cast<int64_t>(1), min(most, 4 * g.ctas / units)) : 1);
+    }
+    *g.head = h;
+    const int e = atomicExch(a.ctrl + kChunkBad, 0);
+    if (e) set_status(a.ctrl, (INT_MAX - e) & 15);
+    a.ctrl[kChunkDone] = 0;
+  }
+}
+
+// ----------------------------------------------------------------------------- stage --
+
+// z + c s of eight elements as binary16, rounded once; a value past binary16's largest stays at it
+// (a group's largest level may round past the largest value that the append takes).
+template <int B>
+__device__ __forceinline__ uint4 expand_f16(const Codes& x) {
+  const __half2 s = as_half2(__byte_perm(x.sz, 0, 0x1010)), z = as_half2(__byte_perm(x.sz, 0, 0x3232));
+  const __half2 k = as_half2(0x64006400u), top = as_half2(0x7BFF7BFFu);  // 1024 (1024 + c is exact), 65504
+  uint32_t p[4];
+  if (B == 8) {
+    p[0] = __byte_perm(x.w.x, 0x64646464u, 0x4140); p[1] = __byte_perm(x.w.x, 0x64646464u, 0x4342);
+    p[2] = __byte_perm(x.w.y, 0x64646464u, 0x4140); p[3] = __byte_perm(x.w.y, 0x64646464u, 0x4342);
+  } else if (B == 4) {
+    uint32_t t[4];  // elements i and i + 4
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = ((x.w.x >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
+    p[0] = __byte_perm(t[0], t[1], 0x5410); p[1] = __byte_perm(t[2], t[3], 0x5410);
+    p[2] = __byte_perm(t[0], t[1], 0x7632); p[3] = __byte_perm(t[2], t[3], 0x7632);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = ((x.w.x >> (4 * i)) & 3u) | ((x.w.x << (14 - 4 * i)) & 0x30000u) | 0x64006400u;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = as_u32(__hmin2(__hfma2(__hsub2(as_half2(p[i]), k), s, z), top));
+  return make_uint4(p[0], p[1], p[2], p[3]);
+}
+
+template <int B, int D>
+__device__ __forceinline__ void stage_rows(const ChunkArgs& g, const ChunkPlan& ch, int chunk, const Found& f, int h0, int h1) {
+  constexpr int c = B == 2 ? 0 : B == 4 ? 1 : B == 8 ? 2 : 3, kLanes = D / 8, kStep = 32 / kLanes, kAhead = 4;
+  const int n = f.count[c], lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
+  if (n == 0) return;
+  for (int j = 2 * h0 + warp; j < 2 * h1; j += kSpanThreads / 32) {
+    const int h = j >> 1, which = j & 1;
+    for (int t0 = lane / kLanes; t0 < n; t0 += kAhead * kStep) {
+      Codes x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int t = t0 + u * kStep;
+        if (t < n) x[u] = load_codes<B, D>(g.a, f.token[c][t].page, f.token[c][t].slot, h, which, e, lg_group);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int t = t0 + u * kStep;
+        if (t >= n) continue;
+        const int row = f.token[c][t].row;  // in the pool's rows
+        uint4 v = x[u].w;
+        if (B != 16) {
+          v = expand_f16<B == 16 ? 2 : B>(x[u]);
+        } else if (which == 1) {
+          // a V that is not finite must not reach rows that do not see it (0 times infinity): such chunks' rows are done one by one
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          bool odd = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+          if (odd) {
+            g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
+            g.head->flagged = 1;
+          }
+        }
+        *reinterpret_cast<uint4*>(staged_tile<D>(g, row / kChunkTile, h, which) + tile_at(row % kChunkTile, e)) = v;
+      }
+    }
+  }
+}
+
+// The tiles that block b's rows see.
+__device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) {
+  const LayerArgs& a = g.a;
+  int lo = 0, hi = g.n - 1;  // its chunk: the last one whose first block is b or before it
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (g.chunk[mid].block0 <= b) lo = mid;
+    else hi = mid - 1;
+  }
+  const ChunkPlan c = g.chunk[lo];
+  const int heads = a.Hq / a.Hkv, full_blocks = (c.full * heads + kBlockRows - 1) / kBlockRows;
+  const bool local = b - c.block0 >= full_blocks;
+  BlockPlan p = {};
+  p.chunk = lo; p.local = local;
+  p.row = (b - c.block0 - (local ? full_blocks : 0)) * kBlockRows;
+  p.rows = min(kBlockRows, (local ? c.local : c.full) * heads - p.row);
+  p.query0 = c.row0 + (local ? c.full : 0);
+  // its queries' last position, and the first that any of them sees past the sinks
+  const int k0 = p.row / heads, k1 = (p.row + p.rows - 1) / heads;
+  const int t = c.start + g.list[p.query0 + k1] - c.row0;
+  int from = 0;
+  if (local) {
+    from = INT_MAX;
+    for (int k = k0 + lane; k <= k1; k += 32) {
+      const int q = g.list[p.query0 + k];
+      from = min(from, max(0, c.start + q - c.row0 - (g.windows ? g.windows[q] : g.window_scalar) + 1));
+    }
+    from = __reduce_min_sync(0xffffffffu, from);
+  }
+  const int head = local ? min(g.sinks, from) : 0;
+  // ranks of three positions in both lists: lanes 0 .. 11, a class of a position each
+  const int which = lane >> 2, cls = lane & 3, x = which == 0 ? head : which == 1 ? from : t + 1;
+  int r = lane < 12 ? place_of(a, c.seq, cls, x).before : 0;
+  const int wide = __shfl_sync(0xffffffffu, r, (lane & ~3) | 3);
+  const int sum = r + __shfl_xor_sync(0xffffffffu, r, 1);  // lanes 0, 1: classes 0 and 1
+  const int narrow = __shfl_sync(0xffffffffu, sum, lane & ~3) + __shfl_sync(0xffffffffu, r, (lane & ~3) | 2);
+  int rank[2][3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int pos = k == 0 ? head : k == 1 ? from : t + 1;
+    rank[0][k] = __shfl_sync(0xffffffffu, narrow, 4 * k) - (pos >= c.lo ? c.dropped[0] : 0);
+    rank[1][k] = __shfl_sync(0xffffffffu, wide, 4 * k) - (pos >= c.lo ? c.dropped[1] : 0);
+  }
+  for (int l = 0; l < 2; ++l) {
+    p.head[l] = (rank[l][0] + kChunkTile - 1) / kChunkTile;
+    p.first[l] = rank[l][1] / kChunkTile;
+    p.last[l] = max(p.first[l], (rank[l][2] + kChunkTile - 1) / kChunkTile);
+    if (p.head[l] >= p.first[l]) p.head[l] = p.first[l] = 0;  // one stretch from the start
+    p.tiles += p.head[l] + p.last[l] - p.first[l];
+  }
+  if (lane == 0) g.block[b] = p;
+}
+
+// Zero rows of heads h0 .. h1 - 1 of a query, by a warp.
+__device__ __forceinline__ void zero_rows(const ChunkArgs& g, int q, int h0, int h1, int lane) {
+  const int64_t at = static_cast<int64_t>(q) * g.a.Hq + h0;
+  uint4* out = reinterpret_cast<uint4*>(g.out + at * g.a.d);
+  for (int i = lane; i < (h1 - h0) * g.a.d / 8; i += 32) out[i] = make_uint4(0, 0, 0, 0);
+  if (g.lse)
+    for (int h = lane; h < h1 - h0; h += 32) g.lse[at + h] = -INFINITY;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSpanThreads) chunk_stage_kernel(const __grid_constant__ ChunkArgs g) {
+  __shared__ Found f;
+  __shared__ int64_t s_sums[kSpanThreads / 32];
+  __shared__ int s_last;
+  const LayerArgs& a = g.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_trigger();
+  const ChunkHeader head = *g.head;
+  if (head.bad) {
+    for (int q = blockIdx.x * (kSpanThreads / 32) + warp; q < g.num_tokens; q += gridDim.x * (kSpanThreads / 32)) zero_rows(g, q, 0, a.Hq, lane);
+    return;
+  }
+  // blocks of rows first: the CTA that plans the last one lays them end to end
+  for (int b = blockIdx.x + warp * gridDim.x; b < head.blocks; b += gridDim.x * (kSpanThreads / 32)) plan_block(g, b, lane);
+  __syncthreads();
+  if (tid == 0) s_last = atom_add_acq_rel(a.ctrl + kChunkPlanned, 1) == static_cast<int>(gridDim.x) - 1;
+  __syncthreads();
+  if (s_last) {
+    __threadfence();
+    int64_t work = 0;
+    for (int x0 = 0; x0 < head.blocks; x0 += kSpanThreads) {
+      const int x = x0 + tid;
+      const int tiles = x < head.blocks ? reinterpret_cast<const volatile BlockPlan*>(g.block)[x].tiles : 0;
+      int64_t all;
+      const int64_t before = work + scan_before(a.Hkv * chunk_cost(tiles), s_sums, &all);
+      work += all;
+      if (x < head.blocks) g.base[x] = before;
+    }
+    if (tid == 0) {
+      g.base[head.blocks] = work;
+      g.head->work = work;
+      g.head->per = max((work + g.ctas - 1) / g.ctas, static_cast<int64_t>(kChunkSegmentCost + 2 * kChunkTileCost));
+      a.ctrl[kChunkPlanned] = 0;
+    }
+  }
+  // units: 64 positions of a chunk's line, some of the KV heads
+  const int per = (a.Hkv + head.splits - 1) / head.splits;
+  int chunk = -1;
+  ChunkPlan c;
+  for (int u = blockIdx.x; u < head.units * head.splits; u += gridDim.x) {
+    const int unit = u / head.splits, h0 = u % head.splits * per, h1 = min(a.Hkv, h0 + per);
+    if (chunk < 0 || unit >= c.unit0 + c.units) {
+      int lo = chunk < 0 ? 0 : chunk, hi = g.n - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (g.chunk[mid].unit0 <= unit) lo = mid;
+        else hi = mid - 1;
+      }
+      chunk = lo;
+      c = g.chunk[chunk];
+    }
+    __syncthreads();  // the last unit's tokens have been read
+    if (tid <= kClasses) f.count[tid] = 0;
+    __syncthreads();
+    const int x = (unit - c.unit0) * kSpan + (tid >> 2), cls = tid & 3;
+    const int pos = x < c.sinks ? x : x - c.sinks + c.lo;
+    Place p{0, -1, 0};
+    if (x < c.span) p = place_of(a, c.seq, cls, pos);
+    // rank among the staged tokens of the class's list: the sum over the list's classes
+    const int sum = p.before + __shfl_xor_sync(0xffffffffu, p.before, 1);
+    const int narrow = __shfl_sync(0xffffffffu, sum, lane & ~3) + __shfl_sync(0xffffffffu, p.before, (lane & ~3) | 2);
+    if (p.page >= 0) {
+      const int l = cls == 3, rank = (l ? p.before : narrow) - (pos >= c.lo ? c.dropped[l] : 0);
+      const int row = (c.tile0 + (l ? c.tiles[0] : 0)) * kChunkTile + rank;
+      f.token[cls][atomicAdd(&f.count[cls], 1)] = Found::Token{a.pool[cls] + p.page * a.page_bytes[cls], p.slot, row};
+      if (h0 == 0) g.pos[row] = pos;
+    }
+    __syncthreads();
+    stage_rows<16, D>(g, c, chunk, f, h0, h1);
+    stage_rows<8, D>(g, c, chunk, f, h0, h1);
+    stage_rows<4, D>(g, c, chunk, f, h0, h1);
+    stage_rows<2, D>(g, c, chunk, f, h0, h1);
+  }
+  // rows of a list's last tile past its tokens are zero and out of sight; queries that read nothing have zero rows
+  for (int k = blockIdx.x; k < 2 * g.n; k += gridDim.x) {
+    const ChunkPlan& p = g.chunk[k >> 1];
+    const int l = k & 1, at = p.tokens[l] % kChunkTile;
+    if (at == 0) continue;
+    const int tile = p.tile0 + (l ? p.tiles[0] : 0) + p.tiles[l] - 1;
+    for (int r = at + tid; r < kChunkTile; r += kSpanThreads) g.pos[static_cast<int64_t>(tile) * kChunkTile + r] = INT_MAX;
+    for (int h = 0; h < a.Hkv; ++h)
+      for (int which = 0; which < 2; ++which)
+        for (int x = tid; x < (kChunkTile - at) * (D / 8); x += kSpanThreads)
+          *reinterpret_cast<uint4*>(staged_tile<D>(g, tile, h, which) + tile_at(at + x / (D / 8), x % (D / 8))) = make_uint4(0, 0, 0, 0);
+  }
+  for (int k = blockIdx.x * (kSpanThreads / 32) + warp; k < g.num_tokens; k += gridDim.x * (kSpanThreads / 32)) {
+    int lo = 0, hi = g.n - 1;  // places of the list: of the last chunk that starts at k or before it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (g.chunk[mid].row0 <= k) lo = mid;
+      else hi = mid - 1;
+    }
+    const ChunkPlan& p = g.chunk[lo];
+    if (k >= p.row0 + p.full + p.local && k < p.row0 + p.len) zero_rows(g, g.list[k], 0, a.Hq, lane);
+  }
+}
+
+// ------------------------------------------------------------------------------ rows --
+
+// One row, a warp: token after token, the statistics of the softmax running along.
+template <int D>
+__device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& c, const RowSource& s, bool local, int kvh, int lane) {
+  constexpr int E = D / 32;
+  const int64_t at = static_cast<int64_t>(s.query) * g.a.Hq + s.head;
+  float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < E; ++i) q[i] = __uint_as_float(static_cast<uint32_t>(g.q[at * D + lane * E + i]) << 16);
+  for (int which = 0; which < 2; ++which) {
+    const int tile0 = c.tile0 + (which ? c.tiles[0] : 0);
+    for (int j = 0; j < c.tokens[which]; ++j) {
+      const int tile = tile0 + j / kChunkTile, r = j % kChunkTile, pos = g.pos[static_cast<int64_t>(tile) * kChunkTile + r];
+      if (pos > s.t) break;
+      if (pos < s.lo && !(local && pos < g.sinks)) continue;
+      const int e = lane * E;
+      const uint16_t* k = reinterpret_cast<const uint16_t*>(staged_tile<D>(g, tile, kvh, 0) + tile_at(r, e >> 3)) + (e & 7);
+      const uint16_t* v = reinterpret_cast<const uint16_t*>(staged_tile<D>(g, tile, kvh, 1) + tile_at(r, e >> 3)) + (e & 7);
+      auto value = [&](uint16_t x) { return which ? __uint_as_float(static_cast<uint32_t>(x) << 16) : __half2float(__ushort_as_half(x)); };
+      float d = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) d += q[i] * value(k[i]);
+      for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
+      d *= g.scale_log2;
+      const float next = fmaxf(m, d), by = m == next ? 1.f : exp2f(m - next), p = d == -INFINITY ? 0.f : exp2f(d - next);
+      m = next;
+      l = l * by + p;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] = o[i] * by + p * value(v[i]);
+    }
+  }
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int i = 0; i < E; i += 2) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(o[i] * inv, o[i + 1] * inv);
+    *reinterpret_cast<__nv_bfloat162*>(g.out + at * D + lane * E + i) = x;
+  }
+  if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) chunk_rows_kernel(const __grid_constant__ ChunkArgs g) {
+  pdl_wait();
+  pdl_trigger();
+  if (g.head->bad) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, blocks = g.head->blocks;
+  for (int64_t x = blockIdx.x; x < static_cast<int64_t>(blocks) * g.a.Hkv; x += gridDim.x) {
+    const BlockPlan& b = g.block[x / g.a.Hkv];
+    const int kvh = static_cast<int>(x % g.a.Hkv);
+    const ChunkPlan& c = g.chunk[b.chunk];
+    if (b.tiles == 0) {  // nothing stored in sight
+      for (int r = warp; r < b.rows; r += 8) {
+        const RowSource s = row_source(g, c, b.query0, b.local, kvh, b.row + r);
+        zero_rows(g, s.query, s.head, s.head + 1, lane);
+      }
+      continue;
+    }
+    for (int r = warp; r < b.rows; r += 8) one_row<D>(g, c, row_source(g, c, b.query0, b.local, kvh, b.row + r), b.local, kvh, lane);
+  }
+}
+
+// ----------------------------------------------------------------------------- calls --
+
+static int64_t most_blocks(const Layout& l, int n, int num_tokens) {
+  return static_cast<int64_t>(num_tokens) * (l.Hq / l.Hkv) / kBlockRows + 2 * static_cast<int64_t>(n);
+}
+
+// Lays the workspace out (b == nullptr: counts its bytes); the tiles take what is left of `bytes`.
+static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, int num_tokens, int ctas, int64_t most_tiles) {
+  int64_t off = 0;
+  auto take = [&](int64_t bytes) {
+    uint8_t* p = b + off;
+    off += (bytes + 255) / 256 * 256;
+    return p;
+  };
+  const int64_t blocks = most_blocks(l, n, num_tokens);
+  g->head = reinterpret_cast<ChunkHeader*>(take(sizeof(ChunkHeader)));
+  g->chunk = reinterpret_cast<ChunkPlan*>(take(static_cast<int64_t>(sizeof(ChunkPlan)) * n));
+  g->list = reinterpret_cast<int32_t*>(take(4ll * num_tokens));
+  g->block = reinterpret_cast<BlockPlan*>(take(static_cast<int64_t>(sizeof(BlockPlan)) * blocks));
+  g->base = reinterpret_cast<int64_t*>(take(8 * (blocks + 1)));
+  g->flag = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
+  g->piece = reinterpret_cast<PieceInfo*>(take(static_cast<int64_t>(sizeof(PieceInfo)) * ctas));
+  g->part_ml = reinterpret_cast<float2*>(take(8ll * 2 * ctas * kBlockRows));
+  g->part_o = reinterpret_cast<float*>(take(4ll * 2 * ctas * kBlockRows * l.d));
+  g->most_blocks = static_cast<int>(blocks);
+  const int64_t fixed = off;
+  g->pos = reinterpret_cast<int32_t*>(take(4 * most_tiles * kChunkTile));
+  g->tile = take(most_tiles * l.Hkv * 2 * kChunkTile * l.d * 2);
+  return most_tiles ? off : fixed;
+}
+
+}  // namespace trr
+
+using namespace trr;
+
+static trr_status check_sizes(const Layout& l, int32_t n, int32_t num_tokens) {
+  if (n < 0 || n > kMostSpans || num_tokens < 0 || num_tokens > kMostChunkTokens) return TRR_ERR_INVALID_ARG;
+  if (l.head_modes) return TRR_ERR_UNSUPPORTED;  // one mode per token
+  return static_cast<int64_t>(num_tokens) * l.Hq > INT_MAX ? TRR_ERR_UNSUPPORTED : TRR_OK;
+}
+
+extern "C" trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num_chunks, int32_t num_tokens, int64_t max_keys, uint64_t* bytes) {
+  if (!cache || !bytes || max_keys < 0) return TRR_ERR_INVALID_ARG;
+  const Layout& l = cache_layout(cache);
+  const trr_status st = check_sizes(l, num_chunks, num_tokens);
+  if (st != TRR_OK) return st;
+  // a chunk's lists end in a partly filled tile each
+  const int64_t keys = std::min(max_keys, static_cast<int64_t>(num_chunks) * l.maxctx), tiles = keys / kChunkTile + 2 * static_cast<int64_t>(num_chunks);
+  if (tiles > INT_MAX / kChunkTile) return TRR_ERR_UNSUPPORTED;
+  ChunkArgs g;
+  *bytes = static_cast<uint64_t>(lay_workspace(&g, nullptr, l, num_chunks, num_tokens, cache_num_sms(cache), tiles));
+  return TRR_OK;
+}
+
+extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t num_chunks, const int32_t* seq_ids, const int32_t* starts,
+                                     const int32_t* offsets, int32_t num_tokens, const void* q_bf16, const uint8_t* modes,
+                                     const int32_t* windows, int32_t window_scalar, int32_t sinks, float softmax_scale,
+                                     void* out_bf16, float* lse, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!cache) return TRR_ERR_INVALID_ARG;
+  const Layout& l = cache_layout(cache);
+  if (layer < 0 || layer >= l.L || sinks < 0) return TRR_ERR_INVALID_ARG;
+  trr_status st = check_sizes(l, num_chunks, num_tokens);
+  if (st != TRR_OK) return st;
+  cache_set_launches(cache, 0);
+  if (num_chunks == 0 || num_tokens == 0) return TRR_OK;
+  if (!seq_ids || !starts || !offsets || !q_bf16 || !modes || !out_bf16) return TRR_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(q_bf16) | reinterpret_cast<uintptr_t>(out_bf16)) & 15) return TRR_ERR_INVALID_ARG;
+  uint64_t least = 0;
+  st = trr_chunk_workspace_bytes(cache, num_chunks, num_tokens, 0, &least);
+  if (st != TRR_OK) return st;
+  if (!workspace || workspace_bytes < least || (reinterpret_cast<uintptr_t>(workspace) & 255)) return TRR_ERR_OUT_OF_MEMORY;
+  ChunkArgs g;
+  g.a = layer_args(l, cache_views(cache), layer);
+  g.a.wait_ns = cache_wait_ns(cache);
+  g.n = num_chunks; g.num_tokens = num_tokens; g.window_scalar = window_scalar; g.sinks = sinks;
+  g.ctas = cache_num_sms(cache);
+  g.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf(static_cast<float>(l.d))) * 1.4426950408889634f;
+  g.seq_ids = seq_ids; g.starts = starts; g.offsets = offsets; g.windows = windows; g.modes = modes;
+  g.q = static_cast<const uint16_t*>(q_bf16);
+  g.out = static_cast<uint16_t*>(out_bf16);
+  g.lse = lse;
+  const int64_t fixed = lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, 0), per_tile = 4ll * kChunkTile + 4ll * l.Hkv * kChunkTile * l.d;
+  const int64_t room = (static_cast<int64_t>(std::min<uint64_t>(workspace_bytes, 1ull << 60)) - fixed) / per_tile;
+  g.most_tiles = static_cast<int>(std::min<int64_t>(room, INT_MAX / kChunkTile));
+  lay_workspace(&g, static_cast<uint8_t*>(workspace), l, num_chunks, num_tokens, g.ctas, g.most_tiles);
+  cache_note_call(cache, layer);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int launches = 0;
+  cudaError_t e = launch_pdl(chunk_plan_kernel, dim3(num_chunks), dim3(kPlanChunkThreads), 0, s, g);
+  if (e == cudaSuccess) {
+    ++launches;
+    e = launch_pdl(l.d == 64 ? chunk_stage_kernel<64> : chunk_stage_kernel<128>, dim3(4 * g.ctas), dim3(kSpanThreads), 0, s, g);
+  }
+  if (e == cudaSuccess) {
+    ++launches;
+    e = launch_pdl(l.d == 64 ? chunk_rows_kernel<64> : chunk_rows_kernel<128>, dim3(4 * g.ctas), dim3(256), 0, s, g);
+  }
+  if (e == cudaSuccess) ++launches;
+  cache_set_launches(cache, launches);
+  return e == cudaSuccess ? TRR_OK : TRR_ERR_CUDA;
+}

@@ -1,0 +1,104 @@
+// trr_chunk.cuh - what the kernels of attention of chunks share: the plan, the staged tiles and the
+// call's arguments and workspace.
+#pragma once
+
+#include "trr_span.cuh"
+
+namespace trr {
+
+constexpr int kChunkTile = 128;      // tokens of a staged tile
+constexpr int kPipeRows = 128;       // rows of a softmax warpgroup: lanes of TMEM
+constexpr int kBlockRows = 2 * kPipeRows;
+constexpr int kPlanChunkThreads = 512;
+constexpr int kMostChunkTokens = 1 << 20;
+
+// One chunk.  Its stored tokens that any of its queries sees lie on a line of positions: 0 .. sinks-1,
+// then lo .. end-1 (sinks 0: one stretch).  They are staged in two lists in order of position: tokens
+// of 2, 4 and 8 bits as binary16, and those of 16 bits as they are.
+struct ChunkPlan {
+  int seq, start, len, row0;    // queries row0 .. row0+len-1 at positions start, start+1, ...
+  int sinks, lo, end, span;     // span: positions on the line
+  int full, local;              // queries of each mode (valid ones); the rest get zero rows
+  int tokens[2], dropped[2];    // staged tokens of each list; tokens between sinks and lo
+  int tile0, tiles[2];          // tiles of the pool: list 0, then list 1
+  int unit0, units;             // units of 64 positions before this chunk, of it
+  int block0, blocks;           // blocks of rows before it, of it
+  int pad[11];
+};
+static_assert(sizeof(ChunkPlan) == 128, "");
+
+// A block of rows: queries of one mode of a chunk (in order), their heads of one KV head.  Of each list
+// it sees tiles 0 .. head-1 (sinks) and first .. last-1.
+struct BlockPlan {
+  int chunk, row, rows, local;  // rows row .. of (list of queries of the mode) x (heads of a KV head)
+  int head[2], first[2], last[2];
+  int query0, tiles;            // the mode's first query in the list
+  int pad[4];
+};
+static_assert(sizeof(BlockPlan) == 64, "");
+
+struct ChunkHeader {
+  int64_t work, per;            // cost of all segments, a CTA's share
+  int bad;                      // error of the whole call: every row is zero
+  int blocks, units, tiles;
+  int splits, flagged;          // shares of the KV heads that staging CTAs take; some V of 16 bits is not finite
+  int pad[6];
+};
+
+// A piece of a segment that a CTA could not finish alone.
+struct PieceInfo {
+  int block, kvh, first_cta, ctas;  // block < 0: none.  The pieces are those of CTAs first_cta ..
+};
+
+struct ChunkArgs {
+  LayerArgs a;
+  int n, num_tokens, window_scalar, sinks, ctas, most_tiles, most_blocks;
+  float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
+  const int32_t *seq_ids, *starts, *offsets, *windows;
+  const uint8_t* modes;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  // workspace
+  ChunkHeader* head;
+  ChunkPlan* chunk;   // [n]
+  int32_t* list;      // [num_tokens] a chunk's queries: its full ones in order, then its local ones, then the rest
+  BlockPlan* block;   // [most_blocks]
+  int64_t* base;      // [most_blocks + 1] cost before each block (all its KV heads)
+  int32_t* flag;      // [n][Hkv] some V of 16 bits staged for it is not finite
+  PieceInfo* piece;   // [ctas] the segment that a CTA began and did not finish
+  float2* part_ml;    // [2 * ctas][256] (m, l) of a CTA's first piece, or its last
+  float* part_o;      // [2 * ctas][256][D]
+  int32_t* pos;       // [most_tiles][128] positions of staged tokens, INT_MAX past the last
+  uint8_t* tile;      // [most_tiles][Hkv][K, V][128 x D] 16 bits, in the tensor core's layout
+};
+
+// A tile's row r holds its 16-byte chunk e at (chunks of 64 columns apart) + 128 r + 16 (e ^ r % 8).
+__device__ __forceinline__ int tile_at(int r, int e) { return (e >> 3) * (kChunkTile * 128) + r * 128 + (((e ^ r) & 7) << 4); }
+template <int D>
+__device__ __forceinline__ uint8_t* staged_tile(const ChunkArgs& g, int tile, int h, int which) {
+  return g.tile + ((static_cast<int64_t>(tile) * g.a.Hkv + h) * 2 + which) * (kChunkTile * D * 2);
+}
+
+// Where a row of a block comes from.
+struct RowSource {
+  int query, head;  // head: of all query heads
+  int t, lo;        // it sees tokens at positions <= t that are >= lo (or below the call's sinks, where it is local)
+};
+__device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkPlan& c, int query0, bool local, int kvh, int row) {
+  const int heads = g.a.Hq / g.a.Hkv;
+  RowSource r;
+  r.query = g.list[query0 + row / heads];
+  r.head = kvh * heads + row % heads;
+  r.t = c.start + r.query - c.row0;
+  r.lo = local ? r.t - (g.windows ? g.windows[r.query] : g.window_scalar) + 1 : 0;
+  return r;
+}
+
+// The cost of a segment: its tiles, and a fixed part for its start and end.
+constexpr int kChunkTileCost = 2, kChunkSegmentCost = 2;
+__device__ __forceinline__ int64_t chunk_cost(int tiles) {
+  return tiles > 0 ? kChunkSegmentCost + static_cast<int64_t>(kChunkTileCost) * tiles : 0;
+}
+
+}  // namespace trr

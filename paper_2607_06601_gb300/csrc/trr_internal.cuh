@@ -24,6 +24,11 @@ enum Ctrl : int {
   kForkError = 13,    // fork: an entry is invalid
   kForkOk = 14,       // fork: 1 when the plan may be carried out
   kGroupDone = 15,    // attention over groups: CTAs of the plan finished (the last one makes the jobs)
+  kReadBad = 16,      // reading back: INT_MAX - (16 * stretch + error) of the lowest failing one (0: none)
+  kReadDone = 17,     // reading back: CTAs finished (the last one records the status)
+  kChunkBad = 18,     // attention of chunks: INT_MAX - (16 * query + error) of the lowest failing one (0: none)
+  kChunkDone = 19,    // attention of chunks: CTAs of the plan finished (the last one lays chunks end to end)
+  kChunkPlanned = 20, // attention of chunks: CTAs that have planned their blocks (the last one lays them end to end)
   kCtrlInts = 64
 };
 

@@ -43,7 +43,7 @@ EXPORTS = ("trr_cache_required_bytes", "trr_create_cache", "trr_kv_append", "trr
            "trr_decode_step", "trr_decode_attn_static", "trr_route_decisions", "trr_kv_append_routed",
            "trr_decode_attn_routed", "trr_destroy", "trr_get_status", "trr_set_wait_limit", "trr_reset",
            "trr_get_region", "trr_workspace_bytes", "trr_fork", "trr_evict", "trr_free_seqs", "trr_compact",
-           "trr_decode_attn_sinks", "trr_decode_attn_shared",
+           "trr_decode_attn_sinks", "trr_decode_attn_shared", "trr_chunk_workspace_bytes", "trr_chunk_attn", "trr_kv_read",
            "trr_last_launch_count")
 
 _lib = None
@@ -87,6 +87,10 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     L.trr_compact.argtypes = [P, P, U64, P]
     L.trr_decode_attn_sinks.argtypes = [P, I32, I32, P, P, P, P, P, I32, I32, ctypes.c_float, P, P, U64, P]
     L.trr_decode_attn_shared.argtypes = [P, I32, I32, P, P, P, P, P, I32, I32, I32, P, ctypes.c_float, P, P, U64, P]
+    I64 = ctypes.c_int64
+    L.trr_chunk_workspace_bytes.argtypes = [P, I32, I32, I64, ctypes.POINTER(U64)]
+    L.trr_chunk_attn.argtypes = [P, I32, I32, P, P, P, I32, P, P, P, I32, I32, ctypes.c_float, P, P, P, U64, P]
+    L.trr_kv_read.argtypes = [P, I32, I32, P, P, P, I32, I32, P, I64, P, I64, P, P]
     for name in EXPORTS:
         getattr(L, name).restype = I32
     _lib = L
@@ -328,6 +332,57 @@ def trr_decode_attn_shared(cache, layer, seq_ids, q_positions, q, modes, windows
         _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
 
 
+def _check_stretches(seq_ids, starts, offsets):
+    n = seq_ids.numel()
+    _same_length(n, starts, "starts")
+    _same_length(n + 1, offsets, "offsets")
+    return n
+
+
+def trr_chunk_workspace_bytes(cache, num_chunks, num_tokens, max_keys) -> int:
+    out = ctypes.c_uint64()
+    _check("trr_chunk_workspace_bytes", load().trr_chunk_workspace_bytes(cache, num_chunks, num_tokens, int(max_keys), ctypes.byref(out)))
+    return int(out.value)
+
+
+def trr_chunk_attn(cache, layer, seq_ids, starts, offsets, q, modes, windows, window_scalar, sinks, softmax_scale, out, lse,
+                   workspace, stream=None):
+    """Attention of chunks of new tokens (see include/trr.h); lse may be None."""
+    n, tokens = _check_stretches(seq_ids, starts, offsets), modes.numel()
+    if windows is not None:
+        _same_length(tokens, windows, "windows")
+    _check("trr_chunk_attn", load().trr_chunk_attn(
+        cache, layer, n, _dev(seq_ids, torch.int32, "seq_ids"), _dev(starts, torch.int32, "starts"),
+        _dev(offsets, torch.int32, "offsets"), tokens, _dev(q, torch.bfloat16, "q"), _dev(modes, torch.uint8, "modes"),
+        _opt(windows, torch.int32, "windows"), int(window_scalar), int(sinks), float(softmax_scale),
+        _dev(out, torch.bfloat16, "out"), _opt(lse, torch.float32, "lse"), _dev(workspace, torch.uint8, "workspace"),
+        workspace.numel(), _stream(stream)))
+
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _rows_at(t, rows, name):
+    """Address and row stride (elements) of a CUDA tensor of `rows` rows, each of them contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in TYPES:
+        raise ValueError(f"{name} must be a CUDA tensor of float32 or bfloat16")
+    if t.dim() < 2 or t.shape[0] != rows or (rows and not t[0].is_contiguous()):
+        raise ValueError(f"{name} must have {rows} rows, each contiguous")
+    return t.data_ptr(), t.stride(0) if rows > 1 else t[0].numel() if rows else 0
+
+
+def trr_kv_read(cache, layer, seq_ids, starts, offsets, k, v, bits, stream=None):
+    """K and V of stretches read back into k and v, [rows][Hkv][d] (see include/trr.h); bits may be None."""
+    n, rows = _check_stretches(seq_ids, starts, offsets), k.shape[0]
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must have one type")
+    (k_at, k_stride), (v_at, v_stride) = _rows_at(k, rows, "k"), _rows_at(v, rows, "v")
+    _check("trr_kv_read", load().trr_kv_read(
+        cache, layer, n, _dev(seq_ids, torch.int32, "seq_ids"), _dev(starts, torch.int32, "starts"),
+        _dev(offsets, torch.int32, "offsets"), rows, TYPES[k.dtype], k_at, k_stride, v_at, v_stride,
+        _opt(bits, torch.uint8, "bits"), _stream(stream)))
+
+
 def trr_destroy(cache):
     _check("trr_destroy", load().trr_destroy(cache))
 
@@ -456,6 +511,55 @@ class Cache:
         trr_decode_attn_shared(self.handle, layer, seq_ids, q_positions, q, modes, windows, window_scalar, sinks,
                                group_offsets, softmax_scale, out, self.workspace(stream), stream)
         return out
+
+    def chunk_workspace(self, num_chunks, num_tokens, max_keys=None, stream=None) -> torch.Tensor:
+        """Device memory of a chunk_attn call on chunks of at most these sizes (see there)."""
+        keys = num_chunks * self.max_context if max_keys is None else max_keys
+        return _new(trr_chunk_workspace_bytes(self.handle, num_chunks, num_tokens, keys), torch.uint8, self.pool.device, stream)
+
+    def chunk_attn(self, layer, seq_ids, starts, offsets, q, modes, windows=None, window_scalar=0, sinks=0, softmax_scale=0.0,
+                   out=None, with_lse=False, lse=None, max_keys=None, workspace=None, stream=None):
+        """Attention of chunks of new tokens, which have been appended before: rows offsets[i] .. offsets[i+1]-1 of q
+        ([n][Hq][d]) are queries of sequence seq_ids[i] at positions starts[i], starts[i] + 1, ...; modes[n] and windows[n]
+        are theirs.  Returns the rows, and with `with_lse` (or an `lse` to write to) the logarithms of their softmax sums,
+        [n][Hq] float32.  Rows of a new `out` that no chunk names are not set.
+
+        max_keys: at most how many positions the chunks reach over, the sum of starts[i] + length; by default every
+        chunk's whole context.  It sizes the workspace, which is allocated for the call unless one of
+        `chunk_workspace` is given."""
+        n = modes.numel()
+        size = n * self.Hq * self.d
+        if q.numel() != size or (out is not None and out.numel() != size):
+            raise ValueError(f"q and out must have {size} elements ([n][Hq][d])")
+        if lse is None and with_lse:
+            lse = _new((n, self.Hq), torch.float32, q.device, stream)
+        if lse is not None and lse.numel() != n * self.Hq:
+            raise ValueError(f"lse must have {n * self.Hq} elements ([n][Hq])")
+        if out is None:
+            out = _new((n, self.Hq, self.d), torch.bfloat16, q.device, stream)
+        if workspace is None:
+            workspace = self.chunk_workspace(seq_ids.numel(), n, max_keys, stream)
+        trr_chunk_attn(self.handle, layer, seq_ids, starts, offsets, q, modes, windows, window_scalar, sinks, softmax_scale,
+                       out, lse, workspace, stream)
+        return out if lse is None else (out, lse)
+
+    def read(self, layer, seq_ids, starts, offsets, rows, dtype=torch.bfloat16, k=None, v=None, bits=None, stream=None):
+        """K, V ([rows][Hkv][d], bfloat16 or float32) and widths ([rows][Hkv] uint8, 0: not stored) of what the cache
+        holds: rows offsets[i] .. offsets[i+1]-1 are positions starts[i], starts[i] + 1, ... of sequence seq_ids[i].
+        k and v may be given (their rows contiguous, at any stride).  Rows of new tensors that no stretch names are
+        not set."""
+        shape = (rows, self.Hkv, self.d)
+        device = self.pool.device
+        k = _new(shape, dtype, device, stream) if k is None else k
+        v = _new(shape, k.dtype, device, stream) if v is None else v
+        bits = _new(shape[:2], torch.uint8, device, stream) if bits is None else bits
+        for t, name in ((k, "k"), (v, "v")):
+            if t.shape[0] != rows or t.numel() != rows * self.Hkv * self.d:
+                raise ValueError(f"{name} must have {rows} rows of {self.Hkv * self.d} elements ([rows][Hkv][d])")
+        if bits.numel() != rows * self.Hkv:
+            raise ValueError(f"bits must have {rows * self.Hkv} elements ([rows][Hkv])")
+        trr_kv_read(self.handle, layer, seq_ids, starts, offsets, k, v, bits, stream)
+        return k, v, bits
 
     def status(self, stream=None) -> int:
         return trr_get_status(self.handle, stream)

@@ -12,7 +12,7 @@ namespace trr {
 // Done once per cache at creation, so that calls stay legal inside stream capture.
 cudaError_t attn_configure() {
   cudaError_t (*const parts[])() = {configure_attn_cc, configure_attn_head_modes, configure_attn_mma,
-                                     configure_attn_step_cc, configure_attn_step_mma, configure_group};
+                                     configure_attn_step_cc, configure_attn_step_mma, configure_group, configure_chunk};
   for (auto part : parts) {
     const cudaError_t e = part();
     if (e != cudaSuccess) return e;

@@ -12,11 +12,17 @@
 //                        layout that the tensor core reads: binary16 for 2, 4 and 8 bits (z + c s rounded
 //                        once, 11 bits against the 8 of the output), bf16 for 16 bits, in lists of their
 //                        own, since a product's operands have one type.  And each block's tiles.
-//   chunk_rows_kernel    the rows.
+//   chunk_attn_kernel    one CTA per SM; all blocks' tiles, for every KV head, laid end to end are cut into
+//                        equal runs, so that a long segment is spread over CTAs and a CTA takes many short ones.
+//   chunk_join_kernel    joins the parts of rows that were cut, (m, l, o) by m' = max m,
+//                        l' = sum l 2^(m - m'), and so for o.
+//
+// A block's weights of tokens that a row does not see are 0, and 0 times infinity is not: where a stored V of
+// 16 bits is not finite (quantised ones always are), the join does that chunk's rows of the KV head one by one.
 #include <algorithm>
 #include <climits>
 
-#include "trr_chunk.cuh"
+#include "trr_chunk_tc.cuh"
 
 namespace trr {
 
@@ -465,24 +471,73 @@ __device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& c, 
   if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
+// One row of a cut segment, by eight lanes: D / 8 values each.
 template <int D>
-__global__ void __launch_bounds__(256) chunk_rows_kernel(const __grid_constant__ ChunkArgs g) {
+__device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const PieceInfo& piece, const BlockPlan& b, int r, int lane) {
+  constexpr int E = D / 8;
+  const int64_t cost = chunk_cost(b.tiles), S = g.base[piece.block] + piece.kvh * cost, per = g.head->per;
+  // parts: the last one of CTA `cta`, the first ones of those that follow
+  auto slot = [&](int j) { return static_cast<int64_t>(2 * j + (j == cta)) * kBlockRows + r; };
+  int end = cta + 1;
+  while (end < g.ctas && chunk_tiles_before(end * per - S, b.tiles) < b.tiles) ++end;
+  float m = -INFINITY, l = 0.f, o[E] = {};
+#pragma unroll 4
+  for (int j = cta; j < end; ++j) m = fmaxf(m, g.part_ml[slot(j)].x);
+#pragma unroll 2
+  for (int j = cta; j < end; ++j) {
+    const float2 ml = g.part_ml[slot(j)];
+    const float4* part = reinterpret_cast<const float4*>(g.part_o + slot(j) * D + lane * 4);
+    const float w = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - m);
+    float4 v[E / 4];
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) v[i] = part[8 * i];
+    l += ml.y * w;
+    if (w == 0.f) continue;  // (a part in which nothing was seen may hold anything)
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) {
+      o[4 * i] += v[i].x * w;
+      o[4 * i + 1] += v[i].y * w;
+      o[4 * i + 2] += v[i].z * w;
+      o[4 * i + 3] += v[i].w * w;
+    }
+  }
+  const RowSource s = row_source(g, g.chunk[b.chunk], b.query0, b.local, piece.kvh, b.row + r);
+  const int64_t at = static_cast<int64_t>(s.query) * g.a.Hq + s.head;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i)
+    *reinterpret_cast<uint2*>(g.out + at * D + 32 * i + 4 * lane) =
+        make_uint2(pack16(true, o[4 * i] * inv, o[4 * i + 1] * inv), pack16(true, o[4 * i + 2] * inv, o[4 * i + 3] * inv));
+  if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) chunk_join_kernel(const __grid_constant__ ChunkArgs g) {
+  constexpr int kJoinRows = 256 / 8;
   pdl_wait();
   pdl_trigger();
   if (g.head->bad) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, blocks = g.head->blocks;
+  const bool flagged = g.head->flagged;
+  auto careful = [&](const BlockPlan& b, int kvh) { return flagged && g.flag[static_cast<int64_t>(b.chunk) * g.a.Hkv + kvh]; };
+  for (int x = blockIdx.x; x < g.ctas * (kBlockRows / kJoinRows); x += gridDim.x) {
+    const int cta = x / (kBlockRows / kJoinRows), r = x % (kBlockRows / kJoinRows) * kJoinRows + threadIdx.x / 8;
+    const PieceInfo piece = g.piece[cta];
+    if (piece.block < 0) continue;
+    const BlockPlan& b = g.block[piece.block];
+    if (r < b.rows && !careful(b, piece.kvh)) join_row<D>(g, cta, piece, b, r, threadIdx.x & 7);
+  }
+  // rows with nothing stored in sight, and those that are done one by one
   for (int64_t x = blockIdx.x; x < static_cast<int64_t>(blocks) * g.a.Hkv; x += gridDim.x) {
     const BlockPlan& b = g.block[x / g.a.Hkv];
     const int kvh = static_cast<int>(x % g.a.Hkv);
+    if (b.tiles > 0 && !careful(b, kvh)) continue;
     const ChunkPlan& c = g.chunk[b.chunk];
-    if (b.tiles == 0) {  // nothing stored in sight
-      for (int r = warp; r < b.rows; r += 8) {
-        const RowSource s = row_source(g, c, b.query0, b.local, kvh, b.row + r);
-        zero_rows(g, s.query, s.head, s.head + 1, lane);
-      }
-      continue;
+    for (int r = warp; r < b.rows; r += 8) {
+      const RowSource s = row_source(g, c, b.query0, b.local, kvh, b.row + r);
+      if (b.tiles == 0) zero_rows(g, s.query, s.head, s.head + 1, lane);
+      else one_row<D>(g, c, s, b.local, kvh, lane);
     }
-    for (int r = warp; r < b.rows; r += 8) one_row<D>(g, c, row_source(g, c, b.query0, b.local, kvh, b.row + r), b.local, kvh, lane);
   }
 }
 
@@ -515,6 +570,19 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->pos = reinterpret_cast<int32_t*>(take(4 * most_tiles * kChunkTile));
   g->tile = take(most_tiles * l.Hkv * 2 * kChunkTile * l.d * 2);
   return most_tiles ? off : fixed;
+}
+
+cudaError_t configure_chunk() {
+  auto one = [](void (*k)(ChunkArgs), int bytes) {
+    // its warpgroups share out the registers of the launch: no fewer than they were counted on
+    cudaFuncAttributes at;
+    const cudaError_t e = cudaFuncGetAttributes(&at, k);
+    if (e != cudaSuccess) return e;
+    if (at.numRegs * kChunkThreads < 256 * kChunkSoftmaxRegisters + 128 * kChunkOtherRegisters) return cudaErrorInvalidConfiguration;
+    return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  const cudaError_t e = one(chunk_attn_kernel<64>, ChunkSmem<64>::kTotal + 1024);
+  return e != cudaSuccess ? e : one(chunk_attn_kernel<128>, ChunkSmem<128>::kTotal + 1024);
 }
 
 }  // namespace trr
@@ -581,7 +649,12 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   }
   if (e == cudaSuccess) {
     ++launches;
-    e = launch_pdl(l.d == 64 ? chunk_rows_kernel<64> : chunk_rows_kernel<128>, dim3(4 * g.ctas), dim3(256), 0, s, g);
+    e = l.d == 64 ? launch_pdl(chunk_attn_kernel<64>, dim3(g.ctas), dim3(kChunkThreads), ChunkSmem<64>::kTotal + 1024, s, g)
+                  : launch_pdl(chunk_attn_kernel<128>, dim3(g.ctas), dim3(kChunkThreads), ChunkSmem<128>::kTotal + 1024, s, g);
+  }
+  if (e == cudaSuccess) {
+    ++launches;
+    e = launch_pdl(l.d == 64 ? chunk_join_kernel<64> : chunk_join_kernel<128>, dim3(8 * g.ctas), dim3(256), 0, s, g);
   }
   if (e == cudaSuccess) ++launches;
   cache_set_launches(cache, launches);

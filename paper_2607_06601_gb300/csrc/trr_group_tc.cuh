@@ -531,14 +531,6 @@ __device__ __forceinline__ void group_mma(const Ctx<D>& x) {
   mbar_wait(x.drained(), 0);
 }
 
-__device__ __forceinline__ uint32_t pack16(bool bf16, float a, float b) {
-  if (bf16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  return as_u32(__floats2half2_rn(a, b));
-}
-
 // Scores out of sight become -infinity: their weight is 0 and they are no maximum.
 template <int N>
 __device__ __forceinline__ void mask_scores(uint32_t (&s)[N], const uint16_t* masks) {
@@ -549,39 +541,6 @@ __device__ __forceinline__ void mask_scores(uint32_t (&s)[N], const uint16_t* ma
     for (int i = 0; i < 16; ++i)
       if (!(mask >> i & 1)) s[16 * k + i] = 0xFF800000u;
   }
-}
-
-template <int N>
-__device__ __forceinline__ float highest(const uint32_t (&s)[N]) {
-  float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // four chains
-#pragma unroll
-  for (int i = 0; i < N; i += 2)
-    asm("max.f32 %0, %0, %1, %2;" : "+f"(t[i / 2 % 4]) : "f"(__uint_as_float(s[i])), "f"(__uint_as_float(s[i + 1])));
-  return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-}
-
-// Scores become their weights 2^(s f + shift); returns the weights' sum.
-template <int N>
-__device__ __forceinline__ float weigh(uint32_t (&s)[N], float f, float shift) {
-  uint64_t sum[2] = {0, 0}, ff, hh;
-  asm("mov.b64 %0, {%1, %1};" : "=l"(ff) : "f"(f));
-  asm("mov.b64 %0, {%1, %1};" : "=l"(hh) : "f"(shift));
-#pragma unroll
-  for (int i = 0; i < N; i += 2) {
-    uint64_t x;
-    float x0, x1;
-    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %4;\n}" : "=l"(x) : "r"(s[i]), "r"(s[i + 1]), "l"(ff), "l"(hh));
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x));
-    x0 = exp2_approx(x0);
-    x1 = exp2_approx(x1);
-    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum[i / 2 % 2]) : "f"(x0), "f"(x1));
-    s[i] = __float_as_uint(x0);
-    s[i + 1] = __float_as_uint(x1);
-  }
-  float a, b, c, d;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(sum[0]));
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(c), "=f"(d) : "l"(sum[1]));
-  return (a + b) + (c + d);
 }
 
 // The softmax warps.  Warps w and w + 4 share 32 rows (lanes of TMEM); of the tokens of a tile

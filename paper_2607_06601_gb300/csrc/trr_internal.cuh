@@ -194,6 +194,7 @@ inline trr_status check_workspace(const trr_cache* c, const void* workspace, uin
 // One-time kernel attribute setup (defined in trr_attn.cu).
 cudaError_t attn_configure();
 cudaError_t configure_group();  // defined in trr_group.cu
+cudaError_t configure_chunk();  // defined in trr_chunk.cu
 
 // ------------------------------------------------------------------ PTX helpers --
 

@@ -91,6 +91,14 @@ __device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint64_t b, uint3
       : "memory");
 }
 
+// The same with A in shared memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+      "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add))
+      : "memory");
+}
+
 // One lane of a converged warp.
 __device__ __forceinline__ bool elected() {
   uint32_t yes;

@@ -40,7 +40,7 @@ struct ChunkSmem {
   static constexpr int kPos = kV + kSlots * kTile;
   static constexpr int kSeg = kPos + kPosSlots * kChunkTile * 4;
   static constexpr int kBars = kSeg + kSpanSlots * static_cast<int>(sizeof(ChunkSegment));
-  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 6;
+  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 7;
   static constexpr int kTotal = kBars + 8 * kNumBars;
   static_assert(kTotal + 1024 <= 227 * 1024, "");
 };
@@ -61,13 +61,13 @@ struct ChunkCtx {
   __device__ uint64_t* pos_empty(int i) const { return bar(4 * L::kSlots + kPosSlots + i); }
   __device__ uint64_t* seg_full(int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + i); }
   __device__ uint64_t* seg_empty(int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + kSpanSlots + i); }
-  __device__ uint64_t* half_bar(int half, int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 6 * half + i); }
+  __device__ uint64_t* half_bar(int half, int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 7 * half + i); }
   __device__ uint64_t* q_full(int half) const { return half_bar(half, 0); }
   __device__ uint64_t* s_full(int half) const { return half_bar(half, 1); }
   __device__ uint64_t* s_read(int half) const { return half_bar(half, 2); }
-  __device__ uint64_t* p_full(int half) const { return half_bar(half, 3); }
-  __device__ uint64_t* o_done(int half) const { return half_bar(half, 4); }
-  __device__ uint64_t* drained(int half) const { return half_bar(half, 5); }
+  __device__ uint64_t* p_full(int half, int part) const { return half_bar(half, 3 + part); }  // the weights of 64 tokens
+  __device__ uint64_t* o_done(int half) const { return half_bar(half, 5); }
+  __device__ uint64_t* drained(int half) const { return half_bar(half, 6); }
   __device__ ChunkSegment& seg(int i) const { return reinterpret_cast<ChunkSegment*>(base + L::kSeg)[i]; }
   __device__ const int32_t* pos(int i) const { return reinterpret_cast<const int32_t*>(base + L::kPos) + i * kChunkTile; }
   // TMEM columns.  d 128: S and O of each half, P over S.  d 64: P has columns of its own, so that the next
@@ -242,22 +242,33 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
     for (int i = 0; i < n && ok; ++i, ++it, ++tile) {
       if (early && i + 1 < n) ok = x.wait_warp(x.s_read(half), it & 1) && scores(tile + 1);
       const int slot = tile % L::kSlots;
-      ok = ok && x.wait_warp(x.v_full(slot), (tile / L::kSlots) & 1) && x.wait_warp(x.p_full(half), it & 1);
-      if (!ok) break;
-      tc_fence_after();
+      ok = ok && x.wait_warp(x.v_full(slot), (tile / L::kSlots) & 1);
       const uint64_t d = tc_desc(smem_u32(x.base) + L::kV + slot * L::kTile, kChunkTile * 128);
-      if (elected()) {
+      for (int part = 0; part < 2 && ok; ++part) {  // 64 tokens at a time, as their weights come
+        ok = x.wait_warp(x.p_full(half, part), it & 1);
+        if (!ok) break;
+        tc_fence_after();
+        if (elected()) {
 #pragma unroll
-        for (int k = 0; k < kChunkTile / 16; ++k)
-          tc_mma(x.col_o(half), x.col_p(half) + 8 * k, d + k * (2048 >> 4), id_o, k > 0 || i > 0 || !first);
-        if (wide) {  // the weights' low parts
+          for (int j = 0; j < kChunkTile / 32; ++j) {
+            const int k = part * (kChunkTile / 32) + j;
+            tc_mma(x.col_o(half), x.col_p(half) + 8 * k, d + k * (2048 >> 4), id_o, k > 0 || i > 0 || !first);
+          }
+          if (wide) {  // the weights' low parts
 #pragma unroll
-          for (int k = 0; k < kChunkTile / 16; ++k) tc_mma(x.col_o(half), x.col_low(half) + 8 * k, d + k * (2048 >> 4), id_o, true);
+            for (int j = 0; j < kChunkTile / 32; ++j) {
+              const int k = part * (kChunkTile / 32) + j;
+              tc_mma(x.col_o(half), x.col_low(half) + 8 * k, d + k * (2048 >> 4), id_o, true);
+            }
+          }
+          if (part == 1) {
+            tc_commit(x.v_empty(slot));
+            tc_commit(x.o_done(half));
+          }
         }
-        tc_commit(x.v_empty(slot));
-        tc_commit(x.o_done(half));
+        __syncwarp();
       }
-      __syncwarp();
+      if (!ok) break;
       if (!early && i + 1 < n) ok = x.wait_warp(x.o_done(half), it & 1) && scores(tile + 1);
     }
   }
@@ -350,20 +361,20 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     const bool local = g.block[sg.block].local;
     if (sg.first) m = -INFINITY, l = 0.f;
     for (int i = 0; i < sg.tiles; ++i, ++it, ++tile) {
+      const int slot = tile % kPosSlots;
+      if (!x.wait_warp(x.pos_full(slot), (tile / kPosSlots) & 1)) return;
+      const int32_t* pos = x.pos(slot);
+      const bool all = __all_sync(0xffffffffu, pos[kChunkTile - 1] <= src.t && pos[0] >= src.lo);
       if (!x.wait_warp(x.s_full(half), it & 1)) return;
       tc_fence_after();
       uint32_t s[2][64];
-      tmem_ld(s[0], col_s);
-      tmem_ld(s[1], col_s + 64);
+      tmem_ld(s, col_s);
       if (D == 64) {  // the next scores may come
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(x.s_read(half));
       }
-      const int slot = tile % kPosSlots;
-      if (!x.wait_warp(x.pos_full(slot), (tile / kPosSlots) & 1)) return;
-      const int32_t* pos = x.pos(slot);
-      if (!__all_sync(0xffffffffu, pos[kChunkTile - 1] <= src.t && pos[0] >= src.lo)) {
+      if (!all) {
         const int c = below(pos, src.t + 1), from = pos[0] >= src.lo ? 0 : below(pos, src.lo), head = local && from > 0 ? below(pos, g.sinks) : 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -417,11 +428,11 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
           for (int k = 0; k < 32; ++k) p[k] = pack16(false, __uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1]));
         }
         tmem_st(col_p + 32 * h, p);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x.p_full(half, h));  // the product of these tokens can start
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(x.p_full(half));
     }
     if (!sg.last) continue;
     // rows out: the output itself, or (m, l, o) for the join
@@ -480,7 +491,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
     for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
     for (int h = 0; h < 2; ++h) {
       mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
-      mbar_init(x.p_full(h), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
+      mbar_init(x.p_full(h, 0), 4), mbar_init(x.p_full(h, 1), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
     }
     fence_barrier_init();
   }

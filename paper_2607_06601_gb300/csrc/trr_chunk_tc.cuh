@@ -2,9 +2,8 @@
 //
 // One CTA per SM.  A producer warp brings tiles of 128 tokens (K, V, positions) into rings of shared
 // memory, as they were staged, with bulk copies.  A block's rows are two halves of 128, one to a lane of
-// TMEM, and each half has a warp that issues its products S = Q K^T and O += P V and a warpgroup that does
-// its softmax, a thread a row; the halves share the tiles and nothing else, so that one's products run
-// under the other's exponentials.  Sums and statistics are binary32.
+// TMEM; one thread issues the products S = Q K^T and O += P V of both, and each half has a warpgroup that
+// does its softmax, a thread a row, under the other half's products.  Sums and statistics are binary32.
 //
 // Tokens of 2, 4 and 8 bits are binary16, and p is rounded to it.  Tokens of 16 bits are bf16, in tiles of
 // their own that follow, and p there is a sum of two bf16 numbers (one, of 8 bits, would add as much error
@@ -15,7 +14,7 @@
 
 namespace trr {
 
-constexpr int kChunkSoftmaxWarps = 8, kChunkProducer = 8, kChunkMma = 9;  // warps 9 and 10 issue the halves' products
+constexpr int kChunkSoftmaxWarps = 8, kChunkProducer = 8, kChunkMma = 9;
 constexpr int kChunkThreads = 384;
 // Registers a thread: 168 at launch; the softmax warpgroups take what the third gives up.
 constexpr int kChunkLaunchRegisters = 168, kChunkSoftmaxRegisters = 208, kChunkOtherRegisters = 88;
@@ -40,7 +39,7 @@ struct ChunkSmem {
   static constexpr int kPos = kV + kSlots * kTile;
   static constexpr int kSeg = kPos + kPosSlots * kChunkTile * 4;
   static constexpr int kBars = kSeg + kSpanSlots * static_cast<int>(sizeof(ChunkSegment));
-  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 7;
+  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 7 + 1;
   static constexpr int kTotal = kBars + 8 * kNumBars;
   static_assert(kTotal + 1024 <= 227 * 1024, "");
 };
@@ -67,14 +66,18 @@ struct ChunkCtx {
   __device__ uint64_t* s_read(int half) const { return half_bar(half, 2); }
   __device__ uint64_t* p_full(int half, int part) const { return half_bar(half, 3 + part); }  // the weights of 64 tokens
   __device__ uint64_t* o_done(int half) const { return half_bar(half, 5); }
-  __device__ uint64_t* drained(int half) const { return half_bar(half, 6); }
+  __device__ uint64_t* o_half(int half) const { return half_bar(half, 6); }  // the first 64 tokens of a wide tile (d 64)
+  __device__ uint64_t* drained() const { return half_bar(2, 0); }
   __device__ ChunkSegment& seg(int i) const { return reinterpret_cast<ChunkSegment*>(base + L::kSeg)[i]; }
   __device__ const int32_t* pos(int i) const { return reinterpret_cast<const int32_t*>(base + L::kPos) + i * kChunkTile; }
-  // TMEM columns.  d 128: S and O of each half, P over S.  d 64: P has columns of its own, so that the next
-  // scores can be issued once these have been read; the low parts of a wide tile's weights lie over S.
+  // TMEM columns.  d 128: S and O of each half, P over S, a wide tile's weights as 64 columns of high parts and
+  // 64 of low ones.  d 64: P has columns of its own, so that the next scores can be issued once these have been
+  // read; a wide tile's weights take turns in them, 64 tokens at a time.
   __device__ uint32_t col_s(int half) const { return tmem + 128 * half; }
-  __device__ uint32_t col_p(int half) const { return D == 128 ? col_s(half) : tmem + 256 + 64 * half; }
-  __device__ uint32_t col_low(int half) const { return D == 128 ? col_s(half) + 64 : col_s(half); }
+  __device__ uint32_t col_p(int half, int part, int wide) const {
+    return D == 128 ? col_s(half) + 32 * part : tmem + 256 + 64 * half + (wide ? 0 : 32 * part);
+  }
+  __device__ uint32_t col_low(int half, int part) const { return D == 128 ? col_s(half) + 64 + 32 * part : tmem + 256 + 64 * half + 32; }
   __device__ uint32_t col_o(int half) const { return tmem + (D == 128 ? 256 + 128 * half : 384 + 64 * half); }
   // A bounded wait; once one has given up, none waits any more.
   __device__ bool wait(uint64_t* b, uint32_t parity) const {
@@ -192,37 +195,30 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   for (int k = max(0, pos_copies - kPosSlots); k < pos_copies; ++k) mbar_wait(x.pos_full(k % kPosSlots), (k / kPosSlots) & 1);
 }
 
-// The warp that issues a half's products (one elected lane does; the whole warp goes along).
+// The warp that issues the products (one elected lane does; the whole warp goes along).  The halves take
+// turns, O += P V of a tile and S of the next: then one half's softmax runs under the other's products.
+// (Left to warps of their own the two fell into step: both waited for the tensor core, then both for the
+// exponentials.)  A wait stands before scores that go over weights: nothing orders the two products.
 template <int D>
-__device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
+__device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x) {
   using L = ChunkSmem<D>;
-  int segs = 0, tile = 0, it = 0, loads = 0;  // tile: of the CTA, it: of this half, loads: of Q
-  const uint32_t q_desc = smem_u32(x.base) + half * L::kTile;
+  int segs = 0, tile = 0, it[2] = {0, 0}, loads[2] = {0, 0};  // tile: of the CTA, it: of a half, loads: of its Q
+  const uint32_t base = smem_u32(x.base);
   for (bool ok = true; ok;) {
     if (!x.wait_warp(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) break;
     const ChunkSegment& sg = x.seg(segs % kSpanSlots);
     const int n = __shfl_sync(0xffffffffu, sg.tiles, 0), wide = __shfl_sync(0xffffffffu, sg.wide, 0);
-    const bool first = __shfl_sync(0xffffffffu, sg.first, 0), live = __shfl_sync(0xffffffffu, sg.rows, 0) > half * kPipeRows;
+    const bool first = __shfl_sync(0xffffffffu, sg.first, 0);
+    const int halves = __shfl_sync(0xffffffffu, sg.rows, 0) > kPipeRows ? 2 : 1;
     __syncwarp();
     if (elected()) mbar_arrive(x.seg_empty(segs % kSpanSlots));
     ++segs;
     if (n == 0) break;
-    if (!live) {  // a half without rows lets the tiles pass
-      for (int i = 0; i < n && ok; ++i, ++tile) {
-        const int slot = tile % L::kSlots, phase = (tile / L::kSlots) & 1;
-        ok = x.wait_warp(x.k_full(slot), phase);
-        if (ok && elected()) mbar_arrive(x.k_empty(slot));
-        ok = ok && x.wait_warp(x.v_full(slot), phase);
-        if (ok && elected()) mbar_arrive(x.v_empty(slot));
-      }
-      continue;
-    }
     const uint32_t id_s = tc_idesc(wide, kChunkTile, false), id_o = tc_idesc(wide, D, true);
-    auto scores = [&](int t) -> bool {  // S of tile t (of the CTA)
+    auto scores = [&](int half, int t) {  // S of tile t (of the CTA), whose K is there
       const int slot = t % L::kSlots;
-      if (!x.wait_warp(x.k_full(slot), (t / L::kSlots) & 1)) return false;
       tc_fence_after();
-      const uint64_t a = tc_desc(q_desc, 16), b = tc_desc(smem_u32(x.base) + L::kK + slot * L::kTile, 16);
+      const uint64_t a = tc_desc(base + half * L::kTile, 16), b = tc_desc(base + L::kK + slot * L::kTile, 16);
       if (elected()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -230,51 +226,70 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
           tc_mma_ss(x.col_s(half), a + o, b + o, id_s, k > 0);
         }
         tc_commit(x.s_full(half));
-        tc_commit(x.k_empty(slot));
+        if (half == halves - 1) tc_commit(x.k_empty(slot));
       }
       __syncwarp();
-      return true;
     };
-    // scores over these columns once the weights there have been used (or, with columns of their own, the last scores read)
-    const bool early = D == 64 && !wide;
-    if (it > 0) ok = x.wait_warp(x.o_done(half), (it - 1) & 1);
-    ok = ok && x.wait_warp(x.q_full(half), loads++ & 1) && scores(tile);
-    for (int i = 0; i < n && ok; ++i, ++it, ++tile) {
-      if (early && i + 1 < n) ok = x.wait_warp(x.s_read(half), it & 1) && scores(tile + 1);
+    auto keys = [&](int t) { return x.wait_warp(x.k_full(t % L::kSlots), (t / L::kSlots) & 1); };
+    auto values = [&](int half, int i) -> bool {  // O += P V of the segment's tile i
       const int slot = tile % L::kSlots;
-      ok = ok && x.wait_warp(x.v_full(slot), (tile / L::kSlots) & 1);
-      const uint64_t d = tc_desc(smem_u32(x.base) + L::kV + slot * L::kTile, kChunkTile * 128);
-      for (int part = 0; part < 2 && ok; ++part) {  // 64 tokens at a time, as their weights come
-        ok = x.wait_warp(x.p_full(half, part), it & 1);
-        if (!ok) break;
+      const uint64_t d = tc_desc(base + L::kV + slot * L::kTile, kChunkTile * 128);
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {  // 64 tokens at a time, as their weights come
+        if (!x.wait_warp(x.p_full(half, part), it[half] & 1)) return false;
         tc_fence_after();
         if (elected()) {
 #pragma unroll
           for (int j = 0; j < kChunkTile / 32; ++j) {
             const int k = part * (kChunkTile / 32) + j;
-            tc_mma(x.col_o(half), x.col_p(half) + 8 * k, d + k * (2048 >> 4), id_o, k > 0 || i > 0 || !first);
+            tc_mma(x.col_o(half), x.col_p(half, part, wide) + 8 * j, d + k * (2048 >> 4), id_o, k > 0 || i > 0 || !first);
           }
           if (wide) {  // the weights' low parts
 #pragma unroll
             for (int j = 0; j < kChunkTile / 32; ++j) {
               const int k = part * (kChunkTile / 32) + j;
-              tc_mma(x.col_o(half), x.col_low(half) + 8 * k, d + k * (2048 >> 4), id_o, true);
+              tc_mma(x.col_o(half), x.col_low(half, part) + 8 * j, d + k * (2048 >> 4), id_o, true);
             }
+            if (D == 64 && part == 0) tc_commit(x.o_half(half));
           }
           if (part == 1) {
-            tc_commit(x.v_empty(slot));
+            if (half == halves - 1) tc_commit(x.v_empty(slot));
             tc_commit(x.o_done(half));
           }
         }
         __syncwarp();
       }
-      if (!ok) break;
-      if (!early && i + 1 < n) ok = x.wait_warp(x.o_done(half), it & 1) && scores(tile + 1);
+      ++it[half];
+      return true;
+    };
+    ok = keys(tile);
+    for (int h = 0; h < halves && ok; ++h) {
+      if (it[h] > 0) ok = x.wait_warp(x.o_done(h), (it[h] - 1) & 1);
+      ok = ok && x.wait_warp(x.q_full(h), loads[h]++ & 1);
+      if (ok) scores(h, tile);
+    }
+    for (int i = 0; i < n && ok; ++i, ++tile) {
+      const bool more = i + 1 < n;
+      if (D == 64 && more) {  // weights have columns of their own: the next scores as soon as these are read
+        ok = keys(tile + 1);
+        for (int h = 0; h < halves && ok; ++h) {
+          ok = x.wait_warp(x.s_read(h), it[h] & 1);
+          if (ok) scores(h, tile + 1);
+        }
+      }
+      ok = ok && x.wait_warp(x.v_full(tile % L::kSlots), (tile / L::kSlots) & 1);
+      for (int h = 0; h < halves && ok; ++h) {
+        ok = values(h, i);
+        if (D == 128 && more && ok) {
+          ok = (h > 0 || keys(tile + 1)) && x.wait_warp(x.o_done(h), (it[h] - 1) & 1);
+          if (ok) scores(h, tile + 1);
+        }
+      }
     }
   }
-  if (elected()) tc_commit(x.drained(half));  // nothing is in flight when the CTA ends
+  if (elected()) tc_commit(x.drained());  // nothing is in flight when the CTA ends
   __syncwarp();
-  mbar_wait(x.drained(half), 0);
+  mbar_wait(x.drained(), 0);
 }
 
 // How many of 128 ascending positions are below v.
@@ -298,8 +313,8 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   using L = ChunkSmem<D>;
   const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
-  const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_low = x.col_low(half) + lanes, col_o = x.col_o(half) + lanes;
-  int segs = 0, tile = 0, it = 0;
+  const uint32_t col_s = x.col_s(half) + lanes, col_o = x.col_o(half) + lanes;
+  int segs = 0, tile = 0, it = 0, wides = 0;
   float m = -INFINITY, l = 0.f, f = 0.f;
   RowSource src = {};
   bool mine = false;
@@ -414,20 +429,21 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         l += weigh(s[h], f, shift);
         if (D == 64 && h == 0 && it > 0 && !x.wait_warp(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
         uint32_t p[32];
-        if (sg.wide) {
+        if (sg.wide) {  // high parts cut off, low parts what is left, rounded
           uint32_t low[32];
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
-            const float a = __uint_as_float(s[h][2 * k]), b = __uint_as_float(s[h][2 * k + 1]);
-            p[k] = pack16(true, a, b);
-            low[k] = pack16(true, a - bf16lo(p[k]), b - bf16hi(p[k]));
+            const uint32_t a = s[h][2 * k], b = s[h][2 * k + 1];
+            p[k] = __byte_perm(a, b, 0x7632);
+            low[k] = pack16(true, __uint_as_float(a) - __uint_as_float(a & 0xFFFF0000u), __uint_as_float(b) - __uint_as_float(b & 0xFFFF0000u));
           }
-          tmem_st(col_low + 32 * h, low);
+          if (D == 64 && h == 1 && !x.wait_warp(x.o_half(half), wides++ & 1)) return;
+          tmem_st(x.col_low(half, h) + lanes, low);
         } else {
 #pragma unroll
           for (int k = 0; k < 32; ++k) p[k] = pack16(false, __uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1]));
         }
-        tmem_st(col_p + 32 * h, p);
+        tmem_st(x.col_p(half, h, sg.wide) + lanes, p);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -486,13 +502,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     s_abort = 0;
-    for (int i = 0; i < L::kSlots; ++i) mbar_init(x.k_full(i), 1), mbar_init(x.k_empty(i), 2), mbar_init(x.v_full(i), 1), mbar_init(x.v_empty(i), 2);
+    for (int i = 0; i < L::kSlots; ++i) mbar_init(x.k_full(i), 1), mbar_init(x.k_empty(i), 1), mbar_init(x.v_full(i), 1), mbar_init(x.v_empty(i), 1);
     for (int i = 0; i < kPosSlots; ++i) mbar_init(x.pos_full(i), 1), mbar_init(x.pos_empty(i), kChunkSoftmaxWarps);
-    for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
+    for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 1);
     for (int h = 0; h < 2; ++h) {
       mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
-      mbar_init(x.p_full(h, 0), 4), mbar_init(x.p_full(h, 1), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
+      mbar_init(x.p_full(h, 0), 4), mbar_init(x.p_full(h, 1), 4), mbar_init(x.o_done(h), 1), mbar_init(x.o_half(h), 1);
     }
+    mbar_init(x.drained(), 1);
     fence_barrier_init();
   }
   pdl_wait();
@@ -512,7 +529,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   } else {
     registers_down<kChunkOtherRegisters>();
     if (warp == kChunkProducer) chunk_produce<D>(g, x, lane);
-    else if (warp < kChunkMma + 2) chunk_mma<D>(x, warp - kChunkMma);
+    else if (warp == kChunkMma) chunk_mma<D>(x);
   }
   __syncwarp();
   tc_fence_before();

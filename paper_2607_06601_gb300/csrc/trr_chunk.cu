@@ -8,23 +8,26 @@
 //   chunk_plan_kernel    a CTA per chunk: its queries sorted by mode (a block of rows then has one mode
 //                        and reads no more than that mode sees), the positions that any of them sees,
 //                        how many tokens are stored there; the CTA that ends last lays chunks end to end.
-//   chunk_stage_kernel   the stored tokens in sight, in order of position, as tiles of 128 tokens in the
-//                        layout that the tensor core reads: binary16 for 2, 4 and 8 bits (z + c s rounded
-//                        once, 11 bits against the 8 of the output), bf16 for 16 bits, in lists of their
-//                        own, since a product's operands have one type.  And each block's tiles.
+//   chunk_stage_kernel   the stored tokens in sight, in order of position, as tiles in the layout that the tensor
+//                        core reads, in binary16: z + c s rounded once (11 bits against the 8 of the output), 16-bit
+//                        values as they are.  And each block's tiles.
 //   chunk_attn_kernel    one CTA per SM; all blocks' tiles, for every KV head, laid end to end are cut into
 //                        equal runs, so that a long segment is spread over CTAs and a CTA takes many short ones.
 //   chunk_join_kernel    joins the parts of rows that were cut, (m, l, o) by m' = max m,
 //                        l' = sum l 2^(m - m'), and so for o.
 //
-// A block's weights of tokens that a row does not see are 0, and 0 times infinity is not: where a stored V of
-// 16 bits is not finite (quantised ones always are), the join does that chunk's rows of the KV head one by one.
+// A 16-bit value that binary16 does not hold flags its chunk and KV head: one of 65536 and more, an infinity or NaN,
+// or bits lost below 2^-24 in a row of K or V that has nothing above 2^-14 (other rows' lost bits are less than a
+// rounding of their largest value).  Flagged rows are done one by one in binary32, from the pages, by the join
+// kernel; so are rows that do not see a V that is not finite safe from it (0 times infinity).
 #include <algorithm>
 #include <climits>
 
 #include "trr_chunk_tc.cuh"
 
 namespace trr {
+
+constexpr int kStageCtas = 3;  // CTAs of the staging kernel on an SM
 
 // ------------------------------------------------------------------------------ plan --
 
@@ -146,10 +149,10 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     if (reads) {
       c.sinks = sinks; c.lo = lo; c.end = end; c.span = sinks + end - lo;
       for (int k = 0; k < kClasses; ++k) {
-        c.dropped[k == 3] += s_before[1][k] - s_before[0][k];
-        c.tokens[k == 3] += s_before[2][k] - s_before[1][k] + s_before[0][k];
+        c.dropped += s_before[1][k] - s_before[0][k];
+        c.tokens += s_before[2][k] - s_before[1][k] + s_before[0][k];
       }
-      for (int k = 0; k < 2; ++k) c.tiles[k] = (c.tokens[k] + kChunkTile - 1) / kChunkTile;
+      c.tiles = (c.tokens + chunk_tile(a.d) - 1) / chunk_tile(a.d);
       c.units = (c.span + kSpan - 1) / kSpan;
       c.blocks = (full * heads + kBlockRows - 1) / kBlockRows + (local * heads + kBlockRows - 1) / kBlockRows;
     }
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     int t = 0, u = 0, b = 0;
     if (x < g.n) {
       const volatile ChunkPlan* c = g.chunk + x;
-      t = c->tiles[0] + c->tiles[1]; u = c->units; b = c->blocks;
+      t = c->tiles; u = c->units; b = c->blocks;
     }
     int64_t all;
     const int64_t t0 = tiles + scan_before(t, s_sums, &all);
@@ -194,7 +197,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
       h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units); h.tiles = static_cast<int>(tiles);
       // a small call's heads are shared out among CTAs, so that staging fills the GPU
       const int64_t most = (2 * a.Hkv + kSpanThreads / 32 - 1) / (kSpanThreads / 32);
-      h.splits = static_cast<int>(units > 0 ? max(static_cast<int64_t>(1), min(most, 4 * g.ctas / units)) : 1);
+      h.splits = static_cast<int>(units > 0 ? max(static_cast<int64_t>(1), min(most, kStageCtas * g.ctas / units)) : 1);
     }
     *g.head = h;
     const int e = atomicExch(a.ctrl + kChunkBad, 0);
@@ -208,65 +211,40 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
 // z + c s of eight elements as binary16, rounded once; a value past binary16's largest stays at it
 // (a group's largest level may round past the largest value that the append takes).
 template <int B>
-__device__ __forceinline__ uint4 expand_f16(const Codes& x) {
-  const __half2 s = as_half2(__byte_perm(x.sz, 0, 0x1010)), z = as_half2(__byte_perm(x.sz, 0, 0x3232));
+__device__ __forceinline__ uint4 expand_f16(uint32_t w0, uint32_t w1, uint32_t sz) {
+  const __half2 s = as_half2(__byte_perm(sz, 0, 0x1010)), z = as_half2(__byte_perm(sz, 0, 0x3232));
   const __half2 k = as_half2(0x64006400u), top = as_half2(0x7BFF7BFFu);  // 1024 (1024 + c is exact), 65504
   uint32_t p[4];
   if (B == 8) {
-    p[0] = __byte_perm(x.w.x, 0x64646464u, 0x4140); p[1] = __byte_perm(x.w.x, 0x64646464u, 0x4342);
-    p[2] = __byte_perm(x.w.y, 0x64646464u, 0x4140); p[3] = __byte_perm(x.w.y, 0x64646464u, 0x4342);
+    p[0] = __byte_perm(w0, 0x64646464u, 0x4140); p[1] = __byte_perm(w0, 0x64646464u, 0x4342);
+    p[2] = __byte_perm(w1, 0x64646464u, 0x4140); p[3] = __byte_perm(w1, 0x64646464u, 0x4342);
   } else if (B == 4) {
     uint32_t t[4];  // elements i and i + 4
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = ((x.w.x >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
+    for (int i = 0; i < 4; ++i) t[i] = ((w0 >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
     p[0] = __byte_perm(t[0], t[1], 0x5410); p[1] = __byte_perm(t[2], t[3], 0x5410);
     p[2] = __byte_perm(t[0], t[1], 0x7632); p[3] = __byte_perm(t[2], t[3], 0x7632);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = ((x.w.x >> (4 * i)) & 3u) | ((x.w.x << (14 - 4 * i)) & 0x30000u) | 0x64006400u;
+    for (int i = 0; i < 4; ++i) p[i] = ((w0 >> (4 * i)) & 3u) | ((w0 << (14 - 4 * i)) & 0x30000u) | 0x64006400u;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) p[i] = as_u32(__hmin2(__hfma2(__hsub2(as_half2(p[i]), k), s, z), top));
   return make_uint4(p[0], p[1], p[2], p[3]);
 }
 
-template <int B, int D>
-__device__ __forceinline__ void stage_rows(const ChunkArgs& g, const ChunkPlan& ch, int chunk, const Found& f, int h0, int h1) {
-  constexpr int c = B == 2 ? 0 : B == 4 ? 1 : B == 8 ? 2 : 3, kLanes = D / 8, kStep = 32 / kLanes, kAhead = 4;
-  const int n = f.count[c], lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
-  if (n == 0) return;
-  for (int j = 2 * h0 + warp; j < 2 * h1; j += kSpanThreads / 32) {
-    const int h = j >> 1, which = j & 1;
-    for (int t0 = lane / kLanes; t0 < n; t0 += kAhead * kStep) {
-      Codes x[kAhead];
+// Eight bf16 values as binary16; their largest magnitude, and whether binary16 lacks bits of one.
+__device__ __forceinline__ uint4 convert_f16(uint4 v, uint32_t* top, bool* lost) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int t = t0 + u * kStep;
-        if (t < n) x[u] = load_codes<B, D>(g.a, f.token[c][t].page, f.token[c][t].slot, h, which, e, lg_group);
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int t = t0 + u * kStep;
-        if (t >= n) continue;
-        const int row = f.token[c][t].row;  // in the pool's rows
-        uint4 v = x[u].w;
-        if (B != 16) {
-          v = expand_f16<B == 16 ? 2 : B>(x[u]);
-        } else if (which == 1) {
-          // a V that is not finite must not reach rows that do not see it (0 times infinity): such chunks' rows are done one by one
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-          bool odd = false;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
-          if (odd) {
-            g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
-            g.head->flagged = 1;
-          }
-        }
-        *reinterpret_cast<uint4*>(staged_tile<D>(g, row / kChunkTile, h, which) + tile_at(row % kChunkTile, e)) = v;
-      }
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float a = bf16lo(w[i]), b = bf16hi(w[i]);
+    *top = max(*top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+    const uint32_t h = pack16(false, a, b);
+    *lost |= __low2float(as_half2(h)) != a || __high2float(as_half2(h)) != b;
+    w[i] = h;
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // The tiles that block b's rows see.
@@ -279,7 +257,7 @@ __device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) 
     else hi = mid - 1;
   }
   const ChunkPlan c = g.chunk[lo];
-  const int heads = a.Hq / a.Hkv, full_blocks = (c.full * heads + kBlockRows - 1) / kBlockRows;
+  const int heads = a.Hq / a.Hkv, full_blocks = (c.full * heads + kBlockRows - 1) / kBlockRows, T = chunk_tile(a.d);
   const bool local = b - c.block0 >= full_blocks;
   BlockPlan p = {};
   p.chunk = lo; p.local = local;
@@ -299,26 +277,18 @@ __device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) 
     from = __reduce_min_sync(0xffffffffu, from);
   }
   const int head = local ? min(g.sinks, from) : 0;
-  // ranks of three positions in both lists: lanes 0 .. 11, a class of a position each
-  const int which = lane >> 2, cls = lane & 3, x = which == 0 ? head : which == 1 ? from : t + 1;
-  int r = lane < 12 ? place_of(a, c.seq, cls, x).before : 0;
-  const int wide = __shfl_sync(0xffffffffu, r, (lane & ~3) | 3);
-  const int sum = r + __shfl_xor_sync(0xffffffffu, r, 1);  // lanes 0, 1: classes 0 and 1
-  const int narrow = __shfl_sync(0xffffffffu, sum, lane & ~3) + __shfl_sync(0xffffffffu, r, (lane & ~3) | 2);
-  int rank[2][3];
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    const int pos = k == 0 ? head : k == 1 ? from : t + 1;
-    rank[0][k] = __shfl_sync(0xffffffffu, narrow, 4 * k) - (pos >= c.lo ? c.dropped[0] : 0);
-    rank[1][k] = __shfl_sync(0xffffffffu, wide, 4 * k) - (pos >= c.lo ? c.dropped[1] : 0);
-  }
-  for (int l = 0; l < 2; ++l) {
-    p.head[l] = (rank[l][0] + kChunkTile - 1) / kChunkTile;
-    p.first[l] = rank[l][1] / kChunkTile;
-    p.last[l] = max(p.first[l], (rank[l][2] + kChunkTile - 1) / kChunkTile);
-    if (p.head[l] >= p.first[l]) p.head[l] = p.first[l] = 0;  // one stretch from the start
-    p.tiles += p.head[l] + p.last[l] - p.first[l];
-  }
+  // ranks of three positions: lanes 0 .. 11, a class of a position each
+  const int which = lane >> 2, x = which == 0 ? head : which == 1 ? from : t + 1;
+  int r = lane < 12 ? place_of(a, c.seq, lane & 3, x).before : 0;
+  r += __shfl_xor_sync(0xffffffffu, r, 1);
+  r += __shfl_xor_sync(0xffffffffu, r, 2);
+  if (x >= c.lo) r -= c.dropped;
+  const int rank0 = __shfl_sync(0xffffffffu, r, 0), rank1 = __shfl_sync(0xffffffffu, r, 4), rank2 = __shfl_sync(0xffffffffu, r, 8);
+  p.head = (rank0 + T - 1) / T;
+  p.first = rank1 / T;
+  p.last = max(p.first, (rank2 + T - 1) / T);
+  if (p.head >= p.first) p.head = p.first = 0;  // one stretch from the start
+  p.tiles = p.head + p.last - p.first;
   if (lane == 0) g.block[b] = p;
 }
 
@@ -331,8 +301,70 @@ __device__ __forceinline__ void zero_rows(const ChunkArgs& g, int q, int h0, int
     for (int h = lane; h < h1 - h0; h += 32) g.lse[at + h] = -INFINITY;
 }
 
+// The tokens that the CTA has found, of heads h0 .. h1 - 1: a warp takes eight (d 64) or four rows of a head's K or V
+// of one class at a time, 16 elements a lane.
 template <int D>
-__global__ void __launch_bounds__(kSpanThreads) chunk_stage_kernel(const __grid_constant__ ChunkArgs g) {
+__device__ __forceinline__ void stage_rows(const ChunkArgs& g, const Found& f, int chunk, int h0, int h1) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kAhead = 4, T = chunk_tile(D);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
+  const int groups = f.groups(kRows), items = 2 * (h1 - h0) * groups;
+  for (int x0 = warp; x0 < items; x0 += kAhead * (kSpanThreads / 32)) {
+    Codes16 x[kAhead];
+    int cls[kAhead], row[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int item = x0 + u * (kSpanThreads / 32), j = item / groups;
+      cls[u] = -1;
+      row[u] = -1;
+      if (item >= items) continue;
+      int first, n;
+      cls[u] = f.group(item - j * groups, kRows, &first, &n);
+      const int t = first + lane / kLanes;
+      if (t < n) {
+        const Found::Token& tok = f.token[cls[u]][t];
+        row[u] = tok.row;
+        x[u] = load_codes16<D>(g.a, cls[u], tok.page, tok.slot, h0 + (j >> 1), j & 1, e, lg_group);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (cls[u] < 0) continue;
+      const int j = (x0 + u * (kSpanThreads / 32)) / groups, h = h0 + (j >> 1);
+      uint4 v[2];
+      if (cls[u] == 3) {
+        uint32_t top = 0;
+        bool lost = false;
+        v[0] = convert_f16(x[u].w[0], &top, &lost);
+        v[1] = convert_f16(x[u].w[1], &top, &lost);
+        if (row[u] < 0) top = 0, lost = false;
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (top >= 0x4780u || (lost && top < 0x3880u)) {  // 65536, 2^-14 as bf16
+          g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
+          g.head->flagged = 1;
+        }
+      } else if (cls[u] == 2) {
+        v[0] = expand_f16<8>(x[u].w[0].x, x[u].w[0].y, x[u].sz);
+        v[1] = expand_f16<8>(x[u].w[0].z, x[u].w[0].w, x[u].sz);
+      } else if (cls[u] == 1) {
+        v[0] = expand_f16<4>(x[u].w[0].x, 0, x[u].sz);
+        v[1] = expand_f16<4>(x[u].w[0].y, 0, x[u].sz);
+      } else {
+        v[0] = expand_f16<2>(x[u].w[0].x, 0, x[u].sz);
+        v[1] = expand_f16<2>(x[u].w[0].x >> 16, 0, x[u].sz);
+      }
+      if (row[u] < 0) continue;
+      // two chunks of a sector, in the order of the row's place in its line
+      const int tile = row[u] / T, r = row[u] - tile * T;
+      const bool odd = r & 1;
+      store_sector(staged_tile<D>(g, tile, h, j & 1) + (tile_at(T, r, 2 * e) & ~31), odd ? v[1] : v[0], odd ? v[0] : v[1]);
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(const __grid_constant__ ChunkArgs g) {
+  constexpr int T = chunk_tile(D);
   __shared__ Found f;
   __shared__ int64_t s_sums[kSpanThreads / 32];
   __shared__ int s_last;
@@ -384,39 +416,28 @@ __global__ void __launch_bounds__(kSpanThreads) chunk_stage_kernel(const __grid_
       chunk = lo;
       c = g.chunk[chunk];
     }
-    __syncthreads();  // the last unit's tokens have been read
-    if (tid <= kClasses) f.count[tid] = 0;
-    __syncthreads();
     const int x = (unit - c.unit0) * kSpan + (tid >> 2), cls = tid & 3;
     const int pos = x < c.sinks ? x : x - c.sinks + c.lo;
     Place p{0, -1, 0};
     if (x < c.span) p = place_of(a, c.seq, cls, pos);
-    // rank among the staged tokens of the class's list: the sum over the list's classes
-    const int sum = p.before + __shfl_xor_sync(0xffffffffu, p.before, 1);
-    const int narrow = __shfl_sync(0xffffffffu, sum, lane & ~3) + __shfl_sync(0xffffffffu, p.before, (lane & ~3) | 2);
-    if (p.page >= 0) {
-      const int l = cls == 3, rank = (l ? p.before : narrow) - (pos >= c.lo ? c.dropped[l] : 0);
-      const int row = (c.tile0 + (l ? c.tiles[0] : 0)) * kChunkTile + rank;
-      f.token[cls][atomicAdd(&f.count[cls], 1)] = Found::Token{a.pool[cls] + p.page * a.page_bytes[cls], p.slot, row};
-      if (h0 == 0) g.pos[row] = pos;
-    }
-    __syncthreads();
-    stage_rows<16, D>(g, c, chunk, f, h0, h1);
-    stage_rows<8, D>(g, c, chunk, f, h0, h1);
-    stage_rows<4, D>(g, c, chunk, f, h0, h1);
-    stage_rows<2, D>(g, c, chunk, f, h0, h1);
+    // rank among the staged tokens: the sum over the classes
+    int rank = p.before;
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    const int row = c.tile0 * T + rank - (pos >= c.lo ? c.dropped : 0);
+    if (p.page >= 0 && h0 == 0) g.pos[row] = pos;
+    f.gather(a, p, cls, p.page >= 0 ? row : -1, tid);
+    stage_rows<D>(g, f, chunk, h0, h1);
   }
-  // rows of a list's last tile past its tokens are zero and out of sight; queries that read nothing have zero rows
-  for (int k = blockIdx.x; k < 2 * g.n; k += gridDim.x) {
-    const ChunkPlan& p = g.chunk[k >> 1];
-    const int l = k & 1, at = p.tokens[l] % kChunkTile;
+  // rows of a chunk's last tile past its tokens are zero and out of sight; queries that read nothing have zero rows
+  for (int k = blockIdx.x; k < g.n; k += gridDim.x) {
+    const ChunkPlan& p = g.chunk[k];
+    const int at = p.tokens % T, tile = p.tile0 + p.tiles - 1;
     if (at == 0) continue;
-    const int tile = p.tile0 + (l ? p.tiles[0] : 0) + p.tiles[l] - 1;
-    for (int r = at + tid; r < kChunkTile; r += kSpanThreads) g.pos[static_cast<int64_t>(tile) * kChunkTile + r] = INT_MAX;
-    for (int h = 0; h < a.Hkv; ++h)
-      for (int which = 0; which < 2; ++which)
-        for (int x = tid; x < (kChunkTile - at) * (D / 8); x += kSpanThreads)
-          *reinterpret_cast<uint4*>(staged_tile<D>(g, tile, h, which) + tile_at(at + x / (D / 8), x % (D / 8))) = make_uint4(0, 0, 0, 0);
+    for (int r = at + tid; r < T; r += kSpanThreads) g.pos[static_cast<int64_t>(tile) * T + r] = INT_MAX;
+    for (int j = 0; j < 2 * a.Hkv; ++j)
+      for (int x = tid; x < (T - at) * (D / 8); x += kSpanThreads)
+        *reinterpret_cast<uint4*>(staged_tile<D>(g, tile, j >> 1, j & 1) + tile_at(T, at + x / (D / 8), x % (D / 8))) = make_uint4(0, 0, 0, 0);
   }
   for (int k = blockIdx.x * (kSpanThreads / 32) + warp; k < g.num_tokens; k += gridDim.x * (kSpanThreads / 32)) {
     int lo = 0, hi = g.n - 1;  // places of the list: of the last chunk that starts at k or before it
@@ -432,34 +453,62 @@ __global__ void __launch_bounds__(kSpanThreads) chunk_stage_kernel(const __grid_
 
 // ------------------------------------------------------------------------------ rows --
 
-// One row, a warp: token after token, the statistics of the softmax running along.
+// Element j of K (which 0) or V (1) of KV head h of a stored token, in binary32.
 template <int D>
-__device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& c, const RowSource& s, bool local, int kvh, int lane) {
+__device__ __forceinline__ float stored_value(const LayerArgs& a, int c, const uint8_t* page, int slot, int h, int which, int j, int lg_group) {
+  const uint8_t* slice = page + a.hdr + static_cast<int64_t>(h) * a.slice[c];
+  const int lg = c + 1, row = D << lg >> 3;  // 2^lg bits an element
+  int64_t o = (static_cast<int64_t>(which) * a.P + slot) * row + (j << lg >> 3);
+  if (c >= 2 && a.swz) o = swz_off(o);
+  if (c == 3) return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(slice + o)) << 16);
+  const int code = slice[o] >> ((j << lg) & 7) & ((1 << (1 << lg)) - 1);
+  const __half2 sz = as_half2(reinterpret_cast<const uint32_t*>(slice + 2 * a.P * row)[(which * a.P + slot) * (D >> lg_group) + (j >> lg_group)]);
+  return __fmaf_rn(static_cast<float>(code), __low2float(sz), __high2float(sz));
+}
+
+// One row from the pages, by a warp: 32 tokens at a time, the statistics of the softmax running along.
+template <int D>
+__device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& ch, const RowSource& s, bool local, int kvh, int lane) {
   constexpr int E = D / 32;
-  const int64_t at = static_cast<int64_t>(s.query) * g.a.Hq + s.head;
-  float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
+  const LayerArgs& a = g.a;
+  const int64_t at = static_cast<int64_t>(s.query) * a.Hq + s.head;
+  const uint16_t* q = g.q + at * D;
+  const int lg_group = __ffs(a.G) - 1;
+  float o[E] = {}, m = -INFINITY, l = 0.f;
+  for (int c = 0; c < kClasses; ++c) {
+    const int64_t list = static_cast<int64_t>(ch.seq) * kClasses + c;
+    const int nt = a.ntok[list];
+    for (int k = 0; k * a.P < nt; ++k) {
+      if (a.pfirst[list * a.MP + k] > s.t) break;
+      const uint8_t* page = a.pool[c] + a.pt[list * a.MP + k] * a.page_bytes[c];
+      for (int s0 = 0; s0 < min(a.P, nt - k * a.P); s0 += 32) {
+        const int slot = s0 + lane;
+        const int pos = slot < min(a.P, nt - k * a.P) ? reinterpret_cast<const int32_t*>(page)[slot] : INT_MAX;
+        const bool see = pos <= s.t && (pos >= s.lo || (local && pos < g.sinks));
+        uint32_t left = __ballot_sync(0xffffffffu, see);
+        if (left == 0) continue;
+        float d = -INFINITY;
+        if (see) {
+          d = 0.f;
+          for (int j = 0; j < D; ++j) d += __uint_as_float(static_cast<uint32_t>(q[j]) << 16) * stored_value<D>(a, c, page, slot, kvh, 0, j, lg_group);
+          d *= g.scale_log2;
+        }
+        float next = fmaxf(m, d);
+        for (int x = 16; x > 0; x >>= 1) next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, x));
+        const float by = m == next ? 1.f : exp2f(m - next), p = d == -INFINITY ? 0.f : exp2f(d - next);
+        m = next;
+        float sum = p;
+        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        l = l * by + sum;
 #pragma unroll
-  for (int i = 0; i < E; ++i) q[i] = __uint_as_float(static_cast<uint32_t>(g.q[at * D + lane * E + i]) << 16);
-  for (int which = 0; which < 2; ++which) {
-    const int tile0 = c.tile0 + (which ? c.tiles[0] : 0);
-    for (int j = 0; j < c.tokens[which]; ++j) {
-      const int tile = tile0 + j / kChunkTile, r = j % kChunkTile, pos = g.pos[static_cast<int64_t>(tile) * kChunkTile + r];
-      if (pos > s.t) break;
-      if (pos < s.lo && !(local && pos < g.sinks)) continue;
-      const int e = lane * E;
-      const uint16_t* k = reinterpret_cast<const uint16_t*>(staged_tile<D>(g, tile, kvh, 0) + tile_at(r, e >> 3)) + (e & 7);
-      const uint16_t* v = reinterpret_cast<const uint16_t*>(staged_tile<D>(g, tile, kvh, 1) + tile_at(r, e >> 3)) + (e & 7);
-      auto value = [&](uint16_t x) { return which ? __uint_as_float(static_cast<uint32_t>(x) << 16) : __half2float(__ushort_as_half(x)); };
-      float d = 0.f;
+        for (int i = 0; i < E; ++i) o[i] *= by;
+        for (; left; left &= left - 1) {
+          const int from = __ffs(left) - 1;
+          const float w = __shfl_sync(0xffffffffu, p, from);
 #pragma unroll
-      for (int i = 0; i < E; ++i) d += q[i] * value(k[i]);
-      for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
-      d *= g.scale_log2;
-      const float next = fmaxf(m, d), by = m == next ? 1.f : exp2f(m - next), p = d == -INFINITY ? 0.f : exp2f(d - next);
-      m = next;
-      l = l * by + p;
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[i] = o[i] * by + p * value(v[i]);
+          for (int i = 0; i < E; ++i) o[i] += w * stored_value<D>(a, c, page, s0 + from, kvh, 1, lane * E + i, lg_group);
+        }
+      }
     }
   }
   const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -528,12 +577,13 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(const __grid_constant__
     if (r < b.rows && !careful(b, piece.kvh)) join_row<D>(g, cta, piece, b, r, threadIdx.x & 7);
   }
   // rows with nothing stored in sight, and those that are done one by one
-  for (int64_t x = blockIdx.x; x < static_cast<int64_t>(blocks) * g.a.Hkv; x += gridDim.x) {
-    const BlockPlan& b = g.block[x / g.a.Hkv];
-    const int kvh = static_cast<int>(x % g.a.Hkv);
+  for (int64_t x = blockIdx.x; x < static_cast<int64_t>(blocks) * g.a.Hkv * (kBlockRows / kJoinRows); x += gridDim.x) {
+    const int64_t y = x / (kBlockRows / kJoinRows);
+    const BlockPlan& b = g.block[y / g.a.Hkv];
+    const int kvh = static_cast<int>(y % g.a.Hkv), r0 = static_cast<int>(x % (kBlockRows / kJoinRows)) * kJoinRows;
     if (b.tiles > 0 && !careful(b, kvh)) continue;
     const ChunkPlan& c = g.chunk[b.chunk];
-    for (int r = warp; r < b.rows; r += 8) {
+    for (int r = r0 + warp; r < min(b.rows, r0 + kJoinRows); r += 8) {
       const RowSource s = row_source(g, c, b.query0, b.local, kvh, b.row + r);
       if (b.tiles == 0) zero_rows(g, s.query, s.head, s.head + 1, lane);
       else one_row<D>(g, c, s, b.local, kvh, lane);
@@ -566,9 +616,9 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->part_ml = reinterpret_cast<float2*>(take(8ll * 2 * ctas * kBlockRows));
   g->part_o = reinterpret_cast<float*>(take(4ll * 2 * ctas * kBlockRows * l.d));
   g->most_blocks = static_cast<int>(blocks);
-  const int64_t fixed = off;
-  g->pos = reinterpret_cast<int32_t*>(take(4 * most_tiles * kChunkTile));
-  g->tile = take(most_tiles * l.Hkv * 2 * kChunkTile * l.d * 2);
+  const int64_t fixed = off, T = chunk_tile(l.d);
+  g->pos = reinterpret_cast<int32_t*>(take(4 * most_tiles * T));
+  g->tile = take((most_tiles * l.Hkv * 2 * T * l.d * 2 + 1023) / 1024 * 1024);
   return most_tiles ? off : fixed;
 }
 
@@ -600,9 +650,9 @@ extern "C" trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t 
   const Layout& l = cache_layout(cache);
   const trr_status st = check_sizes(l, num_chunks, num_tokens);
   if (st != TRR_OK) return st;
-  // a chunk's lists end in a partly filled tile each
-  const int64_t keys = std::min(max_keys, static_cast<int64_t>(num_chunks) * l.maxctx), tiles = keys / kChunkTile + 2 * static_cast<int64_t>(num_chunks);
-  if (tiles > INT_MAX / kChunkTile) return TRR_ERR_UNSUPPORTED;
+  // a chunk ends in a partly filled tile
+  const int64_t keys = std::min(max_keys, static_cast<int64_t>(num_chunks) * l.maxctx), tiles = keys / chunk_tile(l.d) + num_chunks;
+  if (tiles > INT_MAX / chunk_tile(l.d)) return TRR_ERR_UNSUPPORTED;
   ChunkArgs g;
   *bytes = static_cast<uint64_t>(lay_workspace(&g, nullptr, l, num_chunks, num_tokens, cache_num_sms(cache), tiles));
   return TRR_OK;
@@ -635,9 +685,11 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   g.q = static_cast<const uint16_t*>(q_bf16);
   g.out = static_cast<uint16_t*>(out_bf16);
   g.lse = lse;
-  const int64_t fixed = lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, 0), per_tile = 4ll * kChunkTile + 4ll * l.Hkv * kChunkTile * l.d;
-  const int64_t room = (static_cast<int64_t>(std::min<uint64_t>(workspace_bytes, 1ull << 60)) - fixed) / per_tile;
-  g.most_tiles = static_cast<int>(std::min<int64_t>(room, INT_MAX / kChunkTile));
+  const int64_t fixed = lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, 0), T = chunk_tile(l.d), per_tile = 4 * T + 4 * l.Hkv * T * l.d;
+  const int64_t bytes = static_cast<int64_t>(std::min<uint64_t>(workspace_bytes, 1ull << 60));
+  int64_t room = std::min<int64_t>((bytes - fixed) / per_tile, INT_MAX / T);
+  if (lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, room) > bytes) --room;  // (its parts are rounded up)
+  g.most_tiles = static_cast<int>(room);
   lay_workspace(&g, static_cast<uint8_t*>(workspace), l, num_chunks, num_tokens, g.ctas, g.most_tiles);
   cache_note_call(cache, layer);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -645,7 +697,7 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   cudaError_t e = launch_pdl(chunk_plan_kernel, dim3(num_chunks), dim3(kPlanChunkThreads), 0, s, g);
   if (e == cudaSuccess) {
     ++launches;
-    e = launch_pdl(l.d == 64 ? chunk_stage_kernel<64> : chunk_stage_kernel<128>, dim3(4 * g.ctas), dim3(kSpanThreads), 0, s, g);
+    e = launch_pdl(l.d == 64 ? chunk_stage_kernel<64> : chunk_stage_kernel<128>, dim3(kStageCtas * g.ctas), dim3(kSpanThreads), 0, s, g);
   }
   if (e == cudaSuccess) {
     ++launches;

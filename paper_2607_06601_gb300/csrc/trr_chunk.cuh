@@ -6,34 +6,35 @@
 
 namespace trr {
 
-constexpr int kChunkTile = 128;      // tokens of a staged tile
-constexpr int kPipeRows = 128;       // rows of a softmax warpgroup: lanes of TMEM
-constexpr int kBlockRows = 2 * kPipeRows;
+// Tokens of a staged tile: as many as let the scores (binary32), the weights (binary16) and the sums of two halves
+// of 128 rows have TMEM columns of their own: 2 (T + T / 2 + d) <= 512, T a multiple of 16.
+__host__ __device__ constexpr int chunk_tile(int d) { return d == 64 ? 128 : 80; }
+constexpr int kHalfRows = 128;       // rows of a softmax warpgroup: lanes of TMEM
+constexpr int kBlockRows = 2 * kHalfRows;
 constexpr int kPlanChunkThreads = 512;
 constexpr int kMostChunkTokens = 1 << 20;
 
 // One chunk.  Its stored tokens that any of its queries sees lie on a line of positions: 0 .. sinks-1,
-// then lo .. end-1 (sinks 0: one stretch).  They are staged in two lists in order of position: tokens
-// of 2, 4 and 8 bits as binary16, and those of 16 bits as they are.
+// then lo .. end-1 (sinks 0: one stretch).  They are staged in order of position, as binary16.
 struct ChunkPlan {
   int seq, start, len, row0;    // queries row0 .. row0+len-1 at positions start, start+1, ...
   int sinks, lo, end, span;     // span: positions on the line
   int full, local;              // queries of each mode (valid ones); the rest get zero rows
-  int tokens[2], dropped[2];    // staged tokens of each list; tokens between sinks and lo
-  int tile0, tiles[2];          // tiles of the pool: list 0, then list 1
+  int tokens, dropped;          // staged tokens; tokens between sinks and lo
+  int tile0, tiles;             // tiles of the pool
   int unit0, units;             // units of 64 positions before this chunk, of it
   int block0, blocks;           // blocks of rows before it, of it
-  int pad[11];
+  int pad[14];
 };
 static_assert(sizeof(ChunkPlan) == 128, "");
 
-// A block of rows: queries of one mode of a chunk (in order), their heads of one KV head.  Of each list
-// it sees tiles 0 .. head-1 (sinks) and first .. last-1.
+// A block of rows: queries of one mode of a chunk (in order), their heads of one KV head.  It sees
+// the chunk's tiles 0 .. head-1 (sinks) and first .. last-1.
 struct BlockPlan {
   int chunk, row, rows, local;  // rows row .. of (list of queries of the mode) x (heads of a KV head)
-  int head[2], first[2], last[2];
-  int query0, tiles;            // the mode's first query in the list
-  int pad[4];
+  int head, first, last, tiles;
+  int query0;                   // the mode's first query in the list
+  int pad[7];
 };
 static_assert(sizeof(BlockPlan) == 64, "");
 
@@ -41,7 +42,7 @@ struct ChunkHeader {
   int64_t work, per;            // cost of all segments, a CTA's share
   int bad;                      // error of the whole call: every row is zero
   int blocks, units, tiles;
-  int splits, flagged;          // shares of the KV heads that staging CTAs take; some V of 16 bits is not finite
+  int splits, flagged;          // shares of the KV heads that staging CTAs take; some flag is set
   int pad[6];
 };
 
@@ -65,19 +66,19 @@ struct ChunkArgs {
   int32_t* list;      // [num_tokens] a chunk's queries: its full ones in order, then its local ones, then the rest
   BlockPlan* block;   // [most_blocks]
   int64_t* base;      // [most_blocks + 1] cost before each block (all its KV heads)
-  int32_t* flag;      // [n][Hkv] some V of 16 bits staged for it is not finite
+  int32_t* flag;      // [n][Hkv] some stored value is not to be had in binary16: its rows are done one by one
   PieceInfo* piece;   // [ctas] the segment that a CTA began and did not finish
   float2* part_ml;    // [2 * ctas][256] (m, l) of a CTA's first piece, or its last
   float* part_o;      // [2 * ctas][256][D]
-  int32_t* pos;       // [most_tiles][128] positions of staged tokens, INT_MAX past the last
-  uint8_t* tile;      // [most_tiles][Hkv][K, V][128 x D] 16 bits, in the tensor core's layout
+  int32_t* pos;       // [most_tiles][T] positions of staged tokens, INT_MAX past the last
+  uint8_t* tile;      // [most_tiles][Hkv][K, V][T x D] binary16, in the tensor core's layout
 };
 
-// A tile's row r holds its 16-byte chunk e at (chunks of 64 columns apart) + 128 r + 16 (e ^ r % 8).
-__device__ __forceinline__ int tile_at(int r, int e) { return (e >> 3) * (kChunkTile * 128) + r * 128 + (((e ^ r) & 7) << 4); }
+// A tile's row r holds its 16-byte chunk e at (chunks of 64 columns apart) + 128 r + 16 (e ^ r % 8); `rows` of the tile.
+__device__ __forceinline__ int tile_at(int rows, int r, int e) { return (e >> 3) * (rows * 128) + r * 128 + (((e ^ r) & 7) << 4); }
 template <int D>
 __device__ __forceinline__ uint8_t* staged_tile(const ChunkArgs& g, int tile, int h, int which) {
-  return g.tile + ((static_cast<int64_t>(tile) * g.a.Hkv + h) * 2 + which) * (kChunkTile * D * 2);
+  return g.tile + ((static_cast<int64_t>(tile) * g.a.Hkv + h) * 2 + which) * (chunk_tile(D) * D * 2);
 }
 
 // Where a row of a block comes from.

@@ -1,13 +1,18 @@
 // trr_chunk_tc.cuh - attention of blocks of 256 rows over staged tiles, on the tensor cores (tcgen05).
 //
-// One CTA per SM.  A producer warp brings tiles of 128 tokens (K, V, positions) into rings of shared
-// memory, as they were staged, with bulk copies.  A block's rows are two halves of 128, one to a lane of
-// TMEM; one thread issues the products S = Q K^T and O += P V of both, and each half has a warpgroup that
-// does its softmax, a thread a row, under the other half's products.  Sums and statistics are binary32.
+// One CTA per SM.  A producer warp brings tiles of tokens (K, V, positions) into rings of shared memory, as
+// they were staged, with bulk copies.  A block's rows are two halves of 128, one to a lane of TMEM; one thread
+// issues the products S = Q K^T and O += P V of both, and each half has a warpgroup that does its softmax, a
+// thread a row.  A block of 128 rows or fewer has its rows in both halves, which take its tiles in turn and are
+// joined at the end.  K, V and p are binary16, sums and statistics binary32; query rows are scaled by powers of
+// two.
 //
-// Tokens of 2, 4 and 8 bits are binary16, and p is rounded to it.  Tokens of 16 bits are bf16, in tiles of
-// their own that follow, and p there is a sum of two bf16 numbers (one, of 8 bits, would add as much error
-// as the output's own rounding).  Query rows are scaled by powers of two.
+// What bounds it: the products, and the time from a product's end to the next one that waits for it (about 450
+// cycles: completion, barrier, wait, issue).  So no product waits for another: scores, weights and sums have
+// columns of their own, and a tile's scores are issued as soon as the last ones have been read.  For that a tile
+// has 128 tokens at d 64 and 80 at d 128 (TMEM has 512 columns); with 128 tokens at d 128, weights over scores,
+// 2048 queries of 32 heads on 32768 tokens took 860 us.  A product of 128 x 80 x 16 from shared memory takes 51
+// cycles of its bandwidth against 40 of the tensor core's.
 #pragma once
 
 #include "trr_chunk.cuh"
@@ -21,32 +26,38 @@ constexpr int kChunkLaunchRegisters = 168, kChunkSoftmaxRegisters = 208, kChunkO
 static_assert(256 * kChunkSoftmaxRegisters + 128 * kChunkOtherRegisters <= kChunkThreads * kChunkLaunchRegisters, "");
 constexpr int kPosSlots = 4, kSpanSlots = 2;
 
-// A run of tiles of one type for one block and KV head, as the softmax and the product warps need it.
+// A run of tiles for one block and KV head, as the softmax warps and the product warp need it.
 struct ChunkSegment {
-  int tiles;        // 0: no more
-  int wide;         // tiles of 16-bit tokens
-  int first, last;  // of the block's runs in this CTA
-  int block, kvh, rows;
-  int dest;         // -1: the output rows, else the slot of the piece
+  int tiles;              // 0: no more
+  int block, kvh, rows;   // 128 rows or fewer: in both halves, which take the tiles in turn
+  int dest;               // -1: the output rows, else the slot of the piece
+  int pad[3];
 };
 
 template <int D>
 struct ChunkSmem {
-  static constexpr int kTile = kChunkTile * D * 2;  // bytes of K or V of a tile, or of Q of a half
-  static constexpr int kSlots = D == 64 ? 4 : 2;    // of K, and of V
-  static constexpr int kK = 2 * kTile;              // behind Q
+  static constexpr int kT = chunk_tile(D);
+  static constexpr int kQ = kHalfRows * D * 2;      // bytes of Q of a half
+  static constexpr int kTile = kT * D * 2;          // bytes of K or V of a tile
+  static constexpr int kSlots = D == 64 ? 4 : 3;    // of K, and of V
+  static constexpr int kK = 2 * kQ;                 // behind Q
   static constexpr int kV = kK + kSlots * kTile;
   static constexpr int kPos = kV + kSlots * kTile;
-  static constexpr int kSeg = kPos + kPosSlots * kChunkTile * 4;
+  static constexpr int kMl = kPos + kPosSlots * kT * 4;  // (m, l) of the second half's rows, for a join
+  static constexpr int kSeg = kMl + kHalfRows * 8;
   static constexpr int kBars = kSeg + kSpanSlots * static_cast<int>(sizeof(ChunkSegment));
-  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 7 + 1;
+  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 6 + 3;
   static constexpr int kTotal = kBars + 8 * kNumBars;
-  static_assert(kTotal + 1024 <= 227 * 1024, "");
+  static_assert(kTotal + 1024 + 64 <= 227 * 1024, "");
+  static_assert(kTile % 1024 == 0 && kQ >= 32 * kHalfRows * 4, "a join takes 32 columns at a time through Q's place");
 };
 
 template <int D>
 struct ChunkCtx {
   using L = ChunkSmem<D>;
+  static constexpr int kT = L::kT;
+  // a thread's scores are handed on in two parts
+  static constexpr int kPartA = D == 64 ? 64 : 48, kPartB = kT - kPartA;
   uint8_t* base;  // 1024-byte aligned
   uint32_t tmem;
   uint64_t wait_ns;
@@ -60,25 +71,21 @@ struct ChunkCtx {
   __device__ uint64_t* pos_empty(int i) const { return bar(4 * L::kSlots + kPosSlots + i); }
   __device__ uint64_t* seg_full(int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + i); }
   __device__ uint64_t* seg_empty(int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + kSpanSlots + i); }
-  __device__ uint64_t* half_bar(int half, int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 7 * half + i); }
+  __device__ uint64_t* half_bar(int half, int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 6 * half + i); }
   __device__ uint64_t* q_full(int half) const { return half_bar(half, 0); }
   __device__ uint64_t* s_full(int half) const { return half_bar(half, 1); }
   __device__ uint64_t* s_read(int half) const { return half_bar(half, 2); }
-  __device__ uint64_t* p_full(int half, int part) const { return half_bar(half, 3 + part); }  // the weights of 64 tokens
+  __device__ uint64_t* p_full(int half, int part) const { return half_bar(half, 3 + part); }
   __device__ uint64_t* o_done(int half) const { return half_bar(half, 5); }
-  __device__ uint64_t* o_half(int half) const { return half_bar(half, 6); }  // the first 64 tokens of a wide tile (d 64)
   __device__ uint64_t* drained() const { return half_bar(2, 0); }
+  __device__ uint64_t* join_full() const { return half_bar(2, 1); }
+  __device__ uint64_t* join_empty() const { return half_bar(2, 2); }
   __device__ ChunkSegment& seg(int i) const { return reinterpret_cast<ChunkSegment*>(base + L::kSeg)[i]; }
-  __device__ const int32_t* pos(int i) const { return reinterpret_cast<const int32_t*>(base + L::kPos) + i * kChunkTile; }
-  // TMEM columns.  d 128: S and O of each half, P over S, a wide tile's weights as 64 columns of high parts and
-  // 64 of low ones.  d 64: P has columns of its own, so that the next scores can be issued once these have been
-  // read; a wide tile's weights take turns in them, 64 tokens at a time.
-  __device__ uint32_t col_s(int half) const { return tmem + 128 * half; }
-  __device__ uint32_t col_p(int half, int part, int wide) const {
-    return D == 128 ? col_s(half) + 32 * part : tmem + 256 + 64 * half + (wide ? 0 : 32 * part);
-  }
-  __device__ uint32_t col_low(int half, int part) const { return D == 128 ? col_s(half) + 64 + 32 * part : tmem + 256 + 64 * half + 32; }
-  __device__ uint32_t col_o(int half) const { return tmem + (D == 128 ? 256 + 128 * half : 384 + 64 * half); }
+  __device__ const int32_t* pos(int i) const { return reinterpret_cast<const int32_t*>(base + L::kPos) + i * kT; }
+  // TMEM columns: scores, weights (two to a column), sums
+  __device__ uint32_t col_s(int half) const { return tmem + kT * half; }
+  __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 256 + 64 * half : 160 + 48 * half); }
+  __device__ uint32_t col_o(int half) const { return tmem + 512 - D * (2 - half); }
   // A bounded wait; once one has given up, none waits any more.
   __device__ bool wait(uint64_t* b, uint32_t parity) const {
     if (mbar_poll(smem_u32(b), parity, wait_ns)) return true;
@@ -112,8 +119,7 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   int tiles_done = 0, segs = 0, k_copies = 0, pos_copies = 0, v_copies = 0;
   bool ok = true;
   PieceInfo piece = {-1, 0, 0, 0};
-  auto push = [&](const ChunkSegment& s, const BlockPlan& p, const ChunkPlan& c, int from) {
-    if (!ok || s.tiles == 0) return;
+  auto push = [&](const ChunkSegment& s, const BlockPlan& p, int tile0, int from) {
     ok = x.wait_warp(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
     if (!ok) return;
     if (lane == 0) {
@@ -121,11 +127,10 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
       mbar_arrive(x.seg_full(segs % kSpanSlots));
     }
     ++segs;
-    const int l = s.wide, base = c.tile0 + (l ? c.tiles[0] : 0);
-    for (int i = from; i < from + s.tiles; ++i) {
-      const int tile = base + (i < p.head[l] ? i : p.first[l] + i - p.head[l]);
-      const int slot = tiles_done % L::kSlots, at = tiles_done % kPosSlots;
-      ok = x.wait_warp(x.k_empty(slot), ((tiles_done / L::kSlots) & 1) ^ 1);
+    for (int i = from; i < from + s.tiles; ++i, ++tiles_done) {
+      const int tile = tile0 + (i < p.head ? i : p.first + i - p.head);
+      const int slot = tiles_done % L::kSlots, at = tiles_done % kPosSlots, phase = ((tiles_done / L::kSlots) & 1) ^ 1;
+      ok = x.wait_warp(x.k_empty(slot), phase);
       if (!ok) return;
       if (lane == 0) {
         mbar_arrive_expect_tx(x.k_full(slot), L::kTile);
@@ -135,18 +140,17 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
       ok = x.wait_warp(x.pos_empty(at), ((tiles_done / kPosSlots) & 1) ^ 1);
       if (!ok) return;
       if (lane == 0) {
-        mbar_arrive_expect_tx(x.pos_full(at), 4 * kChunkTile);
-        bulk_g2s(x.base + L::kPos + at * 4 * kChunkTile, g.pos + static_cast<int64_t>(tile) * kChunkTile, 4 * kChunkTile, x.pos_full(at));
+        mbar_arrive_expect_tx(x.pos_full(at), 4 * L::kT);
+        bulk_g2s(x.base + L::kPos + at * 4 * L::kT, g.pos + static_cast<int64_t>(tile) * L::kT, 4 * L::kT, x.pos_full(at));
       }
       ++pos_copies;
-      ok = x.wait_warp(x.v_empty(slot), ((tiles_done / L::kSlots) & 1) ^ 1);
+      ok = x.wait_warp(x.v_empty(slot), phase);
       if (!ok) return;
       if (lane == 0) {
         mbar_arrive_expect_tx(x.v_full(slot), L::kTile);
         bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 1), L::kTile, x.v_full(slot));
       }
       ++v_copies;
-      ++tiles_done;
     }
   };
   if (b0 < b1) {
@@ -162,22 +166,18 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
       if (start >= b1) break;
       const BlockPlan p = g.block[b];
       if (p.tiles == 0) continue;
-      const ChunkPlan& c = g.chunk[p.chunk];
+      const int tile0 = g.chunk[p.chunk].tile0;
       const int64_t cost = chunk_cost(p.tiles);
       for (int h = static_cast<int>(max(static_cast<int64_t>(0), (b0 - start) / cost)); h < g.a.Hkv && ok; ++h) {
         const int64_t S = start + h * cost;
         if (S >= b1) break;
         const int t0 = chunk_tiles_before(b0 - S, p.tiles), t1 = chunk_tiles_before(b1 - S, p.tiles);
         if (t0 >= t1) continue;
-        const int narrow = p.head[0] + p.last[0] - p.first[0];
         if (t0 == 0 && t1 < p.tiles) piece = PieceInfo{b, h, 0, 0};
-        ChunkSegment s;
-        s.block = b; s.kvh = h; s.rows = p.rows;
+        ChunkSegment s = {};
+        s.tiles = t1 - t0; s.block = b; s.kvh = h; s.rows = p.rows;
         s.dest = t0 == 0 && t1 == p.tiles ? -1 : 2 * static_cast<int>(blockIdx.x) + (t0 > 0 ? 0 : 1);
-        s.wide = 0; s.tiles = max(0, min(t1, narrow) - t0); s.first = 1; s.last = t1 <= narrow;
-        push(s, p, c, t0);
-        s.wide = 1; s.first = t0 >= narrow; s.last = 1; s.tiles = max(0, t1 - max(t0, narrow));
-        push(s, p, c, max(t0, narrow) - narrow);
+        push(s, p, tile0, t0);
       }
     }
   }
@@ -195,65 +195,57 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   for (int k = max(0, pos_copies - kPosSlots); k < pos_copies; ++k) mbar_wait(x.pos_full(k % kPosSlots), (k / kPosSlots) & 1);
 }
 
-// The warp that issues the products (one elected lane does; the whole warp goes along).  The halves take
-// turns, O += P V of a tile and S of the next: then one half's softmax runs under the other's products.
-// (Left to warps of their own the two fell into step: both waited for the tensor core, then both for the
-// exponentials.)  A wait stands before scores that go over weights: nothing orders the two products.
+// The warp that issues the products (one elected lane does; the whole warp goes along): for each step the
+// halves' next scores, once these have been read, then O += P V as their weights come.
 template <int D>
 __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x) {
   using L = ChunkSmem<D>;
-  int segs = 0, tile = 0, it[2] = {0, 0}, loads[2] = {0, 0};  // tile: of the CTA, it: of a half, loads: of its Q
+  constexpr int T = L::kT;
+  int segs = 0, done = 0, it[2] = {0, 0}, loads[2] = {0, 0};  // done: tiles of the CTA, it: of a half, loads: of its Q
   const uint32_t base = smem_u32(x.base);
+  const uint32_t id_s = tc_idesc(false, T, false), id_o = tc_idesc(false, D, true);
   for (bool ok = true; ok;) {
     if (!x.wait_warp(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) break;
     const ChunkSegment& sg = x.seg(segs % kSpanSlots);
-    const int n = __shfl_sync(0xffffffffu, sg.tiles, 0), wide = __shfl_sync(0xffffffffu, sg.wide, 0);
-    const bool first = __shfl_sync(0xffffffffu, sg.first, 0);
-    const int halves = __shfl_sync(0xffffffffu, sg.rows, 0) > kPipeRows ? 2 : 1;
+    const int n = __shfl_sync(0xffffffffu, sg.tiles, 0);
+    const bool turns = __shfl_sync(0xffffffffu, sg.rows, 0) <= kHalfRows;  // the halves take the tiles in turn
     __syncwarp();
     if (elected()) mbar_arrive(x.seg_empty(segs % kSpanSlots));
     ++segs;
     if (n == 0) break;
-    const uint32_t id_s = tc_idesc(wide, kChunkTile, false), id_o = tc_idesc(wide, D, true);
-    auto scores = [&](int half, int t) {  // S of tile t (of the CTA), whose K is there
-      const int slot = t % L::kSlots;
+    auto tile_of = [&](int half, int step) { return turns ? 2 * step + half : step; };
+    auto scores = [&](int half, int step) -> bool {  // S of the half's tile, where it has one
+      const int t = done + tile_of(half, step), slot = t % L::kSlots;
+      if (tile_of(half, step) >= n) return true;
+      if (!(step == 0 ? x.wait_warp(x.q_full(half), loads[half]++ & 1) : x.wait_warp(x.s_read(half), (it[half] & 1)))) return false;
+      if (!x.wait_warp(x.k_full(slot), (t / L::kSlots) & 1)) return false;
       tc_fence_after();
-      const uint64_t a = tc_desc(base + half * L::kTile, 16), b = tc_desc(base + L::kK + slot * L::kTile, 16);
+      const uint64_t a = tc_desc(base + half * L::kQ, 16), b = tc_desc(base + L::kK + slot * L::kTile, 16);
       if (elected()) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint64_t o = ((k >> 2) * (kChunkTile * 128) + (k & 3) * 32) >> 4;
-          tc_mma_ss(x.col_s(half), a + o, b + o, id_s, k > 0);
-        }
+        for (int k = 0; k < D / 16; ++k)
+          tc_mma_ss(x.col_s(half), a + (((k >> 2) * (kHalfRows * 128) + (k & 3) * 32) >> 4), b + (((k >> 2) * (T * 128) + (k & 3) * 32) >> 4), id_s, k > 0);
         tc_commit(x.s_full(half));
-        if (half == halves - 1) tc_commit(x.k_empty(slot));
+        if (turns || half == 1) tc_commit(x.k_empty(slot));
       }
       __syncwarp();
+      return true;
     };
-    auto keys = [&](int t) { return x.wait_warp(x.k_full(t % L::kSlots), (t / L::kSlots) & 1); };
-    auto values = [&](int half, int i) -> bool {  // O += P V of the segment's tile i
-      const int slot = tile % L::kSlots;
-      const uint64_t d = tc_desc(base + L::kV + slot * L::kTile, kChunkTile * 128);
-#pragma unroll 1
-      for (int part = 0; part < 2; ++part) {  // 64 tokens at a time, as their weights come
+    auto values = [&](int half, int step) -> bool {  // O += P V of the half's tile
+      const int t = done + tile_of(half, step), slot = t % L::kSlots;
+      if (tile_of(half, step) >= n) return true;
+      if (!x.wait_warp(x.v_full(slot), (t / L::kSlots) & 1)) return false;
+      const uint64_t d = tc_desc(base + L::kV + slot * L::kTile, T * 128);
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {  // some tokens, as their weights come
         if (!x.wait_warp(x.p_full(half, part), it[half] & 1)) return false;
         tc_fence_after();
         if (elected()) {
 #pragma unroll
-          for (int j = 0; j < kChunkTile / 32; ++j) {
-            const int k = part * (kChunkTile / 32) + j;
-            tc_mma(x.col_o(half), x.col_p(half, part, wide) + 8 * j, d + k * (2048 >> 4), id_o, k > 0 || i > 0 || !first);
-          }
-          if (wide) {  // the weights' low parts
-#pragma unroll
-            for (int j = 0; j < kChunkTile / 32; ++j) {
-              const int k = part * (kChunkTile / 32) + j;
-              tc_mma(x.col_o(half), x.col_low(half, part) + 8 * j, d + k * (2048 >> 4), id_o, true);
-            }
-            if (D == 64 && part == 0) tc_commit(x.o_half(half));
-          }
+          for (int k = part ? ChunkCtx<D>::kPartA / 16 : 0; k < (part ? T : ChunkCtx<D>::kPartA) / 16; ++k)
+            tc_mma(x.col_o(half), x.col_p(half) + 8 * k, d + k * (2048 >> 4), id_o, k > 0 || step > 0);
           if (part == 1) {
-            if (half == halves - 1) tc_commit(x.v_empty(slot));
+            if (turns || half == 1) tc_commit(x.v_empty(slot));
             tc_commit(x.o_done(half));
           }
         }
@@ -262,43 +254,24 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x) {
       ++it[half];
       return true;
     };
-    ok = keys(tile);
-    for (int h = 0; h < halves && ok; ++h) {
-      if (it[h] > 0) ok = x.wait_warp(x.o_done(h), (it[h] - 1) & 1);
-      ok = ok && x.wait_warp(x.q_full(h), loads[h]++ & 1);
-      if (ok) scores(h, tile);
-    }
-    for (int i = 0; i < n && ok; ++i, ++tile) {
-      const bool more = i + 1 < n;
-      if (D == 64 && more) {  // weights have columns of their own: the next scores as soon as these are read
-        ok = keys(tile + 1);
-        for (int h = 0; h < halves && ok; ++h) {
-          ok = x.wait_warp(x.s_read(h), it[h] & 1);
-          if (ok) scores(h, tile + 1);
-        }
-      }
-      ok = ok && x.wait_warp(x.v_full(tile % L::kSlots), (tile / L::kSlots) & 1);
-      for (int h = 0; h < halves && ok; ++h) {
-        ok = values(h, i);
-        if (D == 128 && more && ok) {
-          ok = (h > 0 || keys(tile + 1)) && x.wait_warp(x.o_done(h), (it[h] - 1) & 1);
-          if (ok) scores(h, tile + 1);
-        }
-      }
-    }
+    const int steps = turns ? (n + 1) / 2 : n;
+    ok = scores(0, 0) && scores(1, 0);
+    for (int i = 0; i < steps && ok; ++i) ok = scores(0, i + 1) && scores(1, i + 1) && values(0, i) && values(1, i);
+    done += n;
   }
   if (elected()) tc_commit(x.drained());  // nothing is in flight when the CTA ends
   __syncwarp();
   mbar_wait(x.drained(), 0);
 }
 
-// How many of 128 ascending positions are below v.
+// How many of T ascending positions are below v.
+template <int T>
 __device__ __forceinline__ int below(const int32_t* pos, int v) {
   int n = 0;
 #pragma unroll
-  for (int step = 64; step > 0; step >>= 1)
-    if (pos[n + step - 1] < v) n += step;
-  return n + (pos[n] < v ? 1 : 0);
+  for (int step = 128; step > 0; step >>= 1)
+    if (n + step <= T && pos[n + step - 1] < v) n += step;
+  return n;
 }
 
 // The 32 of bits 0 .. n-1 that lie in word w.
@@ -307,17 +280,38 @@ __device__ __forceinline__ uint32_t bits_below(int n, int w) {
   return k <= 0 ? 0u : k >= 32 ? 0xffffffffu : (1u << k) - 1;
 }
 
+// Scores out of sight become -infinity; s holds tokens FROM .. FROM + N - 1, bit j of the words is token j's.
+template <int FROM, int N, int W>
+__device__ __forceinline__ void hide(uint32_t (&s)[N], const uint32_t (&seen)[W]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (!(seen[(FROM + j) / 32] >> ((FROM + j) % 32) & 1)) s[j] = 0xFF800000u;
+}
+
+// Weights into TMEM as binary16, two to a column.
+template <int N>
+__device__ __forceinline__ void put_weights(uint32_t col, const uint32_t (&s)[N]) {
+#pragma unroll
+  for (int c = 0; c < N / 2; c += 8) {
+    uint32_t p[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p[k] = pack16(false, __uint_as_float(s[2 * (c + k)]), __uint_as_float(s[2 * (c + k) + 1]));
+    tmem_st(col + c, p);
+  }
+}
+
 // The softmax warps of a half, a thread a row.
 template <int D>
 __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx<D>& x, int half, int quad, int lane) {
   using L = ChunkSmem<D>;
+  using C = ChunkCtx<D>;
+  constexpr int T = L::kT;
   const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
-  const uint32_t col_s = x.col_s(half) + lanes, col_o = x.col_o(half) + lanes;
-  int segs = 0, tile = 0, it = 0, wides = 0;
-  float m = -INFINITY, l = 0.f, f = 0.f;
-  RowSource src = {};
-  bool mine = false;
+  const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
+  float* const exchange = reinterpret_cast<float*>(x.base + L::kQ);  // the second half's Q: 32 columns of 128 rows
+  float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
+  int segs = 0, done = 0, it = 0, joins = 0;
   for (;;) {
     if (!x.wait_warp(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) return;
     const ChunkSegment sg = x.seg(segs % kSpanSlots);
@@ -325,92 +319,86 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     if (lane == 0) mbar_arrive(x.seg_empty(segs % kSpanSlots));
     ++segs;
     if (sg.tiles == 0) return;
-    if (sg.rows <= half * kPipeRows) {
-      for (int i = 0; i < sg.tiles; ++i, ++tile) {
-        if (!x.wait_warp(x.pos_full(tile % kPosSlots), (tile / kPosSlots) & 1)) return;
-        if (lane == 0) mbar_arrive(x.pos_empty(tile % kPosSlots));
-      }
-      continue;
-    }
-    // The row's query into shared memory, in the tiles' type, scaled by the power of two that brings its
-    // largest element to [1, 2): binary16 then holds what it needs of it.  (The last segment's scores are all in.)
-    {
-      const BlockPlan& p = g.block[sg.block];
-      mine = half * kPipeRows + row < sg.rows;
+    const bool turns = sg.rows <= kHalfRows;  // the halves have the same rows and take the tiles in turn
+    const int first_row = turns ? 0 : half * kHalfRows;
+    const BlockPlan& p = g.block[sg.block];
+    const bool local = p.local, mine = first_row + row < sg.rows;
+    RowSource src = {};
+    src.t = INT_MAX - 1;  // (a lane without a row sees every token, so that its warp need not hide any for it)
+    float f = 0.f;
+    // The row's query into shared memory as binary16, scaled by the power of two that brings its largest
+    // element to [1, 2).  (The last segment's scores are all in.)
+    if (!turns || half < sg.tiles) {
       uint4 w[D / 8];
       uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) w[i] = make_uint4(0, 0, 0, 0);
       if (mine) {
-        src = row_source(g, g.chunk[p.chunk], p.query0, p.local, sg.kvh, p.row + half * kPipeRows + row);
+        src = row_source(g, g.chunk[p.chunk], p.query0, local, sg.kvh, p.row + first_row + row);
         const uint4* q = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(src.query) * g.a.Hq + src.head) * D);
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) w[i] = q[i];
+      }
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+      for (int i = 0; i < D / 8; ++i) {
+        const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) top = max(top, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
-        }
-      } else {  // sees every token, so that its warp need not mask for it
-        src.t = INT_MAX - 1;
-        src.lo = 0;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) w[i] = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 4; ++k) top = max(top, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
       }
       int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
       e = max(-100, min(120, e));
       const float down = __int_as_float((127 - e) << 23);
       f = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
-      uint8_t* to = x.base + half * L::kTile;
+      uint8_t* to = x.base + half * L::kQ;
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) {
         const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
         uint32_t o[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = pack16(sg.wide, bf16lo(v[k]) * down, bf16hi(v[k]) * down);
-        *reinterpret_cast<uint4*>(to + tile_at(row, i)) = make_uint4(o[0], o[1], o[2], o[3]);
+        for (int k = 0; k < 4; ++k) o[k] = pack16(false, bf16lo(v[k]) * down, bf16hi(v[k]) * down);
+        *reinterpret_cast<uint4*>(to + tile_at(kHalfRows, row, i)) = make_uint4(o[0], o[1], o[2], o[3]);
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(x.q_full(half));
     }
-    const bool local = g.block[sg.block].local;
-    if (sg.first) m = -INFINITY, l = 0.f;
-    for (int i = 0; i < sg.tiles; ++i, ++it, ++tile) {
-      const int slot = tile % kPosSlots;
-      if (!x.wait_warp(x.pos_full(slot), (tile / kPosSlots) & 1)) return;
-      const int32_t* pos = x.pos(slot);
-      const bool all = __all_sync(0xffffffffu, pos[kChunkTile - 1] <= src.t && pos[0] >= src.lo);
-      if (!x.wait_warp(x.s_full(half), it & 1)) return;
-      tc_fence_after();
-      uint32_t s[2][64];
-      tmem_ld(s, col_s);
-      if (D == 64) {  // the next scores may come
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(x.s_read(half));
+    float m = -INFINITY, l = 0.f;
+    int mine_done = 0;  // tiles of this half
+    for (int i = 0; i < sg.tiles; ++i) {
+      const int slot = (done + i) % kPosSlots;
+      if (!x.wait_warp(x.pos_full(slot), ((done + i) / kPosSlots) & 1)) return;
+      if (turns && (i & 1) != half) {
+        if (lane == 0) mbar_arrive(x.pos_empty(slot));
+        continue;
       }
+      const int32_t* pos = x.pos(slot);
+      const bool all = __all_sync(0xffffffffu, pos[T - 1] <= src.t && pos[0] >= src.lo);
+      uint32_t seen[(T + 31) / 32];
       if (!all) {
-        const int c = below(pos, src.t + 1), from = pos[0] >= src.lo ? 0 : below(pos, src.lo), head = local && from > 0 ? below(pos, g.sinks) : 0;
+        const int c = below<T>(pos, src.t + 1), from = pos[0] >= src.lo ? 0 : below<T>(pos, src.lo), head = local && from > 0 ? below<T>(pos, g.sinks) : 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int word = 2 * h + k;
-            const uint32_t seen = bits_below(c, word) & (~bits_below(from, word) | bits_below(head, word));
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!(seen >> j & 1)) s[h][32 * k + j] = 0xFF800000u;
-          }
+        for (int w = 0; w < (T + 31) / 32; ++w) seen[w] = bits_below(c, w) & (~bits_below(from, w) | bits_below(head, w));
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(x.pos_empty(slot));
-      const float top = fmaxf(highest(s[0]), highest(s[1])) * f;
+      if (!x.wait_warp(x.s_full(half), it & 1)) return;
+      tc_fence_after();
+      uint32_t a[C::kPartA], b[C::kPartB];
+      tmem_ld(a, b, col_s);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(x.s_read(half));  // the next scores may come
+      if (!all) {
+        hide<0>(a, seen);
+        hide<C::kPartA>(b, seen);
+      }
+      const float top = fmaxf(highest(a), highest(b)) * f;
       // m follows the maximum only when that has grown by more than 2^8: p stays within binary16, and O is rarely rescaled
       if (__any_sync(0xffffffffu, top > m + 8.f)) {
         const float next = fmaxf(m, top), by = m == -INFINITY ? 0.f : exp2_approx(m - next);
         l *= by;
         m = next;
-        if (i > 0 || !sg.first) {
+        if (mine_done > 0) {
           if (!x.wait_warp(x.o_done(half), (it - 1) & 1)) return;
           tc_fence_after();
 #pragma unroll 1
@@ -424,64 +412,82 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         }
       }
       const float shift = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        l += weigh(s[h], f, shift);
-        if (D == 64 && h == 0 && it > 0 && !x.wait_warp(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
-        uint32_t p[32];
-        if (sg.wide) {  // high parts cut off, low parts what is left, rounded
-          uint32_t low[32];
-#pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const uint32_t a = s[h][2 * k], b = s[h][2 * k + 1];
-            p[k] = __byte_perm(a, b, 0x7632);
-            low[k] = pack16(true, __uint_as_float(a) - __uint_as_float(a & 0xFFFF0000u), __uint_as_float(b) - __uint_as_float(b & 0xFFFF0000u));
-          }
-          if (D == 64 && h == 1 && !x.wait_warp(x.o_half(half), wides++ & 1)) return;
-          tmem_st(x.col_low(half, h) + lanes, low);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 32; ++k) p[k] = pack16(false, __uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1]));
-        }
-        tmem_st(x.col_p(half, h, sg.wide) + lanes, p);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(x.p_full(half, h));  // the product of these tokens can start
-      }
+      l += weigh(a, f, shift);
+      if (it > 0 && !x.wait_warp(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
+      put_weights(col_p, a);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(x.p_full(half, 0));  // the product of these tokens can start
+      l += weigh(b, f, shift);
+      put_weights(col_p + C::kPartA / 2, b);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(x.p_full(half, 1));
+      ++it;
+      ++mine_done;
     }
-    if (!sg.last) continue;
-    // rows out: the output itself, or (m, l, o) for the join
-    if (!x.wait_warp(x.o_done(half), (it - 1) & 1)) return;
-    tc_fence_after();
-    const int64_t at = static_cast<int64_t>(src.query) * g.a.Hq + src.head;
-    if (sg.dest >= 0) {
-      const int64_t slot = static_cast<int64_t>(sg.dest) * kBlockRows + half * kPipeRows + row;
-      if (mine) g.part_ml[slot] = make_float2(m, l);
+    done += sg.tiles;
+    // rows out: the output itself, or (m, l, o) for the join of pieces
+    if (mine_done > 0) {
+      if (!x.wait_warp(x.o_done(half), (it - 1) & 1)) return;
+      tc_fence_after();
+    }
+    if (turns && half == 1) {  // to the first half, 32 columns at a time
+      exchange_ml[row] = make_float2(m, l);
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
+      for (int c = 0; c < D / 32; ++c, ++joins) {
         uint32_t o[32];
-        tmem_ld(o, col_o + 32 * c);
-        if (mine) {
+        if (mine_done > 0) tmem_ld(o, col_o + 32 * c);
+        if (joins > 0 && !x.wait_warp(x.join_empty(), (joins - 1) & 1)) return;
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) st_global8(g.part_o + slot * D + 32 * c + k, reinterpret_cast<const float*>(o + k));
-        }
+        for (int k = 0; k < 32; ++k) exchange[k * kHalfRows + row] = mine_done > 0 ? __uint_as_float(o[k]) : 0.f;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x.join_full());
       }
-    } else {
-      const float inv = l != 0.f ? 1.f / l : 0.f;
-      if (mine && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      if (!x.wait_warp(x.join_empty(), (joins - 1) & 1)) return;  // Q's place is free again
+      tc_fence_before();
+      continue;
+    }
+    const int64_t at = static_cast<int64_t>(src.query) * g.a.Hq + src.head, slot = static_cast<int64_t>(sg.dest) * kBlockRows + first_row + row;
+    float by = 1.f, other = 0.f, inv = 0.f;  // weights of the halves' sums
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tmem_ld(o, col_o + 32 * c);
-        if (mine) {
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld(o, col_o + 32 * c);
+      if (turns) {
+        if (!x.wait_warp(x.join_full(), joins & 1)) return;
+        if (c == 0) {
+          const float2 ml = exchange_ml[row];
+          const float high = fmaxf(m, ml.x);
+          by = m == -INFINITY ? 0.f : exp2_approx(m - high);
+          other = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - high);
+          m = high;
+          l = l * by + ml.y * other;
+        }
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
-            uint32_t v[4];
+        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by + exchange[k * kHalfRows + row] * other);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x.join_empty());
+        ++joins;
+      }
+      if (c == 0) {
+        inv = l != 0.f ? 1.f / l : 0.f;
+        if (mine && sg.dest >= 0) g.part_ml[slot] = make_float2(m, l);
+        if (mine && sg.dest < 0 && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      }
+      if (!mine) continue;
+      if (sg.dest >= 0) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = pack16(true, __uint_as_float(o[k + 2 * u]) * inv, __uint_as_float(o[k + 2 * u + 1]) * inv);
-            *reinterpret_cast<uint4*>(g.out + at * D + 32 * c + k) = make_uint4(v[0], v[1], v[2], v[3]);
-          }
+        for (int k = 0; k < 32; k += 8) st_global8(g.part_o + slot * D + 32 * c + k, reinterpret_cast<const float*>(o + k));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+          uint32_t v[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u] = pack16(true, __uint_as_float(o[k + 2 * u]) * inv, __uint_as_float(o[k + 2 * u + 1]) * inv);
+          *reinterpret_cast<uint4*>(g.out + at * D + 32 * c + k) = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
     }
@@ -507,9 +513,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
     for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 1);
     for (int h = 0; h < 2; ++h) {
       mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
-      mbar_init(x.p_full(h, 0), 4), mbar_init(x.p_full(h, 1), 4), mbar_init(x.o_done(h), 1), mbar_init(x.o_half(h), 1);
+      mbar_init(x.p_full(h, 0), 4), mbar_init(x.p_full(h, 1), 4), mbar_init(x.o_done(h), 1);
     }
-    mbar_init(x.drained(), 1);
+    mbar_init(x.drained(), 1), mbar_init(x.join_full(), 4), mbar_init(x.join_empty(), 4);
     fence_barrier_init();
   }
   pdl_wait();

@@ -17,6 +17,7 @@
 namespace trr {
 
 constexpr int kMostRows = 1 << 30;
+constexpr int kReadCtas = 3;  // CTAs on an SM
 
 struct ReadArgs {
   LayerArgs a;
@@ -25,86 +26,107 @@ struct ReadArgs {
   void *k, *v;
   uint8_t* bits;
   int64_t k_stride, v_stride;  // elements from a row to the next
+  int sectors;                 // every row starts at 32 bytes
 };
 
-// z + c s of eight elements, in binary32.
+// z + c s of eight elements of b bits, in binary32.
 template <int B>
-__device__ __forceinline__ void expand_f32(const Codes& x, float (&v)[8]) {
-  if (B == 16) {
-    const uint32_t w[4] = {x.w.x, x.w.y, x.w.z, x.w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = bf16lo(w[i]), v[2 * i + 1] = bf16hi(w[i]);
-    return;
-  }
-  const float s = __low2float(as_half2(x.sz)), z = __high2float(as_half2(x.sz));
+__device__ __forceinline__ void expand_f32(uint32_t w0, uint32_t w1, uint32_t sz, float (&v)[8]) {
+  const float s = __low2float(as_half2(sz)), z = __high2float(as_half2(sz));
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const uint32_t w = B == 8 && i >= 4 ? x.w.y : x.w.x;
+    const uint32_t w = B == 8 && i >= 4 ? w1 : w0;
     const uint32_t c = B == 8 ? __byte_perm(w, 0x4B000000u, 0x7540 + (i & 3)) : ((w >> (B * i)) & ((1u << B) - 1)) | 0x4B000000u;
     v[i] = __fmaf_rn(__uint_as_float(c) - 8388608.f, s, z);  // 2^23 + c as binary32: the difference is exact
   }
 }
 
-__device__ __forceinline__ void store8(float* to, const float (&v)[8]) {
-  reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void store8(uint16_t* to, const float (&v)[8]) {
-  uint32_t w[4];
+// Eight elements of half `k` of a lane's sixteen.
+__device__ __forceinline__ void expand(const Codes16& x, int cls, int k, float (&v)[8]) {
+  const uint4 w = x.w[0];
+  if (cls == 3) {
+    const uint4 y = x.w[k];
+    const uint32_t u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&x);
+    for (int i = 0; i < 4; ++i) v[2 * i] = bf16lo(u[i]), v[2 * i + 1] = bf16hi(u[i]);
+  } else if (cls == 2) {
+    expand_f32<8>(k ? w.z : w.x, k ? w.w : w.y, x.sz, v);
+  } else if (cls == 1) {
+    expand_f32<4>(k ? w.y : w.x, 0, x.sz, v);
+  } else if (cls == 0) {
+    expand_f32<2>(k ? w.x >> 16 : w.x, 0, x.sz, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
   }
-  *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Rows of one class (B 0: rows of zeros), heads h0 .. h1 - 1; a warp takes a head's K or V.
-template <int B, int D, typename T>
+__device__ __forceinline__ uint4 as_bf16(const float (&v)[8]) {
+  return make_uint4(pack16(true, v[0], v[1]), pack16(true, v[2], v[3]), pack16(true, v[4], v[5]), pack16(true, v[6], v[7]));
+}
+__device__ __forceinline__ uint4 bits_of(const float* v) {
+  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+
+// The tokens that the CTA has found, of heads h0 .. h1 - 1: a warp takes eight (d 64) or four rows of a head's K or V
+// of one class at a time, 16 elements a lane.  Sector: rows start at 32 bytes.
+template <int D, typename T>
 __device__ __forceinline__ void copy_rows(const ReadArgs& g, const Found& f, int h0, int h1) {
-  constexpr int c = B == 0 ? kClasses : B == 2 ? 0 : B == 4 ? 1 : B == 8 ? 2 : 3, kLanes = D / 8, kStep = 32 / kLanes, kAhead = 4;
-  const int n = f.count[c], lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
-  if (n == 0) return;
-  for (int j = 2 * h0 + warp; j < 2 * h1; j += kSpanThreads / 32) {
-    const int h = j >> 1, which = j & 1;
-    T* out = static_cast<T*>(which ? g.v : g.k) + h * D + 8 * e;
-    const int64_t stride = which ? g.v_stride : g.k_stride;
-    for (int t0 = lane / kLanes; t0 < n; t0 += kAhead * kStep) {
-      Codes x[kAhead];
-      bool there[kAhead];
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kAhead = 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
+  const int groups = f.groups(kRows), items = 2 * (h1 - h0) * groups;
+  for (int x0 = warp; x0 < items; x0 += kAhead * (kSpanThreads / 32)) {
+    Codes16 x[kAhead];
+    int cls[kAhead], row[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int t = t0 + u * kStep;
-        there[u] = t < n;
-        if (B != 0 && there[u]) {
-          const Found::Token& tok = f.token[c][t];
-          if (g.a.maskb) {  // per-head modes: the token may not store this head
-            const uint8_t* slice = tok.page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[c];
-            there[u] = *reinterpret_cast<const uint64_t*>(slice + g.a.slice[c] - g.a.maskb) >> tok.slot & 1;
-          }
-          if (there[u]) x[u] = load_codes<B == 0 ? 2 : B, D>(g.a, tok.page, tok.slot, h, which, e, lg_group);
-        }
+    for (int u = 0; u < kAhead; ++u) {
+      const int item = x0 + u * (kSpanThreads / 32), j = item / groups, h = h0 + (j >> 1);
+      cls[u] = kClasses;
+      row[u] = -1;
+      if (item >= items) continue;
+      int first, n;
+      cls[u] = f.group(item - j * groups, kRows, &first, &n);
+      const int t = first + lane / kLanes;
+      if (t >= n) continue;
+      const Found::Token& tok = f.token[cls[u]][t];
+      row[u] = tok.row;
+      if (g.a.maskb && cls[u] < kClasses) {  // per-head modes: the token may not store this head
+        const uint8_t* slice = tok.page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[cls[u]];
+        if (!(*reinterpret_cast<const uint64_t*>(slice + g.a.slice[cls[u]] - g.a.maskb) >> tok.slot & 1)) cls[u] = kClasses;
       }
+      if (cls[u] < kClasses) x[u] = load_codes16<D>(g.a, cls[u], tok.page, tok.slot, h, j & 1, e, lg_group);
+    }
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int t = t0 + u * kStep;
-        if (t >= n) continue;
-        const int row = f.token[c][t].row;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (B != 0 && there[u]) expand_f32<B == 0 ? 2 : B>(x[u], v);
-        store8(out + row * stride, v);
-        if (g.bits && which == 0 && e == 0) g.bits[static_cast<int64_t>(row) * g.a.Hkv + h] = B != 0 && there[u] ? B : 0;
+    for (int u = 0; u < kAhead; ++u) {
+      if (row[u] < 0) continue;
+      const int j = (x0 + u * (kSpanThreads / 32)) / groups, h = h0 + (j >> 1);
+      T* to = static_cast<T*>(j & 1 ? g.v : g.k) + row[u] * (j & 1 ? g.v_stride : g.k_stride) + h * D + 16 * e;
+      float v[8];
+      uint4 o[4];
+      expand(x[u], cls[u], 0, v);
+      if (sizeof(T) == 2) o[0] = as_bf16(v);
+      else o[0] = bits_of(v), o[1] = bits_of(v + 4);
+      expand(x[u], cls[u], 1, v);
+      if (sizeof(T) == 2) o[1] = as_bf16(v);
+      else o[2] = bits_of(v), o[3] = bits_of(v + 4);
+      if (g.sectors) {
+        store_sector(to, o[0], o[1]);
+        if (sizeof(T) == 4) store_sector(to + 8, o[2], o[3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < static_cast<int>(sizeof(T)); ++k) reinterpret_cast<uint4*>(to)[k] = o[k];
       }
+      if (g.bits && (j & 1) == 0 && e == 0) g.bits[static_cast<int64_t>(row[u]) * g.a.Hkv + h] = cls[u] < kClasses ? 2 << cls[u] : 0;
     }
   }
 }
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kSpanThreads) read_kernel(const __grid_constant__ ReadArgs g) {
+__global__ void __launch_bounds__(kSpanThreads, kReadCtas) read_kernel(const __grid_constant__ ReadArgs g) {
   __shared__ Found f;
   __shared__ int s_bad;
   const LayerArgs& a = g.a;
-  const int i = threadIdx.x >> 2, c = threadIdx.x & 3, lane = threadIdx.x & 31;
+  const int i = threadIdx.x >> 2, c = threadIdx.x & 3;
   if (threadIdx.x == 0) s_bad = 0;
   pdl_wait();
   pdl_trigger();
@@ -131,9 +153,6 @@ __global__ void __launch_bounds__(kSpanThreads) read_kernel(const __grid_constan
   const int row_end = bad ? g.rows : g.offsets[g.n], row_begin = bad ? 0 : g.offsets[0];
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
     const int row = u / g.splits * kSpan + i, h0 = u % g.splits * per, h1 = min(a.Hkv, h0 + per);
-    __syncthreads();  // the last unit's tokens have been read
-    if (threadIdx.x <= kClasses) f.count[threadIdx.x] = 0;
-    __syncthreads();
     const bool mine = row >= row_begin && row < row_end;
     Place p{0, -1, 0};
     if (mine && !bad) {
@@ -146,16 +165,8 @@ __global__ void __launch_bounds__(kSpanThreads) read_kernel(const __grid_constan
       const int seq = g.seq_ids[lo], start = g.starts[lo], len = g.offsets[lo + 1] - g.offsets[lo];
       if (seq >= 0 && seq < a.S && start >= 0 && start <= a.maxctx - len) p = place_of(a, seq, c, start + row - g.offsets[lo]);
     }
-    const bool here = p.page >= 0;
-    const bool any = __ballot_sync(0xffffffffu, here) >> (lane & ~3) & 15;
-    if (here) f.token[c][atomicAdd(&f.count[c], 1)] = Found::Token{a.pool[c] + p.page * a.page_bytes[c], p.slot, row};
-    if (mine && !any && c == 0) f.token[kClasses][atomicAdd(&f.count[kClasses], 1)] = Found::Token{nullptr, 0, row};
-    __syncthreads();
-    copy_rows<16, D, T>(g, f, h0, h1);
-    copy_rows<8, D, T>(g, f, h0, h1);
-    copy_rows<4, D, T>(g, f, h0, h1);
-    copy_rows<2, D, T>(g, f, h0, h1);
-    copy_rows<0, D, T>(g, f, h0, h1);
+    f.gather(a, p, c, mine ? row : -1, threadIdx.x);
+    copy_rows<D, T>(g, f, h0, h1);
   }
   __syncthreads();
   if (threadIdx.x == 0 && atom_add_acq_rel(a.ctrl + kReadDone, 1) == static_cast<int>(gridDim.x) - 1) {
@@ -187,12 +198,15 @@ extern "C" trr_status trr_kv_read(trr_cache* cache, int32_t layer, int32_t n, co
   g.seq_ids = seq_ids; g.starts = starts; g.offsets = offsets;
   g.k = k_out; g.v = v_out; g.bits = bits_out;
   g.k_stride = k_stride; g.v_stride = v_stride;
+  const int64_t size = type == TRR_BF16 ? 2 : 4;
+  g.sectors = ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out) | static_cast<uint64_t>(k_stride * size) |
+                static_cast<uint64_t>(v_stride * size)) & 31) == 0;
   const int sms = cache_num_sms(cache), spans = (num_rows - 1) / kSpan + 1;
   // a small call's heads are shared out among CTAs, so that it fills the GPU too
   const int most = (2 * l.Hkv + kSpanThreads / 32 - 1) / (kSpanThreads / 32);
-  g.splits = std::max(1, std::min(most, 8 * sms / spans));
+  g.splits = std::max(1, std::min(most, kReadCtas * sms / spans));
   const int64_t units = static_cast<int64_t>(spans) * g.splits;
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(units, 8 * sms)));
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(units, kReadCtas * sms)));
   auto kernel = l.d == 64 ? (type == TRR_BF16 ? read_kernel<64, uint16_t> : read_kernel<64, float>)
                           : (type == TRR_BF16 ? read_kernel<128, uint16_t> : read_kernel<128, float>);
   cache_note_call(cache, layer);

@@ -47,7 +47,7 @@ __device__ __forceinline__ Place place_of(const LayerArgs& a, int seq, int c, in
   return Place{k * a.P + l, l < n && pos[l] == p ? page : -1, l};
 }
 
-// Tokens that a CTA has found, class by class; class kClasses: positions that store nothing.
+// Tokens that a CTA has found, class by class, in order; class kClasses: positions that store nothing.
 struct Found {
   struct Token {
     const uint8_t* page;
@@ -55,40 +55,88 @@ struct Found {
   };
   Token token[kClasses + 1][kSpan];
   int count[kClasses + 1];
+  int warp_count[kSpanThreads / 32][kClasses + 1];
+
+  // Thread 4 i + c brings class c's place of position i and the row that its values go to (row < 0: the position is
+  // not asked for).  Every thread of the CTA calls it; what was found before has then been read by all.
+  __device__ __forceinline__ void gather(const LayerArgs& a, const Place& p, int c, int row, int tid) {
+    const int lane = tid & 31, warp = tid >> 5;
+    const uint32_t here = __ballot_sync(0xffffffffu, p.page >= 0), mine = 0x11111111u << c;
+    const uint32_t any = (here | here >> 1 | here >> 2 | here >> 3) & 0x11111111u;  // positions that store a token
+    const uint32_t none = __ballot_sync(0xffffffffu, row >= 0) & ~any & 0x11111111u;
+    __syncthreads();
+    if (lane < 4) warp_count[warp][lane] = __popc(here & 0x11111111u << lane);
+    if (lane == 4) warp_count[warp][kClasses] = __popc(none);
+    __syncthreads();
+    auto before = [&](int k) {
+      int n = 0;
+      for (int w = 0; w < warp; ++w) n += warp_count[w][k];
+      return n;
+    };
+    const uint32_t below = (1u << lane) - 1;
+    if (p.page >= 0) token[c][before(c) + __popc(here & mine & below)] = Token{a.pool[c] + p.page * a.page_bytes[c], p.slot, row};
+    if (none >> lane & 1) token[kClasses][before(kClasses) + __popc(none & below)] = Token{nullptr, 0, row};
+    if (tid <= kClasses) {
+      int n = 0;
+      for (int w = 0; w < kSpanThreads / 32; ++w) n += warp_count[w][tid];
+      count[tid] = n;
+    }
+    __syncthreads();
+  }
+  // Groups of `rows` tokens of one class: how many, and the class, first token and number of tokens of one.
+  __device__ __forceinline__ int groups(int rows) const {
+    int n = 0;
+    for (int c = 0; c <= kClasses; ++c) n += (count[c] + rows - 1) / rows;
+    return n;
+  }
+  __device__ __forceinline__ int group(int i, int rows, int* first, int* n) const {
+    int c = 0;
+    for (; c < kClasses; ++c) {
+      const int k = (count[c] + rows - 1) / rows;
+      if (i < k) break;
+      i -= k;
+    }
+    *first = i * rows;
+    *n = count[c];
+    return c;
+  }
 };
 
-// Eight consecutive elements of a row, as they are stored.
-struct Codes {
-  uint4 w;      // 2, 4 and 8 bits: the codes in w.x (and w.y); 16 bits: the values
+// Sixteen consecutive elements of a row, as they are stored.
+struct Codes16 {
+  uint4 w[2];   // 2, 4 and 8 bits: the codes in the first 4, 8 or 16 bytes; 16 bits: the values
   uint32_t sz;  // scale and zero (binary16) of their group
 };
 
-// Elements 8 e .. 8 e + 7 of K (which 0) or V (1) of KV head h.
-template <int B, int D>
-__device__ __forceinline__ Codes load_codes(const LayerArgs& a, const uint8_t* page, int slot, int h, int which, int e, int lg_group) {
-  constexpr int c = B == 2 ? 0 : B == 4 ? 1 : B == 8 ? 2 : 3, kRow = D * B / 8;
+// Elements 16 e .. 16 e + 15 of K (which 0) or V (1) of KV head h.
+template <int D>
+__device__ __forceinline__ Codes16 load_codes16(const LayerArgs& a, int c, const uint8_t* page, int slot, int h, int which, int e, int lg_group) {
   const uint8_t* slice = page + a.hdr + static_cast<int64_t>(h) * a.slice[c];
-  int o = (which * a.P + slot) * kRow + e * B;
-  if (B >= 8 && a.swz) o = static_cast<int>(swz_off(o));
-  Codes r;
-  r.w = make_uint4(0, 0, 0, 0);
-  r.sz = 0;
-  if (B == 16) {
-    r.w = *reinterpret_cast<const uint4*>(slice + o);
+  const int lg = c + 1, row = D << lg >> 3, o = (which * a.P + slot) * row + (e << (lg + 1));
+  Codes16 r = {};
+  if (c == 3) {
+    r.w[0] = *reinterpret_cast<const uint4*>(slice + (a.swz ? swz_off(o) : o));
+    r.w[1] = *reinterpret_cast<const uint4*>(slice + (a.swz ? swz_off(o + 16) : o + 16));
     return r;
   }
-  if (B == 8) {
+  if (c == 2) {
+    r.w[0] = *reinterpret_cast<const uint4*>(slice + (a.swz ? swz_off(o) : o));
+  } else if (c == 1) {
     const uint2 x = *reinterpret_cast<const uint2*>(slice + o);
-    r.w.x = x.x;
-    r.w.y = x.y;
-  } else if (B == 4) {
-    r.w.x = *reinterpret_cast<const uint32_t*>(slice + o);
+    r.w[0].x = x.x;
+    r.w[0].y = x.y;
   } else {
-    r.w.x = *reinterpret_cast<const uint16_t*>(slice + o);
+    r.w[0].x = *reinterpret_cast<const uint32_t*>(slice + o);
   }
-  const int ng = D >> lg_group;
-  r.sz = reinterpret_cast<const uint32_t*>(slice + 2 * a.P * kRow)[(which * a.P + slot) * ng + (8 * e >> lg_group)];
+  r.sz = reinterpret_cast<const uint32_t*>(slice + 2 * a.P * row)[(which * a.P + slot) * (D >> lg_group) + (16 * e >> lg_group)];
   return r;
+}
+
+// 32 bytes in one store (p aligned to them).
+__device__ __forceinline__ void store_sector(void* p, uint4 a, uint4 b) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z),
+               "r"(b.w)
+               : "memory");
 }
 
 }  // namespace trr

@@ -1,9 +1,8 @@
 // trr_chunk_tc.cuh - attention of blocks of 256 rows over staged tiles, on the tensor cores (tcgen05).
 //
 // One CTA per SM.  A producer warp brings tiles of tokens (K, V, positions) into rings of shared memory, as
-// they were staged, with bulk copies.  A block's rows are two halves of 128, one to a lane of TMEM; one thread
-// issues the products S = Q K^T and O += P V of both, and each half has a warpgroup that does its softmax, a
-// thread a row.  A block of 128 rows or fewer has its rows in both halves, which take its tiles in turn and are
+// they were staged, with bulk copies.  A block's rows are two halves of 128, one to a lane of TMEM; each half has
+// a warp that issues its products S = Q K^T and O += P V and a warpgroup that does its softmax, a thread a row.  A block of 128 rows or fewer has its rows in both halves, which take its tiles in turn and are
 // joined at the end.  K, V and p are binary16, sums and statistics binary32; query rows are scaled by powers of
 // two.
 //
@@ -19,7 +18,7 @@
 
 namespace trr {
 
-constexpr int kChunkSoftmaxWarps = 8, kChunkProducer = 8, kChunkMma = 9;
+constexpr int kChunkSoftmaxWarps = 8, kChunkProducer = 8, kChunkMma = 9;  // warps 9 and 10
 constexpr int kChunkThreads = 384;
 // Registers a thread: 168 at launch; the softmax warpgroups take what the third gives up.
 constexpr int kChunkLaunchRegisters = 168, kChunkSoftmaxRegisters = 208, kChunkOtherRegisters = 88;
@@ -46,7 +45,7 @@ struct ChunkSmem {
   static constexpr int kMl = kPos + kPosSlots * kT * 4;  // (m, l) of the second half's rows, for a join
   static constexpr int kSeg = kMl + kHalfRows * 8;
   static constexpr int kBars = kSeg + kSpanSlots * static_cast<int>(sizeof(ChunkSegment));
-  static constexpr int kNumBars = 4 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 6 + 3;
+  static constexpr int kNumBars = 2 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 6 + 2;
   static constexpr int kTotal = kBars + 8 * kNumBars;
   static_assert(kTotal + 1024 + 64 <= 227 * 1024, "");
   static_assert(kTile % 1024 == 0 && kQ >= 32 * kHalfRows * 4, "a join takes 32 columns at a time through Q's place");
@@ -56,50 +55,47 @@ template <int D>
 struct ChunkCtx {
   using L = ChunkSmem<D>;
   static constexpr int kT = L::kT;
-  // a thread's scores are handed on in two parts
-  static constexpr int kPartA = D == 64 ? 64 : 48, kPartB = kT - kPartA;
+  static constexpr int kPartA = D == 64 ? 64 : 48, kPartB = kT - kPartA;  // a thread's scores, as two arrays
   uint8_t* base;  // 1024-byte aligned
   uint32_t tmem;
   uint64_t wait_ns;
   volatile int* abort_flag;
   __device__ uint64_t* bar(int i) const { return reinterpret_cast<uint64_t*>(base + L::kBars) + i; }
-  __device__ uint64_t* k_full(int i) const { return bar(i); }
-  __device__ uint64_t* k_empty(int i) const { return bar(L::kSlots + i); }
-  __device__ uint64_t* v_full(int i) const { return bar(2 * L::kSlots + i); }
-  __device__ uint64_t* v_empty(int i) const { return bar(3 * L::kSlots + i); }
-  __device__ uint64_t* pos_full(int i) const { return bar(4 * L::kSlots + i); }
-  __device__ uint64_t* pos_empty(int i) const { return bar(4 * L::kSlots + kPosSlots + i); }
-  __device__ uint64_t* seg_full(int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + i); }
-  __device__ uint64_t* seg_empty(int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + kSpanSlots + i); }
-  __device__ uint64_t* half_bar(int half, int i) const { return bar(4 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 6 * half + i); }
+  __device__ uint64_t* kv_full(int i) const { return bar(i); }
+  __device__ uint64_t* kv_empty(int i) const { return bar(L::kSlots + i); }
+  __device__ uint64_t* pos_full(int i) const { return bar(2 * L::kSlots + i); }
+  __device__ uint64_t* pos_empty(int i) const { return bar(2 * L::kSlots + kPosSlots + i); }
+  __device__ uint64_t* seg_full(int i) const { return bar(2 * L::kSlots + 2 * kPosSlots + i); }
+  __device__ uint64_t* seg_empty(int i) const { return bar(2 * L::kSlots + 2 * kPosSlots + kSpanSlots + i); }
+  __device__ uint64_t* half_bar(int half, int i) const { return bar(2 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 6 * half + i); }
   __device__ uint64_t* q_full(int half) const { return half_bar(half, 0); }
   __device__ uint64_t* s_full(int half) const { return half_bar(half, 1); }
   __device__ uint64_t* s_read(int half) const { return half_bar(half, 2); }
-  __device__ uint64_t* p_full(int half, int part) const { return half_bar(half, 3 + part); }
-  __device__ uint64_t* o_done(int half) const { return half_bar(half, 5); }
-  __device__ uint64_t* drained() const { return half_bar(2, 0); }
-  __device__ uint64_t* join_full() const { return half_bar(2, 1); }
-  __device__ uint64_t* join_empty() const { return half_bar(2, 2); }
+  __device__ uint64_t* p_full(int half) const { return half_bar(half, 3); }
+  __device__ uint64_t* o_done(int half) const { return half_bar(half, 4); }
+  __device__ uint64_t* drained(int half) const { return half_bar(half, 5); }
+  __device__ uint64_t* join_full() const { return half_bar(2, 0); }
+  __device__ uint64_t* join_empty() const { return half_bar(2, 1); }
   __device__ ChunkSegment& seg(int i) const { return reinterpret_cast<ChunkSegment*>(base + L::kSeg)[i]; }
   __device__ const int32_t* pos(int i) const { return reinterpret_cast<const int32_t*>(base + L::kPos) + i * kT; }
   // TMEM columns: scores, weights (two to a column), sums
   __device__ uint32_t col_s(int half) const { return tmem + kT * half; }
   __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 256 + 64 * half : 160 + 48 * half); }
   __device__ uint32_t col_o(int half) const { return tmem + 512 - D * (2 - half); }
-  // A bounded wait; once one has given up, none waits any more.
-  __device__ bool wait(uint64_t* b, uint32_t parity) const {
-    if (mbar_poll(smem_u32(b), parity, wait_ns)) return true;
-    const uint64_t t0 = global_ns();
-    while (!mbar_poll(smem_u32(b), parity, wait_ns)) {
-      if (*abort_flag || global_ns() - t0 >= wait_ns) {
+  // A bounded wait by a whole warp; all of its lanes get the same answer.  Once one has given up, none waits any
+  // more.  (Short, since a warp among others' code pays for the fetch of every instruction.)
+  __device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity) const {
+    const uint32_t addr = smem_u32(b);
+    for (uint64_t t0 = 0; !__all_sync(0xffffffffu, mbar_poll(addr, parity, wait_ns));) {
+      const uint64_t now = global_ns();
+      if (t0 == 0) t0 = now;
+      if (__any_sync(0xffffffffu, *abort_flag || now - t0 >= wait_ns)) {
         *abort_flag = 1;
         return false;
       }
     }
     return true;
   }
-  // The same by a whole warp: all of its lanes get the same answer.
-  __device__ bool wait_warp(uint64_t* b, uint32_t parity) const { return __all_sync(0xffffffffu, wait(b, parity)); }
 };
 
 // Tiles of a segment that lie before cost x (counted from the segment's start).
@@ -116,11 +112,11 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   const int64_t per = g.head->per, work = g.head->work;
   const int blocks = g.head->blocks;
   const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
-  int tiles_done = 0, segs = 0, k_copies = 0, pos_copies = 0, v_copies = 0;
+  int tiles_done = 0, segs = 0, copies = 0, pos_copies = 0;
   bool ok = true;
   PieceInfo piece = {-1, 0, 0, 0};
   auto push = [&](const ChunkSegment& s, const BlockPlan& p, int tile0, int from) {
-    ok = x.wait_warp(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
+    ok = x.wait(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
     if (!ok) return;
     if (lane == 0) {
       x.seg(segs % kSpanSlots) = s;
@@ -129,28 +125,22 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
     ++segs;
     for (int i = from; i < from + s.tiles; ++i, ++tiles_done) {
       const int tile = tile0 + (i < p.head ? i : p.first + i - p.head);
-      const int slot = tiles_done % L::kSlots, at = tiles_done % kPosSlots, phase = ((tiles_done / L::kSlots) & 1) ^ 1;
-      ok = x.wait_warp(x.k_empty(slot), phase);
+      const int slot = tiles_done % L::kSlots, at = tiles_done % kPosSlots;
+      ok = x.wait(x.kv_empty(slot), ((tiles_done / L::kSlots) & 1) ^ 1);
       if (!ok) return;
       if (lane == 0) {
-        mbar_arrive_expect_tx(x.k_full(slot), L::kTile);
-        bulk_g2s(x.base + L::kK + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 0), L::kTile, x.k_full(slot));
+        mbar_arrive_expect_tx(x.kv_full(slot), 2 * L::kTile);
+        bulk_g2s(x.base + L::kK + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 0), L::kTile, x.kv_full(slot));
+        bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 1), L::kTile, x.kv_full(slot));
       }
-      ++k_copies;
-      ok = x.wait_warp(x.pos_empty(at), ((tiles_done / kPosSlots) & 1) ^ 1);
+      ++copies;
+      ok = x.wait(x.pos_empty(at), ((tiles_done / kPosSlots) & 1) ^ 1);
       if (!ok) return;
       if (lane == 0) {
         mbar_arrive_expect_tx(x.pos_full(at), 4 * L::kT);
         bulk_g2s(x.base + L::kPos + at * 4 * L::kT, g.pos + static_cast<int64_t>(tile) * L::kT, 4 * L::kT, x.pos_full(at));
       }
       ++pos_copies;
-      ok = x.wait_warp(x.v_empty(slot), phase);
-      if (!ok) return;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(x.v_full(slot), L::kTile);
-        bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 1), L::kTile, x.v_full(slot));
-      }
-      ++v_copies;
     }
   };
   if (b0 < b1) {
@@ -183,29 +173,30 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   }
   if (lane == 0) g.piece[blockIdx.x] = piece;
   if (ok) {  // no more
-    ok = x.wait_warp(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
+    ok = x.wait(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
     if (ok && lane == 0) {
       x.seg(segs % kSpanSlots).tiles = 0;
       mbar_arrive(x.seg_full(segs % kSpanSlots));
     }
   }
   // the CTA stays until its copies have landed
-  for (int k = max(0, k_copies - L::kSlots); k < k_copies; ++k) mbar_wait(x.k_full(k % L::kSlots), (k / L::kSlots) & 1);
-  for (int k = max(0, v_copies - L::kSlots); k < v_copies; ++k) mbar_wait(x.v_full(k % L::kSlots), (k / L::kSlots) & 1);
+  for (int k = max(0, copies - L::kSlots); k < copies; ++k) mbar_wait(x.kv_full(k % L::kSlots), (k / L::kSlots) & 1);
   for (int k = max(0, pos_copies - kPosSlots); k < pos_copies; ++k) mbar_wait(x.pos_full(k % kPosSlots), (k / kPosSlots) & 1);
 }
 
-// The warp that issues the products (one elected lane does; the whole warp goes along): for each step the
-// halves' next scores, once these have been read, then O += P V as their weights come.
+// The warp that issues a half's products (one elected lane does; the whole warp goes along): the next scores
+// once these have been read, then O += P V once the weights are there.  Each half has its own: a wait costs 200
+// cycles, even for what is there, among warps that move scores and weights.
 template <int D>
-__device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x) {
+__device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
   using L = ChunkSmem<D>;
   constexpr int T = L::kT;
-  int segs = 0, done = 0, it[2] = {0, 0}, loads[2] = {0, 0};  // done: tiles of the CTA, it: of a half, loads: of its Q
-  const uint32_t base = smem_u32(x.base);
+  int segs = 0, done = 0, it = 0, loads = 0;  // done: tiles of the CTA, it: of this half, loads: of Q
+  const uint32_t base = smem_u32(x.base), col_s = x.col_s(half), col_p = x.col_p(half), col_o = x.col_o(half);
   const uint32_t id_s = tc_idesc(false, T, false), id_o = tc_idesc(false, D, true);
+  const uint64_t q = tc_desc(base + half * L::kQ, 16);
   for (bool ok = true; ok;) {
-    if (!x.wait_warp(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) break;
+    if (!x.wait(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) break;
     const ChunkSegment& sg = x.seg(segs % kSpanSlots);
     const int n = __shfl_sync(0xffffffffu, sg.tiles, 0);
     const bool turns = __shfl_sync(0xffffffffu, sg.rows, 0) <= kHalfRows;  // the halves take the tiles in turn
@@ -213,55 +204,45 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x) {
     if (elected()) mbar_arrive(x.seg_empty(segs % kSpanSlots));
     ++segs;
     if (n == 0) break;
-    auto tile_of = [&](int half, int step) { return turns ? 2 * step + half : step; };
-    auto scores = [&](int half, int step) -> bool {  // S of the half's tile, where it has one
-      const int t = done + tile_of(half, step), slot = t % L::kSlots;
-      if (tile_of(half, step) >= n) return true;
-      if (!(step == 0 ? x.wait_warp(x.q_full(half), loads[half]++ & 1) : x.wait_warp(x.s_read(half), (it[half] & 1)))) return false;
-      if (!x.wait_warp(x.k_full(slot), (t / L::kSlots) & 1)) return false;
+    const int step = turns ? 2 : 1, first = turns ? half : 0;
+    auto scores = [&](int i) -> bool {  // S of the run's tile i
+      const int slot = (done + i) % L::kSlots;
+      if (!x.wait(x.kv_full(slot), ((done + i) / L::kSlots) & 1)) return false;
       tc_fence_after();
-      const uint64_t a = tc_desc(base + half * L::kQ, 16), b = tc_desc(base + L::kK + slot * L::kTile, 16);
       if (elected()) {
+        const uint64_t k = tc_desc(base + L::kK + slot * L::kTile, 16);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          tc_mma_ss(x.col_s(half), a + (((k >> 2) * (kHalfRows * 128) + (k & 3) * 32) >> 4), b + (((k >> 2) * (T * 128) + (k & 3) * 32) >> 4), id_s, k > 0);
+        for (int j = 0; j < D / 16; ++j) {
+          const int at = (j >> 2) * 8, in = 2 * (j & 3);
+          tc_mma_ss(col_s, q + (at * kHalfRows + in), k + (at * T + in), id_s, j > 0);
+        }
         tc_commit(x.s_full(half));
-        if (turns || half == 1) tc_commit(x.k_empty(slot));
       }
       __syncwarp();
       return true;
     };
-    auto values = [&](int half, int step) -> bool {  // O += P V of the half's tile
-      const int t = done + tile_of(half, step), slot = t % L::kSlots;
-      if (tile_of(half, step) >= n) return true;
-      if (!x.wait_warp(x.v_full(slot), (t / L::kSlots) & 1)) return false;
-      const uint64_t d = tc_desc(base + L::kV + slot * L::kTile, T * 128);
+    if (first < n) ok = x.wait(x.q_full(half), loads++ & 1) && scores(first);
+#pragma unroll 1
+    for (int i = first; i < n && ok; i += step, ++it) {
+      if (i + step < n) ok = x.wait(x.s_read(half), it & 1) && scores(i + step);
+      if (!ok || !(ok = x.wait(x.p_full(half), it & 1))) break;
+      tc_fence_after();
+      if (elected()) {
+        const int slot = (done + i) % L::kSlots;
+        const uint64_t v = tc_desc(base + L::kV + slot * L::kTile, T * 128);
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {  // some tokens, as their weights come
-        if (!x.wait_warp(x.p_full(half, part), it[half] & 1)) return false;
-        tc_fence_after();
-        if (elected()) {
-#pragma unroll
-          for (int k = part ? ChunkCtx<D>::kPartA / 16 : 0; k < (part ? T : ChunkCtx<D>::kPartA) / 16; ++k)
-            tc_mma(x.col_o(half), x.col_p(half) + 8 * k, d + k * (2048 >> 4), id_o, k > 0 || step > 0);
-          if (part == 1) {
-            if (turns || half == 1) tc_commit(x.v_empty(slot));
-            tc_commit(x.o_done(half));
-          }
-        }
-        __syncwarp();
+        for (int k = 0; k < T / 16; ++k) tc_mma(col_o, col_p + 8 * k, v + k * (2048 >> 4), id_o, k > 0 || i > first);
+        tc_commit(x.kv_empty(slot));
+        tc_commit(x.o_done(half));
+        if (turns) mbar_arrive(x.kv_empty(slot));  // (for the other half)
       }
-      ++it[half];
-      return true;
-    };
-    const int steps = turns ? (n + 1) / 2 : n;
-    ok = scores(0, 0) && scores(1, 0);
-    for (int i = 0; i < steps && ok; ++i) ok = scores(0, i + 1) && scores(1, i + 1) && values(0, i) && values(1, i);
+      __syncwarp();
+    }
     done += n;
   }
-  if (elected()) tc_commit(x.drained());  // nothing is in flight when the CTA ends
+  if (elected()) tc_commit(x.drained(half));  // nothing is in flight when the CTA ends
   __syncwarp();
-  mbar_wait(x.drained(), 0);
+  mbar_wait(x.drained(half), 0);
 }
 
 // How many of T ascending positions are below v.
@@ -313,7 +294,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
   int segs = 0, done = 0, it = 0, joins = 0;
   for (;;) {
-    if (!x.wait_warp(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) return;
+    if (!x.wait(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) return;
     const ChunkSegment sg = x.seg(segs % kSpanSlots);
     __syncwarp();
     if (lane == 0) mbar_arrive(x.seg_empty(segs % kSpanSlots));
@@ -366,7 +347,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     int mine_done = 0;  // tiles of this half
     for (int i = 0; i < sg.tiles; ++i) {
       const int slot = (done + i) % kPosSlots;
-      if (!x.wait_warp(x.pos_full(slot), ((done + i) / kPosSlots) & 1)) return;
+      if (!x.wait(x.pos_full(slot), ((done + i) / kPosSlots) & 1)) return;
       if (turns && (i & 1) != half) {
         if (lane == 0) mbar_arrive(x.pos_empty(slot));
         continue;
@@ -381,7 +362,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(x.pos_empty(slot));
-      if (!x.wait_warp(x.s_full(half), it & 1)) return;
+      if (!x.wait(x.s_full(half), it & 1)) return;
       tc_fence_after();
       uint32_t a[C::kPartA], b[C::kPartB];
       tmem_ld(a, b, col_s);
@@ -399,7 +380,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         l *= by;
         m = next;
         if (mine_done > 0) {
-          if (!x.wait_warp(x.o_done(half), (it - 1) & 1)) return;
+          if (!x.wait(x.o_done(half), (it - 1) & 1)) return;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < D / 16; ++c) {
@@ -413,25 +394,21 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       }
       const float shift = m == -INFINITY ? 0.f : -m;
       l += weigh(a, f, shift);
-      if (it > 0 && !x.wait_warp(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
-      put_weights(col_p, a);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(x.p_full(half, 0));  // the product of these tokens can start
       l += weigh(b, f, shift);
+      if (it > 0 && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
+      put_weights(col_p, a);
       put_weights(col_p + C::kPartA / 2, b);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(x.p_full(half, 1));
+      if (lane == 0) mbar_arrive(x.p_full(half));
       ++it;
       ++mine_done;
     }
     done += sg.tiles;
     // rows out: the output itself, or (m, l, o) for the join of pieces
     if (mine_done > 0) {
-      if (!x.wait_warp(x.o_done(half), (it - 1) & 1)) return;
+      if (!x.wait(x.o_done(half), (it - 1) & 1)) return;
       tc_fence_after();
     }
     if (turns && half == 1) {  // to the first half, 32 columns at a time
@@ -440,13 +417,13 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       for (int c = 0; c < D / 32; ++c, ++joins) {
         uint32_t o[32];
         if (mine_done > 0) tmem_ld(o, col_o + 32 * c);
-        if (joins > 0 && !x.wait_warp(x.join_empty(), (joins - 1) & 1)) return;
+        if (joins > 0 && !x.wait(x.join_empty(), (joins - 1) & 1)) return;
 #pragma unroll
         for (int k = 0; k < 32; ++k) exchange[k * kHalfRows + row] = mine_done > 0 ? __uint_as_float(o[k]) : 0.f;
         __syncwarp();
         if (lane == 0) mbar_arrive(x.join_full());
       }
-      if (!x.wait_warp(x.join_empty(), (joins - 1) & 1)) return;  // Q's place is free again
+      if (!x.wait(x.join_empty(), (joins - 1) & 1)) return;  // Q's place is free again
       tc_fence_before();
       continue;
     }
@@ -457,7 +434,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       uint32_t o[32];
       tmem_ld(o, col_o + 32 * c);
       if (turns) {
-        if (!x.wait_warp(x.join_full(), joins & 1)) return;
+        if (!x.wait(x.join_full(), joins & 1)) return;
         if (c == 0) {
           const float2 ml = exchange_ml[row];
           const float high = fmaxf(m, ml.x);
@@ -508,14 +485,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     s_abort = 0;
-    for (int i = 0; i < L::kSlots; ++i) mbar_init(x.k_full(i), 1), mbar_init(x.k_empty(i), 1), mbar_init(x.v_full(i), 1), mbar_init(x.v_empty(i), 1);
+    for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
     for (int i = 0; i < kPosSlots; ++i) mbar_init(x.pos_full(i), 1), mbar_init(x.pos_empty(i), kChunkSoftmaxWarps);
-    for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 1);
+    for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
     for (int h = 0; h < 2; ++h) {
       mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
-      mbar_init(x.p_full(h, 0), 4), mbar_init(x.p_full(h, 1), 4), mbar_init(x.o_done(h), 1);
+      mbar_init(x.p_full(h), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
     }
-    mbar_init(x.drained(), 1), mbar_init(x.join_full(), 4), mbar_init(x.join_empty(), 4);
+    mbar_init(x.join_full(), 4), mbar_init(x.join_empty(), 4);
     fence_barrier_init();
   }
   pdl_wait();
@@ -535,7 +512,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   } else {
     registers_down<kChunkOtherRegisters>();
     if (warp == kChunkProducer) chunk_produce<D>(g, x, lane);
-    else if (warp == kChunkMma) chunk_mma<D>(x);
+    else if (warp < kChunkMma + 2) chunk_mma<D>(x, warp - kChunkMma);
   }
   __syncwarp();
   tc_fence_before();

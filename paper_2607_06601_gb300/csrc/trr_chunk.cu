@@ -264,26 +264,30 @@ __device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) 
   p.row = (b - c.block0 - (local ? full_blocks : 0)) * kBlockRows;
   p.rows = min(kBlockRows, (local ? c.local : c.full) * heads - p.row);
   p.query0 = c.row0 + (local ? c.full : 0);
-  // its queries' last position, and the first that any of them sees past the sinks
+  // its queries' first and last positions, and the first that any of them, and all of them, see past the sinks
   const int k0 = p.row / heads, k1 = (p.row + p.rows - 1) / heads;
-  const int t = c.start + g.list[p.query0 + k1] - c.row0;
-  int from = 0;
+  const int t0 = c.start + g.list[p.query0 + k0] - c.row0, t1 = c.start + g.list[p.query0 + k1] - c.row0;
+  int from = 0, from_all = 0;
   if (local) {
     from = INT_MAX;
     for (int k = k0 + lane; k <= k1; k += 32) {
-      const int q = g.list[p.query0 + k];
-      from = min(from, max(0, c.start + q - c.row0 - (g.windows ? g.windows[q] : g.window_scalar) + 1));
+      const int q = g.list[p.query0 + k], lo_q = max(0, c.start + q - c.row0 - (g.windows ? g.windows[q] : g.window_scalar) + 1);
+      from = min(from, lo_q);
+      from_all = max(from_all, lo_q);
     }
     from = __reduce_min_sync(0xffffffffu, from);
+    from_all = __reduce_max_sync(0xffffffffu, from_all);
   }
   const int head = local ? min(g.sinks, from) : 0;
-  // ranks of three positions: lanes 0 .. 11, a class of a position each
-  const int which = lane >> 2, x = which == 0 ? head : which == 1 ? from : t + 1;
-  int r = lane < 12 ? place_of(a, c.seq, lane & 3, x).before : 0;
+  // ranks of five positions: lanes 0 .. 19, a class of a position each
+  const int which = lane >> 2, x = which == 0 ? head : which == 1 ? from : which == 2 ? t1 + 1 : which == 3 ? from_all : t0 + 1;
+  int r = lane < 20 ? place_of(a, c.seq, lane & 3, x).before : 0;
   r += __shfl_xor_sync(0xffffffffu, r, 1);
   r += __shfl_xor_sync(0xffffffffu, r, 2);
   if (x >= c.lo) r -= c.dropped;
   const int rank0 = __shfl_sync(0xffffffffu, r, 0), rank1 = __shfl_sync(0xffffffffu, r, 4), rank2 = __shfl_sync(0xffffffffu, r, 8);
+  p.clean = (__shfl_sync(0xffffffffu, r, 12) + T - 1) / T;
+  p.clean_end = __shfl_sync(0xffffffffu, r, 16) / T;
   p.head = (rank0 + T - 1) / T;
   p.first = rank1 / T;
   p.last = max(p.first, (rank2 + T - 1) / T);

@@ -29,12 +29,14 @@ struct ChunkPlan {
 static_assert(sizeof(ChunkPlan) == 128, "");
 
 // A block of rows: queries of one mode of a chunk (in order), their heads of one KV head.  It sees
-// the chunk's tiles 0 .. head-1 (sinks) and first .. last-1.
+// the chunk's tiles 0 .. head-1 (sinks) and first .. last-1, of which every row sees the whole of
+// clean .. clean_end-1.
 struct BlockPlan {
   int chunk, row, rows, local;  // rows row .. of (list of queries of the mode) x (heads of a KV head)
   int head, first, last, tiles;
+  int clean, clean_end;
   int query0;                   // the mode's first query in the list
-  int pad[7];
+  int pad[5];
 };
 static_assert(sizeof(BlockPlan) == 64, "");
 

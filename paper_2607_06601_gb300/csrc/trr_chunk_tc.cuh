@@ -30,7 +30,8 @@ struct ChunkSegment {
   int tiles;              // 0: no more
   int block, kvh, rows;   // 128 rows or fewer: in both halves, which take the tiles in turn
   int dest;               // -1: the output rows, else the slot of the piece
-  int pad[3];
+  int clean, clean_end;   // tiles of the run that every row sees whole; the others come with their positions
+  int pad;
 };
 
 template <int D>
@@ -82,6 +83,7 @@ struct ChunkCtx {
   __device__ uint32_t col_s(int half) const { return tmem + kT * half; }
   __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 256 + 64 * half : 160 + 48 * half); }
   __device__ uint32_t col_o(int half) const { return tmem + 512 - D * (2 - half); }
+  __device__ __forceinline__ bool there(uint64_t* b, uint32_t parity) const { return mbar_test_at(smem_u32(b), parity); }
   // A bounded wait by a whole warp; all of its lanes get the same answer.  Once one has given up, none waits any
   // more.  (Short, since a warp among others' code pays for the fetch of every instruction.)
   __device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity) const {
@@ -112,7 +114,7 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   const int64_t per = g.head->per, work = g.head->work;
   const int blocks = g.head->blocks;
   const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
-  int tiles_done = 0, segs = 0, copies = 0, pos_copies = 0;
+  int segs = 0, copies = 0, pos_copies = 0;
   bool ok = true;
   PieceInfo piece = {-1, 0, 0, 0};
   auto push = [&](const ChunkSegment& s, const BlockPlan& p, int tile0, int from) {
@@ -123,24 +125,25 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
       mbar_arrive(x.seg_full(segs % kSpanSlots));
     }
     ++segs;
-    for (int i = from; i < from + s.tiles; ++i, ++tiles_done) {
-      const int tile = tile0 + (i < p.head ? i : p.first + i - p.head);
-      const int slot = tiles_done % L::kSlots, at = tiles_done % kPosSlots;
-      ok = x.wait(x.kv_empty(slot), ((tiles_done / L::kSlots) & 1) ^ 1);
+    for (int i = from; i < from + s.tiles; ++i, ++copies) {
+      const int tile = tile0 + (i < p.head ? i : p.first + i - p.head), slot = copies % L::kSlots;
+      if (i - from < s.clean || i - from >= s.clean_end) {
+        const int at = pos_copies % kPosSlots;
+        ok = x.wait(x.pos_empty(at), ((pos_copies / kPosSlots) & 1) ^ 1);
+        if (!ok) return;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(x.pos_full(at), 4 * L::kT);
+          bulk_g2s(x.base + L::kPos + at * 4 * L::kT, g.pos + static_cast<int64_t>(tile) * L::kT, 4 * L::kT, x.pos_full(at));
+        }
+        ++pos_copies;
+      }
+      ok = x.wait(x.kv_empty(slot), ((copies / L::kSlots) & 1) ^ 1);
       if (!ok) return;
       if (lane == 0) {
         mbar_arrive_expect_tx(x.kv_full(slot), 2 * L::kTile);
         bulk_g2s(x.base + L::kK + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 0), L::kTile, x.kv_full(slot));
         bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 1), L::kTile, x.kv_full(slot));
       }
-      ++copies;
-      ok = x.wait(x.pos_empty(at), ((tiles_done / kPosSlots) & 1) ^ 1);
-      if (!ok) return;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(x.pos_full(at), 4 * L::kT);
-        bulk_g2s(x.base + L::kPos + at * 4 * L::kT, g.pos + static_cast<int64_t>(tile) * L::kT, 4 * L::kT, x.pos_full(at));
-      }
-      ++pos_copies;
     }
   };
   if (b0 < b1) {
@@ -167,6 +170,9 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
         ChunkSegment s = {};
         s.tiles = t1 - t0; s.block = b; s.kvh = h; s.rows = p.rows;
         s.dest = t0 == 0 && t1 == p.tiles ? -1 : 2 * static_cast<int>(blockIdx.x) + (t0 > 0 ? 0 : 1);
+        // (the run's tiles past the sinks' are consecutive: p.first - p.head ahead of their place in the segment)
+        s.clean = max(p.clean, p.first) - (p.first - p.head) - t0;
+        s.clean_end = p.clean_end - (p.first - p.head) - t0;
         push(s, p, tile0, t0);
       }
     }
@@ -292,7 +298,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
   float* const exchange = reinterpret_cast<float*>(x.base + L::kQ);  // the second half's Q: 32 columns of 128 rows
   float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
-  int segs = 0, done = 0, it = 0, joins = 0;
+  int segs = 0, masked = 0, it = 0, joins = 0;  // masked: tiles of the CTA that came with positions
   for (;;) {
     if (!x.wait(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) return;
     const ChunkSegment sg = x.seg(segs % kSpanSlots);
@@ -345,24 +351,25 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     }
     float m = -INFINITY, l = 0.f;
     int mine_done = 0;  // tiles of this half
+    bool ready = false;  // the next scores are there
     for (int i = 0; i < sg.tiles; ++i) {
-      const int slot = (done + i) % kPosSlots;
-      if (!x.wait(x.pos_full(slot), ((done + i) / kPosSlots) & 1)) return;
-      if (turns && (i & 1) != half) {
-        if (lane == 0) mbar_arrive(x.pos_empty(slot));
-        continue;
-      }
-      const int32_t* pos = x.pos(slot);
-      const bool all = __all_sync(0xffffffffu, pos[T - 1] <= src.t && pos[0] >= src.lo);
+      const bool all = i >= sg.clean && i < sg.clean_end, other_half = turns && (i & 1) != half;
       uint32_t seen[(T + 31) / 32];
       if (!all) {
-        const int c = below<T>(pos, src.t + 1), from = pos[0] >= src.lo ? 0 : below<T>(pos, src.lo), head = local && from > 0 ? below<T>(pos, g.sinks) : 0;
+        const int slot = masked % kPosSlots;
+        if (!x.wait(x.pos_full(slot), (masked / kPosSlots) & 1)) return;
+        ++masked;
+        if (!other_half) {
+          const int32_t* pos = x.pos(slot);
+          const int c = below<T>(pos, src.t + 1), from = pos[0] >= src.lo ? 0 : below<T>(pos, src.lo), head = local && from > 0 ? below<T>(pos, g.sinks) : 0;
 #pragma unroll
-        for (int w = 0; w < (T + 31) / 32; ++w) seen[w] = bits_below(c, w) & (~bits_below(from, w) | bits_below(head, w));
+          for (int w = 0; w < (T + 31) / 32; ++w) seen[w] = bits_below(c, w) & (~bits_below(from, w) | bits_below(head, w));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x.pos_empty(slot));
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(x.pos_empty(slot));
-      if (!x.wait(x.s_full(half), it & 1)) return;
+      if (other_half) continue;
+      if (!ready && !x.wait(x.s_full(half), it & 1)) return;
       tc_fence_after();
       uint32_t a[C::kPartA], b[C::kPartB];
       tmem_ld(a, b, col_s);
@@ -393,19 +400,23 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         }
       }
       const float shift = m == -INFINITY ? 0.f : -m;
+      // (asked for before the exponentials, which hide how long the answer takes)
+      const bool used = it == 0 || x.there(x.o_done(half), (it - 1) & 1);
       l += weigh(a, f, shift);
       l += weigh(b, f, shift);
-      if (it > 0 && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
+      if (!__all_sync(0xffffffffu, used) && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
+      tc_fence_after();
       put_weights(col_p, a);
       put_weights(col_p + C::kPartA / 2, b);
+      const bool next = x.there(x.s_full(half), (it + 1) & 1);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(x.p_full(half));
+      ready = __all_sync(0xffffffffu, next);
       ++it;
       ++mine_done;
     }
-    done += sg.tiles;
     // rows out: the output itself, or (m, l, o) for the join of pieces
     if (mine_done > 0) {
       if (!x.wait(x.o_done(half), (it - 1) & 1)) return;

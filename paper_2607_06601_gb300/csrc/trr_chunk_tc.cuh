@@ -211,9 +211,10 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
     ++segs;
     if (n == 0) break;
     const int step = turns ? 2 : 1, first = turns ? half : 0;
-    auto scores = [&](int i) -> bool {  // S of the run's tile i
+    auto tile_there = [&](int i) { return x.there(x.kv_full((done + i) % L::kSlots), ((done + i) / L::kSlots) & 1); };
+    auto scores = [&](int i, bool there) -> bool {  // S of the run's tile i
       const int slot = (done + i) % L::kSlots;
-      if (!x.wait(x.kv_full(slot), ((done + i) / L::kSlots) & 1)) return false;
+      if (!there && !x.wait(x.kv_full(slot), ((done + i) / L::kSlots) & 1)) return false;
       tc_fence_after();
       if (elected()) {
         const uint64_t k = tc_desc(base + L::kK + slot * L::kTile, 16);
@@ -227,11 +228,16 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
       __syncwarp();
       return true;
     };
-    if (first < n) ok = x.wait(x.q_full(half), loads++ & 1) && scores(first);
+    if (first < n) ok = x.wait(x.q_full(half), loads++ & 1) && scores(first, false);
 #pragma unroll 1
     for (int i = first; i < n && ok; i += step, ++it) {
-      if (i + step < n) ok = x.wait(x.s_read(half), it & 1) && scores(i + step);
-      if (!ok || !(ok = x.wait(x.p_full(half), it & 1))) break;
+      // asked together: three answers take little longer than one
+      bool read = x.there(x.s_read(half), it & 1), tile = tile_there(i + step), weights = x.there(x.p_full(half), it & 1);
+      read = __all_sync(0xffffffffu, read);
+      tile = __all_sync(0xffffffffu, tile);
+      weights = __all_sync(0xffffffffu, weights);
+      if (i + step < n) ok = (read || x.wait(x.s_read(half), it & 1)) && scores(i + step, tile);
+      if (!ok || !(ok = weights || x.wait(x.p_full(half), it & 1))) break;
       tc_fence_after();
       if (elected()) {
         const int slot = (done + i) % L::kSlots;

@@ -27,7 +27,7 @@
 
 namespace trr {
 
-constexpr int kStageCtas = 3;  // CTAs of the staging kernel on an SM
+constexpr int kStageCtas = 4;  // CTAs of the staging kernel on an SM
 
 // ------------------------------------------------------------------------------ plan --
 
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     if (!whole) {
       h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units); h.tiles = static_cast<int>(tiles);
       // a small call's heads are shared out among CTAs, so that staging fills the GPU
-      const int64_t most = (2 * a.Hkv + kSpanThreads / 32 - 1) / (kSpanThreads / 32);
+      const int64_t most = (a.Hkv + 1) / 2;
       h.splits = static_cast<int>(units > 0 ? max(static_cast<int64_t>(1), min(most, kStageCtas * g.ctas / units)) : 1);
     }
     *g.head = h;
@@ -208,29 +208,35 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
 
 // ----------------------------------------------------------------------------- stage --
 
-// z + c s of eight elements as binary16, rounded once; a value past binary16's largest stays at it
+// z + c s of sixteen elements of class C as binary16, rounded once; a value past binary16's largest stays at it
 // (a group's largest level may round past the largest value that the append takes).
-template <int B>
-__device__ __forceinline__ uint4 expand_f16(uint32_t w0, uint32_t w1, uint32_t sz) {
-  const __half2 s = as_half2(__byte_perm(sz, 0, 0x1010)), z = as_half2(__byte_perm(sz, 0, 0x3232));
+template <int C>
+__device__ __forceinline__ void expand_f16(const Codes16& x, uint4 (&v)[2]) {
+  constexpr int B = 2 << C;
+  const __half2 s = as_half2(__byte_perm(x.sz, 0, 0x1010)), z = as_half2(__byte_perm(x.sz, 0, 0x3232));
   const __half2 k = as_half2(0x64006400u), top = as_half2(0x7BFF7BFFu);  // 1024 (1024 + c is exact), 65504
-  uint32_t p[4];
-  if (B == 8) {
-    p[0] = __byte_perm(w0, 0x64646464u, 0x4140); p[1] = __byte_perm(w0, 0x64646464u, 0x4342);
-    p[2] = __byte_perm(w1, 0x64646464u, 0x4140); p[3] = __byte_perm(w1, 0x64646464u, 0x4342);
-  } else if (B == 4) {
-    uint32_t t[4];  // elements i and i + 4
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = ((w0 >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
-    p[0] = __byte_perm(t[0], t[1], 0x5410); p[1] = __byte_perm(t[2], t[3], 0x5410);
-    p[2] = __byte_perm(t[0], t[1], 0x7632); p[3] = __byte_perm(t[2], t[3], 0x7632);
-  } else {
+  for (int half = 0; half < 2; ++half) {
+    const uint32_t w0 = B == 8 ? (half ? x.w[0].z : x.w[0].x) : B == 4 ? (half ? x.w[0].y : x.w[0].x) : (half ? x.w[0].x >> 16 : x.w[0].x);
+    uint32_t p[4];
+    if (B == 8) {
+      const uint32_t w1 = half ? x.w[0].w : x.w[0].y;
+      p[0] = __byte_perm(w0, 0x64646464u, 0x4140); p[1] = __byte_perm(w0, 0x64646464u, 0x4342);
+      p[2] = __byte_perm(w1, 0x64646464u, 0x4140); p[3] = __byte_perm(w1, 0x64646464u, 0x4342);
+    } else if (B == 4) {
+      uint32_t t[4];  // elements i and i + 4
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = ((w0 >> (4 * i)) & 3u) | ((w0 << (14 - 4 * i)) & 0x30000u) | 0x64006400u;
+      for (int i = 0; i < 4; ++i) t[i] = ((w0 >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
+      p[0] = __byte_perm(t[0], t[1], 0x5410); p[1] = __byte_perm(t[2], t[3], 0x5410);
+      p[2] = __byte_perm(t[0], t[1], 0x7632); p[3] = __byte_perm(t[2], t[3], 0x7632);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = ((w0 >> (4 * i)) & 3u) | ((w0 << (14 - 4 * i)) & 0x30000u) | 0x64006400u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = as_u32(__hmin2(__hfma2(__hsub2(as_half2(p[i]), k), s, z), top));
+    v[half] = make_uint4(p[0], p[1], p[2], p[3]);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) p[i] = as_u32(__hmin2(__hfma2(__hsub2(as_half2(p[i]), k), s, z), top));
-  return make_uint4(p[0], p[1], p[2], p[3]);
 }
 
 // Eight bf16 values as binary16; their largest magnitude, and whether binary16 lacks bits of one.
@@ -305,63 +311,36 @@ __device__ __forceinline__ void zero_rows(const ChunkArgs& g, int q, int h0, int
     for (int h = lane; h < h1 - h0; h += 32) g.lse[at + h] = -INFINITY;
 }
 
-// The tokens that the CTA has found, of heads h0 .. h1 - 1: a warp takes eight (d 64) or four rows of a head's K or V
-// of one class at a time, 16 elements a lane.
-template <int D>
-__device__ __forceinline__ void stage_rows(const ChunkArgs& g, const Found& f, int chunk, int h0, int h1) {
-  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kAhead = 4, T = chunk_tile(D);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
-  const int groups = f.groups(kRows), items = 2 * (h1 - h0) * groups;
-  for (int x0 = warp; x0 < items; x0 += kAhead * (kSpanThreads / 32)) {
-    Codes16 x[kAhead];
-    int cls[kAhead], row[kAhead];
+// A token's rows of every step-th head into its tile: 16 elements a lane of K and of V.  All lanes of the warp call it.
+template <int C, int D>
+__device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const uint8_t* page, int slot, int row, bool live, int h0, int h1, int step, int e) {
+  constexpr int T = chunk_tile(D), kLanes = D / 16;
+  const CodesAt<C, D> at(g.a, slot, e);
+  const int tile = row / T, r = row - tile * T;
+  uint8_t* to = g.tile + static_cast<int64_t>(tile) * g.a.Hkv * (4 * T * D) + (tile_at(T, r, 2 * e) & ~31);
+  const bool odd = r & 1;  // two chunks of a sector lie in the order of the row's place in its line
+#pragma unroll 2
+  for (int h = h0; h < h1; h += step) {
+    const uint8_t* slice = page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[C];
+    const Codes16 x[2] = {at.load(slice, 0), at.load(slice, 1)};
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int item = x0 + u * (kSpanThreads / 32), j = item / groups;
-      cls[u] = -1;
-      row[u] = -1;
-      if (item >= items) continue;
-      int first, n;
-      cls[u] = f.group(item - j * groups, kRows, &first, &n);
-      const int t = first + lane / kLanes;
-      if (t < n) {
-        const Found::Token& tok = f.token[cls[u]][t];
-        row[u] = tok.row;
-        x[u] = load_codes16<D>(g.a, cls[u], tok.page, tok.slot, h0 + (j >> 1), j & 1, e, lg_group);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (cls[u] < 0) continue;
-      const int j = (x0 + u * (kSpanThreads / 32)) / groups, h = h0 + (j >> 1);
+    for (int which = 0; which < 2; ++which) {
       uint4 v[2];
-      if (cls[u] == 3) {
+      if (C == 3) {
         uint32_t top = 0;
         bool lost = false;
-        v[0] = convert_f16(x[u].w[0], &top, &lost);
-        v[1] = convert_f16(x[u].w[1], &top, &lost);
-        if (row[u] < 0) top = 0, lost = false;
+        v[0] = convert_f16(x[which].w[0], &top, &lost);
+        v[1] = convert_f16(x[which].w[1], &top, &lost);
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (top >= 0x4780u || (lost && top < 0x3880u)) {  // 65536, 2^-14 as bf16
+        if (live && (top >= 0x4780u || (lost && top < 0x3880u))) {  // 65536, 2^-14 as bf16
           g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
           g.head->flagged = 1;
         }
-      } else if (cls[u] == 2) {
-        v[0] = expand_f16<8>(x[u].w[0].x, x[u].w[0].y, x[u].sz);
-        v[1] = expand_f16<8>(x[u].w[0].z, x[u].w[0].w, x[u].sz);
-      } else if (cls[u] == 1) {
-        v[0] = expand_f16<4>(x[u].w[0].x, 0, x[u].sz);
-        v[1] = expand_f16<4>(x[u].w[0].y, 0, x[u].sz);
       } else {
-        v[0] = expand_f16<2>(x[u].w[0].x, 0, x[u].sz);
-        v[1] = expand_f16<2>(x[u].w[0].x >> 16, 0, x[u].sz);
+        expand_f16<C == 3 ? 0 : C>(x[which], v);
       }
-      if (row[u] < 0) continue;
-      // two chunks of a sector, in the order of the row's place in its line
-      const int tile = row[u] / T, r = row[u] - tile * T;
-      const bool odd = r & 1;
-      store_sector(staged_tile<D>(g, tile, h, j & 1) + (tile_at(T, r, 2 * e) & ~31), odd ? v[1] : v[0], odd ? v[0] : v[1]);
+      if (live) store_sector(to + (2 * h + which) * (2 * T * D), odd ? v[1] : v[0], odd ? v[0] : v[1]);
     }
   }
 }
@@ -369,7 +348,8 @@ __device__ __forceinline__ void stage_rows(const ChunkArgs& g, const Found& f, i
 template <int D>
 __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(const __grid_constant__ ChunkArgs g) {
   constexpr int T = chunk_tile(D);
-  __shared__ Found f;
+  constexpr int kLanes = D / 16;
+  __shared__ Found<32 / kLanes> f;
   __shared__ int64_t s_sums[kSpanThreads / 32];
   __shared__ int s_last;
   const LayerArgs& a = g.a;
@@ -431,7 +411,13 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     const int row = c.tile0 * T + rank - (pos >= c.lo ? c.dropped : 0);
     if (p.page >= 0 && h0 == 0) g.pos[row] = pos;
     f.gather(a, p, cls, p.page >= 0 ? row : -1, tid);
-    stage_rows<D>(g, f, chunk, h0, h1);
+    for_groups(f, lg_parts(per), h0, [&](int k, const auto& tok, bool live, int h, int step) {
+      const int e = tid % kLanes;
+      if (k == 0) stage_token<0, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else if (k == 1) stage_token<1, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else if (k == 2) stage_token<2, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else stage_token<3, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+    });
   }
   // rows of a chunk's last tile past its tokens are zero and out of sight; queries that read nothing have zero rows
   for (int k = blockIdx.x; k < g.n; k += gridDim.x) {

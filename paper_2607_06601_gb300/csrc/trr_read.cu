@@ -17,7 +17,7 @@
 namespace trr {
 
 constexpr int kMostRows = 1 << 30;
-constexpr int kReadCtas = 3;  // CTAs on an SM
+constexpr int kReadCtas = 4;  // CTAs on an SM
 
 struct ReadArgs {
   LayerArgs a;
@@ -27,103 +27,116 @@ struct ReadArgs {
   uint8_t* bits;
   int64_t k_stride, v_stride;  // elements from a row to the next
   int sectors;                 // every row starts at 32 bytes
+  int lg_parts;                // a CTA's warps share a group's heads out in 2^lg_parts parts
 };
 
-// z + c s of eight elements of b bits, in binary32.
-template <int B>
-__device__ __forceinline__ void expand_f32(uint32_t w0, uint32_t w1, uint32_t sz, float (&v)[8]) {
-  const float s = __low2float(as_half2(sz)), z = __high2float(as_half2(sz));
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t w = B == 8 && i >= 4 ? w1 : w0;
-    const uint32_t c = B == 8 ? __byte_perm(w, 0x4B000000u, 0x7540 + (i & 3)) : ((w >> (B * i)) & ((1u << B) - 1)) | 0x4B000000u;
-    v[i] = __fmaf_rn(__uint_as_float(c) - 8388608.f, s, z);  // 2^23 + c as binary32: the difference is exact
-  }
+// (a, b) x (f, f) and (a, b) x (f, f) + (z, z).
+__device__ __forceinline__ void scale_pair(float& a, float& b, float f) {
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %2};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}" : "+f"(a), "+f"(b) : "f"(f));
+}
+__device__ __forceinline__ void affine_pair(float& a, float& b, float f, float z) {
+  asm("{\n .reg .b64 x, y, w;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %2};\n mov.b64 w, {%3, %3};\n fma.rn.f32x2 x, x, y, w;\n mov.b64 {%0, %1}, x;\n}"
+      : "+f"(a), "+f"(b)
+      : "f"(f), "f"(z));
 }
 
-// Eight elements of half `k` of a lane's sixteen.
-__device__ __forceinline__ void expand(const Codes16& x, int cls, int k, float (&v)[8]) {
-  const uint4 w = x.w[0];
-  if (cls == 3) {
-    const uint4 y = x.w[k];
-    const uint32_t u[4] = {y.x, y.y, y.z, y.w};
+// z + c s of sixteen elements of class C (kClasses: zeros), in binary32.  A code stays where it is in its word, which
+// is read as a binary32 subnormal, c 2^(p - 149) at bit p: with s 2^(100 - p) and z 2^-49 the sum has the roundings of
+// z + c s (nothing is subnormal: s and z are binary16), 2^-49 times.
+template <int C>
+__device__ __forceinline__ void expand_f32(const Codes16& x, float (&v)[16]) {
+  if constexpr (C == kClasses) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = bf16lo(u[i]), v[2 * i + 1] = bf16hi(u[i]);
-  } else if (cls == 2) {
-    expand_f32<8>(k ? w.z : w.x, k ? w.w : w.y, x.sz, v);
-  } else if (cls == 1) {
-    expand_f32<4>(k ? w.y : w.x, 0, x.sz, v);
-  } else if (cls == 0) {
-    expand_f32<2>(k ? w.x >> 16 : w.x, 0, x.sz, v);
+    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+  } else if constexpr (C == 3) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t w[4] = {x.w[k].x, x.w[k].y, x.w[k].z, x.w[k].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[8 * k + 2 * i] = bf16lo(w[i]), v[8 * k + 2 * i + 1] = bf16hi(w[i]);
+    }
   } else {
+    constexpr int B = 2 << C, kWords = B / 2, kHalf = 16 / B;  // elements in half a word
+    const uint32_t w[4] = {x.w[0].x, x.w[0].y, x.w[0].z, x.w[0].w};
+    const float s = __low2float(as_half2(x.sz)), z = __high2float(as_half2(x.sz)) * 0x1p-49f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    for (int i = 0; i < kHalf; ++i) {
+      const uint32_t mask = ((1u << B) - 1) << (B * i);
+      const float f = s * __int_as_float((127 + 100 - B * i) << 23);
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) {
+        float& a = v[2 * kHalf * k + i];
+        float& b = v[2 * kHalf * k + kHalf + i];
+        a = __uint_as_float(w[k] & mask);
+        b = __uint_as_float((w[k] >> 16) & mask);
+        affine_pair(a, b, f, z);
+        scale_pair(a, b, 0x1p49f);
+      }
+    }
   }
 }
 
-__device__ __forceinline__ uint4 as_bf16(const float (&v)[8]) {
+__device__ __forceinline__ uint4 as_bf16(const float* v) {
   return make_uint4(pack16(true, v[0], v[1]), pack16(true, v[2], v[3]), pack16(true, v[4], v[5]), pack16(true, v[6], v[7]));
 }
 __device__ __forceinline__ uint4 bits_of(const float* v) {
   return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
-// The tokens that the CTA has found, of heads h0 .. h1 - 1: a warp takes eight (d 64) or four rows of a head's K or V
-// of one class at a time, 16 elements a lane.  Sector: rows start at 32 bytes.
-template <int D, typename T>
-__device__ __forceinline__ void copy_rows(const ReadArgs& g, const Found& f, int h0, int h1) {
-  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kAhead = 4;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = lane % kLanes, lg_group = __ffs(g.a.G) - 1;
-  const int groups = f.groups(kRows), items = 2 * (h1 - h0) * groups;
-  for (int x0 = warp; x0 < items; x0 += kAhead * (kSpanThreads / 32)) {
-    Codes16 x[kAhead];
-    int cls[kAhead], row[kAhead];
+__device__ __forceinline__ void store16(const ReadArgs& g, uint16_t* to, const float (&v)[16]) {
+  const uint4 a = as_bf16(v), b = as_bf16(v + 8);
+  if (g.sectors) {
+    store_sector(to, a, b);
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = a;
+    reinterpret_cast<uint4*>(to)[1] = b;
+  }
+}
+__device__ __forceinline__ void store16(const ReadArgs& g, float* to, const float (&v)[16]) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int item = x0 + u * (kSpanThreads / 32), j = item / groups, h = h0 + (j >> 1);
-      cls[u] = kClasses;
-      row[u] = -1;
-      if (item >= items) continue;
-      int first, n;
-      cls[u] = f.group(item - j * groups, kRows, &first, &n);
-      const int t = first + lane / kLanes;
-      if (t >= n) continue;
-      const Found::Token& tok = f.token[cls[u]][t];
-      row[u] = tok.row;
-      if (g.a.maskb && cls[u] < kClasses) {  // per-head modes: the token may not store this head
-        const uint8_t* slice = tok.page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[cls[u]];
-        if (!(*reinterpret_cast<const uint64_t*>(slice + g.a.slice[cls[u]] - g.a.maskb) >> tok.slot & 1)) cls[u] = kClasses;
-      }
-      if (cls[u] < kClasses) x[u] = load_codes16<D>(g.a, cls[u], tok.page, tok.slot, h, j & 1, e, lg_group);
+  for (int k = 0; k < 2; ++k) {
+    const uint4 a = bits_of(v + 8 * k), b = bits_of(v + 8 * k + 4);
+    if (g.sectors) {
+      store_sector(to + 8 * k, a, b);
+    } else {
+      reinterpret_cast<uint4*>(to + 8 * k)[0] = a;
+      reinterpret_cast<uint4*>(to + 8 * k)[1] = b;
     }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (row[u] < 0) continue;
-      const int j = (x0 + u * (kSpanThreads / 32)) / groups, h = h0 + (j >> 1);
-      T* to = static_cast<T*>(j & 1 ? g.v : g.k) + row[u] * (j & 1 ? g.v_stride : g.k_stride) + h * D + 16 * e;
-      float v[8];
-      uint4 o[4];
-      expand(x[u], cls[u], 0, v);
-      if (sizeof(T) == 2) o[0] = as_bf16(v);
-      else o[0] = bits_of(v), o[1] = bits_of(v + 4);
-      expand(x[u], cls[u], 1, v);
-      if (sizeof(T) == 2) o[1] = as_bf16(v);
-      else o[2] = bits_of(v), o[3] = bits_of(v + 4);
-      if (g.sectors) {
-        store_sector(to, o[0], o[1]);
-        if (sizeof(T) == 4) store_sector(to + 8, o[2], o[3]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < static_cast<int>(sizeof(T)); ++k) reinterpret_cast<uint4*>(to)[k] = o[k];
-      }
-      if (g.bits && (j & 1) == 0 && e == 0) g.bits[static_cast<int64_t>(row[u]) * g.a.Hkv + h] = cls[u] < kClasses ? 2 << cls[u] : 0;
+  }
+}
+
+// A token's rows of every step-th head: 16 elements a lane of K and of V.
+template <int C, int D, typename T>
+__device__ __forceinline__ void copy_token(const ReadArgs& g, const uint8_t* page, int slot, int row, bool live, int h0, int h1, int step, int e) {
+  const CodesAt<C == kClasses ? 0 : C, D> at(g.a, slot, e);
+  T* k = static_cast<T*>(g.k) + row * g.k_stride + 16 * e;
+  T* v = static_cast<T*>(g.v) + row * g.v_stride + 16 * e;
+  if (!live) return;
+#pragma unroll 2
+  for (int h = h0; h < h1; h += step) {
+    const uint8_t* slice = page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[C == kClasses ? 0 : C];
+    bool there = C != kClasses;
+    if (C != kClasses && g.a.maskb)  // per-head modes: the token may not store this head
+      there = *reinterpret_cast<const uint64_t*>(slice + g.a.slice[C == kClasses ? 0 : C] - g.a.maskb) >> slot & 1;
+    float x[16], y[16];
+    if (there) {
+      const Codes16 ck = at.load(slice, 0), cv = at.load(slice, 1);
+      expand_f32<C>(ck, x);
+      expand_f32<C>(cv, y);
+    } else {
+      expand_f32<kClasses>(Codes16{}, x);
+      expand_f32<kClasses>(Codes16{}, y);
     }
+    store16(g, k + h * D, x);
+    store16(g, v + h * D, y);
+    if (g.bits && e == 0) g.bits[static_cast<int64_t>(row) * g.a.Hkv + h] = there ? 2 << C : 0;
   }
 }
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kSpanThreads, kReadCtas) read_kernel(const __grid_constant__ ReadArgs g) {
-  __shared__ Found f;
+  constexpr int kLanes = D / 16;
+  __shared__ Found<32 / kLanes> f;
   __shared__ int s_bad;
   const LayerArgs& a = g.a;
   const int i = threadIdx.x >> 2, c = threadIdx.x & 3;
@@ -166,7 +179,14 @@ __global__ void __launch_bounds__(kSpanThreads, kReadCtas) read_kernel(const __g
       if (seq >= 0 && seq < a.S && start >= 0 && start <= a.maxctx - len) p = place_of(a, seq, c, start + row - g.offsets[lo]);
     }
     f.gather(a, p, c, mine ? row : -1, threadIdx.x);
-    copy_rows<D, T>(g, f, h0, h1);
+    for_groups(f, g.lg_parts, h0, [&](int cls, const auto& tok, bool live, int h, int step) {
+      const int e = threadIdx.x % kLanes;
+      if (cls == 0) copy_token<0, D, T>(g, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else if (cls == 1) copy_token<1, D, T>(g, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else if (cls == 2) copy_token<2, D, T>(g, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else if (cls == 3) copy_token<3, D, T>(g, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      else copy_token<kClasses, D, T>(g, nullptr, 0, tok.row, live, h, h1, step, e);
+    });
   }
   __syncthreads();
   if (threadIdx.x == 0 && atom_add_acq_rel(a.ctrl + kReadDone, 1) == static_cast<int>(gridDim.x) - 1) {
@@ -203,9 +223,10 @@ extern "C" trr_status trr_kv_read(trr_cache* cache, int32_t layer, int32_t n, co
                 static_cast<uint64_t>(v_stride * size)) & 31) == 0;
   const int sms = cache_num_sms(cache), spans = (num_rows - 1) / kSpan + 1;
   // a small call's heads are shared out among CTAs, so that it fills the GPU too
-  const int most = (2 * l.Hkv + kSpanThreads / 32 - 1) / (kSpanThreads / 32);
+  const int most = (l.Hkv + 1) / 2;
   g.splits = std::max(1, std::min(most, kReadCtas * sms / spans));
   const int64_t units = static_cast<int64_t>(spans) * g.splits;
+  g.lg_parts = lg_parts((l.Hkv + g.splits - 1) / g.splits);
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(units, kReadCtas * sms)));
   auto kernel = l.d == 64 ? (type == TRR_BF16 ? read_kernel<64, uint16_t> : read_kernel<64, float>)
                           : (type == TRR_BF16 ? read_kernel<128, uint16_t> : read_kernel<128, float>);

@@ -47,15 +47,19 @@ __device__ __forceinline__ Place place_of(const LayerArgs& a, int seq, int c, in
   return Place{k * a.P + l, l < n && pos[l] == p ? page : -1, l};
 }
 
-// Tokens that a CTA has found, class by class, in order; class kClasses: positions that store nothing.
+// Tokens that a CTA has found, class by class, in order; class kClasses: positions that store nothing.  ROWS of a
+// class's, at most, form a group, which a warp takes together.
+template <int ROWS>
 struct Found {
   struct Token {
     const uint8_t* page;
     int slot, row;  // row: where its values go
   };
+  static constexpr int kMostGroups = kSpan / ROWS + kClasses + 1;
   Token token[kClasses + 1][kSpan];
-  int count[kClasses + 1];
   int warp_count[kSpanThreads / 32][kClasses + 1];
+  int count[kClasses + 1], groups;
+  int16_t group_class[kMostGroups], group_first[kMostGroups];
 
   // Thread 4 i + c brings class c's place of position i and the row that its values go to (row < 0: the position is
   // not asked for).  Every thread of the CTA calls it; what was found before has then been read by all.
@@ -76,29 +80,23 @@ struct Found {
     const uint32_t below = (1u << lane) - 1;
     if (p.page >= 0) token[c][before(c) + __popc(here & mine & below)] = Token{a.pool[c] + p.page * a.page_bytes[c], p.slot, row};
     if (none >> lane & 1) token[kClasses][before(kClasses) + __popc(none & below)] = Token{nullptr, 0, row};
-    if (tid <= kClasses) {
+    if (warp == 0) {
       int n = 0;
-      for (int w = 0; w < kSpanThreads / 32; ++w) n += warp_count[w][tid];
-      count[tid] = n;
+      if (lane <= kClasses)
+        for (int w = 0; w < kSpanThreads / 32; ++w) n += warp_count[w][lane];
+      int mine_groups = (n + ROWS - 1) / ROWS, first = mine_groups;
+      for (int o = 1; o < 8; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, first, o);
+        if (lane >= o) first += y;
+      }
+      first -= mine_groups;
+      if (lane <= kClasses) {
+        count[lane] = n;
+        for (int k = 0; k < mine_groups; ++k) group_class[first + k] = lane, group_first[first + k] = k * ROWS;
+        if (lane == kClasses) groups = first + mine_groups;
+      }
     }
     __syncthreads();
-  }
-  // Groups of `rows` tokens of one class: how many, and the class, first token and number of tokens of one.
-  __device__ __forceinline__ int groups(int rows) const {
-    int n = 0;
-    for (int c = 0; c <= kClasses; ++c) n += (count[c] + rows - 1) / rows;
-    return n;
-  }
-  __device__ __forceinline__ int group(int i, int rows, int* first, int* n) const {
-    int c = 0;
-    for (; c < kClasses; ++c) {
-      const int k = (count[c] + rows - 1) / rows;
-      if (i < k) break;
-      i -= k;
-    }
-    *first = i * rows;
-    *n = count[c];
-    return c;
   }
 };
 
@@ -108,29 +106,57 @@ struct Codes16 {
   uint32_t sz;  // scale and zero (binary16) of their group
 };
 
-// Elements 16 e .. 16 e + 15 of K (which 0) or V (1) of KV head h.
-template <int D>
-__device__ __forceinline__ Codes16 load_codes16(const LayerArgs& a, int c, const uint8_t* page, int slot, int h, int which, int e, int lg_group) {
-  const uint8_t* slice = page + a.hdr + static_cast<int64_t>(h) * a.slice[c];
-  const int lg = c + 1, row = D << lg >> 3, o = (which * a.P + slot) * row + (e << (lg + 1));
-  Codes16 r = {};
-  if (c == 3) {
-    r.w[0] = *reinterpret_cast<const uint4*>(slice + (a.swz ? swz_off(o) : o));
-    r.w[1] = *reinterpret_cast<const uint4*>(slice + (a.swz ? swz_off(o + 16) : o + 16));
+// Where elements 16 e .. 16 e + 15 of a token's K and V lie in its slices, the same in every KV head's.
+template <int C, int D>
+struct CodesAt {
+  static constexpr int kRow = (D << (C + 1)) >> 3;  // bytes of a row
+  int code[2][2], sz[2];                            // [K, V], of 16 bits [first, second half]
+  __device__ __forceinline__ CodesAt(const LayerArgs& a, int slot, int e) {
+    const int lg_group = __ffs(a.G) - 1;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const int o = (which * a.P + slot) * kRow + (e << (C + 2));
+      code[which][0] = C >= 2 && a.swz ? static_cast<int>(swz_off(o)) : o;
+      code[which][1] = C == 3 ? (a.swz ? static_cast<int>(swz_off(o + 16)) : o + 16) : 0;
+      sz[which] = 2 * a.P * kRow + ((which * a.P + slot) * (D >> lg_group) + (16 * e >> lg_group)) * 4;
+    }
+  }
+  __device__ __forceinline__ Codes16 load(const uint8_t* slice, int which) const {
+    Codes16 r;
+    const uint8_t* p = slice + code[which][0];
+    if (C == 3) {
+      r.w[0] = *reinterpret_cast<const uint4*>(p);
+      r.w[1] = *reinterpret_cast<const uint4*>(slice + code[which][1]);
+      return r;
+    }
+    if (C == 2) {
+      r.w[0] = *reinterpret_cast<const uint4*>(p);
+    } else if (C == 1) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      r.w[0].x = x.x;
+      r.w[0].y = x.y;
+    } else {
+      r.w[0].x = *reinterpret_cast<const uint32_t*>(p);
+    }
+    r.sz = *reinterpret_cast<const uint32_t*>(slice + sz[which]);
     return r;
   }
-  if (c == 2) {
-    r.w[0] = *reinterpret_cast<const uint4*>(slice + (a.swz ? swz_off(o) : o));
-  } else if (c == 1) {
-    const uint2 x = *reinterpret_cast<const uint2*>(slice + o);
-    r.w[0].x = x.x;
-    r.w[0].y = x.y;
-  } else {
-    r.w[0].x = *reinterpret_cast<const uint32_t*>(slice + o);
+};
+
+// A CTA's groups, shared out with `parts` shares of the heads (a power of two) among its warps: body(class, token,
+// whether the lane has one, first head, step).
+template <int ROWS, typename Body>
+__device__ __forceinline__ void for_groups(const Found<ROWS>& f, int lg_parts, int h0, Body body) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int x = warp; x < f.groups << lg_parts; x += kSpanThreads / 32) {
+    const int g = x >> lg_parts, c = f.group_class[g], t = f.group_first[g] + lane / (32 / ROWS);
+    const bool live = t < f.count[c];
+    body(c, f.token[c][live ? t : 0], live, h0 + (x & ((1 << lg_parts) - 1)), 1 << lg_parts);
   }
-  r.sz = reinterpret_cast<const uint32_t*>(slice + 2 * a.P * row)[(which * a.P + slot) * (D >> lg_group) + (16 * e >> lg_group)];
-  return r;
 }
+
+// Parts that a group's heads are shared out in: enough that eight warps come out nearly even, two heads each at least.
+__host__ __device__ inline int lg_parts(int heads) { return heads >= 8 ? 2 : heads >= 4 ? 1 : 0; }
 
 // 32 bytes in one store (p aligned to them).
 __device__ __forceinline__ void store_sector(void* p, uint4 a, uint4 b) {

@@ -319,10 +319,16 @@ __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const
   const int tile = row / T, r = row - tile * T;
   uint8_t* to = g.tile + static_cast<int64_t>(tile) * g.a.Hkv * (4 * T * D) + (tile_at(T, r, 2 * e) & ~31);
   const bool odd = r & 1;  // two chunks of a sector lie in the order of the row's place in its line
-#pragma unroll 2
+  const int64_t slice_bytes = g.a.slice[C];
+  const uint8_t* slice = page + g.a.hdr + h0 * slice_bytes;
+  // a head's codes are asked for before the last head's are written: nothing moves a load over a store by itself
+  Codes16 next[2];
+  if (h0 < h1) next[0] = at.load(slice, 0), next[1] = at.load(slice, 1);
+#pragma unroll 1
   for (int h = h0; h < h1; h += step) {
-    const uint8_t* slice = page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[C];
-    const Codes16 x[2] = {at.load(slice, 0), at.load(slice, 1)};
+    const Codes16 x[2] = {next[0], next[1]};
+    slice += step * slice_bytes;
+    if (h + step < h1) next[0] = at.load(slice, 0), next[1] = at.load(slice, 1);
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       uint4 v[2];

@@ -112,24 +112,32 @@ __device__ __forceinline__ void copy_token(const ReadArgs& g, const uint8_t* pag
   T* k = static_cast<T*>(g.k) + row * g.k_stride + 16 * e;
   T* v = static_cast<T*>(g.v) + row * g.v_stride + 16 * e;
   if (!live) return;
-#pragma unroll 2
+  const int64_t slice_bytes = g.a.slice[C == kClasses ? 0 : C];
+  const uint8_t* slice = page + g.a.hdr + h0 * slice_bytes;
+  // a head's codes are asked for before the last head's are written: nothing moves a load over a store by itself
+  Codes16 ck = {}, cv = {};
+  bool there = false;
+  auto load = [&](int h) {
+    there = C != kClasses && h < h1;
+    if (there && g.a.maskb)  // per-head modes: the token may not store this head
+      there = *reinterpret_cast<const uint64_t*>(slice + slice_bytes - g.a.maskb) >> slot & 1;
+    if (there) ck = at.load(slice, 0), cv = at.load(slice, 1);
+    slice += step * slice_bytes;
+  };
+  load(h0);
+#pragma unroll 1
   for (int h = h0; h < h1; h += step) {
-    const uint8_t* slice = page + g.a.hdr + static_cast<int64_t>(h) * g.a.slice[C == kClasses ? 0 : C];
-    bool there = C != kClasses;
-    if (C != kClasses && g.a.maskb)  // per-head modes: the token may not store this head
-      there = *reinterpret_cast<const uint64_t*>(slice + g.a.slice[C == kClasses ? 0 : C] - g.a.maskb) >> slot & 1;
-    float x[16], y[16];
-    if (there) {
-      const Codes16 ck = at.load(slice, 0), cv = at.load(slice, 1);
-      expand_f32<C>(ck, x);
-      expand_f32<C>(cv, y);
-    } else {
-      expand_f32<kClasses>(Codes16{}, x);
-      expand_f32<kClasses>(Codes16{}, y);
-    }
+    const Codes16 k0 = ck, v0 = cv;
+    const bool now = there;
+    load(h + step);
+    float x[16];
+    if (now) expand_f32<C>(k0, x);
+    else expand_f32<kClasses>(k0, x);
     store16(g, k + h * D, x);
-    store16(g, v + h * D, y);
-    if (g.bits && e == 0) g.bits[static_cast<int64_t>(row) * g.a.Hkv + h] = there ? 2 << C : 0;
+    if (now) expand_f32<C>(v0, x);
+    else expand_f32<kClasses>(v0, x);
+    store16(g, v + h * D, x);
+    if (g.bits && e == 0) g.bits[static_cast<int64_t>(row) * g.a.Hkv + h] = now ? 2 << C : 0;
   }
 }
 

@@ -64,7 +64,7 @@ __device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* warp_sums, in
 }
 
 __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __grid_constant__ ChunkArgs g) {
-  __shared__ int s_bad, s_lo, s_count[2], s_warp[2][kPlanChunkThreads / 32], s_before[3][kClasses], s_last;
+  __shared__ int s_bad, s_lo, s_count[2], s_warp[2][kPlanChunkThreads / 32], s_before[4][kClasses], s_last;
   __shared__ int64_t s_sums[kPlanChunkThreads / 32];
   const LayerArgs& a = g.a;
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -139,7 +139,11 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
   const bool reads = full + local > 0;
   lo = full > 0 ? 0 : s_lo;
   const int end = start + len, sinks = reads ? min(g.sinks, lo) : 0;
-  if (tid < 3 * kClasses && reads) s_before[tid / kClasses][tid % kClasses] = place_of(a, seq, tid % kClasses, tid < 4 ? sinks : tid < 8 ? lo : end).before;
+  static_assert(kPlanChunkThreads / 32 == 4 * kClasses, "a warp for each class of four positions");
+  if (reads) {
+    const int which = warp / kClasses, before = tokens_before(a, seq, warp % kClasses, which == 0 ? sinks : which == 1 ? lo : which == 2 ? end : min(g.sinks, end), lane);
+    if (lane == 0) s_before[which][warp % kClasses] = before;
+  }
   __syncthreads();
   const int heads = a.Hq / a.Hkv;
   if (tid == 0) {
@@ -151,6 +155,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
       for (int k = 0; k < kClasses; ++k) {
         c.dropped += s_before[1][k] - s_before[0][k];
         c.tokens += s_before[2][k] - s_before[1][k] + s_before[0][k];
+        c.head += s_before[3][k];
       }
       c.tiles = (c.tokens + chunk_tile(a.d) - 1) / chunk_tile(a.d);
       c.units = (c.span + kSpan - 1) / kSpan;
@@ -367,8 +372,9 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     for (int q = blockIdx.x * (kSpanThreads / 32) + warp; q < g.num_tokens; q += gridDim.x * (kSpanThreads / 32)) zero_rows(g, q, 0, a.Hq, lane);
     return;
   }
-  // blocks of rows first: the CTA that plans the last one lays them end to end
-  for (int b = blockIdx.x + warp * gridDim.x; b < head.blocks; b += gridDim.x * (kSpanThreads / 32)) plan_block(g, b, lane);
+  // Three kinds of work, dealt out from the first CTA up, from the middle and from the last one down, so that in a small
+  // call each CTA has one of them.  Blocks of rows first: the CTA that is done last lays them end to end.
+  for (int b = blockIdx.x * (kSpanThreads / 32) + warp; b < head.blocks; b += gridDim.x * (kSpanThreads / 32)) plan_block(g, b, lane);
   __syncthreads();
   if (tid == 0) s_last = atom_add_acq_rel(a.ctrl + kChunkPlanned, 1) == static_cast<int>(gridDim.x) - 1;
   __syncthreads();
@@ -386,15 +392,40 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     if (tid == 0) {
       g.base[head.blocks] = work;
       g.head->work = work;
-      g.head->per = max((work + g.ctas - 1) / g.ctas, static_cast<int64_t>(kChunkSegmentCost + 2 * kChunkTileCost));
+      g.head->per = max((work + g.ctas - 1) / g.ctas, static_cast<int64_t>(kChunkLeastShare));
       a.ctrl[kChunkPlanned] = 0;
     }
+  }
+  // which staged tokens each query sees, by eight lanes: the classes of two positions; queries that read nothing have zero rows
+  for (int k0 = ((blockIdx.x + gridDim.x / 2) % gridDim.x * (kSpanThreads / 32) + warp) * 4; k0 < g.num_tokens; k0 += gridDim.x * (kSpanThreads / 32) * 4) {
+    const int k = k0 + lane / 8;
+    int lo = 0, hi = g.n - 1;  // a place of the list: of the last chunk that starts at k or before it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (g.chunk[mid].row0 <= k) lo = mid;
+      else hi = mid - 1;
+    }
+    const ChunkPlan& p = g.chunk[lo];
+    const bool mine = k < g.num_tokens && k >= p.row0 && k < p.row0 + p.len, reads = mine && k < p.row0 + p.full + p.local;
+    const int q = mine ? g.list[k] : 0;
+    int rank = 0;
+    if (reads) {
+      const int t = p.start + q - p.row0;
+      const int from = k >= p.row0 + p.full ? max(0, t - (g.windows ? g.windows[q] : g.window_scalar) + 1) : 0, x = lane & 4 ? t + 1 : from;
+      rank = place_of(a, p.seq, lane & 3, x).before - ((lane & 3) == 0 && x >= p.lo ? p.dropped : 0);
+    }
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    const int upto = __shfl_xor_sync(0xffffffffu, rank, 4);
+    if (reads && (lane & 7) == 0) g.sight[k] = make_int2(rank, upto);
+    for (uint32_t left = __ballot_sync(0xffffffffu, mine && !reads && (lane & 7) == 0); left; left &= left - 1)
+      zero_rows(g, __shfl_sync(0xffffffffu, q, __ffs(left) - 1), 0, a.Hq, lane);
   }
   // units: 64 positions of a chunk's line, some of the KV heads
   const int per = (a.Hkv + head.splits - 1) / head.splits;
   int chunk = -1;
   ChunkPlan c;
-  for (int u = blockIdx.x; u < head.units * head.splits; u += gridDim.x) {
+  for (int u = gridDim.x - 1 - blockIdx.x; u < head.units * head.splits; u += gridDim.x) {
     const int unit = u / head.splits, h0 = u % head.splits * per, h1 = min(a.Hkv, h0 + per);
     if (chunk < 0 || unit >= c.unit0 + c.units) {
       int lo = chunk < 0 ? 0 : chunk, hi = g.n - 1;
@@ -415,7 +446,6 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     rank += __shfl_xor_sync(0xffffffffu, rank, 1);
     rank += __shfl_xor_sync(0xffffffffu, rank, 2);
     const int row = c.tile0 * T + rank - (pos >= c.lo ? c.dropped : 0);
-    if (p.page >= 0 && h0 == 0) g.pos[row] = pos;
     f.gather(a, p, cls, p.page >= 0 ? row : -1, tid);
     for_groups(f, lg_parts(per), h0, [&](int k, const auto& tok, bool live, int h, int step) {
       const int e = tid % kLanes;
@@ -425,25 +455,14 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
       else stage_token<3, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
     });
   }
-  // rows of a chunk's last tile past its tokens are zero and out of sight; queries that read nothing have zero rows
+  // rows of a chunk's last tile past its tokens are zero (their weights are)
   for (int k = blockIdx.x; k < g.n; k += gridDim.x) {
     const ChunkPlan& p = g.chunk[k];
     const int at = p.tokens % T, tile = p.tile0 + p.tiles - 1;
     if (at == 0) continue;
-    for (int r = at + tid; r < T; r += kSpanThreads) g.pos[static_cast<int64_t>(tile) * T + r] = INT_MAX;
     for (int j = 0; j < 2 * a.Hkv; ++j)
       for (int x = tid; x < (T - at) * (D / 8); x += kSpanThreads)
         *reinterpret_cast<uint4*>(staged_tile<D>(g, tile, j >> 1, j & 1) + tile_at(T, at + x / (D / 8), x % (D / 8))) = make_uint4(0, 0, 0, 0);
-  }
-  for (int k = blockIdx.x * (kSpanThreads / 32) + warp; k < g.num_tokens; k += gridDim.x * (kSpanThreads / 32)) {
-    int lo = 0, hi = g.n - 1;  // places of the list: of the last chunk that starts at k or before it
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (g.chunk[mid].row0 <= k) lo = mid;
-      else hi = mid - 1;
-    }
-    const ChunkPlan& p = g.chunk[lo];
-    if (k >= p.row0 + p.full + p.local && k < p.row0 + p.len) zero_rows(g, g.list[k], 0, a.Hq, lane);
   }
 }
 
@@ -605,6 +624,7 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->head = reinterpret_cast<ChunkHeader*>(take(sizeof(ChunkHeader)));
   g->chunk = reinterpret_cast<ChunkPlan*>(take(static_cast<int64_t>(sizeof(ChunkPlan)) * n));
   g->list = reinterpret_cast<int32_t*>(take(4ll * num_tokens));
+  g->sight = reinterpret_cast<int2*>(take(8ll * num_tokens));
   g->block = reinterpret_cast<BlockPlan*>(take(static_cast<int64_t>(sizeof(BlockPlan)) * blocks));
   g->base = reinterpret_cast<int64_t*>(take(8 * (blocks + 1)));
   g->flag = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
@@ -613,7 +633,6 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->part_o = reinterpret_cast<float*>(take(4ll * 2 * ctas * kBlockRows * l.d));
   g->most_blocks = static_cast<int>(blocks);
   const int64_t fixed = off, T = chunk_tile(l.d);
-  g->pos = reinterpret_cast<int32_t*>(take(4 * most_tiles * T));
   g->tile = take((most_tiles * l.Hkv * 2 * T * l.d * 2 + 1023) / 1024 * 1024);
   return most_tiles ? off : fixed;
 }
@@ -681,7 +700,7 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   g.q = static_cast<const uint16_t*>(q_bf16);
   g.out = static_cast<uint16_t*>(out_bf16);
   g.lse = lse;
-  const int64_t fixed = lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, 0), T = chunk_tile(l.d), per_tile = 4 * T + 4 * l.Hkv * T * l.d;
+  const int64_t fixed = lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, 0), T = chunk_tile(l.d), per_tile = 4 * l.Hkv * T * l.d;
   const int64_t bytes = static_cast<int64_t>(std::min<uint64_t>(workspace_bytes, 1ull << 60));
   int64_t room = std::min<int64_t>((bytes - fixed) / per_tile, INT_MAX / T);
   if (lay_workspace(&g, nullptr, l, num_chunks, num_tokens, g.ctas, room) > bytes) --room;  // (its parts are rounded up)

@@ -23,15 +23,18 @@ constexpr int kChunkThreads = 384;
 // Registers a thread: 168 at launch; the softmax warpgroups take what the third gives up.
 constexpr int kChunkLaunchRegisters = 168, kChunkSoftmaxRegisters = 208, kChunkOtherRegisters = 88;
 static_assert(256 * kChunkSoftmaxRegisters + 128 * kChunkOtherRegisters <= kChunkThreads * kChunkLaunchRegisters, "");
-constexpr int kPosSlots = 4, kSpanSlots = 2;
+constexpr int kRunSlots = 4;
 
-// A run of tiles for one block and KV head, as the softmax warps and the product warp need it.
+// A run of tiles for one block and KV head, as the softmax warps and the product warps need it.
 struct ChunkSegment {
   int tiles;              // 0: no more
   int block, kvh, rows;   // 128 rows or fewer: in both halves, which take the tiles in turn
   int dest;               // -1: the output rows, else the slot of the piece
-  int clean, clean_end;   // tiles of the run that every row sees whole; the others come with their positions
-  int pad;
+  int clean, clean_end;   // tiles of the run that every row sees whole
+  int from, head, skip;   // the run's first tile of the segment's; the segment's first `head` are the chunk's, the others `skip` further
+  int query0, row, local; // of the block
+  int sinks;              // staged tokens that a local row sees beside its window
+  int pad[2];
 };
 
 template <int D>
@@ -42,14 +45,14 @@ struct ChunkSmem {
   static constexpr int kSlots = D == 64 ? 4 : 3;    // of K, and of V
   static constexpr int kK = 2 * kQ;                 // behind Q
   static constexpr int kV = kK + kSlots * kTile;
-  static constexpr int kPos = kV + kSlots * kTile;
-  static constexpr int kMl = kPos + kPosSlots * kT * 4;  // (m, l) of the second half's rows, for a join
+  static constexpr int kExchange = kV + kSlots * kTile;  // 32 columns of the second half's rows, and (m, l), for a join
+  static constexpr int kMl = kExchange + 32 * kHalfRows * 4;
   static constexpr int kSeg = kMl + kHalfRows * 8;
-  static constexpr int kBars = kSeg + kSpanSlots * static_cast<int>(sizeof(ChunkSegment));
-  static constexpr int kNumBars = 2 * kSlots + 2 * kPosSlots + 2 * kSpanSlots + 2 * 6 + 2;
+  static constexpr int kBars = kSeg + kRunSlots * static_cast<int>(sizeof(ChunkSegment));
+  static constexpr int kNumBars = 2 * kSlots + 2 * kRunSlots + 2 * 6 + 2;
   static constexpr int kTotal = kBars + 8 * kNumBars;
   static_assert(kTotal + 1024 + 64 <= 227 * 1024, "");
-  static_assert(kTile % 1024 == 0 && kQ >= 32 * kHalfRows * 4, "a join takes 32 columns at a time through Q's place");
+  static_assert(kTile % 1024 == 0, "");
 };
 
 template <int D>
@@ -64,11 +67,9 @@ struct ChunkCtx {
   __device__ uint64_t* bar(int i) const { return reinterpret_cast<uint64_t*>(base + L::kBars) + i; }
   __device__ uint64_t* kv_full(int i) const { return bar(i); }
   __device__ uint64_t* kv_empty(int i) const { return bar(L::kSlots + i); }
-  __device__ uint64_t* pos_full(int i) const { return bar(2 * L::kSlots + i); }
-  __device__ uint64_t* pos_empty(int i) const { return bar(2 * L::kSlots + kPosSlots + i); }
-  __device__ uint64_t* seg_full(int i) const { return bar(2 * L::kSlots + 2 * kPosSlots + i); }
-  __device__ uint64_t* seg_empty(int i) const { return bar(2 * L::kSlots + 2 * kPosSlots + kSpanSlots + i); }
-  __device__ uint64_t* half_bar(int half, int i) const { return bar(2 * L::kSlots + 2 * kPosSlots + 2 * kSpanSlots + 6 * half + i); }
+  __device__ uint64_t* seg_full(int i) const { return bar(2 * L::kSlots + i); }
+  __device__ uint64_t* seg_empty(int i) const { return bar(2 * L::kSlots + kRunSlots + i); }
+  __device__ uint64_t* half_bar(int half, int i) const { return bar(2 * L::kSlots + 2 * kRunSlots + 6 * half + i); }
   __device__ uint64_t* q_full(int half) const { return half_bar(half, 0); }
   __device__ uint64_t* s_full(int half) const { return half_bar(half, 1); }
   __device__ uint64_t* s_read(int half) const { return half_bar(half, 2); }
@@ -78,7 +79,6 @@ struct ChunkCtx {
   __device__ uint64_t* join_full() const { return half_bar(2, 0); }
   __device__ uint64_t* join_empty() const { return half_bar(2, 1); }
   __device__ ChunkSegment& seg(int i) const { return reinterpret_cast<ChunkSegment*>(base + L::kSeg)[i]; }
-  __device__ const int32_t* pos(int i) const { return reinterpret_cast<const int32_t*>(base + L::kPos) + i * kT; }
   // TMEM columns: scores, weights (two to a column), sums
   __device__ uint32_t col_s(int half) const { return tmem + kT * half; }
   __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 256 + 64 * half : 160 + 48 * half); }
@@ -114,35 +114,30 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   const int64_t per = g.head->per, work = g.head->work;
   const int blocks = g.head->blocks;
   const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
-  int segs = 0, copies = 0, pos_copies = 0;
+  int segs = 0, copies = 0;
   bool ok = true;
   PieceInfo piece = {-1, 0, 0, 0};
-  auto push = [&](const ChunkSegment& s, const BlockPlan& p, int tile0, int from) {
-    ok = x.wait(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
+  auto announce = [&](const ChunkSegment& s) {
+    ok = ok && x.wait(x.seg_empty(segs % kRunSlots), ((segs / kRunSlots) & 1) ^ 1);
     if (!ok) return;
     if (lane == 0) {
-      x.seg(segs % kSpanSlots) = s;
-      mbar_arrive(x.seg_full(segs % kSpanSlots));
+      x.seg(segs % kRunSlots) = s;
+      mbar_arrive(x.seg_full(segs % kRunSlots));
     }
     ++segs;
-    for (int i = from; i < from + s.tiles; ++i, ++copies) {
-      const int tile = tile0 + (i < p.head ? i : p.first + i - p.head), slot = copies % L::kSlots;
-      if (i - from < s.clean || i - from >= s.clean_end) {
-        const int at = pos_copies % kPosSlots;
-        ok = x.wait(x.pos_empty(at), ((pos_copies / kPosSlots) & 1) ^ 1);
-        if (!ok) return;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(x.pos_full(at), 4 * L::kT);
-          bulk_g2s(x.base + L::kPos + at * 4 * L::kT, g.pos + static_cast<int64_t>(tile) * L::kT, 4 * L::kT, x.pos_full(at));
-        }
-        ++pos_copies;
-      }
+  };
+  // A run is announced before the tiles of the one before it are copied, so that its rows can be fetched in good time.
+  ChunkSegment last = {};
+  int last_tile0 = 0;
+  auto copy = [&]() {
+    for (int i = 0; i < last.tiles && ok; ++i, ++copies) {
+      const int at = last.from + i, tile = last_tile0 + at + (at < last.head ? 0 : last.skip), slot = copies % L::kSlots;
       ok = x.wait(x.kv_empty(slot), ((copies / L::kSlots) & 1) ^ 1);
-      if (!ok) return;
+      if (!ok) break;
       if (lane == 0) {
         mbar_arrive_expect_tx(x.kv_full(slot), 2 * L::kTile);
-        bulk_g2s(x.base + L::kK + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 0), L::kTile, x.kv_full(slot));
-        bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, s.kvh, 1), L::kTile, x.kv_full(slot));
+        bulk_g2s(x.base + L::kK + slot * L::kTile, staged_tile<D>(g, tile, last.kvh, 0), L::kTile, x.kv_full(slot));
+        bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, last.kvh, 1), L::kTile, x.kv_full(slot));
       }
     }
   };
@@ -159,7 +154,7 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
       if (start >= b1) break;
       const BlockPlan p = g.block[b];
       if (p.tiles == 0) continue;
-      const int tile0 = g.chunk[p.chunk].tile0;
+      const int tile0 = g.chunk[p.chunk].tile0, sinks = g.chunk[p.chunk].head;
       const int64_t cost = chunk_cost(p.tiles);
       for (int h = static_cast<int>(max(static_cast<int64_t>(0), (b0 - start) / cost)); h < g.a.Hkv && ok; ++h) {
         const int64_t S = start + h * cost;
@@ -170,24 +165,22 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
         ChunkSegment s = {};
         s.tiles = t1 - t0; s.block = b; s.kvh = h; s.rows = p.rows;
         s.dest = t0 == 0 && t1 == p.tiles ? -1 : 2 * static_cast<int>(blockIdx.x) + (t0 > 0 ? 0 : 1);
-        // (the run's tiles past the sinks' are consecutive: p.first - p.head ahead of their place in the segment)
-        s.clean = max(p.clean, p.first) - (p.first - p.head) - t0;
-        s.clean_end = p.clean_end - (p.first - p.head) - t0;
-        push(s, p, tile0, t0);
+        s.from = t0; s.head = p.head; s.skip = p.first - p.head;
+        s.clean = max(p.clean, p.first) - s.skip - t0;
+        s.clean_end = p.clean_end - s.skip - t0;
+        s.query0 = p.query0; s.row = p.row; s.local = p.local; s.sinks = sinks;
+        announce(s);
+        copy();
+        last = s;
+        last_tile0 = tile0;
       }
     }
   }
   if (lane == 0) g.piece[blockIdx.x] = piece;
-  if (ok) {  // no more
-    ok = x.wait(x.seg_empty(segs % kSpanSlots), ((segs / kSpanSlots) & 1) ^ 1);
-    if (ok && lane == 0) {
-      x.seg(segs % kSpanSlots).tiles = 0;
-      mbar_arrive(x.seg_full(segs % kSpanSlots));
-    }
-  }
+  announce(ChunkSegment{});  // no more
+  copy();
   // the CTA stays until its copies have landed
   for (int k = max(0, copies - L::kSlots); k < copies; ++k) mbar_wait(x.kv_full(k % L::kSlots), (k / L::kSlots) & 1);
-  for (int k = max(0, pos_copies - kPosSlots); k < pos_copies; ++k) mbar_wait(x.pos_full(k % kPosSlots), (k / kPosSlots) & 1);
 }
 
 // The warp that issues a half's products (one elected lane does; the whole warp goes along): the next scores
@@ -202,12 +195,12 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
   const uint32_t id_s = tc_idesc(false, T, false), id_o = tc_idesc(false, D, true);
   const uint64_t q = tc_desc(base + half * L::kQ, 16);
   for (bool ok = true; ok;) {
-    if (!x.wait(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) break;
-    const ChunkSegment& sg = x.seg(segs % kSpanSlots);
+    if (!x.wait(x.seg_full(segs % kRunSlots), (segs / kRunSlots) & 1)) break;
+    const ChunkSegment& sg = x.seg(segs % kRunSlots);
     const int n = __shfl_sync(0xffffffffu, sg.tiles, 0);
     const bool turns = __shfl_sync(0xffffffffu, sg.rows, 0) <= kHalfRows;  // the halves take the tiles in turn
     __syncwarp();
-    if (elected()) mbar_arrive(x.seg_empty(segs % kSpanSlots));
+    if (elected()) mbar_arrive(x.seg_empty(segs % kRunSlots));
     ++segs;
     if (n == 0) break;
     const int step = turns ? 2 : 1, first = turns ? half : 0;
@@ -257,16 +250,6 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
   mbar_wait(x.drained(half), 0);
 }
 
-// How many of T ascending positions are below v.
-template <int T>
-__device__ __forceinline__ int below(const int32_t* pos, int v) {
-  int n = 0;
-#pragma unroll
-  for (int step = 128; step > 0; step >>= 1)
-    if (n + step <= T && pos[n + step - 1] < v) n += step;
-  return n;
-}
-
 // The 32 of bits 0 .. n-1 that lie in word w.
 __device__ __forceinline__ uint32_t bits_below(int n, int w) {
   const int k = n - 32 * w;
@@ -281,170 +264,230 @@ __device__ __forceinline__ void hide(uint32_t (&s)[N], const uint32_t (&seen)[W]
     if (!(seen[(FROM + j) / 32] >> ((FROM + j) % 32) & 1)) s[j] = 0xFF800000u;
 }
 
-// Weights into TMEM as binary16, two to a column.
+// Weights 2^(s f + shift) of a thread's scores as binary16, two to a word; returns their sum (in binary32).
 template <int N>
-__device__ __forceinline__ void put_weights(uint32_t col, const uint32_t (&s)[N]) {
+__device__ __forceinline__ float weights_of(const uint32_t (&s)[N], uint32_t (&p)[N / 2], float f, float shift) {
+  uint64_t sum[2] = {0, 0}, ff, hh;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(ff) : "f"(f));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(hh) : "f"(shift));
 #pragma unroll
-  for (int c = 0; c < N / 2; c += 8) {
-    uint32_t p[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) p[k] = pack16(false, __uint_as_float(s[2 * (c + k)]), __uint_as_float(s[2 * (c + k) + 1]));
-    tmem_st(col + c, p);
+  for (int i = 0; i < N; i += 2) {
+    uint64_t x;
+    float x0, x1;
+    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %4;\n}" : "=l"(x) : "r"(s[i]), "r"(s[i + 1]), "l"(ff), "l"(hh));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x));
+    x0 = exp2_approx(x0);
+    x1 = exp2_approx(x1);
+    asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n add.rn.f32x2 %0, %0, t;\n}" : "+l"(sum[i / 2 % 2]) : "f"(x0), "f"(x1));
+    p[i / 2] = pack16(false, x0, x1);
   }
+  float a, b, c, d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(sum[0]));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(c), "=f"(d) : "l"(sum[1]));
+  return (a + b) + (c + d);
+}
+
+// Words into TMEM, in as few stores as may be.
+template <int N, int FROM = 0>
+__device__ __forceinline__ void put_words(uint32_t col, const uint32_t (&p)[N]) {
+  constexpr int W = N - FROM >= 32 ? 32 : N - FROM >= 16 ? 16 : 8;
+  uint32_t x[W];
+#pragma unroll
+  for (int k = 0; k < W; ++k) x[k] = p[FROM + k];
+  tmem_st(col + FROM, x);
+  if constexpr (FROM + W < N) put_words<N, FROM + W>(col, p);
 }
 
 // The softmax warps of a half, a thread a row.
+//
+// A row's reference m only has to keep its weights within binary16, and its first tile's maximum does for most of the
+// tiles that follow: their weights are taken by it at once, without a maximum of their own, and a sum above 2^15 tells
+// that the reference has to move.
 template <int D>
 __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx<D>& x, int half, int quad, int lane) {
   using L = ChunkSmem<D>;
   using C = ChunkCtx<D>;
-  constexpr int T = L::kT;
-  const int row = quad * 32 + lane;
+  constexpr int T = L::kT, A = C::kPartA, B = C::kPartB;
+  constexpr float kMost = 32768.f;
+  const int row = quad * 32 + lane, heads = g.a.Hq / g.a.Hkv;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
-  float* const exchange = reinterpret_cast<float*>(x.base + L::kQ);  // the second half's Q: 32 columns of 128 rows
+  float* const exchange = reinterpret_cast<float*>(x.base + L::kExchange);
   float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
-  int segs = 0, masked = 0, it = 0, joins = 0;  // masked: tiles of the CTA that came with positions
-  for (;;) {
-    if (!x.wait(x.seg_full(segs % kSpanSlots), (segs / kSpanSlots) & 1)) return;
-    const ChunkSegment sg = x.seg(segs % kSpanSlots);
-    __syncwarp();
-    if (lane == 0) mbar_arrive(x.seg_empty(segs % kSpanSlots));
-    ++segs;
-    if (sg.tiles == 0) return;
-    const bool turns = sg.rows <= kHalfRows;  // the halves have the same rows and take the tiles in turn
-    const int first_row = turns ? 0 : half * kHalfRows;
-    const BlockPlan& p = g.block[sg.block];
-    const bool local = p.local, mine = first_row + row < sg.rows;
-    RowSource src = {};
-    src.t = INT_MAX - 1;  // (a lane without a row sees every token, so that its warp need not hide any for it)
-    float f = 0.f;
-    // The row's query into shared memory as binary16, scaled by the power of two that brings its largest
-    // element to [1, 2).  (The last segment's scores are all in.)
-    if (!turns || half < sg.tiles) {
-      uint4 w[D / 8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) w[i] = make_uint4(0, 0, 0, 0);
-      if (mine) {
-        src = row_source(g, g.chunk[p.chunk], p.query0, local, sg.kvh, p.row + first_row + row);
-        const uint4* q = reinterpret_cast<const uint4*>(g.q + (static_cast<int64_t>(src.query) * g.a.Hq + src.head) * D);
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) w[i] = q[i];
-      }
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) top = max(top, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
-      }
-      int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
-      e = max(-100, min(120, e));
-      const float down = __int_as_float((127 - e) << 23);
-      f = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
-      uint8_t* to = x.base + half * L::kQ;
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-        uint32_t o[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = pack16(false, bf16lo(v[k]) * down, bf16hi(v[k]) * down);
-        *reinterpret_cast<uint4*>(to + tile_at(kHalfRows, row, i)) = make_uint4(o[0], o[1], o[2], o[3]);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(x.q_full(half));
+  int segs = 0, it = 0, joins = 0;
+  int64_t at = 0, next_at = 0;  // of the row in q and out
+  int lo = 0, hi = 0, next_lo = 0, next_hi = 0;
+  bool mine = false, next_mine = false;
+  float f = 0.f;
+  // Which row of a run is this thread's, where it is and what it sees.  (A lane without a row sees every token.)
+  auto find_row = [&](const ChunkSegment& s) {
+    const int r = (s.rows <= kHalfRows ? 0 : half * kHalfRows) + row;
+    next_mine = r < s.rows;
+    next_lo = 0;
+    next_hi = INT_MAX;
+    next_at = 0;
+    if (next_mine) {
+      const int k = s.query0 + (s.row + r) / heads, h = s.kvh * heads + (s.row + r) % heads;
+      const int2 see = g.sight[k];
+      next_lo = see.x;
+      next_hi = see.y;
+      next_at = static_cast<int64_t>(g.list[k]) * g.a.Hq + h;
     }
-    float m = -INFINITY, l = 0.f;
-    int mine_done = 0;  // tiles of this half
-    bool ready = false;  // the next scores are there
-    for (int i = 0; i < sg.tiles; ++i) {
-      const bool all = i >= sg.clean && i < sg.clean_end, other_half = turns && (i & 1) != half;
-      uint32_t seen[(T + 31) / 32];
-      if (!all) {
-        const int slot = masked % kPosSlots;
-        if (!x.wait(x.pos_full(slot), (masked / kPosSlots) & 1)) return;
-        ++masked;
-        if (!other_half) {
-          const int32_t* pos = x.pos(slot);
-          const int c = below<T>(pos, src.t + 1), from = pos[0] >= src.lo ? 0 : below<T>(pos, src.lo), head = local && from > 0 ? below<T>(pos, g.sinks) : 0;
+  };
+  // The row's query into shared memory as binary16, scaled by the power of two that brings its largest element to [1, 2).
+  auto put_q = [&](const uint4 (&w)[D / 8]) {
+    uint32_t top = 0;
 #pragma unroll
-          for (int w = 0; w < (T + 31) / 32; ++w) seen[w] = bits_below(c, w) & (~bits_below(from, w) | bits_below(head, w));
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(x.pos_empty(slot));
-      }
-      if (other_half) continue;
+    for (int i = 0; i < D / 8; ++i) {
+      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = max(top, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
+    }
+    int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
+    e = max(-100, min(120, e));
+    const float down = __int_as_float((127 - e) << 23);
+    uint8_t* to = x.base + half * L::kQ;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = pack16(false, bf16lo(v[k]) * down, bf16hi(v[k]) * down);
+      *reinterpret_cast<uint4*>(to + tile_at(kHalfRows, row, i)) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(x.q_full(half));
+    return fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
+  };
+  auto get_q = [&](uint4 (&w)[D / 8]) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) w[i] = next_mine ? reinterpret_cast<const uint4*>(g.q + next_at * D)[i] : make_uint4(0, 0, 0, 0);
+  };
+  // whether this half has a tile of a run
+  auto takes = [&](const ChunkSegment& s) { return s.tiles > (s.rows <= kHalfRows ? half : 0); };
+
+  if (!x.wait(x.seg_full(0), 0)) return;
+  if (x.seg(0).tiles > 0) find_row(x.seg(0));
+  if (takes(x.seg(0))) {
+    uint4 w[D / 8];
+    get_q(w);
+    f = put_q(w);
+  }
+  for (;; ++segs) {
+    const ChunkSegment& sg = x.seg(segs % kRunSlots);
+    const int tiles = sg.tiles, clean = sg.clean, clean_end = sg.clean_end, dest = sg.dest;
+    if (tiles == 0) return;
+    const bool turns = sg.rows <= kHalfRows;  // the halves have the same rows and take the tiles in turn
+    const int step = turns ? 2 : 1, first = turns ? half : 0, first_row = turns ? 0 : half * kHalfRows;
+    at = next_at, lo = next_lo, hi = next_hi, mine = next_mine;
+    float m = -INFINITY, l = 0.f, next_f = 0.f;
+    bool ready = false;  // the next scores are there
+    for (int i = first; i < tiles; i += step, ++it) {
       if (!ready && !x.wait(x.s_full(half), it & 1)) return;
       tc_fence_after();
-      uint32_t a[C::kPartA], b[C::kPartB];
+      uint32_t a[A], b[B];
       tmem_ld(a, b, col_s);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(x.s_read(half));  // the next scores may come
-      if (!all) {
+      if (i < clean || i >= clean_end) {  // not every row sees the whole tile
+        const int s = sg.from + i, before = (s + (s < sg.head ? 0 : sg.skip)) * T;
+        uint32_t seen[(T + 31) / 32];
+#pragma unroll
+        for (int w = 0; w < (T + 31) / 32; ++w)
+          seen[w] = bits_below(hi - before, w) & (~bits_below(lo - before, w) | (sg.local ? bits_below(sg.sinks - before, w) : 0u));
         hide<0>(a, seen);
-        hide<C::kPartA>(b, seen);
+        hide<A>(b, seen);
       }
-      const float top = fmaxf(highest(a), highest(b)) * f;
-      // m follows the maximum only when that has grown by more than 2^8: p stays within binary16, and O is rarely rescaled
-      if (__any_sync(0xffffffffu, top > m + 8.f)) {
-        const float next = fmaxf(m, top), by = m == -INFINITY ? 0.f : exp2_approx(m - next);
+      // the reference moves up to `top`, in whole steps of the exponent (so that weights can follow); O with it
+      auto move = [&](float top) -> bool {
+        const float next = top > m ? (m == -INFINITY ? top : m + ceilf(top - m)) : m;
+        const float by = m == -INFINITY ? 0.f : exp2_approx(m - next);
         l *= by;
         m = next;
-        if (mine_done > 0) {
-          if (!x.wait(x.o_done(half), (it - 1) & 1)) return;
-          tc_fence_after();
+        if (i == first) return true;
+        if (!x.wait(x.o_done(half), (it - 1) & 1)) return false;
+        tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < D / 16; ++c) {
-            uint32_t o[16];
-            tmem_ld(o, col_o + 16 * c);
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t o[16];
+          tmem_ld(o, col_o + 16 * c);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
-            tmem_st(col_o + 16 * c, o);
-          }
+          for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+          tmem_st(col_o + 16 * c, o);
         }
-      }
-      const float shift = m == -INFINITY ? 0.f : -m;
+        return true;
+      };
+      if (__any_sync(0xffffffffu, m == -INFINITY) && !move(fmaxf(highest(a), highest(b)) * f)) return;
+      auto shift = [&] { return m == -INFINITY ? 0.f : -m; };
       // (asked for before the exponentials, which hide how long the answer takes)
       const bool used = it == 0 || x.there(x.o_done(half), (it - 1) & 1);
-      l += weigh(a, f, shift);
-      l += weigh(b, f, shift);
+      uint32_t pa[A / 2], pb[B / 2];
+      float sum = weights_of(a, pa, f, shift());
+      if (__any_sync(0xffffffffu, sum > kMost)) {
+        if (!move(fmaxf(highest(a), highest(b)) * f)) return;
+        sum = weights_of(a, pa, f, shift());
+      }
       if (!__all_sync(0xffffffffu, used) && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
       tc_fence_after();
-      put_weights(col_p, a);
-      put_weights(col_p + C::kPartA / 2, b);
+      put_words(col_p, pa);
+      float more = weights_of(b, pb, f, shift());
+      if (__any_sync(0xffffffffu, more > kMost)) {
+        const float was = m;
+        if (!move(highest(b) * f)) return;
+        const float by = was == -INFINITY ? 0.f : exp2_approx(was - m);
+        const __half2 by2 = __float2half2_rn(by);
+        sum *= by;
+#pragma unroll
+        for (int k = 0; k < A / 2; ++k) pa[k] = as_u32(__hmul2(as_half2(pa[k]), by2));
+        put_words(col_p, pa);
+        more = weights_of(b, pb, f, shift());
+      }
+      put_words(col_p + A / 2, pb);
+      l += sum + more;
       const bool next = x.there(x.s_full(half), (it + 1) & 1);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(x.p_full(half));
       ready = __all_sync(0xffffffffu, next);
-      ++it;
-      ++mine_done;
+    }
+    const bool some = first < tiles;
+    // the next run's rows, while this one's last product runs
+    if (!x.wait(x.seg_full((segs + 1) % kRunSlots), ((segs + 1) / kRunSlots) & 1)) return;
+    const ChunkSegment& next = x.seg((segs + 1) % kRunSlots);
+    if (next.tiles > 0) find_row(next);
+    if (takes(next)) {  // (this run's scores are all in: Q's place is free)
+      uint4 w[D / 8];
+      get_q(w);
+      next_f = put_q(w);
     }
     // rows out: the output itself, or (m, l, o) for the join of pieces
-    if (mine_done > 0) {
+    if (some) {
       if (!x.wait(x.o_done(half), (it - 1) & 1)) return;
       tc_fence_after();
     }
+    f = next_f;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(x.seg_empty(segs % kRunSlots));
     if (turns && half == 1) {  // to the first half, 32 columns at a time
+      if (joins > 0 && !x.wait(x.join_empty(), (joins - 1) & 1)) return;
       exchange_ml[row] = make_float2(m, l);
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c, ++joins) {
         uint32_t o[32];
-        if (mine_done > 0) tmem_ld(o, col_o + 32 * c);
-        if (joins > 0 && !x.wait(x.join_empty(), (joins - 1) & 1)) return;
+        if (some) tmem_ld(o, col_o + 32 * c);
+        if (c > 0 && !x.wait(x.join_empty(), (joins - 1) & 1)) return;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) exchange[k * kHalfRows + row] = mine_done > 0 ? __uint_as_float(o[k]) : 0.f;
+        for (int k = 0; k < 32; ++k) exchange[k * kHalfRows + row] = some ? __uint_as_float(o[k]) : 0.f;
         __syncwarp();
         if (lane == 0) mbar_arrive(x.join_full());
       }
-      if (!x.wait(x.join_empty(), (joins - 1) & 1)) return;  // Q's place is free again
       tc_fence_before();
       continue;
     }
-    const int64_t at = static_cast<int64_t>(src.query) * g.a.Hq + src.head, slot = static_cast<int64_t>(sg.dest) * kBlockRows + first_row + row;
+    const int64_t slot = static_cast<int64_t>(dest) * kBlockRows + first_row + row;
     float by = 1.f, other = 0.f, inv = 0.f;  // weights of the halves' sums
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -468,20 +511,21 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       }
       if (c == 0) {
         inv = l != 0.f ? 1.f / l : 0.f;
-        if (mine && sg.dest >= 0) g.part_ml[slot] = make_float2(m, l);
-        if (mine && sg.dest < 0 && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (mine && dest >= 0) g.part_ml[slot] = make_float2(m, l);
+        if (mine && dest < 0 && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
       if (!mine) continue;
-      if (sg.dest >= 0) {
+      if (dest >= 0) {
 #pragma unroll
         for (int k = 0; k < 32; k += 8) st_global8(g.part_o + slot * D + 32 * c + k, reinterpret_cast<const float*>(o + k));
       } else {
 #pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-          uint32_t v[4];
+        for (int k = 0; k < 32; k += 16) {
+          uint32_t v[8];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = pack16(true, __uint_as_float(o[k + 2 * u]) * inv, __uint_as_float(o[k + 2 * u + 1]) * inv);
+          for (int u = 0; u < 8; ++u) v[u] = pack16(true, __uint_as_float(o[k + 2 * u]) * inv, __uint_as_float(o[k + 2 * u + 1]) * inv);
           *reinterpret_cast<uint4*>(g.out + at * D + 32 * c + k) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4*>(g.out + at * D + 32 * c + k + 8) = make_uint4(v[4], v[5], v[6], v[7]);
         }
       }
     }
@@ -503,8 +547,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
-    for (int i = 0; i < kPosSlots; ++i) mbar_init(x.pos_full(i), 1), mbar_init(x.pos_empty(i), kChunkSoftmaxWarps);
-    for (int i = 0; i < kSpanSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
+    for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
     for (int h = 0; h < 2; ++h) {
       mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
       mbar_init(x.p_full(h), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);

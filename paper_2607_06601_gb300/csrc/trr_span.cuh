@@ -47,6 +47,28 @@ __device__ __forceinline__ Place place_of(const LayerArgs& a, int seq, int c, in
   return Place{k * a.P + l, l < n && pos[l] == p ? page : -1, l};
 }
 
+// The same count by a whole warp, 32 probes at a time: for a position that others wait for.
+__device__ __forceinline__ int tokens_before(const LayerArgs& a, int seq, int c, int p, int lane) {
+  const int64_t row = static_cast<int64_t>(seq) * kClasses + c;
+  const int nt = a.ntok[row];
+  const int32_t* first = a.pfirst + row * a.MP;
+  int lo = 0, hi = (nt + a.P - 1) / a.P;
+  while (lo < hi) {  // pages whose first token is before p
+    const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+    const int k = __popc(__ballot_sync(0xffffffffu, i < hi && first[i] < p));
+    if (k == 0) break;
+    const int last = lo + (k - 1) * step;
+    hi = min(hi, last + step);
+    lo = last + 1;
+  }
+  if (lo == 0) return 0;
+  const int k = lo - 1, n = min(a.P, nt - k * a.P);
+  const int32_t* pos = reinterpret_cast<const int32_t*>(a.pool[c] + a.pt[row * a.MP + k] * a.page_bytes[c]);
+  int below = 0;
+  for (int s = 0; s < n; s += 32) below += __popc(__ballot_sync(0xffffffffu, s + lane < n && pos[s + lane] < p));
+  return k * a.P + below;
+}
+
 // Tokens that a CTA has found, class by class, in order; class kClasses: positions that store nothing.  ROWS of a
 // class's, at most, form a group, which a warp takes together.
 template <int ROWS>

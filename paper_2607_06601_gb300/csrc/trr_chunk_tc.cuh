@@ -382,15 +382,15 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     const int step = turns ? 2 : 1, first = turns ? half : 0, first_row = turns ? 0 : half * kHalfRows;
     at = next_at, lo = next_lo, hi = next_hi, mine = next_mine;
     float m = -INFINITY, l = 0.f, next_f = 0.f;
-    bool ready = false;  // the next scores are there
+    bool ready = false;    // the next scores are there
+    bool settled = false;  // every row of the warp has a reference
     for (int i = first; i < tiles; i += step, ++it) {
       if (!ready && !x.wait(x.s_full(half), it & 1)) return;
       tc_fence_after();
       uint32_t a[A], b[B];
       tmem_ld(a, b, col_s);
       tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(x.s_read(half));  // the next scores may come
+      mbar_arrive(x.s_read(half));  // the next scores may come (every thread says so: one for all would cost 100 cycles)
       if (i < clean || i >= clean_end) {  // not every row sees the whole tile
         const int s = sg.from + i, before = (s + (s < sg.head ? 0 : sg.skip)) * T;
         uint32_t seen[(T + 31) / 32];
@@ -419,17 +419,22 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         }
         return true;
       };
-      if (__any_sync(0xffffffffu, m == -INFINITY) && !move(fmaxf(highest(a), highest(b)) * f)) return;
+      if (!settled) {
+        if (!move(fmaxf(highest(a), highest(b)) * f)) return;
+        settled = __all_sync(0xffffffffu, m != -INFINITY);
+      }
       auto shift = [&] { return m == -INFINITY ? 0.f : -m; };
       // (asked for before the exponentials, which hide how long the answer takes)
       const bool used = it == 0 || x.there(x.o_done(half), (it - 1) & 1);
       uint32_t pa[A / 2], pb[B / 2];
       float sum = weights_of(a, pa, f, shift());
-      if (__any_sync(0xffffffffu, sum > kMost)) {
-        if (!move(fmaxf(highest(a), highest(b)) * f)) return;
-        sum = weights_of(a, pa, f, shift());
+      if (__any_sync(0xffffffffu, sum > kMost || !used)) {
+        if (it > 0 && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
+        if (__any_sync(0xffffffffu, sum > kMost)) {
+          if (!move(fmaxf(highest(a), highest(b)) * f)) return;
+          sum = weights_of(a, pa, f, shift());
+        }
       }
-      if (!__all_sync(0xffffffffu, used) && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
       tc_fence_after();
       put_words(col_p, pa);
       float more = weights_of(b, pb, f, shift());
@@ -449,8 +454,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       const bool next = x.there(x.s_full(half), (it + 1) & 1);
       tmem_wait_st();
       tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(x.p_full(half));
+      mbar_arrive(x.p_full(half));
       ready = __all_sync(0xffffffffu, next);
     }
     const bool some = first < tiles;
@@ -549,8 +553,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
     for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
     for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
     for (int h = 0; h < 2; ++h) {
-      mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
-      mbar_init(x.p_full(h), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
+      mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), kHalfRows);
+      mbar_init(x.p_full(h), kHalfRows), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
     }
     mbar_init(x.join_full(), 4), mbar_init(x.join_empty(), 4);
     fence_barrier_init();

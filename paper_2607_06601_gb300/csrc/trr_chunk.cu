@@ -304,6 +304,10 @@ __device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) 
   p.last = max(p.first, (rank2 + T - 1) / T);
   if (p.head >= p.first) p.head = p.first = 0;  // one stretch from the start
   p.tiles = p.head + p.last - p.first;
+  if (p.tiles > 0) {
+    const int whole = max(0, min(p.clean_end, p.last) - max(p.clean, p.first));
+    p.tile_cost = kChunkTileCost + (kChunkMaskedCost * (p.tiles - whole) + p.tiles / 2) / p.tiles;
+  }
   if (lane == 0) g.block[b] = p;
 }
 
@@ -383,9 +387,13 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     int64_t work = 0;
     for (int x0 = 0; x0 < head.blocks; x0 += kSpanThreads) {
       const int x = x0 + tid;
-      const int tiles = x < head.blocks ? reinterpret_cast<const volatile BlockPlan*>(g.block)[x].tiles : 0;
+      BlockPlan b = {};
+      if (x < head.blocks) {
+        b.tiles = reinterpret_cast<const volatile BlockPlan*>(g.block)[x].tiles;
+        b.tile_cost = reinterpret_cast<const volatile BlockPlan*>(g.block)[x].tile_cost;
+      }
       int64_t all;
-      const int64_t before = work + scan_before(a.Hkv * chunk_cost(tiles), s_sums, &all);
+      const int64_t before = work + scan_before(a.Hkv * chunk_cost(b), s_sums, &all);
       work += all;
       if (x < head.blocks) g.base[x] = before;
     }
@@ -539,11 +547,11 @@ __device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& ch,
 template <int D>
 __device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const PieceInfo& piece, const BlockPlan& b, int r, int lane) {
   constexpr int E = D / 8;
-  const int64_t cost = chunk_cost(b.tiles), S = g.base[piece.block] + piece.kvh * cost, per = g.head->per;
+  const int64_t cost = chunk_cost(b), S = g.base[piece.block] + piece.kvh * cost, per = g.head->per;
   // parts: the last one of CTA `cta`, the first ones of those that follow
   auto slot = [&](int j) { return static_cast<int64_t>(2 * j + (j == cta)) * kBlockRows + r; };
   int end = cta + 1;
-  while (end < g.ctas && chunk_tiles_before(end * per - S, b.tiles) < b.tiles) ++end;
+  while (end < g.ctas && chunk_tiles_before(end * per - S, b) < b.tiles) ++end;
   float m = -INFINITY, l = 0.f, o[E] = {};
 #pragma unroll 4
   for (int j = cta; j < end; ++j) m = fmaxf(m, g.part_ml[slot(j)].x);

@@ -37,7 +37,8 @@ struct BlockPlan {
   int head, first, last, tiles;
   int clean, clean_end;
   int query0;                   // the mode's first query in the list
-  int pad[5];
+  int tile_cost;
+  int pad[4];
 };
 static_assert(sizeof(BlockPlan) == 64, "");
 
@@ -100,13 +101,20 @@ __device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkP
   return r;
 }
 
-// The cost of a segment: its tiles, and a fixed part for its start and end and for the tiles that not every row sees
-// whole.  With a fixed part of one tile instead of five, 4096 queries on themselves, 32 heads of 64, took 202 us
-// against 150, as the CTAs with the shortest segments came in last.
-constexpr int kChunkTileCost = 2, kChunkSegmentCost = 10;
-constexpr int kChunkLeastShare = 6;  // of a CTA: three tiles
-__device__ __forceinline__ int64_t chunk_cost(int tiles) {
-  return tiles > 0 ? kChunkSegmentCost + static_cast<int64_t>(kChunkTileCost) * tiles : 0;
+// The cost of a segment: its tiles, those dearer that not every row sees whole, and a fixed part for its start and end
+// (in eighths of a tile's 2100 cycles at d 64; measured 3600 for a tile with rows hidden, 8000 for a segment, before
+// both were cut).  With every tile alike and a fixed part of one tile, 4096 queries on themselves, 32 heads of 64, took
+// 202 us against 150 with one of five, as the CTAs with the shortest segments came in last.
+constexpr int kChunkTileCost = 8, kChunkMaskedCost = 4, kChunkSegmentCost = 30;
+constexpr int kChunkLeastShare = 24;  // of a CTA: three tiles
+__device__ __forceinline__ int64_t chunk_cost(const BlockPlan& b) {
+  return b.tiles > 0 ? kChunkSegmentCost + static_cast<int64_t>(b.tile_cost) * b.tiles : 0;
+}
+// Tiles of a segment that lie before cost x (counted from the segment's start).
+__device__ __forceinline__ int chunk_tiles_before(int64_t x, const BlockPlan& b) {
+  if (x <= kChunkSegmentCost) return 0;
+  const int64_t t = (x - kChunkSegmentCost + b.tile_cost - 1) / b.tile_cost;
+  return t < b.tiles ? static_cast<int>(t) : b.tiles;
 }
 
 }  // namespace trr

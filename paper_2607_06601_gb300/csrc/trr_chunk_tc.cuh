@@ -18,7 +18,7 @@
 
 namespace trr {
 
-constexpr int kChunkSoftmaxWarps = 8, kChunkProducer = 8, kChunkMma = 9;  // warps 9 and 10
+constexpr int kChunkSoftmaxWarps = 8, kChunkProducer = 8, kChunkMma = 9, kChunkFinder = 11;  // products: warps 9 and 10
 constexpr int kChunkThreads = 384;
 // Registers a thread: 168 at launch; the softmax warpgroups take what the third gives up.
 constexpr int kChunkLaunchRegisters = 168, kChunkSoftmaxRegisters = 208, kChunkOtherRegisters = 88;
@@ -37,6 +37,11 @@ struct ChunkSegment {
   int pad[2];
 };
 
+// A row of a run: its place among all (query, head), and which of the chunk's staged tokens it sees, lo .. hi - 1.
+struct ChunkRow {
+  int at, lo, hi;  // at < 0: no row
+};
+
 template <int D>
 struct ChunkSmem {
   static constexpr int kT = chunk_tile(D);
@@ -47,9 +52,10 @@ struct ChunkSmem {
   static constexpr int kV = kK + kSlots * kTile;
   static constexpr int kExchange = kV + kSlots * kTile;  // 32 columns of the second half's rows, and (m, l), for a join
   static constexpr int kMl = kExchange + 32 * kHalfRows * 4;
-  static constexpr int kSeg = kMl + kHalfRows * 8;
+  static constexpr int kRows = kMl + kHalfRows * 8;
+  static constexpr int kSeg = kRows + kRunSlots * kBlockRows * static_cast<int>(sizeof(ChunkRow));
   static constexpr int kBars = kSeg + kRunSlots * static_cast<int>(sizeof(ChunkSegment));
-  static constexpr int kNumBars = 2 * kSlots + 2 * kRunSlots + 2 * 6 + 2;
+  static constexpr int kNumBars = 2 * kSlots + 3 * kRunSlots + 2 * 6 + 2;
   static constexpr int kTotal = kBars + 8 * kNumBars;
   static_assert(kTotal + 1024 + 64 <= 227 * 1024, "");
   static_assert(kTile % 1024 == 0, "");
@@ -69,7 +75,8 @@ struct ChunkCtx {
   __device__ uint64_t* kv_empty(int i) const { return bar(L::kSlots + i); }
   __device__ uint64_t* seg_full(int i) const { return bar(2 * L::kSlots + i); }
   __device__ uint64_t* seg_empty(int i) const { return bar(2 * L::kSlots + kRunSlots + i); }
-  __device__ uint64_t* half_bar(int half, int i) const { return bar(2 * L::kSlots + 2 * kRunSlots + 6 * half + i); }
+  __device__ uint64_t* rows_full(int i) const { return bar(2 * L::kSlots + 2 * kRunSlots + i); }
+  __device__ uint64_t* half_bar(int half, int i) const { return bar(2 * L::kSlots + 3 * kRunSlots + 6 * half + i); }
   __device__ uint64_t* q_full(int half) const { return half_bar(half, 0); }
   __device__ uint64_t* s_full(int half) const { return half_bar(half, 1); }
   __device__ uint64_t* s_read(int half) const { return half_bar(half, 2); }
@@ -79,6 +86,7 @@ struct ChunkCtx {
   __device__ uint64_t* join_full() const { return half_bar(2, 0); }
   __device__ uint64_t* join_empty() const { return half_bar(2, 1); }
   __device__ ChunkSegment& seg(int i) const { return reinterpret_cast<ChunkSegment*>(base + L::kSeg)[i]; }
+  __device__ ChunkRow* rows(int i) const { return reinterpret_cast<ChunkRow*>(base + L::kRows) + i * kBlockRows; }
   // TMEM columns: scores, weights (two to a column), sums
   __device__ uint32_t col_s(int half) const { return tmem + kT * half; }
   __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 256 + 64 * half : 160 + 48 * half); }
@@ -99,13 +107,6 @@ struct ChunkCtx {
     return true;
   }
 };
-
-// Tiles of a segment that lie before cost x (counted from the segment's start).
-__device__ __forceinline__ int chunk_tiles_before(int64_t x, int tiles) {
-  if (x <= kChunkSegmentCost) return 0;
-  const int64_t t = (x - kChunkSegmentCost + kChunkTileCost - 1) / kChunkTileCost;
-  return t < tiles ? static_cast<int>(t) : tiles;
-}
 
 // The producer warp: the runs of this CTA's share, and the copies of their tiles.
 template <int D>
@@ -155,11 +156,11 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
       const BlockPlan p = g.block[b];
       if (p.tiles == 0) continue;
       const int tile0 = g.chunk[p.chunk].tile0, sinks = g.chunk[p.chunk].head;
-      const int64_t cost = chunk_cost(p.tiles);
+      const int64_t cost = chunk_cost(p);
       for (int h = static_cast<int>(max(static_cast<int64_t>(0), (b0 - start) / cost)); h < g.a.Hkv && ok; ++h) {
         const int64_t S = start + h * cost;
         if (S >= b1) break;
-        const int t0 = chunk_tiles_before(b0 - S, p.tiles), t1 = chunk_tiles_before(b1 - S, p.tiles);
+        const int t0 = chunk_tiles_before(b0 - S, p), t1 = chunk_tiles_before(b1 - S, p);
         if (t0 >= t1) continue;
         if (t0 == 0 && t1 < p.tiles) piece = PieceInfo{b, h, 0, 0};
         ChunkSegment s = {};
@@ -181,6 +182,38 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   copy();
   // the CTA stays until its copies have landed
   for (int k = max(0, copies - L::kSlots); k < copies; ++k) mbar_wait(x.kv_full(k % L::kSlots), (k / L::kSlots) & 1);
+}
+
+// The warp that finds the rows of each run as it is announced, and brings their queries to L1: two chains of loads that
+// the softmax warps would wait for.
+template <int D>
+__device__ __forceinline__ void chunk_find_rows(const ChunkArgs& g, const ChunkCtx<D>& x, int lane) {
+  const int heads = g.a.Hq / g.a.Hkv;
+  for (int segs = 0;; ++segs) {
+    const int slot = segs % kRunSlots;
+    if (!x.wait(x.seg_full(slot), (segs / kRunSlots) & 1)) return;
+    const ChunkSegment& s = x.seg(slot);
+    const int rows = s.rows, tiles = s.tiles, query0 = s.query0, row0 = s.row, head0 = s.kvh * heads;
+    if (tiles == 0) return;
+#pragma unroll 4
+    for (int r = lane; r < kBlockRows; r += 32) {
+      ChunkRow row = {-1, 0, INT_MAX};  // (a lane without a row sees every token)
+      if (r < rows) {
+        const int k = query0 + (row0 + r) / heads;
+        const int2 sight = g.sight[k];
+        row = ChunkRow{g.list[k] * g.a.Hq + head0 + (row0 + r) % heads, sight.x, sight.y};
+        const uint16_t* q = g.q + static_cast<int64_t>(row.at) * D;
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(q));
+        if (D == 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(q + 64));
+      }
+      x.rows(slot)[r] = row;
+    }
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(x.rows_full(slot));
+      mbar_arrive(x.seg_empty(slot));
+    }
+  }
 }
 
 // The warp that issues a half's products (one elected lane does; the whole warp goes along): the next scores
@@ -256,12 +289,18 @@ __device__ __forceinline__ uint32_t bits_below(int n, int w) {
   return k <= 0 ? 0u : k >= 32 ? 0xffffffffu : (1u << k) - 1;
 }
 
-// Scores out of sight become -infinity; s holds tokens FROM .. FROM + N - 1, bit j of the words is token j's.
+// Scores out of sight become -infinity; s holds tokens FROM .. FROM + N - 1, bit j of the words is token j's.  Sixteen
+// at a time, where a row of the warp does not see them all.
 template <int FROM, int N, int W>
 __device__ __forceinline__ void hide(uint32_t (&s)[N], const uint32_t (&seen)[W]) {
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (!(seen[(FROM + j) / 32] >> ((FROM + j) % 32) & 1)) s[j] = 0xFF800000u;
+  for (int j0 = 0; j0 < N; j0 += 16) {
+    const uint32_t bits = seen[(FROM + j0) / 32] >> ((FROM + j0) % 32) & 0xFFFFu;
+    if (__all_sync(0xffffffffu, bits == 0xFFFFu)) continue;
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (!(bits >> j & 1)) s[j0 + j] = 0xFF800000u;
+  }
 }
 
 // Weights 2^(s f + shift) of a thread's scores as binary16, two to a word; returns their sum (in binary32).
@@ -309,31 +348,13 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   using C = ChunkCtx<D>;
   constexpr int T = L::kT, A = C::kPartA, B = C::kPartB;
   constexpr float kMost = 32768.f;
-  const int row = quad * 32 + lane, heads = g.a.Hq / g.a.Hkv;
+  const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
   float* const exchange = reinterpret_cast<float*>(x.base + L::kExchange);
   float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
   int segs = 0, it = 0, joins = 0;
-  int64_t at = 0, next_at = 0;  // of the row in q and out
-  int lo = 0, hi = 0, next_lo = 0, next_hi = 0;
-  bool mine = false, next_mine = false;
   float f = 0.f;
-  // Which row of a run is this thread's, where it is and what it sees.  (A lane without a row sees every token.)
-  auto find_row = [&](const ChunkSegment& s) {
-    const int r = (s.rows <= kHalfRows ? 0 : half * kHalfRows) + row;
-    next_mine = r < s.rows;
-    next_lo = 0;
-    next_hi = INT_MAX;
-    next_at = 0;
-    if (next_mine) {
-      const int k = s.query0 + (s.row + r) / heads, h = s.kvh * heads + (s.row + r) % heads;
-      const int2 see = g.sight[k];
-      next_lo = see.x;
-      next_hi = see.y;
-      next_at = static_cast<int64_t>(g.list[k]) * g.a.Hq + h;
-    }
-  };
   // The row's query into shared memory as binary16, scaled by the power of two that brings its largest element to [1, 2).
   auto put_q = [&](const uint4 (&w)[D / 8]) {
     uint32_t top = 0;
@@ -360,28 +381,29 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     if (lane == 0) mbar_arrive(x.q_full(half));
     return fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
   };
-  auto get_q = [&](uint4 (&w)[D / 8]) {
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) w[i] = next_mine ? reinterpret_cast<const uint4*>(g.q + next_at * D)[i] : make_uint4(0, 0, 0, 0);
-  };
-  // whether this half has a tile of a run
-  auto takes = [&](const ChunkSegment& s) { return s.tiles > (s.rows <= kHalfRows ? half : 0); };
-
-  if (!x.wait(x.seg_full(0), 0)) return;
-  if (x.seg(0).tiles > 0) find_row(x.seg(0));
-  if (takes(x.seg(0))) {
+  // The rows of run k into shared memory, if the half has a tile of it; the factor from products to base-2 exponents.
+  auto load_rows = [&](int k) -> bool {
+    const int slot = k % kRunSlots;
+    if (!x.wait(x.seg_full(slot), (k / kRunSlots) & 1)) return false;
+    const bool turns = x.seg(slot).rows <= kHalfRows;
+    if (x.seg(slot).tiles <= (turns ? half : 0)) return true;
+    if (!x.wait(x.rows_full(slot), (k / kRunSlots) & 1)) return false;
+    const int at = x.rows(slot)[(turns ? 0 : half * kHalfRows) + row].at;
     uint4 w[D / 8];
-    get_q(w);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) w[i] = at >= 0 ? reinterpret_cast<const uint4*>(g.q + static_cast<int64_t>(at) * D)[i] : make_uint4(0, 0, 0, 0);
     f = put_q(w);
-  }
+    return true;
+  };
+
+  if (!load_rows(0)) return;
   for (;; ++segs) {
     const ChunkSegment& sg = x.seg(segs % kRunSlots);
     const int tiles = sg.tiles, clean = sg.clean, clean_end = sg.clean_end, dest = sg.dest;
     if (tiles == 0) return;
     const bool turns = sg.rows <= kHalfRows;  // the halves have the same rows and take the tiles in turn
     const int step = turns ? 2 : 1, first = turns ? half : 0, first_row = turns ? 0 : half * kHalfRows;
-    at = next_at, lo = next_lo, hi = next_hi, mine = next_mine;
-    float m = -INFINITY, l = 0.f, next_f = 0.f;
+    float m = -INFINITY, l = 0.f;
     bool ready = false;    // the next scores are there
     bool settled = false;  // every row of the warp has a reference
     for (int i = first; i < tiles; i += step, ++it) {
@@ -393,10 +415,24 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       mbar_arrive(x.s_read(half));  // the next scores may come (every thread says so: one for all would cost 100 cycles)
       if (i < clean || i >= clean_end) {  // not every row sees the whole tile
         const int s = sg.from + i, before = (s + (s < sg.head ? 0 : sg.skip)) * T;
-        uint32_t seen[(T + 31) / 32];
+        const ChunkRow r = x.rows(segs % kRunSlots)[first_row + row];
+        const int hi = r.hi - before, lo = r.lo - before, sinks = sg.local ? sg.sinks - before : 0;
+        uint32_t seen[(T + 31) / 32], any = 0;
 #pragma unroll
-        for (int w = 0; w < (T + 31) / 32; ++w)
-          seen[w] = bits_below(hi - before, w) & (~bits_below(lo - before, w) | (sg.local ? bits_below(sg.sinks - before, w) : 0u));
+        for (int w = 0; w < (T + 31) / 32; ++w) {
+          seen[w] = bits_below(hi, w) & (~bits_below(lo, w) | bits_below(sinks, w));
+          any |= seen[w];
+        }
+        if (!__any_sync(0xffffffffu, any)) {  // none of the warp's rows sees any of it
+          if (it > 0 && !x.wait(x.o_done(half), (it - 1) & 1)) return;
+          const uint32_t none[T / 2] = {};
+          put_words(col_p, none);
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(x.p_full(half));
+          ready = false;
+          continue;
+        }
         hide<0>(a, seen);
         hide<A>(b, seen);
       }
@@ -458,21 +494,15 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       ready = __all_sync(0xffffffffu, next);
     }
     const bool some = first < tiles;
-    // the next run's rows, while this one's last product runs
-    if (!x.wait(x.seg_full((segs + 1) % kRunSlots), ((segs + 1) / kRunSlots) & 1)) return;
-    const ChunkSegment& next = x.seg((segs + 1) % kRunSlots);
-    if (next.tiles > 0) find_row(next);
-    if (takes(next)) {  // (this run's scores are all in: Q's place is free)
-      uint4 w[D / 8];
-      get_q(w);
-      next_f = put_q(w);
-    }
+    const int at = x.rows(segs % kRunSlots)[first_row + row].at;
+    const bool mine = at >= 0;
+    // the next run's rows, while this one's last product runs (its scores are all in: Q's place is free)
+    if (!load_rows(segs + 1)) return;
     // rows out: the output itself, or (m, l, o) for the join of pieces
     if (some) {
       if (!x.wait(x.o_done(half), (it - 1) & 1)) return;
       tc_fence_after();
     }
-    f = next_f;
     __syncwarp();
     if (lane == 0) mbar_arrive(x.seg_empty(segs % kRunSlots));
     if (turns && half == 1) {  // to the first half, 32 columns at a time
@@ -492,6 +522,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       continue;
     }
     const int64_t slot = static_cast<int64_t>(dest) * kBlockRows + first_row + row;
+    uint16_t* const out = g.out + static_cast<int64_t>(at) * D;
     float by = 1.f, other = 0.f, inv = 0.f;  // weights of the halves' sums
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -528,8 +559,8 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
           uint32_t v[8];
 #pragma unroll
           for (int u = 0; u < 8; ++u) v[u] = pack16(true, __uint_as_float(o[k + 2 * u]) * inv, __uint_as_float(o[k + 2 * u + 1]) * inv);
-          *reinterpret_cast<uint4*>(g.out + at * D + 32 * c + k) = make_uint4(v[0], v[1], v[2], v[3]);
-          *reinterpret_cast<uint4*>(g.out + at * D + 32 * c + k + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+          *reinterpret_cast<uint4*>(out + 32 * c + k) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4*>(out + 32 * c + k + 8) = make_uint4(v[4], v[5], v[6], v[7]);
         }
       }
     }
@@ -551,7 +582,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
-    for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 2);
+    for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 3), mbar_init(x.rows_full(i), 1);
     for (int h = 0; h < 2; ++h) {
       mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), kHalfRows);
       mbar_init(x.p_full(h), kHalfRows), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
@@ -576,7 +607,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   } else {
     registers_down<kChunkOtherRegisters>();
     if (warp == kChunkProducer) chunk_produce<D>(g, x, lane);
-    else if (warp < kChunkMma + 2) chunk_mma<D>(x, warp - kChunkMma);
+    else if (warp == kChunkFinder) chunk_find_rows<D>(g, x, lane);
+    else chunk_mma<D>(x, warp - kChunkMma);
   }
   __syncwarp();
   tc_fence_before();

@@ -31,13 +31,6 @@ constexpr int kStageCtas = 4;  // CTAs of the staging kernel on an SM
 
 // ------------------------------------------------------------------------------ plan --
 
-// Error of chunk i, 0 when it is valid (the offsets are).
-__device__ __forceinline__ int chunk_error(const ChunkArgs& g, int i) {
-  const int seq = g.seq_ids[i], start = g.starts[i], len = g.offsets[i + 1] - g.offsets[i];
-  if (seq < 0 || seq >= g.a.S) return TRR_ERR_INVALID_ARG;
-  return start < 0 || start > g.a.maxctx - len ? TRR_ERR_BAD_POSITION : 0;
-}
-
 // Errors of a call: the lowest failing query's, kept as INT_MAX - (16 query + error) so that 0 means none.
 __device__ __forceinline__ void chunk_fail(const ChunkArgs& g, int query, int err) {
   atomicMax(g.a.ctrl + kChunkBad, INT_MAX - (16 * query + err));
@@ -77,10 +70,11 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     if (o < 0 || o > g.num_tokens || next < o) s_bad = 1;
   }
   for (int h = tid; h < a.Hkv; h += kPlanChunkThreads) g.flag[static_cast<int64_t>(i) * a.Hkv + h] = 0;
+  const int begin = g.offsets[i], upto = g.offsets[i + 1], seq = g.seq_ids[i], start = g.starts[i];
   __syncthreads();
   const bool bad = s_bad;
-  const int row0 = bad ? 0 : g.offsets[i], len = bad ? 0 : g.offsets[i + 1] - row0;
-  const int seq = g.seq_ids[i], start = g.starts[i], err = bad ? TRR_ERR_INVALID_ARG : chunk_error(g, i);
+  const int row0 = bad ? 0 : begin, len = bad ? 0 : upto - begin;
+  const int err = bad ? TRR_ERR_INVALID_ARG : seq < 0 || seq >= a.S ? TRR_ERR_INVALID_ARG : start < 0 || start > a.maxctx - len ? TRR_ERR_BAD_POSITION : 0;
   if (tid == 0 && err && (bad || len > 0)) chunk_fail(g, row0, err);
   // a query's place: 0 full, 1 local, 2 a zero row
   auto kind_of = [&](int k, int* window) -> int {
@@ -200,9 +194,8 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     h.bad = whole;
     if (!whole) {
       h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units); h.tiles = static_cast<int>(tiles);
-      // a small call's heads are shared out among CTAs, so that staging fills the GPU
-      const int64_t most = (a.Hkv + 1) / 2;
-      h.splits = static_cast<int>(units > 0 ? max(static_cast<int64_t>(1), min(most, kStageCtas * g.ctas / units)) : 1);
+      const int stagers = kStageCtas * g.ctas;
+      h.splits = units > 0 ? shares_of(units, (a.Hkv + 1) / 2, stagers, copy_ns(5ll * a.Hkv * a.d, stagers)) : 1;
     }
     *g.head = h;
     const int e = atomicExch(a.ctrl + kChunkBad, 0);
@@ -583,8 +576,10 @@ __device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const Piec
   if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
+constexpr int kJoinCtas = 4;
+
 template <int D>
-__global__ void __launch_bounds__(256) chunk_join_kernel(const __grid_constant__ ChunkArgs g) {
+__global__ void __launch_bounds__(256, kJoinCtas) chunk_join_kernel(const __grid_constant__ ChunkArgs g) {
   constexpr int kJoinRows = 256 / 8;
   pdl_wait();
   pdl_trigger();

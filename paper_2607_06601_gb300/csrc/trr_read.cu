@@ -217,7 +217,7 @@ extern "C" trr_status trr_kv_read(trr_cache* cache, int32_t layer, int32_t n, co
   cache_set_launches(cache, 0);
   if (n == 0 || num_rows == 0) return TRR_OK;
   if (!seq_ids || !starts || !offsets || !k_out || !v_out) return TRR_ERR_INVALID_ARG;
-  const int64_t row = static_cast<int64_t>(l.Hkv) * l.d, unit = type == TRR_BF16 ? 8 : 4;
+  const int64_t row = static_cast<int64_t>(l.Hkv) * l.d, unit_bytes = type == TRR_BF16 ? 2 : 4, unit = 16 / unit_bytes;
   if (k_stride < row || v_stride < row || k_stride % unit || v_stride % unit) return TRR_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 15) return TRR_ERR_INVALID_ARG;
   ReadArgs g;
@@ -226,13 +226,12 @@ extern "C" trr_status trr_kv_read(trr_cache* cache, int32_t layer, int32_t n, co
   g.seq_ids = seq_ids; g.starts = starts; g.offsets = offsets;
   g.k = k_out; g.v = v_out; g.bits = bits_out;
   g.k_stride = k_stride; g.v_stride = v_stride;
-  const int64_t size = type == TRR_BF16 ? 2 : 4;
-  g.sectors = ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out) | static_cast<uint64_t>(k_stride * size) |
-                static_cast<uint64_t>(v_stride * size)) & 31) == 0;
+  g.sectors = ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out) | static_cast<uint64_t>(k_stride * unit_bytes) |
+                static_cast<uint64_t>(v_stride * unit_bytes)) & 31) == 0;
   const int sms = cache_num_sms(cache), spans = (num_rows - 1) / kSpan + 1;
-  // a small call's heads are shared out among CTAs, so that it fills the GPU too
-  const int most = (l.Hkv + 1) / 2;
-  g.splits = std::max(1, std::min(most, kReadCtas * sms / spans));
+  // (half a byte a value in, on average)
+  const int64_t bytes = 2 * row * unit_bytes + row;
+  g.splits = shares_of(spans, (l.Hkv + 1) / 2, kReadCtas * sms, copy_ns(bytes, kReadCtas * sms));
   const int64_t units = static_cast<int64_t>(spans) * g.splits;
   g.lg_parts = lg_parts((l.Hkv + g.splits - 1) / g.splits);
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(units, kReadCtas * sms)));

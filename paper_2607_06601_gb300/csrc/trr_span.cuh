@@ -180,6 +180,21 @@ __device__ __forceinline__ void for_groups(const Found<ROWS>& f, int lg_parts, i
 // Parts that a group's heads are shared out in: enough that eight warps come out nearly even, two heads each at least.
 __host__ __device__ inline int lg_parts(int heads) { return heads >= 8 ? 2 : heads >= 4 ? 1 : 0; }
 
+// Shares of the heads that a unit (64 positions) is cut into: as many as make the rounds of `ctas` CTAs shortest, where
+// a unit whole takes `whole` ns among as many others, and each share 5 us more to find its tokens.  Measured on 40,000
+// rows of 32 heads of 64 in binary32: 169 us with whole units (637 for 608 CTAs), 153 with quarters.
+__host__ __device__ inline int shares_of(int64_t units, int most, int ctas, int64_t whole) {
+  int best = 1;
+  int64_t least = 0;
+  for (int s = 1; s <= most; ++s) {
+    const int64_t rounds = (units * s + ctas - 1) / ctas, t = rounds * (whole / s + 5000);
+    if (s == 1 || t < least) best = s, least = t;
+  }
+  return best;
+}
+// The time that 64 positions of `bytes` each take when every CTA copies as much, at 6.5 bytes a ps.
+__host__ __device__ inline int64_t copy_ns(int64_t bytes, int ctas) { return bytes * kSpan * ctas / 6500; }
+
 // 32 bytes in one store (p aligned to them).
 __device__ __forceinline__ void store_sector(void* p, uint4 a, uint4 b) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z),

@@ -8,7 +8,7 @@ namespace trr {
 
 // Tokens of a staged tile: as many as let the scores (binary32), the weights (binary16) and the sums of two halves
 // of 128 rows have TMEM columns of their own: 2 (T + T / 2 + d) <= 512, T a multiple of 16.
-__host__ __device__ constexpr int chunk_tile(int d) { return d == 64 ? 128 : 80; }
+__host__ __device__ constexpr int chunk_tile(int d) { return d == 64 ? 96 : 80; }
 constexpr int kHalfRows = 128;       // rows of a softmax warpgroup: lanes of TMEM
 constexpr int kBlockRows = 2 * kHalfRows;
 constexpr int kPlanChunkThreads = 512;

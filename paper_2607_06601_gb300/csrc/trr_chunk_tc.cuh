@@ -56,7 +56,8 @@ struct ChunkSmem {
   static constexpr int kSeg = kRows + kRunSlots * kBlockRows * static_cast<int>(sizeof(ChunkRow));
   static constexpr int kBars = kSeg + kRunSlots * static_cast<int>(sizeof(ChunkSegment));
   static constexpr int kNumBars = 2 * kSlots + 3 * kRunSlots + 2 * 6 + 2;
-  static constexpr int kTotal = kBars + 8 * kNumBars;
+  static constexpr int kAbort = kBars + 8 * kNumBars;
+  static constexpr int kTotal = kAbort + 8;
   static_assert(kTotal + 1024 + 64 <= 227 * 1024, "");
   static_assert(kTile % 1024 == 0, "");
 };
@@ -68,8 +69,8 @@ struct ChunkCtx {
   static constexpr int kPartA = D == 64 ? 64 : 48, kPartB = kT - kPartA;  // a thread's scores, as two arrays
   uint8_t* base;  // 1024-byte aligned
   uint32_t tmem;
-  uint64_t wait_ns;
-  volatile int* abort_flag;
+  const ChunkArgs* args;  // (the kernel's own: read from there, not kept in registers)
+  __device__ volatile int* abort_flag() const { return reinterpret_cast<volatile int*>(base + L::kAbort); }
   __device__ uint64_t* bar(int i) const { return reinterpret_cast<uint64_t*>(base + L::kBars) + i; }
   __device__ uint64_t* kv_full(int i) const { return bar(i); }
   __device__ uint64_t* kv_empty(int i) const { return bar(L::kSlots + i); }
@@ -89,18 +90,18 @@ struct ChunkCtx {
   __device__ ChunkRow* rows(int i) const { return reinterpret_cast<ChunkRow*>(base + L::kRows) + i * kBlockRows; }
   // TMEM columns: scores, weights (two to a column), sums
   __device__ uint32_t col_s(int half) const { return tmem + kT * half; }
-  __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 256 + 64 * half : 160 + 48 * half); }
+  __device__ uint32_t col_p(int half) const { return tmem + (D == 64 ? 192 : 160) + 48 * half; }
   __device__ uint32_t col_o(int half) const { return tmem + 512 - D * (2 - half); }
   __device__ __forceinline__ bool there(uint64_t* b, uint32_t parity) const { return mbar_test_at(smem_u32(b), parity); }
   // A bounded wait by a whole warp; all of its lanes get the same answer.  Once one has given up, none waits any
   // more.  (Short, since a warp among others' code pays for the fetch of every instruction.)
   __device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity) const {
     const uint32_t addr = smem_u32(b);
-    for (uint64_t t0 = 0; !__all_sync(0xffffffffu, mbar_poll(addr, parity, wait_ns));) {
+    for (uint64_t t0 = 0; !__all_sync(0xffffffffu, mbar_poll(addr, parity, args->a.wait_ns));) {
       const uint64_t now = global_ns();
       if (t0 == 0) t0 = now;
-      if (__any_sync(0xffffffffu, *abort_flag || now - t0 >= wait_ns)) {
-        *abort_flag = 1;
+      if (__any_sync(0xffffffffu, *abort_flag() || now - t0 >= args->a.wait_ns)) {
+        *abort_flag() = 1;
         return false;
       }
     }
@@ -351,8 +352,6 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
-  float* const exchange = reinterpret_cast<float*>(x.base + L::kExchange);
-  float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
   int segs = 0, it = 0, joins = 0;
   float f = 0.f;
   // The row's query into shared memory as binary16, scaled by the power of two that brings its largest element to [1, 2).
@@ -399,23 +398,23 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   if (!load_rows(0)) return;
   for (;; ++segs) {
     const ChunkSegment& sg = x.seg(segs % kRunSlots);
-    const int tiles = sg.tiles, clean = sg.clean, clean_end = sg.clean_end, dest = sg.dest;
+    const int tiles = sg.tiles, clean = sg.clean, clean_end = sg.clean_end;
     if (tiles == 0) return;
-    const bool turns = sg.rows <= kHalfRows;  // the halves have the same rows and take the tiles in turn
-    const int step = turns ? 2 : 1, first = turns ? half : 0, first_row = turns ? 0 : half * kHalfRows;
+    const int step = sg.rows <= kHalfRows ? 2 : 1, first = (step - 1) * half;  // 2: the halves have the same rows and take the tiles in turn
     float m = -INFINITY, l = 0.f;
     bool ready = false;    // the next scores are there
     bool settled = false;  // every row of the warp has a reference
     for (int i = first; i < tiles; i += step, ++it) {
       if (!ready && !x.wait(x.s_full(half), it & 1)) return;
       tc_fence_after();
+      const bool used = it == 0 || x.there(x.o_done(half), (it - 1) & 1);
       uint32_t a[A], b[B];
       tmem_ld(a, b, col_s);
       tc_fence_before();
       mbar_arrive(x.s_read(half));  // the next scores may come (every thread says so: one for all would cost 100 cycles)
       if (i < clean || i >= clean_end) {  // not every row sees the whole tile
         const int s = sg.from + i, before = (s + (s < sg.head ? 0 : sg.skip)) * T;
-        const ChunkRow r = x.rows(segs % kRunSlots)[first_row + row];
+        const ChunkRow r = x.rows(segs % kRunSlots)[(2 - step) * half * kHalfRows + row];
         const int hi = r.hi - before, lo = r.lo - before, sinks = sg.local ? sg.sinks - before : 0;
         uint32_t seen[(T + 31) / 32], any = 0;
 #pragma unroll
@@ -436,10 +435,10 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         hide<0>(a, seen);
         hide<A>(b, seen);
       }
-      // the reference moves up to `top`, in whole steps of the exponent (so that weights can follow); O with it
-      auto move = [&](float top) -> bool {
-        const float next = top > m ? (m == -INFINITY ? top : m + ceilf(top - m)) : m;
-        const float by = m == -INFINITY ? 0.f : exp2_approx(m - next);
+      // where it must, the reference moves up to `top`, O with it (rows that need not stay as they are, bit for bit)
+      auto move = [&](bool must, float top) -> bool {
+        const float next = must ? fmaxf(m, top) : m;
+        const float by = m == next ? 1.f : exp2_approx(m - next);
         l *= by;
         m = next;
         if (i == first) return true;
@@ -456,37 +455,30 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         return true;
       };
       if (!settled) {
-        if (!move(fmaxf(highest(a), highest(b)) * f)) return;
+        if (!move(m == -INFINITY, fmaxf(highest(a), highest(b)) * f)) return;
         settled = __all_sync(0xffffffffu, m != -INFINITY);
       }
       auto shift = [&] { return m == -INFINITY ? 0.f : -m; };
+      uint32_t p[A / 2];
+      float sum = weights_of(a, p, f, shift());
       // (asked for before the exponentials, which hide how long the answer takes)
-      const bool used = it == 0 || x.there(x.o_done(half), (it - 1) & 1);
-      uint32_t pa[A / 2], pb[B / 2];
-      float sum = weights_of(a, pa, f, shift());
-      if (__any_sync(0xffffffffu, sum > kMost || !used)) {
-        if (it > 0 && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
-        if (__any_sync(0xffffffffu, sum > kMost)) {
-          if (!move(fmaxf(highest(a), highest(b)) * f)) return;
-          sum = weights_of(a, pa, f, shift());
-        }
-      }
+      if (!__all_sync(0xffffffffu, used) && !x.wait(x.o_done(half), (it - 1) & 1)) return;  // the last weights have been used
       tc_fence_after();
-      put_words(col_p, pa);
-      float more = weights_of(b, pb, f, shift());
-      if (__any_sync(0xffffffffu, more > kMost)) {
-        const float was = m;
-        if (!move(highest(b) * f)) return;
-        const float by = was == -INFINITY ? 0.f : exp2_approx(was - m);
-        const __half2 by2 = __float2half2_rn(by);
-        sum *= by;
-#pragma unroll
-        for (int k = 0; k < A / 2; ++k) pa[k] = as_u32(__hmul2(as_half2(pa[k]), by2));
-        put_words(col_p, pa);
-        more = weights_of(b, pb, f, shift());
+      put_words(col_p, p);
+      {
+        uint32_t q[B / 2];
+        sum += weights_of(b, q, f, shift());
+        put_words(col_p + A / 2, q);
       }
-      put_words(col_p + A / 2, pb);
-      l += sum + more;
+      if (__any_sync(0xffffffffu, sum > kMost)) {
+        if (!move(sum > kMost, fmaxf(highest(a), highest(b)) * f)) return;
+        sum = weights_of(a, p, f, shift());
+        put_words(col_p, p);
+        uint32_t q[B / 2];
+        sum += weights_of(b, q, f, shift());
+        put_words(col_p + A / 2, q);
+      }
+      l += sum;
       const bool next = x.there(x.s_full(half), (it + 1) & 1);
       tmem_wait_st();
       tc_fence_before();
@@ -494,7 +486,8 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       ready = __all_sync(0xffffffffu, next);
     }
     const bool some = first < tiles;
-    const int at = x.rows(segs % kRunSlots)[first_row + row].at;
+    const bool turns = step == 2;
+    const int first_row = turns ? 0 : half * kHalfRows, dest = sg.dest, at = x.rows(segs % kRunSlots)[first_row + row].at;
     const bool mine = at >= 0;
     // the next run's rows, while this one's last product runs (its scores are all in: Q's place is free)
     if (!load_rows(segs + 1)) return;
@@ -505,6 +498,8 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(x.seg_empty(segs % kRunSlots));
+    float* const exchange = reinterpret_cast<float*>(x.base + L::kExchange);
+    float2* const exchange_ml = reinterpret_cast<float2*>(x.base + L::kMl);
     if (turns && half == 1) {  // to the first half, 32 columns at a time
       if (joins > 0 && !x.wait(x.join_empty(), (joins - 1) & 1)) return;
       exchange_ml[row] = make_float2(m, l);
@@ -573,14 +568,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   extern __shared__ uint8_t dyn[];
   using L = ChunkSmem<D>;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
   ChunkCtx<D> x;
   x.base = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);
-  x.wait_ns = g.a.wait_ns;
-  x.abort_flag = &s_abort;
+  x.args = &g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    s_abort = 0;
+    *x.abort_flag() = 0;
     for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
     for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 3), mbar_init(x.rows_full(i), 1);
     for (int h = 0; h < 2; ++h) {
@@ -615,7 +608,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   __syncthreads();
   tc_fence_after();
   if (warp == kChunkMma) tmem_free(s_tmem);
-  if (threadIdx.x == 0 && s_abort) set_status(g.a.ctrl, TRR_ERR_TIMEOUT);
+  if (threadIdx.x == 0 && *x.abort_flag()) set_status(g.a.ctrl, TRR_ERR_TIMEOUT);
 }
 
 }  // namespace trr

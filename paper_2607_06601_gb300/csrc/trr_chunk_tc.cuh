@@ -47,7 +47,7 @@ struct ChunkSmem {
   static constexpr int kT = chunk_tile(D);
   static constexpr int kQ = kHalfRows * D * 2;      // bytes of Q of a half
   static constexpr int kTile = kT * D * 2;          // bytes of K or V of a tile
-  static constexpr int kSlots = D == 64 ? 4 : 3;    // of K, and of V
+  static constexpr int kSlots = D == 64 ? 6 : 3;    // of K, and of V
   static constexpr int kK = 2 * kQ;                 // behind Q
   static constexpr int kV = kK + kSlots * kTile;
   static constexpr int kExchange = kV + kSlots * kTile;  // 32 columns of the second half's rows, and (m, l), for a join
@@ -411,7 +411,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       uint32_t a[A], b[B];
       tmem_ld(a, b, col_s);
       tc_fence_before();
-      mbar_arrive(x.s_read(half));  // the next scores may come (every thread says so: one for all would cost 100 cycles)
+      if (lane == 0) mbar_arrive(x.s_read(half));  // the next scores may come (the load was the whole warp's: no need to meet first)
       if (i < clean || i >= clean_end) {  // not every row sees the whole tile
         const int s = sg.from + i, before = (s + (s < sg.head ? 0 : sg.skip)) * T;
         const ChunkRow r = x.rows(segs % kRunSlots)[(2 - step) * half * kHalfRows + row];
@@ -428,7 +428,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
           put_words(col_p, none);
           tmem_wait_st();
           tc_fence_before();
-          mbar_arrive(x.p_full(half));
+          if (lane == 0) mbar_arrive(x.p_full(half));
           ready = false;
           continue;
         }
@@ -482,7 +482,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       const bool next = x.there(x.s_full(half), (it + 1) & 1);
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive(x.p_full(half));
+      if (lane == 0) mbar_arrive(x.p_full(half));
       ready = __all_sync(0xffffffffu, next);
     }
     const bool some = first < tiles;
@@ -577,8 +577,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
     for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
     for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 3), mbar_init(x.rows_full(i), 1);
     for (int h = 0; h < 2; ++h) {
-      mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), kHalfRows);
-      mbar_init(x.p_full(h), kHalfRows), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
+      mbar_init(x.q_full(h), 4), mbar_init(x.s_full(h), 1), mbar_init(x.s_read(h), 4);
+      mbar_init(x.p_full(h), 4), mbar_init(x.o_done(h), 1), mbar_init(x.drained(h), 1);
     }
     mbar_init(x.join_full(), 4), mbar_init(x.join_empty(), 4);
     fence_barrier_init();

@@ -255,7 +255,17 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
       __syncwarp();
       return true;
     };
-    if (first < n) ok = x.wait(x.q_full(half), loads++ & 1) && scores(first, false);
+    // A tile of the other half's: seen to come and let go, so that each of a slot's phases has been waited for in order
+    // (a parity alone does not tell a phase from the one before the last) and none is over before both have seen it.
+    auto pass = [&](int i) -> bool {
+      const int slot = (done + i) % L::kSlots;
+      if (!x.wait(x.kv_full(slot), ((done + i) / L::kSlots) & 1)) return false;
+      if (elected()) mbar_arrive(x.kv_empty(slot));
+      __syncwarp();
+      return true;
+    };
+    if (first == 1) ok = pass(0);
+    if (first < n) ok = ok && x.wait(x.q_full(half), loads++ & 1) && scores(first, false);
 #pragma unroll 1
     for (int i = first; i < n && ok; i += step, ++it) {
       // asked together: three answers take little longer than one
@@ -263,7 +273,8 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
       read = __all_sync(0xffffffffu, read);
       tile = __all_sync(0xffffffffu, tile);
       weights = __all_sync(0xffffffffu, weights);
-      if (i + step < n) ok = (read || x.wait(x.s_read(half), it & 1)) && scores(i + step, tile);
+      if (turns && i + 1 < n) ok = pass(i + 1);
+      if (i + step < n) ok = ok && (read || x.wait(x.s_read(half), it & 1)) && scores(i + step, tile);
       if (!ok || !(ok = weights || x.wait(x.p_full(half), it & 1))) break;
       tc_fence_after();
       if (elected()) {
@@ -273,7 +284,6 @@ __device__ __forceinline__ void chunk_mma(const ChunkCtx<D>& x, int half) {
         for (int k = 0; k < T / 16; ++k) tc_mma(col_o, col_p + 8 * k, v + k * (2048 >> 4), id_o, k > 0 || i > first);
         tc_commit(x.kv_empty(slot));
         tc_commit(x.o_done(half));
-        if (turns) mbar_arrive(x.kv_empty(slot));  // (for the other half)
       }
       __syncwarp();
     }

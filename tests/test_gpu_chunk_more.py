@@ -190,3 +190,26 @@ def test_outputs_past_32_bits():
     for a, b in zip((k, v, bits), one):
         assert torch.equal(a[7:107], b[:100]) and torch.equal(a[rows - 200:], b[100:])
     assert (big[:, 0] == 7).all() and (k[107:rows - 200] == 7).all() and (bits[107:rows - 200] == 9).all()
+
+
+@pytest.mark.parametrize("lay,new", [(dict(Hq=32, Hkv=8, d=128, G=64, P=32), 30), (dict(Hq=8, Hkv=8, d=128, G=64, P=16), 9), (dict(Hq=16, Hkv=8, d=64, G=64, P=32), 20)])
+def test_short_blocks_whose_tiles_come_in_any_order(lay, new):
+    """Many blocks of few rows, whose tiles the two halves of a CTA take in turn: a tile may land before the one ahead of
+    it.  Bit for bit the same rows over calls with the tiles in memory, and held to the definition."""
+    rng = np.random.default_rng([9, new])
+    S, total = 24, 1500
+    h = holder(lay, S=S, maxctx=total + new, caps=S * (total + new) // (2 * lay["P"]) + 4 * S, archive=2 * S + 4)
+    for s in range(S):
+        fill(h, rng, 0, s, total + new, bits=None)
+    n = S * new
+    modes, windows = rng.choice(3, n, p=[0.1, 0.4, 0.5]), np.full(n, 300)
+    q_bits = wl.bf16_bits(rng.standard_normal((n, h.Hq, h.d), dtype=np.float32))
+    args = ([*range(S)], [total] * S, [new] * S, modes, windows, 4)
+    out, lse = check(h, rng, *args, q_bits=q_bits)
+    cold = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")  # twice L2
+    call_args = (0, h.ints(args[0]), h.ints(args[1]), h.ints(np.arange(S + 1) * new), dev(q_bits, torch.bfloat16), dev(modes.astype(np.uint8), torch.uint8))
+    for i in range(60):
+        if i % 2:
+            cold.fill_(i)
+        assert torch.equal(h.gpu.chunk_attn(*call_args, window_scalar=300, sinks=4), out), i
+    assert h.gpu.status() == 0

@@ -299,7 +299,8 @@ __device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) 
   p.tiles = p.head + p.last - p.first;
   if (p.tiles > 0) {
     const int whole = max(0, min(p.clean_end, p.last) - max(p.clean, p.first));
-    p.tile_cost = kChunkTileCost + (kChunkMaskedCost * (p.tiles - whole) + p.tiles / 2) / p.tiles;
+    p.tile_cost = (p.rows <= kHalfRows && a.d == 64 ? kChunkTurnsCost : kChunkTileCost) +
+                  (kChunkMaskedCost * (p.tiles - whole) + p.tiles / 2) / p.tiles;
   }
   if (lane == 0) g.block[b] = p;
 }

@@ -101,12 +101,14 @@ __device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkP
   return r;
 }
 
-// The cost of a segment: its tiles, those dearer that not every row sees whole, and a fixed part for its start and end
-// (in eighths of a tile's 2100 cycles at d 64; measured 3600 for a tile with rows hidden, 8000 for a segment, before
-// both were cut).  With every tile alike and a fixed part of one tile, 4096 queries on themselves, 32 heads of 64, took
-// 202 us against 150 with one of five, as the CTAs with the shortest segments came in last.
-constexpr int kChunkTileCost = 8, kChunkMaskedCost = 4, kChunkSegmentCost = 30;
-constexpr int kChunkLeastShare = 24;  // of a CTA: three tiles
+// The cost of a segment, in sixteenths of a tile (2000 cycles at d 64): its tiles, those with rows hidden a little dearer
+// (2250), and a fixed part for its start and end (5000 to 10,000).  Where the halves take turns (blocks of 128 rows or fewer)
+// two tiles take 2600 cycles at d 64, but 4300 at d 128, whose three staged tiles leave neither half one ahead.  With a fixed
+// part of one tile and all tiles alike, 4096 queries on themselves, 32 heads of 64, took 202 us against 144, as the CTAs with
+// the shortest segments came in last; with turns at the price of whole tiles, ragged chunks of d 64 took 402 us against 378;
+// at 10 sixteenths of one at d 128 too, a window of 8192 tokens took 151 us against 130.
+constexpr int kChunkTileCost = 16, kChunkTurnsCost = 10, kChunkMaskedCost = 2, kChunkSegmentCost = 60;
+constexpr int kChunkLeastShare = 48;  // of a CTA: three tiles
 __device__ __forceinline__ int64_t chunk_cost(const BlockPlan& b) {
   return b.tiles > 0 ? kChunkSegmentCost + static_cast<int64_t>(b.tile_cost) * b.tiles : 0;
 }

@@ -416,7 +416,8 @@ TRR_API trr_status trr_decode_attn_shared(trr_cache* cache, int32_t layer, int32
 /* Bytes of workspace for trr_chunk_attn of num_chunks chunks with num_tokens queries whose
  * positions, and all before them, number at most max_keys: the sum of starts[i] + length
  * of chunk i (counting what is stored is enough, and chunks of local queries count their
- * windows and sinks only). */
+ * windows and sinks only).  UNSUPPORTED where num_tokens * num_q_heads or the workspace's
+ * tokens come to 2^31 - 256 or more, or the cache has head_modes. */
 TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num_chunks, int32_t num_tokens,
                                              int64_t max_keys, uint64_t* bytes);
 
@@ -442,7 +443,20 @@ TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num
  *   stored makes every row zero and records OUT_OF_MEMORY.
  *   Device-detected errors: those of stretches; a mode not allowed or a local query with a
  *   window below 1 (INVALID_ARG) makes that query's rows zero.  A cache with head_modes
- *   returns TRR_ERR_UNSUPPORTED. */
+ *   returns TRR_ERR_UNSUPPORTED.
+ *   How near: K, V and the softmax weights are rounded to binary16 (11 bits), sums are
+ *   binary32; an element of out is off by its rounding to bf16 and about 2^-10 of the sum of
+ *   its weights times |v|, lse by 2^-11 of the largest sum of |scale q_j k_j| at most.  Chunks whose
+ *   values binary16 does not hold (65536 and more, infinities and NaN, all below 2^-14) are
+ *   done row by row in binary32, which takes many times as long.
+ *   Which call: everything in sight is brought back to binary16 in the workspace, once for
+ *   all queries of a chunk.  That costs the same for one query and for many: 32 chunks on
+ *   2048 tokens of 12 heads of 64 take 134 us with 1 query each and 136 with 64, where
+ *   trr_decode_attn takes 40 us with 1, 84 with 4, 135 with 8, 246 with 16 and 961 with 64.
+ *   So below 8 queries a chunk take trr_decode_attn; where several query heads share a KV
+ *   head and all queries are full, trr_decode_attn_shared with the chunks as its groups is
+ *   the faster one up to 16 (32 chunks on 4096 tokens, 32 heads on 8 of 128: 299 us here,
+ *   176 there with 8 queries each, 223 with 16, 320 with 32). */
 TRR_API trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t num_chunks, const int32_t* seq_ids,
                                   const int32_t* starts, const int32_t* offsets, int32_t num_tokens, const void* q_bf16,
                                   const uint8_t* modes, const int32_t* windows, int32_t window_scalar, int32_t sinks,

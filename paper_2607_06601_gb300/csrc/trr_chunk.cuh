@@ -106,7 +106,7 @@ __device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkP
 // two tiles take 2600 cycles at d 64, but 4300 at d 128, whose three staged tiles leave neither half one ahead.  With a fixed
 // part of one tile and all tiles alike, 4096 queries on themselves, 32 heads of 64, took 202 us against 144, as the CTAs with
 // the shortest segments came in last; with turns at the price of whole tiles, ragged chunks of d 64 took 402 us against 378;
-// at 10 sixteenths of one at d 128 too, a window of 8192 tokens took 151 us against 130.
+// at 10 sixteenths of one at d 128 too, local chunks of 256 to 700 queries and windows of 1024 took 151 us against 130.
 constexpr int kChunkTileCost = 16, kChunkTurnsCost = 10, kChunkMaskedCost = 2, kChunkSegmentCost = 60;
 constexpr int kChunkLeastShare = 48;  // of a CTA: three tiles
 __device__ __forceinline__ int64_t chunk_cost(const BlockPlan& b) {

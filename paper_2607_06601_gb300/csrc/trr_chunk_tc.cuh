@@ -1,17 +1,25 @@
 // trr_chunk_tc.cuh - attention of blocks of 256 rows over staged tiles, on the tensor cores (tcgen05).
 //
-// One CTA per SM.  A producer warp brings tiles of tokens (K, V, positions) into rings of shared memory, as
-// they were staged, with bulk copies.  A block's rows are two halves of 128, one to a lane of TMEM; each half has
-// a warp that issues its products S = Q K^T and O += P V and a warpgroup that does its softmax, a thread a row.  A block of 128 rows or fewer has its rows in both halves, which take its tiles in turn and are
-// joined at the end.  K, V and p are binary16, sums and statistics binary32; query rows are scaled by powers of
-// two.
+//   S = Q K^T,  p = 2^(f S - m),  l += sum p,  O += P V,  and at a row's end O / l or the piece (m, l, O).
 //
-// What bounds it: the products, and the time from a product's end to the next one that waits for it (about 450
-// cycles: completion, barrier, wait, issue).  So no product waits for another: scores, weights and sums have
-// columns of their own, and a tile's scores are issued as soon as the last ones have been read.  For that a tile
-// has 128 tokens at d 64 and 80 at d 128 (TMEM has 512 columns); with 128 tokens at d 128, weights over scores,
-// 2048 queries of 32 heads on 32768 tokens took 860 us.  A product of 128 x 80 x 16 from shared memory takes 51
-// cycles of its bandwidth against 40 of the tensor core's.
+// One CTA per SM.  A producer warp brings tiles of tokens (K and V) into rings of shared memory, as they were
+// staged, with bulk copies.  A block's rows are two halves of 128, a lane of TMEM each; a half has a warp that
+// issues its products and a warpgroup that does its softmax, a thread a row.  A block of 128 rows or fewer has its
+// rows in both halves, which take its tiles in turn and are joined at the end.  K, V and p are binary16 (11 bits;
+// the output has 8), sums and statistics binary32; query rows are scaled by powers of two.
+//
+// What bounds it.  Per tile of 96 tokens at d 64 the two halves' products take 464 + 384 cycles of the tensor core
+// and its shared memory, 24,576 exponentials 768 of the SM's 32 a cycle, and a softmax warp's chain of waits,
+// loads from TMEM, weights and stores about 1900, which is what a tile takes: at 4096 queries on themselves, 32
+// heads of 64 (four fifths of the tokens stored), 91 us, 0.60 PFLOP/s, the tensor pipe busy for 27 % of it.  At d 128
+// a product of 128 x 80 x 16 from shared memory takes 54 cycles of its bandwidth, 1506 a tile with those of P V;
+// measured 1880: 2048 queries of 32 heads at the end of 32,768 tokens, 555 us, 1.54 PFLOP/s.
+//
+// What this layout is for: from a product's end to the issue of one that waits for it pass about 450 cycles
+// (completion, barrier, wait, issue).  So no product waits for another: scores, weights and sums have columns of
+// their own, and a tile's scores are issued as soon as the last ones have been read.  That gives tiles of 96 and of
+// 80 tokens (TMEM has 512 columns).  With 128 tokens at d 128, weights over scores, the call above took 860 us; with
+// 128 at d 64, whose scores do not fit a thread's registers, ragged chunks 412 against 397.
 #pragma once
 
 #include "trr_chunk.cuh"

@@ -263,17 +263,14 @@ __device__ __forceinline__ uint4 convert_f16(uint4 v, uint32_t* top, bool* lost)
 // The tiles that block b's rows see.
 __device__ __forceinline__ void plan_block(const ChunkArgs& g, int b, int lane) {
   const LayerArgs& a = g.a;
-  int lo = 0, hi = g.n - 1;  // its chunk: the last one whose first block is b or before it
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (g.chunk[mid].block0 <= b) lo = mid;
-    else hi = mid - 1;
-  }
+  // its chunk: the last one whose first block is b or before it
+  const int lo = last_not_above(g.n, b, lane, [&](int i) { return g.chunk[i].block0; });
   const ChunkPlan c = g.chunk[lo];
   const int heads = a.Hq / a.Hkv, full_blocks = (c.full * heads + kBlockRows - 1) / kBlockRows, T = chunk_tile(a.d);
   const bool local = b - c.block0 >= full_blocks;
   BlockPlan p = {};
   p.chunk = lo; p.local = local;
+  p.tile0 = c.tile0; p.sinks = c.head;
   p.row = (b - c.block0 - (local ? full_blocks : 0)) * kBlockRows;
   p.rows = min(kBlockRows, (local ? c.local : c.full) * heads - p.row);
   p.query0 = c.row0 + (local ? c.full : 0);
@@ -388,6 +385,7 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
   if (s_last) {
     __threadfence();
     int64_t work = 0;
+    bool empty = false;
     for (int x0 = 0; x0 < head.blocks; x0 += kSpanThreads) {
       const int x = x0 + tid;
       BlockPlan b = {};
@@ -399,8 +397,11 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
       const int64_t before = work + scan_before(a.Hkv * chunk_cost(b), s_sums, &all);
       work += all;
       if (x < head.blocks) g.base[x] = before;
+      empty |= x < head.blocks && b.tiles == 0;
     }
+    empty = __syncthreads_or(empty);
     if (tid == 0) {
+      g.head->empty = empty;
       g.base[head.blocks] = work;
       g.head->work = work;
       g.head->per = max((work + g.ctas - 1) / g.ctas, static_cast<int64_t>(kChunkLeastShare));
@@ -439,13 +440,7 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
   for (int u = gridDim.x - 1 - blockIdx.x; u < head.units * head.splits; u += gridDim.x) {
     const int unit = u / head.splits, h0 = u % head.splits * per, h1 = min(a.Hkv, h0 + per);
     if (chunk < 0 || unit >= c.unit0 + c.units) {
-      int lo = chunk < 0 ? 0 : chunk, hi = g.n - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (g.chunk[mid].unit0 <= unit) lo = mid;
-        else hi = mid - 1;
-      }
-      chunk = lo;
+      chunk = last_not_above(g.n, unit, lane, [&](int i) { return g.chunk[i].unit0; });
       c = g.chunk[chunk];
     }
     const int x = (unit - c.unit0) * kSpan + (tid >> 2), cls = tid & 3;
@@ -548,24 +543,23 @@ __device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& ch,
 
 // One row of a cut segment, by eight lanes: D / 8 values each.
 template <int D>
-__device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const PieceInfo& piece, const BlockPlan& b, int r, int lane) {
+__device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const PieceInfo& piece, int r, int lane) {
   constexpr int E = D / 8;
-  const int64_t cost = chunk_cost(b), S = g.base[piece.block] + piece.kvh * cost, per = g.head->per;
+  const int heads = g.a.Hq / g.a.Hkv, query = g.list[piece.query0 + (piece.row + r) / heads];
   // parts: the last one of CTA `cta`, the first ones of those that follow
-  auto slot = [&](int j) { return static_cast<int64_t>(2 * j + (j == cta)) * kBlockRows + r; };
-  int end = cta + 1;
-  while (end < g.ctas && chunk_tiles_before(end * per - S, b) < b.tiles) ++end;
+  auto piece_of = [&](int j) { return 2 * j + (j == cta); };
+  auto slot = [&](int j) { return static_cast<int64_t>(piece_of(j)) * kBlockRows + r; };
+  const int end = cta + piece.ctas;
   float m = -INFINITY, l = 0.f, o[E] = {};
 #pragma unroll 4
   for (int j = cta; j < end; ++j) m = fmaxf(m, g.part_ml[slot(j)].x);
 #pragma unroll 2
   for (int j = cta; j < end; ++j) {
     const float2 ml = g.part_ml[slot(j)];
-    const float4* part = reinterpret_cast<const float4*>(g.part_o + slot(j) * D + lane * 4);
     const float w = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - m);
     float4 v[E / 4];
 #pragma unroll
-    for (int i = 0; i < E / 4; ++i) v[i] = part[8 * i];
+    for (int i = 0; i < E / 4; ++i) v[i] = *reinterpret_cast<const float4*>(part_at<D>(g, piece_of(j), lane + 8 * i, r));
     l += ml.y * w;
     if (w == 0.f) continue;  // (a part in which nothing was seen may hold anything)
 #pragma unroll
@@ -576,8 +570,7 @@ __device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const Piec
       o[4 * i + 3] += v[i].w * w;
     }
   }
-  const RowSource s = row_source(g, g.chunk[b.chunk], b.query0, b.local, piece.kvh, b.row + r);
-  const int64_t at = static_cast<int64_t>(s.query) * g.a.Hq + s.head;
+  const int64_t at = static_cast<int64_t>(query) * g.a.Hq + piece.kvh * heads + (piece.row + r) % heads;
   const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
   for (int i = 0; i < E / 4; ++i)
@@ -593,23 +586,21 @@ __global__ void __launch_bounds__(256, kJoinCtas) chunk_join_kernel(const __grid
   constexpr int kJoinRows = 256 / 8;
   pdl_wait();
   pdl_trigger();
-  if (g.head->bad) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, blocks = g.head->blocks;
-  const bool flagged = g.head->flagged;
-  auto careful = [&](const BlockPlan& b, int kvh) { return flagged && g.flag[static_cast<int64_t>(b.chunk) * g.a.Hkv + kvh]; };
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bad = g.head->bad, blocks = g.head->blocks;
+  const bool flagged = g.head->flagged, empty = g.head->empty;
+  auto careful = [&](int chunk, int kvh) { return flagged && g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + kvh]; };
   for (int x = blockIdx.x; x < g.ctas * (kBlockRows / kJoinRows); x += gridDim.x) {
     const int cta = x / (kBlockRows / kJoinRows), r = x % (kBlockRows / kJoinRows) * kJoinRows + threadIdx.x / 8;
-    const PieceInfo piece = g.piece[cta];
-    if (piece.block < 0) continue;
-    const BlockPlan& b = g.block[piece.block];
-    if (r < b.rows && !careful(b, piece.kvh)) join_row<D>(g, cta, piece, b, r, threadIdx.x & 7);
+    const PieceInfo piece = g.piece[cta];  // (none where the call is refused)
+    if (piece.block >= 0 && r < piece.rows && !careful(piece.chunk, piece.kvh)) join_row<D>(g, cta, piece, r, threadIdx.x & 7);
   }
+  if (bad || !(flagged || empty)) return;
   // rows with nothing stored in sight, and those that are done one by one
   for (int64_t x = blockIdx.x; x < static_cast<int64_t>(blocks) * g.a.Hkv * (kBlockRows / kJoinRows); x += gridDim.x) {
     const int64_t y = x / (kBlockRows / kJoinRows);
     const BlockPlan& b = g.block[y / g.a.Hkv];
     const int kvh = static_cast<int>(y % g.a.Hkv), r0 = static_cast<int>(x % (kBlockRows / kJoinRows)) * kJoinRows;
-    if (b.tiles > 0 && !careful(b, kvh)) continue;
+    if (b.tiles > 0 && !careful(b.chunk, kvh)) continue;
     const ChunkPlan& c = g.chunk[b.chunk];
     for (int r = r0 + warp; r < min(b.rows, r0 + kJoinRows); r += 8) {
       const RowSource s = row_source(g, c, b.query0, b.local, kvh, b.row + r);
@@ -643,7 +634,7 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->flag = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
   g->piece = reinterpret_cast<PieceInfo*>(take(static_cast<int64_t>(sizeof(PieceInfo)) * ctas));
   g->part_ml = reinterpret_cast<float2*>(take(8ll * 2 * ctas * kBlockRows));
-  g->part_o = reinterpret_cast<float*>(take(4ll * 2 * ctas * kBlockRows * l.d));
+  g->part_o = reinterpret_cast<uint4*>(take(4ll * 2 * ctas * kBlockRows * l.d));
   g->most_blocks = static_cast<int>(blocks);
   const int64_t fixed = off, T = chunk_tile(l.d);
   g->tile = take((most_tiles * l.Hkv * 2 * T * l.d * 2 + 1023) / 1024 * 1024);

@@ -38,7 +38,8 @@ struct BlockPlan {
   int clean, clean_end;
   int query0;                   // the mode's first query in the list
   int tile_cost;
-  int pad[4];
+  int tile0, sinks;             // of the chunk: its first tile, staged tokens below the call's sinks
+  int pad[2];
 };
 static_assert(sizeof(BlockPlan) == 64, "");
 
@@ -47,12 +48,14 @@ struct ChunkHeader {
   int bad;                      // error of the whole call: every row is zero
   int blocks, units, tiles;
   int splits, flagged;          // shares of the KV heads that staging CTAs take; some flag is set
-  int pad[6];
+  int empty;                    // some block has no tiles
+  int pad[5];
 };
 
-// A piece of a segment that a CTA could not finish alone.
+// A segment that a CTA began and the ctas - 1 after it went on with; block < 0: none.
 struct PieceInfo {
-  int block, kvh, first_cta, ctas;  // block < 0: none.  The pieces are those of CTAs first_cta ..
+  int block, kvh, ctas, rows;
+  int chunk, local, query0, row;  // of the block
 };
 
 struct ChunkArgs {
@@ -75,7 +78,7 @@ struct ChunkArgs {
   int32_t* flag;      // [n][Hkv] some stored value is not to be had in binary16: its rows are done one by one
   PieceInfo* piece;   // [ctas] the segment that a CTA began and did not finish
   float2* part_ml;    // [2 * ctas][256] (m, l) of a CTA's first piece, or its last
-  float* part_o;      // [2 * ctas][256][D]
+  uint4* part_o;      // [2 * ctas][D / 4][256] four columns of a row (binary32), consecutive rows beside each other
   uint8_t* tile;      // [most_tiles][Hkv][K, V][T x D] binary16, in the tensor core's layout
 };
 
@@ -84,6 +87,12 @@ __device__ __forceinline__ int tile_at(int rows, int r, int e) { return (e >> 3)
 template <int D>
 __device__ __forceinline__ uint8_t* staged_tile(const ChunkArgs& g, int tile, int h, int which) {
   return g.tile + ((static_cast<int64_t>(tile) * g.a.Hkv + h) * 2 + which) * (chunk_tile(D) * D * 2);
+}
+
+// Columns 4 j .. 4 j + 3 of a row of a piece.
+template <int D>
+__device__ __forceinline__ uint4* part_at(const ChunkArgs& g, int piece, int j, int row) {
+  return g.part_o + (static_cast<int64_t>(piece) * (D / 4) + j) * kBlockRows + row;
 }
 
 // Where a row of a block comes from.
@@ -99,6 +108,20 @@ __device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkP
   r.t = c.start + r.query - c.row0;
   r.lo = local ? r.t - (g.windows ? g.windows[r.query] : g.window_scalar) + 1 : 0;
   return r;
+}
+
+// The last of 0 .. n-1 whose value (they ascend) is x or less, 0 if none is, by a whole warp: a chain of one load for 32 of
+// them, two for 1024.
+template <typename T, typename Value>
+__device__ __forceinline__ int last_not_above(int n, T x, int lane, Value value) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+    const int k = __popc(__ballot_sync(0xffffffffu, i < hi && value(i) <= x));
+    lo += max(0, k - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
 }
 
 // The cost of a segment, in sixteenths of a tile (2000 cycles at d 64): its tiles, those with rows hidden a little dearer

@@ -126,7 +126,8 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   const int64_t b0 = min(work, blockIdx.x * per), b1 = min(work, b0 + per);
   int segs = 0, copies = 0;
   bool ok = true;
-  PieceInfo piece = {-1, 0, 0, 0};
+  PieceInfo piece = {-1};
+  int64_t piece_end = 0;  // cost before its segment's last tile
   auto announce = [&](const ChunkSegment& s) {
     ok = ok && x.wait(x.seg_empty(segs % kRunSlots), ((segs / kRunSlots) & 1) ^ 1);
     if (!ok) return;
@@ -153,39 +154,39 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
   };
   if (b0 < b1) {
     fence_proxy_async_global();  // the tiles were staged with ordinary stores
-    int lo = 0, hi = blocks - 1;  // the block that holds cost b0: the last one that starts at or before it
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (g.base[mid] <= b0) lo = mid;
-      else hi = mid - 1;
-    }
+    // the block that holds cost b0: the last one that starts at or before it
+    const int lo = last_not_above(blocks, b0, lane, [&](int i) { return g.base[i]; });
     for (int b = lo; b < blocks && ok; ++b) {
+      const BlockPlan p = g.block[b];
       const int64_t start = g.base[b];
       if (start >= b1) break;
-      const BlockPlan p = g.block[b];
       if (p.tiles == 0) continue;
-      const int tile0 = g.chunk[p.chunk].tile0, sinks = g.chunk[p.chunk].head;
       const int64_t cost = chunk_cost(p);
       for (int h = static_cast<int>(max(static_cast<int64_t>(0), (b0 - start) / cost)); h < g.a.Hkv && ok; ++h) {
         const int64_t S = start + h * cost;
         if (S >= b1) break;
         const int t0 = chunk_tiles_before(b0 - S, p), t1 = chunk_tiles_before(b1 - S, p);
         if (t0 >= t1) continue;
-        if (t0 == 0 && t1 < p.tiles) piece = PieceInfo{b, h, 0, 0};
+        if (t0 == 0 && t1 < p.tiles) {
+          piece = PieceInfo{b, h, 0, p.rows, p.chunk, p.local, p.query0, p.row};
+          piece_end = S + cost - p.tile_cost;
+        }
         ChunkSegment s = {};
         s.tiles = t1 - t0; s.block = b; s.kvh = h; s.rows = p.rows;
         s.dest = t0 == 0 && t1 == p.tiles ? -1 : 2 * static_cast<int>(blockIdx.x) + (t0 > 0 ? 0 : 1);
         s.from = t0; s.head = p.head; s.skip = p.first - p.head;
         s.clean = max(p.clean, p.first) - s.skip - t0;
         s.clean_end = p.clean_end - s.skip - t0;
-        s.query0 = p.query0; s.row = p.row; s.local = p.local; s.sinks = sinks;
+        s.query0 = p.query0; s.row = p.row; s.local = p.local; s.sinks = p.sinks;
         announce(s);
         copy();
         last = s;
-        last_tile0 = tile0;
+        last_tile0 = p.tile0;
       }
     }
   }
+  // the last tile is that of the last CTA whose share begins before it or there
+  if (piece.block >= 0) piece.ctas = static_cast<int>(min(static_cast<int64_t>(g.ctas), piece_end / per + 1)) - static_cast<int>(blockIdx.x);
   if (lane == 0) g.piece[blockIdx.x] = piece;
   announce(ChunkSegment{});  // no more
   copy();
@@ -356,6 +357,24 @@ __device__ __forceinline__ void put_words(uint32_t col, const uint32_t (&p)[N]) 
   if constexpr (FROM + W < N) put_words<N, FROM + W>(col, p);
 }
 
+// v[j] of lane 4 g + i becomes v[i] of lane 4 g + j.
+__device__ __forceinline__ void turn4(uint32_t (&v)[4][4], int lane) {
+#pragma unroll
+  for (int s = 1; s < 4; s <<= 1) {
+    const bool up = lane & s;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k & s) continue;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t a = v[k][u], b = v[k | s][u], got = __shfl_xor_sync(0xffffffffu, up ? a : b, s);
+        v[k][u] = up ? got : a;
+        v[k | s][u] = up ? b : got;
+      }
+    }
+  }
+}
+
 // The softmax warps of a half, a thread a row.
 //
 // A row's reference m only has to keep its weights within binary16, and its first tile's maximum does for most of the
@@ -372,33 +391,9 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
   int segs = 0, it = 0, joins = 0;
   float f = 0.f;
-  // The row's query into shared memory as binary16, scaled by the power of two that brings its largest element to [1, 2).
-  auto put_q = [&](const uint4 (&w)[D / 8]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) top = max(top, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
-    }
-    int e = top == 0 || top >= 0x7F80u ? 0 : static_cast<int>(top >> 7) - 127;
-    e = max(-100, min(120, e));
-    const float down = __int_as_float((127 - e) << 23);
-    uint8_t* to = x.base + half * L::kQ;
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-      uint32_t o[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = pack16(false, bf16lo(v[k]) * down, bf16hi(v[k]) * down);
-      *reinterpret_cast<uint4*>(to + tile_at(kHalfRows, row, i)) = make_uint4(o[0], o[1], o[2], o[3]);
-    }
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(x.q_full(half));
-    return fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
-  };
-  // The rows of run k into shared memory, if the half has a tile of it; the factor from products to base-2 exponents.
+  // The rows of run k into shared memory, if the half has a tile of it, as binary16 and scaled by the power of two that
+  // brings a row's largest element to [1, 2); the factor from products to base-2 exponents.  Whole lines at a time, as
+  // rows are stored: with a row a lane, 32 lines an access, a run's end took 5000 cycles at d 64 and up to 10,000 at 128.
   auto load_rows = [&](int k) -> bool {
     const int slot = k % kRunSlots;
     if (!x.wait(x.seg_full(slot), (k / kRunSlots) & 1)) return false;
@@ -406,10 +401,37 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     if (x.seg(slot).tiles <= (turns ? half : 0)) return true;
     if (!x.wait(x.rows_full(slot), (k / kRunSlots) & 1)) return false;
     const int at = x.rows(slot)[(turns ? 0 : half * kHalfRows) + row].at;
-    uint4 w[D / 8];
+    // 16 bytes a lane, consecutive lanes along a row
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+    const int sub = lane / kLanes, chunk = lane % kLanes;
+    uint4 w[kLanes];
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) w[i] = at >= 0 ? reinterpret_cast<const uint4*>(g.q + static_cast<int64_t>(at) * D)[i] : make_uint4(0, 0, 0, 0);
-    f = put_q(w);
+    for (int i = 0; i < kLanes; ++i) {
+      const int from = __shfl_sync(0xffffffffu, at, i * kRows + sub);
+      w[i] = from >= 0 ? reinterpret_cast<const uint4*>(g.q + static_cast<int64_t>(from) * D)[chunk] : make_uint4(0, 0, 0, 0);
+    }
+    int e = 0;
+#pragma unroll
+    for (int i = 0; i < kLanes; ++i) {
+      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+      uint32_t o[4], top = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = __vmaxu2(top, v[k] & 0x7FFF7FFFu);
+      top = max(top & 0xFFFFu, top >> 16);
+#pragma unroll
+      for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const int of_row = top == 0 || top >= 0x7F80u ? 0 : max(-100, min(120, static_cast<int>(top >> 7) - 127));
+      const float down = __int_as_float((127 - of_row) << 23);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = pack16(false, bf16lo(v[k]) * down, bf16hi(v[k]) * down);
+      *reinterpret_cast<uint4*>(x.base + half * L::kQ + tile_at(kHalfRows, quad * 32 + i * kRows + sub, chunk)) = make_uint4(o[0], o[1], o[2], o[3]);
+      const int mine = __shfl_sync(0xffffffffu, of_row, lane % kRows * kLanes);
+      if (lane / kRows == i) e = mine;
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(x.q_full(half));
+    f = fmaxf(g.scale_log2 * __int_as_float((127 + e) << 23), 1.17549435e-38f);
     return true;
   };
 
@@ -534,8 +556,9 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       tc_fence_before();
       continue;
     }
-    const int64_t slot = static_cast<int64_t>(dest) * kBlockRows + first_row + row;
-    uint16_t* const out = g.out + static_cast<int64_t>(at) * D;
+    int to[4];  // rows of the lane and its three neighbours
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[k] = __shfl_sync(0xffffffffu, at, (lane & ~3) + k);
     float by = 1.f, other = 0.f, inv = 0.f;  // weights of the halves' sums
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -559,22 +582,23 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       }
       if (c == 0) {
         inv = l != 0.f ? 1.f / l : 0.f;
-        if (mine && dest >= 0) g.part_ml[slot] = make_float2(m, l);
+        if (mine && dest >= 0) g.part_ml[static_cast<int64_t>(dest) * kBlockRows + first_row + row] = make_float2(m, l);
         if (mine && dest < 0 && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
-      if (!mine) continue;
       if (dest >= 0) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 8) st_global8(g.part_o + slot * D + 32 * c + k, reinterpret_cast<const float*>(o + k));
+        for (int k = 0; k < 32; k += 4)
+          if (mine) *part_at<D>(g, dest, 8 * c + k / 4, first_row + row) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
       } else {
+        uint32_t v[4][4];
 #pragma unroll
-        for (int k = 0; k < 32; k += 16) {
-          uint32_t v[8];
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int u = 0; u < 8; ++u) v[u] = pack16(true, __uint_as_float(o[k + 2 * u]) * inv, __uint_as_float(o[k + 2 * u + 1]) * inv);
-          *reinterpret_cast<uint4*>(out + 32 * c + k) = make_uint4(v[0], v[1], v[2], v[3]);
-          *reinterpret_cast<uint4*>(out + 32 * c + k + 8) = make_uint4(v[4], v[5], v[6], v[7]);
-        }
+          for (int u = 0; u < 4; ++u) v[k][u] = pack16(true, __uint_as_float(o[8 * k + 2 * u]) * inv, __uint_as_float(o[8 * k + 2 * u + 1]) * inv);
+        turn4(v, lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (to[k] >= 0) *reinterpret_cast<uint4*>(g.out + static_cast<int64_t>(to[k]) * D + 32 * c + 8 * (lane & 3)) = make_uint4(v[k][0], v[k][1], v[k][2], v[k][3]);
       }
     }
     tc_fence_before();

@@ -66,11 +66,11 @@ __device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* warp_sums, in
 }
 
 __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __grid_constant__ ChunkArgs g) {
-  __shared__ int s_bad, s_lo, s_count[2], s_warp[2][kPlanChunkThreads / 32], s_before[4][kClasses], s_last;
+  __shared__ int s_bad, s_lo, s_before[4][kClasses], s_last;
   __shared__ int64_t s_sums[kPlanChunkThreads / 32];
   const LayerArgs& a = g.a;
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) s_bad = 0, s_lo = INT_MAX, s_count[0] = s_count[1] = 0;
+  if (tid == 0) s_bad = 0, s_lo = INT_MAX;
   pdl_wait();
   pdl_trigger();
   __syncthreads();
@@ -100,43 +100,34 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     chunk_fail(g, q, TRR_ERR_INVALID_ARG);
     return 2;
   };
-  int full = 0, local = 0, lo = INT_MAX;
-  for (int k = tid; k < len; k += kPlanChunkThreads) {
+  // A thread takes some queries in a row, twice: to count each kind, and to put them in their places, queries of one kind
+  // behind another, each kind in order.  (Short code: in a small call each first pass of an instruction costs.)
+  const int share = (len + kPlanChunkThreads - 1) / kPlanChunkThreads, first = min(len, tid * share), last = min(len, first + share);
+  constexpr int kCount = 21;  // bits of a count
+  static_assert(kMostChunkTokens < 1 << kCount, "");
+  int64_t kinds = 0, all = 0;
+  int lo = INT_MAX;
+#pragma unroll 1
+  for (int k = first; k < last; ++k) {
     int w = 0;
     const int kind = kind_of(k, &w);
-    full += kind == 0;
-    local += kind == 1;
+    kinds += 1ll << (kCount * kind);
     if (kind == 1) lo = min(lo, max(0, start + k - w + 1));
   }
-  full = __reduce_add_sync(0xffffffffu, full);
-  local = __reduce_add_sync(0xffffffffu, local);
   lo = __reduce_min_sync(0xffffffffu, lo);
-  if (lane == 0) {
-    atomicAdd(&s_count[0], full);
-    atomicAdd(&s_count[1], local);
-    atomicMin(&s_lo, lo);
-  }
-  __syncthreads();
-  full = s_count[0];
-  local = s_count[1];
-  // queries of one kind behind another, each kind in order
-  int done[3] = {0, full, full + local};
-  for (int k0 = 0; k0 < len; k0 += kPlanChunkThreads) {
-    const int k = k0 + tid;
+  if (lane == 0) atomicMin(&s_lo, lo);
+  const int64_t before = scan_before(kinds, s_sums, &all);
+  auto count = [](int64_t x, int kind) { return static_cast<int>(x >> (kCount * kind) & ((1 << kCount) - 1)); };
+  const int full = count(all, 0), local = count(all, 1);
+  int place[3] = {row0 + count(before, 0), row0 + full + count(before, 1), row0 + full + local + count(before, 2)};
+#pragma unroll 1
+  for (int k = first; k < last; ++k) {
     int w = 0;
-    const int kind = k < len ? kind_of(k, &w) : 3;
-    const uint32_t below = (1u << lane) - 1;
-    const uint32_t b0 = __ballot_sync(0xffffffffu, kind == 0), b1 = __ballot_sync(0xffffffffu, kind == 1), b2 = __ballot_sync(0xffffffffu, kind == 2);
-    if (lane == 0) s_warp[0][warp] = __popc(b0) | __popc(b1) << 16, s_warp[1][warp] = __popc(b2);
-    __syncthreads();
-    int at[3] = {done[0], done[1], done[2]};
-    for (int v = 0; v < kPlanChunkThreads / 32; ++v) {
-      const int x = s_warp[0][v], y = s_warp[1][v];
-      if (v < warp) at[0] += x & 0xFFFF, at[1] += x >> 16, at[2] += y;
-      done[0] += x & 0xFFFF, done[1] += x >> 16, done[2] += y;
-    }
-    if (kind < 3) g.list[row0 + (kind == 0 ? at[0] + __popc(b0 & below) : kind == 1 ? at[1] + __popc(b1 & below) : at[2] + __popc(b2 & below))] = row0 + k;
-    __syncthreads();
+    const int kind = kind_of(k, &w);
+    g.list[kind == 0 ? place[0] : kind == 1 ? place[1] : place[2]] = row0 + k;
+    place[0] += kind == 0;
+    place[1] += kind == 1;
+    place[2] += kind == 2;
   }
   // the positions in sight of any query, and the tokens stored there
   const bool reads = full + local > 0;

@@ -125,7 +125,8 @@ __device__ __forceinline__ int last_not_above(int n, T x, int lane, Value value)
 }
 
 // The cost of a segment, in sixteenths of a tile (2000 cycles at d 64): its tiles, those with rows hidden a little dearer
-// (2250), and a fixed part for its start and end (5000 to 10,000).  Where the halves take turns (blocks of 128 rows or fewer)
+// (2250), and a fixed part for its start and end (4500 to 8000; with 30 sixteenths 4096 queries on themselves took 155 us
+// against 144 with 60).  Where the halves take turns (blocks of 128 rows or fewer)
 // two tiles take 2600 cycles at d 64, but 4300 at d 128, whose three staged tiles leave neither half one ahead.  With a fixed
 // part of one tile and all tiles alike, 4096 queries on themselves, 32 heads of 64, took 202 us against 144, as the CTAs with
 // the shortest segments came in last; with turns at the price of whole tiles, ragged chunks of d 64 took 402 us against 378;

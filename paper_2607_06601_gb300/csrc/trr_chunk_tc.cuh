@@ -13,7 +13,7 @@
 // loads from TMEM, weights and stores about 1900, which is what a tile takes: at 4096 queries on themselves, 32
 // heads of 64 (four fifths of the tokens stored), 91 us, 0.60 PFLOP/s, the tensor pipe busy for 27 % of it.  At d 128
 // a product of 128 x 80 x 16 from shared memory takes 54 cycles of its bandwidth, 1506 a tile with those of P V;
-// measured 1880: 2048 queries of 32 heads at the end of 32,768 tokens, 555 us, 1.54 PFLOP/s.
+// measured 1880: 2048 queries of 32 heads at the end of 32,768 tokens, 546 us, 1.56 PFLOP/s.
 //
 // What this layout is for: from a product's end to the issue of one that waits for it pass about 450 cycles
 // (completion, barrier, wait, issue).  So no product waits for another: scores, weights and sums have columns of
@@ -393,7 +393,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   float f = 0.f;
   // The rows of run k into shared memory, if the half has a tile of it, as binary16 and scaled by the power of two that
   // brings a row's largest element to [1, 2); the factor from products to base-2 exponents.  Whole lines at a time, as
-  // rows are stored: with a row a lane, 32 lines an access, a run's end took 5000 cycles at d 64 and up to 10,000 at 128.
+  // rows are stored: with a row a lane, 32 lines an access, a run's end took 5500 cycles at d 64 and up to 10,000 at 128; now 4500 and 7000.
   auto load_rows = [&](int k) -> bool {
     const int slot = k % kRunSlots;
     if (!x.wait(x.seg_full(slot), (k / kRunSlots) & 1)) return false;

@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     if (!whole) {
       h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units); h.tiles = static_cast<int>(tiles);
       const int stagers = kStageCtas * g.ctas;
-      h.splits = units > 0 ? shares_of(units, (a.Hkv + 1) / 2, stagers, copy_ns(5ll * a.Hkv * a.d, stagers)) : 1;
+      h.splits = units > 0 ? shares_of_heads(units, (a.Hkv + 1) / 2, stagers, copy_ns(5ll * a.Hkv * a.d, stagers)) : 1;
     }
     *g.head = h;
     const int e = atomicExch(a.ctrl + kChunkBad, 0);

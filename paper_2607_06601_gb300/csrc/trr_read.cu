@@ -10,14 +10,14 @@
 // average) and leaves as 256.  A warp takes one head's K and V rows of a class at a time, 16 values a
 // lane, consecutive lanes along a row, so that whole lines are written.
 //
-// 65,536 rows of 12 heads of 64 in bf16 take 59 us, 40,000 of 32 heads in binary32 146 us (DRAM 5.0
-// TB/s, 107 MB read and 622 written), 131,072 of 8 heads of 128 in bf16 131 us; a copy of as many
+// With cold caches 65,536 rows of 12 heads of 64 in bf16 take 65 us, 40,000 of 32 heads in binary32 151 us (DRAM
+// 5.0 TB/s, 107 MB read and 622 written), 131,072 of 8 heads of 128 in bf16 131 us; a copy of as many
 // bytes 40, 114 and 96.  What is left are the searches before a CTA's first rows (5 us in which
-// nothing is written), the last round and the loads' latency under so many stores.  Two heads' loads
-// ahead at 80 registers and three CTAs an SM gave 71, 149 and 132 us with cold caches where this gives
-// 69, 153 and 138.
+// nothing is written) and the loads' latency under so many stores.  Two heads' loads ahead at 80 registers
+// and three CTAs an SM were no gain: 71, 149 and 132 us where one head's at four CTAs then took 69, 153 and 138.
 #include <algorithm>
 #include <climits>
+#include <cstdint>
 
 #include "trr_span.cuh"
 
@@ -28,7 +28,7 @@ constexpr int kReadCtas = 4;  // CTAs on an SM
 
 struct ReadArgs {
   LayerArgs a;
-  int n, rows, splits;  // stretches, rows of the outputs, shares of the KV heads that CTAs take
+  int n, rows, span, splits;  // stretches, rows of the outputs; how many of them, and shares of the KV heads, CTAs take
   const int32_t *seq_ids, *starts, *offsets;
   void *k, *v;
   uint8_t* bits;
@@ -177,11 +177,11 @@ __global__ void __launch_bounds__(kSpanThreads, kReadCtas) read_kernel(const __g
       else if (start < 0 || start > a.maxctx - len) fail(x, TRR_ERR_BAD_POSITION);
     }
   }
-  const int units = (g.rows + kSpan - 1) / kSpan * g.splits, per = (a.Hkv + g.splits - 1) / g.splits;
+  const int units = (g.rows + g.span - 1) / g.span * g.splits, per = (a.Hkv + g.splits - 1) / g.splits;
   const int row_end = bad ? g.rows : g.offsets[g.n], row_begin = bad ? 0 : g.offsets[0];
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
-    const int row = u / g.splits * kSpan + i, h0 = u % g.splits * per, h1 = min(a.Hkv, h0 + per);
-    const bool mine = row >= row_begin && row < row_end;
+    const int row = u / g.splits * g.span + i, h0 = u % g.splits * per, h1 = min(a.Hkv, h0 + per);
+    const bool mine = i < g.span && row >= row_begin && row < row_end;
     Place p{0, -1, 0};
     if (mine && !bad) {
       int lo = 0, hi = g.n - 1;  // the last stretch that starts at the row or before it
@@ -211,6 +211,27 @@ __global__ void __launch_bounds__(kSpanThreads, kReadCtas) read_kernel(const __g
   }
 }
 
+// How the rows are cut into units: some of them (48 to 64) of a share of the heads.  With the heads in s shares a unit has
+// as many rows as fill the fewest rounds of `ctas` CTAs evenly; of all s the one that takes least, where 64 rows of all
+// heads take `whole` ns among as many others and a unit 5 us more to find its tokens.  Cold caches, against units of 64
+// rows always: 65,536 rows of 12 heads of 64 in bf16 65 us against 69 (2 rounds of 54 rows, the second one was 0.7 full),
+// 131,072 of 8 heads of 128 130 against 138; with 32 rows as the least, 40,000 of 32 heads in binary32 157 against 153.
+struct Shares {
+  int span, splits;  // rows; shares of the heads
+};
+static Shares shares_of(int64_t rows, int heads, int ctas, int64_t whole) {
+  constexpr int64_t kLeastSpan = 48;
+  Shares best = {kSpan, 1};
+  int64_t least = INT64_MAX;
+  for (int s = 1; s <= (heads + 1) / 2; ++s) {
+    const int64_t units = (rows + kSpan - 1) / kSpan, rounds = (units * s + ctas - 1) / ctas, room = rounds * ctas / s;
+    const int64_t span = std::max(kLeastSpan, (rows + room - 1) / room), per = (heads + s - 1) / s;
+    const int64_t t = rounds * (whole * span * per / (kSpan * heads) + 5000);
+    if (t < least) best = Shares{static_cast<int>(span), s}, least = t;
+  }
+  return best;
+}
+
 }  // namespace trr
 
 using namespace trr;
@@ -235,11 +256,13 @@ extern "C" trr_status trr_kv_read(trr_cache* cache, int32_t layer, int32_t n, co
   g.k_stride = k_stride; g.v_stride = v_stride;
   g.sectors = ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out) | static_cast<uint64_t>(k_stride * unit_bytes) |
                 static_cast<uint64_t>(v_stride * unit_bytes)) & 31) == 0;
-  const int sms = cache_num_sms(cache), spans = (num_rows - 1) / kSpan + 1;
+  const int sms = cache_num_sms(cache);
   // (half a byte a value in, on average)
   const int64_t bytes = 2 * row * unit_bytes + row;
-  g.splits = shares_of(spans, (l.Hkv + 1) / 2, kReadCtas * sms, copy_ns(bytes, kReadCtas * sms));
-  const int64_t units = static_cast<int64_t>(spans) * g.splits;
+  const Shares shares = shares_of(num_rows, l.Hkv, kReadCtas * sms, copy_ns(bytes, kReadCtas * sms));
+  g.span = shares.span;
+  g.splits = shares.splits;
+  const int64_t units = static_cast<int64_t>((num_rows - 1) / g.span + 1) * g.splits;
   g.lg_parts = lg_parts((l.Hkv + g.splits - 1) / g.splits);
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(units, kReadCtas * sms)));
   auto kernel = l.d == 64 ? (type == TRR_BF16 ? read_kernel<64, uint16_t> : read_kernel<64, float>)

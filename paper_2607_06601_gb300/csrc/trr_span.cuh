@@ -16,7 +16,7 @@
 
 namespace trr {
 
-constexpr int kSpan = 64;            // positions that a CTA takes at a time
+constexpr int kSpan = 64;            // positions that a CTA takes at a time (reading back: at most)
 constexpr int kSpanThreads = 4 * kSpan;
 constexpr int kMostSpans = 4096;     // stretches of a call
 
@@ -181,13 +181,15 @@ __device__ __forceinline__ void for_groups(const Found<ROWS>& f, int lg_parts, i
 __host__ __device__ inline int lg_parts(int heads) { return heads >= 8 ? 2 : heads >= 4 ? 1 : 0; }
 
 // Shares of the heads that a unit (64 positions) is cut into: as many as make the rounds of `ctas` CTAs shortest, where
-// a unit whole takes `whole` ns among as many others, and each share 5 us more to find its tokens.  Measured on 40,000
-// rows of 32 heads of 64 in binary32: 169 us with whole units (637 for 608 CTAs), 153 with quarters.
-__host__ __device__ inline int shares_of(int64_t units, int most, int ctas, int64_t whole) {
+// a unit whole takes `whole` ns among as many others, and each share 5 us more to find its tokens.  Measured where
+// 40,000 rows of 32 heads of 64 are read back in binary32: 169 us with whole units (637 for 608 CTAs), 153 with quarters.
+// Units of fewer positions, as reading back has them, were no gain here: the longer plan took what they gave.
+__device__ __forceinline__ int shares_of_heads(int64_t units, int most, int ctas, int64_t whole) {
   int best = 1;
-  int64_t least = 0;
-  for (int s = 1; s <= most; ++s) {
-    const int64_t rounds = (units * s + ctas - 1) / ctas, t = rounds * (whole / s + 5000);
+  float least = 0.f;
+#pragma unroll 1
+  for (int s = 1; s <= most; ++s) {  // (a choice only: no more than binary32)
+    const float t = ceilf(static_cast<float>(units) * s / ctas) * (static_cast<float>(whole) / s + 5000.f);
     if (s == 1 || t < least) best = s, least = t;
   }
   return best;

@@ -389,7 +389,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
-  int segs = 0, it = 0, joins = 0;
+  int it = 0, joins = 0;
   float f = 0.f;
   // The rows of run k into shared memory, if the half has a tile of it, as binary16 and scaled by the power of two that
   // brings a row's largest element to [1, 2); the factor from products to base-2 exponents.  Whole lines at a time, as
@@ -435,12 +435,14 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     return true;
   };
 
-  if (!load_rows(0)) return;
-  for (;; ++segs) {
-    const ChunkSegment& sg = x.seg(segs % kRunSlots);
-    const int tiles = sg.tiles, clean = sg.clean, clean_end = sg.clean_end;
-    if (tiles == 0) return;
-    const int step = sg.rows <= kHalfRows ? 2 : 1, first = (step - 1) * half;  // 2: the halves have the same rows and take the tiles in turn
+  // (from -1: one place in the code brings rows, the first ones too, since what runs for the first time is waited for)
+#pragma unroll 1
+  for (int segs = -1;; ++segs) {
+    const bool begun = segs >= 0;
+    const ChunkSegment& sg = x.seg(begun ? segs % kRunSlots : 0);
+    const int tiles = begun ? sg.tiles : 0, clean = sg.clean, clean_end = sg.clean_end;
+    if (begun && tiles == 0) return;
+    const int step = begun && sg.rows <= kHalfRows ? 2 : 1, first = (step - 1) * half;  // 2: the halves have the same rows and take the tiles in turn
     float m = -INFINITY, l = 0.f;
     bool ready = false;    // the next scores are there
     bool settled = false;  // every row of the warp has a reference
@@ -527,10 +529,11 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     }
     const bool some = first < tiles;
     const bool turns = step == 2;
-    const int first_row = turns ? 0 : half * kHalfRows, dest = sg.dest, at = x.rows(segs % kRunSlots)[first_row + row].at;
+    const int first_row = turns ? 0 : half * kHalfRows, dest = sg.dest, at = begun ? x.rows(segs % kRunSlots)[first_row + row].at : -1;
     const bool mine = at >= 0;
     // the next run's rows, while this one's last product runs (its scores are all in: Q's place is free)
     if (!load_rows(segs + 1)) return;
+    if (!begun) continue;
     // rows out: the output itself, or (m, l, o) for the join of pieces
     if (some) {
       if (!x.wait(x.o_done(half), (it - 1) & 1)) return;

@@ -17,11 +17,11 @@
 //                        l' = sum l 2^(m - m'), and so for o.
 //
 // Alone, from cold caches, in us (plan, stage, attention, join): one chunk of 512 queries of 12 heads on 2048 tokens
-// 13, 12, 19, 9; 32 chunks of 8 on 2048 tokens of 12 heads 11, 57, 45, 6; 4096 queries on themselves, 32 heads of 64,
-// 16, 20, 91 to 95, 11; 2048 at the end of 32,768 tokens, 8 KV heads of 128, 12, 37, 546, 16.  Plan and join are chains
+// 11, 12, 18, 9; 32 chunks of 8 on 2048 tokens of 12 heads 11, 56, 44, 6; 4096 queries on themselves, 32 heads of 64,
+// 15, 21, 91 to 97, 12; 2048 at the end of 32,768 tokens, 8 KV heads of 128, 11, 36, 540, 16.  Plan and join are chains
 // of dependent loads and of code that is read for the first time; a launch's start hides behind its forerunner's end.
-//   Staging is bound by the memory: 4.5 bits a value in and 16 out.  The 32 chunks above write 201 MB in 57 us, 4 TB/s
-// with what is read, as reading back does, and the attention reads it at 4.5 TB/s.  Four CTAs an SM, a head's loads
+//   Staging is bound by the memory: 4.5 bits a value in and 16 out.  The 32 chunks above write 201 MB in 56 us, 4 TB/s
+// with what is read, as reading back does, and the attention reads it at 4.6 TB/s.  Four CTAs an SM, a head's loads
 // ahead: with two or three heads ahead that call took 151 and 163 us against 130, with 3 CTAs an SM 145 (registers
 // spilled), with 5 no less.
 //

@@ -9,7 +9,7 @@ import torch
 
 from _parity import check_attention, dev
 from _shared import Holder
-from paper_2607_06601_gb300 import workloads as wl
+from paper_2607_06601_gb300 import trr, workloads as wl
 from test_gpu_chunk import LAYOUTS, call, check, fill, holder, truth
 
 pytestmark = pytest.mark.gpu
@@ -213,3 +213,10 @@ def test_short_blocks_whose_tiles_come_in_any_order(lay, new):
             cold.fill_(i)
         assert torch.equal(h.gpu.chunk_attn(*call_args, window_scalar=300, sinks=4), out), i
     assert h.gpu.status() == 0
+
+
+def test_more_rows_than_32_bits_count_are_refused():
+    c = trr.Cache(1, 1, 2048, 1, 64, 64, 16, 64, [4] * 4, max_append=16, max_queries=1)
+    with pytest.raises(trr.TrrError):
+        trr.trr_chunk_workspace_bytes(c.handle, 1, 1 << 20, 64)
+    assert trr.trr_chunk_workspace_bytes(c.handle, 1, (1 << 20) - 1, 64) > 0

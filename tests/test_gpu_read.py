@@ -124,6 +124,22 @@ def test_many_stretches_of_one_position():
     check(h, 0, [1] * 900, starts, [1] * 900)
 
 
+@pytest.mark.parametrize("lay", LAYOUTS[1:4:2])
+def test_many_rows(lay):
+    """As many rows as make units of 48 to 64 positions and one, two and more of them a CTA; the same rows all along."""
+    rng = np.random.default_rng(8)
+    h = holder(lay, S=1)
+    h.append(rng, 0, 0, np.arange(131), p_skip=0.2)
+    want = truth(h, 0, [0], [0], [131])
+    for times in (220, 250, 280, 297, 430, 600):
+        n = 131 * times
+        k, v, bits = h.gpu.read(0, h.ints([0] * times), h.ints([0] * times), h.ints(np.arange(times + 1) * 131), n, dtype=torch.float32)
+        assert h.gpu.status() == 0
+        for got, ref in ((k, want[0]), (v, want[1]), (bits, want[2])):
+            ref = torch.from_numpy(ref.astype(np.uint8 if got is bits else np.float32)).cuda()
+            assert torch.equal(got.view(times, 131, *got.shape[1:]), ref.expand(times, *ref.shape))
+
+
 def test_values_far_apart_and_not_finite():
     """Scales from binary16's smallest to its largest; 16-bit rows that hold infinities and NaN."""
     rng = np.random.default_rng(7)

@@ -377,15 +377,19 @@ __device__ __forceinline__ void turn4(uint32_t (&v)[4][4], int lane) {
 
 // The softmax warps of a half, a thread a row.
 //
-// A row's reference m only has to keep its weights within binary16, and its first tile's maximum does for most of the
-// tiles that follow: their weights are taken by it at once, without a maximum of their own, and a sum above 2^15 tells
-// that the reference has to move.
+// A row's reference m only has to keep its weights within binary16, and one from its first tile's maximum does for most
+// of the tiles that follow: their weights are taken by it at once, without a maximum of their own, and a sum above
+// binary16's largest value tells that the reference has to move.  It stands kRoom below the maximum (in base 2): binary16
+// has steps of 2^-24 at its low end, so a weight is off by 2^-11 of itself or by 2^-33 of the largest one.  With the maximum
+// itself as the reference, weights 17 nats below it were half lost, all of what a token that draws much of a row's weight
+// (and adds little to its sum) leaves to the others.  A tile's weights then sum to 96 x 2^8 at most where it has just moved.
 template <int D>
 __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx<D>& x, int half, int quad, int lane) {
   using L = ChunkSmem<D>;
   using C = ChunkCtx<D>;
   constexpr int T = L::kT, A = C::kPartA, B = C::kPartB;
-  constexpr float kMost = 32768.f;
+  constexpr float kMost = 65504.f, kRoom = 8.f;
+  static_assert(T * 256 < 65504, "");
   const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
   const uint32_t col_s = x.col_s(half) + lanes, col_p = x.col_p(half) + lanes, col_o = x.col_o(half) + lanes;
@@ -477,9 +481,9 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         hide<0>(a, seen);
         hide<A>(b, seen);
       }
-      // where it must, the reference moves up to `top`, O with it (rows that need not stay as they are, bit for bit)
+      // where it must, the reference moves up to kRoom below `top`, O with it (rows that need not stay as they are, bit for bit)
       auto move = [&](bool must, float top) -> bool {
-        const float next = must ? fmaxf(m, top) : m;
+        const float next = must ? fmaxf(m, top - kRoom) : m;
         const float by = m == next ? 1.f : exp2_approx(m - next);
         l *= by;
         m = next;

@@ -1,0 +1,78 @@
+"""How near rows and logarithms of attention of chunks come to the definition.
+
+Scores here are exact: K has one channel that is not zero, q is 1 there, both are numbers that binary16 holds, so that
+only weights, V and sums are rounded.  Then an element of a row is off by
+  2^-8 of itself: half a step of bf16;
+  2^-11 sum w |v|: half a step of binary16 of each weight; V of 16 bits is exact unless it lies below 2^-14;
+  2^-33 w_top sum |v|, w_top the row's largest weight: half of binary16's smallest step, 2^-25, where a weight lies below
+  2^-14 of a reference that stands at 2^-8 of some weight of the row;
+  2^-12 sum w |v|: binary32 sums and exponentials."""
+import numpy as np
+import pytest
+import torch
+
+from _parity import dev
+from _shared import Holder
+from paper_2607_06601_gb300 import workloads as wl
+from test_gpu_chunk import call
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    torch.cuda.set_device(0)
+
+
+WIDE = [dict(Hq=4, Hkv=4, d=64, G=32, P=16), dict(Hq=8, Hkv=2, d=128, G=64, P=32)]
+
+
+def one_channel(n, heads, d, size):
+    """[n][heads][d] rows, `size` in channel 0 and zeros, as bf16 bits."""
+    x = np.zeros((n, heads, d), np.float32)
+    x[:, :, 0] = np.asarray(size, np.float32).reshape(-1, 1)
+    bits = wl.bf16_bits(x)
+    assert np.array_equal(wl.bf16_to_f32(bits), x)
+    return bits
+
+
+def exact_rows(h, scores, v, starts_at, new):
+    """Rows of full queries at positions starts_at .. over scores[n] (the same for all queries and heads) and v [n][Hkv][d];
+    what the weights add up |v| to, and w_top sum |v|."""
+    x, w = np.repeat(v, h.Hq // h.Hkv, axis=1), np.exp(scores - scores.max())
+    rows, total = np.s_[starts_at:starts_at + new], w.cumsum()
+    over = lambda y: y.cumsum(0)[rows] / total[rows, None, None]  # noqa: E731
+    top = np.maximum.accumulate(w)[rows] / total[rows]
+    return over(w[:, None, None] * x), over(w[:, None, None] * np.abs(x)), top[:, None, None] * np.abs(x).cumsum(0)[rows]
+
+
+def within(got, ref, spread, most, extra=0.0):
+    off = np.abs(got.double().cpu().numpy() - ref)
+    bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -12) * spread + 2.0 ** -33 * most + extra
+    assert (off <= bound).all(), f"{(off / np.maximum(bound, 1e-300)).max():.2f} times the bound"
+
+
+@pytest.mark.parametrize("top", [8, 12, 15, 17, 18, 20])
+@pytest.mark.parametrize("lay,n,new", [(WIDE[0], 250, 20), (WIDE[0], 270, 200), (WIDE[1], 230, 10), (WIDE[1], 220, 150),
+                                       (dict(Hq=32, Hkv=8, d=64, G=64, P=32), 3000, 1000)])
+def test_weights_far_below_a_first_token_that_adds_nothing(lay, n, new, top):
+    """A first token that draws most of each row's weight and has V = 0, `top` nats above all others: the rows are what the
+    others' weights leave of them, in one run and over long ones."""
+    rng = np.random.default_rng([1, n, top])
+    h = Holder(1, 1, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], n, [n // lay["P"] + 2] * 4, archive=4)
+    scores = np.zeros(n)
+    scores[0] = top
+    v_bits = wl.bf16_bits((1.0 + 0.5 * rng.standard_normal((n, h.Hkv, h.d))).astype(np.float32))
+    v_bits[0] = 0
+    k_bits = one_channel(n, h.Hkv, h.d, scores)
+    for at in range(0, n, 1000):
+        part = slice(at, min(n, at + 1000))
+        h.append(rng, 0, 0, np.arange(n)[part], k=k_bits[part], v=v_bits[part], bits=np.full(n, 16)[part], p_skip=0.0)
+    q_bits = one_channel(new, h.Hq, h.d, np.ones(new))
+    out, lse, *_ = call(h, rng, [0], [n - new], [new], [2] * new, [1] * new, scale=1.0, q_bits=q_bits)
+    ref, spread, most = exact_rows(h, scores, wl.bf16_to_f32(v_bits).astype(np.float64), n - new, new)
+    within(out, ref, spread, most)
+    total = np.log(np.exp(scores - top).cumsum())[n - new:, None] + top
+    assert (np.abs(lse.double().cpu().numpy() - total) <= 2.0 ** -16).all()

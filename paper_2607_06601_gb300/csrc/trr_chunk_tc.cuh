@@ -79,6 +79,7 @@ struct ChunkCtx {
   uint32_t tmem;
   const ChunkArgs* args;  // (the kernel's own: read from there, not kept in registers)
   __device__ volatile int* abort_flag() const { return reinterpret_cast<volatile int*>(base + L::kAbort); }
+  __device__ volatile int* copied() const { return reinterpret_cast<volatile int*>(base + L::kAbort + 4); }  // tiles that the producer has asked for
   __device__ uint64_t* bar(int i) const { return reinterpret_cast<uint64_t*>(base + L::kBars) + i; }
   __device__ uint64_t* kv_full(int i) const { return bar(i); }
   __device__ uint64_t* kv_empty(int i) const { return bar(L::kSlots + i); }
@@ -108,6 +109,21 @@ struct ChunkCtx {
     for (uint64_t t0 = 0; !__all_sync(0xffffffffu, mbar_poll(addr, parity, args->a.wait_ns));) {
       const uint64_t now = global_ns();
       if (t0 == 0) t0 = now;
+      if (__any_sync(0xffffffffu, *abort_flag() || now - t0 >= args->a.wait_ns)) {
+        *abort_flag() = 1;
+        return false;
+      }
+    }
+    return true;
+  }
+  // The same for what comes behind the copies of all of a run's tiles, however many: the bound is on the time between two.
+  __device__ __forceinline__ bool wait_behind_copies(uint64_t* b, uint32_t parity) const {
+    const uint32_t addr = smem_u32(b);
+    uint64_t t0 = 0;
+    for (int before = -1; !__all_sync(0xffffffffu, mbar_poll(addr, parity, args->a.wait_ns));) {
+      const uint64_t now = global_ns();
+      const int tiles = *copied();
+      if (tiles != before) t0 = now, before = tiles;
       if (__any_sync(0xffffffffu, *abort_flag() || now - t0 >= args->a.wait_ns)) {
         *abort_flag() = 1;
         return false;
@@ -149,6 +165,7 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
         mbar_arrive_expect_tx(x.kv_full(slot), 2 * L::kTile);
         bulk_g2s(x.base + L::kK + slot * L::kTile, staged_tile<D>(g, tile, last.kvh, 0), L::kTile, x.kv_full(slot));
         bulk_g2s(x.base + L::kV + slot * L::kTile, staged_tile<D>(g, tile, last.kvh, 1), L::kTile, x.kv_full(slot));
+        *x.copied() = copies + 1;
       }
     }
   };
@@ -201,7 +218,7 @@ __device__ __forceinline__ void chunk_find_rows(const ChunkArgs& g, const ChunkC
   const int heads = g.a.Hq / g.a.Hkv;
   for (int segs = 0;; ++segs) {
     const int slot = segs % kRunSlots;
-    if (!x.wait(x.seg_full(slot), (segs / kRunSlots) & 1)) return;
+    if (!x.wait_behind_copies(x.seg_full(slot), (segs / kRunSlots) & 1)) return;  // (a run ahead of the others)
     const ChunkSegment& s = x.seg(slot);
     const int rows = s.rows, tiles = s.tiles, query0 = s.query0, row0 = s.row, head0 = s.kvh * heads;
     if (tiles == 0) return;
@@ -623,6 +640,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_attn_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     *x.abort_flag() = 0;
+    *x.copied() = 0;
     for (int i = 0; i < L::kSlots; ++i) mbar_init(x.kv_full(i), 1), mbar_init(x.kv_empty(i), 2);
     for (int i = 0; i < kRunSlots; ++i) mbar_init(x.seg_full(i), 1), mbar_init(x.seg_empty(i), kChunkSoftmaxWarps + 3), mbar_init(x.rows_full(i), 1);
     for (int h = 0; h < 2; ++h) {

@@ -395,17 +395,24 @@ __device__ __forceinline__ void turn4(uint32_t (&v)[4][4], int lane) {
 // The softmax warps of a half, a thread a row.
 //
 // A row's reference m only has to keep its weights within binary16, and one from its first tile's maximum does for most
-// of the tiles that follow: their weights are taken by it at once, without a maximum of their own, and a sum above
-// binary16's largest value tells that the reference has to move.  It stands kRoom below the maximum (in base 2): binary16
-// has steps of 2^-24 at its low end, so a weight is off by 2^-11 of itself or by 2^-33 of the largest one.  With the maximum
-// itself as the reference, weights 17 nats below it were half lost, all of what a token that draws much of a row's weight
-// (and adds little to its sum) leaves to the others.  A tile's weights then sum to 96 x 2^8 at most where it has just moved.
+// of the tiles that follow: their weights are taken by it at once, without a maximum of their own, and their sum tells
+// whether the reference has to move.  Up, where the sum passes binary16's largest value.  Down, where it shows weights that
+// binary16, whose steps end at 2^-24, is too coarse for: less than 2^-14 for each token in sight, or for each but the largest
+// in the first tile.  (Sums are binary32, so they may grow where the reference falls, by 2^60 at a time and not past 2^100.)
+// So a weight is off by 2^-11 of itself or of its tile's mean weight, however much a token elsewhere draws of the row.  With
+// the first maximum as the reference for good, a first token of V = 0 left rows 44 % off whose other tokens lay 17 nats below.
+//   The first reference stands 2^3 below the maximum, for other tokens of its tile than one that draws most of it.  At 2^8
+// below and with no way down references moved more often: ragged chunks took 409 us (384 so, 377 with the maximum for good),
+// 2048 queries at the end of 32,768 tokens 685 (654, 645).
 template <int D>
 __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx<D>& x, int half, int quad, int lane) {
   using L = ChunkSmem<D>;
   using C = ChunkCtx<D>;
   constexpr int T = L::kT, A = C::kPartA, B = C::kPartB;
-  constexpr float kMost = 65504.f, kRoom = 8.f;
+  constexpr float kMost = 65504.f, kSmall = 0x1p-14f;         // binary16's largest, and smallest of 11 bits
+  constexpr float kRoom = 3.f, kFirst = 8.f ;                 // a first reference's distance from the largest weight; that weight
+  constexpr float kRoomUp = 8.f, kRoomAlone = 15.f;           // of one moved up; of one whose largest weight stands alone
+  constexpr float kDown = 60.f, kGrown = 0x1p40f;             // a reference falls by so much at most, and no more once the row's sum is so large
   static_assert(T * 256 < 65504, "");
   const int row = quad * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quad) << 21;  // the warp's 32 lanes of TMEM
@@ -475,15 +482,17 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       tmem_ld(a, b, col_s);
       tc_fence_before();
       if (lane == 0) mbar_arrive(x.s_read(half));  // the next scores may come (the load was the whole warp's: no need to meet first)
+      float least = T * kSmall;  // of the weights' sum
       if (i < clean || i >= clean_end) {  // not every row sees the whole tile
         const int s = sg.from + i, before = (s + (s < sg.head ? 0 : sg.skip)) * T;
         const ChunkRow r = x.rows(segs % kRunSlots)[(2 - step) * half * kHalfRows + row];
-        const int hi = r.hi - before, lo = r.lo - before, sinks = sg.local ? sg.sinks - before : 0;
-        uint32_t seen[(T + 31) / 32], any = 0;
+        const int hi = min(T, r.hi - before), lo = r.lo - before, sinks = sg.local ? sg.sinks - before : 0;
+        uint32_t seen[(T + 31) / 32];
+        int any = 0;
 #pragma unroll
         for (int w = 0; w < (T + 31) / 32; ++w) {
           seen[w] = bits_below(hi, w) & (~bits_below(lo, w) | bits_below(sinks, w));
-          any |= seen[w];
+          any += __popc(seen[w]);
         }
         if (!__any_sync(0xffffffffu, any)) {  // none of the warp's rows sees any of it
           if (it > 0 && !x.wait(x.o_done(half), (it - 1) & 1)) return;
@@ -495,15 +504,15 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
           ready = false;
           continue;
         }
+        least = any * kSmall;
         hide<0>(a, seen);
         hide<A>(b, seen);
       }
-      // where it must, the reference moves up to kRoom below `top`, O with it (rows that need not stay as they are, bit for bit)
-      auto move = [&](bool must, float top) -> bool {
-        const float next = must ? fmaxf(m, top - kRoom) : m;
-        const float by = m == next ? 1.f : exp2_approx(m - next);
+      // the reference moves, O with it (rows whose own stays are as they were, bit for bit)
+      auto move = [&](float to) -> bool {
+        const float by = m == to ? 1.f : exp2_approx(m - to);
         l *= by;
-        m = next;
+        m = to;
         if (i == first) return true;
         if (!x.wait(x.o_done(half), (it - 1) & 1)) return false;
         tc_fence_after();
@@ -517,8 +526,11 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         }
         return true;
       };
+      bool begins = false;  // the row has its first reference from this tile
       if (!settled) {
-        if (!move(m == -INFINITY, fmaxf(highest(a), highest(b)) * f)) return;
+        const float top = fmaxf(highest(a), highest(b)) * f;
+        begins = m == -INFINITY && top != -INFINITY;
+        if (!move(begins ? top - kRoom : m)) return;
         settled = __all_sync(0xffffffffu, m != -INFINITY);
       }
       auto shift = [&] { return m == -INFINITY ? 0.f : -m; };
@@ -533,8 +545,10 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         sum += weights_of(b, q, f, shift());
         put_words(col_p + A / 2, q);
       }
-      if (__any_sync(0xffffffffu, sum > kMost)) {
-        if (!move(sum > kMost, fmaxf(highest(a), highest(b)) * f)) return;
+      const bool up = sum > kMost, down = l < kGrown && (begins ? sum - kFirst < least - kSmall : sum < least);
+      if (__any_sync(0xffffffffu, up || down)) {
+        const float top = fmaxf(highest(a), highest(b)) * f;
+        if (!move(up ? fmaxf(m, top - kRoomUp) : !down ? m : begins ? m + (kRoom - kRoomAlone) : fmaxf(top - kRoom, m - kDown))) return;
         sum = weights_of(a, p, f, shift());
         put_words(col_p, p);
         uint32_t q[B / 2];

@@ -76,3 +76,33 @@ def test_weights_far_below_a_first_token_that_adds_nothing(lay, n, new, top):
     within(out, ref, spread, most)
     total = np.log(np.exp(scores - top).cumsum())[n - new:, None] + top
     assert (np.abs(lse.double().cpu().numpy() - total) <= 2.0 ** -16).all()
+
+
+@pytest.mark.parametrize("top", [12, 17, 20, 60])
+@pytest.mark.parametrize("lay,n,new,at,window,sinks", [
+    (WIDE[0], 700, 20, [350], 0, 0), (WIDE[0], 700, 200, [1, 349, 520], 0, 0), (WIDE[1], 500, 150, [0, 260], 0, 0), (WIDE[0], 700, 150, [0], 150, 1),
+    (WIDE[1], 600, 20, [0], 170, 1), (dict(Hq=16, Hkv=4, d=128, G=64, P=64), 4000, 1000, [0, 2000], 0, 0)])
+def test_tokens_that_add_nothing_anywhere(lay, n, new, at, window, sinks, top):
+    """The same with such tokens within runs, with two of them, and with one that is kept in sight before a window."""
+    rng = np.random.default_rng([2, n, new, top])
+    h = Holder(1, 1, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], n, [n // lay["P"] + 2] * 4, archive=5)
+    scores = np.zeros(n)
+    scores[at] = top
+    v_bits = wl.bf16_bits((1.0 + 0.5 * rng.standard_normal((n, h.Hkv, h.d))).astype(np.float32))
+    v_bits[at] = 0
+    k_bits = one_channel(n, h.Hkv, h.d, scores)
+    for a in range(0, n, 1000):
+        part = slice(a, min(n, a + 1000))
+        h.append(rng, 0, 0, np.arange(n)[part], k=k_bits[part], v=v_bits[part], bits=np.full(n, 16)[part], p_skip=0.0)
+    q_bits = one_channel(new, h.Hq, h.d, np.ones(new))
+    out, lse, *_ = call(h, rng, [0], [n - new], [new], [1 if window else 2] * new, [max(1, window)] * new, sinks, scale=1.0, q_bits=q_bits)
+    v, w = wl.bf16_to_f32(v_bits).astype(np.float64), np.exp(scores - top)
+    t, pos = np.arange(n - new, n)[:, None], np.arange(n)
+    w = np.where((pos <= t) & ((window == 0) | (pos > t - window) | (pos < sinks)), w, 0.0)
+    total = w.sum(1)
+    over = lambda y: np.repeat(np.einsum("qt,thd->qhd", w / total[:, None], y, optimize=True), h.Hq // h.Hkv, axis=1)  # noqa: E731
+    # weights below 2^-14 of a reference: 2^-33 of the row's largest, or 2^-11 of the mean weight of its tile's other tokens,
+    # all of which weigh alike here, so that the bound on weights holds that too
+    seen = np.repeat(np.einsum("qt,thd->qhd", (w > 0).astype(float), np.abs(v), optimize=True), h.Hq // h.Hkv, axis=1)
+    within(out, over(v), over(np.abs(v)), (w.max(1) / total)[:, None, None] * seen)
+    assert (np.abs(lse.double().cpu().numpy() - (np.log(total) + top)[:, None]) <= 2.0 ** -16 + 2.0 ** -22 * top).all()

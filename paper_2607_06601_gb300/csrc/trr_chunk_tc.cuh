@@ -547,6 +547,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       }
       const bool up = sum > kMost, down = l < kGrown && (begins ? sum - kFirst < least - kSmall : sum < least);
       if (__any_sync(0xffffffffu, up || down)) {
+        tmem_wait_st();  // the weights stored above are stored again below: the first stores land first
         const float top = fmaxf(highest(a), highest(b)) * f;
         if (!move(up ? fmaxf(m, top - kRoomUp) : !down ? m : begins ? m + (kRoom - kRoomAlone) : fmaxf(top - kRoom, m - kDown))) return;
         sum = weights_of(a, p, f, shift());

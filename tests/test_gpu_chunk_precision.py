@@ -106,3 +106,27 @@ def test_tokens_that_add_nothing_anywhere(lay, n, new, at, window, sinks, top):
     seen = np.repeat(np.einsum("qt,thd->qhd", (w > 0).astype(float), np.abs(v), optimize=True), h.Hq // h.Hkv, axis=1)
     within(out, over(v), over(np.abs(v)), (w.max(1) / total)[:, None, None] * seen)
     assert (np.abs(lse.double().cpu().numpy() - (np.log(total) + top)[:, None]) <= 2.0 ** -16 + 2.0 ** -22 * top).all()
+
+
+@pytest.mark.parametrize("shape", ["up", "down", "up and down", "two steps"])
+@pytest.mark.parametrize("lay,new", [(WIDE[0], 20), (WIDE[0], 200), (WIDE[1], 20), (WIDE[1], 150)])
+def test_references_that_move_with_every_tile(lay, new, shape):
+    """Scores in steps of 24 every 40 tokens: each tile's weights are taken twice.  Bit for bit the same over calls, with the
+    tiles in memory and not."""
+    rng = np.random.default_rng([3, new])
+    n = 400
+    h = Holder(1, 1, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], n, [n // lay["P"] + 2] * 4, archive=2)
+    stair = np.arange(n) // 40
+    scores = 24.0 * {"up": stair, "down": 9 - stair, "up and down": np.minimum(stair, 9 - stair), "two steps": 4 * (stair % 2)}[shape]
+    v_bits = wl.bf16_bits(rng.standard_normal((n, h.Hkv, h.d), dtype=np.float32))
+    h.append(rng, 0, 0, np.arange(n), k=one_channel(n, h.Hkv, h.d, scores), v=v_bits, bits=np.full(n, 16), p_skip=0.0)
+    q_bits = one_channel(new, h.Hq, h.d, np.ones(new))
+    out, lse, *_ = call(h, rng, [0], [n - new], [new], [2] * new, [1] * new, scale=1.0, q_bits=q_bits)
+    ref, spread, most = exact_rows(h, scores, wl.bf16_to_f32(v_bits).astype(np.float64), n - new, new)
+    within(out, ref, spread, most)
+    cold = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")  # twice L2
+    for i in range(6):
+        if i % 2:
+            cold.fill_(i)
+        again = call(h, rng, [0], [n - new], [new], [2] * new, [1] * new, scale=1.0, q_bits=q_bits)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)

@@ -420,8 +420,9 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
   int it = 0, joins = 0;
   float f = 0.f;
   // The rows of run k into shared memory, if the half has a tile of it, as binary16 and scaled by the power of two that
-  // brings a row's largest element to [1, 2); the factor from products to base-2 exponents.  Whole lines at a time, as
-  // rows are stored: with a row a lane, 32 lines an access, a run's end took 5500 cycles at d 64 and up to 10,000 at 128; now 4500 and 7000.
+  // brings a row's largest element to [2^14, 2^15), so that elements down to 2^-28 of it keep their bits; the factor from
+  // products to base-2 exponents.  Whole lines at a time, as rows are stored: with a row a lane, 32 lines an access, a
+  // run's end took 5500 cycles at d 64 and up to 10,000 at 128; now 4500 and 7000.
   auto load_rows = [&](int k) -> bool {
     const int slot = k % kRunSlots;
     if (!x.wait(x.seg_full(slot), (k / kRunSlots) & 1)) return false;
@@ -448,7 +449,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       top = max(top & 0xFFFFu, top >> 16);
 #pragma unroll
       for (int d = 1; d < kLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-      const int of_row = top == 0 || top >= 0x7F80u ? 0 : max(-100, min(120, static_cast<int>(top >> 7) - 127));
+      const int of_row = top == 0 || top >= 0x7F80u ? 0 : max(-114, static_cast<int>(top >> 7) - (127 + 14));
       const float down = __int_as_float((127 - of_row) << 23);
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] = pack16(false, bf16lo(v[k]) * down, bf16hi(v[k]) * down);

@@ -130,3 +130,24 @@ def test_references_that_move_with_every_tile(lay, new, shape):
             cold.fill_(i)
         again = call(h, rng, [0], [n - new], [new], [2] * new, [1] * new, scale=1.0, q_bits=q_bits)
         assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("size", [-14, -20, -27])
+@pytest.mark.parametrize("lay", WIDE)
+def test_small_elements_of_queries_before_large_keys(lay, size):
+    """Query rows with one element of 1 and others far below it, over keys that are 0 at the one and large at the others: scores
+    as near as sum |scale q k| lets them be (half a step of binary16: 2^-11 of it).  A token in sight each, so that the
+    logarithm is the score; 2^-16 stands for exponentials and sums."""
+    rng = np.random.default_rng([4, -size])
+    n = 160
+    h = Holder(1, 1, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], n, [n // lay["P"] + 2] * 4, archive=2)
+    k, q = rng.standard_normal((n, h.Hkv, h.d)) * 2.0 ** 12, rng.standard_normal((n, h.Hq, h.d)) * 2.0 ** size
+    k[:, :, 5], q[:, :, 5] = 0.0, 1.0
+    k_bits, q_bits = wl.bf16_bits(k.astype(np.float32)), wl.bf16_bits(q.astype(np.float32))
+    h.append(rng, 0, 0, np.arange(n), k=k_bits, bits=np.full(n, 16), p_skip=0.0)
+    scale = 2.0 ** (-8 - size)
+    _, lse, *_ = call(h, rng, [0], [0], [n], [1] * n, [1] * n, scale=scale, q_bits=q_bits)
+    q, k = (wl.bf16_to_f32(x).astype(np.float64) for x in (q_bits, k_bits))
+    k = np.repeat(k, h.Hq // h.Hkv, axis=1)
+    off = np.abs(lse.double().cpu().numpy() - scale * (q * k).sum(-1))
+    assert (off <= 2.0 ** -11 * scale * np.abs(q * k).sum(-1) + 2.0 ** -16).all()

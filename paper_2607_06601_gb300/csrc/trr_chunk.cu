@@ -5,7 +5,7 @@
 //
 // A chunk's many queries read the same tokens, so those are brought back from their codes once, not
 // once for each block of rows:
-//   chunk_plan_kernel    a CTA per chunk: its queries sorted by mode (a block of rows then has one mode
+//   chunk_plan_kernel    some CTAs per chunk: its keys' common offset; its queries sorted by mode (a block of rows then has one mode
 //                        and reads no more than that mode sees), the positions that any of them sees,
 //                        how many tokens are stored there; the CTA that ends last lays chunks end to end.
 //   chunk_stage_kernel   the stored tokens in sight, in order of position, as tiles in the layout that the tensor
@@ -31,6 +31,7 @@
 // kernel; so are rows that do not see a V that is not finite safe from it (0 times infinity).
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "trr_chunk_tc.cuh"
 
@@ -65,26 +66,81 @@ __device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* warp_sums, in
   return before + s - x;
 }
 
-__global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __grid_constant__ ChunkArgs g) {
-  __shared__ int s_bad, s_lo, s_before[4][kClasses], s_last;
-  __shared__ int64_t s_sums[kPlanChunkThreads / 32];
+// What is common to a chunk's keys.  Binary16 rounds a key by 2^-11 of itself, so where an offset is common to all keys of a
+// channel, scores are off by 2^-11 of what it adds to them, though it adds the same to all and changes no weight: with 50
+// added to keys of standard deviation 1, rows were up to 2 % off.  Keys are therefore staged less an offset in channels where
+// eight tokens, spread over all that the sequence stores, lie within half of their middle; it is that middle.  Any number
+// would do, whatever it is taken from.  (Of normal numbers around 0 one channel in ten million passes for one with an offset.)
+constexpr int kSamples = 8, kMostParts = 8;
+// By one of the CTAs that share a chunk's channels out; `part` of them.
+__device__ __forceinline__ void find_offsets(const ChunkArgs& g, int chunk, int part) {
+  __shared__ const uint8_t* s_page[kSamples];
+  __shared__ int s_class[kSamples], s_slot[kSamples], s_total, s_moved[kPlanChunkThreads / 64];
   const LayerArgs& a = g.a;
-  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) s_bad = 0, s_lo = INT_MAX;
-  pdl_wait();
-  pdl_trigger();
-  __syncthreads();
-  for (int x = tid; x <= g.n; x += kPlanChunkThreads) {
-    const int o = g.offsets[x], next = x < g.n ? g.offsets[x + 1] : o;
-    if (o < 0 || o > g.num_tokens || next < o) s_bad = 1;
+  const int tid = threadIdx.x, lg_group = __ffs(a.G) - 1, lg_d = __ffs(a.d) - 1, heads = kPlanChunkThreads >> lg_d;
+  const int64_t head0 = static_cast<int64_t>(chunk) * a.Hkv;
+  if (tid < kSamples) {
+    const int seq = g.seq_ids[chunk];
+    const bool none = g.offsets[chunk + 1] <= g.offsets[chunk] || seq < 0 || seq >= a.S;  // (or refused: nothing is staged then)
+    const int64_t list = static_cast<int64_t>(none ? 0 : seq) * kClasses;
+    int nt[kClasses], total = 0;
+#pragma unroll
+    for (int c = 0; c < kClasses; ++c) total += nt[c] = none ? 0 : a.ntok[list + c];
+    int at = total > 0 ? static_cast<int>(static_cast<int64_t>(tid) * (total - 1) / (kSamples - 1)) : 0, cls = 0;
+#pragma unroll
+    for (int c = 0; c < kClasses - 1; ++c)
+      if (cls == c && at >= nt[c]) at -= nt[c], cls = c + 1;
+    if (total > 0) s_page[tid] = a.pool[cls] + a.pt[(list + cls) * a.MP + at / a.P] * a.page_bytes[cls] + a.hdr;
+    s_class[tid] = cls;
+    s_slot[tid] = at % a.P;
+    if (tid == 0) s_total = total;
   }
+  for (int x0 = part * kPlanChunkThreads; x0 < a.Hkv * a.d; x0 += g.parts * kPlanChunkThreads) {
+    const int x = x0 + tid, h = x >> lg_d, j = x & (a.d - 1);
+    if (tid < heads) s_moved[tid] = 0;
+    __syncthreads();
+    bool moved = false;
+    float middle = 0.f;
+    if (s_total > 0 && h < a.Hkv) {
+      uint32_t w[kSamples], sz[kSamples];
+#pragma unroll
+      for (int s = 0; s < kSamples; ++s) {  // all loads first, of one form for every class
+        const int c = s_class[s], row = a.d << (c + 1) >> 3;
+        const uint8_t* slice = s_page[s] + static_cast<int64_t>(h) * a.slice[c];
+        int o = s_slot[s] * row + (j << (c + 1) >> 3);
+        if (c >= 2 && a.swz) o = static_cast<int>(swz_off(o));
+        w[s] = *reinterpret_cast<const uint16_t*>(slice + (o & ~1)) >> 8 * (o & 1);
+        sz[s] = *reinterpret_cast<const uint32_t*>(slice + (c == 3 ? 0 : 2 * a.P * row + ((s_slot[s] << lg_d >> lg_group) + (j >> lg_group)) * 4));
+      }
+      float lo = INFINITY, hi = -INFINITY;
+      bool number = true;
+#pragma unroll
+      for (int s = 0; s < kSamples; ++s) {
+        const int lg = s_class[s] + 1, code = w[s] >> ((j << lg) & 7) & ((1 << (1 << lg)) - 1);
+        const float k = lg == 4 ? __uint_as_float(w[s] << 16) : __fmaf_rn(static_cast<float>(code), __low2float(as_half2(sz[s])), __high2float(as_half2(sz[s])));
+        number = number && fabsf(k) < 32768.f;
+        lo = fminf(lo, k);
+        hi = fmaxf(hi, k);
+      }
+      middle = 0.5f * (lo + hi);
+      moved = number && hi - lo < 0.5f * fabsf(middle);
+    }
+    if (h < a.Hkv) g.offset[(head0 << lg_d) + x] = __float2half_rn(moved ? middle : 0.f);
+    if (moved) s_moved[tid >> lg_d] = 1;
+    __syncthreads();
+    if (tid < heads && (x0 >> lg_d) + tid < a.Hkv) {
+      g.moved[head0 + (x0 >> lg_d) + tid] = s_moved[tid];
+      if (s_moved[tid]) a.ctrl[kChunkMoved] = 1;
+    }
+  }
+}
+
+// One chunk: its queries in their places, what they see, how much is stored there.
+__device__ __forceinline__ void plan_chunk(const ChunkArgs& g, int i, int seq, int start, int row0, int len, int err, int64_t* s_sums, int& s_lo,
+                                           int (&s_before)[4][kClasses]) {
+  const LayerArgs& a = g.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   for (int h = tid; h < a.Hkv; h += kPlanChunkThreads) g.flag[static_cast<int64_t>(i) * a.Hkv + h] = 0;
-  const int begin = g.offsets[i], upto = g.offsets[i + 1], seq = g.seq_ids[i], start = g.starts[i];
-  __syncthreads();
-  const bool bad = s_bad;
-  const int row0 = bad ? 0 : begin, len = bad ? 0 : upto - begin;
-  const int err = bad ? TRR_ERR_INVALID_ARG : seq < 0 || seq >= a.S ? TRR_ERR_INVALID_ARG : start < 0 || start > a.maxctx - len ? TRR_ERR_BAD_POSITION : 0;
-  if (tid == 0 && err && (bad || len > 0)) chunk_fail(g, row0, err);
   // a query's place: 0 full, 1 local, 2 a zero row
   auto kind_of = [&](int k, int* window) -> int {
     const int q = row0 + k, mode = g.modes[q];
@@ -156,8 +212,36 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
       c.blocks = (full * heads + kBlockRows - 1) / kBlockRows + (local * heads + kBlockRows - 1) / kBlockRows;
     }
     g.chunk[i] = c;
-    s_last = atom_add_acq_rel(a.ctrl + kChunkDone, 1) == g.n - 1;
   }
+}
+
+__global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __grid_constant__ ChunkArgs g) {
+  __shared__ int s_bad, s_lo, s_before[4][kClasses], s_last;
+  __shared__ int64_t s_sums[kPlanChunkThreads / 32];
+  const LayerArgs& a = g.a;
+  const int tid = threadIdx.x, i = blockIdx.x;
+  if (tid == 0) s_bad = 0, s_lo = INT_MAX;
+  pdl_wait();
+  pdl_trigger();
+  if (i >= g.n) {  // the CTAs behind the chunks' look for their keys' offsets
+    find_offsets(g, (i - g.n) / g.parts, (i - g.n) % g.parts);
+  } else {
+    __syncthreads();
+    for (int x = tid; x <= g.n; x += kPlanChunkThreads) {
+      const int o = g.offsets[x], next = x < g.n ? g.offsets[x + 1] : o;
+      if (o < 0 || o > g.num_tokens || next < o) s_bad = 1;
+    }
+    const int begin = g.offsets[i], upto = g.offsets[i + 1], seq = g.seq_ids[i], start = g.starts[i];
+    __syncthreads();
+    const bool bad = s_bad;
+    const int row0 = bad ? 0 : begin, len = bad ? 0 : upto - begin;
+    const int err = bad ? TRR_ERR_INVALID_ARG : seq < 0 || seq >= a.S ? TRR_ERR_INVALID_ARG : start < 0 || start > a.maxctx - len ? TRR_ERR_BAD_POSITION : 0;
+    if (tid == 0 && err && (bad || len > 0)) chunk_fail(g, row0, err);
+    plan_chunk(g, i, seq, start, row0, len, err, s_sums, s_lo, s_before);
+    if (tid == 0 && bad) a.ctrl[kChunkRefused] = 1;
+  }
+  __syncthreads();
+  if (tid == 0) s_last = atom_add_acq_rel(a.ctrl + kChunkDone, 1) == g.n * (1 + g.parts) - 1;
   __syncthreads();
   if (!s_last) return;
   __threadfence();
@@ -185,7 +269,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     }
   }
   if (tid == 0) {
-    int whole = bad ? TRR_ERR_INVALID_ARG : 0;
+    int whole = atomicExch(a.ctrl + kChunkRefused, 0) ? TRR_ERR_INVALID_ARG : 0;
     if (!whole && tiles > g.most_tiles) {  // the workspace is too small for what is stored
       whole = TRR_ERR_OUT_OF_MEMORY;
       chunk_fail(g, 0, whole);
@@ -197,6 +281,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
       const int stagers = kStageCtas * g.ctas;
       h.splits = units > 0 ? shares_of_heads(units, (a.Hkv + 1) / 2, stagers, copy_ns(5ll * a.Hkv * a.d, stagers)) : 1;
     }
+    h.moved = atomicExch(a.ctrl + kChunkMoved, 0);
     *g.head = h;
     const int e = atomicExch(a.ctrl + kChunkBad, 0);
     if (e) set_status(a.ctrl, (INT_MAX - e) & 15);
@@ -311,8 +396,40 @@ __device__ __forceinline__ void zero_rows(const ChunkArgs& g, int q, int h0, int
     for (int h = lane; h < h1 - h0; h += 32) g.lse[at + h] = -INFINITY;
 }
 
-// A token's rows of every step-th head into its tile: 16 elements a lane of K and of V.  All lanes of the warp call it.
+// Sixteen elements of a key into its tile, less their offset (the difference in binary32, rounded once).  Out of line: few
+// calls need it, and the staging kernel has no registers left.
 template <int C, int D>
+__device__ __noinline__ void stage_moved_key(const ChunkArgs& g, int chunk, int h, const uint8_t* slice, int slot, int e, uint8_t* to, bool odd) {
+  const CodesAt<C, D> at(g.a, slot, e);
+  float k[16];
+  expand_f32<C>(at.load(slice, 0), k);
+  const uint4* offset = reinterpret_cast<const uint4*>(g.offset + (static_cast<int64_t>(chunk) * g.a.Hkv + h) * D + 16 * e);
+  uint4 v[2];
+  float most = 0.f;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const uint4 o = offset[half];
+    const uint32_t x[4] = {o.x, o.y, o.z, o.w};
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = k[8 * half + 2 * i] - __low2float(as_half2(x[i])), b = k[8 * half + 2 * i + 1] - __high2float(as_half2(x[i]));
+      most = fmaxf(most, fmaxf(fabsf(a), fabsf(b)));
+      w[i] = pack16(false, a, b);
+    }
+    v[half] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  if (most > 65504.f) {  // (infinities and NaN are flagged as they are stored)
+    g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
+    g.head->flagged = 1;
+  }
+  store_sector(to, odd ? v[1] : v[0], odd ? v[0] : v[1]);
+}
+
+// A token's rows of every step-th head into its tile: 16 elements a lane of K and of V.  All lanes of the warp call it.
+// (MOVED: some chunk's keys may have an offset.  The loop without is as fast as if there were none; with a test in it, ragged
+// chunks took 400 us against 384.)
+template <int C, int D, bool MOVED>
 __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const uint8_t* page, int slot, int row, bool live, int h0, int h1, int step, int e) {
   constexpr int T = chunk_tile(D), kLanes = D / 16;
   const CodesAt<C, D> at(g.a, slot, e);
@@ -348,6 +465,8 @@ __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const
       }
       if (live) store_sector(to + (2 * h + which) * (2 * T * D), odd ? v[1] : v[0], odd ? v[0] : v[1]);
     }
+    if (MOVED && live && g.moved[static_cast<int64_t>(chunk) * g.a.Hkv + h])
+      stage_moved_key<C, D>(g, chunk, h, slice - step * slice_bytes, slot, e, to + 2 * h * (2 * T * D), odd);
   }
 }
 
@@ -444,13 +563,18 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     rank += __shfl_xor_sync(0xffffffffu, rank, 2);
     const int row = c.tile0 * T + rank - (pos >= c.lo ? c.dropped : 0);
     f.gather(a, p, cls, p.page >= 0 ? row : -1, tid);
-    for_groups(f, lg_parts(per), h0, [&](int k, const auto& tok, bool live, int h, int step) {
-      const int e = tid % kLanes;
-      if (k == 0) stage_token<0, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-      else if (k == 1) stage_token<1, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-      else if (k == 2) stage_token<2, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-      else stage_token<3, D>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-    });
+    auto stage = [&](auto moved) {
+      for_groups(f, lg_parts(per), h0, [&](int k, const auto& tok, bool live, int h, int step) {
+        constexpr bool M = decltype(moved)::value;
+        const int e = tid % kLanes;
+        if (k == 0) stage_token<0, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+        else if (k == 1) stage_token<1, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+        else if (k == 2) stage_token<2, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+        else stage_token<3, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+      });
+    };
+    if (head.moved) stage(std::true_type{});
+    else stage(std::false_type{});
   }
   // rows of a chunk's last tile past its tokens are zero (their weights are)
   for (int k = blockIdx.x; k < g.n; k += gridDim.x) {
@@ -567,7 +691,7 @@ __device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const Piec
   for (int i = 0; i < E / 4; ++i)
     *reinterpret_cast<uint2*>(g.out + at * D + 32 * i + 4 * lane) =
         make_uint2(pack16(true, o[4 * i] * inv, o[4 * i + 1] * inv), pack16(true, o[4 * i + 2] * inv, o[4 * i + 3] * inv));
-  if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f + moved_score<D>(g, piece.chunk, piece.kvh, at) : -INFINITY;
 }
 
 constexpr int kJoinCtas = 4;
@@ -623,10 +747,11 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->block = reinterpret_cast<BlockPlan*>(take(static_cast<int64_t>(sizeof(BlockPlan)) * blocks));
   g->base = reinterpret_cast<int64_t*>(take(8 * (blocks + 1)));
   g->flag = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
+  g->moved = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
+  g->offset = reinterpret_cast<__half*>(take(2ll * n * l.Hkv * l.d));
   g->piece = reinterpret_cast<PieceInfo*>(take(static_cast<int64_t>(sizeof(PieceInfo)) * ctas));
   g->part_ml = reinterpret_cast<float2*>(take(8ll * 2 * ctas * kBlockRows));
   g->part_o = reinterpret_cast<uint4*>(take(4ll * 2 * ctas * kBlockRows * l.d));
-  g->most_blocks = static_cast<int>(blocks);
   const int64_t fixed = off, T = chunk_tile(l.d);
   g->tile = take((most_tiles * l.Hkv * 2 * T * l.d * 2 + 1023) / 1024 * 1024);
   return most_tiles ? off : fixed;
@@ -690,6 +815,8 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   g.a.wait_ns = cache_wait_ns(cache);
   g.n = num_chunks; g.num_tokens = num_tokens; g.window_scalar = window_scalar; g.sinks = sinks;
   g.ctas = cache_num_sms(cache);
+  g.parts = (l.Hkv * l.d + kPlanChunkThreads - 1) / kPlanChunkThreads;
+  if (g.parts > kMostParts) g.parts = kMostParts;
   g.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf(static_cast<float>(l.d))) * 1.4426950408889634f;
   g.seq_ids = seq_ids; g.starts = starts; g.offsets = offsets; g.windows = windows; g.modes = modes;
   g.q = static_cast<const uint16_t*>(q_bf16);
@@ -704,7 +831,7 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   cache_note_call(cache, layer);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int launches = 0;
-  cudaError_t e = launch_pdl(chunk_plan_kernel, dim3(num_chunks), dim3(kPlanChunkThreads), 0, s, g);
+  cudaError_t e = launch_pdl(chunk_plan_kernel, dim3(num_chunks * (1 + g.parts)), dim3(kPlanChunkThreads), 0, s, g);
   if (e == cudaSuccess) {
     ++launches;
     e = launch_pdl(l.d == 64 ? chunk_stage_kernel<64> : chunk_stage_kernel<128>, dim3(kStageCtas * g.ctas), dim3(kSpanThreads), 0, s, g);

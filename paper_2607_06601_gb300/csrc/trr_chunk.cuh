@@ -49,7 +49,8 @@ struct ChunkHeader {
   int blocks, units, tiles;
   int splits, flagged;          // shares of the KV heads that staging CTAs take; some flag is set
   int empty;                    // some block has no tiles
-  int pad[5];
+  int moved;                    // some chunk's keys are staged less an offset
+  int pad[4];
 };
 
 // A segment that a CTA began and the ctas - 1 after it went on with; block < 0: none.
@@ -60,7 +61,8 @@ struct PieceInfo {
 
 struct ChunkArgs {
   LayerArgs a;
-  int n, num_tokens, window_scalar, sinks, ctas, most_tiles, most_blocks;
+  int n, num_tokens, window_scalar, sinks, ctas, most_tiles;
+  int parts;         // CTAs that look for the offsets of a chunk's keys
   float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
   const int32_t *seq_ids, *starts, *offsets, *windows;
   const uint8_t* modes;
@@ -76,6 +78,8 @@ struct ChunkArgs {
   BlockPlan* block;   // [most_blocks]
   int64_t* base;      // [most_blocks + 1] cost before each block (all its KV heads)
   int32_t* flag;      // [n][Hkv] some stored value is not to be had in binary16: its rows are done one by one
+  int32_t* moved;     // [n][Hkv] keys are staged less their offset
+  __half* offset;     // [n][Hkv][D] what is common to the keys, 0 in channels where little is
   PieceInfo* piece;   // [ctas] the segment that a CTA began and did not finish
   float2* part_ml;    // [2 * ctas][256] (m, l) of a CTA's first piece, or its last
   uint4* part_o;      // [2 * ctas][D / 4][256] four columns of a row (binary32), consecutive rows beside each other
@@ -108,6 +112,18 @@ __device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkP
   r.t = c.start + r.query - c.row0;
   r.lo = local ? r.t - (g.windows ? g.windows[r.query] : g.window_scalar) + 1 : 0;
   return r;
+}
+
+// What the keys' offset adds to the scores of row `at` (query and head), in units of the natural logarithm: staged keys
+// are less by it, which moves all of a row's scores by as much, no weight, and the logarithm of their sum.
+template <int D>
+__device__ __forceinline__ float moved_score(const ChunkArgs& g, int chunk, int kvh, int64_t at) {
+  const int64_t k = static_cast<int64_t>(chunk) * g.a.Hkv + kvh;
+  if (!g.head->moved || !g.moved[k]) return 0.f;
+  float sum = 0.f;
+#pragma unroll 1
+  for (int j = 0; j < D; ++j) sum += __uint_as_float(static_cast<uint32_t>(g.q[at * D + j]) << 16) * __half2float(g.offset[k * D + j]);
+  return sum * g.scale_log2 * 0.6931471805599453f;
 }
 
 // The last of 0 .. n-1 whose value (they ascend) is x or less, 0 if none is, by a whole warp: a chain of one load for 32 of

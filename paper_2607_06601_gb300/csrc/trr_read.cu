@@ -37,52 +37,6 @@ struct ReadArgs {
   int lg_parts;                // a CTA's warps share a group's heads out in 2^lg_parts parts
 };
 
-// (a, b) x (f, f) and (a, b) x (f, f) + (z, z).
-__device__ __forceinline__ void scale_pair(float& a, float& b, float f) {
-  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %2};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}" : "+f"(a), "+f"(b) : "f"(f));
-}
-__device__ __forceinline__ void affine_pair(float& a, float& b, float f, float z) {
-  asm("{\n .reg .b64 x, y, w;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %2};\n mov.b64 w, {%3, %3};\n fma.rn.f32x2 x, x, y, w;\n mov.b64 {%0, %1}, x;\n}"
-      : "+f"(a), "+f"(b)
-      : "f"(f), "f"(z));
-}
-
-// z + c s of sixteen elements of class C (kClasses: zeros), in binary32.  A code stays where it is in its word, which
-// is read as a binary32 subnormal, c 2^(p - 149) at bit p: with s 2^(100 - p) and z 2^-49 the sum has the roundings of
-// z + c s (nothing is subnormal: s and z are binary16), 2^-49 times.
-template <int C>
-__device__ __forceinline__ void expand_f32(const Codes16& x, float (&v)[16]) {
-  if constexpr (C == kClasses) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.f;
-  } else if constexpr (C == 3) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t w[4] = {x.w[k].x, x.w[k].y, x.w[k].z, x.w[k].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[8 * k + 2 * i] = bf16lo(w[i]), v[8 * k + 2 * i + 1] = bf16hi(w[i]);
-    }
-  } else {
-    constexpr int B = 2 << C, kWords = B / 2, kHalf = 16 / B;  // elements in half a word
-    const uint32_t w[4] = {x.w[0].x, x.w[0].y, x.w[0].z, x.w[0].w};
-    const float s = __low2float(as_half2(x.sz)), z = __high2float(as_half2(x.sz)) * 0x1p-49f;
-#pragma unroll
-    for (int i = 0; i < kHalf; ++i) {
-      const uint32_t mask = ((1u << B) - 1) << (B * i);
-      const float f = s * __int_as_float((127 + 100 - B * i) << 23);
-#pragma unroll
-      for (int k = 0; k < kWords; ++k) {
-        float& a = v[2 * kHalf * k + i];
-        float& b = v[2 * kHalf * k + kHalf + i];
-        a = __uint_as_float(w[k] & mask);
-        b = __uint_as_float((w[k] >> 16) & mask);
-        affine_pair(a, b, f, z);
-        scale_pair(a, b, 0x1p49f);
-      }
-    }
-  }
-}
-
 __device__ __forceinline__ uint4 as_bf16(const float* v) {
   return make_uint4(pack16(true, v[0], v[1]), pack16(true, v[2], v[3]), pack16(true, v[4], v[5]), pack16(true, v[6], v[7]));
 }

@@ -5,8 +5,8 @@
 //
 // A chunk's many queries read the same tokens, so those are brought back from their codes once, not
 // once for each block of rows:
-//   chunk_plan_kernel    some CTAs per chunk: its keys' common offset; its queries sorted by mode (a block of rows then has one mode
-//                        and reads no more than that mode sees), the positions that any of them sees,
+//   chunk_plan_kernel    some CTAs per chunk: what its tokens have in common; its queries sorted by mode (a block of rows then
+//                        has one mode and reads no more than that mode sees), the positions that any of them sees,
 //                        how many tokens are stored there; the CTA that ends last lays chunks end to end.
 //   chunk_stage_kernel   the stored tokens in sight, in order of position, as tiles in the layout that the tensor
 //                        core reads, in binary16: z + c s rounded once (11 bits against the 8 of the output), 16-bit
@@ -31,7 +31,6 @@
 // kernel; so are rows that do not see a V that is not finite safe from it (0 times infinity).
 #include <algorithm>
 #include <climits>
-#include <type_traits>
 
 #include "trr_chunk_tc.cuh"
 
@@ -66,19 +65,28 @@ __device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* warp_sums, in
   return before + s - x;
 }
 
-// What is common to a chunk's keys.  Binary16 rounds a key by 2^-11 of itself, so where an offset is common to all keys of a
-// channel, scores are off by 2^-11 of what it adds to them, though it adds the same to all and changes no weight: with 50
-// added to keys of standard deviation 1, rows were up to 2 % off.  Keys are therefore staged less an offset in channels where
-// eight tokens, spread over all that the sequence stores, lie within half of their middle; it is that middle.  Any number
-// would do, whatever it is taken from.  (Of normal numbers around 0 one channel in ten million passes for one with an offset.)
-constexpr int kSamples = 8, kMostParts = 8;
+// What is common to the tokens of a channel, taken from eight of them that are spread over all that the sequence stores.  Any
+// choice gives the same rows but for rounding.
+//   Keys: binary16 rounds one by 2^-11 of itself, so where an offset is common to all keys of a channel, scores are off by 2^-11
+// of what it adds to them, though it adds the same to all and changes no weight: with 50 added to keys of standard deviation
+// 1, rows were up to 3 % off.  Keys are staged less an offset where the eight lie within a third of their middle; it is that middle.
+// (Of normal numbers around 0 one channel in ten million passes for one with an offset.)
+//   Values: binary16's steps end at 2^-24, so where a channel's are that small, its sums have few bits left or none, beside
+// channels that are none the worse.  Where the eight are below 2^-12, values are staged times the power of two that brings
+// their largest to 2^-8 (so that a value may be 2^23 times as large and be in binary16's range), and rows are divided by it as
+// they are written.
+// (With 16, and half as many channels a CTA, 32 chunks of 12 heads took 126.5 us against 122.5.)
+constexpr int kSamples = 8;
+// CTAs that share a chunk's channels out: a pass each, but no more than the GPU holds at once.
+constexpr int kMostParts = 8, kMostCommonCtas = 512;
 // By one of the CTAs that share a chunk's channels out; `part` of them.
-__device__ __forceinline__ void find_offsets(const ChunkArgs& g, int chunk, int part) {
+__device__ __forceinline__ void find_common(const ChunkArgs& g, int chunk, int part) {
   __shared__ const uint8_t* s_page[kSamples];
   __shared__ int s_class[kSamples], s_slot[kSamples], s_total, s_moved[kPlanChunkThreads / 64];
   const LayerArgs& a = g.a;
   const int tid = threadIdx.x, lg_group = __ffs(a.G) - 1, lg_d = __ffs(a.d) - 1, heads = kPlanChunkThreads >> lg_d;
-  const int64_t head0 = static_cast<int64_t>(chunk) * a.Hkv;
+  const int64_t head0 = static_cast<int64_t>(chunk) * 2 * a.Hkv;
+  const int both = 2 * a.Hkv;  // K of each KV head, then V of each
   if (tid < kSamples) {
     const int seq = g.seq_ids[chunk];
     const bool none = g.offsets[chunk + 1] <= g.offsets[chunk] || seq < 0 || seq >= a.S;  // (or refused: nothing is staged then)
@@ -95,25 +103,23 @@ __device__ __forceinline__ void find_offsets(const ChunkArgs& g, int chunk, int 
     s_slot[tid] = at % a.P;
     if (tid == 0) s_total = total;
   }
-  for (int x0 = part * kPlanChunkThreads; x0 < a.Hkv * a.d; x0 += g.parts * kPlanChunkThreads) {
-    const int x = x0 + tid, h = x >> lg_d, j = x & (a.d - 1);
+  for (int x0 = part * kPlanChunkThreads; x0 < both * a.d; x0 += g.parts * kPlanChunkThreads) {
+    const int x = x0 + tid, which = x >> lg_d >= a.Hkv, h = (x >> lg_d) - which * a.Hkv, j = x & (a.d - 1);
     if (tid < heads) s_moved[tid] = 0;
     __syncthreads();
-    bool moved = false;
-    float middle = 0.f;
-    if (s_total > 0 && h < a.Hkv) {
+    float lo = INFINITY, hi = -INFINITY;
+    bool number = s_total > 0 && h < a.Hkv;
+    if (number) {
       uint32_t w[kSamples], sz[kSamples];
 #pragma unroll
       for (int s = 0; s < kSamples; ++s) {  // all loads first, of one form for every class
-        const int c = s_class[s], row = a.d << (c + 1) >> 3;
+        const int c = s_class[s], row = a.d << (c + 1) >> 3, at = which * a.P + s_slot[s];
         const uint8_t* slice = s_page[s] + static_cast<int64_t>(h) * a.slice[c];
-        int o = s_slot[s] * row + (j << (c + 1) >> 3);
+        int o = at * row + (j << (c + 1) >> 3);
         if (c >= 2 && a.swz) o = static_cast<int>(swz_off(o));
         w[s] = *reinterpret_cast<const uint16_t*>(slice + (o & ~1)) >> 8 * (o & 1);
-        sz[s] = *reinterpret_cast<const uint32_t*>(slice + (c == 3 ? 0 : 2 * a.P * row + ((s_slot[s] << lg_d >> lg_group) + (j >> lg_group)) * 4));
+        sz[s] = *reinterpret_cast<const uint32_t*>(slice + (c == 3 ? 0 : 2 * a.P * row + ((at << lg_d >> lg_group) + (j >> lg_group)) * 4));
       }
-      float lo = INFINITY, hi = -INFINITY;
-      bool number = true;
 #pragma unroll
       for (int s = 0; s < kSamples; ++s) {
         const int lg = s_class[s] + 1, code = w[s] >> ((j << lg) & 7) & ((1 << (1 << lg)) - 1);
@@ -122,13 +128,16 @@ __device__ __forceinline__ void find_offsets(const ChunkArgs& g, int chunk, int 
         lo = fminf(lo, k);
         hi = fmaxf(hi, k);
       }
-      middle = 0.5f * (lo + hi);
-      moved = number && hi - lo < 0.5f * fabsf(middle);
     }
-    if (h < a.Hkv) g.offset[(head0 << lg_d) + x] = __float2half_rn(moved ? middle : 0.f);
+    const float middle = 0.5f * (lo + hi), top = fmaxf(hi, -lo);
+    const bool moved = number && (which ? top > 0.f && top < 0x1p-12f : 3.f * (hi - lo) < fabsf(middle));
+    float common = which ? 1.f : 0.f;
+    if (moved) common = which ? __int_as_float((246 - static_cast<int>(__float_as_uint(top) >> 23)) << 23) : middle;
+    // (an offset is rounded to binary16, a power of two is a bf16 number)
+    if (h < a.Hkv) g.common[(head0 << lg_d) + x] = which ? __float_as_uint(common) >> 16 : __half_as_ushort(__float2half_rn(common));
     if (moved) s_moved[tid >> lg_d] = 1;
     __syncthreads();
-    if (tid < heads && (x0 >> lg_d) + tid < a.Hkv) {
+    if (tid < heads && (x0 >> lg_d) + tid < both) {
       g.moved[head0 + (x0 >> lg_d) + tid] = s_moved[tid];
       if (s_moved[tid]) a.ctrl[kChunkMoved] = 1;
     }
@@ -223,8 +232,8 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
   if (tid == 0) s_bad = 0, s_lo = INT_MAX;
   pdl_wait();
   pdl_trigger();
-  if (i >= g.n) {  // the CTAs behind the chunks' look for their keys' offsets
-    find_offsets(g, (i - g.n) / g.parts, (i - g.n) % g.parts);
+  if (i >= g.n) {  // the CTAs behind the chunks' look for what their tokens have in common
+    find_common(g, (i - g.n) / g.parts, (i - g.n) % g.parts);
   } else {
     __syncthreads();
     for (int x = tid; x <= g.n; x += kPlanChunkThreads) {
@@ -396,39 +405,32 @@ __device__ __forceinline__ void zero_rows(const ChunkArgs& g, int q, int h0, int
     for (int h = lane; h < h1 - h0; h += 32) g.lse[at + h] = -INFINITY;
 }
 
-// Sixteen elements of a key into its tile, less their offset (the difference in binary32, rounded once).  Out of line: few
-// calls need it, and the staging kernel has no registers left.
+// Sixteen elements of a token's K less their offset, or of its V times their powers of two (a x b + c, in binary32), rounded once to
+// binary16; their largest magnitude's bits, and whether binary16 lacks bits of one.
 template <int C, int D>
-__device__ __noinline__ void stage_moved_key(const ChunkArgs& g, int chunk, int h, const uint8_t* slice, int slot, int e, uint8_t* to, bool odd) {
-  const CodesAt<C, D> at(g.a, slot, e);
-  float k[16];
-  expand_f32<C>(at.load(slice, 0), k);
-  const uint4* offset = reinterpret_cast<const uint4*>(g.offset + (static_cast<int64_t>(chunk) * g.a.Hkv + h) * D + 16 * e);
-  uint4 v[2];
-  float most = 0.f;
+__device__ __forceinline__ void expand_moved(const Codes16& x, int which, const uint16_t* common, uint4 (&v)[2], uint32_t* top, bool* lost) {
+  float y[16];
+  expand_f32<C>(x, y);
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const uint4 o = offset[half];
-    const uint32_t x[4] = {o.x, o.y, o.z, o.w};
-    uint32_t w[4];
+    const uint4 c = reinterpret_cast<const uint4*>(common)[half];
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    uint32_t o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = k[8 * half + 2 * i] - __low2float(as_half2(x[i])), b = k[8 * half + 2 * i + 1] - __high2float(as_half2(x[i]));
-      most = fmaxf(most, fmaxf(fabsf(a), fabsf(b)));
-      w[i] = pack16(false, a, b);
+      float a = y[8 * half + 2 * i], b = y[8 * half + 2 * i + 1];
+      a = which ? a * bf16lo(w[i]) : a - __low2float(as_half2(w[i]));
+      b = which ? b * bf16hi(w[i]) : b - __high2float(as_half2(w[i]));
+      o[i] = pack16(false, a, b);
+      *top = max(*top, max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu));
+      if (C == 3) *lost |= __low2float(as_half2(o[i])) != a || __high2float(as_half2(o[i])) != b;
     }
-    v[half] = make_uint4(w[0], w[1], w[2], w[3]);
+    v[half] = make_uint4(o[0], o[1], o[2], o[3]);
   }
-  if (most > 65504.f) {  // (infinities and NaN are flagged as they are stored)
-    g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
-    g.head->flagged = 1;
-  }
-  store_sector(to, odd ? v[1] : v[0], odd ? v[0] : v[1]);
 }
 
 // A token's rows of every step-th head into its tile: 16 elements a lane of K and of V.  All lanes of the warp call it.
-// (MOVED: some chunk's keys may have an offset.  The loop without is as fast as if there were none; with a test in it, ragged
-// chunks took 400 us against 384.)
+// (MOVED: what is common to some chunk's tokens is taken out.)
 template <int C, int D, bool MOVED>
 __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const uint8_t* page, int slot, int row, bool live, int h0, int h1, int step, int e) {
   constexpr int T = chunk_tile(D), kLanes = D / 16;
@@ -449,14 +451,21 @@ __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       uint4 v[2];
-      if (C == 3) {
+      if (C == 3 || MOVED) {
+        constexpr uint32_t kPast = MOVED ? 0x477FE001u : 0x4780u, kNear = MOVED ? 0x38800000u : 0x3880u;  // beyond 65504 (binary32), 65536 (bf16); 2^-14
         uint32_t top = 0;
         bool lost = false;
-        v[0] = convert_f16(x[which].w[0], &top, &lost);
-        v[1] = convert_f16(x[which].w[1], &top, &lost);
+        if (MOVED) {
+          expand_moved<C, D>(x[which], which, common_of<D>(g, chunk, h, which) + 16 * e, v, &top, &lost);
+        } else {
+          v[0] = convert_f16(x[which].w[0], &top, &lost);
+          v[1] = convert_f16(x[which].w[1], &top, &lost);
+        }
+        if (C == 3) {
 #pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (live && (top >= 0x4780u || (lost && top < 0x3880u))) {  // 65536, 2^-14 as bf16
+          for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        }
+        if (live && (top >= kPast || (lost && top < kNear))) {
           g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + h] = 1;
           g.head->flagged = 1;
         }
@@ -465,9 +474,52 @@ __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const
       }
       if (live) store_sector(to + (2 * h + which) * (2 * T * D), odd ? v[1] : v[0], odd ? v[0] : v[1]);
     }
-    if (MOVED && live && g.moved[static_cast<int64_t>(chunk) * g.a.Hkv + h])
-      stage_moved_key<C, D>(g, chunk, h, slice - step * slice_bytes, slot, e, to + 2 * h * (2 * T * D), odd);
   }
+}
+
+// The tokens that a CTA has found, of KV heads h0 .. h1 - 1.
+template <int D, bool MOVED>
+__device__ __forceinline__ void stage_unit(const ChunkArgs& g, const Found<32 / (D / 16)>& f, int chunk, int h0, int h1, int lg) {
+  for_groups(f, lg, h0, [&](int k, const auto& tok, bool live, int h, int step) {
+    const int e = threadIdx.x % (D / 16);
+    if (k == 0) stage_token<0, D, MOVED>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+    else if (k == 1) stage_token<1, D, MOVED>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+    else if (k == 2) stage_token<2, D, MOVED>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+    else stage_token<3, D, MOVED>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
+  });
+}
+// A CTA's units: 64 positions of a chunk's line, some of the KV heads.
+template <int D, bool MOVED>
+__device__ __forceinline__ void stage_units(const ChunkArgs& g, Found<32 / (D / 16)>& f, int units, int splits) {
+  constexpr int T = chunk_tile(D);
+  const LayerArgs& a = g.a;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int per = (a.Hkv + splits - 1) / splits;
+  int chunk = -1;
+  ChunkPlan c;
+  for (int u = gridDim.x - 1 - blockIdx.x; u < units * splits; u += gridDim.x) {
+    const int unit = u / splits, h0 = u % splits * per, h1 = min(a.Hkv, h0 + per);
+    if (chunk < 0 || unit >= c.unit0 + c.units) {
+      chunk = last_not_above(g.n, unit, lane, [&](int i) { return g.chunk[i].unit0; });
+      c = g.chunk[chunk];
+    }
+    const int x = (unit - c.unit0) * kSpan + (tid >> 2), cls = tid & 3;
+    const int pos = x < c.sinks ? x : x - c.sinks + c.lo;
+    Place p{0, -1, 0};
+    if (x < c.span) p = place_of(a, c.seq, cls, pos);
+    // rank among the staged tokens: the sum over the classes
+    int rank = p.before;
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    const int row = c.tile0 * T + rank - (pos >= c.lo ? c.dropped : 0);
+    f.gather(a, p, cls, p.page >= 0 ? row : -1, tid);
+    stage_unit<D, MOVED>(g, f, chunk, h0, h1, lg_parts(per));
+  }
+}
+// (Out of line, and called where nothing else is live, so that the loop without is as fast as if this were not there.)
+template <int D>
+__device__ __noinline__ void stage_moved_units(const ChunkArgs& g, Found<32 / (D / 16)>& f, int units, int splits) {
+  stage_units<D, true>(g, f, units, splits);
 }
 
 template <int D>
@@ -543,39 +595,8 @@ __global__ void __launch_bounds__(kSpanThreads, kStageCtas) chunk_stage_kernel(c
     for (uint32_t left = __ballot_sync(0xffffffffu, mine && !reads && (lane & 7) == 0); left; left &= left - 1)
       zero_rows(g, __shfl_sync(0xffffffffu, q, __ffs(left) - 1), 0, a.Hq, lane);
   }
-  // units: 64 positions of a chunk's line, some of the KV heads
-  const int per = (a.Hkv + head.splits - 1) / head.splits;
-  int chunk = -1;
-  ChunkPlan c;
-  for (int u = gridDim.x - 1 - blockIdx.x; u < head.units * head.splits; u += gridDim.x) {
-    const int unit = u / head.splits, h0 = u % head.splits * per, h1 = min(a.Hkv, h0 + per);
-    if (chunk < 0 || unit >= c.unit0 + c.units) {
-      chunk = last_not_above(g.n, unit, lane, [&](int i) { return g.chunk[i].unit0; });
-      c = g.chunk[chunk];
-    }
-    const int x = (unit - c.unit0) * kSpan + (tid >> 2), cls = tid & 3;
-    const int pos = x < c.sinks ? x : x - c.sinks + c.lo;
-    Place p{0, -1, 0};
-    if (x < c.span) p = place_of(a, c.seq, cls, pos);
-    // rank among the staged tokens: the sum over the classes
-    int rank = p.before;
-    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
-    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-    const int row = c.tile0 * T + rank - (pos >= c.lo ? c.dropped : 0);
-    f.gather(a, p, cls, p.page >= 0 ? row : -1, tid);
-    auto stage = [&](auto moved) {
-      for_groups(f, lg_parts(per), h0, [&](int k, const auto& tok, bool live, int h, int step) {
-        constexpr bool M = decltype(moved)::value;
-        const int e = tid % kLanes;
-        if (k == 0) stage_token<0, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-        else if (k == 1) stage_token<1, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-        else if (k == 2) stage_token<2, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-        else stage_token<3, D, M>(g, chunk, tok.page, tok.slot, tok.row, live, h, h1, step, e);
-      });
-    };
-    if (head.moved) stage(std::true_type{});
-    else stage(std::false_type{});
-  }
+  if (head.moved) stage_moved_units<D>(g, f, head.units, head.splits);
+  else stage_units<D, false>(g, f, head.units, head.splits);
   // rows of a chunk's last tile past its tokens are zero (their weights are)
   for (int k = blockIdx.x; k < g.n; k += gridDim.x) {
     const ChunkPlan& p = g.chunk[k];
@@ -656,9 +677,39 @@ __device__ __forceinline__ void one_row(const ChunkArgs& g, const ChunkPlan& ch,
   if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
+// What the keys' offset adds to the scores of row `at` (query and head), in units of the natural logarithm, summed over elements
+// first, first + step, ...: staged keys are less by it, which moves all of a row's scores by as much, no weight, and the
+// logarithm of their sum.
+template <int D>
+__device__ __forceinline__ float moved_score(const ChunkArgs& g, int chunk, int kvh, int64_t at, int first, int step) {
+  const uint16_t *q = g.q + at * D, *offset = common_of<D>(g, chunk, kvh, 0);
+  float sum = 0.f;
+#pragma unroll 1
+  for (int j = first; j < D; j += step) sum += __uint_as_float(static_cast<uint32_t>(q[j]) << 16) * __half2float(__ushort_as_half(offset[j]));
+  return sum * g.scale_log2 * 0.6931471805599453f;
+}
+
+// What was taken out of a row's K and V put back, by a warp.  V was staged times powers of two, by which a bf16 number is
+// divided without a rounding.
+template <int D>
+__device__ __forceinline__ void put_back(const ChunkArgs& g, int chunk, int kvh, int64_t at, int lane) {
+  if (g.lse && moved_head(g, chunk, kvh, 0)) {
+    float sum = moved_score<D>(g, chunk, kvh, at, lane, 32);
+    for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+    if (lane == 0 && g.lse[at] != -INFINITY) g.lse[at] += sum;
+  }
+  if (moved_head(g, chunk, kvh, 1)) {
+    const uint16_t* power = common_of<D>(g, chunk, kvh, 1);
+    for (int j = lane; j < D; j += 32) {
+      uint16_t* o = g.out + at * D + j;
+      *o = __bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(static_cast<uint32_t>(*o) << 16) * one_over(power[j])));
+    }
+  }
+}
+
 // One row of a cut segment, by eight lanes: D / 8 values each.
 template <int D>
-__device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const PieceInfo& piece, int r, int lane) {
+__device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const PieceInfo& piece, int r, int lane, bool moved) {
   constexpr int E = D / 8;
   const int heads = g.a.Hq / g.a.Hkv, query = g.list[piece.query0 + (piece.row + r) / heads];
   // parts: the last one of CTA `cta`, the first ones of those that follow
@@ -687,11 +738,20 @@ __device__ __forceinline__ void join_row(const ChunkArgs& g, int cta, const Piec
   }
   const int64_t at = static_cast<int64_t>(query) * g.a.Hq + piece.kvh * heads + (piece.row + r) % heads;
   const float inv = l != 0.f ? 1.f / l : 0.f;
+  float score = 0.f;
+  if (moved) {
+    if (g.lse && moved_head(g, piece.chunk, piece.kvh, 0)) score = moved_score<D>(g, piece.chunk, piece.kvh, at, 0, 1);
+    if (moved_head(g, piece.chunk, piece.kvh, 1)) {
+      const uint16_t* power = common_of<D>(g, piece.chunk, piece.kvh, 1) + 4 * lane;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] *= one_over(power[i / 4 * 32 + i % 4]);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < E / 4; ++i)
     *reinterpret_cast<uint2*>(g.out + at * D + 32 * i + 4 * lane) =
         make_uint2(pack16(true, o[4 * i] * inv, o[4 * i + 1] * inv), pack16(true, o[4 * i + 2] * inv, o[4 * i + 3] * inv));
-  if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f + moved_score<D>(g, piece.chunk, piece.kvh, at) : -INFINITY;
+  if (g.lse && lane == 0) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f + score : -INFINITY;
 }
 
 constexpr int kJoinCtas = 4;
@@ -702,25 +762,27 @@ __global__ void __launch_bounds__(256, kJoinCtas) chunk_join_kernel(const __grid
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bad = g.head->bad, blocks = g.head->blocks;
-  const bool flagged = g.head->flagged, empty = g.head->empty;
+  const bool flagged = g.head->flagged, empty = g.head->empty, moved = g.head->moved;
   auto careful = [&](int chunk, int kvh) { return flagged && g.flag[static_cast<int64_t>(chunk) * g.a.Hkv + kvh]; };
   for (int x = blockIdx.x; x < g.ctas * (kBlockRows / kJoinRows); x += gridDim.x) {
     const int cta = x / (kBlockRows / kJoinRows), r = x % (kBlockRows / kJoinRows) * kJoinRows + threadIdx.x / 8;
     const PieceInfo piece = g.piece[cta];  // (none where the call is refused)
-    if (piece.block >= 0 && r < piece.rows && !careful(piece.chunk, piece.kvh)) join_row<D>(g, cta, piece, r, threadIdx.x & 7);
+    if (piece.block >= 0 && r < piece.rows && !careful(piece.chunk, piece.kvh)) join_row<D>(g, cta, piece, r, threadIdx.x & 7, moved);
   }
-  if (bad || !(flagged || empty)) return;
-  // rows with nothing stored in sight, and those that are done one by one
+  if (bad || !(flagged || empty || moved)) return;
+  // rows with nothing stored in sight, those that are done one by one, and whole ones of which something was taken out
   for (int64_t x = blockIdx.x; x < static_cast<int64_t>(blocks) * g.a.Hkv * (kBlockRows / kJoinRows); x += gridDim.x) {
     const int64_t y = x / (kBlockRows / kJoinRows);
     const BlockPlan& b = g.block[y / g.a.Hkv];
     const int kvh = static_cast<int>(y % g.a.Hkv), r0 = static_cast<int>(x % (kBlockRows / kJoinRows)) * kJoinRows;
-    if (b.tiles > 0 && !careful(b.chunk, kvh)) continue;
+    const bool by_one = b.tiles > 0 && careful(b.chunk, kvh);
+    if (b.tiles > 0 && !by_one && !(moved && chunk_uncut(g.base[y / g.a.Hkv] + kvh * chunk_cost(b), g.head->per, b))) continue;
     const ChunkPlan& c = g.chunk[b.chunk];
     for (int r = r0 + warp; r < min(b.rows, r0 + kJoinRows); r += 8) {
       const RowSource s = row_source(g, c, b.query0, b.local, kvh, b.row + r);
       if (b.tiles == 0) zero_rows(g, s.query, s.head, s.head + 1, lane);
-      else one_row<D>(g, c, s, b.local, kvh, lane);
+      else if (by_one) one_row<D>(g, c, s, b.local, kvh, lane);
+      else put_back<D>(g, b.chunk, kvh, static_cast<int64_t>(s.query) * g.a.Hq + s.head, lane);
     }
   }
 }
@@ -747,8 +809,8 @@ static int64_t lay_workspace(ChunkArgs* g, uint8_t* b, const Layout& l, int n, i
   g->block = reinterpret_cast<BlockPlan*>(take(static_cast<int64_t>(sizeof(BlockPlan)) * blocks));
   g->base = reinterpret_cast<int64_t*>(take(8 * (blocks + 1)));
   g->flag = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
-  g->moved = reinterpret_cast<int32_t*>(take(4ll * n * l.Hkv));
-  g->offset = reinterpret_cast<__half*>(take(2ll * n * l.Hkv * l.d));
+  g->moved = reinterpret_cast<int32_t*>(take(8ll * n * l.Hkv));
+  g->common = reinterpret_cast<uint16_t*>(take(4ll * n * l.Hkv * l.d));
   g->piece = reinterpret_cast<PieceInfo*>(take(static_cast<int64_t>(sizeof(PieceInfo)) * ctas));
   g->part_ml = reinterpret_cast<float2*>(take(8ll * 2 * ctas * kBlockRows));
   g->part_o = reinterpret_cast<uint4*>(take(4ll * 2 * ctas * kBlockRows * l.d));
@@ -815,8 +877,7 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   g.a.wait_ns = cache_wait_ns(cache);
   g.n = num_chunks; g.num_tokens = num_tokens; g.window_scalar = window_scalar; g.sinks = sinks;
   g.ctas = cache_num_sms(cache);
-  g.parts = (l.Hkv * l.d + kPlanChunkThreads - 1) / kPlanChunkThreads;
-  if (g.parts > kMostParts) g.parts = kMostParts;
+  g.parts = std::max(1, std::min({kMostParts, kMostCommonCtas / num_chunks, (2 * l.Hkv * l.d + kPlanChunkThreads - 1) / kPlanChunkThreads}));
   g.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf(static_cast<float>(l.d))) * 1.4426950408889634f;
   g.seq_ids = seq_ids; g.starts = starts; g.offsets = offsets; g.windows = windows; g.modes = modes;
   g.q = static_cast<const uint16_t*>(q_bf16);

@@ -49,7 +49,7 @@ struct ChunkHeader {
   int blocks, units, tiles;
   int splits, flagged;          // shares of the KV heads that staging CTAs take; some flag is set
   int empty;                    // some block has no tiles
-  int moved;                    // some chunk's keys are staged less an offset
+  int moved;                    // what is common to some chunk's tokens is taken out of them
   int pad[4];
 };
 
@@ -62,7 +62,7 @@ struct PieceInfo {
 struct ChunkArgs {
   LayerArgs a;
   int n, num_tokens, window_scalar, sinks, ctas, most_tiles;
-  int parts;         // CTAs that look for the offsets of a chunk's keys
+  int parts;         // CTAs that look for what a chunk's tokens have in common
   float scale_log2;  // softmax scale times log2(e): exponentials are taken in base 2
   const int32_t *seq_ids, *starts, *offsets, *windows;
   const uint8_t* modes;
@@ -78,8 +78,8 @@ struct ChunkArgs {
   BlockPlan* block;   // [most_blocks]
   int64_t* base;      // [most_blocks + 1] cost before each block (all its KV heads)
   int32_t* flag;      // [n][Hkv] some stored value is not to be had in binary16: its rows are done one by one
-  int32_t* moved;     // [n][Hkv] keys are staged less their offset
-  __half* offset;     // [n][Hkv][D] what is common to the keys, 0 in channels where little is
+  int32_t* moved;     // [n][K, V][Hkv] keys are staged less their offset, values times powers of two
+  uint16_t* common;   // [n][K, V][Hkv][D] the offsets (binary16, 0 in channels that have none), the powers (bf16)
   PieceInfo* piece;   // [ctas] the segment that a CTA began and did not finish
   float2* part_ml;    // [2 * ctas][256] (m, l) of a CTA's first piece, or its last
   uint4* part_o;      // [2 * ctas][D / 4][256] four columns of a row (binary32), consecutive rows beside each other
@@ -114,17 +114,16 @@ __device__ __forceinline__ RowSource row_source(const ChunkArgs& g, const ChunkP
   return r;
 }
 
-// What the keys' offset adds to the scores of row `at` (query and head), in units of the natural logarithm: staged keys
-// are less by it, which moves all of a row's scores by as much, no weight, and the logarithm of their sum.
-template <int D>
-__device__ __forceinline__ float moved_score(const ChunkArgs& g, int chunk, int kvh, int64_t at) {
-  const int64_t k = static_cast<int64_t>(chunk) * g.a.Hkv + kvh;
-  if (!g.head->moved || !g.moved[k]) return 0.f;
-  float sum = 0.f;
-#pragma unroll 1
-  for (int j = 0; j < D; ++j) sum += __uint_as_float(static_cast<uint32_t>(g.q[at * D + j]) << 16) * __half2float(g.offset[k * D + j]);
-  return sum * g.scale_log2 * 0.6931471805599453f;
+// Whether something common was taken out of a chunk's K (which 0) or V of a KV head, and what, by channel.
+__device__ __forceinline__ bool moved_head(const ChunkArgs& g, int chunk, int kvh, int which) {
+  return g.moved[(2ll * chunk + which) * g.a.Hkv + kvh];
 }
+template <int D>
+__device__ __forceinline__ const uint16_t* common_of(const ChunkArgs& g, int chunk, int kvh, int which) {
+  return g.common + ((2ll * chunk + which) * g.a.Hkv + kvh) * D;
+}
+// One over a power of two that is given as a bf16 number.
+__device__ __forceinline__ float one_over(uint32_t power) { return __int_as_float((254 << 23) - static_cast<int>(power << 16)); }
 
 // The last of 0 .. n-1 whose value (they ascend) is x or less, 0 if none is, by a whole warp: a chain of one load for 32 of
 // them, two for 1024.
@@ -151,6 +150,11 @@ constexpr int kChunkTileCost = 16, kChunkTurnsCost = 10, kChunkMaskedCost = 2, k
 constexpr int kChunkLeastShare = 48;  // of a CTA: three tiles
 __device__ __forceinline__ int64_t chunk_cost(const BlockPlan& b) {
   return b.tiles > 0 ? kChunkSegmentCost + static_cast<int64_t>(b.tile_cost) * b.tiles : 0;
+}
+// Whether tile 0 and the last tile of the segment that starts at cost `start` are in one CTA's share: its rows are whole then.
+__device__ __forceinline__ bool chunk_uncut(int64_t start, int64_t per, const BlockPlan& b) {
+  const int64_t first = start + kChunkSegmentCost;
+  return first / per == (first + static_cast<int64_t>(b.tile_cost) * (b.tiles - 1)) / per;
 }
 // Tiles of a segment that lie before cost x (counted from the segment's start).
 __device__ __forceinline__ int chunk_tiles_before(int64_t x, const BlockPlan& b) {

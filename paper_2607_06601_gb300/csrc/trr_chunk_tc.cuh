@@ -42,8 +42,7 @@ struct ChunkSegment {
   int from, head, skip;   // the run's first tile of the segment's; the segment's first `head` are the chunk's, the others `skip` further
   int query0, row, local; // of the block
   int sinks;              // staged tokens that a local row sees beside its window
-  int chunk;
-  int pad[1];
+  int pad[2];
 };
 
 // A row of a run: its place among all (query, head), and which of the chunk's staged tokens it sees, lo .. hi - 1.
@@ -195,7 +194,7 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
         s.from = t0; s.head = p.head; s.skip = p.first - p.head;
         s.clean = max(p.clean, p.first) - s.skip - t0;
         s.clean_end = p.clean_end - s.skip - t0;
-        s.query0 = p.query0; s.row = p.row; s.local = p.local; s.sinks = p.sinks; s.chunk = p.chunk;
+        s.query0 = p.query0; s.row = p.row; s.local = p.local; s.sinks = p.sinks;
         announce(s);
         copy();
         last = s;
@@ -548,7 +547,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
         put_words(col_p + A / 2, q);
       }
       const bool up = sum > kMost, down = l < kGrown && (begins ? sum - kFirst < least - kSmall : sum < least);
-      if (__any_sync(0xffffffffu, up || down)) {
+      if (__builtin_expect(__any_sync(0xffffffffu, up || down), 0)) {
         tmem_wait_st();  // the weights stored above are stored again below: the first stores land first
         const float top = fmaxf(highest(a), highest(b)) * f;
         if (!move(up ? fmaxf(m, top - kRoomUp) : !down ? m : begins ? m + (kRoom - kRoomAlone) : fmaxf(top - kRoom, m - kDown))) return;
@@ -567,7 +566,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
     }
     const bool some = first < tiles;
     const bool turns = step == 2;
-    const int first_row = turns ? 0 : half * kHalfRows, dest = sg.dest, chunk = sg.chunk, kvh = sg.kvh, at = begun ? x.rows(segs % kRunSlots)[first_row + row].at : -1;
+    const int first_row = turns ? 0 : half * kHalfRows, dest = sg.dest, at = begun ? x.rows(segs % kRunSlots)[first_row + row].at : -1;
     const bool mine = at >= 0;
     // the next run's rows, while this one's last product runs (its scores are all in: Q's place is free)
     if (!load_rows(segs + 1)) return;
@@ -624,7 +623,7 @@ __device__ __forceinline__ void chunk_softmax(const ChunkArgs& g, const ChunkCtx
       if (c == 0) {
         inv = l != 0.f ? 1.f / l : 0.f;
         if (mine && dest >= 0) g.part_ml[static_cast<int64_t>(dest) * kBlockRows + first_row + row] = make_float2(m, l);
-        if (mine && dest < 0 && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f + moved_score<D>(g, chunk, kvh, at) : -INFINITY;
+        if (mine && dest < 0 && g.lse) g.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
       if (dest >= 0) {
 #pragma unroll

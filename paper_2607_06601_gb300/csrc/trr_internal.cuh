@@ -29,7 +29,7 @@ enum Ctrl : int {
   kChunkBad = 18,     // attention of chunks: INT_MAX - (16 * query + error) of the lowest failing one (0: none)
   kChunkDone = 19,    // attention of chunks: CTAs of the plan finished (the last one lays chunks end to end)
   kChunkPlanned = 20, // attention of chunks: CTAs that have planned their blocks (the last one lays them end to end)
-  kChunkMoved = 21,   // attention of chunks: 1 when some chunk's keys are staged less an offset
+  kChunkMoved = 21,   // attention of chunks: 1 when what is common to some chunk's tokens is taken out of them
   kChunkRefused = 22, // attention of chunks: 1 when the call's offsets do not ascend
   kCtrlInts = 64
 };

@@ -151,3 +151,42 @@ def test_small_elements_of_queries_before_large_keys(lay, size):
     k = np.repeat(k, h.Hq // h.Hkv, axis=1)
     off = np.abs(lse.double().cpu().numpy() - scale * (q * k).sum(-1))
     assert (off <= 2.0 ** -11 * scale * np.abs(q * k).sum(-1) + 2.0 ** -16).all()
+
+
+@pytest.mark.parametrize("lay,n,new", [(WIDE[0], 300, 20), (WIDE[0], 300, 160), (WIDE[1], 260, 100), (dict(Hq=4, Hkv=2, d=64, G=32, P=16), 3000, 30),
+                                       (dict(Hq=2, Hkv=2, d=128, G=64, P=16), 2500, 40)])
+def test_channels_far_apart(lay, n, new):
+    """V of 16 bits whose channels are 2^0 to 2^-70 in size, one of them zeros: each channel as near as its own values are.  (Binary16's steps are 2^-16 of what a channel's samples are scaled to, 2^-8: less than the 2^-12 of sums.)"""
+    rng = np.random.default_rng([5, n, new])
+    h = Holder(1, 1, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], n, [n // lay["P"] + 2] * 4, archive=4)
+    v = rng.standard_normal((n, h.Hkv, h.d)) * 2.0 ** (-7.0 * (np.arange(h.d) % 11))
+    v[:, 0, 20] = 0.0
+    v_bits = wl.bf16_bits(v.astype(np.float32))
+    scores = rng.integers(-8, 8, n) / 4.0
+    k_bits = one_channel(n, h.Hkv, h.d, scores)
+    for at in range(0, n, 1000):
+        part = slice(at, min(n, at + 1000))
+        h.append(rng, 0, 0, np.arange(n)[part], k=k_bits[part], v=v_bits[part], bits=np.full(n, 16)[part], p_skip=0.0)
+    out, *_ = call(h, rng, [0], [n - new], [new], [2] * new, [1] * new, scale=1.0, q_bits=one_channel(new, h.Hq, h.d, np.ones(new)))
+    ref, spread, _ = exact_rows(h, scores, wl.bf16_to_f32(v_bits).astype(np.float64), n - new, new)
+    within(out, ref, spread, 0.0)
+
+
+def test_channels_that_are_small_but_for_one_token():
+    """Scaled by what the others need, one value is more than binary16 holds; and beside it tokens of fewer bits."""
+    rng = np.random.default_rng(6)
+    lay, n, new = WIDE[0], 400, 140
+    h = Holder(1, 2, lay["Hq"], lay["Hkv"], lay["d"], lay["G"], lay["P"], n, [2 * n // lay["P"] + 2] * 4, archive=4)
+    scores = rng.integers(-16, 1, n) / 4.0  # (their groups' least value, which is stored as it is)
+    for seq, bits in ((0, np.full(n, 16)), (1, rng.choice([8, 16], n))):
+        v = rng.standard_normal((n, h.Hkv, h.d)) * 2.0 ** -20
+        if seq == 0:
+            v[37, 1, 3], v[200, 3, 60] = 3000.0, -5.0
+        h.append(rng, 0, seq, np.arange(n), k=one_channel(n, h.Hkv, h.d, scores), v=wl.bf16_bits(v.astype(np.float32)), bits=bits, p_skip=0.0)
+    for seq in (0, 1):
+        out, *_ = call(h, rng, [seq], [n - new], [new], [2] * new, [1] * new, scale=1.0, q_bits=one_channel(new, h.Hq, h.d, np.ones(new)))
+        v = np.stack([h.values(0, seq, head)[2] for head in range(h.Hkv)], 1)
+        k = np.stack([h.values(0, seq, head)[1][:, 0] for head in range(h.Hkv)], 1)
+        assert np.array_equal(k, np.repeat(scores[:, None], h.Hkv, 1))
+        ref, spread, most = exact_rows(h, scores, v, n - new, new)
+        within(out, ref, spread, most)

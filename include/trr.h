@@ -416,7 +416,8 @@ TRR_API trr_status trr_decode_attn_shared(trr_cache* cache, int32_t layer, int32
 /* Bytes of workspace for trr_chunk_attn of num_chunks chunks with num_tokens queries whose
  * positions, and all before them, number at most max_keys: the sum of starts[i] + length
  * of chunk i (counting what is stored is enough, and chunks of local queries count their
- * windows and sinks only).  UNSUPPORTED where num_tokens * num_q_heads or the workspace's
+ * windows and sinks only).  A chunk counts max_context, or what the four pools hold, at most;
+ * a token takes 4 * num_kv_heads * head_dim bytes.  UNSUPPORTED where num_tokens * num_q_heads or the workspace's
  * tokens come to 2^31 - 256 or more, or the cache has head_modes. */
 TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num_chunks, int32_t num_tokens,
                                              int64_t max_keys, uint64_t* bytes);

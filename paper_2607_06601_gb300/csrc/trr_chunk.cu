@@ -847,8 +847,10 @@ extern "C" trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t 
   const Layout& l = cache_layout(cache);
   const trr_status st = check_sizes(l, num_chunks, num_tokens);
   if (st != TRR_OK) return st;
-  // a chunk ends in a partly filled tile
-  const int64_t keys = std::min(max_keys, static_cast<int64_t>(num_chunks) * l.maxctx), tiles = keys / chunk_tile(l.d) + num_chunks;
+  // a sequence stores no more tokens than it has positions, or the pools have slots; a chunk ends in a partly filled tile
+  int64_t slots = 0;
+  for (int c = 0; c < kClasses; ++c) slots += static_cast<int64_t>(l.cap[c]) * l.P;
+  const int64_t keys = std::min(max_keys, num_chunks * std::min<int64_t>(l.maxctx, slots)), tiles = keys / chunk_tile(l.d) + num_chunks;
   if (tiles > INT_MAX / chunk_tile(l.d)) return TRR_ERR_UNSUPPORTED;
   ChunkArgs g;
   *bytes = static_cast<uint64_t>(lay_workspace(&g, nullptr, l, num_chunks, num_tokens, cache_num_sms(cache), tiles));

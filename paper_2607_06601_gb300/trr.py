@@ -529,8 +529,9 @@ class Cache:
         [n][Hq] float32.  Rows of a new `out` that no chunk names are not set.
 
         max_keys: at most how many positions the chunks reach over, the sum of starts[i] + length; by default every
-        chunk's whole context.  It sizes the workspace, which is allocated for the call unless one of
-        `chunk_workspace` is given."""
+        chunk's whole context, or all that the pools hold where that is less.  It sizes the workspace, 4 * Hkv * d bytes
+        a position, which is allocated for the call unless one of `chunk_workspace` is given: a cache of many long
+        contexts should give one of the two (32 chunks of 131,072 positions of 32 heads of 64 come to 34 GB)."""
         n = modes.numel()
         size = n * self.Hq * self.d
         if q.numel() != size or (out is not None and out.numel() != size):

@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kPlanChunkThreads) chunk_plan_kernel(const __g
     ChunkHeader h = {};
     h.bad = whole;
     if (!whole) {
-      h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units); h.tiles = static_cast<int>(tiles);
+      h.blocks = static_cast<int>(blocks); h.units = static_cast<int>(units);
       const int stagers = kStageCtas * g.ctas;
       h.splits = units > 0 ? shares_of_heads(units, (a.Hkv + 1) / 2, stagers, copy_ns(5ll * a.Hkv * a.d, stagers)) : 1;
     }

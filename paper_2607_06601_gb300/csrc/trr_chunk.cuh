@@ -46,17 +46,18 @@ static_assert(sizeof(BlockPlan) == 64, "");
 struct ChunkHeader {
   int64_t work, per;            // cost of all segments, a CTA's share
   int bad;                      // error of the whole call: every row is zero
-  int blocks, units, tiles;
+  int blocks, units;
   int splits, flagged;          // shares of the KV heads that staging CTAs take; some flag is set
   int empty;                    // some block has no tiles
   int moved;                    // what is common to some chunk's tokens is taken out of them
-  int pad[4];
+  int pad[5];
 };
 
 // A segment that a CTA began and the ctas - 1 after it went on with; block < 0: none.
 struct PieceInfo {
   int block, kvh, ctas, rows;
-  int chunk, local, query0, row;  // of the block
+  int chunk, query0, row;         // of the block
+  int pad;
 };
 
 struct ChunkArgs {

@@ -185,7 +185,7 @@ __device__ __forceinline__ void chunk_produce(const ChunkArgs& g, const ChunkCtx
         const int t0 = chunk_tiles_before(b0 - S, p), t1 = chunk_tiles_before(b1 - S, p);
         if (t0 >= t1) continue;
         if (t0 == 0 && t1 < p.tiles) {
-          piece = PieceInfo{b, h, 0, p.rows, p.chunk, p.local, p.query0, p.row};
+          piece = PieceInfo{b, h, 0, p.rows, p.chunk, p.query0, p.row};
           piece_end = S + cost - p.tile_cost;
         }
         ChunkSegment s = {};

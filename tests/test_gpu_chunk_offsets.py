@@ -93,3 +93,22 @@ def test_few_tokens():
         h.append(rng, 0, s, np.arange(s + 1), k=k, bits=bits, p_skip=0.0)
     lens = [*range(1, 10)]
     check(h, rng, [*range(9)], [0] * 9, lens, [2] * 45, [1] * 45)
+
+
+@pytest.mark.parametrize("lay", [dict(Hq=8, Hkv=8, d=128, G=64, P=16), dict(Hq=16, Hkv=8, d=64, G=32, P=32)])
+def test_more_segments_than_shares(lay):
+    """Segments that one CTA has whole beside others that are cut; keys with an offset, values with small channels, both and
+    neither, sequence by sequence; with rows that see nothing."""
+    rng = np.random.default_rng(6)
+    S, n, new = 24, 260, 20
+    h = holder(lay, S=S, maxctx=300, caps=S * 10, archive=S + 1)
+    for s in range(S):
+        k, bits = keys(rng, h, n, "all" if s % 2 else "none")
+        v = rng.standard_normal((n, h.Hkv, h.d))
+        if s % 4 > 1:
+            v[:, :, ::3] *= 2.0 ** -22
+            bits[:] = 16
+        h.append(rng, 0, s, np.arange(20, 20 + n), k=k, v=wl.bf16_bits(v.astype(np.float32)), bits=bits)
+    starts = [20 + n - new - (s % 5) * 50 for s in range(S)]
+    starts[3], starts[7] = 5, 0
+    check(h, rng, [*range(S)], starts, [new] * S, rng.choice(3, S * new, p=[.1, .4, .5]), rng.integers(1, 300, S * new), 0)

@@ -437,7 +437,7 @@ TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num
  *   logarithm of the sum of exp(softmax_scale * q.k) over the tokens in sight, -infinity
  *   for a zero row; with it, rows over parts of a past can be joined.
  *   seq_ids, starts, offsets, q, modes, windows, out, lse: device; q and out 16-byte
- *   aligned; 0 <= num_tokens <= 2^20; sinks >= 0.
+ *   aligned and not overlapping, lse 4-byte aligned; 0 <= num_tokens <= 2^20; sinks >= 0.
  *   workspace: device memory, 256-byte aligned, trr_chunk_workspace_bytes of it, used only
  *   while the call runs.  One that is smaller than that of max_keys 0 or misaligned returns
  *   TRR_ERR_OUT_OF_MEMORY and enqueues nothing; one that turns out too small for what is

@@ -869,7 +869,9 @@ extern "C" trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t nu
   cache_set_launches(cache, 0);
   if (num_chunks == 0 || num_tokens == 0) return TRR_OK;
   if (!seq_ids || !starts || !offsets || !q_bf16 || !modes || !out_bf16) return TRR_ERR_INVALID_ARG;
-  if ((reinterpret_cast<uintptr_t>(q_bf16) | reinterpret_cast<uintptr_t>(out_bf16)) & 15) return TRR_ERR_INVALID_ARG;
+  const uintptr_t q0 = reinterpret_cast<uintptr_t>(q_bf16), out0 = reinterpret_cast<uintptr_t>(out_bf16), row_bytes = 2ull * num_tokens * l.Hq * l.d;
+  if (((q0 | out0) & 15) || (reinterpret_cast<uintptr_t>(lse) & 3)) return TRR_ERR_INVALID_ARG;
+  if (q0 < out0 + row_bytes && out0 < q0 + row_bytes) return TRR_ERR_INVALID_ARG;  // (queries are read again where a row is done one by one)
   uint64_t least = 0;
   st = trr_chunk_workspace_bytes(cache, num_chunks, num_tokens, 0, &least);
   if (st != TRR_OK) return st;

@@ -417,8 +417,8 @@ TRR_API trr_status trr_decode_attn_shared(trr_cache* cache, int32_t layer, int32
  * positions, and all before them, number at most max_keys: the sum of starts[i] + length
  * of chunk i (counting what is stored is enough, and chunks of local queries count their
  * windows and sinks only).  A chunk counts max_context, or what the four pools hold, at most;
- * a token takes 4 * num_kv_heads * head_dim bytes.  UNSUPPORTED where num_tokens * num_q_heads or the workspace's
- * tokens come to 2^31 - 256 or more, or the cache has head_modes. */
+ * a token takes 4 * num_kv_heads * head_dim bytes.  UNSUPPORTED where num_tokens *
+ * num_q_heads or the workspace's tokens come to 2^31 - 256 or more, or the cache has head_modes. */
 TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num_chunks, int32_t num_tokens,
                                              int64_t max_keys, uint64_t* bytes);
 
@@ -432,8 +432,8 @@ TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num
  *     local: softmax attention over the stored tokens j <= t with j >= t-w+1 or
  *            j < sinks, w = windows[r] (or window_scalar when windows == NULL), w >= 1
  *     full : softmax attention over the stored tokens j <= t,
- *   as trr_decode_attn_sinks computes it for the same queries: out[r][Hq][d] (bf16), a zero
- *   row where nothing is in sight.  lse (may be NULL): lse[r][Hq] float32, the natural
+ *   as trr_decode_attn_sinks has it for the same queries (but for rounding, see below):
+ *   out[r][Hq][d] (bf16), a zero row where nothing is in sight.  lse (may be NULL): lse[r][Hq] float32, the natural
  *   logarithm of the sum of exp(softmax_scale * q.k) over the tokens in sight, -infinity
  *   for a zero row; with it, rows over parts of a past can be joined.
  *   seq_ids, starts, offsets, q, modes, windows, out, lse: device; q and out 16-byte
@@ -445,19 +445,36 @@ TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num
  *   Device-detected errors: those of stretches; a mode not allowed or a local query with a
  *   window below 1 (INVALID_ARG) makes that query's rows zero.  A cache with head_modes
  *   returns TRR_ERR_UNSUPPORTED.
- *   How near: K, V and the softmax weights are rounded to binary16 (11 bits), sums are
- *   binary32; an element of out is off by its rounding to bf16 and about 2^-10 of the sum of
- *   its weights times |v|, lse by 2^-11 of the largest sum of |scale q_j k_j| at most.  Chunks whose
- *   values binary16 does not hold (65536 and more, infinities and NaN, all below 2^-14) are
- *   done row by row in binary32, which takes many times as long.
- *   Which call: everything in sight is brought back to binary16 in the workspace, once for
- *   all queries of a chunk.  That costs the same for one query and for many: 32 chunks on
- *   2048 tokens of 12 heads of 64 take 134 us with 1 query each and 136 with 64, where
- *   trr_decode_attn takes 40 us with 1, 84 with 4, 135 with 8, 246 with 16 and 961 with 64.
- *   So below 8 queries a chunk take trr_decode_attn; where several query heads share a KV
- *   head and all queries are full, trr_decode_attn_shared with the chunks as its groups is
- *   the faster one up to 16 (32 chunks on 4096 tokens, 32 heads on 8 of 128: 299 us here,
- *   176 there with 8 queries each, 223 with 16, 320 with 32). */
+ *   How near: K, V and the softmax weights are rounded to binary16 (11 bits, in steps of 2^-24
+ *   below 2^-14), sums are binary32.
+ *     A score is off by up to 2^-11 of the sum over channels of |softmax_scale q_j (k_j - c_j)|,
+ *     c_j being what the channel's keys have in common (the middle of eight of them that lie
+ *     within a third of it, else 0); 16-bit keys below 2^-14 by 2^-25 |softmax_scale q_j| each.
+ *     That moves the token's weight by as large a part of it, and lse by no more.
+ *     Beside that an element of out is off by its rounding to bf16, and by its weights' and
+ *     values' roundings: a weight's by 2^-11 of it, or of the mean weight of its neighbours
+ *     (blocks of 96 tokens in order of position at head_dim 64, of 80 at 128), a value's by
+ *     2^-11 of it, or 2^-13 of the largest of eight values of its channel.
+ *   Tokens of which binary16 holds too little make all rows of their chunk's KV head be done one
+ *   by one in binary32: 16-bit values of 65536 and more, infinities, NaN, keys further than 65504
+ *   from c, a 16-bit K or V row all of which lies below 2^-14 (of V: of what its channels are
+ *   scaled to) and loses bits.  One such token in every head took 512 queries on 16,384 tokens
+ *   (32 heads on 8 of 128) from 0.17 to 114 ms, 4096 on themselves (32 heads of 64) from 0.16 to
+ *   33 ms, 32 chunks of 8 on 2,048 (12 heads of 64) from 0.16 to 3.5 ms.
+ *   Which call: everything in sight is brought back to binary16 in the workspace, once for all
+ *   queries of a chunk, and that costs the same for one query and for 64; trr_decode_attn reads
+ *   the past once for each query, trr_decode_attn_shared (full queries, chunks as its groups)
+ *   about once for each chunk and 128 rows.  From how many queries a chunk this call is the
+ *   fastest depends on how many chunks fill the GPU and on the heads.  GPU time of full queries
+ *   with cold caches, in us, this call / trr_decode_attn / trr_decode_attn_shared:
+ *     32 chunks on 2,048 tokens, 12 heads of 64, of 1 query each: 132 / 40 / 58, of 4:
+ *       131 / 83 / 73, of 8: 131 / 136 / 132, of 16: 133 / 246 / 155, of 64: 135 / 961 / 318;
+ *     32 chunks on 4,096, 32 heads on 8 of 128, of 1: 292 / 86 / 79, of 8: 296 / 301 / 176,
+ *       of 16: 298 / 573 / 223, of 32: 303 / 1080 / 318;
+ *     1 chunk on 2,048, 12 heads of 64, of 8: 44 / 28 / 40, of 32: 44 / 37 / 41,
+ *       of 128: 48 / 81 / 61;
+ *     1 chunk on 32,768, 32 heads on 8 of 128, of 8: 119 / 118 / 69, of 32: 145 / 297 / 71,
+ *       of 128: 138 / 1006 / 150. */
 TRR_API trr_status trr_chunk_attn(trr_cache* cache, int32_t layer, int32_t num_chunks, const int32_t* seq_ids,
                                   const int32_t* starts, const int32_t* offsets, int32_t num_tokens, const void* q_bf16,
                                   const uint8_t* modes, const int32_t* windows, int32_t window_scalar, int32_t sinks,

@@ -5,30 +5,32 @@
 //
 // A chunk's many queries read the same tokens, so those are brought back from their codes once, not
 // once for each block of rows:
-//   chunk_plan_kernel    some CTAs per chunk: what its tokens have in common; its queries sorted by mode (a block of rows then
-//                        has one mode and reads no more than that mode sees), the positions that any of them sees,
-//                        how many tokens are stored there; the CTA that ends last lays chunks end to end.
+//   chunk_plan_kernel    a CTA per chunk: its queries sorted by mode (a block of rows then has one mode and
+//                        reads no more than that mode sees), the positions that any of them sees, how
+//                        many tokens are stored there.  Some more per chunk: what its tokens have in
+//                        common (see there).  The CTA that ends last lays chunks end to end.
 //   chunk_stage_kernel   the stored tokens in sight, in order of position, as tiles in the layout that the tensor
 //                        core reads, in binary16: z + c s rounded once (11 bits against the 8 of the output), 16-bit
-//                        values as they are.  And each block's tiles.
+//                        values as they are, less what is common.  And each block's tiles.
 //   chunk_attn_kernel    one CTA per SM; all blocks' tiles, for every KV head, laid end to end are cut into
 //                        equal runs, so that a long segment is spread over CTAs and a CTA takes many short ones.
 //   chunk_join_kernel    joins the parts of rows that were cut, (m, l, o) by m' = max m,
-//                        l' = sum l 2^(m - m'), and so for o.
+//                        l' = sum l 2^(m - m'), and so for o; puts back what was taken out of K and V.
 //
 // Alone, from cold caches, in us (plan, stage, attention, join): one chunk of 512 queries of 12 heads on 2048 tokens
-// 11, 12, 18, 9; 32 chunks of 8 on 2048 tokens of 12 heads 11, 56, 44, 6; 4096 queries on themselves, 32 heads of 64,
-// 15, 21, 91 to 97, 12; 2048 at the end of 32,768 tokens, 8 KV heads of 128, 11, 36, 540, 16.  Plan and join are chains
+// 11, 12, 19, 9; 32 chunks of 8 on 2048 tokens of 12 heads 11, 57, 45, 6; 4096 queries on themselves, 32 heads of 64,
+// 14, 21, 98 to 101, 11; 2048 at the end of 32,768 tokens, 8 KV heads of 128, 11, 37, 555, 17.  Plan and join are chains
 // of dependent loads and of code that is read for the first time; a launch's start hides behind its forerunner's end.
-//   Staging is bound by the memory: 4.5 bits a value in and 16 out.  The 32 chunks above write 201 MB in 56 us, 4 TB/s
+//   Staging is bound by the memory: 4.5 bits a value in and 16 out.  The 32 chunks above write 201 MB in 57 us, 4 TB/s
 // with what is read, as reading back does, and the attention reads it at 4.6 TB/s.  Four CTAs an SM, a head's loads
-// ahead: with two or three heads ahead that call took 151 and 163 us against 130, with 3 CTAs an SM 145 (registers
-// spilled), with 5 no less.
+// ahead: with two or three heads ahead that call, which took 130 us then, took 151 and 163, with 3 CTAs an SM 145, with 5
+// no less.  At 64 registers 52 bytes a thread are spilled (80 loaded); the loop that takes out what is common spills
+// 472 (692), and the 32 chunks above take 50 us more where keys have an offset.
 //
-// A 16-bit value that binary16 does not hold flags its chunk and KV head: one of 65536 and more, an infinity or NaN,
-// or bits lost below 2^-24 in a row of K or V that has nothing above 2^-14 (other rows' lost bits are less than a
-// rounding of their largest value).  Flagged rows are done one by one in binary32, from the pages, by the join
-// kernel; so are rows that do not see a V that is not finite safe from it (0 times infinity).
+// Tokens of which binary16 holds too little flag their chunk and KV head: a 16-bit value of 65536 and more, an infinity or
+// NaN; a key further than 65504 from its offset; bits lost below 2^-24 in a 16-bit row of K or V that has nothing above 2^-14
+// (of V: as it is scaled).  Rows of a flagged head are done one by one in binary32, from the pages, by the join kernel, since
+// 0 times infinity would reach rows that do not see the token.  That takes 20 to 700 times as long (the header has figures).
 #include <algorithm>
 #include <climits>
 
@@ -75,7 +77,7 @@ __device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* warp_sums, in
 // channels that are none the worse.  Where the eight are below 2^-12, values are staged times the power of two that brings
 // their largest to 2^-8 (so that a value may be 2^23 times as large and be in binary16's range), and rows are divided by it as
 // they are written.
-// (With 16, and half as many channels a CTA, 32 chunks of 12 heads took 126.5 us against 122.5.)
+// (With 16, and half as many channels a CTA, 32 chunks of 12 heads took 126.5 us against 125.)
 constexpr int kSamples = 8;
 // CTAs that share a chunk's channels out: a pass each, but no more than the GPU holds at once.
 constexpr int kMostParts = 8, kMostCommonCtas = 512;

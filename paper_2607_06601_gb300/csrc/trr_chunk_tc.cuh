@@ -11,9 +11,10 @@
 // What bounds it.  Per tile of 96 tokens at d 64 the two halves' products take 464 + 384 cycles of the tensor core
 // and its shared memory, 24,576 exponentials 768 of the SM's 32 a cycle, and a softmax warp's chain of waits,
 // loads from TMEM, weights and stores about 1900, which is what a tile takes: at 4096 queries on themselves, 32
-// heads of 64 (four fifths of the tokens stored), 91 to 97 us, 0.6 PFLOP/s, the tensor pipe busy for 27 % of it.  At d 128
+// heads of 64 (four fifths of the tokens stored), 98 to 101 us, 0.55 PFLOP/s, the tensor pipe busy for 25 % of it.  At d 128
 // a product of 128 x 80 x 16 from shared memory takes 54 cycles of its bandwidth, 1506 a tile with those of P V;
-// measured 1880: 2048 queries of 32 heads at the end of 32,768 tokens, 540 us, 1.58 PFLOP/s.
+// measured 1930: 2048 queries of 32 heads at the end of 32,768 tokens, 555 us, 1.54 PFLOP/s, the tensor pipe busy for 65 %.
+// (The kernel at d 64 spills 20 bytes a thread of stores and 24 of loads.)
 //
 // What this layout is for: from a product's end to the issue of one that waits for it pass about 450 cycles
 // (completion, barrier, wait, issue).  So no product waits for another: scores, weights and sums have columns of

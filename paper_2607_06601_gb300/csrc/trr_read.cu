@@ -10,11 +10,12 @@
 // average) and leaves as 256.  A warp takes one head's K and V rows of a class at a time, 16 values a
 // lane, consecutive lanes along a row, so that whole lines are written.
 //
-// With cold caches 65,536 rows of 12 heads of 64 in bf16 take 65 us, 40,000 of 32 heads in binary32 151 us (DRAM
-// 5.0 TB/s, 107 MB read and 622 written), 131,072 of 8 heads of 128 in bf16 131 us; a copy of as many
+// Alone, from cold caches, 65,536 rows of 12 heads of 64 in bf16 take 58 us, 40,000 of 32 heads in binary32 141 us (DRAM
+// 5.2 TB/s, 112 MB read and 623 written), 131,072 of 8 heads of 128 in bf16 122 us; a copy of as many
 // bytes 40, 114 and 96.  What is left are the searches before a CTA's first rows (5 us in which
 // nothing is written) and the loads' latency under so many stores.  Two heads' loads ahead at 80 registers
-// and three CTAs an SM were no gain: 71, 149 and 132 us where one head's at four CTAs then took 69, 153 and 138.
+// and three CTAs an SM were no gain: 71, 149 and 132 us a whole call where one head's at four CTAs then took 69, 153
+// and 138.  At 64 registers 32 to 44 bytes a thread are spilled.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(kSpanThreads, kReadCtas) read_kernel(const __g
 
 // How the rows are cut into units: some of them (48 to 64) of a share of the heads.  With the heads in s shares a unit has
 // as many rows as fill the fewest rounds of `ctas` CTAs evenly; of all s the one that takes least, where 64 rows of all
-// heads take `whole` ns among as many others and a unit 5 us more to find its tokens.  Cold caches, against units of 64
+// heads take `whole` ns among as many others and a unit 5 us more to find its tokens.  Whole calls with cold caches, against units of 64
 // rows always: 65,536 rows of 12 heads of 64 in bf16 65 us against 69 (2 rounds of 54 rows, the second one was 0.7 full),
 // 131,072 of 8 heads of 128 130 against 138; with 32 rows as the least, 40,000 of 32 heads in binary32 157 against 153.
 struct Shares {

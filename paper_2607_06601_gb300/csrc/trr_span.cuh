@@ -227,9 +227,9 @@ __device__ __forceinline__ void for_groups(const Found<ROWS>& f, int lg_parts, i
 __host__ __device__ inline int lg_parts(int heads) { return heads >= 8 ? 2 : heads >= 4 ? 1 : 0; }
 
 // Shares of the heads that a unit (64 positions) is cut into: as many as make the rounds of `ctas` CTAs shortest, where
-// a unit whole takes `whole` ns among as many others, and each share 5 us more to find its tokens.  Measured where
-// 40,000 rows of 32 heads of 64 are read back in binary32: 169 us with whole units (637 for 608 CTAs), 153 with quarters.
-// Units of fewer positions, as reading back has them, were no gain here: the longer plan took what they gave.
+// a unit whole takes `whole` ns among as many others, and each share 5 us more to find its tokens.  For staging: reading
+// back took this rule over with units of fewer positions besides (there, with what both measured), which were no gain for
+// staging, as the longer plan took what they gave.
 __device__ __forceinline__ int shares_of_heads(int64_t units, int most, int ctas, int64_t whole) {
   int best = 1;
   float least = 0.f;

@@ -454,7 +454,7 @@ TRR_API trr_status trr_chunk_workspace_bytes(const trr_cache* cache, int32_t num
  *     Beside that an element of out is off by its rounding to bf16, and by its weights' and
  *     values' roundings: a weight's by 2^-11 of it, or of the mean weight of its neighbours
  *     (blocks of 96 tokens in order of position at head_dim 64, of 80 at 128), a value's by
- *     2^-11 of it, or 2^-13 of the largest of eight values of its channel.
+ *     2^-11 of it, or 2^-13 of the largest of eight values of its channel (2^-25, were those 0).
  *   Tokens of which binary16 holds too little make all rows of their chunk's KV head be done one
  *   by one in binary32: 16-bit values of 65536 and more, infinities, NaN, keys further than 65504
  *   from c, a 16-bit K or V row all of which lies below 2^-14 (of V: of what its channels are

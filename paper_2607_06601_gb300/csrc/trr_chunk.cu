@@ -407,7 +407,7 @@ __device__ __forceinline__ void zero_rows(const ChunkArgs& g, int q, int h0, int
     for (int h = lane; h < h1 - h0; h += 32) g.lse[at + h] = -INFINITY;
 }
 
-// Sixteen elements of a token's K less their offset, or of its V times their powers of two (a x b + c, in binary32), rounded once to
+// Sixteen elements of a token's K less their offset, or of its V times their powers of two, from binary32 rounded once to
 // binary16; their largest magnitude's bits, and whether binary16 lacks bits of one.
 template <int C, int D>
 __device__ __forceinline__ void expand_moved(const Codes16& x, int which, const uint16_t* common, uint4 (&v)[2], uint32_t* top, bool* lost) {
@@ -454,7 +454,8 @@ __device__ __forceinline__ void stage_token(const ChunkArgs& g, int chunk, const
     for (int which = 0; which < 2; ++which) {
       uint4 v[2];
       if (C == 3 || MOVED) {
-        constexpr uint32_t kPast = MOVED ? 0x477FE001u : 0x4780u, kNear = MOVED ? 0x38800000u : 0x3880u;  // beyond 65504 (binary32), 65536 (bf16); 2^-14
+        // beyond 65504 as binary32, 65536 as bf16; 2^-14
+        constexpr uint32_t kPast = MOVED ? 0x477FE001u : 0x4780u, kNear = MOVED ? 0x38800000u : 0x3880u;
         uint32_t top = 0;
         bool lost = false;
         if (MOVED) {
